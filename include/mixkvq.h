@@ -230,6 +230,33 @@ size_t mixkvq_prefill_scratch_bytes(const mixkvq_config* cfg, int n_tokens);
 int mixkvq_prefill(mixkvq_cache* cache, int layer, const void* k_dev, const void* v_dev, const void* q_dev, int n_tokens,
                    float* out_dev, float softmax_scale, void* scratch_dev, size_t scratch_bytes, void* stream);
 
+/* Attention of a chunk of new tokens over a layer that may hold tokens already: the later chunks of a prompt, or drafted tokens whose
+ * acceptance is decided afterwards.  Sequence b has n_tokens_host[b] new tokens (0 <= n_tokens_host[b] <= n_tokens_max; HOST array [B], or
+ * NULL: n_tokens_max each), the first rows of
+ *   k_dev, v_dev [B, Hkv, n_tokens_max, 128], q_dev [B, Hq, n_tokens_max, 128] bf16 (post-RoPE)  ->  out_dev [B, Hq, n_tokens_max, 128]
+ * New token j attends to everything the sequence holds (sink, packed blocks dequantized by Eq. 3, residual window) and to the new tokens
+ * 0 .. j in full precision.  out_type: MIXKVQ_OUT_FLOAT or MIXKVQ_OUT_BF16 (rounded once, to nearest).  Rows behind a sequence's count are neither
+ * read nor written.  The sequences may hold different numbers of tokens.  An empty layer gives the causal attention of mixkvq_prefill.
+ * mixkvq_chunk_attention appends nothing: accepted tokens go in with mixkvq_quantize_append_ragged, which takes the same tensors.
+ * mixkvq_chunk_step is mixkvq_chunk_attention, then the chunk is appended as mixkvq_quantize_append_ragged does it; on
+ * MIXKVQ_E_CAPACITY nothing was enqueued.
+ *   scratch_dev: at least mixkvq_chunk_scratch_bytes(cfg, n_tokens_max) bytes, contents are scratch, free for reuse once the call's work has
+ *   run (two calls that may overlap on the GPU need one each, two captured graphs too unless they never run at the same time).
+ * Numeric range: products are fp16 with fp32 accumulation, so |q|, |k|, |v| and dequantized elements must stay below 65504; elements below
+ * 2^-14 round to fp16 subnormals.  A NaN or an infinity among the new tokens reaches the rows that attend to it and no others.
+ * softmax_scale > 0; fragment layout; n_tokens_max <= MIXKVQ_CHUNK_MAX_TOKENS (MIXKVQ_E_UNSUPPORTED otherwise); scratch too small:
+ * MIXKVQ_E_BUFFER_TOO_SMALL.  A wait that runs out sets MIXKVQ_DEV_COPY_TIMEOUT; the rows concerned are then wrong (0 where nothing
+ * contributed).  Nothing is allocated and nothing synchronises with the host. */
+enum { MIXKVQ_OUT_FLOAT = 0, MIXKVQ_OUT_BF16 = 1 };
+#define MIXKVQ_CHUNK_MAX_TOKENS (1 << 24)
+size_t mixkvq_chunk_scratch_bytes(const mixkvq_config* cfg, int n_tokens_max);
+int mixkvq_chunk_attention(mixkvq_cache* cache, int layer, const void* k_dev, const void* v_dev, const void* q_dev, int n_tokens_max,
+                           const int32_t* n_tokens_host, void* out_dev, int out_type, float softmax_scale, void* scratch_dev,
+                           size_t scratch_bytes, void* stream);
+int mixkvq_chunk_step(mixkvq_cache* cache, int layer, const void* k_dev, const void* v_dev, const void* q_dev, int n_tokens_max,
+                      const int32_t* n_tokens_host, void* out_dev, int out_type, float softmax_scale, void* scratch_dev,
+                      size_t scratch_bytes, void* stream);
+
 /* Appendix D ("saliency evaluation is performed post-transformation"): for models with rotary position embeddings the
  * scores, the stored keys and the attention all use rotated queries and keys.  These two calls rotate before they
  * append.  k_dev [B, Hkv, n_tokens, 128] and q_dev [B, Hq, n_tokens, 128] (bf16) are rotated IN PLACE: afterwards q_dev

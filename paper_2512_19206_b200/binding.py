@@ -20,10 +20,11 @@ EXPORTS = [
     "mixkvq_select_channels", "mixkvq_select_channels_raw", "mixkvq_quantize_append",
     "mixkvq_decode_attention", "mixkvq_decode_attention_noalloc", "mixkvq_decode_step", "mixkvq_set_attention_kernel", "mixkvq_query_status",
     "mixkvq_cache_describe", "mixkvq_last_attention", "mixkvq_last_attention_ctas", "mixkvq_launch_count", "mixkvq_status_string",
-    "mixkvq_cache_written_externally", "mixkvq_test_arm_copy_timeout", "mixkvq_test_arm_value_copy_timeout", "mixkvq_rope_append", "mixkvq_rope_decode_step", "mixkvq_prefill", "mixkvq_prefill_scratch_bytes", "mixkvq_quantize_append_ragged", "mixkvq_sequence_fill", "mixkvq_decode_attention_partial", "mixkvq_merge_partials",
+    "mixkvq_cache_written_externally", "mixkvq_test_arm_copy_timeout", "mixkvq_test_arm_value_copy_timeout", "mixkvq_rope_append", "mixkvq_rope_decode_step", "mixkvq_prefill", "mixkvq_prefill_scratch_bytes", "mixkvq_chunk_attention", "mixkvq_chunk_step", "mixkvq_chunk_scratch_bytes", "mixkvq_quantize_append_ragged", "mixkvq_sequence_fill", "mixkvq_decode_attention_partial", "mixkvq_merge_partials",
 ]
 
 DEV_EXTRAS_FULL, DEV_COPY_TIMEOUT = 1, 2
+_OUT_TYPES = {torch.float32: 0, torch.bfloat16: 1}
 ATTN_ONE_UNIT, ATTN_TWO_UNITS, ATTN_DIRECT, ATTN_EARLY, ATTN_OTHER, ATTN_EIGHT_PAIRS = 1, 2, 4, 8, 16, 32
 
 
@@ -81,6 +82,9 @@ def lib():
         L.mixkvq_prefill.argtypes = [vp, i32, vp, vp, vp, i32, vp, f32, vp, C.c_size_t, vp]
         L.mixkvq_prefill_scratch_bytes.argtypes = [C.POINTER(Config), i32]
         L.mixkvq_prefill_scratch_bytes.restype = C.c_size_t
+        L.mixkvq_chunk_scratch_bytes.argtypes = [C.POINTER(Config), i32]
+        L.mixkvq_chunk_scratch_bytes.restype = C.c_size_t
+        L.mixkvq_chunk_attention.argtypes = L.mixkvq_chunk_step.argtypes = [vp, i32, vp, vp, vp, i32, C.POINTER(C.c_int32), vp, i32, f32, vp, C.c_size_t, vp]
         L.mixkvq_rope_append.argtypes = [vp, i32, vp, vp, vp, vp, vp, i32, i32, vp]
         L.mixkvq_rope_decode_step.argtypes = [vp, i32, vp, vp, vp, vp, vp, i32, vp, f32, vp, C.c_size_t, vp]
         L.mixkvq_cache_written_externally.argtypes = [vp]
@@ -92,7 +96,7 @@ def lib():
         L.mixkvq_status_string.argtypes = [i32]
         L.mixkvq_status_string.restype = C.c_char_p
         for name in EXPORTS:
-            if name not in ("mixkvq_launch_count", "mixkvq_status_string", "mixkvq_prefill_scratch_bytes"):
+            if name not in ("mixkvq_launch_count", "mixkvq_status_string", "mixkvq_prefill_scratch_bytes", "mixkvq_chunk_scratch_bytes"):
                 getattr(L, name).restype = i32
         _lib = L
     return _lib
@@ -273,6 +277,45 @@ class Cache:
 
     def prefill_scratch_bytes(self, n_tokens):
         return int(lib().mixkvq_prefill_scratch_bytes(C.byref(self.cfg), int(n_tokens)))
+
+    def chunk_attention(self, layer, k, v, q, scale, counts=None, out=None, scratch=None, dtype=torch.float32):
+        """n new tokens per sequence (k, v [B,Hkv,n,128], q [B,Hq,n,128] bf16) attend to what the layer holds and causally to themselves ->
+        [B,Hq,n,128]; nothing is appended.  `counts`: new tokens per sequence (host ints, n each when absent); rows behind a sequence's count
+        are left as they are.  `out`: float32 or bfloat16 (allocated as `dtype` when absent, zeros behind the counts).  `scratch`: a uint8
+        device tensor of at least chunk_scratch_bytes(n) bytes (allocated here when absent)."""
+        return self._chunk(lib().mixkvq_chunk_attention, "mixkvq_chunk_attention", layer, k, v, q, scale, counts, out, scratch, dtype)
+
+    def chunk_step(self, layer, k, v, q, scale, counts=None, out=None, scratch=None, dtype=torch.float32):
+        """chunk_attention, then the chunk is appended: the later chunk of a prompt (the first one too, on an empty layer)."""
+        return self._chunk(lib().mixkvq_chunk_step, "mixkvq_chunk_step", layer, k, v, q, scale, counts, out, scratch, dtype)
+
+    def _chunk(self, call, name, layer, k, v, q, scale, counts, out, scratch, dtype):
+        cfg, n, dev = self.cfg, k.shape[2] if k.dim() == 4 else 0, self.mem.device
+        if out is None:
+            if dtype not in _OUT_TYPES:
+                raise ValueError(f"{name}: the output is float32 or bfloat16")
+            out = (torch.empty if counts is None else torch.zeros)(q.shape, dtype=dtype, device=dev)
+        for t, heads, what in ((k, cfg.n_kv_heads, "k"), (v, cfg.n_kv_heads, "v"), (q, cfg.n_q_heads, "q"), (out, cfg.n_q_heads, "out")):
+            if t.shape != (cfg.batch, heads, n, 128) or not t.is_contiguous() or t.device != dev:
+                raise ValueError(f"{name}: {what} must be a contiguous [{cfg.batch}, {heads}, n, 128] tensor on {dev}")
+            if t.dtype != torch.bfloat16 and (t is not out or t.dtype != torch.float32):
+                raise ValueError(f"{name}: {what} has dtype {t.dtype}")
+        if scratch is None:
+            scratch = torch.empty(self.chunk_scratch_bytes(n), dtype=torch.uint8, device=dev)
+        elif scratch.dtype != torch.uint8 or not scratch.is_contiguous() or scratch.device != dev:
+            raise ValueError(f"{name}: scratch must be a contiguous uint8 tensor on {dev}")
+        arr = None
+        if counts is not None:
+            if len(counts) != cfg.batch:
+                raise ValueError(f"{name}: {cfg.batch} counts are needed, {len(counts)} were given")
+            arr = (C.c_int32 * cfg.batch)(*[int(c) for c in counts])
+        with torch.cuda.device(dev):
+            _check(call(self.handle, layer, k.data_ptr(), v.data_ptr(), q.data_ptr(), n, arr, out.data_ptr(), _OUT_TYPES[out.dtype], float(scale),
+                        scratch.data_ptr(), scratch.numel(), _stream()), name)
+        return out
+
+    def chunk_scratch_bytes(self, n_tokens):
+        return int(lib().mixkvq_chunk_scratch_bytes(C.byref(self.cfg), int(n_tokens)))
 
     def rope_append(self, layer, k, v, q, cos, sin, pos0):
         """Rotates k [B,Hkv,n,128] and q [B,Hq,n,128] (bf16) IN PLACE with rows pos0.. of the float32 tables cos, sin

@@ -4,7 +4,7 @@
 #include <new>
 #include <vector>
 
-#include "common.cuh"
+#include "chunk.cuh"
 
 using namespace mixkvq;
 
@@ -326,6 +326,54 @@ int append_run(mixkvq_cache* cache, int layer, int b0, int nb, const void* k_dev
   return rc;
 }
 
+// Chunk attention whose arguments have been checked: up to kChunkMaxSeqs sequences per launch.
+int run_chunk(mixkvq_cache* cache, int layer, const void* k_dev, const void* v_dev, const void* q_dev, int n_tokens_max, const int32_t* n_tokens_host,
+              void* out_dev, int out_type, float softmax_scale, void* scratch_dev, cudaStream_t st) {
+  const int B = cache->cfg.batch;
+  for (int b0 = 0; b0 < B; b0 += kChunkMaxSeqs) {
+    const int nb = std::min(B - b0, kChunkMaxSeqs);
+    LayerView lv = view(cache, layer, b0, nb);
+    ChunkArgs a{};
+    const size_t kv = (size_t)b0 * cache->cfg.n_kv_heads * n_tokens_max * kD, qo = (size_t)b0 * cache->cfg.n_q_heads * n_tokens_max * kD;
+    a.k = static_cast<const uint16_t*>(k_dev) + kv;
+    a.v = static_cast<const uint16_t*>(v_dev) + kv;
+    a.q = static_cast<const uint16_t*>(q_dev) + qo;
+    a.out = static_cast<char*>(out_dev) + qo * (out_type == MIXKVQ_OUT_BF16 ? 2 : 4);
+    a.out_bf16 = out_type == MIXKVQ_OUT_BF16;
+    a.parts = static_cast<float*>(scratch_dev);
+    a.stride = n_tokens_max;
+    a.scale_log2e = softmax_scale * 1.4426950408889634f;
+    a.max_polls = cache->test_wait_polls;
+    a.test_silent = cache->test_extra_tx;
+    for (int b = 0; b < nb; ++b) {
+      const int i = fi(cache, layer, b0 + b);
+      a.seq[b].units = cache->n_blocks[i] * cache->U;
+      a.seq[b].tail = cache->r[i] | cache->n_sink[i] << 16;
+      a.seq[b].n = n_tokens_host ? n_tokens_host[b0 + b] : n_tokens_max;
+    }
+    int launches = 0;
+    const cudaError_t e = launch_chunk_attention(lv, a, cache->n_sms, st, &launches);
+    cache->launches += launches;
+    if (launches) note_enqueued(cache, st, kNoPackedWrite);
+    if (e != cudaSuccess) return MIXKVQ_E_CUDA;
+  }
+  return MIXKVQ_OK;
+}
+
+int check_chunk(const mixkvq_cache* cache, int layer, const void* k_dev, const void* v_dev, const void* q_dev, int n_tokens_max,
+                const int32_t* n_tokens_host, const void* out_dev, int out_type, float softmax_scale, const void* scratch_dev, size_t scratch_bytes) {
+  if (!cache || !k_dev || !v_dev || !q_dev || !out_dev || !scratch_dev || layer < 0 || layer >= cache->cfg.n_layers || n_tokens_max < 1 ||
+      (out_type != MIXKVQ_OUT_FLOAT && out_type != MIXKVQ_OUT_BF16) || !(softmax_scale > 0.f))
+    return MIXKVQ_E_INVALID_ARG;
+  if (n_tokens_host)
+    for (int b = 0; b < cache->cfg.batch; ++b)
+      if (n_tokens_host[b] < 0 || n_tokens_host[b] > n_tokens_max) return MIXKVQ_E_INVALID_ARG;
+  if (!aligned16(k_dev) || !aligned16(v_dev) || !aligned16(q_dev) || !aligned16(out_dev) || !aligned16(scratch_dev)) return MIXKVQ_E_ALIGNMENT;
+  if (cache->tile || n_tokens_max > MIXKVQ_CHUNK_MAX_TOKENS) return MIXKVQ_E_UNSUPPORTED;
+  if (scratch_bytes < chunk_scratch_bytes(cache->g, n_tokens_max)) return MIXKVQ_E_BUFFER_TOO_SMALL;
+  return MIXKVQ_OK;
+}
+
 // A decode step whose arguments have been checked.  rope_cos / rope_sin: the position's rows of the tables (null: no rotation); the
 // split kernel rotates what it reads and the call's last kernel leaves the rotated rows in the caller's tensors, so that the rotation is
 // no launch in front of the step.
@@ -422,7 +470,7 @@ int mixkvq_cache_init(const mixkvq_config* cfg, void* cache_dev, size_t bytes, v
   if (cudaMemsetAsync(h->mem, 0, kHeaderBytes, st) != cudaSuccess) { delete h; return MIXKVQ_E_CUDA; }
   if (zero_all_layers(h, st) != MIXKVQ_OK) { delete h; return MIXKVQ_E_CUDA; }
   if (attention_ws_setup() != cudaSuccess || attention_tc_setup() != cudaSuccess || prefill_attention_setup() != cudaSuccess ||
-      flush_setup() != cudaSuccess) { delete h; return MIXKVQ_E_CUDA; }
+      chunk_attention_setup() != cudaSuccess || flush_setup() != cudaSuccess) { delete h; return MIXKVQ_E_CUDA; }
   *out = h;
   return MIXKVQ_OK;
 }
@@ -582,6 +630,34 @@ int mixkvq_prefill(mixkvq_cache* cache, int layer, const void* k_dev, const void
   cache->launches += 2;
   note_enqueued(cache, static_cast<cudaStream_t>(stream), kNoPackedWrite);
   return append_run(cache, layer, 0, cache->cfg.batch, k_dev, v_dev, q_dev, n_tokens, n_tokens, true, static_cast<cudaStream_t>(stream));
+}
+
+size_t mixkvq_chunk_scratch_bytes(const mixkvq_config* cfg, int n_tokens_max) {
+  if (check_config(cfg) != MIXKVQ_OK || n_tokens_max < 1 || n_tokens_max > MIXKVQ_CHUNK_MAX_TOKENS) return 0;
+  return chunk_scratch_bytes(cfg->n_q_heads / cfg->n_kv_heads, n_tokens_max);
+}
+
+int mixkvq_chunk_attention(mixkvq_cache* cache, int layer, const void* k_dev, const void* v_dev, const void* q_dev, int n_tokens_max,
+                           const int32_t* n_tokens_host, void* out_dev, int out_type, float softmax_scale, void* scratch_dev, size_t scratch_bytes,
+                           void* stream) {
+  const int rc = check_chunk(cache, layer, k_dev, v_dev, q_dev, n_tokens_max, n_tokens_host, out_dev, out_type, softmax_scale, scratch_dev, scratch_bytes);
+  if (rc != MIXKVQ_OK) return rc;
+  return run_chunk(cache, layer, k_dev, v_dev, q_dev, n_tokens_max, n_tokens_host, out_dev, out_type, softmax_scale, scratch_dev,
+                   static_cast<cudaStream_t>(stream));
+}
+
+int mixkvq_chunk_step(mixkvq_cache* cache, int layer, const void* k_dev, const void* v_dev, const void* q_dev, int n_tokens_max,
+                      const int32_t* n_tokens_host, void* out_dev, int out_type, float softmax_scale, void* scratch_dev, size_t scratch_bytes,
+                      void* stream) {
+  int rc = check_chunk(cache, layer, k_dev, v_dev, q_dev, n_tokens_max, n_tokens_host, out_dev, out_type, softmax_scale, scratch_dev, scratch_bytes);
+  if (rc != MIXKVQ_OK) return rc;
+  for (int b = 0; b < cache->cfg.batch; ++b)
+    if (tokens_held(cache, layer, b) + (n_tokens_host ? n_tokens_host[b] : n_tokens_max) > cache->cfg.max_tokens) return MIXKVQ_E_CAPACITY;
+  rc = run_chunk(cache, layer, k_dev, v_dev, q_dev, n_tokens_max, n_tokens_host, out_dev, out_type, softmax_scale, scratch_dev,
+                 static_cast<cudaStream_t>(stream));
+  if (rc != MIXKVQ_OK) return rc;
+  return n_tokens_host ? mixkvq_quantize_append_ragged(cache, layer, k_dev, v_dev, q_dev, n_tokens_max, n_tokens_host, stream)
+                       : mixkvq_quantize_append(cache, layer, k_dev, v_dev, q_dev, n_tokens_max, stream);
 }
 
 int mixkvq_rope_append(mixkvq_cache* cache, int layer, void* k_dev, const void* v_dev, void* q_dev, const float* cos_dev,

@@ -34,7 +34,7 @@
 // Rows: with 256 rows of one head per CTA the last row tile of 4 x 777 tokens (8b shape) held 9 rows of 256 and the diagonal tiles were
 // half empty; side by side the heads take 13 row tiles with 49 key tiles per stream instead of 16 with 76: attention 75 -> 54 us,
 // whole call 108 -> 93 us per layer.
-#include "common.cuh"
+#include "tc_ops.cuh"
 
 namespace mixkvq {
 
@@ -49,110 +49,6 @@ constexpr int kSmem = 6 * kTileBytes + 256;      // two Q tiles, two K and two V
 enum Bar { kKFull = 0, kVFull = 2, kKEmpty = 4, kVEmpty = 6, kSFull = 8, kPHalf = 10, kPReady = 12, kDoneA = 14, kDoneB = 15, kDone = 16 };
 constexpr uint32_t kPolls = 1u << 21;
 
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-// Canonical layout without swizzle: 8-row x 16-byte core matrices; row r, 16-bit element k of a 128 x 128 K-major tile
-// sits at byte (r / 8) * 2048 + (k / 8) * 128 + (r % 8) * 16 + (k % 8) * 2.
-__device__ __forceinline__ uint64_t make_desc(uint32_t saddr, uint32_t lbo_bytes, uint32_t sbo_bytes) {
-  return (uint64_t)((saddr >> 4) & 0x3FFF) | ((uint64_t)((lbo_bytes >> 4) & 0x3FFF) << 16) |
-         ((uint64_t)((sbo_bytes >> 4) & 0x3FFF) << 32) | ((uint64_t)1 << 46);
-}
-// instruction descriptor of kind::f16: fp32 accumulator; operand formats 0 = fp16, 1 = bf16; B K-major (0) or MN-major (1)
-__device__ __forceinline__ constexpr uint32_t make_idesc(int M, int N, int fmt, int b_mn_major) {
-  return (1u << 4) | ((uint32_t)fmt << 7) | ((uint32_t)fmt << 10) | ((uint32_t)b_mn_major << 16) |
-         ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
-}
-__device__ __forceinline__ void mbar_init(uint32_t bar, int count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
-}
-__device__ __forceinline__ bool mbar_wait_polls(uint32_t bar, uint32_t parity, uint32_t max_polls) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\tmov.u32 n, 0;\n"
-      "PREFILL_WAIT:\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 1000;\n\t"
-      "@p bra PREFILL_DONE;\n\t"
-      "add.u32 n, n, 1;\n\t"
-      "setp.lt.u32 q, n, %3;\n\t"
-      "@q bra PREFILL_WAIT;\n"
-      "PREFILL_DONE:\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity), "r"(max_polls)
-      : "memory");
-  return ok != 0;
-}
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-// D (tensor memory) = A (shared memory) * B (shared memory) [+ D]
-__device__ __forceinline__ void tc_mma_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
-                                          uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-// A load of 16 columns of the thread's tensor-memory lane.  The registers are valid only after tmem_wait_ld16 on them (the wait names
-//  the registers as operands, so that no use of them is scheduled before it).  tcgen05.wait::ld covers every load
-// the thread has issued, so a load issued before a block of arithmetic and waited for after it runs under that arithmetic.
-__device__ __forceinline__ void tmem_ld16_issue(uint32_t taddr, uint32_t (&u)[16]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]),
-        "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
-      : "r"(taddr)
-      : "memory");
-}
-__device__ __forceinline__ void tmem_wait_ld16(uint32_t (&u)[16]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(u[0]), "+r"(u[1]), "+r"(u[2]), "+r"(u[3]), "+r"(u[4]), "+r"(u[5]), "+r"(u[6]), "+r"(u[7]), "+r"(u[8]),
-                 "+r"(u[9]), "+r"(u[10]), "+r"(u[11]), "+r"(u[12]), "+r"(u[13]), "+r"(u[14]), "+r"(u[15])
-               :
-               : "memory");
-}
-__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&w)[8]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(w[0]), "r"(w[1]),
-               "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-               : "memory");
-}
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
-  __half2 h = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<uint32_t*>(&h);
-}
-__device__ __forceinline__ uint32_t bf16x2_to_f16x2(uint32_t w) {
-  return pack_half2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
-}
-
-
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
-               "l"(src), "r"(bytes), "r"(bar)
-               : "memory");
-}
-// D (tensor memory) = A (tensor memory, 16-bit pairs per column) * B (shared memory) [+ D]
-__device__ __forceinline__ void tc_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
-                                          uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
 // K, V [B * Hkv][L][128] bf16 -> tile images [B * Hkv][n_tiles][32 KB]: K as the K-major B operand of Q K^T (bf16),
 // V as the MN-major B operand of P V (fp16); rows past L are zero.  Consecutive threads write consecutive 16 bytes.
 __global__ void __launch_bounds__(256)
@@ -182,66 +78,6 @@ prefill_pack_kernel(const __nv_bfloat16* __restrict__ k, const __nv_bfloat16* __
     const int i = threadIdx.x + 256 * n;
     kd[i] = x[n];
     vd[i] = make_uint4(bf16x2_to_f16x2(y[n].x), bf16x2_to_f16x2(y[n].y), bf16x2_to_f16x2(y[n].z), bf16x2_to_f16x2(y[n].w));
-  }
-}
-
-// Two fp32 values in one 64-bit register: the FMA pipe does both halves of these with one instruction.
-__device__ __forceinline__ uint64_t pack2(float a, float b) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ uint64_t pack2u(uint32_t a, uint32_t b) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(a), "r"(b));
-  return r;
-}
-__device__ __forceinline__ void unpack2(uint64_t x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-
-// Calls f(piece, columns) for the pieces of 16 columns below n_pieces of the thread's tensor-memory row, the next piece in flight.
-template <bool kAll, typename F>
-__device__ __forceinline__ void for_pieces(uint32_t taddr, int n_pieces, F f) {
-  if constexpr (kAll) {
-    uint32_t a[16], b[16];
-    tmem_ld16_issue(taddr, a);
-#pragma unroll
-    for (int h = 0; h < 8; h += 2) {
-      tmem_wait_ld16(a);
-      tmem_ld16_issue(taddr + 16 * h + 16, b);
-      f(h, a);
-      tmem_wait_ld16(b);
-      if (h < 6) tmem_ld16_issue(taddr + 16 * h + 32, a);
-      f(h + 1, b);
-    }
-  } else {
-    uint32_t a[16], b[16];
-    tmem_ld16_issue(taddr, a);
-#pragma unroll 1
-    for (int h = 0; h < n_pieces; h += 2) {
-      tmem_wait_ld16(a);
-      if (h + 1 < n_pieces) tmem_ld16_issue(taddr + 16 * h + 16, b);
-      f(h, a);
-      if (h + 1 < n_pieces) {
-        tmem_wait_ld16(b);
-        if (h + 2 < n_pieces) tmem_ld16_issue(taddr + 16 * h + 32, a);
-        f(h + 1, b);
-      }
-    }
   }
 }
 
