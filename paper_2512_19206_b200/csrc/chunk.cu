@@ -3,11 +3,11 @@
 //   o_j = sum_t softmax_t(scale q_j . k_t) v_t,   t over the sink, the packed blocks (dequantized, Eq. 3), the residual window and the
 //   new tokens up to j.
 //
-// One thread block of 640 threads per SM, persistent over its share of the (item, key tile) line (chunk.cuh).  Per key tile of 128 keys:
-//   warps 8-11, 12-15   make the tile: four warps the keys, four the values, one 32-token unit each.  Packed codes become fp16 in registers
+// One thread block of 896 threads per SM, persistent over its share of the (item, key tile) line (chunk.cuh).  Per key tile of 128 keys:
+//   warps 8-15, 16-23   make the tile: eight warps the keys, eight the values, half a 32-token unit each.  Packed codes become fp16 in registers
 //                       (c s + z, one rounding) and go to shared memory in the tensor core's canonical layout; an unquantized row is copied
 //                       with bf16 -> fp16.  The packed bytes are read once per 256 query rows and never written back dequantized.
-//   warp 16             one thread issues every tcgen05.mma: S = Q K^T (operands in shared memory), O += P V (P in tensor memory).
+//   warp 24             one thread issues every tcgen05.mma: S = Q K^T (operands in shared memory), O += P V (P in tensor memory).
 //   warps 0-3, 4-7      two softmax groups ("slots"), thread = query row = lane of tensor memory.  An item of more than 128 rows has its first 128 rows
 //                       in slot 0 and the others in slot 1; in a smaller one both slots have the same rows, slot 0 the even key tiles and slot 1
 //                       the odd ones, and their results meet at the end: the tensor core works for one slot while the other is in its softmax.
@@ -27,16 +27,20 @@ namespace {
 
 constexpr int kTile = kChunkTile;
 constexpr int kTileBytes = kTile * kD * 2;
-constexpr int kThreads = 640;                             // 96 registers a thread at launch: 61440, shared out below as 2 x 128 x 112, 2 x 128 x 112, 128 x 32
+constexpr int kThreads = 896;                             // 72 registers a thread at launch: 64512, shared out below as 256 x 104, 512 x 64, 128 x 40
 constexpr int kSoftmaxThreads = 256;
-constexpr int kScratchOff = 6 * kTileBytes;               // per producer warp 1 KB: scales and zero-points as fp16 pairs
-constexpr int kMlOff = kScratchOff + 8 * 1024;            // slot 1's maxima and denominators (128 x 8 bytes)
+constexpr int kIssueWarp = 24;
+constexpr int kScratchOff = 6 * kTileBytes;               // per producer warp 512 bytes: scales and zero-points as fp16 pairs
+constexpr int kMlOff = kScratchOff + 16 * 512;            // slot 1's maxima and denominators (128 x 8 bytes)
 constexpr int kBarOff = kMlOff + 1024;
-constexpr int kBars = 17;
-constexpr int kSmem = kBarOff + 8 * kBars + 8;
-enum Bar { kQFull = 0, kKFull = 1, kVFull = 3, kKEmpty = 5, kVEmpty = 7, kSFull = 9, kPReady = 11, kODone = 13, kDone = 15 };
+constexpr int kBars = 20;
+constexpr int kReaders = 26;                              // of a segment: 8 softmax, 16 producer warps, the issuing thread, the L2 requests
+constexpr int kSegOff = kBarOff + 8 * kBars + 16;         // (the tensor-memory address and the producers' progress behind the barriers)
+constexpr int kSmem = kSegOff + 2 * 64;
+enum Bar { kQFull = 0, kKFull = 1, kVFull = 3, kKEmpty = 5, kVEmpty = 7, kSFull = 9, kPReady = 11, kODone = 13, kDone = 15, kSegFull = 16, kSegEmpty = 18 };
 constexpr uint32_t kPolls = 1u << 21;
-constexpr float kRaise = 8.f;
+constexpr float kRaise = 10.f;
+constexpr int kAhead = 8;
 
 __device__ __forceinline__ void sts32(uint32_t a, uint32_t x) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(a), "r"(x) : "memory"); }
 __device__ __forceinline__ void sts16(uint32_t a, uint32_t x) { asm volatile("st.shared.u16 [%0], %1;" ::"r"(a), "h"((uint16_t)x) : "memory"); }
@@ -52,6 +56,25 @@ __device__ __forceinline__ uint32_t hfma2_u(uint32_t a, uint32_t b, uint32_t c) 
   uint32_t d;
   asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
   return d;
+}
+// Polls a phase of a barrier up to max_polls times; false if it never completed.  (Without a time hint: with one the instruction becomes a loop of
+// sleeps and polls, and two dozen waiting warps took half of the SM's issue slots.)
+__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, uint32_t max_polls) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\tmov.u32 n, 0;\n"
+      "CHUNK_WAIT:\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "@p bra CHUNK_DONE;\n\t"
+      "add.u32 n, n, 1;\n\t"
+      "setp.lt.u32 q, n, %3;\n\t"
+      "@q bra CHUNK_WAIT;\n"
+      "CHUNK_DONE:\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity), "r"(max_polls)
+      : "memory");
+  return ok != 0;
 }
 __device__ __forceinline__ uint4 rows_to_half(uint4 x) {
   return make_uint4(bf16x2_to_f16x2(x.x), bf16x2_to_f16x2(x.y), bf16x2_to_f16x2(x.z), bf16x2_to_f16x2(x.w));
@@ -77,79 +100,67 @@ __device__ __forceinline__ uint32_t codes4(uint32_t lo, uint32_t hi, int f) {
   return hfma2_u((l & (0x00030003u << (2 * ff))) | (h & (0x000C000Cu << (2 * ff))) | 0x64006400u, inv_pow4(ff), neg_1024_pow4(ff));
 }
 
-struct Stream {                          // where an item's keys and values are
-  const char *base, *extras;
-  const uint32_t* table;
-  const uint16_t *resk, *resv, *sinkk, *sinkv, *newk, *newv;
-  int units, r, c0, total;               // packed units; residual rows; residual and sink rows; all unquantized rows that the item may see
-};
-__device__ inline Stream stream_of(const LayerView& lv, const ChunkArgs& a, const ChunkItem& it) {
-  Stream x;
-  const int s = it.b * lv.Hkv + it.hk;
-  const ChunkSeq sq = a.seq[it.b];
-  x.base = lv.base + (size_t)s * lv.base_stride;
-  x.extras = lv.extras + (size_t)s * lv.extras_stride;
-  x.table = reinterpret_cast<const uint32_t*>(lv.table + (size_t)s * lv.table_stride);
-  x.resk = reinterpret_cast<const uint16_t*>(lv.resk + (size_t)s * lv.resk_stride);
-  x.resv = reinterpret_cast<const uint16_t*>(lv.resv + (size_t)s * lv.resv_stride);
-  x.sinkk = reinterpret_cast<const uint16_t*>(lv.sink + (size_t)s * lv.sink_stride);
-  x.sinkv = x.sinkk + (size_t)lv.sink_len * kD;
-  x.newk = a.k + (size_t)s * a.stride * kD;
-  x.newv = a.v + (size_t)s * a.stride * kD;
-  x.units = sq.units;
-  x.r = sq.tail & 0xFFFF;
-  x.c0 = chunk_tail_rows(sq);
-  x.total = x.c0 + sq.n;
-  return x;
-}
-__device__ __forceinline__ const uint16_t* tail_row(const uint16_t* res, const uint16_t* sink, const uint16_t* fresh, const Stream& x, int i) {
-  return i < x.r ? res + (size_t)i * kD : i < x.c0 ? sink + (size_t)(i - x.r) * kD : fresh + (size_t)(i - x.c0) * kD;
+// Block and unit inside it of a unit number (below 2^26): inv = 2^32 / U rounded up, 0 for U = 1.
+__device__ __forceinline__ int block_of(int unit, uint32_t inv) { return inv == 0u ? unit : (int)__umulhi((uint32_t)unit, inv); }
+
+__device__ __forceinline__ void prefetch_bulk(const void* p, uint32_t bytes) {
+  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
 }
 
-// One unit's packed keys or values on their way to shared memory: requested one tile ahead.
+__device__ __forceinline__ uint32_t inverse_units(const LayerView& lv) { return lv.U == 1 ? 0u : 0xFFFFFFFFu / (uint32_t)lv.U + 1u; }
+
+struct Rows {                            // a stream's unquantized rows: residual window, sink, new tokens
+  const uint16_t *res, *sink, *fresh;
+  int r, c0, total;                      // rows of the window; of the window and the sink; all
+  __device__ __forceinline__ const uint4* row(int i) const {
+    return reinterpret_cast<const uint4*>(i < r ? res + (size_t)i * kD : i < c0 ? sink + (size_t)(i - r) * kD : fresh + (size_t)(i - c0) * kD);
+  }
+};
+
+// Half a unit's packed keys or values on their way to shared memory: requested one tile ahead.
 struct Packed {
-  uint4 c0, c1, h0, h1, meta;
+  uint4 c, h, meta;
 };
+// A unit's place in its block (VG = 128 / G says how many units share a group's scales: 1, 2 or 4).
+__device__ __forceinline__ uint32_t group_shift(const LayerView& lv) { return lv.VG == 4 ? 0u : lv.VG == 2 ? 1u : 2u; }
 
-// ---- keys: warp w makes rows 32 w .. 32 w + 31 of the tile at shared address `tile`
+// ---- keys: warp (w, mt) makes rows 32 w + 16 mt .. + 15 of the tile at shared address `tile`
 template <bool kDense>
-__device__ __forceinline__ Packed request_keys(const LayerView& lv, const Stream& x, int unit, uint2 entry, int lane) {
-  Packed p;
-  const int bi = unit / lv.U, u = unit - bi * lv.U;
-  const char* blk = x.base + (size_t)bi * lv.base_bytes;
-  const uint4* codes = reinterpret_cast<const uint4*>(blk + frag_unit_off(u, lv.G, lv.unit_bytes));
-  p.c0 = codes[lane];
-  p.c1 = codes[32 + lane];
-  p.meta = reinterpret_cast<const uint4*>(blk + frag_meta_off((u * 32) / lv.G, lv.G, lv.unit_bytes))[lane];
+__device__ __forceinline__ Packed request_keys(const LayerView& lv, const char* base, const char* extras, uint32_t inv_u, int unit, uint2 entry, int mt, int lane) {
+  Packed p{};
+  const int bi = block_of(unit, inv_u), u = unit - bi * lv.U;
+  const uint32_t group = (uint32_t)u >> group_shift(lv);
+  const char* blk = base + (size_t)bi * lv.base_bytes;
+  p.c = reinterpret_cast<const uint4*>(blk + (uint32_t)u * lv.unit_bytes + 512u * (group + 1))[32 * mt + lane];
+  p.meta = reinterpret_cast<const uint4*>(blk + (group << group_shift(lv)) * lv.unit_bytes + 512u * group)[lane];
   if (kDense) {
     const int n16 = entry.y & 0xFF, n4 = (entry.y >> 8) & 0xFF;
-    if (n4 != 0) {
-      const uint4* hi = reinterpret_cast<const uint4*>(x.extras + (size_t)entry.x * 16 + extras_header_bytes(n16, n4) +
-                                                       (size_t)u * extras_unit_bytes(n16, n4, true) + 128 * ((n16 + 1) >> 1));
-      p.h0 = hi[lane];
-      p.h1 = hi[32 + lane];
-    } else {
-      p.h0 = p.h1 = make_uint4(0u, 0u, 0u, 0u);
-    }
+    if (n4 != 0)
+      p.h = reinterpret_cast<const uint4*>(extras + (size_t)entry.x * 16 + extras_header_bytes(n16, n4) +
+                                           (size_t)u * extras_unit_bytes(n16, n4, true) + 128 * ((n16 + 1) >> 1))[32 * mt + lane];
   }
   return p;
 }
 
 template <bool kDense>
-__device__ __forceinline__ void make_keys(const LayerView& lv, const Stream& x, const Packed& p, int unit, uint2 entry, uint32_t tile, uint32_t scratch,
-                                          int w, int lane) {
-  const int bi = unit / lv.U, u = unit - bi * lv.U;
+__device__ __forceinline__ void make_keys(const LayerView& lv, const char* base, const char* extras, uint32_t inv_u, const Packed& p, int unit, uint2 entry,
+                                          uint32_t tile, uint32_t scratch, int w, int mt, int lane) {
   const int n16 = entry.y & 0xFF, n4 = (entry.y >> 8) & 0xFF, n16p = (n16 + 1) >> 1;
-  const char* ex = x.extras + (size_t)entry.x * 16;
-  const char* exu = ex + extras_header_bytes(n16, n4) + (size_t)u * extras_unit_bytes(n16, n4, kDense);
-  // the promoted channels' first four pairs and their numbers are under way while the codes are worked on
-  uint4 head = make_uint4(~0u, ~0u, ~0u, ~0u);
-  uint32_t raw[4] = {0u, 0u, 0u, 0u};
-  if (n16 > 0) {
-    head = *reinterpret_cast<const uint4*>(ex);
+  // Promoted channels: the lane's token is tok = 16 mt + lane % 16 of the unit, and of the pairs it takes every second one.  The first two and their
+  // channel numbers are under way while the codes are worked on.
+  const int tok = 16 * mt + (lane & 15), par = lane >> 4;
+  const char *ex = nullptr, *exu = nullptr;
+  uint32_t ids[2] = {~0u, ~0u}, raw[2] = {0u, 0u};
+  if (n16 + n4 > 0) {
+    const int u = unit - block_of(unit, inv_u) * lv.U;
+    ex = extras + (size_t)entry.x * 16;
+    exu = ex + extras_header_bytes(n16, n4) + (size_t)u * extras_unit_bytes(n16, n4, kDense);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (i < n16p) raw[i] = reinterpret_cast<const uint32_t*>(exu)[i * 32 + lane];
+    for (int i = 0; i < 2; ++i)
+      if (2 * i + par < n16p) {
+        ids[i] = reinterpret_cast<const uint16_t*>(ex)[2 * i + par];
+        raw[i] = reinterpret_cast<const uint32_t*>(exu)[(2 * i + par) * 32 + tok];
+      }
   }
   // scales and zero-points of channel pairs (16 kt + 8 ch + 2 t, + 1) as fp16 pairs: word 16 t + 8 ch + kt, zero-points 64 words on.  The lane has the
   // pairs 2 lane and 2 lane + 1: kt = lane / 4, ch = lane / 2 % 2, t = 2 (lane % 2) and the next.
@@ -161,157 +172,154 @@ __device__ __forceinline__ void make_keys(const LayerView& lv, const Stream& x, 
     sts32(at + 64 + 256, bf16x2_to_f16x2(__byte_perm(p.meta.z, p.meta.w, 0x7632)));
   }
   __syncwarp();
-  const uint32_t c[2][4] = {{p.c0.x, p.c0.y, p.c0.z, p.c0.w}, {p.c1.x, p.c1.y, p.c1.z, p.c1.w}};
-  const uint32_t h[2][4] = {{p.h0.x, p.h0.y, p.h0.z, p.h0.w}, {p.h1.x, p.h1.y, p.h1.z, p.h1.w}};
-  const uint32_t out = tile + 4 * w * 2048 + 4 * lane;
+  // (a rolled loop: every role's straight-line code together runs out of the instruction cache)
+  uint32_t c0 = p.c.x, c1 = p.c.y, h0 = p.h.x, h1 = p.h.y;
+  uint32_t to = tile + (4 * w + 2 * mt) * 2048 + 4 * lane, at = scratch + 64 * (lane & 3);
+#pragma unroll 1
+  for (int ch = 0; ch < 2; ++ch) {       // the upper or lower 8 of every 16 channels
 #pragma unroll
-  for (int ch = 0; ch < 2; ++ch) {
-    const uint32_t at = scratch + 4 * (16 * (lane & 3) + 8 * ch);
-    const uint4 sa = lds128(at), sb = lds128(at + 16), za = lds128(at + 256), zb = lds128(at + 272);
-    const uint32_t s[8] = {sa.x, sa.y, sa.z, sa.w, sb.x, sb.y, sb.z, sb.w}, z[8] = {za.x, za.y, za.z, za.w, zb.x, zb.y, zb.z, zb.w};
+    for (int kh = 0; kh < 2; ++kh) {
+      const uint4 s4 = lds128(at + 16 * kh), z4 = lds128(at + 256 + 16 * kh);
+      const uint32_t s[4] = {s4.x, s4.y, s4.z, s4.w}, z[4] = {z4.x, z4.y, z4.z, z4.w};
 #pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-      for (int rh = 0; rh < 2; ++rh) {
-        const uint32_t wd = c[mt][2 * ch + rh], hd = h[mt][2 * ch + rh];
-#pragma unroll
-        for (int kt = 0; kt < 8; ++kt)
-          sts32(out + (2 * mt + rh) * 2048 + (2 * kt + ch) * 128, hfma2_u(kDense ? codes4(wd, hd, kt) : codes2(wd, kt), s[kt], z[kt]));
+      for (int k = 0; k < 4; ++k) {
+        const int kt = 4 * kh + k;
+        sts32(to + 2 * kt * 128, hfma2_u(kDense ? codes4(c0, h0, kt) : codes2(c0, kt), s[k], z[k]));
+        sts32(to + 2048 + 2 * kt * 128, hfma2_u(kDense ? codes4(c1, h1, kt) : codes2(c1, kt), s[k], z[k]));
       }
+    }
+    c0 = p.c.z;
+    c1 = p.c.w;
+    h0 = p.h.z;
+    h1 = p.h.w;
+    to += 128;
+    at += 32;
   }
   if ((n16 | (kDense ? 0 : n4)) == 0) return;
-  __syncwarp();                          // the base codes are stored: promoted channels replace theirs.  The lane's token: 32 w + lane
-  const uint32_t row = tile + (4 * w + (lane >> 3)) * 2048 + (lane & 7) * 16;
+  __syncwarp();                          // the base codes are stored: promoted channels replace theirs
+  const uint32_t row = tile + (4 * w + (tok >> 3)) * 2048 + (tok & 7) * 16;
   auto put = [&](uint32_t d, float value) { sts16(row + (d >> 3) * 128 + (d & 7) * 2, (uint32_t)__half_as_ushort(__float2half_rn(value))); };
 #pragma unroll 1
   for (int i0 = 0; i0 < n16p; i0 += 4) {
-    uint32_t ids[2] = {head.x, head.y};
-    if (i0 > 0) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (i0 + i < n16p) raw[i] = reinterpret_cast<const uint32_t*>(exu)[(i0 + i) * 32 + lane];
-      const uint2 more = *reinterpret_cast<const uint2*>(ex + 2 * i0);
-      ids[0] = more.x;
-      ids[1] = more.y;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (i0 + i < n16p) {
-        const uint32_t id = ids[i >> 1] >> (16 * (i & 1)), d0 = id & 0xFF, d1 = (id >> 8) & 0xFF;
-        if (d0 < kD) put(d0, bf_lo(raw[i]));
-        if (d1 < kD) put(d1, bf_hi(raw[i]));
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t d0 = ids[i] & 0xFF, d1 = (ids[i] >> 8) & 0xFF;
+      if (d0 < kD) put(d0, bf_lo(raw[i]));
+      if (d1 < kD) put(d1, bf_hi(raw[i]));
+      ids[i] = ~0u;
+      const int next = i0 + 4 + 2 * i + par;
+      if (next < n16p) {
+        ids[i] = reinterpret_cast<const uint16_t*>(ex)[next];
+        raw[i] = reinterpret_cast<const uint32_t*>(exu)[next * 32 + tok];
       }
+    }
   }
-  if (!kDense && n4 > 0) {               // UINT4 channels: c = c_lo + 4 c_hi, with s and z from the block's scales
-    const char* blk = x.base + (size_t)bi * lv.base_bytes;
-    const uint32_t* low = reinterpret_cast<const uint32_t*>(blk + frag_unit_off(u, lv.G, lv.unit_bytes));
-    const uint32_t* meta = reinterpret_cast<const uint32_t*>(blk + frag_meta_off((u * 32) / lv.G, lv.G, lv.unit_bytes));
-    const uint32_t* high = reinterpret_cast<const uint32_t*>(exu + 128 * n16p);
-    const int mt = lane >> 4, rh = (lane >> 3) & 1, r = lane & 7;
-    const int lane_word = mt * 128 + 16 * r + rh, hi_bit = 8 * (r >> 2) + 2 * (2 * mt + rh);
-#pragma unroll 2
+  if (!kDense && n4 > 0) {               // UINT4 channels: c = c_lo + 4 c_hi, with s and z from the block's scales; of a pair the lane has channel `par`
+    const int bi = block_of(unit, inv_u), u = unit - bi * lv.U;
+    const uint32_t group = (uint32_t)u >> group_shift(lv);
+    const char* blk = base + (size_t)bi * lv.base_bytes;
+    const int rh = (lane >> 3) & 1, r = lane & 7;
+    const uint32_t* low = reinterpret_cast<const uint32_t*>(blk + (uint32_t)u * lv.unit_bytes + 512u * (group + 1)) + mt * 128 + 16 * r + rh;
+    const uint32_t* meta = reinterpret_cast<const uint32_t*>(blk + (group << group_shift(lv)) * lv.unit_bytes + 512u * group);
+    const uint32_t* high = reinterpret_cast<const uint32_t*>(exu + 128 * n16p) + (r & 3);
+    const uint8_t* chans = reinterpret_cast<const uint8_t*>(ex + 2 * n16p) + par;
+    const int hi_bit = 16 * par + 8 * (r >> 2) + 2 * (2 * mt + rh);
+#pragma unroll 4
     for (int i = 0; i < (n4 + 1) >> 1; ++i) {
-      const uint32_t id = *reinterpret_cast<const uint16_t*>(ex + 2 * n16p + 2 * i), hw = high[4 * i + (r & 3)] >> hi_bit;
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const uint32_t d = (id >> (8 * e)) & 0xFF;
-        if (d < kD) {
-          const uint32_t lw = low[lane_word + 4 * ((d & 7) >> 1) + 2 * ((d >> 3) & 1)], mz = meta[d];
-          const uint32_t code = ((lw >> (16 * (d & 1) + 2 * (d >> 4))) & 3u) | (((hw >> (16 * e)) & 3u) << 2);
-          put(d, fmaf((float)code, bf_lo(mz), bf_hi(mz)));
-        }
+      const uint32_t d = chans[2 * i], hw = high[4 * i];
+      if (d < kD) {
+        const uint32_t lw = low[4 * ((d & 7) >> 1) + 2 * ((d >> 3) & 1)], mz = meta[d];
+        const uint32_t code = ((lw >> (16 * (d & 1) + 2 * (d >> 4))) & 3u) | (((hw >> hi_bit) & 3u) << 2);
+        put(d, fmaf((float)code, bf_lo(mz), bf_hi(mz)));
       }
     }
   }
 }
 
-// ---- values: warp w makes keys 32 w .. 32 w + 31 of the tile, stored channel by channel (K-major for O = P V)
+// ---- values: warp (w, half) makes keys 32 w .. 32 w + 31 of channels 64 half .. + 63, stored channel by channel (K-major for O = P V)
 template <bool kV4>
-__device__ __forceinline__ Packed request_values(const LayerView& lv, const Stream& x, int unit, int lane) {
-  Packed p;
-  const int bi = unit / lv.U, u = unit - bi * lv.U;
-  const char* at = x.base + (size_t)bi * lv.base_bytes + frag_unit_off(u, lv.G, lv.unit_bytes);
-  p.c0 = reinterpret_cast<const uint4*>(at + 1024)[lane];
-  p.c1 = reinterpret_cast<const uint4*>(at + 1024)[32 + lane];
-  const char* meta = at + 2048 + lane * 4 * lv.VG;
-  p.meta = make_uint4(0u, 0u, 0u, 0u);
+__device__ __forceinline__ Packed request_values(const LayerView& lv, const char* base, uint32_t inv_u, int unit, int half, int lane) {
+  Packed p{};
+  const int bi = block_of(unit, inv_u), u = unit - bi * lv.U;
+  const char* at = base + (size_t)bi * lv.base_bytes + (uint32_t)u * lv.unit_bytes + 512u * (((uint32_t)u >> group_shift(lv)) + 1);
+  p.c = reinterpret_cast<const uint4*>(at + 1024)[32 * half + lane];
+  // the scales of the half's two groups of 32 channels (the same one twice where a group is wider)
   if (lv.VG == 4) {
-    p.meta = *reinterpret_cast<const uint4*>(meta);
-  } else if (lv.VG == 2) {
-    const uint2 m = *reinterpret_cast<const uint2*>(meta);
+    const uint2 m = reinterpret_cast<const uint2*>(at + 2048)[2 * lane + half];
     p.meta.x = m.x;
     p.meta.y = m.y;
   } else {
-    p.meta.x = *reinterpret_cast<const uint32_t*>(meta);
+    p.meta.x = p.meta.y = reinterpret_cast<const uint32_t*>(at + 2048)[lv.VG == 2 ? 2 * lane + half : lane];
   }
-  if (kV4) {
-    const uint4* hi = reinterpret_cast<const uint4*>(at + 2048 + 128 * lv.VG);
-    p.h0 = hi[lane];
-    p.h1 = hi[32 + lane];
-  }
+  if (kV4) p.h = reinterpret_cast<const uint4*>(at + 2048 + 128 * lv.VG)[32 * half + lane];
   return p;
 }
 
 template <bool kV4>
-__device__ __forceinline__ void make_values(const LayerView& lv, const Packed& p, uint32_t tile, uint32_t scratch, int w, int lane) {
-  // scales of tokens (8 o + 2 t, + 1) as fp16 pairs: word 16 vg + 4 t + o, zero-points 64 words on; the lane has token 8 o + 2 t + e = lane
+__device__ __forceinline__ void make_values(const Packed& p, uint32_t tile, uint32_t scratch, int w, int half, int lane) {
+  // scales of tokens (8 o + 2 t, + 1) as fp16 pairs: word 16 i + 4 t + o for 32 channels i, zero-points 32 words on; the lane has token
+  // 8 o + 2 t + e = lane
   {
-    const uint32_t m[4] = {p.meta.x, p.meta.y, p.meta.z, p.meta.w};
     const uint32_t at = scratch + 4 * (4 * ((lane >> 1) & 3) + (lane >> 3)) + 2 * (lane & 1);
-#pragma unroll
-    for (int vg = 0; vg < 4; ++vg)
-      if (vg < lv.VG) {
-        const uint32_t h = bf16x2_to_f16x2(m[vg]);
-        sts16(at + 64 * vg, h & 0xFFFFu);
-        sts16(at + 64 * vg + 256, h >> 16);
-      }
+    const uint32_t a = bf16x2_to_f16x2(p.meta.x), b = bf16x2_to_f16x2(p.meta.y);
+    sts16(at, a & 0xFFFFu);
+    sts16(at + 128, a >> 16);
+    sts16(at + 64, b & 0xFFFFu);
+    sts16(at + 192, b >> 16);
   }
   __syncwarp();
-  const uint32_t c[8] = {p.c0.x, p.c0.y, p.c0.z, p.c0.w, p.c1.x, p.c1.y, p.c1.z, p.c1.w};
-  const uint32_t h[8] = {p.h0.x, p.h0.y, p.h0.z, p.h0.w, p.h1.x, p.h1.y, p.h1.z, p.h1.w};
-  const uint32_t out = tile + 4 * w * 128 + 4 * lane;
-  const int lg = lv.VG == 4 ? 1 : lv.VG == 2 ? 2 : 3;        // a value group has 2^lg pieces of 16 channels
-  uint4 s4 = make_uint4(0u, 0u, 0u, 0u), z4 = s4;
-#pragma unroll
-  for (int ct = 0; ct < 8; ++ct) {
-    if ((ct & ((1 << lg) - 1)) == 0) {
-      const uint32_t at = scratch + 64 * (ct >> lg) + 16 * (lane & 3);
-      s4 = lds128(at);
-      z4 = lds128(at + 256);
-    }
+  uint32_t c0 = p.c.x, c1 = p.c.y, h0 = p.h.x, h1 = p.h.y;
+  uint32_t to = tile + half * 8 * 2048 + 4 * w * 128 + 4 * lane, at = scratch + 16 * (lane & 3);
+#pragma unroll 1
+  for (int i = 0; i < 2; ++i) {          // 32 channels
+    const uint4 s4 = lds128(at), z4 = lds128(at + 128);
     const uint32_t s[4] = {s4.x, s4.y, s4.z, s4.w}, z[4] = {z4.x, z4.y, z4.z, z4.w};
 #pragma unroll
-    for (int rh = 0; rh < 2; ++rh)
+    for (int f = 0; f < 8; ++f)
+      sts32(to + (f >> 2) * 2048 + (f & 3) * 128, hfma2_u(kV4 ? codes4(c0, h0, f) : codes2(c0, f), s[f & 3], z[f & 3]));
 #pragma unroll
-      for (int o = 0; o < 4; ++o)
-        sts32(out + (2 * ct + rh) * 2048 + o * 128, hfma2_u(kV4 ? codes4(c[ct], h[ct], 4 * rh + o) : codes2(c[ct], 4 * rh + o), s[o], z[o]));
+    for (int f = 0; f < 8; ++f)
+      sts32(to + (2 + (f >> 2)) * 2048 + (f & 3) * 128, hfma2_u(kV4 ? codes4(c1, h1, f) : codes2(c1, f), s[f & 3], z[f & 3]));
+    c0 = p.c.z;
+    c1 = p.c.w;
+    h0 = p.h.z;
+    h1 = p.h.w;
+    to += 4 * 2048;
+    at += 64;
   }
 }
 
-// Unquantized rows 128 t + 32 w .. + 31: keys K-major, values as they lie (MN-major); rows past the last are zeros.
-__device__ __forceinline__ void copy_key_rows(const Stream& x, int t, uint32_t tile, int w, int lane) {
-  uint4 y[16];
+// Unquantized rows of tail tile t, rows past the last as zeros.  Keys K-major, warp (w, mt) rows 32 w + 16 mt .. + 15; values as they lie
+// (MN-major), warp (w, half) rows 32 w .. + 31 of channels 64 half .. + 63.
+__device__ __forceinline__ void copy_key_rows(const Rows& x, int t, uint32_t tile, int w, int mt, int lane) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int row = kTile * t + 32 * w + 8 * (i & 3) + (lane & 7);
-    y[i] = make_uint4(0u, 0u, 0u, 0u);
-    if (row < x.total) y[i] = reinterpret_cast<const uint4*>(tail_row(x.resk, x.sinkk, x.newk, x, row))[4 * (i >> 2) + (lane >> 3)];
+  for (int c = 0; c < 4; c += 2) {       // (all at once took more registers than the warps have)
+    uint4 y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = kTile * t + 32 * w + 16 * mt + 8 * (i & 1) + (lane & 7);
+      y[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (row < x.total) y[i] = x.row(row)[4 * (c + (i >> 1)) + (lane >> 3)];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      sts128(tile + (4 * w + 2 * mt + (i & 1)) * 2048 + (4 * (c + (i >> 1)) + (lane >> 3)) * 128 + (lane & 7) * 16, rows_to_half(y[i]));
   }
-#pragma unroll
-  for (int i = 0; i < 16; ++i)
-    sts128(tile + (4 * w + (i & 3)) * 2048 + (4 * (i >> 2) + (lane >> 3)) * 128 + (lane & 7) * 16, rows_to_half(y[i]));
 }
-__device__ __forceinline__ void copy_value_rows(const Stream& x, int t, uint32_t tile, int w, int lane) {
+__device__ __forceinline__ void copy_value_rows(const Rows& x, int t, uint32_t tile, int w, int half, int lane) {
   const int row = kTile * t + 32 * w + lane;
-  const uint4* src = row < x.total ? reinterpret_cast<const uint4*>(tail_row(x.resv, x.sinkv, x.newv, x, row)) : nullptr;
-  uint4 y[16];
+  const uint4* src = row < x.total ? x.row(row) + 8 * half : nullptr;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) y[i] = src != nullptr ? src[i] : make_uint4(0u, 0u, 0u, 0u);
+  for (int c = 0; c < 8; c += 4) {
+    uint4 y[4];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) sts128(tile + i * 2048 + (4 * w + (lane >> 3)) * 128 + (lane & 7) * 16, rows_to_half(y[i]));
+    for (int i = 0; i < 4; ++i) y[i] = src != nullptr ? src[c + i] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sts128(tile + (8 * half + c + i) * 2048 + (4 * w + (lane >> 3)) * 128 + (lane & 7) * 16, rows_to_half(y[i]));
+  }
 }
 
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&u)[32]) {
+__device__ __forceinline__ void tmem_ld32_issue(uint32_t taddr, uint32_t (&u)[32]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,"
       "%27,%28,%29,%30,%31}, [%32];"
@@ -320,6 +328,8 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&u)[32]) {
         "=r"(u[21]), "=r"(u[22]), "=r"(u[23]), "=r"(u[24]), "=r"(u[25]), "=r"(u[26]), "=r"(u[27]), "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
       : "r"(taddr)
       : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld32(uint32_t (&u)[32]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;"
                : "+r"(u[0]), "+r"(u[1]), "+r"(u[2]), "+r"(u[3]), "+r"(u[4]), "+r"(u[5]), "+r"(u[6]), "+r"(u[7]), "+r"(u[8]), "+r"(u[9]),
                  "+r"(u[10]), "+r"(u[11]), "+r"(u[12]), "+r"(u[13]), "+r"(u[14]), "+r"(u[15]), "+r"(u[16]), "+r"(u[17]), "+r"(u[18]), "+r"(u[19]),
@@ -328,68 +338,107 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&u)[32]) {
                :
                : "memory");
 }
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&u)[32]) {
+  tmem_ld32_issue(taddr, u);
+  tmem_wait_ld32(u);
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&w)[16]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr), "r"(w[0]),
+               "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]), "r"(w[8]), "r"(w[9]), "r"(w[10]), "r"(w[11]), "r"(w[12]),
+               "r"(w[13]), "r"(w[14]), "r"(w[15])
+               : "memory");
+}
 
-// One tile of one slot's softmax: the thread's row of S (128 fp32 at s_addr) becomes P (fp16 pairs over the first 64 of those columns).  kMask: the row
-// sees the columns <= last only.
-template <bool kMask>
-__device__ __forceinline__ void softmax_tile(uint32_t s_addr, uint32_t o_addr, int last, bool first, float scale_log2e, float& m_ref, float& l_run) {
-  float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-  for_pieces<true>(s_addr, 8, [&](int h, const uint32_t (&u)[16]) {
-    const int lim = last - 16 * h;
-#pragma unroll
-    for (int i = 0; i < 16; i += 2) {
-      const float x0 = kMask && i > lim ? -INFINITY : __uint_as_float(u[i]);
-      const float x1 = kMask && i + 1 > lim ? -INFINITY : __uint_as_float(u[i + 1]);
-      mx4[(i >> 1) & 3] = fmaxf(fmaxf(mx4[(i >> 1) & 3], x0), x1);
-    }
-  });
-  const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * scale_log2e;
-  if (first) {
-    m_ref = mx;
-  } else if (__any_sync(0xffffffffu, mx > m_ref + kRaise)) {
-    // (the products before this tile are complete: S is behind them in the tensor core's order)
-    const float m_new = fmaxf(m_ref, mx), alpha = m_new == -INFINITY ? 1.f : ex2(m_ref - m_new);
-#pragma unroll
+// The state of a row's softmax: its reference (in the log2 domain) and the sum of its probabilities, two halves.
+struct RowState {
+  float m;
+  uint64_t l;
+  __device__ __forceinline__ float sum() const {
+    float a, b;
+    unpack2(l, a, b);
+    return a + b;
+  }
+};
+
+// Raises the reference to at least mx: what lies in tensor memory on the old one is rescaled, the sums at o_addr (unless they are the first tile's, which
+// are not there yet) and `written` pieces of P at s_addr.  The products before this tile are complete: S is behind them in the tensor core's order.
+__device__ __forceinline__ void raise(uint32_t s_addr, uint32_t o_addr, int from, int written, bool first, float mx, RowState& row) {
+  const float m_new = fmaxf(row.m, mx), alpha = m_new == -INFINITY ? 1.f : ex2(row.m - m_new);
+  row.l = mul2(row.l, pack2(alpha, alpha));
+  row.m = m_new;
+  if (!first) {
+#pragma unroll 1
     for (int d = 0; d < kD; d += 16) {
       uint32_t u[16];
       tmem_ld16_issue(o_addr + d, u);
       tmem_wait_ld16(u);
-      uint32_t a[8], b[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        a[i] = __float_as_uint(__uint_as_float(u[i]) * alpha);
-        b[i] = __float_as_uint(__uint_as_float(u[8 + i]) * alpha);
-      }
-      tmem_st8(o_addr + d, a);
-      tmem_st8(o_addr + d + 8, b);
+      for (int i = 0; i < 16; ++i) u[i] = __float_as_uint(__uint_as_float(u[i]) * alpha);
+      tmem_st16(o_addr + d, u);
     }
-    l_run *= alpha;
-    m_ref = m_new;
   }
-  const float ref = m_ref == -INFINITY ? 0.f : m_ref;          // a row that has seen no key yet: all its logits are -inf, its P is 0
-  const uint64_t scale2 = pack2(scale_log2e, scale_log2e), ref2 = pack2(-ref, -ref);
-  uint64_t sum[2] = {0ull, 0ull};
-  for_pieces<true>(s_addr, 8, [&](int h, const uint32_t (&u)[16]) {
-    uint32_t wd[8];
-    const int lim = last - 16 * h;
+  const __half2 a2 = __float2half2_rn(alpha);
+#pragma unroll 1
+  for (int h = from; h < written; ++h) {
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+    uint32_t u[16];
+    tmem_ld16_issue(s_addr + 16 * h, u);
+    tmem_wait_ld16(u);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 16; ++i) {
+      const __half2 p = __hmul2(*reinterpret_cast<const __half2*>(&u[i]), a2);
+      u[i] = *reinterpret_cast<const uint32_t*>(&p);
+    }
+    tmem_st16(s_addr + 16 * h, u);
+  }
+}
+
+// One tile of one slot's softmax, in one pass: the thread's row of S (128 fp32 at s_addr) becomes P (fp16 pairs over the first 64 of those columns), 32
+// columns at a time.  Piece h of P lies inside the columns of S's pieces <= h.  The reference is raised only when a piece's
+// largest logit exceeds it by more than 2^kRaise: P stays below 2^10, far inside fp16, and that is rare behind the first tile.  The row's own pieces are
+// h0 .. h1 - 1 (another lane has the same row's others); P is zero in the others.  kMask: the row sees the columns <= last only.
+template <bool kMask>
+__device__ __forceinline__ void softmax_tile(uint32_t s_addr, uint32_t o_addr, int h0, int h1, int last, bool first, float scale_log2e, RowState& row) {
+  const uint64_t scale2 = pack2(scale_log2e, scale_log2e);
+  auto piece = [&](uint32_t (&u)[32], int h) {
+    const int lim = last - 32 * h;
+    float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) {
+      if (kMask) {
+        u[i] = i > lim ? 0xFF800000u : u[i];
+        u[i + 1] = i + 1 > lim ? 0xFF800000u : u[i + 1];
+      }
+      mx4[(i >> 1) & 3] = fmaxf(fmaxf(mx4[(i >> 1) & 3], __uint_as_float(u[i])), __uint_as_float(u[i + 1]));
+    }
+    const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * scale_log2e;
+    if (__any_sync(0xffffffffu, mx > row.m + kRaise)) raise(s_addr, o_addr, h0, h, first, mx, row);
+    const float ref = row.m == -INFINITY ? 0.f : row.m;        // a row that has seen no key yet: all its logits are -inf, its P is 0
+    const uint64_t ref2 = pack2(-ref, -ref);
+    uint32_t wd[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
       float x0, x1;
       unpack2(fma2(pack2u(u[2 * i], u[2 * i + 1]), scale2, ref2), x0, x1);
-      float p0 = ex2(x0), p1 = ex2(x1);
-      if constexpr (kMask) {
-        p0 = 2 * i <= lim ? p0 : 0.f;
-        p1 = 2 * i + 1 <= lim ? p1 : 0.f;
-      }
-      sum[i & 1] = add2(sum[i & 1], pack2(p0, p1));
+      const float p0 = ex2(x0), p1 = ex2(x1);
+      row.l = add2(row.l, pack2(p0, p1));
       wd[i] = pack_half2(p0, p1);
     }
-    tmem_st8(s_addr + 8 * h, wd);
-  });
+    tmem_st16(s_addr + 16 * h, wd);
+  };
+#pragma unroll 1
+  for (int h = h0; h < h1; ++h) {
+    uint32_t u[32];
+    tmem_ld32(s_addr + 32 * h, u);
+    piece(u, h);
+  }
+  if (h1 - h0 < 4) {
+    const uint32_t zero[16] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+#pragma unroll 1
+    for (int h = 0; h < 4; ++h)
+      if (h < h0 || h >= h1) tmem_st16(s_addr + 16 * h, zero);
+  }
   asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-  float s0, s1;
-  unpack2(add2(sum[0], sum[1]), s0, s1);
-  l_run += s0 + s1;
 }
 
 // 32 channels of an output row
@@ -413,22 +462,63 @@ __device__ __forceinline__ void store_row(const ChunkArgs& a, size_t row, int d,
   }
 }
 
+// What the roles need to know of a segment (a thread block's key tiles of one item); stream < 0: there is none left.
+struct Segment {
+  int stream, j0, j1, packed_tiles;
+  int units, r, c0, total;               // packed units; residual rows; residual and sink rows; unquantized rows that the item's rows may see
+  int row0, rows_all, dual, whole;       // first row; rows of the stream; more than 128 rows; all of the item's key tiles
+  int part, pad[3];                      // which of the thread block's two results
+};
+
+// the first lane's value, the whole warp's
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
+__device__ __forceinline__ bool elect_one() {
+  uint32_t e;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+  return e != 0;
+}
+
+// `ok` of all softmax threads: none goes on alone, and so none waits alone in the barriers that they share
+__device__ __forceinline__ bool softmax_all(bool ok) {
+  uint32_t all;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+               : "=r"(all)
+               : "r"((uint32_t)ok)
+               : "memory");
+  return all != 0;
+}
+__device__ __forceinline__ void softmax_sync() { asm volatile("barrier.cta.sync 1, 256;" ::: "memory"); }
+
+// 4 channels of an output row
+__device__ __forceinline__ void store4(const ChunkArgs& a, size_t at, float4 y) {
+  if (a.out_bf16) {
+    const __nv_bfloat162 p0 = __floats2bfloat162_rn(y.x, y.y), p1 = __floats2bfloat162_rn(y.z, y.w);
+    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + at) =
+        make_uint2(*reinterpret_cast<const uint32_t*>(&p0), *reinterpret_cast<const uint32_t*>(&p1));
+  } else {
+    *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at) = y;
+  }
+}
+
 template <bool kDense, bool kV4>
 __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __grid_constant__ LayerView lv, const __grid_constant__ ChunkArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
   const uint32_t sbase = smem_u32(smem), qs = sbase, ks = sbase + 2 * kTileBytes, vs = sbase + 4 * kTileBytes;
   auto bar = [&](int i) { return sbase + (uint32_t)kBarOff + 8u * (uint32_t)i; };
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + kBarOff + 8 * kBars);
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lv.g;
-  const long long begin = chunk_begin(a.total, a.ctas, blockIdx.x), end = chunk_begin(a.total, a.ctas, blockIdx.x + 1);
+  volatile int* progress = reinterpret_cast<volatile int*>(tmem_slot + 1);     // the tile that the producers are at
+  Segment* segments = reinterpret_cast<Segment*>(smem + kSegOff);              // two places
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
-  if (warp == 16) {
+  if (warp == kIssueWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   if (tid == 0) {
     for (int i = 0; i < kBars; ++i)
-      mbar_init(bar(i), i == kQFull ? kSoftmaxThreads : (i >= kKFull && i < kKEmpty) ? 4 : (i >= kPReady && i < kODone) ? kTile : 1);
+      mbar_init(bar(i), i == kQFull ? kSoftmaxThreads : (i >= kKFull && i < kKEmpty) ? 8 : (i >= kPReady && i < kODone) ? kTile : i >= kSegEmpty ? kReaders : 1);
+    *progress = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   tc_fence_before();
@@ -439,59 +529,70 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
   // tensor-memory columns: S / P of slot 0 at 0, of slot 1 at 128, O of slot 0 at 256, of slot 1 at 384
   bool dead = false;
   auto wait = [&](int i, uint32_t parity) {
-    if (!dead && !mbar_wait_polls(bar(i), parity, a.max_polls)) {
+    if (!dead && !wait_phase(bar(i), parity, a.max_polls)) {
       dead = true;
       atomicOr(lv.status, (uint32_t)MIXKVQ_DEV_COPY_TIMEOUT);
     }
     return !dead;
   };
-  // walks the thread block's segments: f(item, first key tile, key tiles behind the last)
-  auto for_segments = [&](auto f) {
-    if (begin >= end) return;
-    ChunkItem it = chunk_locate(a, lv.B, lv.Hkv, g, begin);
-    for (;;) {
-      int j0, j1;
-      chunk_tiles(it, begin, end, j0, j1);
-      if (j0 < j1) f(it, j0, j1);
-      if (it.x0 + (long long)it.weight * it.kt >= end) break;
-      chunk_next(a, lv.Hkv, g, it);
-    }
+  // the n-th segment is there; (a reader's warp has taken what it needs)
+  auto segment_there = [&](int n) { return wait(kSegFull + (n & 1), (uint32_t)(n >> 1) & 1u); };
+  auto segment_taken = [&](int n) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar(kSegEmpty + (n & 1)));
   };
 
-  if (warp >= 16) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 32;" ::: "memory");
-    if (warp == 16 && lane == 0) {
+  if (warp >= kIssueWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;" ::: "memory");
+    if (warp == kIssueWarp) {
       // ---------------------------------------------------------------- tensor-core issue
-      const uint32_t idesc_s = make_idesc(128, 128, 0, 0), idesc_packed = make_idesc(128, 128, 0, 0), idesc_rows = make_idesc(128, 128, 0, 1);
-      int tile0 = 0, seg = 0, cnt[2] = {0, 0};           // key tiles and segments before this one; steps per slot
-      for_segments([&](const ChunkItem& it, int j0, int j1) {
-        if (dead) return;
-        const bool dual = it.weight == 2;
-        const int nt = j1 - j0, steps = dual ? 2 * nt : nt;
-        if (!wait(kQFull, seg & 1)) return;
+      // (The whole warp goes through the loop and one lane issues: with one lane alone in here every descriptor is moved to the uniform registers word by
+      // word in front of its instruction.)
+      constexpr uint32_t kIdesc = make_idesc(128, 128, 0, 0), kIdescRows = make_idesc(128, 128, 0, 1);
+      const uint32_t tb = uniform(tbase), sb = uniform(sbase);
+      const uint64_t qd = make_desc(sb, 128, 2048), kd = make_desc(sb + 2 * kTileBytes, 128, 2048), vd = make_desc(sb + 4 * kTileBytes, 128, 2048);
+      constexpr uint64_t kStep = kTileBytes >> 4;        // a tile further, in a descriptor
+      const bool leader = elect_one();
+      auto there = [&](int i, uint32_t parity) { return __all_sync(0xffffffffu, wait(i, parity)) != 0; };
+      auto commit = [&](int i) {
+        if (leader) tc_commit(bar(i));
+      };
+      int tile0 = 0, cnt[2] = {0, 0};                    // key tiles before the segment; steps per slot
+      for (int n = 0; there(kSegFull + (n & 1), (uint32_t)(n >> 1) & 1u); ++n) {
+        const Segment& sg = segments[n & 1];
+        const int stream = uniform(sg.stream), nt = uniform(sg.j1 - sg.j0), packed = uniform(sg.packed_tiles - sg.j0), sh = uniform(sg.dual);
+        segment_taken(n);
+        if (stream < 0 || !there(kQFull, n & 1)) break;
         tc_fence_after();
+        const int steps = nt << sh;                      // step u: slot u % 2, key tile u (more than 128 rows: u / 2) of the segment
         auto issue_s = [&](int u) {
-          const int slot = u & 1, kc = tile0 + (dual ? u >> 1 : u), st = kc & 1;
-          if (!wait(kKFull + st, (kc >> 1) & 1)) return false;
+          const int slot = u & 1, kc = tile0 + (u >> sh), st = kc & 1;
+          if (!there(kKFull + st, (uint32_t)(kc >> 1) & 1u)) return false;
           tc_fence_after();
-          const uint64_t qd = make_desc(qs + (dual ? slot : 0) * kTileBytes, 128, 2048), kd = make_desc(ks + st * kTileBytes, 128, 2048);
+          const uint64_t q = qd + (sh & slot ? kStep : 0), k = kd + (st ? kStep : 0);
+          const uint32_t d = tb + 128 * slot;
+          if (leader) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) tc_mma_ss(tbase + 128 * slot, qd + (uint64_t)(16 * i), kd + (uint64_t)(16 * i), idesc_s, i > 0);
-          tc_commit(bar(kSFull + slot));
-          if (!dual || slot == 1) tc_commit(bar(kKEmpty + st));
+            for (int i = 0; i < 8; ++i) tc_mma_ss(d, q + (uint64_t)(16 * i), k + (uint64_t)(16 * i), kIdesc, i > 0);
+          }
+          commit(kSFull + slot);
+          if (sh <= slot) commit(kKEmpty + st);
           return true;
         };
         auto issue_o = [&](int u) {
-          const int slot = u & 1, j = dual ? u >> 1 : u, kc = tile0 + j, st = kc & 1;
-          if (!wait(kVFull + st, (kc >> 1) & 1) || !wait(kPReady + slot, cnt[slot] & 1)) return false;
+          const int slot = u & 1, j = u >> sh, kc = tile0 + j, st = kc & 1;
+          if (!there(kVFull + st, (uint32_t)(kc >> 1) & 1u) || !there(kPReady + slot, (uint32_t)cnt[slot] & 1u)) return false;
           cnt[slot] += 1;
           tc_fence_after();
-          const uint64_t vd = make_desc(vs + st * kTileBytes, 128, 2048);
-          const uint32_t idesc = j0 + j < it.packed_tiles ? idesc_packed : idesc_rows, o = tbase + 256 + 128 * slot, p = tbase + 128 * slot;
+          const uint64_t v = vd + (st ? kStep : 0);
+          const uint32_t o = tb + 256 + 128 * slot, p = tb + 128 * slot, idesc = j < packed ? kIdesc : kIdescRows;
+          if (leader) {
+            tc_mma_ts(o, p, v, idesc, u > 1);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) tc_mma_ts(o, p + 8 * i, vd + (uint64_t)(16 * i), idesc, u > 1 || i > 0);
-          if (!dual || slot == 1) tc_commit(bar(kVEmpty + st));
-          if (u + 2 >= steps) tc_commit(bar(kODone + slot));
+            for (int i = 1; i < 8; ++i) tc_mma_ts(o, p + 8 * i, v + (uint64_t)(16 * i), idesc, 1);
+          }
+          if (sh <= slot) commit(kVEmpty + st);
+          if (u + 2 >= steps) commit(kODone + slot);
           return true;
         };
         bool ok = issue_s(0);
@@ -501,89 +602,208 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
           if (ok && u + 2 < steps) ok = issue_s(u + 2);
         }
         tile0 += nt;
-        seg += 1;
-      });
-      tc_commit(bar(kDone));                             // every product issued above has finished when this one fires
+      }
+      commit(kDone);                                     // every product issued above has finished when this one fires
       dead = false;
-      wait(kDone, 0);
+      there(kDone, 0);
+    } else if (warp == kIssueWarp + 1 && lane == 0) {
+      // ---------------------------------------------------------------- the thread block's segments
+      const int g = lv.g;
+      const long long begin = chunk_begin(a.total, a.ctas, blockIdx.x), end = chunk_begin(a.total, a.ctas, blockIdx.x + 1);
+      int n = 0;
+      auto publish = [&](const Segment& sg) {
+        if (n >= 2 && !wait(kSegEmpty + (n & 1), (uint32_t)((n >> 1) - 1) & 1u)) return false;
+        segments[n & 1] = sg;
+        mbar_arrive(bar(kSegFull + (n & 1)));
+        n += 1;
+        return true;
+      };
+      bool ok = true;
+      if (begin < end) {
+        ChunkItem it = chunk_locate(a, lv.B, lv.Hkv, g, begin);
+        for (;;) {
+          Segment sg;
+          chunk_tiles(it, begin, end, sg.j0, sg.j1);
+          if (sg.j0 < sg.j1) {
+            const ChunkSeq sq = a.seq[it.b];
+            sg.stream = it.b * lv.Hkv + it.hk;
+            sg.packed_tiles = it.packed_tiles;
+            sg.units = sq.units;
+            sg.r = sq.tail & 0xFFFF;
+            sg.c0 = chunk_tail_rows(sq);
+            sg.total = sg.c0 + sq.n;
+            sg.row0 = kChunkRows * it.rt;
+            sg.rows_all = sq.n * g;
+            sg.dual = it.weight - 1;
+            sg.whole = sg.j0 == 0 && sg.j1 == it.kt;
+            sg.part = it.x0 <= begin ? 0 : 1;
+            ok = publish(sg);
+          }
+          if (!ok || it.x0 + (long long)it.weight * it.kt >= end) break;
+          chunk_next(a, lv.Hkv, g, it);
+        }
+      }
+      if (ok) {
+        Segment none{};
+        none.stream = -1;
+        publish(none);
+      }
+    } else if (warp == kIssueWarp + 2) {
+      // ---------------------------------------------------------------- requests into L2
+      // The producers load one tile ahead, which is less than a round trip to memory: what they will load goes to L2 kAhead tiles before.  Lanes 0 .. 3
+      // the units of a tile, lanes 4 .. 7 their blocks' promoted channels.
+      int kc = 0;
+      for (int n = 0; segment_there(n); ++n) {
+        const Segment& sg = segments[n & 1];
+        const int stream = sg.stream, j0 = sg.j0, j1 = min(sg.j1, sg.packed_tiles), nt = sg.j1 - j0, units = sg.units;
+        segment_taken(n);
+        if (stream < 0) break;
+        const uint32_t inv_u = inverse_units(lv);
+        for (int j = j0; j < j1; ++j) {
+          // (a bounded wait, and nothing depends on it)
+          for (int i = 0; i < 100 && *progress + kAhead < kc + j - j0; ++i) __nanosleep(200);
+          const int unit = 4 * j + (lane & 3);
+          if (lane >= 8 || unit >= units) continue;
+          const int bi = block_of(unit, inv_u), u = unit - bi * lv.U;
+          if (lane < 4) {
+            prefetch_bulk(lv.base + (size_t)stream * lv.base_stride + (size_t)bi * lv.base_bytes + (uint32_t)u * lv.unit_bytes +
+                              512u * ((uint32_t)u >> group_shift(lv)),
+                          lv.unit_bytes + 512);
+          } else {
+            const uint2 e = reinterpret_cast<const uint2*>(lv.table + (size_t)stream * lv.table_stride)[bi];
+            const int n16 = e.y & 0xFF, n4 = (e.y >> 8) & 0xFF;
+            const uint32_t bytes = extras_unit_bytes(n16, n4, kDense);                 // (a multiple of 16)
+            if (n16 + n4 > 0)
+              prefetch_bulk(lv.extras + (size_t)stream * lv.extras_stride + (size_t)e.x * 16 + extras_header_bytes(n16, n4) + (size_t)u * bytes, bytes);
+          }
+        }
+        kc += nt;
+      }
+    }
+  } else if (warp >= 16) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;" ::: "memory");
+    // ------------------------------------------------------------------ value tiles
+    const int w = (warp >> 1) & 3, half = warp & 1;
+    const uint32_t scratch = sbase + kScratchOff + (warp - 8) * 512, inv_u = inverse_units(lv);
+    int kc = 0;
+    auto stage = [&]() { return vs + (kc & 1) * kTileBytes; };
+    auto free_stage = [&]() { return kc < 2 || wait(kVEmpty + (kc & 1), (uint32_t)((kc >> 1) - 1) & 1u); };
+    auto made = [&]() {
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(kVFull + (kc & 1)));
+      ++kc;
+    };
+    for (int n = 0; segment_there(n); ++n) {
+      const Segment& sg = segments[n & 1];
+      const int stream = sg.stream, j1 = sg.j1, packed_tiles = sg.packed_tiles, units = sg.units, r = sg.r, c0 = sg.c0, total = sg.total;
+      int j = sg.j0;
+      segment_taken(n);
+      if (stream < 0) break;
+      const char* base = lv.base + (size_t)stream * lv.base_stride;
+      auto request = [&](int unit) { return request_values<kV4>(lv, base, inv_u, min(unit, units - 1), half, lane); };
+      const int end = min(j1, packed_tiles);
+      if (j < end) {
+        Packed p = request(4 * j + w);
+        for (; j < end; ++j) {
+          if (!free_stage()) break;
+          if (4 * j + w < units) {
+            make_values<kV4>(p, stage(), scratch, w, half, lane);
+          } else {
+            // past the last block: the probabilities are zeros, and so must the values be (a NaN from earlier contents would survive the product)
+            for (int i = lane; i < 8 * 32; i += 32)
+              sts128(stage() + (8 * half + (i >> 5)) * 2048 + (4 * w) * 128 + (i & 31) * 16, make_uint4(0u, 0u, 0u, 0u));
+          }
+          p = request(4 * j + 4 + w);
+          made();
+        }
+      }
+      for (; j < j1 && !dead; ++j) {
+        const Rows x{reinterpret_cast<const uint16_t*>(lv.resv + (size_t)stream * lv.resv_stride),
+                     reinterpret_cast<const uint16_t*>(lv.sink + (size_t)stream * lv.sink_stride) + (size_t)lv.sink_len * kD,
+                     a.v + (size_t)stream * a.stride * kD, r, c0, total};
+        if (!free_stage()) break;
+        copy_value_rows(x, j - packed_tiles, stage(), w, half, lane);
+        made();
+      }
+      if (dead) break;
     }
   } else if (warp >= 8) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 112;" ::: "memory");
-    // ------------------------------------------------------------------ key and value tiles
-    const bool keys = warp < 12;
-    const int w = warp & 3;
-    const uint32_t scratch = sbase + kScratchOff + (warp - 8) * 1024, tiles = keys ? ks : vs;
-    const int full = keys ? kKFull : kVFull, empty = keys ? kKEmpty : kVEmpty;
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;" ::: "memory");
+    // ------------------------------------------------------------------ key tiles
+    const int w = (warp >> 1) & 3, mt = warp & 1;
+    const uint32_t scratch = sbase + kScratchOff + (warp - 8) * 512, inv_u = inverse_units(lv);
     int kc = 0;
-    for_segments([&](const ChunkItem& it, int j0, int j1) {
-      if (dead) return;
-      const Stream x = stream_of(lv, a, it);
-      auto entry_of = [&](int j) {
-        const int unit = 4 * j + w;
-        return j < it.packed_tiles && unit < x.units ? *reinterpret_cast<const uint2*>(x.table + 2 * (unit / lv.U)) : make_uint2(0u, 0u);
-      };
-      auto request = [&](int j, uint2 entry) {
-        const int unit = 4 * j + w;
-        Packed p{};
-        if (j < it.packed_tiles && unit < x.units) p = keys ? request_keys<kDense>(lv, x, unit, entry, lane) : request_values<kV4>(lv, x, unit, lane);
-        return p;
-      };
-      uint2 entry = make_uint2(0u, 0u), entry_next = entry;
-      if (keys) {
-        entry = entry_of(j0);
-        entry_next = j0 + 1 < j1 ? entry_of(j0 + 1) : entry;
-      }
-      Packed next = request(j0, entry);
-      for (int j = j0; j < j1; ++j, ++kc) {
-        const Packed cur = next;
-        const uint2 entry_cur = entry;
-        entry = entry_next;
-        if (j + 1 < j1) next = request(j + 1, entry);
-        if (keys && j + 2 < j1) entry_next = entry_of(j + 2);
-        const int st = kc & 1;
-        const uint32_t tile = tiles + st * kTileBytes;
-        if (kc >= 2 && !wait(empty + st, ((kc >> 1) - 1) & 1)) return;
-        if (j >= it.packed_tiles) {
-          if (keys)
-            copy_key_rows(x, j - it.packed_tiles, tile, w, lane);
-          else
-            copy_value_rows(x, j - it.packed_tiles, tile, w, lane);
-        } else if (4 * j + w < x.units) {
-          if (keys)
-            make_keys<kDense>(lv, x, cur, 4 * j + w, entry_cur, tile, scratch, w, lane);
-          else
-            make_values<kV4>(lv, cur, tile, scratch, w, lane);
-        } else if (!keys) {
-          // past the last block: the probabilities are zeros, and so must the values be (a NaN from earlier contents would survive the product)
-          for (int i = lane; i < 16 * 32; i += 32) sts128(tile + (i >> 5) * 2048 + (4 * w) * 128 + (i & 31) * 16, make_uint4(0u, 0u, 0u, 0u));
+    auto stage = [&]() { return ks + (kc & 1) * kTileBytes; };
+    auto free_stage = [&]() { return kc < 2 || wait(kKEmpty + (kc & 1), (uint32_t)((kc >> 1) - 1) & 1u); };
+    auto made = [&]() {
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0 && !(a.test_silent && kc == 0)) mbar_arrive(bar(kKFull + (kc & 1)));
+      ++kc;
+    };
+    for (int n = 0; segment_there(n); ++n) {
+      const Segment& sg = segments[n & 1];
+      const int stream = sg.stream, j1 = sg.j1, packed_tiles = sg.packed_tiles, units = sg.units, r = sg.r, c0 = sg.c0, total = sg.total;
+      int j = sg.j0;
+      segment_taken(n);
+      if (stream < 0) break;
+      const char *base = lv.base + (size_t)stream * lv.base_stride, *extras = lv.extras + (size_t)stream * lv.extras_stride;
+      const uint2* table = reinterpret_cast<const uint2*>(lv.table + (size_t)stream * lv.table_stride);
+      const int end = min(j1, packed_tiles);
+      auto entry_of = [&](int unit) { return table[block_of(min(unit, units - 1), inv_u)]; };
+      auto request = [&](int unit, uint2 entry) { return request_keys<kDense>(lv, base, extras, inv_u, min(unit, units - 1), entry, mt, lane); };
+      if (j < end) {
+        uint2 entry = entry_of(4 * j + w), entry_next = entry_of(4 * j + 4 + w);
+        Packed p = request(4 * j + w, entry);
+        for (; j < end; ++j) {
+          if (!free_stage()) break;
+          if (warp == 8 && lane == 0) *progress = kc;
+          // (past the last block the logits are masked, whatever the keys are)
+          if (4 * j + w < units) make_keys<kDense>(lv, base, extras, inv_u, p, 4 * j + w, entry, stage(), scratch, w, mt, lane);
+          entry = entry_next;
+          p = request(4 * j + 4 + w, entry);
+          entry_next = entry_of(4 * j + 8 + w);
+          made();
         }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0 && !(a.test_silent && keys && kc == 0)) mbar_arrive(bar(full + st));
       }
-    });
+      for (; j < j1 && !dead; ++j) {
+        const Rows x{reinterpret_cast<const uint16_t*>(lv.resk + (size_t)stream * lv.resk_stride),
+                     reinterpret_cast<const uint16_t*>(lv.sink + (size_t)stream * lv.sink_stride), a.k + (size_t)stream * a.stride * kD, r, c0, total};
+        if (!free_stage()) break;
+        if (warp == 8 && lane == 0) *progress = kc;
+        copy_key_rows(x, j - packed_tiles, stage(), w, mt, lane);
+        made();
+      }
+      if (dead) break;
+    }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 112;" ::: "memory");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 104;" ::: "memory");
     // ------------------------------------------------------------------ softmax and output rows
-    const int slot = warp >> 2, row_in = tid & 127;
+    const int slot = warp >> 2, row_in = tid & 127, g = lv.g;
     const uint32_t lane_base = tbase + ((uint32_t)((warp & 3) * 32) << 16);
     const uint32_t s_addr = lane_base + 128 * slot, o_addr = lane_base + 256 + 128 * slot;
     int cnt = 0, ended[2] = {0, 0};                      // steps of this slot, segments in which a slot had steps
     // (what follows a wait is the whole warp's: tensor-memory loads and stores)
     auto all_wait = [&](int i, uint32_t parity) { return __all_sync(0xffffffffu, wait(i, parity)) != 0; };
-    for_segments([&](const ChunkItem& it, int j0, int j1) {
-      const bool dual = it.weight == 2;
-      const ChunkSeq sq = a.seq[it.b];
-      const int nt = j1 - j0, rows_all = sq.n * g, c0 = chunk_tail_rows(sq);
-      // both slots are behind the segment before: the queries may go, and what slot 1 left there for slot 0
-      asm volatile("bar.sync 1, 256;" ::: "memory");
+    for (int n = 0;; ++n) {
+      // (both slots are behind the segment before: the queries may go, and what slot 1 left there for slot 0)
+      if (!softmax_all(segment_there(n))) break;
+      const Segment& sg = segments[n & 1];
+      const int stream = sg.stream, j0 = sg.j0, j1 = sg.j1, packed_tiles = sg.packed_tiles, units = sg.units, c0 = sg.c0, rows_all = sg.rows_all;
+      const int row0 = sg.row0, dual = sg.dual, whole = sg.whole, part_no = sg.part;
+      segment_taken(n);
+      if (stream < 0) break;
+      // Rows of a tile: with more than 128 rows slot 0 has the first 128 of them and slot 1 the others.  Otherwise both have the same ones, and with at most
+      // 64 (32) every row 2 (4) times over, 64 (32) lanes apart, each copy for a half (a quarter) of the tile's keys: a warp's softmax is that much
+      // shorter, and the copies' results meet at the end like the slots'.
+      const int rows = min(rows_all - row0, kChunkRows), lg_copies = dual || rows > 64 ? 0 : rows > 32 ? 1 : 2, per = kTile >> lg_copies;
       {
-        // 16-byte piece p of the image: row 8 (p / 128) + p % 8, channels 8 (p / 8 % 16) ..
-        const int pieces = dual ? 4096 : 2048;
-        const uint16_t* qb = a.q + ((size_t)it.b * lv.Hq + it.hk * g) * a.stride * kD;
-#pragma unroll 8
-        for (int p = tid; p < pieces; p += kSoftmaxThreads) {
-          const int row = kChunkRows * it.rt + 8 * (p >> 7) + (p & 7), c = (p >> 3) & 15;
+        // 16-byte piece p of the image: lane 8 (p / 128) + p % 8, channels 8 (p / 8 % 16) ..
+        const uint16_t* qb = a.q + (size_t)stream * g * a.stride * kD;
+#pragma unroll 4
+        for (int p = tid; p < 2048 << dual; p += kSoftmaxThreads) {
+          const int at = 8 * (p >> 7) + (p & 7), row = row0 + (dual ? at : at & (per - 1)), c = (p >> 3) & 15;
           uint4 y = make_uint4(0u, 0u, 0u, 0u);
           if (row < rows_all) {
             const int tok = row / g;
@@ -595,106 +815,151 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       tc_fence_before();
       mbar_arrive(bar(kQFull));
-      const int row = kChunkRows * it.rt + (dual ? slot * kTile : 0) + row_in;
+      const int row = row0 + (dual ? slot * kTile + row_in : row_in & (per - 1));
       const int tok = min(row, rows_all - 1) / g;
       const bool idle = (row & ~31) >= rows_all;         // no row of the warp exists
-      float m_ref = -INFINITY, l_run = 0.f;
-      const int stride = dual ? 1 : 2;
-      bool ok = true;
-      for (int j = j0 + (dual ? 0 : slot); j < j1; j += stride, ++cnt) {
-        ok = all_wait(kSFull + slot, cnt & 1);
+      const int h0 = (row_in >> (7 - lg_copies)) << (2 - lg_copies), h1 = h0 + (4 >> lg_copies);
+      RowState state{-INFINITY, 0ull};
+      bool ok = true, first = true;
+      for (int j = j0 + (dual ? 0 : slot); j < j1; j += 2 - dual, ++cnt) {
+        ok = all_wait(kSFull + slot, (uint32_t)cnt & 1u);
         if (!ok) break;
         tc_fence_after();
         if (!idle) {
-          const int last = j < it.packed_tiles ? 32 * (sq.units - 4 * j) - 1 : c0 + tok - kTile * (j - it.packed_tiles);
-          const bool first = j < j0 + stride;
+          const int last = j < packed_tiles ? 32 * (units - 4 * j) - 1 : c0 + tok - kTile * (j - packed_tiles);
           if (__all_sync(0xffffffffu, last >= kTile - 1))
-            softmax_tile<false>(s_addr, o_addr, 0, first, a.scale_log2e, m_ref, l_run);
+            softmax_tile<false>(s_addr, o_addr, h0, h1, 0, first, a.scale_log2e, state);
           else
-            softmax_tile<true>(s_addr, o_addr, last, first, a.scale_log2e, m_ref, l_run);
+            softmax_tile<true>(s_addr, o_addr, h0, h1, last, first, a.scale_log2e, state);
+          first = false;
         }
         tc_fence_before();
         mbar_arrive(bar(kPReady + slot));
       }
       // ---- the segment's result
-      const bool had[2] = {true, dual || nt > 1};
-      const bool whole = j0 == 0 && j1 == it.kt;
-      auto o_ready = [&](int s) { return had[s] && all_wait(kODone + s, ended[s] & 1); };
-      bool mine = o_ready(slot) && ok;
-      const bool apart = dual || !had[1];                // this slot's rows are no other's
-      if (!apart) {
-        mine = o_ready(1 - slot) && mine;                // slot 1's sums go where the queries were: no product may still read them
-        tc_fence_after();
-        // slot 1's row to shared memory: 16-byte piece c of row r at piece c ^ (r % 32)
-        if (slot == 1) {
-          const uint32_t at = qs + row_in * 512;
+      const bool both = dual || j1 - j0 > 1;             // slot 1 had steps (slot 0 has in every segment)
+      bool mine = ok && (slot == 0 || both) && all_wait(kODone + slot, (uint32_t)ended[slot] & 1u);
+      if (!dual && both) mine = all_wait(kODone + 1 - slot, (uint32_t)ended[1 - slot] & 1u) && mine;      // (the sums go where the queries were)
+      tc_fence_after();
+      ended[0] += 1;
+      ended[1] += both;
+      float* part = a.parts + ((size_t)blockIdx.x * 2 + part_no) * a.rows_cap * (kD + 2);
+      const float l_run = mine ? state.sum() : 0.f, m_run = mine ? state.m : -INFINITY;
+      auto weight = [](float m, float l, float top) { return m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : ex2(m - top); };   // (a row of NaNs counts)
+      if (dual) {
+        if (!idle) {
+          const bool exists = row < rows_all;
+          const float inv = whole ? (l_run == 0.f ? 0.f : 1.f / l_run) : l_run == 0.f ? 0.f : 1.f;
+          const size_t orow = ((size_t)stream * g + (row - tok * g)) * a.stride + tok;
+#pragma unroll 1
+          for (int d = 0; d < kD; d += 32) {
+            uint32_t u[32];
+            float y[32];
+            tmem_ld32(o_addr + d, u);
+            if (!exists) continue;
 #pragma unroll
+            for (int i = 0; i < 32; ++i) y[i] = inv == 0.f ? 0.f : __uint_as_float(u[i]) * inv;
+            if (whole) {
+              store_row(a, orow, d, y);
+            } else {
+              float4* dst = reinterpret_cast<float4*>(part + (size_t)(row - row0) * kD + d);
+#pragma unroll
+              for (int i = 0; i < 32; i += 4) dst[i / 4] = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
+            }
+          }
+          if (!whole && exists) reinterpret_cast<float2*>(part + (size_t)a.rows_cap * kD)[row - row0] = make_float2(m_run, l_run);
+        }
+      } else {
+        // Both slots' and all copies' results of a row: slot 1 leaves its lanes' sums in shared memory (16-byte piece c of lane r at piece
+        // c ^ (r % 32)), slot 0 adds its own, then all 256 threads finish rows, 2 << lg_copies threads each.
+        float2* ml = reinterpret_cast<float2*>(smem + kMlOff);
+        const uint32_t at = qs + row_in * 512;
+        auto piece_at = [&](int c) { return at + ((c ^ (row_in & 31)) << 4); };
+        if (slot == 1) {
+          ml[row_in] = make_float2(m_run, l_run);
+          if (!idle && both) {
+#pragma unroll 1
+            for (int d = 0; d < kD; d += 32) {
+              uint32_t u[32];
+              tmem_ld32(o_addr + d, u);
+#pragma unroll
+              for (int i = 0; i < 32; i += 4) sts128(piece_at((d + i) / 4), make_uint4(u[i], u[i + 1], u[i + 2], u[i + 3]));
+            }
+          }
+        }
+        softmax_sync();
+        if (slot == 0 && !idle) {
+          const float2 other = ml[row_in];
+          const float top = fmaxf(m_run, other.x), f0 = l_run == 0.f ? 0.f : weight(m_run, l_run, top), f1 = weight(other.x, other.y, top);
+          ml[row_in] = make_float2(top, l_run * f0 + other.y * f1);
+#pragma unroll 1
           for (int d = 0; d < kD; d += 32) {
             uint32_t u[32];
             tmem_ld32(o_addr + d, u);
 #pragma unroll
-            for (int i = 0; i < 32; i += 4) sts128(at + (((d + i) / 4) ^ (row_in & 31)) * 16, make_uint4(u[i], u[i + 1], u[i + 2], u[i + 3]));
-          }
-          reinterpret_cast<float2*>(smem + kMlOff)[row_in] = make_float2(mine ? m_ref : -INFINITY, mine ? l_run : 0.f);
-        }
-        asm volatile("bar.sync 1, 256;" ::: "memory");
-      }
-      if (had[0]) ended[0] += 1;
-      if (had[1]) ended[1] += 1;
-      if ((dual || slot == 0) && !idle) {
-        const bool exists = row < rows_all;
-        tc_fence_after();
-        float m = mine ? m_ref : -INFINITY, l = mine ? l_run : 0.f, f0 = 1.f, f1 = 0.f;
-        if (!apart) {
-          const float2 other = reinterpret_cast<const float2*>(smem + kMlOff)[row_in];
-          const float top = fmaxf(m, other.x);
-          f0 = m == -INFINITY ? 0.f : ex2(m - top);
-          f1 = other.x == -INFINITY ? 0.f : ex2(other.x - top);
-          l = l * f0 + other.y * f1;
-          m = top;
-        }
-        if (l_run == 0.f || !mine) f0 = 0.f;
-        const int first_seg = it.x0 <= begin ? 0 : 1;
-        float* part = a.parts + ((size_t)blockIdx.x * 2 + first_seg) * a.rows_cap * (kD + 2);
-        const int prow = (dual ? slot * kTile : 0) + row_in;
-        const float inv = whole ? (l > 0.f ? 1.f / l : 0.f) : 1.f;
-        const size_t orow = ((size_t)it.b * lv.Hq + it.hk * g + (row - tok * g)) * a.stride + tok;
-#pragma unroll 1
-        for (int d = 0; d < kD; d += 32) {
-          uint32_t u[32];
-          float y[32];
-          tmem_ld32(o_addr + d, u);
-#pragma unroll
-          for (int i = 0; i < 32; ++i) y[i] = f0 == 0.f ? 0.f : __uint_as_float(u[i]) * f0;
-          if (f1 != 0.f) {
-#pragma unroll
             for (int i = 0; i < 32; i += 4) {
-              const uint4 o = lds128(qs + row_in * 512 + (((d + i) / 4) ^ (row_in & 31)) * 16);
-              y[i] = fmaf(__uint_as_float(o.x), f1, y[i]);
-              y[i + 1] = fmaf(__uint_as_float(o.y), f1, y[i + 1]);
-              y[i + 2] = fmaf(__uint_as_float(o.z), f1, y[i + 2]);
-              y[i + 3] = fmaf(__uint_as_float(o.w), f1, y[i + 3]);
+              float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+              if (f0 != 0.f)
+                y = make_float4(__uint_as_float(u[i]) * f0, __uint_as_float(u[i + 1]) * f0, __uint_as_float(u[i + 2]) * f0, __uint_as_float(u[i + 3]) * f0);
+              const uint32_t p = piece_at((d + i) / 4);
+              if (f1 != 0.f) {
+                const uint4 o = lds128(p);
+                y.x = fmaf(__uint_as_float(o.x), f1, y.x);
+                y.y = fmaf(__uint_as_float(o.y), f1, y.y);
+                y.z = fmaf(__uint_as_float(o.z), f1, y.z);
+                y.w = fmaf(__uint_as_float(o.w), f1, y.w);
+              }
+              sts128(p, make_uint4(__float_as_uint(y.x), __float_as_uint(y.y), __float_as_uint(y.z), __float_as_uint(y.w)));
             }
           }
-          if (!exists) continue;
-          if (whole) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) y[i] *= inv;
-            store_row(a, orow, d, y);
-          } else {
-            float4* dst = reinterpret_cast<float4*>(part + (size_t)prow * kD + d);
-#pragma unroll
-            for (int i = 0; i < 32; i += 4) dst[i / 4] = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
-          }
         }
-        if (!whole && exists) reinterpret_cast<float2*>(part + (size_t)a.rows_cap * kD)[prow] = make_float2(m, l);
+        softmax_sync();
+        const int lg_threads = 1 + lg_copies, r = tid >> lg_threads;             // row r of the item, pieces of 4 channels from c on
+        if (r < rows) {
+          float top = -INFINITY, l = 0.f, f[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (i < 1 << lg_copies) top = fmaxf(top, ml[r + i * per].x);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            f[i] = 0.f;
+            if (i < 1 << lg_copies) {
+              const float2 x = ml[r + i * per];
+              f[i] = weight(x.x, x.y, top);
+              l += x.y * f[i];
+            }
+          }
+          const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+          const int t = (row0 + r) / g;
+          const size_t orow = ((size_t)stream * g + (row0 + r - t * g)) * a.stride + t;
+#pragma unroll 1
+          for (int c = tid & ((1 << lg_threads) - 1); c < 32; c += 1 << lg_threads) {
+            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (f[i] != 0.f) {
+                const int v = r + i * per;
+                const uint4 o = lds128(qs + v * 512 + ((c ^ (v & 31)) << 4));
+                y.x = fmaf(__uint_as_float(o.x), f[i], y.x);
+                y.y = fmaf(__uint_as_float(o.y), f[i], y.y);
+                y.z = fmaf(__uint_as_float(o.z), f[i], y.z);
+                y.w = fmaf(__uint_as_float(o.w), f[i], y.w);
+              }
+            y.x *= inv; y.y *= inv; y.z *= inv; y.w *= inv;
+            if (whole)
+              store4(a, orow * kD + 4 * c, y);
+            else
+              reinterpret_cast<float4*>(part + (size_t)r * kD)[c] = y;
+          }
+          if (!whole && (tid & ((1 << lg_threads) - 1)) == 0) reinterpret_cast<float2*>(part + (size_t)a.rows_cap * kD)[r] = make_float2(top, l);
+        }
       }
       tc_fence_before();
-    });
+    }
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 16) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tbase), "r"(512) : "memory");
+  if (warp == kIssueWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tbase), "r"(512) : "memory");
 }
 
 // The items that several thread blocks share: block x has the one around the boundary x + 1, if no earlier boundary lies inside it.  kRows rows of
@@ -785,13 +1050,7 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant_
   const int row = kChunkRows * it.rt + prow, tok = row / g;
   const size_t at = ((((size_t)it.b * lv.Hq + it.hk * g + (row - tok * g)) * a.stride + tok) * kD) + 4 * lane;
   o.x *= inv; o.y *= inv; o.z *= inv; o.w *= inv;
-  if (a.out_bf16) {
-    const __nv_bfloat162 p0 = __floats2bfloat162_rn(o.x, o.y), p1 = __floats2bfloat162_rn(o.z, o.w);
-    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + at) =
-        make_uint2(*reinterpret_cast<const uint32_t*>(&p0), *reinterpret_cast<const uint32_t*>(&p1));
-  } else {
-    *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at) = o;
-  }
+  store4(a, at, o);
 }
 
 template <bool kDense, bool kV4>
