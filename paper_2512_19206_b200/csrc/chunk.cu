@@ -4,7 +4,7 @@
 //   new tokens up to j.
 //
 // One thread block of 896 threads per SM, persistent over its share of the (item, key tile) line (chunk.cuh).  Per key tile of 128 keys:
-//   warps 8-15, 16-23   make the tile: eight warps the keys, eight the values, half a 32-token unit each.  Packed codes become fp16 in registers
+//   warps 8-15, 16-23   make the tiles: four warps the keys of even tiles, four those of odd ones, eight the values.  Packed codes become fp16 in registers
 //                       (c s + z, one rounding) and go to shared memory in the tensor core's canonical layout; an unquantized row is copied
 //                       with bf16 -> fp16.  The packed bytes are read once per 256 query rows and never written back dequantized.
 //   warp 24             one thread issues every tcgen05.mma: S = Q K^T (operands in shared memory), O += P V (P in tensor memory).
@@ -27,11 +27,11 @@ namespace {
 
 constexpr int kTile = kChunkTile;
 constexpr int kTileBytes = kTile * kD * 2;
-constexpr int kThreads = 896;                             // 72 registers a thread at launch: 64512, shared out below as 256 x 104, 512 x 64, 128 x 40
+constexpr int kThreads = 896;                             // 72 registers a thread at launch: 64512, shared out below as 256 x 96, 256 x 80, 256 x 56, 128 x 40
 constexpr int kSoftmaxThreads = 256;
 constexpr int kIssueWarp = 24;
-constexpr int kScratchOff = 6 * kTileBytes;               // per producer warp 512 bytes: scales and zero-points as fp16 pairs
-constexpr int kMlOff = kScratchOff + 16 * 512;            // slot 1's maxima and denominators (128 x 8 bytes)
+constexpr int kScratchOff = 6 * kTileBytes;               // per producer warp 640 bytes: scales and zero-points as fp16 pairs
+constexpr int kMlOff = kScratchOff + 16 * 640;            // slot 1's maxima and denominators (128 x 8 bytes)
 constexpr int kBarOff = kMlOff + 1024;
 constexpr int kBars = 20;
 constexpr int kReaders = 26;                              // of a segment: 8 softmax, 16 producer warps, the issuing thread, the L2 requests
@@ -82,32 +82,48 @@ __device__ __forceinline__ uint4 rows_to_half(uint4 x) {
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
-// fp16 pair of 4^-f and of -1024 4^-f, f = 0 .. 4
-__device__ __forceinline__ constexpr uint32_t inv_pow4(int f) { return (uint32_t)((15 - 2 * f) << 10) * 0x00010001u; }
-__device__ __forceinline__ constexpr uint32_t neg_1024_pow4(int f) { return (0x8000u | (uint32_t)((25 - 2 * f) << 10)) * 0x00010001u; }
-
-// The codes of field f (2 bits at bit 2 f of each half word) as an fp16 pair: 1024 + c 4^f is the number with the field's bits in its
-// mantissa, and (1024 + c 4^f) 4^-f - 1024 4^-f is exact.  f is at most 4 after the shift (the mantissa has 10 bits).
-__device__ __forceinline__ uint32_t codes2(uint32_t w, int f) {
-  const int sh = f > 4 ? 10 : 0, ff = f > 4 ? f - 5 : f;
-  return hfma2_u(((w >> sh) & (0x00030003u << (2 * ff))) | 0x64006400u, inv_pow4(ff), neg_1024_pow4(ff));
+__device__ __forceinline__ uint32_t hadd2_u(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("add.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
 }
-// The same for 4-bit codes whose low and high pairs of bits are in two planes: hi4 = high plane << 2.  The top field's high bits are taken after the
-// shift, where hi4's lost ones are still there (`hi` itself).
-__device__ __forceinline__ uint32_t codes4(uint32_t lo, uint32_t hi, int f) {
-  const int sh = f > 3 ? 8 : 0, ff = f > 3 ? f - 4 : f;
-  const uint32_t l = lo >> sh, h = sh ? hi >> (sh - 2) : hi << 2;
-  return hfma2_u((l & (0x00030003u << (2 * ff))) | (h & (0x000C000Cu << (2 * ff))) | 0x64006400u, inv_pow4(ff), neg_1024_pow4(ff));
+__device__ __forceinline__ uint32_t hmul2_u(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
 }
+constexpr uint32_t kQuarter2 = 0x34003400u;               // the fp16 pair (0.25, 0.25)
 
-// Block and unit inside it of a unit number (below 2^26): inv = 2^32 / U rounded up, 0 for U = 1.
-__device__ __forceinline__ int block_of(int unit, uint32_t inv) { return inv == 0u ? unit : (int)__umulhi((uint32_t)unit, inv); }
+// c s + z of field f (2 bits at bit 2 f of each half word), one rounding.  The number with the field's bits in its mantissa is 1024 + c (f even) or
+// 1024 + 4 c (f odd), less 1024 it is exact, and for odd fields `s` is a quarter of the scale (exact as well: the scale has 8 significant bits; fewer than
+// two shifts and one constant per pair of fields, where a scale factor per field would cost a register or a move each).
+__device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t d;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+  return d;
+}
+struct Magic {                           // the fp16 pairs 1024 and -1024, kept in registers (as literals each use cost a move)
+  uint32_t plus, minus;
+  __device__ __forceinline__ Magic() {
+    asm volatile("mov.u32 %0, 0x64006400;" : "=r"(plus));
+    asm volatile("mov.u32 %0, 0xE400E400;" : "=r"(minus));
+  }
+};
+__device__ __forceinline__ uint32_t dequant2(const Magic& m, uint32_t w, int f, uint32_t s, uint32_t z) {
+  const uint32_t x = and_or(w >> (4 * (f >> 1)), 0x00030003u << (2 * (f & 1)), m.plus);
+  return hfma2_u(hadd2_u(x, m.minus), s, z);
+}
+// The same for 4-bit codes whose low and high pairs of bits are in two planes.
+__device__ __forceinline__ uint32_t dequant4(const Magic& m, uint32_t lo, uint32_t hi, int f, uint32_t s, uint32_t z) {
+  const int sh = 4 * (f >> 1), p = 2 * (f & 1);
+  const uint32_t low = 0x00030003u << p, l = lo >> sh, h = sh == 0 ? hi << 2 : hi >> (sh - 2);
+  const uint32_t c = (l & low) | (h & ~low), x = and_or(c, 0x000F000Fu << p, m.plus);
+  return hfma2_u(hadd2_u(x, m.minus), s, z);
+}
 
 __device__ __forceinline__ void prefetch_bulk(const void* p, uint32_t bytes) {
   asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
 }
-
-__device__ __forceinline__ uint32_t inverse_units(const LayerView& lv) { return lv.U == 1 ? 0u : 0xFFFFFFFFu / (uint32_t)lv.U + 1u; }
 
 struct Rows {                            // a stream's unquantized rows: residual window, sink, new tokens
   const uint16_t *res, *sink, *fresh;
@@ -117,154 +133,196 @@ struct Rows {                            // a stream's unquantized rows: residua
   }
 };
 
-// Half a unit's packed keys or values on their way to shared memory: requested one tile ahead.
-struct Packed {
-  uint4 c, h, meta;
+// A warp's unit: every fourth (the keys' warps: every eighth) one of the stream, from tile to tile.  (Blocks and units are counted on; a division and two long multiplications per tile
+// and warp were a fifth of the instructions.)
+struct Cursor {
+  const char* blk;                       // its block
+  const uint2* entry;                    // the block's table entry
+  int unit, u;                           // its number in the stream and in the block
+  uint32_t shift;                        // units of a key group: 2^shift
+  __device__ __forceinline__ Cursor(const LayerView& lv, int stream, int first) {
+    const int bi = first / lv.U;
+    blk = lv.base + (size_t)stream * lv.base_stride + (size_t)bi * lv.base_bytes;
+    entry = reinterpret_cast<const uint2*>(lv.table + (size_t)stream * lv.table_stride) + bi;
+    unit = first;
+    u = first - bi * lv.U;
+    shift = lv.VG == 4 ? 0u : lv.VG == 2 ? 1u : 2u;
+  }
+  // n units on: n / U blocks and n % U units
+  __device__ __forceinline__ void next(const LayerView& lv, int n, int blocks, int units) {
+    unit += n;
+    u += units;
+    if (u >= lv.U) {
+      u -= lv.U;
+      blocks += 1;
+    }
+    blk += (uint32_t)blocks * lv.base_bytes;
+    entry += blocks;
+  }
+  __device__ __forceinline__ const char* codes(const LayerView& lv) const { return blk + ((uint32_t)u * lv.unit_bytes + 512u * (((uint32_t)u >> shift) + 1)); }
+  __device__ __forceinline__ const char* meta(const LayerView& lv) const {
+    const uint32_t group = (uint32_t)u >> shift;
+    return blk + ((group << shift) * lv.unit_bytes + 512u * group);
+  }
 };
-// A unit's place in its block (VG = 128 / G says how many units share a group's scales: 1, 2 or 4).
-__device__ __forceinline__ uint32_t group_shift(const LayerView& lv) { return lv.VG == 4 ? 0u : lv.VG == 2 ? 1u : 2u; }
 
-// ---- keys: warp (w, mt) makes rows 32 w + 16 mt .. + 15 of the tile at shared address `tile`
+// Half a unit's packed values (a unit's keys) on their way to shared memory: requested one tile ahead.
+struct Packed {
+  uint4 c, h;
+  uint2 meta;
+};
+struct PackedKeys {
+  uint4 c0, c1, h0, h1, meta;
+};
+
+// ---- keys: warp w of four makes rows 32 w .. 32 w + 31 of the tile at shared address `tile`; two such groups of warps take the tiles in turn, so that two
+// are on their way at any time (a tile is mostly latency: loads, barriers, chains of a few dependent instructions)
+// A block's promoted channels: `id` is the lane's entry of the list of BF16 channels, raw their first two pairs (the lane's token), ex the block's extras,
+// exu this unit's.
+struct Promoted {
+  int n16, n4;
+  uint32_t id, raw[2];
+  const char *ex, *exu;
+};
 template <bool kDense>
-__device__ __forceinline__ Packed request_keys(const LayerView& lv, const char* base, const char* extras, uint32_t inv_u, int unit, uint2 entry, int mt, int lane) {
-  Packed p{};
-  const int bi = block_of(unit, inv_u), u = unit - bi * lv.U;
-  const uint32_t group = (uint32_t)u >> group_shift(lv);
-  const char* blk = base + (size_t)bi * lv.base_bytes;
-  p.c = reinterpret_cast<const uint4*>(blk + (uint32_t)u * lv.unit_bytes + 512u * (group + 1))[32 * mt + lane];
-  p.meta = reinterpret_cast<const uint4*>(blk + (group << group_shift(lv)) * lv.unit_bytes + 512u * group)[lane];
-  if (kDense) {
-    const int n16 = entry.y & 0xFF, n4 = (entry.y >> 8) & 0xFF;
-    if (n4 != 0)
-      p.h = reinterpret_cast<const uint4*>(extras + (size_t)entry.x * 16 + extras_header_bytes(n16, n4) +
-                                           (size_t)u * extras_unit_bytes(n16, n4, true) + 128 * ((n16 + 1) >> 1))[32 * mt + lane];
+__device__ __forceinline__ Promoted request_promoted(const char* extras, uint2 entry, int u, int lane) {
+  Promoted p;
+  p.n16 = entry.y & 0xFF;
+  p.n4 = (entry.y >> 8) & 0xFF;
+  p.id = kD;
+  p.raw[0] = p.raw[1] = 0u;
+  p.ex = extras + (size_t)entry.x * 16;
+  p.exu = p.ex + extras_header_bytes(p.n16, p.n4) + (uint32_t)u * extras_unit_bytes(p.n16, p.n4, kDense);
+  if (lane < p.n16) p.id = reinterpret_cast<const uint8_t*>(p.ex)[lane];
+  if (p.n16 > 0) p.raw[0] = reinterpret_cast<const uint32_t*>(p.exu)[lane];
+  if (p.n16 > 2) p.raw[1] = reinterpret_cast<const uint32_t*>(p.exu)[32 + lane];
+  return p;
+}
+template <bool kDense>
+__device__ __forceinline__ PackedKeys request_keys(const LayerView& lv, const Cursor& at, const Promoted& more, int lane) {
+  PackedKeys p{};
+  const uint4* codes = reinterpret_cast<const uint4*>(at.codes(lv)) + lane;
+  p.c0 = codes[0];
+  p.c1 = codes[32];
+  p.meta = reinterpret_cast<const uint4*>(at.meta(lv))[lane];
+  if (kDense && more.n4 != 0) {
+    const uint4* hi = reinterpret_cast<const uint4*>(more.exu + 128 * ((more.n16 + 1) >> 1)) + lane;
+    p.h0 = hi[0];
+    p.h1 = hi[32];
   }
   return p;
 }
 
+// The unit's two-bit (kDense: four-bit) codes.
 template <bool kDense>
-__device__ __forceinline__ void make_keys(const LayerView& lv, const char* base, const char* extras, uint32_t inv_u, const Packed& p, int unit, uint2 entry,
-                                          uint32_t tile, uint32_t scratch, int w, int mt, int lane) {
-  const int n16 = entry.y & 0xFF, n4 = (entry.y >> 8) & 0xFF, n16p = (n16 + 1) >> 1;
-  // Promoted channels: the lane's token is tok = 16 mt + lane % 16 of the unit, and of the pairs it takes every second one.  The first two and their
-  // channel numbers are under way while the codes are worked on.
-  const int tok = 16 * mt + (lane & 15), par = lane >> 4;
-  const char *ex = nullptr, *exu = nullptr;
-  uint32_t ids[2] = {~0u, ~0u}, raw[2] = {0u, 0u};
-  if (n16 + n4 > 0) {
-    const int u = unit - block_of(unit, inv_u) * lv.U;
-    ex = extras + (size_t)entry.x * 16;
-    exu = ex + extras_header_bytes(n16, n4) + (size_t)u * extras_unit_bytes(n16, n4, kDense);
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      if (2 * i + par < n16p) {
-        ids[i] = reinterpret_cast<const uint16_t*>(ex)[2 * i + par];
-        raw[i] = reinterpret_cast<const uint32_t*>(exu)[(2 * i + par) * 32 + tok];
-      }
-  }
-  // scales and zero-points of channel pairs (16 kt + 8 ch + 2 t, + 1) as fp16 pairs: word 16 t + 8 ch + kt, zero-points 64 words on.  The lane has the
-  // pairs 2 lane and 2 lane + 1: kt = lane / 4, ch = lane / 2 % 2, t = 2 (lane % 2) and the next.
+__device__ __forceinline__ void make_keys(const PackedKeys& p, uint32_t tile, uint32_t scratch, int w, int lane, const Magic& magic) {
+  // Scales and zero-points of channel pairs (16 kt + 8 ch + 2 t, + 1) as fp16 pairs: word 36 ch + 8 t + kt, zero-points 72 words on (odd kt: a quarter of the
+  // scale).  The lane has the pairs 2 lane and 2 lane + 1: kt = lane / 4, ch = lane / 2 % 2, t = 2 (lane % 2) and the next.
   {
-    const uint32_t at = scratch + 4 * (16 * 2 * (lane & 1) + 8 * ((lane >> 1) & 1) + (lane >> 2));
-    sts32(at, bf16x2_to_f16x2(__byte_perm(p.meta.x, p.meta.y, 0x5410)));
-    sts32(at + 256, bf16x2_to_f16x2(__byte_perm(p.meta.x, p.meta.y, 0x7632)));
-    sts32(at + 64, bf16x2_to_f16x2(__byte_perm(p.meta.z, p.meta.w, 0x5410)));
-    sts32(at + 64 + 256, bf16x2_to_f16x2(__byte_perm(p.meta.z, p.meta.w, 0x7632)));
+    const uint32_t at = scratch + 4 * (36 * ((lane >> 1) & 1) + 16 * (lane & 1) + (lane >> 2));
+    const uint32_t s0 = bf16x2_to_f16x2(__byte_perm(p.meta.x, p.meta.y, 0x5410)), s1 = bf16x2_to_f16x2(__byte_perm(p.meta.z, p.meta.w, 0x5410));
+    sts32(at, lane & 4 ? hmul2_u(s0, kQuarter2) : s0);
+    sts32(at + 32, lane & 4 ? hmul2_u(s1, kQuarter2) : s1);
+    sts32(at + 288, bf16x2_to_f16x2(__byte_perm(p.meta.x, p.meta.y, 0x7632)));
+    sts32(at + 320, bf16x2_to_f16x2(__byte_perm(p.meta.z, p.meta.w, 0x7632)));
   }
   __syncwarp();
   // (a rolled loop: every role's straight-line code together runs out of the instruction cache)
-  uint32_t c0 = p.c.x, c1 = p.c.y, h0 = p.h.x, h1 = p.h.y;
-  uint32_t to = tile + (4 * w + 2 * mt) * 2048 + 4 * lane, at = scratch + 64 * (lane & 3);
+  const uint32_t out = tile + 4 * w * 2048 + 4 * lane, in = scratch + 32 * (lane & 3);
 #pragma unroll 1
-  for (int ch = 0; ch < 2; ++ch) {       // the upper or lower 8 of every 16 channels
+  for (int i = 0; i < 4; ++i) {          // of every 16 channels the upper or lower 8 (ch), channels 64 kh ..
+    const int ch = i >> 1, kh = i & 1;
+    const uint32_t at = in + 144 * ch + 16 * kh, to = out + 128 * ch + 1024 * kh;
+    const uint4 s4 = lds128(at), z4 = lds128(at + 288);
+    const uint32_t s[4] = {s4.x, s4.y, s4.z, s4.w}, z[4] = {z4.x, z4.y, z4.z, z4.w};
+    const uint32_t c[4] = {(ch ? p.c0.z : p.c0.x) >> (8 * kh), (ch ? p.c0.w : p.c0.y) >> (8 * kh), (ch ? p.c1.z : p.c1.x) >> (8 * kh),
+                           (ch ? p.c1.w : p.c1.y) >> (8 * kh)};
+    const uint32_t h[4] = {(ch ? p.h0.z : p.h0.x) >> (8 * kh), (ch ? p.h0.w : p.h0.y) >> (8 * kh), (ch ? p.h1.z : p.h1.x) >> (8 * kh),
+                           (ch ? p.h1.w : p.h1.y) >> (8 * kh)};
 #pragma unroll
-    for (int kh = 0; kh < 2; ++kh) {
-      const uint4 s4 = lds128(at + 16 * kh), z4 = lds128(at + 256 + 16 * kh);
-      const uint32_t s[4] = {s4.x, s4.y, s4.z, s4.w}, z[4] = {z4.x, z4.y, z4.z, z4.w};
+    for (int r = 0; r < 4; ++r)          // rows 8 r ..
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        sts32(to + r * 2048 + 2 * k * 128, kDense ? dequant4(magic, c[r], h[r], k, s[k], z[k]) : dequant2(magic, c[r], k, s[k], z[k]));
+  }
+}
+
+// The promoted channels replace their codes' values.
+template <bool kDense>
+__device__ __forceinline__ void put_promoted(const LayerView& lv, const Cursor& at, Promoted& p, uint32_t tile, int w, int lane) {
+  if ((p.n16 | (kDense ? 0 : p.n4)) == 0) return;
+  __syncwarp();                          // the base codes are stored
+  const uint32_t row = tile + (4 * w + (lane >> 3)) * 2048 + (lane & 7) * 16;           // the lane's token
+  auto offset = [](uint32_t d) { return (d >> 3) * 128 + (d & 7) * 2; };
+  uint32_t mine = offset(p.id);          // of the lane's list entry
+#pragma unroll 1
+  for (int i = 0; 2 * i < p.n16; ++i) {
+    const uint32_t o0 = __shfl_sync(0xffffffffu, mine, (2 * i) & 31), o1 = __shfl_sync(0xffffffffu, mine, (2 * i + 1) & 31), both = bf16x2_to_f16x2(p.raw[0]);
+    sts16(row + o0, both & 0xFFFFu);
+    if (2 * i + 1 < p.n16) sts16(row + o1, both >> 16);
+    p.raw[0] = p.raw[1];
+    if (2 * i + 4 < p.n16) p.raw[1] = reinterpret_cast<const uint32_t*>(p.exu)[(i + 2) * 32 + lane];
+    if (((2 * i + 2) & 31) == 0 && 2 * i + 2 + lane < p.n16) mine = offset(reinterpret_cast<const uint8_t*>(p.ex)[2 * i + 2 + lane]);
+  }
+  if (!kDense && p.n4 > 0) {             // UINT4 channels: c = c_lo + 4 c_hi, with s and z from the block's scales; four at a time, their loads in flight together
+    const int n16p = (p.n16 + 1) >> 1, mt = lane >> 4, rh = (lane >> 3) & 1, r = lane & 7;
+    const uint32_t* low = reinterpret_cast<const uint32_t*>(at.codes(lv)) + mt * 128 + 16 * r + rh;
+    const uint32_t* meta = reinterpret_cast<const uint32_t*>(at.meta(lv));
+    const uint32_t* high = reinterpret_cast<const uint32_t*>(p.exu + 128 * n16p) + (r & 3);
+    const uint16_t* chans = reinterpret_cast<const uint16_t*>(p.ex + 2 * n16p);          // (pairs; the last may hold 0xFF)
+    const int hi_bit = 8 * (r >> 2) + 2 * (2 * mt + rh), pairs = (p.n4 + 1) >> 1;
+    uint32_t id = lane < pairs ? chans[lane] : 0xFFFFu;
+#pragma unroll 1
+    for (int i0 = 0; i0 < pairs; i0 += 2) {
+      if (i0 == 32) id = 32 + lane < pairs ? chans[32 + lane] : 0xFFFFu;
+      uint32_t d[4], hw[2], lw[4], mz[4];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t two = __shfl_sync(0xffffffffu, id, (i0 + k) & 31);
+        d[2 * k] = i0 + k < pairs ? two & 0xFF : 0xFFu;
+        d[2 * k + 1] = i0 + k < pairs ? two >> 8 : 0xFFu;
+        hw[k] = i0 + k < pairs ? high[4 * (i0 + k)] >> hi_bit : 0u;
+      }
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const int kt = 4 * kh + k;
-        sts32(to + 2 * kt * 128, hfma2_u(kDense ? codes4(c0, h0, kt) : codes2(c0, kt), s[k], z[k]));
-        sts32(to + 2048 + 2 * kt * 128, hfma2_u(kDense ? codes4(c1, h1, kt) : codes2(c1, kt), s[k], z[k]));
+        lw[k] = mz[k] = 0u;
+        if (d[k] < kD) {
+          lw[k] = low[4 * ((d[k] & 7) >> 1) + 2 * ((d[k] >> 3) & 1)];
+          mz[k] = meta[d[k]];
+        }
       }
-    }
-    c0 = p.c.z;
-    c1 = p.c.w;
-    h0 = p.h.z;
-    h1 = p.h.w;
-    to += 128;
-    at += 32;
-  }
-  if ((n16 | (kDense ? 0 : n4)) == 0) return;
-  __syncwarp();                          // the base codes are stored: promoted channels replace theirs
-  const uint32_t row = tile + (4 * w + (tok >> 3)) * 2048 + (tok & 7) * 16;
-  auto put = [&](uint32_t d, float value) { sts16(row + (d >> 3) * 128 + (d & 7) * 2, (uint32_t)__half_as_ushort(__float2half_rn(value))); };
-#pragma unroll 1
-  for (int i0 = 0; i0 < n16p; i0 += 4) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint32_t d0 = ids[i] & 0xFF, d1 = (ids[i] >> 8) & 0xFF;
-      if (d0 < kD) put(d0, bf_lo(raw[i]));
-      if (d1 < kD) put(d1, bf_hi(raw[i]));
-      ids[i] = ~0u;
-      const int next = i0 + 4 + 2 * i + par;
-      if (next < n16p) {
-        ids[i] = reinterpret_cast<const uint16_t*>(ex)[next];
-        raw[i] = reinterpret_cast<const uint32_t*>(exu)[next * 32 + tok];
-      }
-    }
-  }
-  if (!kDense && n4 > 0) {               // UINT4 channels: c = c_lo + 4 c_hi, with s and z from the block's scales; of a pair the lane has channel `par`
-    const int bi = block_of(unit, inv_u), u = unit - bi * lv.U;
-    const uint32_t group = (uint32_t)u >> group_shift(lv);
-    const char* blk = base + (size_t)bi * lv.base_bytes;
-    const int rh = (lane >> 3) & 1, r = lane & 7;
-    const uint32_t* low = reinterpret_cast<const uint32_t*>(blk + (uint32_t)u * lv.unit_bytes + 512u * (group + 1)) + mt * 128 + 16 * r + rh;
-    const uint32_t* meta = reinterpret_cast<const uint32_t*>(blk + (group << group_shift(lv)) * lv.unit_bytes + 512u * group);
-    const uint32_t* high = reinterpret_cast<const uint32_t*>(exu + 128 * n16p) + (r & 3);
-    const uint8_t* chans = reinterpret_cast<const uint8_t*>(ex + 2 * n16p) + par;
-    const int hi_bit = 16 * par + 8 * (r >> 2) + 2 * (2 * mt + rh);
-#pragma unroll 4
-    for (int i = 0; i < (n4 + 1) >> 1; ++i) {
-      const uint32_t d = chans[2 * i], hw = high[4 * i];
-      if (d < kD) {
-        const uint32_t lw = low[4 * ((d & 7) >> 1) + 2 * ((d >> 3) & 1)], mz = meta[d];
-        const uint32_t code = ((lw >> (16 * (d & 1) + 2 * (d >> 4))) & 3u) | (((hw >> hi_bit) & 3u) << 2);
-        put(d, fmaf((float)code, bf_lo(mz), bf_hi(mz)));
-      }
+      for (int k = 0; k < 4; ++k)
+        if (d[k] < kD) {
+          const uint32_t code = ((lw[k] >> (16 * (d[k] & 1) + 2 * (d[k] >> 4))) & 3u) | (((hw[k >> 1] >> (16 * (k & 1))) & 3u) << 2);
+          sts16(row + offset(d[k]), (uint32_t)__half_as_ushort(__float2half_rn(fmaf((float)code, bf_lo(mz[k]), bf_hi(mz[k])))));
+        }
     }
   }
 }
 
 // ---- values: warp (w, half) makes keys 32 w .. 32 w + 31 of channels 64 half .. + 63, stored channel by channel (K-major for O = P V)
+// meta0, meta1: where the lane's token has the scales of the half's two groups of 32 channels (the same one twice where a group is wider)
 template <bool kV4>
-__device__ __forceinline__ Packed request_values(const LayerView& lv, const char* base, uint32_t inv_u, int unit, int half, int lane) {
+__device__ __forceinline__ Packed request_values(const LayerView& lv, const Cursor& at, int half, int lane, uint32_t meta0, uint32_t meta1) {
   Packed p{};
-  const int bi = block_of(unit, inv_u), u = unit - bi * lv.U;
-  const char* at = base + (size_t)bi * lv.base_bytes + (uint32_t)u * lv.unit_bytes + 512u * (((uint32_t)u >> group_shift(lv)) + 1);
-  p.c = reinterpret_cast<const uint4*>(at + 1024)[32 * half + lane];
-  // the scales of the half's two groups of 32 channels (the same one twice where a group is wider)
-  if (lv.VG == 4) {
-    const uint2 m = reinterpret_cast<const uint2*>(at + 2048)[2 * lane + half];
-    p.meta.x = m.x;
-    p.meta.y = m.y;
-  } else {
-    p.meta.x = p.meta.y = reinterpret_cast<const uint32_t*>(at + 2048)[lv.VG == 2 ? 2 * lane + half : lane];
-  }
-  if (kV4) p.h = reinterpret_cast<const uint4*>(at + 2048 + 128 * lv.VG)[32 * half + lane];
+  const char* unit = at.codes(lv);
+  p.c = reinterpret_cast<const uint4*>(unit + 1024)[32 * half + lane];
+  p.meta = make_uint2(*reinterpret_cast<const uint32_t*>(unit + meta0), *reinterpret_cast<const uint32_t*>(unit + meta1));
+  if (kV4) p.h = reinterpret_cast<const uint4*>(unit + 2048 + 128 * lv.VG)[32 * half + lane];
   return p;
 }
 
 template <bool kV4>
-__device__ __forceinline__ void make_values(const Packed& p, uint32_t tile, uint32_t scratch, int w, int half, int lane) {
+__device__ __forceinline__ void make_values(const Packed& p, uint32_t tile, uint32_t scratch, int w, int half, int lane, const Magic& magic) {
   // scales of tokens (8 o + 2 t, + 1) as fp16 pairs: word 16 i + 4 t + o for 32 channels i, zero-points 32 words on; the lane has token
   // 8 o + 2 t + e = lane
   {
     const uint32_t at = scratch + 4 * (4 * ((lane >> 1) & 3) + (lane >> 3)) + 2 * (lane & 1);
     const uint32_t a = bf16x2_to_f16x2(p.meta.x), b = bf16x2_to_f16x2(p.meta.y);
-    sts16(at, a & 0xFFFFu);
+    sts16(at, (lane & 8 ? hmul2_u(a, kQuarter2) : a) & 0xFFFFu);       // (odd o: a quarter of the scale)
     sts16(at + 128, a >> 16);
-    sts16(at + 64, b & 0xFFFFu);
+    sts16(at + 64, (lane & 8 ? hmul2_u(b, kQuarter2) : b) & 0xFFFFu);
     sts16(at + 192, b >> 16);
   }
   __syncwarp();
@@ -276,10 +334,10 @@ __device__ __forceinline__ void make_values(const Packed& p, uint32_t tile, uint
     const uint32_t s[4] = {s4.x, s4.y, s4.z, s4.w}, z[4] = {z4.x, z4.y, z4.z, z4.w};
 #pragma unroll
     for (int f = 0; f < 8; ++f)
-      sts32(to + (f >> 2) * 2048 + (f & 3) * 128, hfma2_u(kV4 ? codes4(c0, h0, f) : codes2(c0, f), s[f & 3], z[f & 3]));
+      sts32(to + (f >> 2) * 2048 + (f & 3) * 128, kV4 ? dequant4(magic, c0, h0, f, s[f & 3], z[f & 3]) : dequant2(magic, c0, f, s[f & 3], z[f & 3]));
 #pragma unroll
     for (int f = 0; f < 8; ++f)
-      sts32(to + (2 + (f >> 2)) * 2048 + (f & 3) * 128, hfma2_u(kV4 ? codes4(c1, h1, f) : codes2(c1, f), s[f & 3], z[f & 3]));
+      sts32(to + (2 + (f >> 2)) * 2048 + (f & 3) * 128, kV4 ? dequant4(magic, c1, h1, f, s[f & 3], z[f & 3]) : dequant2(magic, c1, f, s[f & 3], z[f & 3]));
     c0 = p.c.z;
     c1 = p.c.w;
     h0 = p.h.z;
@@ -289,21 +347,20 @@ __device__ __forceinline__ void make_values(const Packed& p, uint32_t tile, uint
   }
 }
 
-// Unquantized rows of tail tile t, rows past the last as zeros.  Keys K-major, warp (w, mt) rows 32 w + 16 mt .. + 15; values as they lie
-// (MN-major), warp (w, half) rows 32 w .. + 31 of channels 64 half .. + 63.
-__device__ __forceinline__ void copy_key_rows(const Rows& x, int t, uint32_t tile, int w, int mt, int lane) {
+// Unquantized rows 32 w .. + 31 of tail tile t, rows past the last as zeros.  Keys K-major (warp w), values as they lie (MN-major; warp (w, half): channels
+// 64 half .. + 63).
+__device__ __forceinline__ void copy_key_rows(const Rows& x, int t, uint32_t tile, int w, int lane) {
 #pragma unroll
-  for (int c = 0; c < 4; c += 2) {       // (all at once took more registers than the warps have)
+  for (int c = 0; c < 16; c += 4) {      // (all at once took more registers than the warps have)
     uint4 y[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int row = kTile * t + 32 * w + 16 * mt + 8 * (i & 1) + (lane & 7);
+      const int row = kTile * t + 32 * w + 8 * i + (lane & 7);
       y[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (row < x.total) y[i] = x.row(row)[4 * (c + (i >> 1)) + (lane >> 3)];
+      if (row < x.total) y[i] = x.row(row)[c + (lane >> 3)];
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      sts128(tile + (4 * w + 2 * mt + (i & 1)) * 2048 + (4 * (c + (i >> 1)) + (lane >> 3)) * 128 + (lane & 7) * 16, rows_to_half(y[i]));
+    for (int i = 0; i < 4; ++i) sts128(tile + (4 * w + i) * 2048 + (c + (lane >> 3)) * 128 + (lane & 7) * 16, rows_to_half(y[i]));
   }
 }
 __device__ __forceinline__ void copy_value_rows(const Rows& x, int t, uint32_t tile, int w, int half, int lane) {
@@ -479,15 +536,6 @@ __device__ __forceinline__ bool elect_one() {
   return e != 0;
 }
 
-// `ok` of all softmax threads: none goes on alone, and so none waits alone in the barriers that they share
-__device__ __forceinline__ bool softmax_all(bool ok) {
-  uint32_t all;
-  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-               : "=r"(all)
-               : "r"((uint32_t)ok)
-               : "memory");
-  return all != 0;
-}
 __device__ __forceinline__ void softmax_sync() { asm volatile("barrier.cta.sync 1, 256;" ::: "memory"); }
 
 // 4 channels of an output row
@@ -517,7 +565,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
   }
   if (tid == 0) {
     for (int i = 0; i < kBars; ++i)
-      mbar_init(bar(i), i == kQFull ? kSoftmaxThreads : (i >= kKFull && i < kKEmpty) ? 8 : (i >= kPReady && i < kODone) ? kTile : i >= kSegEmpty ? kReaders : 1);
+      mbar_init(bar(i), i == kQFull || (i >= kVFull && i < kKEmpty) ? 8 : (i >= kKFull && i < kVFull) ? 4 : (i >= kPReady && i < kODone) ? 4 : (i >= kSegEmpty ? kReaders : 1));
     *progress = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -534,6 +582,17 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       atomicOr(lv.status, (uint32_t)MIXKVQ_DEV_COPY_TIMEOUT);
     }
     return !dead;
+  };
+  // The same for a group of `threads` threads: one warp polls, the others wait for it in the named barrier `id`, which costs no issue slots (two dozen
+  // polling warps took a third of them).  The polling warp comes to the barrier in any case, and all learn what it saw.
+  auto group_wait = [&](int id, int threads, bool polls, int i, uint32_t parity) {
+    uint32_t ok = 1;
+    if (polls && i >= 0) ok = wait(i, parity);
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %0, 0;\n\tbarrier.cta.red.and.pred q, %1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "+r"(ok)
+                 : "r"(id), "r"(threads)
+                 : "memory");
+    return ok != 0;
   };
   // the n-th segment is there; (a reader's warp has taken what it needs)
   auto segment_there = [&](int n) { return wait(kSegFull + (n & 1), (uint32_t)(n >> 1) & 1u); };
@@ -652,133 +711,154 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       // ---------------------------------------------------------------- requests into L2
       // The producers load one tile ahead, which is less than a round trip to memory: what they will load goes to L2 kAhead tiles before.  Lanes 0 .. 3
       // the units of a tile, lanes 4 .. 7 their blocks' promoted channels.
+      const int step_blocks = 4 / lv.U, step_units = 4 - step_blocks * lv.U;
       int kc = 0;
       for (int n = 0; segment_there(n); ++n) {
         const Segment& sg = segments[n & 1];
         const int stream = sg.stream, j0 = sg.j0, j1 = min(sg.j1, sg.packed_tiles), nt = sg.j1 - j0, units = sg.units;
         segment_taken(n);
         if (stream < 0) break;
-        const uint32_t inv_u = inverse_units(lv);
+        Cursor at(lv, stream, 4 * j0 + (lane & 3));
+        const char* extras = lv.extras + (size_t)stream * lv.extras_stride;
         for (int j = j0; j < j1; ++j) {
           // (a bounded wait, and nothing depends on it)
           for (int i = 0; i < 100 && *progress + kAhead < kc + j - j0; ++i) __nanosleep(200);
-          const int unit = 4 * j + (lane & 3);
-          if (lane >= 8 || unit >= units) continue;
-          const int bi = block_of(unit, inv_u), u = unit - bi * lv.U;
-          if (lane < 4) {
-            prefetch_bulk(lv.base + (size_t)stream * lv.base_stride + (size_t)bi * lv.base_bytes + (uint32_t)u * lv.unit_bytes +
-                              512u * ((uint32_t)u >> group_shift(lv)),
-                          lv.unit_bytes + 512);
-          } else {
-            const uint2 e = reinterpret_cast<const uint2*>(lv.table + (size_t)stream * lv.table_stride)[bi];
-            const int n16 = e.y & 0xFF, n4 = (e.y >> 8) & 0xFF;
-            const uint32_t bytes = extras_unit_bytes(n16, n4, kDense);                 // (a multiple of 16)
-            if (n16 + n4 > 0)
-              prefetch_bulk(lv.extras + (size_t)stream * lv.extras_stride + (size_t)e.x * 16 + extras_header_bytes(n16, n4) + (size_t)u * bytes, bytes);
+          if (lane < 8 && at.unit < units) {
+            if (lane < 4) {
+              prefetch_bulk(at.codes(lv) - 512, lv.unit_bytes + 512);
+            } else {
+              const uint2 e = *at.entry;
+              const int n16 = e.y & 0xFF, n4 = (e.y >> 8) & 0xFF;
+              const uint32_t bytes = extras_unit_bytes(n16, n4, kDense);               // (a multiple of 16)
+              if (n16 + n4 > 0) prefetch_bulk(extras + (size_t)e.x * 16 + extras_header_bytes(n16, n4) + (uint32_t)at.u * bytes, bytes);
+            }
           }
+          at.next(lv, 4, step_blocks, step_units);
         }
         kc += nt;
       }
     }
   } else if (warp >= 16) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;" ::: "memory");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;" ::: "memory");
     // ------------------------------------------------------------------ value tiles
     const int w = (warp >> 1) & 3, half = warp & 1;
-    const uint32_t scratch = sbase + kScratchOff + (warp - 8) * 512, inv_u = inverse_units(lv);
+    const uint32_t scratch = sbase + kScratchOff + (warp - 8) * 640;
+    const int step_blocks = 4 / lv.U, step_units = 4 - step_blocks * lv.U;
+    const uint32_t meta0 = 2048 + 4 * (lane * lv.VG + (lv.VG == 4 ? 2 * half : lv.VG == 2 ? half : 0)), meta1 = meta0 + (lv.VG == 4 ? 4 : 0);
+    const Magic magic;
     int kc = 0;
+    bool ok = true;
     auto stage = [&]() { return vs + (kc & 1) * kTileBytes; };
-    auto free_stage = [&]() { return kc < 2 || wait(kVEmpty + (kc & 1), (uint32_t)((kc >> 1) - 1) & 1u); };
+    auto free_stage = [&]() { return group_wait(6, 256, warp == 16, kc < 2 ? -1 : kVEmpty + (kc & 1), (uint32_t)((kc >> 1) - 1) & 1u); };
     auto made = [&]() {
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(kVFull + (kc & 1)));
       ++kc;
     };
-    for (int n = 0; segment_there(n); ++n) {
+    for (int n = 0; group_wait(6, 256, warp == 16, kSegFull + (n & 1), (uint32_t)(n >> 1) & 1u); ++n) {
       const Segment& sg = segments[n & 1];
       const int stream = sg.stream, j1 = sg.j1, packed_tiles = sg.packed_tiles, units = sg.units, r = sg.r, c0 = sg.c0, total = sg.total;
       int j = sg.j0;
       segment_taken(n);
       if (stream < 0) break;
-      const char* base = lv.base + (size_t)stream * lv.base_stride;
-      auto request = [&](int unit) { return request_values<kV4>(lv, base, inv_u, min(unit, units - 1), half, lane); };
       const int end = min(j1, packed_tiles);
       if (j < end) {
-        Packed p = request(4 * j + w);
+        Cursor at(lv, stream, 4 * j + w);
+        Packed p{};
+        if (at.unit < units) p = request_values<kV4>(lv, at, half, lane, meta0, meta1);
         for (; j < end; ++j) {
-          if (!free_stage()) break;
-          if (4 * j + w < units) {
-            make_values<kV4>(p, stage(), scratch, w, half, lane);
+          if (!(ok = free_stage())) break;
+          if (at.unit < units) {
+            make_values<kV4>(p, stage(), scratch, w, half, lane, magic);
           } else {
             // past the last block: the probabilities are zeros, and so must the values be (a NaN from earlier contents would survive the product)
             for (int i = lane; i < 8 * 32; i += 32)
               sts128(stage() + (8 * half + (i >> 5)) * 2048 + (4 * w) * 128 + (i & 31) * 16, make_uint4(0u, 0u, 0u, 0u));
           }
-          p = request(4 * j + 4 + w);
+          at.next(lv, 4, step_blocks, step_units);
+          if (at.unit < units) p = request_values<kV4>(lv, at, half, lane, meta0, meta1);
           made();
         }
       }
-      for (; j < j1 && !dead; ++j) {
+      for (; j < j1 && ok; ++j) {
         const Rows x{reinterpret_cast<const uint16_t*>(lv.resv + (size_t)stream * lv.resv_stride),
                      reinterpret_cast<const uint16_t*>(lv.sink + (size_t)stream * lv.sink_stride) + (size_t)lv.sink_len * kD,
                      a.v + (size_t)stream * a.stride * kD, r, c0, total};
-        if (!free_stage()) break;
+        if (!(ok = free_stage())) break;
         copy_value_rows(x, j - packed_tiles, stage(), w, half, lane);
         made();
       }
-      if (dead) break;
+      if (!ok) break;
     }
   } else if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;" ::: "memory");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 80;" ::: "memory");
     // ------------------------------------------------------------------ key tiles
-    const int w = (warp >> 1) & 3, mt = warp & 1;
-    const uint32_t scratch = sbase + kScratchOff + (warp - 8) * 512, inv_u = inverse_units(lv);
-    int kc = 0;
-    auto stage = [&]() { return ks + (kc & 1) * kTileBytes; };
-    auto free_stage = [&]() { return kc < 2 || wait(kKEmpty + (kc & 1), (uint32_t)((kc >> 1) - 1) & 1u); };
+    // (the group's tiles are the even or the odd ones of the thread block, counted through all segments: it has one stage to itself)
+    const int w = warp & 3, group = (warp >> 2) & 1, first_warp = 8 + 4 * group;
+    const uint32_t scratch = sbase + kScratchOff + (warp - 8) * 640, stage = ks + group * kTileBytes;
+    const int step_blocks = 8 / lv.U, step_units = 8 - step_blocks * lv.U;
+    const Magic magic;
+    int kc = 0, made_tiles = 0;                          // tiles of the thread block before the segment; of this group so far
+    bool ok = true;
+    auto free_stage = [&]() { return group_wait(2 + group, 128, warp == first_warp, made_tiles == 0 ? -1 : kKEmpty + group, (uint32_t)(made_tiles - 1) & 1u); };
     auto made = [&]() {
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
-      if (lane == 0 && !(a.test_silent && kc == 0)) mbar_arrive(bar(kKFull + (kc & 1)));
-      ++kc;
+      if (lane == 0 && !(a.test_silent && group == 0 && made_tiles == 0)) mbar_arrive(bar(kKFull + group));
+      ++made_tiles;
     };
-    for (int n = 0; segment_there(n); ++n) {
+    for (int n = 0; group_wait(2 + group, 128, warp == first_warp, kSegFull + (n & 1), (uint32_t)(n >> 1) & 1u); ++n) {
       const Segment& sg = segments[n & 1];
       const int stream = sg.stream, j1 = sg.j1, packed_tiles = sg.packed_tiles, units = sg.units, r = sg.r, c0 = sg.c0, total = sg.total;
-      int j = sg.j0;
+      const int j0 = sg.j0;
       segment_taken(n);
       if (stream < 0) break;
-      const char *base = lv.base + (size_t)stream * lv.base_stride, *extras = lv.extras + (size_t)stream * lv.extras_stride;
-      const uint2* table = reinterpret_cast<const uint2*>(lv.table + (size_t)stream * lv.table_stride);
+      int j = j0 + ((kc ^ group) & 1);
       const int end = min(j1, packed_tiles);
-      auto entry_of = [&](int unit) { return table[block_of(min(unit, units - 1), inv_u)]; };
-      auto request = [&](int unit, uint2 entry) { return request_keys<kDense>(lv, base, extras, inv_u, min(unit, units - 1), entry, mt, lane); };
       if (j < end) {
-        uint2 entry = entry_of(4 * j + w), entry_next = entry_of(4 * j + 4 + w);
-        Packed p = request(4 * j + w, entry);
-        for (; j < end; ++j) {
-          if (!free_stage()) break;
-          if (warp == 8 && lane == 0) *progress = kc;
+        // the unit that is worked on, its promoted channels and codes; the next one's block's table entry
+        const char* extras = lv.extras + (size_t)stream * lv.extras_stride;
+        Cursor at(lv, stream, 4 * j + w);
+        Promoted more{};
+        PackedKeys p{};
+        if (at.unit < units) {
+          more = request_promoted<kDense>(extras, *at.entry, at.u, lane);
+          p = request_keys<kDense>(lv, at, more, lane);
+        }
+        for (; j < end; j += 2) {
+          Cursor next = at;
+          next.next(lv, 8, step_blocks, step_units);
+          uint2 entry = make_uint2(0u, 0u);
+          if (next.unit < units) entry = *next.entry;
+          if (!(ok = free_stage())) break;
+          if (w == 0 && lane == 0) *progress = kc + j - j0;
           // (past the last block the logits are masked, whatever the keys are)
-          if (4 * j + w < units) make_keys<kDense>(lv, base, extras, inv_u, p, 4 * j + w, entry, stage(), scratch, w, mt, lane);
-          entry = entry_next;
-          p = request(4 * j + 4 + w, entry);
-          entry_next = entry_of(4 * j + 8 + w);
+          if (at.unit < units) {
+            make_keys<kDense>(p, stage, scratch, w, lane, magic);
+            put_promoted<kDense>(lv, at, more, stage, w, lane);
+          }
+          at = next;
+          if (at.unit < units) {
+            more = request_promoted<kDense>(extras, entry, at.u, lane);
+            p = request_keys<kDense>(lv, at, more, lane);
+          }
           made();
         }
       }
-      for (; j < j1 && !dead; ++j) {
+      for (; j < j1 && ok; j += 2) {
         const Rows x{reinterpret_cast<const uint16_t*>(lv.resk + (size_t)stream * lv.resk_stride),
                      reinterpret_cast<const uint16_t*>(lv.sink + (size_t)stream * lv.sink_stride), a.k + (size_t)stream * a.stride * kD, r, c0, total};
-        if (!free_stage()) break;
-        if (warp == 8 && lane == 0) *progress = kc;
-        copy_key_rows(x, j - packed_tiles, stage(), w, mt, lane);
+        if (!(ok = free_stage())) break;
+        if (w == 0 && lane == 0) *progress = kc + j - j0;
+        copy_key_rows(x, j - packed_tiles, stage, w, lane);
         made();
       }
-      if (dead) break;
+      if (!ok) break;
+      kc += j1 - j0;
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 104;" ::: "memory");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 96;" ::: "memory");
     // ------------------------------------------------------------------ softmax and output rows
     const int slot = warp >> 2, row_in = tid & 127, g = lv.g;
     const uint32_t lane_base = tbase + ((uint32_t)((warp & 3) * 32) << 16);
@@ -788,7 +868,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
     auto all_wait = [&](int i, uint32_t parity) { return __all_sync(0xffffffffu, wait(i, parity)) != 0; };
     for (int n = 0;; ++n) {
       // (both slots are behind the segment before: the queries may go, and what slot 1 left there for slot 0)
-      if (!softmax_all(segment_there(n))) break;
+      if (!group_wait(1, kSoftmaxThreads, warp == 0, kSegFull + (n & 1), (uint32_t)(n >> 1) & 1u)) break;
       const Segment& sg = segments[n & 1];
       const int stream = sg.stream, j0 = sg.j0, j1 = sg.j1, packed_tiles = sg.packed_tiles, units = sg.units, c0 = sg.c0, rows_all = sg.rows_all;
       const int row0 = sg.row0, dual = sg.dual, whole = sg.whole, part_no = sg.part;
@@ -814,7 +894,8 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       tc_fence_before();
-      mbar_arrive(bar(kQFull));
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(kQFull));
       const int row = row0 + (dual ? slot * kTile + row_in : row_in & (per - 1));
       const int tok = min(row, rows_all - 1) / g;
       const bool idle = (row & ~31) >= rows_all;         // no row of the warp exists
@@ -822,7 +903,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       RowState state{-INFINITY, 0ull};
       bool ok = true, first = true;
       for (int j = j0 + (dual ? 0 : slot); j < j1; j += 2 - dual, ++cnt) {
-        ok = all_wait(kSFull + slot, (uint32_t)cnt & 1u);
+        ok = group_wait(4 + slot, kTile, (warp & 3) == 0, kSFull + slot, (uint32_t)cnt & 1u);
         if (!ok) break;
         tc_fence_after();
         if (!idle) {
@@ -834,7 +915,8 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
           first = false;
         }
         tc_fence_before();
-        mbar_arrive(bar(kPReady + slot));
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(kPReady + slot));
       }
       // ---- the segment's result
       const bool both = dual || j1 - j0 > 1;             // slot 1 had steps (slot 0 has in every segment)
