@@ -33,11 +33,11 @@ constexpr int kIssueWarp = 24;
 constexpr int kScratchOff = 6 * kTileBytes;               // per producer warp 640 bytes: scales and zero-points as fp16 pairs
 constexpr int kMlOff = kScratchOff + 16 * 640;            // slot 1's maxima and denominators (128 x 8 bytes)
 constexpr int kBarOff = kMlOff + 1024;
-constexpr int kBars = 20;
-constexpr int kReaders = 26;                              // of a segment: 8 softmax, 16 producer warps, the issuing thread, the L2 requests
+constexpr int kBars = 21;
+constexpr int kReaders = 26;                              // of a segment: 8 softmax, 16 producer warps, the issuing one, the L2 requests
 constexpr int kSegOff = kBarOff + 8 * kBars + 16;         // (the tensor-memory address and the producers' progress behind the barriers)
 constexpr int kSmem = kSegOff + 2 * 64;
-enum Bar { kQFull = 0, kKFull = 1, kVFull = 3, kKEmpty = 5, kVEmpty = 7, kSFull = 9, kPReady = 11, kODone = 13, kDone = 15, kSegFull = 16, kSegEmpty = 18 };
+enum Bar { kQFull = 0, kKFull = 1, kVFull = 3, kKEmpty = 5, kVEmpty = 7, kSFull = 9, kPReady = 11, kODone = 13, kDone = 15, kSegFull = 17, kSegEmpty = 19 };
 constexpr uint32_t kPolls = 1u << 21;
 constexpr float kRaise = 10.f;
 constexpr int kAhead = 8;
@@ -74,6 +74,14 @@ __device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, uint32
       : "=r"(ok)
       : "r"(bar), "r"(parity), "r"(max_polls)
       : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ bool phase_over(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(ok)
+               : "r"(bar), "r"(parity)
+               : "memory");
   return ok != 0;
 }
 __device__ __forceinline__ uint4 rows_to_half(uint4 x) {
@@ -399,13 +407,16 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&u)[32]) {
   tmem_ld32_issue(taddr, u);
   tmem_wait_ld32(u);
 }
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&w)[16]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr), "r"(w[0]),
-               "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]), "r"(w[8]), "r"(w[9]), "r"(w[10]), "r"(w[11]), "r"(w[12]),
-               "r"(w[13]), "r"(w[14]), "r"(w[15])
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&u)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7])
+               : "r"(taddr)
+               : "memory");
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(u[0]), "+r"(u[1]), "+r"(u[2]), "+r"(u[3]), "+r"(u[4]), "+r"(u[5]), "+r"(u[6]), "+r"(u[7])
+               :
                : "memory");
 }
-
 // The state of a row's softmax: its reference (in the log2 domain) and the sum of its probabilities, two halves.
 struct RowState {
   float m;
@@ -418,82 +429,80 @@ struct RowState {
 };
 
 // Raises the reference to at least mx: what lies in tensor memory on the old one is rescaled, the sums at o_addr (unless they are the first tile's, which
-// are not there yet) and `written` pieces of P at s_addr.  The products before this tile are complete: S is behind them in the tensor core's order.
-__device__ __forceinline__ void raise(uint32_t s_addr, uint32_t o_addr, int from, int written, bool first, float mx, RowState& row) {
+// are not there yet) and the pieces of P before `written` at s_addr.  The products before this tile are complete: S is behind them in the tensor core's order.
+__device__ __forceinline__ void raise(uint32_t s_addr, uint32_t o_addr, int written, bool first, float mx, RowState& row) {
   const float m_new = fmaxf(row.m, mx), alpha = m_new == -INFINITY ? 1.f : ex2(row.m - m_new);
   row.l = mul2(row.l, pack2(alpha, alpha));
   row.m = m_new;
   if (!first) {
 #pragma unroll 1
-    for (int d = 0; d < kD; d += 16) {
-      uint32_t u[16];
-      tmem_ld16_issue(o_addr + d, u);
-      tmem_wait_ld16(u);
+    for (int d = 0; d < kD; d += 8) {
+      uint32_t u[8];
+      tmem_ld8(o_addr + d, u);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) u[i] = __float_as_uint(__uint_as_float(u[i]) * alpha);
-      tmem_st16(o_addr + d, u);
+      for (int i = 0; i < 8; ++i) u[i] = __float_as_uint(__uint_as_float(u[i]) * alpha);
+      tmem_st8(o_addr + d, u);
     }
   }
   const __half2 a2 = __float2half2_rn(alpha);
 #pragma unroll 1
-  for (int h = from; h < written; ++h) {
+  for (int h = 0; h < 2 * written; ++h) {
     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-    uint32_t u[16];
-    tmem_ld16_issue(s_addr + 16 * h, u);
-    tmem_wait_ld16(u);
+    uint32_t u[8];
+    tmem_ld8(s_addr + 8 * h, u);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < 8; ++i) {
       const __half2 p = __hmul2(*reinterpret_cast<const __half2*>(&u[i]), a2);
       u[i] = *reinterpret_cast<const uint32_t*>(&p);
     }
-    tmem_st16(s_addr + 16 * h, u);
+    tmem_st8(s_addr + 8 * h, u);
   }
 }
 
 // One tile of one slot's softmax, in one pass: the thread's row of S (128 fp32 at s_addr) becomes P (fp16 pairs over the first 64 of those columns), 32
-// columns at a time.  Piece h of P lies inside the columns of S's pieces <= h.  The reference is raised only when a piece's
-// largest logit exceeds it by more than 2^kRaise: P stays below 2^10, far inside fp16, and that is rare behind the first tile.  The row's own pieces are
-// h0 .. h1 - 1 (another lane has the same row's others); P is zero in the others.  kMask: the row sees the columns <= last only.
+// columns at a time.  Piece h of P lies inside the columns of S's pieces <= h.  The reference is raised only when a piece's largest logit exceeds it by
+// more than 2^kRaise: P stays below 2^10, far inside fp16, and that is rare behind the first tile.  The row's own pieces are h0 .. h1 - 1 (another lane has
+// the same row's others); P is zero in the others.  kMask: the row sees the columns <= last only.
 template <bool kMask>
 __device__ __forceinline__ void softmax_tile(uint32_t s_addr, uint32_t o_addr, int h0, int h1, int last, bool first, float scale_log2e, RowState& row) {
   const uint64_t scale2 = pack2(scale_log2e, scale_log2e);
-  auto piece = [&](uint32_t (&u)[32], int h) {
-    const int lim = last - 32 * h;
-    float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+  for (int h = 0; h < 4; ++h) {
+    if (h >= h0 && h < h1) {
+      uint32_t u[32];
+      tmem_ld32(s_addr + 32 * h, u);
+      const int lim = last - 32 * h;
+      float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-    for (int i = 0; i < 32; i += 2) {
-      if (kMask) {
-        u[i] = i > lim ? 0xFF800000u : u[i];
-        u[i + 1] = i + 1 > lim ? 0xFF800000u : u[i + 1];
+      for (int i = 0; i < 32; i += 2) {
+        if (kMask) {
+          u[i] = i > lim ? 0xFF800000u : u[i];
+          u[i + 1] = i + 1 > lim ? 0xFF800000u : u[i + 1];
+        }
+        mx4[(i >> 1) & 3] = fmaxf(fmaxf(mx4[(i >> 1) & 3], __uint_as_float(u[i])), __uint_as_float(u[i + 1]));
       }
-      mx4[(i >> 1) & 3] = fmaxf(fmaxf(mx4[(i >> 1) & 3], __uint_as_float(u[i])), __uint_as_float(u[i + 1]));
-    }
-    const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * scale_log2e;
-    if (__any_sync(0xffffffffu, mx > row.m + kRaise)) raise(s_addr, o_addr, h0, h, first, mx, row);
-    const float ref = row.m == -INFINITY ? 0.f : row.m;        // a row that has seen no key yet: all its logits are -inf, its P is 0
-    const uint64_t ref2 = pack2(-ref, -ref);
-    uint32_t wd[16];
+      const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * scale_log2e;
+      if (__any_sync(0xffffffffu, mx > row.m + kRaise)) raise(s_addr, o_addr, h, first, mx, row);
+      const float ref = row.m == -INFINITY ? 0.f : row.m;      // a row that has seen no key yet: all its logits are -inf, its P is 0
+      const uint64_t ref2 = pack2(-ref, -ref);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float x0, x1;
-      unpack2(fma2(pack2u(u[2 * i], u[2 * i + 1]), scale2, ref2), x0, x1);
-      const float p0 = ex2(x0), p1 = ex2(x1);
-      row.l = add2(row.l, pack2(p0, p1));
-      wd[i] = pack_half2(p0, p1);
+      for (int k = 0; k < 2; ++k) {
+        uint32_t wd[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          float x0, x1;
+          unpack2(fma2(pack2u(u[16 * k + 2 * i], u[16 * k + 2 * i + 1]), scale2, ref2), x0, x1);
+          const float p0 = ex2(x0), p1 = ex2(x1);
+          row.l = add2(row.l, pack2(p0, p1));
+          wd[i] = pack_half2(p0, p1);
+        }
+        tmem_st8(s_addr + 16 * h + 8 * k, wd);
+      }
+    } else {
+      const uint32_t zero[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+      tmem_st8(s_addr + 16 * h, zero);
+      tmem_st8(s_addr + 16 * h + 8, zero);
     }
-    tmem_st16(s_addr + 16 * h, wd);
-  };
-#pragma unroll 1
-  for (int h = h0; h < h1; ++h) {
-    uint32_t u[32];
-    tmem_ld32(s_addr + 32 * h, u);
-    piece(u, h);
-  }
-  if (h1 - h0 < 4) {
-    const uint32_t zero[16] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
-#pragma unroll 1
-    for (int h = 0; h < 4; ++h)
-      if (h < h0 || h >= h1) tmem_st16(s_addr + 16 * h, zero);
   }
   asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
@@ -519,12 +528,24 @@ __device__ __forceinline__ void store_row(const ChunkArgs& a, size_t row, int d,
   }
 }
 
+// warps that arrive on a barrier
+__device__ constexpr int arrivals(int i) {
+  if (i == kQFull || i == kVFull || i == kVFull + 1) return 8;
+  if (i == kKFull || i == kKFull + 1 || i == kPReady || i == kPReady + 1) return 4;
+  return i == kSegEmpty || i == kSegEmpty + 1 ? kReaders : 1;
+}
+
 // What the roles need to know of a segment (a thread block's key tiles of one item); stream < 0: there is none left.
 struct Segment {
   int stream, j0, j1, packed_tiles;
   int units, r, c0, total;               // packed units; residual rows; residual and sink rows; unquantized rows that the item's rows may see
   int row0, rows_all, dual, whole;       // first row; rows of the stream; more than 128 rows; all of the item's key tiles
   int part, pad[3];                      // which of the thread block's two results
+};
+
+template <int n>
+struct Literal {
+  __host__ __device__ constexpr operator int() const { return n; }
 };
 
 // the first lane's value, the whole warp's
@@ -564,8 +585,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   if (tid == 0) {
-    for (int i = 0; i < kBars; ++i)
-      mbar_init(bar(i), i == kQFull || (i >= kVFull && i < kKEmpty) ? 8 : (i >= kKFull && i < kVFull) ? 4 : (i >= kPReady && i < kODone) ? 4 : (i >= kSegEmpty ? kReaders : 1));
+    for (int i = 0; i < kBars; ++i) mbar_init(bar(i), arrivals(i));
     *progress = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -605,64 +625,102 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
     asm volatile("setmaxnreg.dec.sync.aligned.u32 40;" ::: "memory");
     if (warp == kIssueWarp) {
       // ---------------------------------------------------------------- tensor-core issue
-      // (The whole warp goes through the loop and one lane issues: with one lane alone in here every descriptor is moved to the uniform registers word by
-      // word in front of its instruction.)
+      // The whole warp goes through the loops and one lane issues; slots and stages are literals, and tensor memory starts at 0 (all of it was allocated), so
+      // that descriptors and addresses are constants in uniform registers: moved there word by word, they took longer than the products.
       constexpr uint32_t kIdesc = make_idesc(128, 128, 0, 0), kIdescRows = make_idesc(128, 128, 0, 1);
-      const uint32_t tb = uniform(tbase), sb = uniform(sbase);
-      const uint64_t qd = make_desc(sb, 128, 2048), kd = make_desc(sb + 2 * kTileBytes, 128, 2048), vd = make_desc(sb + 4 * kTileBytes, 128, 2048);
-      constexpr uint64_t kStep = kTileBytes >> 4;        // a tile further, in a descriptor
       const bool leader = elect_one();
-      auto there = [&](int i, uint32_t parity) { return __all_sync(0xffffffffu, wait(i, parity)) != 0; };
-      auto commit = [&](int i) {
-        if (leader) tc_commit(bar(i));
+      auto there = [&](int i, uint32_t parity) {
+        if (__all_sync(0xffffffffu, phase_over(bar(i), parity))) return true;
+        return __all_sync(0xffffffffu, wait(i, parity)) != 0;
       };
-      int tile0 = 0, cnt[2] = {0, 0};                    // key tiles before the segment; steps per slot
+      uint32_t used = 0, cnt = 0;                        // bit st: parity of the tiles that stage st has had; bit slot: parity of the slot's steps
+      // S of `slot` from Q tile `qt` and key stage st; kLast: the stage's last use
+      auto issue_s = [&](auto slot_, auto st_, auto qt_, auto last_) {
+        constexpr int slot = slot_, st = st_, qt = qt_;
+        tc_fence_after();
+        if (leader) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            tc_mma_ss(128 * slot, make_desc(qs + qt * kTileBytes + 256 * i, 128, 2048), make_desc(ks + st * kTileBytes + 256 * i, 128, 2048), kIdesc, i > 0);
+          tc_commit(bar(kSFull + slot));
+          if (last_) tc_commit(bar(kKEmpty + st));
+        }
+      };
+      auto issue_o = [&](auto slot_, auto st_, auto last_, uint32_t idesc, bool first, bool end) {
+        constexpr int slot = slot_, st = st_;
+        if (!there(kPReady + slot, (cnt >> slot) & 1u)) return false;
+        cnt ^= 1u << slot;
+        tc_fence_after();
+        if (leader) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            tc_mma_ts(256 + 128 * slot, 128 * slot + 8 * i, make_desc(vs + st * kTileBytes + 256 * i, 128, 2048), idesc, i > 0 || !first);
+          if (last_) tc_commit(bar(kVEmpty + st));
+          if (end) tc_commit(bar(kODone + slot));
+        }
+        return true;
+      };
+      constexpr Literal<0> k0{};
+      constexpr Literal<1> k1{};
       for (int n = 0; there(kSegFull + (n & 1), (uint32_t)(n >> 1) & 1u); ++n) {
         const Segment& sg = segments[n & 1];
-        const int stream = uniform(sg.stream), nt = uniform(sg.j1 - sg.j0), packed = uniform(sg.packed_tiles - sg.j0), sh = uniform(sg.dual);
+        const int stream = uniform(sg.stream), nt = uniform(sg.j1 - sg.j0), packed = uniform(sg.packed_tiles - sg.j0), dual = uniform(sg.dual);
         segment_taken(n);
         if (stream < 0 || !there(kQFull, n & 1)) break;
-        tc_fence_after();
-        const int steps = nt << sh;                      // step u: slot u % 2, key tile u (more than 128 rows: u / 2) of the segment
-        auto issue_s = [&](int u) {
-          const int slot = u & 1, kc = tile0 + (u >> sh), st = kc & 1;
-          if (!there(kKFull + st, (uint32_t)(kc >> 1) & 1u)) return false;
-          tc_fence_after();
-          const uint64_t q = qd + (sh & slot ? kStep : 0), k = kd + (st ? kStep : 0);
-          const uint32_t d = tb + 128 * slot;
-          if (leader) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) tc_mma_ss(d, q + (uint64_t)(16 * i), k + (uint64_t)(16 * i), kIdesc, i > 0);
+        auto keys_there = [&](int st) { return there(kKFull + st, (used >> st) & 1u); };
+        auto idesc_of = [&](int j) { return j < packed ? kIdesc : kIdescRows; };
+        bool ok;
+        if (dual) {
+          // tile j in stage j % 2, both slots: S(slot, j + 1) goes in behind O(slot, j)
+          auto tile = [&](auto st, auto next, int j) {
+            const uint32_t idesc = idesc_of(j);
+            const bool more = j + 1 < nt;
+            if (!there(kVFull + st, (used >> st) & 1u)) return false;
+            used ^= 1u << st;
+            if (!issue_o(k0, st, k0, idesc, j == 0, !more)) return false;
+            if (more) {
+              if (!keys_there(next)) return false;
+              issue_s(k0, next, k0, k0);
+            }
+            if (!issue_o(k1, st, k1, idesc, j == 0, !more)) return false;
+            if (more) issue_s(k1, next, k1, k1);
+            return true;
+          };
+          ok = keys_there(0);
+          if (ok) {
+            issue_s(k0, k0, k0, k0);
+            issue_s(k1, k0, k1, k1);
           }
-          commit(kSFull + slot);
-          if (sh <= slot) commit(kKEmpty + st);
-          return true;
-        };
-        auto issue_o = [&](int u) {
-          const int slot = u & 1, j = u >> sh, kc = tile0 + j, st = kc & 1;
-          if (!there(kVFull + st, (uint32_t)(kc >> 1) & 1u) || !there(kPReady + slot, (uint32_t)cnt[slot] & 1u)) return false;
-          cnt[slot] += 1;
-          tc_fence_after();
-          const uint64_t v = vd + (st ? kStep : 0);
-          const uint32_t o = tb + 256 + 128 * slot, p = tb + 128 * slot, idesc = j < packed ? kIdesc : kIdescRows;
-          if (leader) {
-            tc_mma_ts(o, p, v, idesc, u > 1);
-#pragma unroll
-            for (int i = 1; i < 8; ++i) tc_mma_ts(o, p + 8 * i, v + (uint64_t)(16 * i), idesc, 1);
+          for (int j = 0; ok && j < nt; j += 2) {
+            ok = tile(k0, k1, j);
+            if (ok && j + 1 < nt) ok = tile(k1, k0, j + 1);
           }
-          if (sh <= slot) commit(kVEmpty + st);
-          if (u + 2 >= steps) commit(kODone + slot);
-          return true;
-        };
-        bool ok = issue_s(0);
-        if (ok && steps > 1) ok = issue_s(1);
-        for (int u = 0; ok && u < steps; ++u) {
-          ok = issue_o(u);
-          if (ok && u + 2 < steps) ok = issue_s(u + 2);
+        } else {
+          // tile j in stage and slot j % 2: S(j + 2) goes in behind O(j)
+          auto tile = [&](auto st, int j) {
+            if (!there(kVFull + st, (used >> st) & 1u)) return false;
+            used ^= 1u << st;
+            if (!issue_o(st, st, k1, idesc_of(j), j < 2, j + 2 >= nt)) return false;
+            if (j + 2 < nt) {
+              if (!keys_there(st)) return false;
+              issue_s(st, st, k0, k1);
+            }
+            return true;
+          };
+          ok = keys_there(0);
+          if (ok) issue_s(k0, k0, k0, k1);
+          if (ok && nt > 1) {
+            ok = keys_there(1);
+            if (ok) issue_s(k1, k1, k0, k1);
+          }
+          for (int j = 0; ok && j < nt; j += 2) {
+            ok = tile(k0, j);
+            if (ok && j + 1 < nt) ok = tile(k1, j + 1);
+          }
         }
-        tile0 += nt;
+        if (!ok) break;
       }
-      commit(kDone);                                     // every product issued above has finished when this one fires
+      if (leader) tc_commit(bar(kDone));                 // every product issued above has finished when this one fires
       dead = false;
       there(kDone, 0);
     } else if (warp == kIssueWarp + 1 && lane == 0) {
@@ -746,15 +804,19 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
     const int step_blocks = 4 / lv.U, step_units = 4 - step_blocks * lv.U;
     const uint32_t meta0 = 2048 + 4 * (lane * lv.VG + (lv.VG == 4 ? 2 * half : lv.VG == 2 ? half : 0)), meta1 = meta0 + (lv.VG == 4 ? 4 : 0);
     const Magic magic;
-    int kc = 0;
+    uint32_t st = 0, had[2] = {0, 0};                    // the tile's stage (a segment starts in stage 0); tiles that each stage has had
     bool ok = true;
-    auto stage = [&]() { return vs + (kc & 1) * kTileBytes; };
-    auto free_stage = [&]() { return group_wait(6, 256, warp == 16, kc < 2 ? -1 : kVEmpty + (kc & 1), (uint32_t)((kc >> 1) - 1) & 1u); };
+    auto stage = [&]() { return vs + st * kTileBytes; };
+    auto free_stage = [&]() {
+      const uint32_t h = st ? had[1] : had[0];
+      return group_wait(6, 256, warp == 16, h == 0 ? -1 : (int)(kVEmpty + st), (h - 1) & 1u);
+    };
     auto made = [&]() {
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar(kVFull + (kc & 1)));
-      ++kc;
+      if (lane == 0) mbar_arrive(bar(kVFull + st));
+      if (st) ++had[1]; else ++had[0];
+      st ^= 1;
     };
     for (int n = 0; group_wait(6, 256, warp == 16, kSegFull + (n & 1), (uint32_t)(n >> 1) & 1u); ++n) {
       const Segment& sg = segments[n & 1];
@@ -762,6 +824,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       int j = sg.j0;
       segment_taken(n);
       if (stream < 0) break;
+      st = 0;
       const int end = min(j1, packed_tiles);
       if (j < end) {
         Cursor at(lv, stream, 4 * j + w);
@@ -794,12 +857,12 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
   } else if (warp >= 8) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 80;" ::: "memory");
     // ------------------------------------------------------------------ key tiles
-    // (the group's tiles are the even or the odd ones of the thread block, counted through all segments: it has one stage to itself)
+    // (the group's tiles are the even or the odd ones of every segment: it has one stage to itself)
     const int w = warp & 3, group = (warp >> 2) & 1, first_warp = 8 + 4 * group;
     const uint32_t scratch = sbase + kScratchOff + (warp - 8) * 640, stage = ks + group * kTileBytes;
     const int step_blocks = 8 / lv.U, step_units = 8 - step_blocks * lv.U;
     const Magic magic;
-    int kc = 0, made_tiles = 0;                          // tiles of the thread block before the segment; of this group so far
+    int kc = 0, made_tiles = 0;                          // tiles of the thread block before the segment; tiles that this group has made
     bool ok = true;
     auto free_stage = [&]() { return group_wait(2 + group, 128, warp == first_warp, made_tiles == 0 ? -1 : kKEmpty + group, (uint32_t)(made_tiles - 1) & 1u); };
     auto made = [&]() {
@@ -814,7 +877,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       const int j0 = sg.j0;
       segment_taken(n);
       if (stream < 0) break;
-      int j = j0 + ((kc ^ group) & 1);
+      int j = j0 + group;
       const int end = min(j1, packed_tiles);
       if (j < end) {
         // the unit that is worked on, its promoted channels and codes; the next one's block's table entry
@@ -869,18 +932,20 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
     for (int n = 0;; ++n) {
       // (both slots are behind the segment before: the queries may go, and what slot 1 left there for slot 0)
       if (!group_wait(1, kSoftmaxThreads, warp == 0, kSegFull + (n & 1), (uint32_t)(n >> 1) & 1u)) break;
-      const Segment& sg = segments[n & 1];
-      const int stream = sg.stream, j0 = sg.j0, j1 = sg.j1, packed_tiles = sg.packed_tiles, units = sg.units, c0 = sg.c0, rows_all = sg.rows_all;
-      const int row0 = sg.row0, dual = sg.dual, whole = sg.whole, part_no = sg.part;
-      segment_taken(n);
-      if (stream < 0) break;
+      // (read again where it is needed: the tiles' loop has no registers to keep it in)
+      const volatile Segment& sg = segments[n & 1];
+      if (sg.stream < 0) break;
       // Rows of a tile: with more than 128 rows slot 0 has the first 128 of them and slot 1 the others.  Otherwise both have the same ones, and with at most
       // 64 (32) every row 2 (4) times over, 64 (32) lanes apart, each copy for a half (a quarter) of the tile's keys: a warp's softmax is that much
       // shorter, and the copies' results meet at the end like the slots'.
-      const int rows = min(rows_all - row0, kChunkRows), lg_copies = dual || rows > 64 ? 0 : rows > 32 ? 1 : 2, per = kTile >> lg_copies;
+      auto copies_of = [&]() {
+        const int rows = sg.rows_all - sg.row0;
+        return rows > 64 ? 0 : rows > 32 ? 1 : 2;
+      };
       {
+        const int row0 = sg.row0, rows_all = sg.rows_all, dual = sg.dual, per = kTile >> copies_of();
         // 16-byte piece p of the image: lane 8 (p / 128) + p % 8, channels 8 (p / 8 % 16) ..
-        const uint16_t* qb = a.q + (size_t)stream * g * a.stride * kD;
+        const uint16_t* qb = a.q + (size_t)sg.stream * g * a.stride * kD;
 #pragma unroll 4
         for (int p = tid; p < 2048 << dual; p += kSoftmaxThreads) {
           const int at = 8 * (p >> 7) + (p & 7), row = row0 + (dual ? at : at & (per - 1)), c = (p >> 3) & 15;
@@ -896,42 +961,52 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(kQFull));
-      const int row = row0 + (dual ? slot * kTile + row_in : row_in & (per - 1));
-      const int tok = min(row, rows_all - 1) / g;
-      const bool idle = (row & ~31) >= rows_all;         // no row of the warp exists
-      const int h0 = (row_in >> (7 - lg_copies)) << (2 - lg_copies), h1 = h0 + (4 >> lg_copies);
       RowState state{-INFINITY, 0ull};
-      bool ok = true, first = true;
-      for (int j = j0 + (dual ? 0 : slot); j < j1; j += 2 - dual, ++cnt) {
-        ok = group_wait(4 + slot, kTile, (warp & 3) == 0, kSFull + slot, (uint32_t)cnt & 1u);
-        if (!ok) break;
-        tc_fence_after();
-        if (!idle) {
-          const int last = j < packed_tiles ? 32 * (units - 4 * j) - 1 : c0 + tok - kTile * (j - packed_tiles);
-          if (__all_sync(0xffffffffu, last >= kTile - 1))
-            softmax_tile<false>(s_addr, o_addr, h0, h1, 0, first, a.scale_log2e, state);
-          else
-            softmax_tile<true>(s_addr, o_addr, h0, h1, last, first, a.scale_log2e, state);
-          first = false;
+      bool ok = true;
+      {
+        const int dual = sg.dual, lg_copies = copies_of(), step = 2 - dual, j1 = sg.j1, packed_tiles = sg.packed_tiles, units = sg.units;
+        const int row = sg.row0 + (dual ? slot * kTile + row_in : row_in & ((kTile >> lg_copies) - 1));
+        const bool idle = (row & ~31) >= sg.rows_all;    // no row of the warp exists
+        const int sees = sg.c0 + min(row, sg.rows_all - 1) / g + kTile * packed_tiles;          // the last unquantized row that the row sees
+        const int h0 = (row_in >> (7 - lg_copies)) << (2 - lg_copies), h1 = h0 + (4 >> lg_copies);
+        bool first = true;
+        for (int j = sg.j0 + (dual ? 0 : slot); j < j1; j += step, ++cnt) {
+          ok = group_wait(4 + slot, kTile, (warp & 3) == 0, kSFull + slot, (uint32_t)cnt & 1u);
+          if (!ok) break;
+          tc_fence_after();
+          if (!idle) {
+            const int last = (j < packed_tiles ? 32 * units - 1 : sees) - kTile * j;
+            if (__all_sync(0xffffffffu, last >= kTile - 1))
+              softmax_tile<false>(s_addr, o_addr, h0, h1, 0, first, a.scale_log2e, state);
+            else
+              softmax_tile<true>(s_addr, o_addr, h0, h1, last, first, a.scale_log2e, state);
+            first = false;
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(kPReady + slot));
         }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(kPReady + slot));
       }
       // ---- the segment's result
-      const bool both = dual || j1 - j0 > 1;             // slot 1 had steps (slot 0 has in every segment)
+      const int stream = sg.stream, dual = sg.dual, row0 = sg.row0, rows_all = sg.rows_all, whole = sg.whole;
+      const int rows = min(rows_all - row0, kChunkRows), lg_copies = copies_of(), per = kTile >> lg_copies;
+      const int row = row0 + (dual ? slot * kTile + row_in : row_in & (per - 1));
+      const bool idle = (row & ~31) >= rows_all;
+      const bool both = dual || sg.j1 - sg.j0 > 1;       // slot 1 had steps (slot 0 has in every segment)
       bool mine = ok && (slot == 0 || both) && all_wait(kODone + slot, (uint32_t)ended[slot] & 1u);
       if (!dual && both) mine = all_wait(kODone + 1 - slot, (uint32_t)ended[1 - slot] & 1u) && mine;      // (the sums go where the queries were)
       tc_fence_after();
       ended[0] += 1;
       ended[1] += both;
-      float* part = a.parts + ((size_t)blockIdx.x * 2 + part_no) * a.rows_cap * (kD + 2);
+      float* part = a.parts + ((size_t)blockIdx.x * 2 + sg.part) * a.rows_cap * (kD + 2);
+      segment_taken(n);
       const float l_run = mine ? state.sum() : 0.f, m_run = mine ? state.m : -INFINITY;
       auto weight = [](float m, float l, float top) { return m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : ex2(m - top); };   // (a row of NaNs counts)
       if (dual) {
         if (!idle) {
           const bool exists = row < rows_all;
           const float inv = whole ? (l_run == 0.f ? 0.f : 1.f / l_run) : l_run == 0.f ? 0.f : 1.f;
+          const int tok = min(row, rows_all - 1) / g;
           const size_t orow = ((size_t)stream * g + (row - tok * g)) * a.stride + tok;
 #pragma unroll 1
           for (int d = 0; d < kD; d += 32) {
