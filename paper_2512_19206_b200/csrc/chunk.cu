@@ -27,7 +27,7 @@ namespace {
 
 constexpr int kTile = kChunkTile;
 constexpr int kTileBytes = kTile * kD * 2;
-constexpr int kThreads = 896;                             // 72 registers a thread at launch: 64512, shared out below as 256 x 96, 256 x 80, 256 x 56, 128 x 40
+constexpr int kThreads = 896;                             // 72 registers a thread at launch: 64512, shared out below as 256 x 112, 256 x 72, 256 x 48, 128 x 40
 constexpr int kSoftmaxThreads = 256;
 constexpr int kIssueWarp = 24;
 constexpr int kScratchOff = 6 * kTileBytes;               // per producer warp 640 bytes: scales and zero-points as fp16 pairs
@@ -41,6 +41,7 @@ enum Bar { kQFull = 0, kKFull = 1, kVFull = 3, kKEmpty = 5, kVEmpty = 7, kSFull 
 constexpr uint32_t kPolls = 1u << 21;
 constexpr float kRaise = 10.f;
 constexpr int kAhead = 8;
+constexpr int kProducerNap = 40;
 
 __device__ __forceinline__ void sts32(uint32_t a, uint32_t x) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(a), "r"(x) : "memory"); }
 __device__ __forceinline__ void sts16(uint32_t a, uint32_t x) { asm volatile("st.shared.u16 [%0], %1;" ::"r"(a), "h"((uint16_t)x) : "memory"); }
@@ -57,25 +58,6 @@ __device__ __forceinline__ uint32_t hfma2_u(uint32_t a, uint32_t b, uint32_t c) 
   asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
   return d;
 }
-// Polls a phase of a barrier up to max_polls times; false if it never completed.  (Without a time hint: with one the instruction becomes a loop of
-// sleeps and polls, and two dozen waiting warps took half of the SM's issue slots.)
-__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, uint32_t max_polls) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\tmov.u32 n, 0;\n"
-      "CHUNK_WAIT:\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "@p bra CHUNK_DONE;\n\t"
-      "add.u32 n, n, 1;\n\t"
-      "setp.lt.u32 q, n, %3;\n\t"
-      "@q bra CHUNK_WAIT;\n"
-      "CHUNK_DONE:\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity), "r"(max_polls)
-      : "memory");
-  return ok != 0;
-}
 __device__ __forceinline__ bool phase_over(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
@@ -83,6 +65,18 @@ __device__ __forceinline__ bool phase_over(uint32_t bar, uint32_t parity) {
                : "r"(bar), "r"(parity)
                : "memory");
   return ok != 0;
+}
+// Polls a phase of a barrier up to max_polls times; false if it never completed.  (Without a time hint: with one the instruction becomes a loop of
+// sleeps and polls.)  Who has time sleeps `ns` nanoseconds after a poll: a poll returns after a few dozen cycles, and those of the warps that wait for most
+// of the time took a third of the SM's issue slots.
+template <int ns>
+__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, uint32_t max_polls) {
+#pragma unroll 1
+  for (uint32_t n = 0;; ++n) {
+    if (phase_over(bar, parity)) return true;
+    if (n >= max_polls) return false;
+    if (ns > 0) __nanosleep(ns);
+  }
 }
 __device__ __forceinline__ uint4 rows_to_half(uint4 x) {
   return make_uint4(bf16x2_to_f16x2(x.x), bf16x2_to_f16x2(x.y), bf16x2_to_f16x2(x.z), bf16x2_to_f16x2(x.w));
@@ -110,6 +104,25 @@ __device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t b, uint32_t c) {
   asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
   return d;
 }
+// Products whose operands' descriptors (canonical layout, 128 bytes and 2048 bytes between core matrices) are given by their low words, address / 16 with the
+// first distance: neighbouring steps differ by one 32-bit addition.
+constexpr uint32_t kDescHi = (2048 >> 4) | (1u << 14);
+__device__ __forceinline__ uint32_t desc_lo(uint32_t saddr) { return ((saddr >> 4) & 0x3FFFu) | ((128u >> 4) << 16); }
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}" ::"r"(d),
+      "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "n"(kDescHi)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a_tmem, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 b, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}" ::"r"(d),
+      "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"(accumulate), "n"(kDescHi)
+      : "memory");
+}
+
 struct Magic {                           // the fp16 pairs 1024 and -1024, kept in registers (as literals each use cost a move)
   uint32_t plus, minus;
   __device__ __forceinline__ Magic() {
@@ -446,7 +459,7 @@ __device__ __forceinline__ void raise(uint32_t s_addr, uint32_t o_addr, int writ
   }
   const __half2 a2 = __float2half2_rn(alpha);
 #pragma unroll 1
-  for (int h = 0; h < 2 * written; ++h) {
+  for (int h = 0; h < 4 * written; ++h) {
     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
     uint32_t u[8];
     tmem_ld8(s_addr + 8 * h, u);
@@ -467,14 +480,19 @@ template <bool kMask>
 __device__ __forceinline__ void softmax_tile(uint32_t s_addr, uint32_t o_addr, int h0, int h1, int last, bool first, float scale_log2e, RowState& row) {
   const uint64_t scale2 = pack2(scale_log2e, scale_log2e);
 #pragma unroll 1
-  for (int h = 0; h < 4; ++h) {
-    if (h >= h0 && h < h1) {
-      uint32_t u[32];
-      tmem_ld32(s_addr + 32 * h, u);
-      const int lim = last - 32 * h;
+  for (int h = 0; h < 2; ++h) {
+    if (2 * h >= h0 && 2 * h < h1) {
+      uint32_t u[64];
+      uint32_t(&ua)[32] = *reinterpret_cast<uint32_t(*)[32]>(&u[0]);
+      uint32_t(&ub)[32] = *reinterpret_cast<uint32_t(*)[32]>(&u[32]);
+      tmem_ld32_issue(s_addr + 64 * h, ua);
+      tmem_ld32_issue(s_addr + 64 * h + 32, ub);
+      tmem_wait_ld32(ua);
+      tmem_wait_ld32(ub);
+      const int lim = last - 64 * h;
       float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-      for (int i = 0; i < 32; i += 2) {
+      for (int i = 0; i < 64; i += 2) {
         if (kMask) {
           u[i] = i > lim ? 0xFF800000u : u[i];
           u[i + 1] = i + 1 > lim ? 0xFF800000u : u[i + 1];
@@ -486,22 +504,26 @@ __device__ __forceinline__ void softmax_tile(uint32_t s_addr, uint32_t o_addr, i
       const float ref = row.m == -INFINITY ? 0.f : row.m;      // a row that has seen no key yet: all its logits are -inf, its P is 0
       const uint64_t ref2 = pack2(-ref, -ref);
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
+      for (int k = 0; k < 4; ++k) {
         uint32_t wd[8];
+        uint64_t l2 = 0ull;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           float x0, x1;
           unpack2(fma2(pack2u(u[16 * k + 2 * i], u[16 * k + 2 * i + 1]), scale2, ref2), x0, x1);
           const float p0 = ex2(x0), p1 = ex2(x1);
-          row.l = add2(row.l, pack2(p0, p1));
+          l2 = add2(l2, pack2(p0, p1));
           wd[i] = pack_half2(p0, p1);
         }
-        tmem_st8(s_addr + 16 * h + 8 * k, wd);
+        row.l = add2(row.l, l2);
+        tmem_st8(s_addr + 32 * h + 8 * k, wd);
       }
     } else {
       const uint32_t zero[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
-      tmem_st8(s_addr + 16 * h, zero);
-      tmem_st8(s_addr + 16 * h + 8, zero);
+      tmem_st8(s_addr + 32 * h, zero);
+      tmem_st8(s_addr + 32 * h + 8, zero);
+      tmem_st8(s_addr + 32 * h + 16, zero);
+      tmem_st8(s_addr + 32 * h + 24, zero);
     }
   }
   asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
@@ -545,6 +567,7 @@ struct Segment {
 
 template <int n>
 struct Literal {
+  static constexpr int value = n;
   __host__ __device__ constexpr operator int() const { return n; }
 };
 
@@ -596,18 +619,19 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
   dependency_wait();
   // tensor-memory columns: S / P of slot 0 at 0, of slot 1 at 128, O of slot 0 at 256, of slot 1 at 384
   bool dead = false;
-  auto wait = [&](int i, uint32_t parity) {
-    if (!dead && !wait_phase(bar(i), parity, a.max_polls)) {
+  auto wait_ns = [&](auto ns, int i, uint32_t parity) {
+    if (!dead && !wait_phase<decltype(ns)::value>(bar(i), parity, a.max_polls)) {
       dead = true;
       atomicOr(lv.status, (uint32_t)MIXKVQ_DEV_COPY_TIMEOUT);
     }
     return !dead;
   };
+  auto wait = [&](int i, uint32_t parity) { return wait_ns(Literal<0>{}, i, parity); };
   // The same for a group of `threads` threads: one warp polls, the others wait for it in the named barrier `id`, which costs no issue slots (two dozen
   // polling warps took a third of them).  The polling warp comes to the barrier in any case, and all learn what it saw.
   auto group_wait = [&](int id, int threads, bool polls, int i, uint32_t parity) {
     uint32_t ok = 1;
-    if (polls && i >= 0) ok = wait(i, parity);
+    if (polls && i >= 0) ok = wait_ns(Literal<kProducerNap>{}, i, parity);
     asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %0, 0;\n\tbarrier.cta.red.and.pred q, %1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
                  : "+r"(ok)
                  : "r"(id), "r"(threads)
@@ -615,7 +639,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
     return ok != 0;
   };
   // the n-th segment is there; (a reader's warp has taken what it needs)
-  auto segment_there = [&](int n) { return wait(kSegFull + (n & 1), (uint32_t)(n >> 1) & 1u); };
+  auto segment_there = [&](int n) { return wait_ns(Literal<200>{}, kSegFull + (n & 1), (uint32_t)(n >> 1) & 1u); };
   auto segment_taken = [&](int n) {
     __syncwarp();
     if (lane == 0) mbar_arrive(bar(kSegEmpty + (n & 1)));
@@ -628,6 +652,8 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       // The whole warp goes through the loops and one lane issues; slots and stages are literals, and tensor memory starts at 0 (all of it was allocated), so
       // that descriptors and addresses are constants in uniform registers: moved there word by word, they took longer than the products.
       constexpr uint32_t kIdesc = make_idesc(128, 128, 0, 0), kIdescRows = make_idesc(128, 128, 0, 1);
+      constexpr uint32_t kStep = kTileBytes >> 4;        // a tile further, in a descriptor
+      const uint32_t qd = desc_lo(qs), kd = desc_lo(ks), vd = desc_lo(vs);
       const bool leader = elect_one();
       auto there = [&](int i, uint32_t parity) {
         if (__all_sync(0xffffffffu, phase_over(bar(i), parity))) return true;
@@ -641,7 +667,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
         if (leader) {
 #pragma unroll
           for (int i = 0; i < 8; ++i)
-            tc_mma_ss(128 * slot, make_desc(qs + qt * kTileBytes + 256 * i, 128, 2048), make_desc(ks + st * kTileBytes + 256 * i, 128, 2048), kIdesc, i > 0);
+            mma_ss(128 * slot, qd + qt * kStep + 16 * i, kd + st * kStep + 16 * i, kIdesc, i > 0);
           tc_commit(bar(kSFull + slot));
           if (last_) tc_commit(bar(kKEmpty + st));
         }
@@ -654,7 +680,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
         if (leader) {
 #pragma unroll
           for (int i = 0; i < 8; ++i)
-            tc_mma_ts(256 + 128 * slot, 128 * slot + 8 * i, make_desc(vs + st * kTileBytes + 256 * i, 128, 2048), idesc, i > 0 || !first);
+            mma_ts(256 + 128 * slot, 128 * slot + 8 * i, vd + st * kStep + 16 * i, idesc, i > 0 || !first);
           if (last_) tc_commit(bar(kVEmpty + st));
           if (end) tc_commit(bar(kODone + slot));
         }
@@ -729,7 +755,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       const long long begin = chunk_begin(a.total, a.ctas, blockIdx.x), end = chunk_begin(a.total, a.ctas, blockIdx.x + 1);
       int n = 0;
       auto publish = [&](const Segment& sg) {
-        if (n >= 2 && !wait(kSegEmpty + (n & 1), (uint32_t)((n >> 1) - 1) & 1u)) return false;
+        if (n >= 2 && !wait_ns(Literal<500>{}, kSegEmpty + (n & 1), (uint32_t)((n >> 1) - 1) & 1u)) return false;
         segments[n & 1] = sg;
         mbar_arrive(bar(kSegFull + (n & 1)));
         n += 1;
@@ -797,7 +823,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       }
     }
   } else if (warp >= 16) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;" ::: "memory");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;" ::: "memory");
     // ------------------------------------------------------------------ value tiles
     const int w = (warp >> 1) & 3, half = warp & 1;
     const uint32_t scratch = sbase + kScratchOff + (warp - 8) * 640;
@@ -855,7 +881,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       if (!ok) break;
     }
   } else if (warp >= 8) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 80;" ::: "memory");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;" ::: "memory");
     // ------------------------------------------------------------------ key tiles
     // (the group's tiles are the even or the odd ones of every segment: it has one stage to itself)
     const int w = warp & 3, group = (warp >> 2) & 1, first_warp = 8 + 4 * group;
@@ -921,7 +947,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       kc += j1 - j0;
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 96;" ::: "memory");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 112;" ::: "memory");
     // ------------------------------------------------------------------ softmax and output rows
     const int slot = warp >> 2, row_in = tid & 127, g = lv.g;
     const uint32_t lane_base = tbase + ((uint32_t)((warp & 3) * 32) << 16);
@@ -940,7 +966,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       // shorter, and the copies' results meet at the end like the slots'.
       auto copies_of = [&]() {
         const int rows = sg.rows_all - sg.row0;
-        return rows > 64 ? 0 : rows > 32 ? 1 : 2;
+        return rows > 64 ? 0 : 1;
       };
       {
         const int row0 = sg.row0, rows_all = sg.rows_all, dual = sg.dual, per = kTile >> copies_of();
