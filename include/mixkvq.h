@@ -57,6 +57,7 @@ enum {
                                          channels then read as 0 and its UINT4 channels lose their high plane, so the
                                          layer's attention is wrong from that block on, until the cache is reset
                                          (with a larger extras_budget_bytes).  Earlier blocks are unaffected            */
+  MIXKVQ_DEV_BAD_POSITION = 4,        /* a rotation with several axes met a coordinate beyond the tables: that token's rows were left alone */
   MIXKVQ_DEV_COPY_TIMEOUT = 2         /* a bounded wait (for a staged bulk copy, or for the partner warp of a pair) ran out:
                                          the warps concerned contributed nothing to that call's output, which is
                                          therefore wrong (0 where no warp contributed); later calls are unaffected    */
@@ -274,6 +275,31 @@ int mixkvq_rope_append(mixkvq_cache* cache, int layer, void* k_dev, const void* 
 int mixkvq_rope_decode_step(mixkvq_cache* cache, int layer, void* k_dev, const void* v_dev, void* q_dev,
                             const float* cos_dev, const float* sin_dev, int pos, float* out_dev, float softmax_scale,
                             void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* The rotation for tokens with several coordinates (time, height, width of an image patch or a video frame; up to MIXKVQ_ROPE_MAX_AXES axes, and a
+ * position of its own for every sequence): channel pair (i, i + 64) of token j of sequence b turns by row positions_dev[axis_of_pair_host[i]][b][j] of the
+ * tables.  Arithmetic, pairing and tables as for mixkvq_rope_append; n_positions is the tables' number of rows.
+ *   positions_dev [n_axes, B, n_tokens] int32, DEVICE.  A token with a negative coordinate on an axis that some pair uses is none (padding of
+ *   a ragged batch): its rows of the outputs are left as they are.  So are those of a token with a coordinate of n_positions or more, and that sets
+ *   MIXKVQ_DEV_BAD_POSITION.
+ *   axis_of_pair_host [64]: HOST array, every entry below n_axes.
+ * mixkvq_rope_axes is stateless but for the status word: from q_dev, k_dev (and v_dev, which is copied; NULL with v_out_dev NULL: left out) in any
+ * layout whose last dimension is contiguous, the fused projection's [B, n, Hq + 2 Hkv, 128] included, to head-major
+ * q_out_dev [B, Hq, n, 128], k_out_dev, v_out_dev [B, Hkv, n, 128]: what the append, prefill and chunk calls take.
+ *   strides_host [9]: HOST array, the distances in elements from one batch element, head and token to the next, for q, k, v in turn (0 or more,
+ *   multiples of 8); NULL: head-major.  An output may be its own input where that is head-major; no output may overlap anything else
+ *   (MIXKVQ_E_INVALID_ARG).
+ * mixkvq_rope_axes_append and mixkvq_rope_axes_decode_step rotate k_dev and q_dev in place and then do what mixkvq_quantize_append and
+ * mixkvq_decode_step do (one more launch than mixkvq_rope_decode_step); on MIXKVQ_E_CAPACITY nothing was rotated. */
+#define MIXKVQ_ROPE_MAX_AXES 4
+int mixkvq_rope_axes(mixkvq_cache* cache, const void* q_dev, const void* k_dev, const void* v_dev, const int64_t* strides_host, int n_tokens,
+                     const float* cos_dev, const float* sin_dev, int n_positions, const int32_t* positions_dev, int n_axes,
+                     const uint8_t* axis_of_pair_host, void* q_out_dev, void* k_out_dev, void* v_out_dev, void* stream);
+int mixkvq_rope_axes_append(mixkvq_cache* cache, int layer, void* k_dev, const void* v_dev, void* q_dev, const float* cos_dev, const float* sin_dev,
+                            int n_positions, const int32_t* positions_dev, int n_axes, const uint8_t* axis_of_pair_host, int n_tokens, void* stream);
+int mixkvq_rope_axes_decode_step(mixkvq_cache* cache, int layer, void* k_dev, const void* v_dev, void* q_dev, const float* cos_dev, const float* sin_dev,
+                                 int n_positions, const int32_t* positions_dev, int n_axes, const uint8_t* axis_of_pair_host, float* out_dev,
+                                 float softmax_scale, void* workspace_dev, size_t workspace_bytes, void* stream);
 
 /* (The paper has no counterpart of this entry point; it exists for integration reasons only.)
  * Same computation and same results as mixkvq_decode_attention, for callers that have no way to hand

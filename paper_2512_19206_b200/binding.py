@@ -20,10 +20,10 @@ EXPORTS = [
     "mixkvq_select_channels", "mixkvq_select_channels_raw", "mixkvq_quantize_append",
     "mixkvq_decode_attention", "mixkvq_decode_attention_noalloc", "mixkvq_decode_step", "mixkvq_set_attention_kernel", "mixkvq_query_status",
     "mixkvq_cache_describe", "mixkvq_last_attention", "mixkvq_last_attention_ctas", "mixkvq_launch_count", "mixkvq_status_string",
-    "mixkvq_cache_written_externally", "mixkvq_test_arm_copy_timeout", "mixkvq_test_arm_value_copy_timeout", "mixkvq_rope_append", "mixkvq_rope_decode_step", "mixkvq_prefill", "mixkvq_prefill_scratch_bytes", "mixkvq_chunk_attention", "mixkvq_chunk_step", "mixkvq_chunk_scratch_bytes", "mixkvq_quantize_append_ragged", "mixkvq_sequence_fill", "mixkvq_decode_attention_partial", "mixkvq_merge_partials",
+    "mixkvq_cache_written_externally", "mixkvq_test_arm_copy_timeout", "mixkvq_test_arm_value_copy_timeout", "mixkvq_rope_append", "mixkvq_rope_decode_step", "mixkvq_prefill", "mixkvq_prefill_scratch_bytes", "mixkvq_chunk_attention", "mixkvq_chunk_step", "mixkvq_chunk_scratch_bytes", "mixkvq_rope_axes", "mixkvq_rope_axes_append", "mixkvq_rope_axes_decode_step", "mixkvq_quantize_append_ragged", "mixkvq_sequence_fill", "mixkvq_decode_attention_partial", "mixkvq_merge_partials",
 ]
 
-DEV_EXTRAS_FULL, DEV_COPY_TIMEOUT = 1, 2
+DEV_EXTRAS_FULL, DEV_COPY_TIMEOUT, DEV_BAD_POSITION = 1, 2, 4
 _OUT_TYPES = {torch.float32: 0, torch.bfloat16: 1}
 ATTN_ONE_UNIT, ATTN_TWO_UNITS, ATTN_DIRECT, ATTN_EARLY, ATTN_OTHER, ATTN_EIGHT_PAIRS = 1, 2, 4, 8, 16, 32
 
@@ -85,6 +85,10 @@ def lib():
         L.mixkvq_chunk_scratch_bytes.argtypes = [C.POINTER(Config), i32]
         L.mixkvq_chunk_scratch_bytes.restype = C.c_size_t
         L.mixkvq_chunk_attention.argtypes = L.mixkvq_chunk_step.argtypes = [vp, i32, vp, vp, vp, i32, C.POINTER(C.c_int32), vp, i32, f32, vp, C.c_size_t, vp]
+        i64s, u8s = C.POINTER(C.c_int64), C.c_char_p
+        L.mixkvq_rope_axes.argtypes = [vp, vp, vp, vp, i64s, i32, vp, vp, i32, vp, i32, u8s, vp, vp, vp, vp]
+        L.mixkvq_rope_axes_append.argtypes = [vp, i32, vp, vp, vp, vp, vp, i32, vp, i32, u8s, i32, vp]
+        L.mixkvq_rope_axes_decode_step.argtypes = [vp, i32, vp, vp, vp, vp, vp, i32, vp, i32, u8s, vp, f32, vp, C.c_size_t, vp]
         L.mixkvq_rope_append.argtypes = [vp, i32, vp, vp, vp, vp, vp, i32, i32, vp]
         L.mixkvq_rope_decode_step.argtypes = [vp, i32, vp, vp, vp, vp, vp, i32, vp, f32, vp, C.c_size_t, vp]
         L.mixkvq_cache_written_externally.argtypes = [vp]
@@ -178,6 +182,23 @@ def select_channels_raw(q: torch.Tensor, k: torch.Tensor, score_bits, tau_bf16, 
     _check(lib().mixkvq_select_channels_raw(_ptr(q), _ptr(k), B, Hq, Hkv, Lq, Lk, score_bits, tau_bf16, tau_u4,
                                             _ptr(tiers), _ptr(sal), _stream()), "mixkvq_select_channels_raw")
     return tiers, sal
+
+
+def axis_sections(sections, interleaved=False):
+    """The axis of each of the 64 channel pairs, for rope_axes: sections[a] pairs for axis a, one section behind another or, `interleaved`, one pair
+    of every axis in turn as long as it has some left."""
+    left = [int(n) for n in sections]
+    if sum(left) != 64 or min(left) < 0:
+        raise ValueError(f"the sections are 64 channel pairs together, not {sections}")
+    if not interleaved:
+        return [a for a, n in enumerate(left) for _ in range(n)]
+    pairs = []
+    while len(pairs) < 64:
+        for a, n in enumerate(left):
+            if n:
+                pairs.append(a)
+                left[a] -= 1
+    return pairs
 
 
 class Cache:
@@ -332,6 +353,76 @@ class Cache:
                                                       self.workspace, self.workspace.numel(), _stream())
         if code:
             raise MixKVQError(code, "mixkvq_rope_decode_step")
+        return out
+
+    def _angles(self, name, cos, sin, positions, axes, n):
+        """The arguments that say what a rotation with several axes turns by."""
+        dev = self.mem.device
+        if cos.dtype != torch.float32 or cos.dim() != 2 or cos.shape[1] != 64 or cos.shape != sin.shape or sin.dtype != torch.float32:
+            raise ValueError(f"{name}: cos and sin must be float32 tables [n_positions, 64]")
+        if positions.dtype != torch.int32 or positions.dim() != 3 or positions.shape[1:] != (self.cfg.batch, n):
+            raise ValueError(f"{name}: positions must be int32 [axes, {self.cfg.batch}, {n}]")
+        for t in (cos, sin, positions):
+            if not t.is_contiguous() or t.device != dev:
+                raise ValueError(f"{name}: cos, sin and positions must be contiguous tensors on {dev}")
+        if len(axes) != 64:
+            raise ValueError(f"{name}: the axes of 64 channel pairs are needed, {len(axes)} were given")
+        return cos.data_ptr(), sin.data_ptr(), cos.shape[0], positions.data_ptr(), positions.shape[0], bytes(axes)
+
+    def rope_axes(self, q, k, v, cos, sin, positions, axes, out=None):
+        """Rotates q [B,Hq,n,128] and k [B,Hkv,n,128] (bf16, any strides with a contiguous last dimension: views of a fused projection's output too)
+        by one position per axis: positions int32 [axes,B,n] (negative: no token, its rows are left alone), axes: the axis of each of the 64
+        channel pairs (axis_sections makes it), cos, sin float32 [n_positions,64].  v (or None) is copied.  Returns the head-major (q, k, v):
+        `out`, which may be (q, k, v) itself where they are head-major, or new tensors (zeros for rows without a token)."""
+        cfg, dev, n = self.cfg, self.mem.device, q.shape[2] if q.dim() == 4 else 0
+        angles = self._angles("rope_axes", cos, sin, positions, axes, n)
+        ins = (q, k, v)
+        if out is None:
+            out = tuple(None if t is None else torch.zeros(t.shape, dtype=torch.bfloat16, device=dev) for t in ins)
+        strides = (C.c_int64 * 9)()
+        for i, (t, o, heads) in enumerate(zip(ins, out, (cfg.n_q_heads, cfg.n_kv_heads, cfg.n_kv_heads))):
+            if i == 2 and t is None and o is None:
+                continue
+            if t is None or o is None:
+                raise ValueError("rope_axes: an input and its output come together")
+            shape = (cfg.batch, heads, n, 128)
+            if t.shape != shape or o.shape != shape or t.dtype != torch.bfloat16 or o.dtype != torch.bfloat16 or t.device != dev or o.device != dev:
+                raise ValueError(f"rope_axes: {'qkv'[i]} and its output must be bfloat16 {list(shape)} tensors on {dev}")
+            s = t.stride()
+            if s[3] != 1 or not o.is_contiguous():
+                raise ValueError("rope_axes: the inputs' last dimension and the outputs must be contiguous")
+            strides[3 * i], strides[3 * i + 1], strides[3 * i + 2] = s[:3]
+        ptr = [0 if t is None else t.data_ptr() for t in (*ins, *out)]
+        with torch.cuda.device(dev):
+            _check(lib().mixkvq_rope_axes(self.handle, ptr[0], ptr[1], ptr[2], strides, n, *angles, ptr[3], ptr[4], ptr[5], _stream()), "mixkvq_rope_axes")
+        return out
+
+    def _head_major(self, name, n, **tensors):
+        cfg, dev = self.cfg, self.mem.device
+        for what, t in tensors.items():
+            shape = (cfg.batch, cfg.n_q_heads if what == "q" else cfg.n_kv_heads, n, 128)
+            if t.shape != shape or t.dtype != torch.bfloat16 or not t.is_contiguous() or t.device != dev:
+                raise ValueError(f"{name}: {what} must be a contiguous bfloat16 {list(shape)} tensor on {dev}")
+
+    def rope_axes_append(self, layer, k, v, q, cos, sin, positions, axes):
+        """rope_axes on k and q in place (all head-major), then quantize_append."""
+        n = k.shape[2] if k.dim() == 4 else 0
+        self._head_major("rope_axes_append", n, k=k, v=v, q=q)
+        angles = self._angles("rope_axes_append", cos, sin, positions, axes, n)
+        with torch.cuda.device(self.mem.device):
+            _check(lib().mixkvq_rope_axes_append(self.handle, layer, _ptr(k), _ptr(v), _ptr(q), *angles, n, _stream()), "mixkvq_rope_axes_append")
+
+    def rope_axes_decode_step(self, layer, k, v, q, cos, sin, positions, axes, scale, out=None):
+        """One decode step with rope_axes of k and q (in place) in front: positions int32 [axes,B,1]; see decode_step."""
+        self._head_major("rope_axes_decode_step", 1, k=k, v=v, q=q)
+        angles = self._angles("rope_axes_decode_step", cos, sin, positions, axes, 1)
+        if out is None:
+            out = torch.empty((q.shape[0], q.shape[1], 128), dtype=torch.float32, device=q.device)
+        elif out.shape != (q.shape[0], q.shape[1], 128) or out.dtype != torch.float32 or out.device != q.device:
+            raise ValueError("rope_axes_decode_step: out must be a float32 [B, Hq, 128] tensor on the cache's device")
+        with torch.cuda.device(self.mem.device):
+            _check(lib().mixkvq_rope_axes_decode_step(self.handle, layer, _ptr(k), _ptr(v), _ptr(q), *angles, _ptr(out), float(scale), *self._ws, _stream()),
+                   "mixkvq_rope_axes_decode_step")
         return out
 
     def decode_attention_noalloc(self, layer, q, scale, out=None):

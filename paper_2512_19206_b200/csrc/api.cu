@@ -374,6 +374,67 @@ int check_chunk(const mixkvq_cache* cache, int layer, const void* k_dev, const v
   return MIXKVQ_OK;
 }
 
+// Rotation with several axes: fills in the launch's arguments, or says what is wrong with the call's.  in_place: the outputs are the inputs.
+int plan_rope_axes(const mixkvq_cache* cache, const void* q_dev, const void* k_dev, const void* v_dev, const int64_t* strides_host, int n_tokens,
+                   const float* cos_dev, const float* sin_dev, int n_positions, const int32_t* positions_dev, int n_axes,
+                   const uint8_t* axis_of_pair_host, void* q_out, void* k_out, void* v_out, RopeAxes* a) {
+  if (!cache || !q_dev || !k_dev || !q_out || !k_out || (v_dev == nullptr) != (v_out == nullptr) || !cos_dev || !sin_dev || !positions_dev ||
+      !axis_of_pair_host || n_tokens < 1 || n_positions < 1 || n_axes < 1 || n_axes > MIXKVQ_ROPE_MAX_AXES)
+    return MIXKVQ_E_INVALID_ARG;
+  const int B = cache->cfg.batch, Hq = cache->cfg.n_q_heads, Hkv = cache->cfg.n_kv_heads;
+  *a = RopeAxes{};
+  for (int i = 0; i < 64; ++i) {
+    if (axis_of_pair_host[i] >= n_axes) return MIXKVQ_E_INVALID_ARG;
+    a->axis_of_pair[i] = axis_of_pair_host[i];
+    a->used |= 1u << axis_of_pair_host[i];
+  }
+  if ((long long)B * n_tokens > 0x7FFFFFFFll) return MIXKVQ_E_UNSUPPORTED;               // (thread blocks of a grid)
+  const void* in[3] = {q_dev, k_dev, v_dev};
+  void* out[3] = {q_out, k_out, v_out};
+  RopeTensor* t[3] = {&a->tq, &a->tk, &a->tv};
+  uintptr_t lo[6], hi[6];                                  // bytes that the inputs and the outputs lie in
+  for (int i = 0; i < 3; ++i) {
+    const int H = i == 0 ? Hq : Hkv;
+    const RopeTensor whole{(long long)H * n_tokens * kD, (long long)n_tokens * kD, kD};
+    *t[i] = strides_host ? RopeTensor{strides_host[3 * i], strides_host[3 * i + 1], strides_host[3 * i + 2]} : whole;
+    lo[i] = hi[i] = lo[3 + i] = hi[3 + i] = 0;
+    if (in[i] == nullptr) continue;
+    if (!aligned16(in[i]) || !aligned16(out[i])) return MIXKVQ_E_ALIGNMENT;
+    const RopeTensor& x = *t[i];
+    if (x.batch < 0 || x.head < 0 || x.token < 0) return MIXKVQ_E_INVALID_ARG;
+    if ((x.batch | x.head | x.token) & 7) return MIXKVQ_E_ALIGNMENT;
+    lo[i] = reinterpret_cast<uintptr_t>(in[i]);
+    hi[i] = lo[i] + 2 * (uintptr_t)((B - 1) * x.batch + (H - 1) * x.head + (long long)(n_tokens - 1) * x.token + kD);
+    lo[3 + i] = reinterpret_cast<uintptr_t>(out[i]);
+    hi[3 + i] = lo[3 + i] + 2 * (uintptr_t)(B * whole.batch);
+  }
+  // An output may be its own input where that is head-major already; nothing else may overlap an output.
+  for (int o = 3; o < 6; ++o)
+    for (int i = 0; i < 6; ++i) {
+      if (i == o || lo[o] >= hi[i] || lo[i] >= hi[o]) continue;
+      const RopeTensor& x = *t[o - 3];
+      const int H = o == 3 ? Hq : Hkv;
+      const bool same = i == o - 3 && lo[i] == lo[o] && (B == 1 || x.batch == (long long)H * n_tokens * kD) && (H == 1 || x.head == (long long)n_tokens * kD) &&
+                        (n_tokens == 1 || x.token == kD);
+      if (!same) return MIXKVQ_E_INVALID_ARG;
+    }
+  if (!aligned16(cos_dev) || !aligned16(sin_dev) || (reinterpret_cast<uintptr_t>(positions_dev) & 3u)) return MIXKVQ_E_ALIGNMENT;
+  a->q = q_dev; a->k = k_dev; a->v = v_dev;
+  a->q_out = q_out; a->k_out = k_out; a->v_out = v_out;
+  a->cos_t = cos_dev; a->sin_t = sin_dev;
+  a->positions = positions_dev;
+  a->status = reinterpret_cast<uint32_t*>(cache->mem);
+  a->B = B; a->Hq = Hq; a->Hkv = Hkv; a->n = n_tokens; a->n_positions = n_positions; a->n_axes = n_axes;
+  return MIXKVQ_OK;
+}
+
+int run_rope_axes(mixkvq_cache* cache, const RopeAxes& a, cudaStream_t st) {
+  if (launch_rope_axes(a, cache->n_sms, st) != cudaSuccess) return MIXKVQ_E_CUDA;
+  cache->launches += 1;
+  note_enqueued(cache, st, kNoPackedWrite);
+  return MIXKVQ_OK;
+}
+
 // A decode step whose arguments have been checked.  rope_cos / rope_sin: the position's rows of the tables (null: no rotation); the
 // split kernel rotates what it reads and the call's last kernel leaves the rotated rows in the caller's tensors, so that the rotation is
 // no launch in front of the step.
@@ -689,6 +750,44 @@ int mixkvq_rope_decode_step(mixkvq_cache* cache, int layer, void* k_dev, const v
   if (max_tokens_held(cache, layer) + 1 > cache->cfg.max_tokens) return MIXKVQ_E_CAPACITY;
   return run_decode_step(cache, layer, k_dev, v_dev, q_dev, out_dev, softmax_scale, workspace_dev, static_cast<cudaStream_t>(stream),
                          cos_dev + (size_t)pos * 64, sin_dev + (size_t)pos * 64);
+}
+
+int mixkvq_rope_axes(mixkvq_cache* cache, const void* q_dev, const void* k_dev, const void* v_dev, const int64_t* strides_host, int n_tokens,
+                     const float* cos_dev, const float* sin_dev, int n_positions, const int32_t* positions_dev, int n_axes,
+                     const uint8_t* axis_of_pair_host, void* q_out_dev, void* k_out_dev, void* v_out_dev, void* stream) {
+  RopeAxes a;
+  const int rc = plan_rope_axes(cache, q_dev, k_dev, v_dev, strides_host, n_tokens, cos_dev, sin_dev, n_positions, positions_dev, n_axes,
+                                axis_of_pair_host, q_out_dev, k_out_dev, v_out_dev, &a);
+  return rc != MIXKVQ_OK ? rc : run_rope_axes(cache, a, static_cast<cudaStream_t>(stream));
+}
+
+int mixkvq_rope_axes_append(mixkvq_cache* cache, int layer, void* k_dev, const void* v_dev, void* q_dev, const float* cos_dev, const float* sin_dev,
+                            int n_positions, const int32_t* positions_dev, int n_axes, const uint8_t* axis_of_pair_host, int n_tokens, void* stream) {
+  RopeAxes a;
+  int rc = plan_rope_axes(cache, q_dev, k_dev, nullptr, nullptr, n_tokens, cos_dev, sin_dev, n_positions, positions_dev, n_axes, axis_of_pair_host, q_dev,
+                          k_dev, nullptr, &a);
+  if (rc != MIXKVQ_OK) return rc;
+  if (!v_dev || layer < 0 || layer >= cache->cfg.n_layers) return MIXKVQ_E_INVALID_ARG;
+  if (!aligned16(v_dev)) return MIXKVQ_E_ALIGNMENT;
+  if (max_tokens_held(cache, layer) + n_tokens > cache->cfg.max_tokens) return MIXKVQ_E_CAPACITY;      // nothing is rotated either
+  rc = run_rope_axes(cache, a, static_cast<cudaStream_t>(stream));
+  return rc != MIXKVQ_OK ? rc : mixkvq_quantize_append(cache, layer, k_dev, v_dev, q_dev, n_tokens, stream);
+}
+
+int mixkvq_rope_axes_decode_step(mixkvq_cache* cache, int layer, void* k_dev, const void* v_dev, void* q_dev, const float* cos_dev, const float* sin_dev,
+                                 int n_positions, const int32_t* positions_dev, int n_axes, const uint8_t* axis_of_pair_host, float* out_dev,
+                                 float softmax_scale, void* workspace_dev, size_t workspace_bytes_given, void* stream) {
+  RopeAxes a;
+  int rc = plan_rope_axes(cache, q_dev, k_dev, nullptr, nullptr, 1, cos_dev, sin_dev, n_positions, positions_dev, n_axes, axis_of_pair_host, q_dev, k_dev,
+                          nullptr, &a);
+  if (rc != MIXKVQ_OK) return rc;
+  if (!v_dev || !out_dev || !workspace_dev || layer < 0 || layer >= cache->cfg.n_layers) return MIXKVQ_E_INVALID_ARG;
+  if (!aligned16(v_dev) || !aligned16(out_dev) || !aligned16(workspace_dev)) return MIXKVQ_E_ALIGNMENT;
+  if (workspace_bytes_given < workspace_bytes(cache->S)) return MIXKVQ_E_BUFFER_TOO_SMALL;
+  if (max_tokens_held(cache, layer) + 1 > cache->cfg.max_tokens) return MIXKVQ_E_CAPACITY;
+  rc = run_rope_axes(cache, a, static_cast<cudaStream_t>(stream));
+  return rc != MIXKVQ_OK ? rc
+                         : run_decode_step(cache, layer, k_dev, v_dev, q_dev, out_dev, softmax_scale, workspace_dev, static_cast<cudaStream_t>(stream));
 }
 
 // ---- decode attention with the split partials in storage compiled into the library (no allocation)

@@ -997,7 +997,8 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
         const int h0 = (row_in >> (7 - lg_copies)) << (2 - lg_copies), h1 = h0 + (4 >> lg_copies);
         bool first = true;
         for (int j = sg.j0 + (dual ? 0 : slot); j < j1; j += step, ++cnt) {
-          ok = group_wait(4 + slot, kTile, (warp & 3) == 0, kSFull + slot, (uint32_t)cnt & 1u);
+          ok = __all_sync(0xffffffffu, phase_over(bar(kSFull + slot), (uint32_t)cnt & 1u)) ||
+               __all_sync(0xffffffffu, wait_ns(Literal<20>{}, kSFull + slot, (uint32_t)cnt & 1u));
           if (!ok) break;
           tc_fence_after();
           if (!idle) {

@@ -262,6 +262,20 @@ cudaError_t launch_merge_partials(const float* o_parts, const float* lse_parts, 
                                   cudaStream_t stream);
 cudaError_t launch_rope(void* k, void* q, const float* cos_t, const float* sin_t, int B, int Hkv, int Hq, int n_tokens,
                         int pos0, cudaStream_t stream);
+// rotary positions with several axes: q, k (rotated) and v (copied, may be null) of n tokens per sequence into head-major tensors
+struct RopeTensor { long long batch, head, token; };      // distances in elements
+struct RopeAxes {
+  const void *q, *k, *v;
+  void *q_out, *k_out, *v_out;
+  RopeTensor tq, tk, tv;
+  const float *cos_t, *sin_t;
+  const int32_t* positions;                               // [n_axes][B][n]
+  uint32_t* status;
+  int B, Hq, Hkv, n, n_positions, n_axes;
+  uint32_t used;                                          // bit x: some pair belongs to axis x
+  uint8_t axis_of_pair[64];
+};
+cudaError_t launch_rope_axes(const RopeAxes& a, int n_sms, cudaStream_t stream);
 cudaError_t launch_flush(const LayerView& lv, cudaStream_t stream);
 cudaError_t launch_flush_bulk(const LayerView& lv, const void* k, const void* v, const void* q, int n_tokens, int t0,
                               int nb, int tail, bool behind_prefill, cudaStream_t stream);
