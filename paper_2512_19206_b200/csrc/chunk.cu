@@ -53,6 +53,11 @@ __device__ __forceinline__ uint4 lds128(uint32_t a) {
   asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
   return v;
 }
+__device__ __forceinline__ uint32_t lds16(uint32_t a) {
+  uint16_t v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a));
+  return v;
+}
 __device__ __forceinline__ uint32_t hfma2_u(uint32_t a, uint32_t b, uint32_t c) {
   uint32_t d;
   asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
@@ -198,14 +203,19 @@ struct PackedKeys {
 
 // ---- keys: warp w of four makes rows 32 w .. 32 w + 31 of the tile at shared address `tile`; two such groups of warps take the tiles in turn, so that two
 // are on their way at any time (a tile is mostly latency: loads, barriers, chains of a few dependent instructions)
-// A block's promoted channels: `id` is the lane's entry of the list of BF16 channels, raw their first two pairs (the lane's token), ex the block's extras,
-// exu this unit's.
+// A block's promoted channels: `id` is the lane's entry of the list of BF16 channels, raw their first two pairs (the lane's token), `pair4` the lane's
+// entry of the list of UINT4 channel pairs, high the first four pairs' high plane, ex the block's extras, exu this unit's.
 struct Promoted {
   int n16, n4;
-  uint32_t id, raw[2];
+  uint32_t id, raw[2], pair4, high[4];
   const char *ex, *exu;
 };
-template <bool kDense>
+// Word of the UINT4 high plane that holds the lane's token, of pair 0, and the place of its two bits there (the pair's second channel: 16 further on)
+__device__ __forceinline__ const uint32_t* high_plane(const Promoted& p, int lane) {
+  return reinterpret_cast<const uint32_t*>(p.exu + 128 * ((p.n16 + 1) >> 1)) + (lane & 3);
+}
+__device__ __forceinline__ int high_bit(int lane) { return 8 * ((lane >> 2) & 1) + 2 * (2 * (lane >> 4) + ((lane >> 3) & 1)); }
+template <int kU4>
 __device__ __forceinline__ Promoted request_promoted(const char* extras, uint2 entry, int u, int lane) {
   Promoted p;
   p.n16 = entry.y & 0xFF;
@@ -213,20 +223,28 @@ __device__ __forceinline__ Promoted request_promoted(const char* extras, uint2 e
   p.id = kD;
   p.raw[0] = p.raw[1] = 0u;
   p.ex = extras + (size_t)entry.x * 16;
-  p.exu = p.ex + extras_header_bytes(p.n16, p.n4) + (uint32_t)u * extras_unit_bytes(p.n16, p.n4, kDense);
+  p.exu = p.ex + extras_header_bytes(p.n16, p.n4) + (uint32_t)u * extras_unit_bytes(p.n16, p.n4, kU4 == 2);
   if (lane < p.n16) p.id = reinterpret_cast<const uint8_t*>(p.ex)[lane];
   if (p.n16 > 0) p.raw[0] = reinterpret_cast<const uint32_t*>(p.exu)[lane];
   if (p.n16 > 2) p.raw[1] = reinterpret_cast<const uint32_t*>(p.exu)[32 + lane];
+  if (kU4 == 1 && p.n4 > 0) {
+    const int pairs = (p.n4 + 1) >> 1;
+    p.pair4 = 0xFFFFu;
+    if (lane < pairs) p.pair4 = reinterpret_cast<const uint16_t*>(p.ex + ((p.n16 + 1) & ~1))[lane];
+    const uint32_t* high = high_plane(p, lane);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p.high[i] = i < pairs ? high[4 * i] : 0u;
+  }
   return p;
 }
-template <bool kDense>
+template <int kU4>
 __device__ __forceinline__ PackedKeys request_keys(const LayerView& lv, const Cursor& at, const Promoted& more, int lane) {
   PackedKeys p{};
   const uint4* codes = reinterpret_cast<const uint4*>(at.codes(lv)) + lane;
   p.c0 = codes[0];
   p.c1 = codes[32];
   p.meta = reinterpret_cast<const uint4*>(at.meta(lv))[lane];
-  if (kDense && more.n4 != 0) {
+  if (kU4 == 2 && more.n4 != 0) {
     const uint4* hi = reinterpret_cast<const uint4*>(more.exu + 128 * ((more.n16 + 1) >> 1)) + lane;
     p.h0 = hi[0];
     p.h1 = hi[32];
@@ -234,8 +252,8 @@ __device__ __forceinline__ PackedKeys request_keys(const LayerView& lv, const Cu
   return p;
 }
 
-// The unit's two-bit (kDense: four-bit) codes.
-template <bool kDense>
+// The unit's two-bit (kU4 = 2: four-bit) codes.
+template <int kU4>
 __device__ __forceinline__ void make_keys(const PackedKeys& p, uint32_t tile, uint32_t scratch, int w, int lane, const Magic& magic) {
   // Scales and zero-points of channel pairs (16 kt + 8 ch + 2 t, + 1) as fp16 pairs: word 36 ch + 8 t + kt, zero-points 72 words on (odd kt: a quarter of the
   // scale).  The lane has the pairs 2 lane and 2 lane + 1: kt = lane / 4, ch = lane / 2 % 2, t = 2 (lane % 2) and the next.
@@ -264,14 +282,14 @@ __device__ __forceinline__ void make_keys(const PackedKeys& p, uint32_t tile, ui
     for (int r = 0; r < 4; ++r)          // rows 8 r ..
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        sts32(to + r * 2048 + 2 * k * 128, kDense ? dequant4(magic, c[r], h[r], k, s[k], z[k]) : dequant2(magic, c[r], k, s[k], z[k]));
+        sts32(to + r * 2048 + 2 * k * 128, kU4 == 2 ? dequant4(magic, c[r], h[r], k, s[k], z[k]) : dequant2(magic, c[r], k, s[k], z[k]));
   }
 }
 
 // The promoted channels replace their codes' values.
-template <bool kDense>
-__device__ __forceinline__ void put_promoted(const LayerView& lv, const Cursor& at, Promoted& p, uint32_t tile, int w, int lane) {
-  if ((p.n16 | (kDense ? 0 : p.n4)) == 0) return;
+template <int kU4>
+__device__ __forceinline__ void put_promoted(Promoted& p, uint32_t tile, uint32_t scratch, int w, int lane) {
+  if ((p.n16 | (kU4 == 1 ? p.n4 : 0)) == 0) return;
   __syncwarp();                          // the base codes are stored
   const uint32_t row = tile + (4 * w + (lane >> 3)) * 2048 + (lane & 7) * 16;           // the lane's token
   auto offset = [](uint32_t d) { return (d >> 3) * 128 + (d & 7) * 2; };
@@ -285,39 +303,34 @@ __device__ __forceinline__ void put_promoted(const LayerView& lv, const Cursor& 
     if (2 * i + 4 < p.n16) p.raw[1] = reinterpret_cast<const uint32_t*>(p.exu)[(i + 2) * 32 + lane];
     if (((2 * i + 2) & 31) == 0 && 2 * i + 2 + lane < p.n16) mine = offset(reinterpret_cast<const uint8_t*>(p.ex)[2 * i + 2 + lane]);
   }
-  if (!kDense && p.n4 > 0) {             // UINT4 channels: c = c_lo + 4 c_hi, with s and z from the block's scales; four at a time, their loads in flight together
-    const int n16p = (p.n16 + 1) >> 1, mt = lane >> 4, rh = (lane >> 3) & 1, r = lane & 7;
-    const uint32_t* low = reinterpret_cast<const uint32_t*>(at.codes(lv)) + mt * 128 + 16 * r + rh;
-    const uint32_t* meta = reinterpret_cast<const uint32_t*>(at.meta(lv));
-    const uint32_t* high = reinterpret_cast<const uint32_t*>(p.exu + 128 * n16p) + (r & 3);
-    const uint16_t* chans = reinterpret_cast<const uint16_t*>(p.ex + 2 * n16p);          // (pairs; the last may hold 0xFF)
-    const int hi_bit = 8 * (r >> 2) + 2 * (2 * mt + rh), pairs = (p.n4 + 1) >> 1;
-    uint32_t id = lane < pairs ? chans[lane] : 0xFFFFu;
+  if (kU4 == 1 && p.n4 > 0) {
+    // UINT4 channels: (c_lo + 4 c_hi) s + z is what the base store left, plus 4 c_hi s.  (A second rounding to fp16.  With the low codes read again, to round
+    // once, every four channels cost a round trip to the L2 cache: 7b shape, three tiers, draft-sized chunk of eight sequences, LOW / HIGH us.)
+    const int pairs = (p.n4 + 1) >> 1, bit = high_bit(lane);
+    const uint32_t* high = high_plane(p, lane);
 #pragma unroll 1
-    for (int i0 = 0; i0 < pairs; i0 += 2) {
-      if (i0 == 32) id = 32 + lane < pairs ? chans[32 + lane] : 0xFFFFu;
-      uint32_t d[4], hw[2], lw[4], mz[4];
+    for (int i0 = 0; i0 < pairs; i0 += 4) {
+      if (i0 == 32) p.pair4 = 32 + lane < pairs ? reinterpret_cast<const uint16_t*>(p.ex + ((p.n16 + 1) & ~1))[32 + lane] : 0xFFFFu;
+      uint32_t hw[4];
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const uint32_t two = __shfl_sync(0xffffffffu, id, (i0 + k) & 31);
-        d[2 * k] = i0 + k < pairs ? two & 0xFF : 0xFFu;
-        d[2 * k + 1] = i0 + k < pairs ? two >> 8 : 0xFFu;
-        hw[k] = i0 + k < pairs ? high[4 * (i0 + k)] >> hi_bit : 0u;
+      for (int k = 0; k < 4; ++k) {
+        hw[k] = p.high[k];
+        if (i0 + 4 + k < pairs) p.high[k] = high[4 * (i0 + 4 + k)];
       }
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        lw[k] = mz[k] = 0u;
-        if (d[k] < kD) {
-          lw[k] = low[4 * ((d[k] & 7) >> 1) + 2 * ((d[k] >> 3) & 1)];
-          mz[k] = meta[d[k]];
+        const uint32_t two = i0 + k < pairs ? __shfl_sync(0xffffffffu, p.pair4, (i0 + k) & 31) : 0xFFFFu;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t d = e ? two >> 8 : two & 0xFFu;
+          if (d < kD) {                  // (the whole warp's decision; odd 16-channel pieces have a quarter of the scale in store)
+            const uint32_t s = lds16(scratch + 4 * (36 * ((d >> 3) & 1) + 8 * ((d & 7) >> 1) + (d >> 4)) + 2 * (d & 1)), at = row + offset(d);
+            const float old = __half2float(__ushort_as_half((unsigned short)lds16(at))), scale = __half2float(__ushort_as_half((unsigned short)s));
+            const float c = (float)((hw[k] >> (bit + 16 * e)) & 3u) * (d & 16 ? 16.f : 4.f);
+            sts16(at, (uint32_t)__half_as_ushort(__float2half_rn(fmaf(c, scale, old))));
+          }
         }
       }
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (d[k] < kD) {
-          const uint32_t code = ((lw[k] >> (16 * (d[k] & 1) + 2 * (d[k] >> 4))) & 3u) | (((hw[k >> 1] >> (16 * (k & 1))) & 3u) << 2);
-          sts16(row + offset(d[k]), (uint32_t)__half_as_ushort(__float2half_rn(fmaf((float)code, bf_lo(mz[k]), bf_hi(mz[k])))));
-        }
     }
   }
 }
@@ -593,7 +606,9 @@ __device__ __forceinline__ void store4(const ChunkArgs& a, size_t at, float4 y) 
   }
 }
 
-template <bool kDense, bool kV4>
+// kU4: how the configuration can use the UINT4 tier: 0 never (no threshold or budget puts a channel there), 1 some channels (high plane per channel pair),
+// 2 the 4-bit base (dense high plane)
+template <int kU4, bool kV4>
 __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __grid_constant__ LayerView lv, const __grid_constant__ ChunkArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
   const uint32_t sbase = smem_u32(smem), qs = sbase, ks = sbase + 2 * kTileBytes, vs = sbase + 4 * kTileBytes;
@@ -813,7 +828,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
             } else {
               const uint2 e = *at.entry;
               const int n16 = e.y & 0xFF, n4 = (e.y >> 8) & 0xFF;
-              const uint32_t bytes = extras_unit_bytes(n16, n4, kDense);               // (a multiple of 16)
+              const uint32_t bytes = extras_unit_bytes(n16, n4, kU4 == 2);               // (a multiple of 16)
               if (n16 + n4 > 0) prefetch_bulk(extras + (size_t)e.x * 16 + extras_header_bytes(n16, n4) + (uint32_t)at.u * bytes, bytes);
             }
           }
@@ -912,8 +927,8 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
         Promoted more{};
         PackedKeys p{};
         if (at.unit < units) {
-          more = request_promoted<kDense>(extras, *at.entry, at.u, lane);
-          p = request_keys<kDense>(lv, at, more, lane);
+          more = request_promoted<kU4>(extras, *at.entry, at.u, lane);
+          p = request_keys<kU4>(lv, at, more, lane);
         }
         for (; j < end; j += 2) {
           Cursor next = at;
@@ -924,13 +939,13 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
           if (w == 0 && lane == 0) *progress = kc + j - j0;
           // (past the last block the logits are masked, whatever the keys are)
           if (at.unit < units) {
-            make_keys<kDense>(p, stage, scratch, w, lane, magic);
-            put_promoted<kDense>(lv, at, more, stage, w, lane);
+            make_keys<kU4>(p, stage, scratch, w, lane, magic);
+            put_promoted<kU4>(more, stage, scratch, w, lane);
           }
           at = next;
           if (at.unit < units) {
-            more = request_promoted<kDense>(extras, entry, at.u, lane);
-            p = request_keys<kDense>(lv, at, more, lane);
+            more = request_promoted<kU4>(extras, entry, at.u, lane);
+            p = request_keys<kU4>(lv, at, more, lane);
           }
           made();
         }
@@ -1237,16 +1252,16 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant_
   store4(a, at, o);
 }
 
-template <bool kDense, bool kV4>
+template <int kU4, bool kV4>
 cudaError_t launch_one(const LayerView& lv, const ChunkArgs& a, cudaStream_t stream) {
-  return launch_dependent(chunk_attention_kernel<kDense, kV4>, dim3((unsigned)a.ctas), kThreads, kSmem, stream, lv, a);
+  return launch_dependent(chunk_attention_kernel<kU4, kV4>, dim3((unsigned)a.ctas), kThreads, kSmem, stream, lv, a);
 }
 
 }  // namespace
 
 cudaError_t chunk_attention_setup() {
-  for (auto kernel : {chunk_attention_kernel<false, false>, chunk_attention_kernel<false, true>, chunk_attention_kernel<true, false>,
-                      chunk_attention_kernel<true, true>}) {
+  for (auto kernel : {chunk_attention_kernel<0, false>, chunk_attention_kernel<0, true>, chunk_attention_kernel<1, false>, chunk_attention_kernel<1, true>,
+                      chunk_attention_kernel<2, false>, chunk_attention_kernel<2, true>}) {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e != cudaSuccess) return e;
   }
@@ -1279,8 +1294,10 @@ cudaError_t launch_chunk_attention(const LayerView& lv, ChunkArgs& a, int n_sms,
   a.rows_cap = rows_cap(lv.g, a.stride);
   a.ctas = (int)std::min<long long>(std::min(n_sms, kChunkMaxCtas), (a.total + 1) / 2);
   a.max_polls = a.max_polls ? a.max_polls : kPolls;
-  cudaError_t e = lv.dense_hi ? (lv.v_bits == 4 ? launch_one<true, true>(lv, a, stream) : launch_one<true, false>(lv, a, stream))
-                              : (lv.v_bits == 4 ? launch_one<false, true>(lv, a, stream) : launch_one<false, false>(lv, a, stream));
+  const bool some = lv.budget_bf16 + lv.budget_u4 > 0 ? lv.budget_u4 > 0 : lv.tau_u4 < lv.tau_bf16;
+  cudaError_t e = lv.dense_hi ? (lv.v_bits == 4 ? launch_one<2, true>(lv, a, stream) : launch_one<2, false>(lv, a, stream))
+                  : some      ? (lv.v_bits == 4 ? launch_one<1, true>(lv, a, stream) : launch_one<1, false>(lv, a, stream))
+                              : (lv.v_bits == 4 ? launch_one<0, true>(lv, a, stream) : launch_one<0, false>(lv, a, stream));
   if (e != cudaSuccess) return e;
   *launches = 1;
   if (a.ctas == 1) return cudaSuccess;
