@@ -27,7 +27,7 @@ namespace {
 
 constexpr int kTile = kChunkTile;
 constexpr int kTileBytes = kTile * kD * 2;
-constexpr int kThreads = 896;                             // 72 registers a thread at launch: 64512, shared out below as 256 x 112, 256 x 72, 256 x 48, 128 x 40
+constexpr int kThreads = 896;                             // 72 registers a thread at launch, shared out anew among the roles
 constexpr int kSoftmaxThreads = 256;
 constexpr int kIssueWarp = 24;
 constexpr int kScratchOff = 6 * kTileBytes;               // per producer warp 640 bytes: scales and zero-points as fp16 pairs
@@ -606,10 +606,31 @@ __device__ __forceinline__ void store4(const ChunkArgs& a, size_t at, float4 y) 
   }
 }
 
+// Registers per thread of the roles: together no more than the block is launched with.
+constexpr int kLaunchRegs = 72, kIssueRegs = 40;
+struct Registers {
+  int softmax, keys, values;
+};
+__host__ __device__ constexpr Registers registers_of(int u4, bool v4) {
+  return u4 == 0 ? (v4 ? Registers{104, 72, 56} : Registers{112, 72, 48}) : (v4 ? Registers{96, 80, 56} : Registers{104, 80, 48});
+}
+__host__ __device__ constexpr bool registers_fit(Registers r) { return 256 * (r.softmax + r.keys + r.values) + 128 * kIssueRegs <= kThreads * kLaunchRegs; }
+static_assert(registers_fit(registers_of(0, false)) && registers_fit(registers_of(0, true)) && registers_fit(registers_of(1, false)) &&
+                  registers_fit(registers_of(1, true)) && registers_fit(registers_of(2, false)) && registers_fit(registers_of(2, true)),
+              "the shares are taken from what the thread block was launched with");
+template <bool kMore, int kRegs>
+__device__ __forceinline__ void set_registers() {
+  if constexpr (kMore)
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs) : "memory");
+  else
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs) : "memory");
+}
+
 // kU4: how the configuration can use the UINT4 tier: 0 never (no threshold or budget puts a channel there), 1 some channels (high plane per channel pair),
 // 2 the 4-bit base (dense high plane)
 template <int kU4, bool kV4>
 __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __grid_constant__ LayerView lv, const __grid_constant__ ChunkArgs a) {
+  constexpr Registers kRegs = registers_of(kU4, kV4);
   extern __shared__ __align__(128) unsigned char smem[];
   const uint32_t sbase = smem_u32(smem), qs = sbase, ks = sbase + 2 * kTileBytes, vs = sbase + 4 * kTileBytes;
   auto bar = [&](int i) { return sbase + (uint32_t)kBarOff + 8u * (uint32_t)i; };
@@ -661,7 +682,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
   };
 
   if (warp >= kIssueWarp) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;" ::: "memory");
+    set_registers<false, kIssueRegs>();
     if (warp == kIssueWarp) {
       // ---------------------------------------------------------------- tensor-core issue
       // The whole warp goes through the loops and one lane issues; slots and stages are literals, and tensor memory starts at 0 (all of it was allocated), so
@@ -838,7 +859,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       }
     }
   } else if (warp >= 16) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;" ::: "memory");
+    set_registers<false, kRegs.values>();
     // ------------------------------------------------------------------ value tiles
     const int w = (warp >> 1) & 3, half = warp & 1;
     const uint32_t scratch = sbase + kScratchOff + (warp - 8) * 640;
@@ -896,7 +917,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       if (!ok) break;
     }
   } else if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;" ::: "memory");
+    set_registers<(kRegs.keys > kLaunchRegs), kRegs.keys>();
     // ------------------------------------------------------------------ key tiles
     // (the group's tiles are the even or the odd ones of every segment: it has one stage to itself)
     const int w = warp & 3, group = (warp >> 2) & 1, first_warp = 8 + 4 * group;
@@ -962,7 +983,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       kc += j1 - j0;
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 112;" ::: "memory");
+    set_registers<true, kRegs.softmax>();
     // ------------------------------------------------------------------ softmax and output rows
     const int slot = warp >> 2, row_in = tid & 127, g = lv.g;
     const uint32_t lane_base = tbase + ((uint32_t)((warp & 3) * 32) << 16);
