@@ -785,21 +785,22 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       if (leader) tc_commit(bar(kDone));                 // every product issued above has finished when this one fires
       dead = false;
       there(kDone, 0);
-    } else if (warp == kIssueWarp + 1 && lane == 0) {
+    } else if (warp == kIssueWarp + 1) {
       // ---------------------------------------------------------------- the thread block's segments
       const int g = lv.g;
       const long long begin = chunk_begin(a.total, a.ctas, blockIdx.x), end = chunk_begin(a.total, a.ctas, blockIdx.x + 1);
-      int n = 0;
-      auto publish = [&](const Segment& sg) {
-        if (n >= 2 && !wait_ns(Literal<500>{}, kSegEmpty + (n & 1), (uint32_t)((n >> 1) - 1) & 1u)) return false;
-        segments[n & 1] = sg;
-        mbar_arrive(bar(kSegFull + (n & 1)));
-        n += 1;
-        return true;
-      };
-      bool ok = true;
-      if (begin < end) {
-        ChunkItem it = chunk_locate(a, lv.B, lv.Hkv, g, begin);
+      ChunkItem it = chunk_locate(a, lv.B, lv.Hkv, g, begin, lane);
+      if (lane == 0) {
+        a.at[blockIdx.x] = it;
+        int n = 0;
+        auto publish = [&](const Segment& sg) {
+          if (n >= 2 && !wait_ns(Literal<500>{}, kSegEmpty + (n & 1), (uint32_t)((n >> 1) - 1) & 1u)) return false;
+          segments[n & 1] = sg;
+          mbar_arrive(bar(kSegFull + (n & 1)));
+          n += 1;
+          return true;
+        };
+        bool ok = true;
         for (;;) {
           Segment sg;
           chunk_tiles(it, begin, end, sg.j0, sg.j1);
@@ -821,11 +822,11 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
           if (!ok || it.x0 + (long long)it.weight * it.kt >= end) break;
           chunk_next(a, lv.Hkv, g, it);
         }
-      }
-      if (ok) {
-        Segment none{};
-        none.stream = -1;
-        publish(none);
+        if (ok) {
+          Segment none{};
+          none.stream = -1;
+          publish(none);
+        }
       }
     } else if (warp == kIssueWarp + 2) {
       // ---------------------------------------------------------------- requests into L2
@@ -1182,95 +1183,102 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
   if (warp == kIssueWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tbase), "r"(512) : "memory");
 }
 
-// The items that several thread blocks share: block x has the one around the boundary x + 1, if no earlier boundary lies inside it.  kRows rows of
-// 8 / kRows warps each; a warp takes every (8 / kRows)-th result, kFlight of them in flight.
+// The items that several thread blocks share: block x has the one around the boundary x + 1, if no earlier boundary lies inside it.  kRows rows at a time of
+// 8 / kRows warps each; a warp takes every (8 / kRows)-th result of its row, kFlight of them in flight.
 template <int kRows>
-__global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant__ LayerView lv, const __grid_constant__ ChunkArgs a) {
+__global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant__ LayerView lv, const __grid_constant__ ChunkArgs a, int rows_per_block) {
   constexpr int kWarps = 8 / kRows, kFlight = 8;
   __shared__ float2 mlS[8];
   __shared__ __align__(16) float oS[8][kD];
+  __shared__ int partS[kChunkMaxCtas];                     // the results that there are, by thread block: which of its two, or -1
+  __shared__ int wholeS;
   const int g = lv.g, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c1 = blockIdx.x + 1;
-  const long long x = chunk_begin(a.total, a.ctas, c1);
-  const ChunkItem it = chunk_locate(a, lv.B, lv.Hkv, g, x);
+  const long long x = chunk_begin(a.total, a.ctas, c1), x_before = chunk_begin(a.total, a.ctas, c1 - 1);
+  if (threadIdx.x == 0) wholeS = 0;
   dependency_wait();
-  const int prow = blockIdx.y * kRows + warp / kWarps, sub = warp % kWarps;
-  if (it.x0 == x || (c1 > 1 && chunk_begin(a.total, a.ctas, c1 - 1) > it.x0) || (int)blockIdx.y * kRows >= it.rows) return;
+  const ChunkItem it = a.at[c1];
+  const int row_first = blockIdx.y * rows_per_block, row_end = min(it.rows, row_first + rows_per_block);
+  if (it.x0 == x || (c1 > 1 && x_before > it.x0) || row_first >= row_end) return;
   const long long x1 = it.x0 + (long long)it.weight * it.kt;
   const int c0 = c1 - 1, count = (int)((x1 * a.ctas + a.total - 1) / a.total) - c0;
-  auto share = [&](int i, int& j0, int& j1) {
-    chunk_tiles(it, chunk_begin(a.total, a.ctas, c0 + i), chunk_begin(a.total, a.ctas, c0 + i + 1), j0, j1);
-  };
-  // (positions come two to a tile: an item across a boundary may still be one block's, which then wrote the output)
-  for (int i = 0; i < min(count, 2); ++i) {
+  __syncthreads();
+  if ((int)threadIdx.x < count) {
+    const long long begin = chunk_begin(a.total, a.ctas, c0 + threadIdx.x), end = chunk_begin(a.total, a.ctas, c0 + threadIdx.x + 1);
     int j0, j1;
-    share(i, j0, j1);
-    if (j0 == 0 && j1 == it.kt) return;
+    chunk_tiles(it, begin, end, j0, j1);
+    partS[threadIdx.x] = j0 < j1 ? (it.x0 <= begin ? 0 : 1) : -1;
+    // (positions come two to a tile: an item across a boundary may still be one block's, which then wrote the output)
+    if (j0 == 0 && j1 == it.kt) wholeS = 1;
   }
-  const bool exists = prow < it.rows;
+  __syncthreads();
+  if (wholeS) return;
   const size_t part_floats = (size_t)a.rows_cap * (kD + 2);
-  float M = -INFINITY, l = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int i0 = sub; exists && i0 < count; i0 += kWarps * kFlight) {
-    float2 ml[kFlight];
-    float4 y[kFlight];
+  const int sub = warp % kWarps;
+  for (int row0 = row_first; row0 < row_end; row0 += kRows) {
+    const int prow = row0 + warp / kWarps;
+    const bool exists = prow < row_end;
+    float M = -INFINITY, l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i0 = sub; exists && i0 < count; i0 += kWarps * kFlight) {
+      float2 ml[kFlight];
+      float4 y[kFlight];
 #pragma unroll
-    for (int k = 0; k < kFlight; ++k) {
-      const int i = i0 + k * kWarps;
-      ml[k] = make_float2(-INFINITY, 0.f);
-      y[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (i < count) {
-        int j0, j1;
-        share(i, j0, j1);
-        if (j0 < j1) {
-          const float* part = a.parts + ((size_t)(c0 + i) * 2 + (it.x0 <= chunk_begin(a.total, a.ctas, c0 + i) ? 0 : 1)) * part_floats;
+      for (int k = 0; k < kFlight; ++k) {
+        const int i = i0 + k * kWarps, which = i < count ? partS[i] : -1;
+        ml[k] = make_float2(-INFINITY, 0.f);
+        y[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (which >= 0) {
+          const float* part = a.parts + ((size_t)(c0 + i) * 2 + which) * part_floats;
           ml[k] = reinterpret_cast<const float2*>(part + (size_t)a.rows_cap * kD)[prow];
           y[k] = reinterpret_cast<const float4*>(part + (size_t)prow * kD)[lane];
         }
       }
+      float top = M;
+#pragma unroll
+      for (int k = 0; k < kFlight; ++k) top = fmaxf(top, ml[k].x);
+      const float f = M == -INFINITY ? (l == 0.f ? 0.f : 1.f) : exp2f(M - top);
+      l *= f;
+      o.x *= f; o.y *= f; o.z *= f; o.w *= f;
+#pragma unroll
+      for (int k = 0; k < kFlight; ++k) {
+        // (NaN sums of a row whose logits hold a NaN: their maximum may be -inf, and they count all the same)
+        const float w = ml[k].x == -INFINITY ? (ml[k].y == 0.f ? 0.f : 1.f) : exp2f(ml[k].x - top);
+        if (w != 0.f) {
+          l = fmaf(w, ml[k].y, l);
+          o.x = fmaf(w, y[k].x, o.x); o.y = fmaf(w, y[k].y, o.y); o.z = fmaf(w, y[k].z, o.z); o.w = fmaf(w, y[k].w, o.w);
+        }
+      }
+      M = top;
     }
-    float top = M;
-#pragma unroll
-    for (int k = 0; k < kFlight; ++k) top = fmaxf(top, ml[k].x);
-    const float f = M == -INFINITY ? 0.f : exp2f(M - top);
-    l *= f;
-    o.x *= f; o.y *= f; o.z *= f; o.w *= f;
-#pragma unroll
-    for (int k = 0; k < kFlight; ++k) {
-      // (NaN sums of a row whose logits hold a NaN: their maximum may be -inf, and they count all the same)
-      const float w = ml[k].x == -INFINITY ? (ml[k].y == 0.f ? 0.f : 1.f) : exp2f(ml[k].x - top);
-      if (w != 0.f) {
-        l = fmaf(w, ml[k].y, l);
-        o.x = fmaf(w, y[k].x, o.x); o.y = fmaf(w, y[k].y, o.y); o.z = fmaf(w, y[k].z, o.z); o.w = fmaf(w, y[k].w, o.w);
+    if constexpr (kWarps > 1) {
+      if (lane == 0) mlS[warp] = make_float2(M, l);
+      reinterpret_cast<float4*>(oS[warp])[lane] = o;
+      __syncthreads();
+      if (sub == 0) {
+        float top = M;
+        for (int w = 1; w < kWarps; ++w) top = fmaxf(top, mlS[warp + w].x);
+        const float f = M == -INFINITY ? (l == 0.f ? 0.f : 1.f) : exp2f(M - top);
+        l *= f;
+        o.x *= f; o.y *= f; o.z *= f; o.w *= f;
+        for (int w = 1; w < kWarps; ++w) {
+          const float2 ml = mlS[warp + w];
+          const float fw = ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : 1.f) : exp2f(ml.x - top);
+          if (fw != 0.f) {
+            const float4 y = reinterpret_cast<const float4*>(oS[warp + w])[lane];
+            l = fmaf(fw, ml.y, l);
+            o.x = fmaf(fw, y.x, o.x); o.y = fmaf(fw, y.y, o.y); o.z = fmaf(fw, y.z, o.z); o.w = fmaf(fw, y.w, o.w);
+          }
+        }
       }
     }
-    M = top;
-  }
-  if constexpr (kWarps > 1) {
-    if (lane == 0) mlS[warp] = make_float2(M, l);
-    reinterpret_cast<float4*>(oS[warp])[lane] = o;
-    __syncthreads();
-    if (sub != 0) return;
-    float top = M;
-    for (int w = 1; w < kWarps; ++w) top = fmaxf(top, mlS[warp + w].x);
-    const float f = M == -INFINITY ? (l == 0.f ? 0.f : 1.f) : exp2f(M - top);
-    l *= f;
-    o.x *= f; o.y *= f; o.z *= f; o.w *= f;
-    for (int w = 1; w < kWarps; ++w) {
-      const float2 ml = mlS[warp + w];
-      const float fw = ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : 1.f) : exp2f(ml.x - top);
-      if (fw != 0.f) {
-        const float4 y = reinterpret_cast<const float4*>(oS[warp + w])[lane];
-        l = fmaf(fw, ml.y, l);
-        o.x = fmaf(fw, y.x, o.x); o.y = fmaf(fw, y.y, o.y); o.z = fmaf(fw, y.z, o.z); o.w = fmaf(fw, y.w, o.w);
-      }
+    if (exists && sub == 0) {
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const int row = kChunkRows * it.rt + prow, tok = row / g;
+      const size_t at = ((((size_t)it.b * lv.Hq + it.hk * g + (row - tok * g)) * a.stride + tok) * kD) + 4 * lane;
+      store4(a, at, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
     }
+    if constexpr (kWarps > 1) __syncthreads();
   }
-  if (!exists) return;
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  const int row = kChunkRows * it.rt + prow, tok = row / g;
-  const size_t at = ((((size_t)it.b * lv.Hq + it.hk * g + (row - tok * g)) * a.stride + tok) * kD) + 4 * lane;
-  o.x *= inv; o.y *= inv; o.z *= inv; o.w *= inv;
-  store4(a, at, o);
 }
 
 template <int kU4, bool kV4>
@@ -1292,7 +1300,9 @@ cudaError_t chunk_attention_setup() {
 // Rows that a thread block's result can have: an item's, and an even number, so that every result starts on 16 bytes.
 static int rows_cap(int g, int n_tokens) { return (int)std::min<long long>(kChunkRows, ((long long)n_tokens * g + 1) & ~1ll); }
 
-size_t chunk_scratch_bytes(int g, int n_tokens) { return (size_t)kChunkMaxCtas * 2 * rows_cap(g, n_tokens) * (kD + 2) * sizeof(float); }
+static size_t parts_bytes(int g, int n_tokens) { return (size_t)kChunkMaxCtas * 2 * rows_cap(g, n_tokens) * (kD + 2) * sizeof(float); }
+
+size_t chunk_scratch_bytes(int g, int n_tokens) { return parts_bytes(g, n_tokens) + kChunkMaxCtas * sizeof(ChunkItem); }
 
 cudaError_t launch_chunk_attention(const LayerView& lv, ChunkArgs& a, int n_sms, cudaStream_t stream, int* launches) {
   *launches = 0;
@@ -1314,6 +1324,7 @@ cudaError_t launch_chunk_attention(const LayerView& lv, ChunkArgs& a, int n_sms,
   if (a.total == 0) return cudaSuccess;
   a.rows_cap = rows_cap(lv.g, a.stride);
   a.ctas = (int)std::min<long long>(std::min(n_sms, kChunkMaxCtas), (a.total + 1) / 2);
+  a.at = reinterpret_cast<ChunkItem*>(reinterpret_cast<char*>(a.parts) + parts_bytes(lv.g, a.stride));
   a.max_polls = a.max_polls ? a.max_polls : kPolls;
   const bool some = lv.budget_bf16 + lv.budget_u4 > 0 ? lv.budget_u4 > 0 : lv.tau_u4 < lv.tau_bf16;
   cudaError_t e = lv.dense_hi ? (lv.v_bits == 4 ? launch_one<2, true>(lv, a, stream) : launch_one<2, false>(lv, a, stream))
@@ -1322,10 +1333,12 @@ cudaError_t launch_chunk_attention(const LayerView& lv, ChunkArgs& a, int n_sms,
   if (e != cudaSuccess) return e;
   *launches = 1;
   if (a.ctas == 1) return cudaSuccess;
+  // Few results per item: a warp per row, 32 rows per block.  Many (one or two long sequences): the eight warps of a block share a row's results, one row after
+  // another; then there are few rows, one per block.
   if (a.ctas > 8 * items)
-    e = launch_dependent(chunk_merge_kernel<1>, dim3((unsigned)(a.ctas - 1), (unsigned)a.rows_cap), 256, 0, stream, lv, a);
+    e = launch_dependent(chunk_merge_kernel<1>, dim3((unsigned)(a.ctas - 1), (unsigned)a.rows_cap), 256, 0, stream, lv, a, 1);
   else
-    e = launch_dependent(chunk_merge_kernel<8>, dim3((unsigned)(a.ctas - 1), (unsigned)((a.rows_cap + 7) / 8)), 256, 0, stream, lv, a);
+    e = launch_dependent(chunk_merge_kernel<8>, dim3((unsigned)(a.ctas - 1), (unsigned)((a.rows_cap + 31) / 32)), 256, 0, stream, lv, a, 32);
   if (e != cudaSuccess) return e;
   *launches = 2;
   return cudaSuccess;

@@ -10,6 +10,7 @@ constexpr int kChunkMaxCtas = 148;     // thread blocks of one launch: one per S
 constexpr int kChunkRows = 256;        // query rows of an item
 constexpr int kChunkTile = 128;        // keys of a tile
 
+struct ChunkItem;
 struct ChunkSeq {
   int units;                           // packed 32-token units
   int tail;                            // residual and sink rows: r | n_sink << 16
@@ -21,6 +22,7 @@ struct ChunkSeq {
 // streams lie one behind another on a line, an item of more than 128 rows two positions long per key tile, any other one; thread block c has
 // the positions [total c / ctas, total (c + 1) / ctas).
 struct ChunkArgs {
+  struct ChunkItem* at;                // per thread block: the item that its first position lies in (behind parts; the merge reads it)
   const uint16_t *k, *v, *q;           // [B, Hkv, stride, 128], [B, Hq, stride, 128] bf16
   void* out;                           // [B, Hq, stride, 128]
   float* parts;                        // two results of rows_cap rows per thread block: [rows_cap][128] sums, [rows_cap] (maximum, denominator)
@@ -53,8 +55,8 @@ __host__ __device__ inline void chunk_item_of(const ChunkSeq& s, int g, ChunkIte
   it.weight = it.rows > kChunkTile ? 2 : 1;
 }
 
-// The item at position x (0 <= x < total).
-__device__ inline ChunkItem chunk_locate(const ChunkArgs& a, int B, int Hkv, int g, long long x) {
+// The item at position x (0 <= x < total), found by a whole warp: row tiles 32 at a time.
+__device__ inline ChunkItem chunk_locate(const ChunkArgs& a, int B, int Hkv, int g, long long x, int lane) {
   ChunkItem it;
   int lo = 0, hi = B;                  // prefix[lo] <= x < prefix[hi]
   while (hi - lo > 1) {
@@ -66,11 +68,25 @@ __device__ inline ChunkItem chunk_locate(const ChunkArgs& a, int B, int Hkv, int
   it.hk = (int)((x - a.prefix[lo]) / per);
   it.x0 = a.prefix[lo] + per * it.hk;
   const ChunkSeq s = a.seq[lo];
-  for (it.rt = 0;; ++it.rt) {
+  const int n_rt = (s.n * g + kChunkRows - 1) / kChunkRows;
+  for (int first = 0;; first += 32) {
+    it.rt = first + lane < n_rt ? first + lane : n_rt - 1;
     chunk_item_of(s, g, it);
-    const long long next = it.x0 + (long long)it.weight * it.kt;
-    if (x < next || it.rt + 1 >= it.n_rt) return it;
-    it.x0 = next;
+    long long end = first + lane < n_rt ? (long long)it.weight * it.kt : 0;            // positions up to the end of the lane's row tile
+    for (int d = 1; d < 32; d <<= 1) {
+      const long long other = __shfl_up_sync(0xffffffffu, end, d);
+      if (lane >= d) end += other;
+    }
+    const uint32_t behind = __ballot_sync(0xffffffffu, it.x0 + end > x);
+    if (behind != 0u || first + 32 >= n_rt) {
+      const int hit = behind != 0u ? __ffs(behind) - 1 : n_rt - 1 - first;
+      const long long before = __shfl_sync(0xffffffffu, end, hit > 0 ? hit - 1 : 0);
+      it.x0 += hit > 0 ? before : 0;
+      it.rt = first + hit;
+      chunk_item_of(s, g, it);
+      return it;
+    }
+    it.x0 += __shfl_sync(0xffffffffu, end, 31);
   }
 }
 
