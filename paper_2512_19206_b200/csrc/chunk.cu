@@ -1007,17 +1007,25 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       };
       {
         const int row0 = sg.row0, rows_all = sg.rows_all, dual = sg.dual, per = kTile >> copies_of();
-        // 16-byte piece p of the image: lane 8 (p / 128) + p % 8, channels 8 (p / 8 % 16) ..
-        const uint16_t* qb = a.q + (size_t)sg.stream * g * a.stride * kD;
-#pragma unroll 4
-        for (int p = tid; p < 2048 << dual; p += kSoftmaxThreads) {
-          const int at = 8 * (p >> 7) + (p & 7), row = row0 + (dual ? at : at & (per - 1)), c = (p >> 3) & 15;
-          uint4 y = make_uint4(0u, 0u, 0u, 0u);
-          if (row < rows_all) {
-            const int tok = row / g;
-            y = reinterpret_cast<const uint4*>(qb + ((size_t)(row - tok * g) * a.stride + tok) * kD)[c];
+        // 16-byte piece p of the image: lane 8 (p / 128) + p % 8, channels 8 (p / 8 % 16) ..  A thread's pieces are 16 lanes apart; eight of them are
+        // under way at once, and their rows divided by the heads by one multiplication (one after the other, each behind a division, they took 18 thousand
+        // cycles of a 256-row item).
+        const uint16_t* qb = a.q + (size_t)sg.stream * g * a.stride * kD + 8 * ((tid >> 3) & 15);
+        const uint32_t inv_g = g == 1 ? 0u : 0xFFFFFFFFu / (uint32_t)g + 1u;         // exact for rows below 2^29
+#pragma unroll 1
+        for (int i0 = 0; i0 < 8 << dual; i0 += 8) {
+          uint4 y[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int at = 16 * (i0 + i) + 8 * (tid >> 7) + (tid & 7), row = row0 + (dual ? at : at & (per - 1));
+            y[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (row < rows_all) {
+              const int tok = inv_g == 0u ? row : (int)__umulhi((uint32_t)row, inv_g);
+              y[i] = *reinterpret_cast<const uint4*>(qb + ((size_t)(row - tok * g) * a.stride + tok) * kD);
+            }
           }
-          sts128(qs + 16 * p, rows_to_half(y));
+#pragma unroll
+          for (int i = 0; i < 8; ++i) sts128(qs + 16 * (tid + 256 * (i0 + i)), rows_to_half(y[i]));
         }
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -1333,12 +1341,12 @@ cudaError_t launch_chunk_attention(const LayerView& lv, ChunkArgs& a, int n_sms,
   if (e != cudaSuccess) return e;
   *launches = 1;
   if (a.ctas == 1) return cudaSuccess;
-  // Few results per item: a warp per row, 32 rows per block.  Many (one or two long sequences): the eight warps of a block share a row's results, one row after
+  // Few results per item: a warp per row, 16 rows per block.  Many (one or two long sequences): the eight warps of a block share a row's results, one row after
   // another; then there are few rows, one per block.
   if (a.ctas > 8 * items)
     e = launch_dependent(chunk_merge_kernel<1>, dim3((unsigned)(a.ctas - 1), (unsigned)a.rows_cap), 256, 0, stream, lv, a, 1);
   else
-    e = launch_dependent(chunk_merge_kernel<8>, dim3((unsigned)(a.ctas - 1), (unsigned)((a.rows_cap + 31) / 32)), 256, 0, stream, lv, a, 32);
+    e = launch_dependent(chunk_merge_kernel<8>, dim3((unsigned)(a.ctas - 1), (unsigned)((a.rows_cap + 15) / 16)), 256, 0, stream, lv, a, 16);
   if (e != cudaSuccess) return e;
   *launches = 2;
   return cudaSuccess;
