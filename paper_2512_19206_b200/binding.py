@@ -7,6 +7,7 @@ module raises: there is no CPU or PyTorch fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 
@@ -136,6 +137,14 @@ def _stream():
     """The current stream's handle as an int.  (torch.cuda.current_stream() builds a Stream object: 3.3 us of a call whose
     launches take 5; the raw handle takes 0.1.)"""
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+
+_HERE_ALREADY = contextlib.nullcontext()
+
+
+def _device_of(dev):
+    """A context with `dev` current.  (Where it is already, torch's own costs 2 us for nothing.)"""
+    return _HERE_ALREADY if torch._C._cuda_getDevice() == dev.index else torch.cuda.device(dev)
 
 
 def _ptr(t: torch.Tensor | None):
@@ -304,35 +313,35 @@ class Cache:
         [B,Hq,n,128]; nothing is appended.  `counts`: new tokens per sequence (host ints, n each when absent); rows behind a sequence's count
         are left as they are.  `out`: float32 or bfloat16 (allocated as `dtype` when absent, zeros behind the counts).  `scratch`: a uint8
         device tensor of at least chunk_scratch_bytes(n) bytes (allocated here when absent)."""
-        return self._chunk(lib().mixkvq_chunk_attention, "mixkvq_chunk_attention", layer, k, v, q, scale, counts, out, scratch, dtype)
+        return self._chunk(0, "mixkvq_chunk_attention", layer, k, v, q, scale, counts, out, scratch, dtype)
 
     def chunk_step(self, layer, k, v, q, scale, counts=None, out=None, scratch=None, dtype=torch.float32):
         """chunk_attention, then the chunk is appended: the later chunk of a prompt (the first one too, on an empty layer)."""
-        return self._chunk(lib().mixkvq_chunk_step, "mixkvq_chunk_step", layer, k, v, q, scale, counts, out, scratch, dtype)
+        return self._chunk(1, "mixkvq_chunk_step", layer, k, v, q, scale, counts, out, scratch, dtype)
 
-    def _chunk(self, call, name, layer, k, v, q, scale, counts, out, scratch, dtype):
+    def _chunk(self, append, name, layer, k, v, q, scale, counts, out, scratch, dtype):
         cfg, n, dev = self.cfg, k.shape[2] if k.dim() == 4 else 0, self.mem.device
         if out is None:
             if dtype not in _OUT_TYPES:
                 raise ValueError(f"{name}: the output is float32 or bfloat16")
             out = (torch.empty if counts is None else torch.zeros)(q.shape, dtype=dtype, device=dev)
-        for t, heads, what in ((k, cfg.n_kv_heads, "k"), (v, cfg.n_kv_heads, "v"), (q, cfg.n_q_heads, "q"), (out, cfg.n_q_heads, "out")):
-            if t.shape != (cfg.batch, heads, n, 128) or not t.is_contiguous() or t.device != dev:
-                raise ValueError(f"{name}: {what} must be a contiguous [{cfg.batch}, {heads}, n, 128] tensor on {dev}")
+        kv, qo = (cfg.batch, cfg.n_kv_heads, n, 128), (cfg.batch, cfg.n_q_heads, n, 128)
+        for t, shape, what in ((k, kv, "k"), (v, kv, "v"), (q, qo, "q"), (out, qo, "out")):
+            if t.shape != shape or not t.is_contiguous() or t.device != dev:
+                raise ValueError(f"{name}: {what} must be a contiguous [{shape[0]}, {shape[1]}, n, 128] tensor on {dev}")
             if t.dtype != torch.bfloat16 and (t is not out or t.dtype != torch.float32):
                 raise ValueError(f"{name}: {what} has dtype {t.dtype}")
         if scratch is None:
             scratch = torch.empty(self.chunk_scratch_bytes(n), dtype=torch.uint8, device=dev)
         elif scratch.dtype != torch.uint8 or not scratch.is_contiguous() or scratch.device != dev:
             raise ValueError(f"{name}: scratch must be a contiguous uint8 tensor on {dev}")
-        arr = None
-        if counts is not None:
-            if len(counts) != cfg.batch:
-                raise ValueError(f"{name}: {cfg.batch} counts are needed, {len(counts)} were given")
-            arr = (C.c_int32 * cfg.batch)(*[int(c) for c in counts])
-        with torch.cuda.device(dev):
-            _check(call(self.handle, layer, k.data_ptr(), v.data_ptr(), q.data_ptr(), n, arr, out.data_ptr(), _OUT_TYPES[out.dtype], float(scale),
-                        scratch.data_ptr(), scratch.numel(), _stream()), name)
+        if counts is not None and len(counts) != cfg.batch:
+            raise ValueError(f"{name}: {cfg.batch} counts are needed, {len(counts)} were given")
+        call = (_native or _calls()).chunk
+        with _device_of(dev):
+            code = call(append, self.handle.value, layer, k, v, q, n, counts, out, _OUT_TYPES[out.dtype], scale, scratch, scratch.numel(), _stream())
+        if code:
+            raise MixKVQError(code, name)
         return out
 
     def chunk_scratch_bytes(self, n_tokens):
@@ -379,9 +388,12 @@ class Cache:
         ins = (q, k, v)
         if out is None:
             out = tuple(None if t is None else torch.zeros(t.shape, dtype=torch.bfloat16, device=dev) for t in ins)
-        strides = (C.c_int64 * 9)()
+        strides, ptrs, outs = [], [], []
         for i, (t, o, heads) in enumerate(zip(ins, out, (cfg.n_q_heads, cfg.n_kv_heads, cfg.n_kv_heads))):
             if i == 2 and t is None and o is None:
+                strides += (0, 0, 0)
+                ptrs.append(None)
+                outs.append(None)
                 continue
             if t is None or o is None:
                 raise ValueError("rope_axes: an input and its output come together")
@@ -391,10 +403,14 @@ class Cache:
             s = t.stride()
             if s[3] != 1 or not o.is_contiguous():
                 raise ValueError("rope_axes: the inputs' last dimension and the outputs must be contiguous")
-            strides[3 * i], strides[3 * i + 1], strides[3 * i + 2] = s[:3]
-        ptr = [0 if t is None else t.data_ptr() for t in (*ins, *out)]
-        with torch.cuda.device(dev):
-            _check(lib().mixkvq_rope_axes(self.handle, ptr[0], ptr[1], ptr[2], strides, n, *angles, ptr[3], ptr[4], ptr[5], _stream()), "mixkvq_rope_axes")
+            strides += s[:3]
+            ptrs.append(t.data_ptr())
+            outs.append(o.data_ptr())
+        call = (_native or _calls()).rope_axes
+        with _device_of(dev):
+            code = call(self.handle.value, *ptrs, strides, n, *angles, *outs, _stream())
+        if code:
+            raise MixKVQError(code, "mixkvq_rope_axes")
         return out
 
     def _head_major(self, name, n, **tensors):
@@ -409,7 +425,7 @@ class Cache:
         n = k.shape[2] if k.dim() == 4 else 0
         self._head_major("rope_axes_append", n, k=k, v=v, q=q)
         angles = self._angles("rope_axes_append", cos, sin, positions, axes, n)
-        with torch.cuda.device(self.mem.device):
+        with _device_of(self.mem.device):
             _check(lib().mixkvq_rope_axes_append(self.handle, layer, _ptr(k), _ptr(v), _ptr(q), *angles, n, _stream()), "mixkvq_rope_axes_append")
 
     def rope_axes_decode_step(self, layer, k, v, q, cos, sin, positions, axes, scale, out=None):
@@ -420,7 +436,7 @@ class Cache:
             out = torch.empty((q.shape[0], q.shape[1], 128), dtype=torch.float32, device=q.device)
         elif out.shape != (q.shape[0], q.shape[1], 128) or out.dtype != torch.float32 or out.device != q.device:
             raise ValueError("rope_axes_decode_step: out must be a float32 [B, Hq, 128] tensor on the cache's device")
-        with torch.cuda.device(self.mem.device):
+        with _device_of(self.mem.device):
             _check(lib().mixkvq_rope_axes_decode_step(self.handle, layer, _ptr(k), _ptr(v), _ptr(q), *angles, _ptr(out), float(scale), *self._ws, _stream()),
                    "mixkvq_rope_axes_decode_step")
         return out

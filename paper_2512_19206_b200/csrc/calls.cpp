@@ -3,10 +3,12 @@
 // A call on a small cache is bound by the host: its kernels take 3 to 4 us and the launch about 2.  ctypes converts ten
 // arguments in 2.6 us (measured on a null handle) and the address of a tensor costs 0.4 us of Python; here both
 // are a few attribute lookups in C (0.15 us on the null handle).  decode_attention on one sequence of 1024 tokens, calls
-// one after the other: 6.30 -> 5.26 us; calls whose GPU work is longer than the host's are unchanged.  Only the calls that a generation loop makes per layer and token are here; the
+// one after the other: 6.30 -> 5.26 us; calls whose GPU work is longer than the host's are unchanged.  Only the calls that a generation loop makes per layer and token (or draft) are here; the
 // others move enough data for ctypes not to matter.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
+
+#include <vector>
 
 #include "../../include/mixkvq.h"
 
@@ -139,6 +141,77 @@ PyObject* quantize_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return PyLong_FromLong(rc);
 }
 
+// Whole numbers of a sequence, as Int.
+template <typename Int>
+bool whole_numbers(PyObject* o, std::vector<Int>* v) {
+  PyObject* x = PySequence_Fast(o, "a sequence of whole numbers is needed");
+  if (!x) return false;
+  const Py_ssize_t n = PySequence_Fast_GET_SIZE(x);
+  bool ok = true;
+  try {
+    v->resize((size_t)n);
+  } catch (...) {
+    PyErr_NoMemory();
+    ok = false;
+  }
+  for (Py_ssize_t i = 0; ok && i < n; ++i) {
+    int over = 0;
+    const long long value = PyLong_AsLongLongAndOverflow(PySequence_Fast_GET_ITEM(x, i), &over);
+    if (PyErr_Occurred()) {
+      ok = false;
+    } else if (over || value != (long long)(Int)value) {
+      PyErr_SetString(PyExc_OverflowError, "a number is out of range");
+      ok = false;
+    } else {
+      (*v)[(size_t)i] = (Int)value;
+    }
+  }
+  Py_DECREF(x);
+  return ok;
+}
+
+// (whether the chunk is appended, handle, layer, k, v, q, tokens, counts or None, out, output type, scale, scratch, scratch bytes, stream)
+PyObject* chunk(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  void *h, *k, *v, *q, *out, *scratch, *st;
+  int append, layer, tokens, type, rc;
+  float scale;
+  size_t bytes;
+  std::vector<int32_t> counts;
+  if (!count_is(n, 14) || !integer(a[0], &append) || !raw(a[1], &h) || !integer(a[2], &layer) || !address(a[3], &k) || !address(a[4], &v) ||
+      !address(a[5], &q) || !integer(a[6], &tokens) || (a[7] != Py_None && !whole_numbers(a[7], &counts)) || !address(a[8], &out) ||
+      !integer(a[9], &type) || !real(a[10], &scale) || !address(a[11], &scratch) || !size(a[12], &bytes) || !raw(a[13], &st))
+    return nullptr;
+  const int32_t* per_sequence = a[7] != Py_None ? counts.data() : nullptr;
+  Py_BEGIN_ALLOW_THREADS
+  rc = append ? mixkvq_chunk_step(cache_of(h), layer, k, v, q, tokens, per_sequence, out, type, scale, scratch, bytes, st)
+              : mixkvq_chunk_attention(cache_of(h), layer, k, v, q, tokens, per_sequence, out, type, scale, scratch, bytes, st);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+// (handle, addresses of q, k, v, their nine strides, tokens, addresses of cos and sin, positions in the tables, address of the coordinates, axes, the axis
+// of every pair (bytes), addresses of the outputs, stream)
+PyObject* rope_axes(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  void *p[10], *st;
+  int tokens, positions, axes, rc;
+  std::vector<int64_t> strides;
+  char* pairs;
+  Py_ssize_t n_pairs;
+  if (!count_is(n, 16) || !raw(a[0], &p[0]) || !raw(a[1], &p[1]) || !raw(a[2], &p[2]) || !raw(a[3], &p[3]) || !whole_numbers(a[4], &strides) ||
+      !integer(a[5], &tokens) || !raw(a[6], &p[4]) || !raw(a[7], &p[5]) || !integer(a[8], &positions) || !raw(a[9], &p[6]) || !integer(a[10], &axes) ||
+      PyBytes_AsStringAndSize(a[11], &pairs, &n_pairs) || !raw(a[12], &p[7]) || !raw(a[13], &p[8]) || !raw(a[14], &p[9]) || !raw(a[15], &st))
+    return nullptr;
+  if (strides.size() != 9 || n_pairs != 64) {
+    PyErr_SetString(PyExc_ValueError, "nine strides and 64 channel pairs are needed");
+    return nullptr;
+  }
+  Py_BEGIN_ALLOW_THREADS
+  rc = mixkvq_rope_axes(cache_of(p[0]), p[1], p[2], p[3], strides.data(), tokens, static_cast<const float*>(p[4]), static_cast<const float*>(p[5]),
+                        positions, static_cast<const int32_t*>(p[6]), axes, reinterpret_cast<const uint8_t*>(pairs), p[7], p[8], p[9], st);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
 template <typename F>
 PyCFunction fast(F f) {
   return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f));
@@ -148,6 +221,8 @@ PyMethodDef methods[] = {{"decode_attention", fast(decode_attention), METH_FASTC
                          {"decode_step", fast(decode_step), METH_FASTCALL, nullptr},
                          {"rope_decode_step", fast(rope_decode_step), METH_FASTCALL, nullptr},
                          {"quantize_append", fast(quantize_append), METH_FASTCALL, nullptr},
+                         {"chunk", fast(chunk), METH_FASTCALL, nullptr},
+                         {"rope_axes", fast(rope_axes), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
