@@ -246,8 +246,7 @@ int mixkvq_prefill(mixkvq_cache* cache, int layer, const void* k_dev, const void
  * Numeric range: products are fp16 with fp32 accumulation, so |q|, |k|, |v| and dequantized elements must stay below 65504; elements below
  * 2^-14 round to fp16 subnormals.  A NaN or an infinity among the new tokens reaches the rows that attend to it and no others.
  * softmax_scale > 0; fragment layout; n_tokens_max <= MIXKVQ_CHUNK_MAX_TOKENS (MIXKVQ_E_UNSUPPORTED otherwise); scratch too small:
- * MIXKVQ_E_BUFFER_TOO_SMALL.  A wait that runs out sets MIXKVQ_DEV_COPY_TIMEOUT; the rows concerned are then wrong (0 where nothing
- * contributed).  Nothing is allocated and nothing synchronises with the host. */
+ * MIXKVQ_E_BUFFER_TOO_SMALL.  A wait that runs out sets MIXKVQ_DEV_COPY_TIMEOUT; the rows concerned are then wrong.  Nothing is allocated and nothing synchronises with the host. */
 enum { MIXKVQ_OUT_FLOAT = 0, MIXKVQ_OUT_BF16 = 1 };
 #define MIXKVQ_CHUNK_MAX_TOKENS (1 << 24)
 size_t mixkvq_chunk_scratch_bytes(const mixkvq_config* cfg, int n_tokens_max);
@@ -328,11 +327,12 @@ int mixkvq_decode_attention_noalloc(mixkvq_cache* cache, int layer, const void* 
  * handle: the next decode attention of every layer then waits for all earlier work of the stream before its first read. */
 int mixkvq_cache_written_externally(mixkvq_cache* cache);
 
-/* Test hook for the give-up path of the decode-attention kernel (fragment layout) and of the prefill attention.  While
+/* Test hook for the give-up paths of the decode-attention kernel (fragment layout), the prefill and the chunk attention.  While
  * extra_bytes > 0 (a multiple of 16), the barrier of the first staged copy of every warp pair (decode) or of every
  * CTA's first key tile (prefill) is armed for extra_bytes more than the copy delivers, so it never completes, and every
  * wait gives up after max_polls polls (0: the default): the call returns, the device status word carries
- * MIXKVQ_DEV_COPY_TIMEOUT, the decode output rows are zero and the prefill output is left unwritten.  Nothing faults or
+ * MIXKVQ_DEV_COPY_TIMEOUT, the decode output rows are zero and the prefill output is left unwritten.  In the chunk attention
+ * the CTAs leave out the announcement of their first key tile instead; its output is then undefined.  Nothing faults or
  * hangs: the copies themselves are the normal ones.  (0, 0) restores normal operation. */
 int mixkvq_test_arm_copy_timeout(mixkvq_cache* cache, uint32_t extra_bytes, uint32_t max_polls);
 

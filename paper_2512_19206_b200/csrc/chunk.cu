@@ -36,9 +36,10 @@ constexpr int kBarOff = kMlOff + 1024;
 constexpr int kBars = 21;
 constexpr int kReaders = 26;                              // of a segment: 8 softmax, 16 producer warps, the issuing one, the L2 requests
 constexpr int kSegOff = kBarOff + 8 * kBars + 16;         // (the tensor-memory address and the producers' progress behind the barriers)
-constexpr int kSmem = kSegOff + 2 * 64;
+constexpr int kPoisonOff = kSegOff + 2 * 64;            // two segments' Poison
+constexpr int kSmem = kPoisonOff + 2 * (4 + 3 * kD * 4);
 enum Bar { kQFull = 0, kKFull = 1, kVFull = 3, kKEmpty = 5, kVEmpty = 7, kSFull = 9, kPReady = 11, kODone = 13, kDone = 15, kSegFull = 17, kSegEmpty = 19 };
-constexpr uint32_t kPolls = 1u << 21;
+constexpr uint32_t kPolls = 1u << 19;                    // a poll that finds nothing returns after about 4 us: two seconds
 constexpr float kRaise = 10.f;
 constexpr int kAhead = 8;
 constexpr int kProducerNap = 40;
@@ -159,8 +160,8 @@ struct Rows {                            // a stream's unquantized rows: residua
   }
 };
 
-// A warp's unit: every fourth (the keys' warps: every eighth) one of the stream, from tile to tile.  (Blocks and units are counted on; a division and two long multiplications per tile
-// and warp were a fifth of the instructions.)
+// A warp's unit: every fourth (the keys' warps: every eighth) one of the stream, from tile to tile.  (Blocks and units are counted on; a division and
+// two long multiplications per tile and warp were a fifth of the instructions.)
 struct Cursor {
   const char* blk;                       // its block
   const uint2* entry;                    // the block's table entry
@@ -305,7 +306,7 @@ __device__ __forceinline__ void put_promoted(Promoted& p, uint32_t tile, uint32_
   }
   if (kU4 == 1 && p.n4 > 0) {
     // UINT4 channels: (c_lo + 4 c_hi) s + z is what the base store left, plus 4 c_hi s.  (A second rounding to fp16.  With the low codes read again, to round
-    // once, every four channels cost a round trip to the L2 cache: 7b shape, three tiers, draft-sized chunk of eight sequences, LOW / HIGH us.)
+    // once, every four channels cost a round trip to the L2 cache: 7b shape, three tiers, draft-sized chunk of eight sequences, 158 / 137 us.)
     const int pairs = (p.n4 + 1) >> 1, bit = high_bit(lane);
     const uint32_t* high = high_plane(p, lane);
 #pragma unroll 1
@@ -397,16 +398,45 @@ __device__ __forceinline__ void copy_key_rows(const Rows& x, int t, uint32_t til
     for (int i = 0; i < 4; ++i) sts128(tile + (4 * w + i) * 2048 + (c + (lane >> 3)) * 128 + (lane & 7) * 16, rows_to_half(y[i]));
   }
 }
-__device__ __forceinline__ void copy_value_rows(const Rows& x, int t, uint32_t tile, int w, int half, int lane) {
+// Values that are no numbers (in fp16: beyond 65504 too).  The tensor core multiplies a masked value with a probability of 0, and 0 times NaN or infinity
+// is NaN: one such element among the new tokens would reach the rows before its own.  They go to the product as zeros, and what they do to the rows that see
+// them is kept per channel: the first new token (-1: a row of the window or the sink) with a NaN, with infinity, with minus infinity.  `any`: there is one.
+struct Poison {
+  int any, first[3][kD];
+};
+constexpr int kNever = 0x7FFFFFFF;
+__device__ __forceinline__ float poison_of(const Poison& p, int channel, int tok) {     // what a row of token tok has to add
+  const bool nan = p.first[0][channel] <= tok, plus = p.first[1][channel] <= tok, minus = p.first[2][channel] <= tok;
+  return nan || (plus && minus) ? __int_as_float(0x7FFFFFFF) : plus ? INFINITY : minus ? -INFINITY : 0.f;
+}
+__device__ __forceinline__ uint32_t not_finite(uint32_t h) { return ((h & 0x7C007C00u) + 0x04000400u) & 0x80008000u; }   // (either half of an fp16 pair)
+
+__device__ __forceinline__ void copy_value_rows(const Rows& x, int t, uint32_t tile, int w, int half, int lane, Poison* poison) {
   const int row = kTile * t + 32 * w + lane;
   const uint4* src = row < x.total ? x.row(row) + 8 * half : nullptr;
+  const uint32_t to = tile + 8 * half * 2048 + (4 * w + (lane >> 3)) * 128 + (lane & 7) * 16;
+  uint32_t bad = 0u;
 #pragma unroll
   for (int c = 0; c < 8; c += 4) {
     uint4 y[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) y[i] = src != nullptr ? src[c + i] : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sts128(tile + (8 * half + c + i) * 2048 + (4 * w + (lane >> 3)) * 128 + (lane & 7) * 16, rows_to_half(y[i]));
+    for (int i = 0; i < 4; ++i) {
+      y[i] = rows_to_half(y[i]);
+      bad |= not_finite(y[i].x) | not_finite(y[i].y) | not_finite(y[i].z) | not_finite(y[i].w);
+      sts128(to + (c + i) * 2048, y[i]);
+    }
+  }
+  if (bad != 0u) {                       // (the lane's own pieces; a call here took the kernel's registers apart)
+#pragma unroll 1
+    for (int e = 0; e < kD / 2; ++e) {
+      const uint32_t at = to + (e >> 3) * 2048 + 2 * (e & 7), h = lds16(at);
+      if ((h & 0x7C00u) != 0x7C00u) continue;
+      atomicMin(&poison->first[(h & 0x3FFu) ? 0 : (h & 0x8000u) ? 2 : 1][64 * half + e], row < x.c0 ? -1 : row - x.c0);
+      sts16(at, 0u);
+    }
+    *reinterpret_cast<volatile int*>(&poison->any) = 1;
   }
 }
 
@@ -637,6 +667,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + kBarOff + 8 * kBars);
   volatile int* progress = reinterpret_cast<volatile int*>(tmem_slot + 1);     // the tile that the producers are at
   Segment* segments = reinterpret_cast<Segment*>(smem + kSegOff);              // two places
+  Poison* poison = reinterpret_cast<Poison*>(smem + kPoisonOff);               // of the segments in them
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   if (warp == kIssueWarp) {
@@ -646,8 +677,10 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
   if (tid == 0) {
     for (int i = 0; i < kBars; ++i) mbar_init(bar(i), arrivals(i));
     *progress = 0;
+    poison[0].any = poison[1].any = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  if (tid < 2 * 3 * kD) poison[tid / (3 * kD)].first[tid / kD % 3][tid % kD] = kNever;
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -795,6 +828,10 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
         int n = 0;
         auto publish = [&](const Segment& sg) {
           if (n >= 2 && !wait_ns(Literal<500>{}, kSegEmpty + (n & 1), (uint32_t)((n >> 1) - 1) & 1u)) return false;
+          if (n >= 2 && poison[n & 1].any != 0) {          // (all of the segment before in this place is over, its output too)
+            for (int i = 0; i < 3 * kD; ++i) poison[n & 1].first[i / kD][i % kD] = kNever;
+            poison[n & 1].any = 0;
+          }
           segments[n & 1] = sg;
           mbar_arrive(bar(kSegFull + (n & 1)));
           n += 1;
@@ -912,7 +949,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
                      reinterpret_cast<const uint16_t*>(lv.sink + (size_t)stream * lv.sink_stride) + (size_t)lv.sink_len * kD,
                      a.v + (size_t)stream * a.stride * kD, r, c0, total};
         if (!(ok = free_stage())) break;
-        copy_value_rows(x, j - packed_tiles, stage(), w, half, lane);
+        copy_value_rows(x, j - packed_tiles, stage(), w, half, lane, poison + (n & 1));
         made();
       }
       if (!ok) break;
@@ -1071,13 +1108,17 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       ended[0] += 1;
       ended[1] += both;
       float* part = a.parts + ((size_t)blockIdx.x * 2 + sg.part) * a.rows_cap * (kD + 2);
-      segment_taken(n);
+      // (read when all products of the segment are known to be over)
+      const Poison& bad = poison[n & 1];
+      auto any_bad = [&]() { return *reinterpret_cast<const volatile int*>(&bad.any) != 0; };
       const float l_run = mine ? state.sum() : 0.f, m_run = mine ? state.m : -INFINITY;
       auto weight = [](float m, float l, float top) { return m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : ex2(m - top); };   // (a row of NaNs counts)
       if (dual) {
         if (!idle) {
           const bool exists = row < rows_all;
-          const float inv = whole ? (l_run == 0.f ? 0.f : 1.f / l_run) : l_run == 0.f ? 0.f : 1.f;
+          // (every row sees a key: a sum of 0 means that all its logits are -inf, and gives NaN)
+          const float inv = whole ? 1.f / l_run : l_run == 0.f ? 0.f : 1.f;
+          const bool add_bad = any_bad();
           const int tok = min(row, rows_all - 1) / g;
           const size_t orow = ((size_t)stream * g + (row - tok * g)) * a.stride + tok;
 #pragma unroll 1
@@ -1088,6 +1129,10 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
             if (!exists) continue;
 #pragma unroll
             for (int i = 0; i < 32; ++i) y[i] = inv == 0.f ? 0.f : __uint_as_float(u[i]) * inv;
+            if (add_bad) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) y[i] += poison_of(bad, d + i, tok);
+            }
             if (whole) {
               store_row(a, orow, d, y);
             } else {
@@ -1158,7 +1203,8 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
               l += x.y * f[i];
             }
           }
-          const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+          const float inv = whole ? 1.f / l : 1.f;
+          const bool add_bad = any_bad();
           const int t = (row0 + r) / g;
           const size_t orow = ((size_t)stream * g + (row0 + r - t * g)) * a.stride + t;
 #pragma unroll 1
@@ -1175,6 +1221,12 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
                 y.w = fmaf(__uint_as_float(o.w), f[i], y.w);
               }
             y.x *= inv; y.y *= inv; y.z *= inv; y.w *= inv;
+            if (add_bad) {
+              y.x += poison_of(bad, 4 * c, t);
+              y.y += poison_of(bad, 4 * c + 1, t);
+              y.z += poison_of(bad, 4 * c + 2, t);
+              y.w += poison_of(bad, 4 * c + 3, t);
+            }
             if (whole)
               store4(a, orow * kD + 4 * c, y);
             else
@@ -1183,6 +1235,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
           if (!whole && (tid & ((1 << lg_threads) - 1)) == 0) reinterpret_cast<float2*>(part + (size_t)a.rows_cap * kD)[r] = make_float2(top, l);
         }
       }
+      segment_taken(n);
       tc_fence_before();
     }
   }
@@ -1280,7 +1333,7 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant_
       }
     }
     if (exists && sub == 0) {
-      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const float inv = 1.f / l;
       const int row = kChunkRows * it.rt + prow, tok = row / g;
       const size_t at = ((((size_t)it.b * lv.Hq + it.hk * g + (row - tok * g)) * a.stride + tok) * kD) + 4 * lane;
       store4(a, at, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));

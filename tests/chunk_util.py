@@ -47,8 +47,8 @@ def allowed(p, q, K, V, scale):
 def check(w, out, sts, kn, vn, qn, counts, scale=None, only=None):
     """Compares out [B, Hq, n, 128] with the oracle's streams; rows behind a count are the caller's affair."""
     scale = scale or W.softmax_scale()
-    out = out.double().cpu()
     step = {torch.bfloat16: 2.0 ** -8}.get(out.dtype, 0.0)
+    out = out.double().cpu()
     for (b, hk), st in sts.items():
         m = counts[b]
         if m == 0 or (only and (b, hk) not in only):
