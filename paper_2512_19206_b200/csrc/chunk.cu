@@ -829,7 +829,8 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
         auto publish = [&](const Segment& sg) {
           if (n >= 2 && !wait_ns(Literal<500>{}, kSegEmpty + (n & 1), (uint32_t)((n >> 1) - 1) & 1u)) return false;
           if (n >= 2 && poison[n & 1].any != 0) {          // (all of the segment before in this place is over, its output too)
-            for (int i = 0; i < 3 * kD; ++i) poison[n & 1].first[i / kD][i % kD] = kNever;
+#pragma unroll 1
+            for (int i = 0; i < 3 * kD; ++i) poison[n & 1].first[0][i] = kNever;
             poison[n & 1].any = 0;
           }
           segments[n & 1] = sg;
@@ -1108,9 +1109,6 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       ended[0] += 1;
       ended[1] += both;
       float* part = a.parts + ((size_t)blockIdx.x * 2 + sg.part) * a.rows_cap * (kD + 2);
-      // (read when all products of the segment are known to be over)
-      const Poison& bad = poison[n & 1];
-      auto any_bad = [&]() { return *reinterpret_cast<const volatile int*>(&bad.any) != 0; };
       const float l_run = mine ? state.sum() : 0.f, m_run = mine ? state.m : -INFINITY;
       auto weight = [](float m, float l, float top) { return m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : ex2(m - top); };   // (a row of NaNs counts)
       if (dual) {
@@ -1118,7 +1116,6 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
           const bool exists = row < rows_all;
           // (every row sees a key: a sum of 0 means that all its logits are -inf, and gives NaN)
           const float inv = whole ? 1.f / l_run : l_run == 0.f ? 0.f : 1.f;
-          const bool add_bad = any_bad();
           const int tok = min(row, rows_all - 1) / g;
           const size_t orow = ((size_t)stream * g + (row - tok * g)) * a.stride + tok;
 #pragma unroll 1
@@ -1129,10 +1126,6 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
             if (!exists) continue;
 #pragma unroll
             for (int i = 0; i < 32; ++i) y[i] = inv == 0.f ? 0.f : __uint_as_float(u[i]) * inv;
-            if (add_bad) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) y[i] += poison_of(bad, d + i, tok);
-            }
             if (whole) {
               store_row(a, orow, d, y);
             } else {
@@ -1204,7 +1197,6 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
             }
           }
           const float inv = whole ? 1.f / l : 1.f;
-          const bool add_bad = any_bad();
           const int t = (row0 + r) / g;
           const size_t orow = ((size_t)stream * g + (row0 + r - t * g)) * a.stride + t;
 #pragma unroll 1
@@ -1221,18 +1213,27 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
                 y.w = fmaf(__uint_as_float(o.w), f[i], y.w);
               }
             y.x *= inv; y.y *= inv; y.z *= inv; y.w *= inv;
-            if (add_bad) {
-              y.x += poison_of(bad, 4 * c, t);
-              y.y += poison_of(bad, 4 * c + 1, t);
-              y.z += poison_of(bad, 4 * c + 2, t);
-              y.w += poison_of(bad, 4 * c + 3, t);
-            }
             if (whole)
               store4(a, orow * kD + 4 * c, y);
             else
               reinterpret_cast<float4*>(part + (size_t)r * kD)[c] = y;
           }
           if (!whole && (tid & ((1 << lg_threads) - 1)) == 0) reinterpret_cast<float2*>(part + (size_t)a.rows_cap * kD)[r] = make_float2(top, l);
+        }
+      }
+      if (*reinterpret_cast<volatile int*>(&poison[n & 1].any) != 0) {     // (the segment's products are over, and the thread's own outputs stored)
+        const int lg_threads = dual ? 0 : 1 + lg_copies, r = tid >> lg_threads, t = (row0 + r) / g;
+        const size_t orow = ((size_t)stream * g + (row0 + r - t * g)) * a.stride + t;
+#pragma unroll 1
+        for (int d = 0; d < kD && r < rows; ++d) {
+          const float x = poison_of(poison[n & 1], d, t);
+          if (x == 0.f || (((d >> 2) ^ tid) & ((1 << lg_threads) - 1)) != 0) continue;
+          if (!whole)
+            part[(size_t)r * kD + d] += x;
+          else if (a.out_bf16)
+            static_cast<__nv_bfloat16*>(a.out)[orow * kD + d] += __float2bfloat16_rn(x);
+          else
+            static_cast<float*>(a.out)[orow * kD + d] += x;
         }
       }
       segment_taken(n);
