@@ -217,8 +217,8 @@ int mixkvq_merge_partials(const float* o_parts_dev, const float* lse_parts_dev, 
 /* The prefill phase of Section 4.2 for one layer: causal attention of the prompt over itself in full precision (Eq. 1,
  * position i sees positions 0..i), then the prompt's keys and values go into the cache exactly as
  * mixkvq_quantize_append(n_tokens) would put them (complete windows quantized, the last 1..R tokens in the residual
- * window).  The layer must be empty (MIXKVQ_E_UNSUPPORTED otherwise: a later chunk would have to attend to a
- * dequantized cache).
+ * window).  The layer must be empty (MIXKVQ_E_UNSUPPORTED otherwise: a later chunk attends to a
+ * dequantized cache, which is mixkvq_chunk_step).
  *   k_dev, v_dev [B, Hkv, n_tokens, 128], q_dev [B, Hq, n_tokens, 128] bf16 (post-RoPE)  ->  out_dev [B, Hq, n_tokens, 128] float
  *   scratch_dev: device memory of at least mixkvq_prefill_scratch_bytes(cfg, n_tokens) bytes, 16-byte aligned, owned by
  *   the caller and free for reuse once the work enqueued by this call has run (it holds K and V of the prompt
@@ -245,8 +245,10 @@ int mixkvq_prefill(mixkvq_cache* cache, int layer, const void* k_dev, const void
  *   run (two calls that may overlap on the GPU need one each, two captured graphs too unless they never run at the same time).
  * Numeric range: products are fp16 with fp32 accumulation, so |q|, |k|, |v| and dequantized elements must stay below 65504; elements below
  * 2^-14 round to fp16 subnormals.  A NaN or an infinity among the new tokens reaches the rows that attend to it and no others.
- * softmax_scale > 0; fragment layout; n_tokens_max <= MIXKVQ_CHUNK_MAX_TOKENS (MIXKVQ_E_UNSUPPORTED otherwise); scratch too small:
- * MIXKVQ_E_BUFFER_TOO_SMALL.  A wait that runs out sets MIXKVQ_DEV_COPY_TIMEOUT; the rows concerned are then wrong.  Nothing is allocated and nothing synchronises with the host. */
+ * The tensor core's sums are truncated, not rounded: about 3.5e-7 of the output per 128 tokens held, in one direction (1.8e-4 at 65536).
+ * softmax_scale > 0; out_dev and scratch_dev overlap no other argument (MIXKVQ_E_INVALID_ARG); fragment layout, n_tokens_max <=
+ * MIXKVQ_CHUNK_MAX_TOKENS (MIXKVQ_E_UNSUPPORTED otherwise); scratch too small: MIXKVQ_E_BUFFER_TOO_SMALL.  A wait that runs out sets
+ * MIXKVQ_DEV_COPY_TIMEOUT; the rows concerned are then wrong.  Nothing is allocated and nothing synchronises with the host. */
 enum { MIXKVQ_OUT_FLOAT = 0, MIXKVQ_OUT_BF16 = 1 };
 #define MIXKVQ_CHUNK_MAX_TOKENS (1 << 24)
 size_t mixkvq_chunk_scratch_bytes(const mixkvq_config* cfg, int n_tokens_max);

@@ -254,9 +254,12 @@ def test_refusals(binding):
         with pytest.raises(ValueError):
             cache.chunk_attention(0, **{**dict(k=k, v=v, q=q, scale=SCALE), **bad})
     small = torch.empty(cache.chunk_scratch_bytes(8) - 16, dtype=torch.uint8, device="cuda")
+    over = torch.empty(cache.chunk_scratch_bytes(8) + v.numel() * 2, dtype=torch.uint8, device="cuda")
+    inside = over[-v.numel() * 2 - 16:-16].view(torch.bfloat16).view(v.shape)
     odd = torch.empty(cache.chunk_scratch_bytes(8) + 16, dtype=torch.uint8, device="cuda")[1:]
     for bad, code in ((dict(counts=[9, 1]), -1), (dict(counts=[-1, 1]), -1), (dict(scale=0.0), -1), (dict(scale=float("nan")), -1), (dict(layer=1), -1),
-                      (dict(scratch=small), -4), (dict(scratch=odd), -3)):
+                      (dict(scratch=small), -4), (dict(scratch=odd), -3), (dict(out=q), -1),
+                      (dict(v=inside, scratch=over), -1)):
         with pytest.raises(binding.MixKVQError) as e:
             cache.chunk_attention(**{**dict(layer=0, k=k, v=v, q=q, scale=SCALE), **bad})
         assert e.value.code == code

@@ -165,7 +165,7 @@ def test_refusals(binding):
         with pytest.raises(ValueError):
             cache.rope_axes(**{**args, **bad})
     wide = torch.zeros((B, Hq, n, 128 + 4), dtype=torch.bfloat16, device="cuda")
-    for bad, code in ((dict(axes=[2] * 64), -1), (dict(q=wide[..., :128]), -3), (dict(out=(q, q[:, :Hkv].view(B, Hkv, n, 128) if False else k, k)), -1)):
+    for bad, code in ((dict(axes=[2] * 64), -1), (dict(q=wide[..., :128]), -3), (dict(out=(q, k, k)), -1)):
         args = dict(q=q, k=k, v=v, cos=cos, sin=sin, positions=pos, axes=axes)
         with pytest.raises(binding.MixKVQError) as e:
             cache.rope_axes(**{**args, **bad})
