@@ -49,6 +49,10 @@ __device__ __forceinline__ void sts16(uint32_t a, uint32_t x) { asm volatile("st
 __device__ __forceinline__ void sts128(uint32_t a, uint4 x) {
   asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
 }
+// Four 8 x 8 pieces of 16-bit elements, a lane holding two neighbouring ones of row lane / 4 of each; lane 8 m + i gives the address of row i of piece m.
+__device__ __forceinline__ void store_pieces(uint32_t a, uint32_t x0, uint32_t x1, uint32_t x2, uint32_t x3) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x0), "r"(x1), "r"(x2), "r"(x3) : "memory");
+}
 __device__ __forceinline__ uint4 lds128(uint32_t a) {
   uint4 v;
   asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
@@ -267,8 +271,9 @@ __device__ __forceinline__ void make_keys(const PackedKeys& p, uint32_t tile, ui
     sts32(at + 320, bf16x2_to_f16x2(__byte_perm(p.meta.z, p.meta.w, 0x7632)));
   }
   __syncwarp();
-  // (a rolled loop: every role's straight-line code together runs out of the instruction cache)
-  const uint32_t out = tile + 4 * w * 2048 + 4 * lane, in = scratch + 32 * (lane & 3);
+  // (a rolled loop: every role's straight-line code together runs out of the instruction cache.  Four pieces a store: against a store of 4 bytes per piece
+  // and lane, draft-sized chunk over 8 sequences of the 7b shape 108 us and 111; the values' warps, which have fewer registers, gained nothing by it.)
+  const uint32_t out = tile + 4 * w * 2048 + 256 * (lane >> 3) + 16 * (lane & 7), in = scratch + 32 * (lane & 3);
 #pragma unroll 1
   for (int i = 0; i < 4; ++i) {          // of every 16 channels the upper or lower 8 (ch), channels 64 kh ..
     const int ch = i >> 1, kh = i & 1;
@@ -281,9 +286,12 @@ __device__ __forceinline__ void make_keys(const PackedKeys& p, uint32_t tile, ui
                            (ch ? p.h1.w : p.h1.y) >> (8 * kh)};
 #pragma unroll
     for (int r = 0; r < 4; ++r)          // rows 8 r ..
+    {
+      uint32_t x[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        sts32(to + r * 2048 + 2 * k * 128, kU4 == 2 ? dequant4(magic, c[r], h[r], k, s[k], z[k]) : dequant2(magic, c[r], k, s[k], z[k]));
+      for (int k = 0; k < 4; ++k) x[k] = kU4 == 2 ? dequant4(magic, c[r], h[r], k, s[k], z[k]) : dequant2(magic, c[r], k, s[k], z[k]);
+      store_pieces(to + r * 2048, x[0], x[1], x[2], x[3]);
+    }
   }
 }
 
@@ -636,18 +644,15 @@ __device__ __forceinline__ void store4(const ChunkArgs& a, size_t at, float4 y) 
   }
 }
 
-// Registers per thread of the roles: together no more than the block is launched with.
+// Registers per thread of the roles: together no more than the block is launched with.  (Eight more for the keys' warps at the softmax warps' cost, 112 and
+// 72: one sequence of 120000 tokens, 8b shape, one new token, 94 us and 91; 7b shape, a chunk of 2048 tokens behind 32768, 1162 and 1173.)
 constexpr int kLaunchRegs = 72, kIssueRegs = 40;
 struct Registers {
   int softmax, keys, values;
 };
-__host__ __device__ constexpr Registers registers_of(int u4, bool v4) {
-  return u4 == 0 ? (v4 ? Registers{104, 72, 56} : Registers{112, 72, 48}) : (v4 ? Registers{96, 80, 56} : Registers{104, 80, 48});
-}
+__host__ __device__ constexpr Registers registers_of(bool v4) { return v4 ? Registers{96, 80, 56} : Registers{104, 80, 48}; }
 __host__ __device__ constexpr bool registers_fit(Registers r) { return 256 * (r.softmax + r.keys + r.values) + 128 * kIssueRegs <= kThreads * kLaunchRegs; }
-static_assert(registers_fit(registers_of(0, false)) && registers_fit(registers_of(0, true)) && registers_fit(registers_of(1, false)) &&
-                  registers_fit(registers_of(1, true)) && registers_fit(registers_of(2, false)) && registers_fit(registers_of(2, true)),
-              "the shares are taken from what the thread block was launched with");
+static_assert(registers_fit(registers_of(false)) && registers_fit(registers_of(true)), "the shares are taken from what the thread block was launched with");
 template <bool kMore, int kRegs>
 __device__ __forceinline__ void set_registers() {
   if constexpr (kMore)
@@ -660,7 +665,7 @@ __device__ __forceinline__ void set_registers() {
 // 2 the 4-bit base (dense high plane)
 template <int kU4, bool kV4>
 __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __grid_constant__ LayerView lv, const __grid_constant__ ChunkArgs a) {
-  constexpr Registers kRegs = registers_of(kU4, kV4);
+  constexpr Registers kRegs = registers_of(kV4);
   extern __shared__ __align__(128) unsigned char smem[];
   const uint32_t sbase = smem_u32(smem), qs = sbase, ks = sbase + 2 * kTileBytes, vs = sbase + 4 * kTileBytes;
   auto bar = [&](int i) { return sbase + (uint32_t)kBarOff + 8u * (uint32_t)i; };
