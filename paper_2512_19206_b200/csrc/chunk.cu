@@ -7,15 +7,22 @@
 //   warps 8-15, 16-23   make the tiles: four warps the keys of even tiles, four those of odd ones, eight the values.  Packed codes become fp16 in registers
 //                       (c s + z, one rounding) and go to shared memory in the tensor core's canonical layout; an unquantized row is copied
 //                       with bf16 -> fp16.  The packed bytes are read once per 256 query rows and never written back dequantized.
-//   warp 24             one thread issues every tcgen05.mma: S = Q K^T (operands in shared memory), O += P V (P in tensor memory).
+//   warp 24             issues every tcgen05.mma: S = Q K^T (operands in shared memory), O += P V (P in tensor memory).
+//   warp 25, warp 26    the thread block's segments (its part of an item), two ahead; requests of later tiles' bytes into the L2 cache.
 //   warps 0-3, 4-7      two softmax groups ("slots"), thread = query row = lane of tensor memory.  An item of more than 128 rows has its first 128 rows
 //                       in slot 0 and the others in slot 1; in a smaller one both slots have the same rows, slot 0 the even key tiles and slot 1
 //                       the odd ones, and their results meet at the end: the tensor core works for one slot while the other is in its softmax.
 // Codes lie in the cache as mma.sync A fragments: the lane with row r and pair t of an 8 x 8 piece holds its two neighbouring channels (keys) or
 // tokens (values).  With keys and values both stored K-major in shared memory that pair is 4 bytes at 16 r + 4 t = 4 lane of a core matrix, so a
-// warp's store is 128 contiguous bytes.
-// The running maximum is raised (and O rescaled, in tensor memory) only when a row's logits exceed it by more than 2^8: P stays below 256, far
+// warp's store is 128 contiguous bytes (the keys': four of them).
+// The running maximum is raised (and O rescaled, in tensor memory) only when a row's logits exceed it by more than 2^10: P stays below 1024, far
 // inside fp16, and the rescaling is rare.  P is fp16 (11 significant bits); sums, maxima, O are fp32.
+//
+// What bounds it (B200).  Few rows, long caches: the making of the tiles.  A key tile of 128 x 128 takes about 7000 warp instructions, half of them logic and
+// fp16 operations on codes, and 58 % of the issue slots are taken; a tile every 2900 cycles.  Eight sequences of 32768 tokens, 7b shape, 5 new tokens each:
+// 105 us (the first version, one warp for every task's waits and loads in the loops, 225), 1.05 TB/s of the packed bytes.  Many rows: a slot's chain of
+// product, softmax (3400 cycles of 128 logits a thread beside the tiles' making) and product: 2048 tokens behind 32768, 7b shape, 1179 us = 0.84 PFLOP/s
+// (2328 at first), the tensor pipe a third to a half of the time.
 #include <algorithm>
 
 #include "chunk.cuh"
