@@ -20,8 +20,8 @@
 //
 // What bounds it (B200).  Few rows, long caches: the making of the tiles.  A key tile of 128 x 128 takes about 7000 warp instructions, half of them logic and
 // fp16 operations on codes, and 58 % of the issue slots are taken; a tile every 2900 cycles.  Eight sequences of 32768 tokens, 7b shape, 5 new tokens each:
-// 105 us (the first version, one warp for every task's waits and loads in the loops, 225), 1.05 TB/s of the packed bytes.  Many rows: a slot's chain of
-// product, softmax (3400 cycles of 128 logits a thread beside the tiles' making) and product: 2048 tokens behind 32768, 7b shape, 1179 us = 0.84 PFLOP/s
+// 104 us (the first version, one warp for every task's waits and loads in the loops, 225), 1.05 TB/s of the packed bytes.  Many rows: a slot's chain of
+// product, softmax (3400 cycles of 128 logits a thread beside the tiles' making) and product: 2048 tokens behind 32768, 7b shape, 1158 us = 0.86 PFLOP/s
 // (2328 at first), the tensor pipe a third to a half of the time.
 #include <algorithm>
 
@@ -839,7 +839,14 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
         a.at[blockIdx.x] = it;
         int n = 0;
         auto publish = [&](const Segment& sg) {
-          if (n >= 2 && !wait_ns(Literal<500>{}, kSegEmpty + (n & 1), (uint32_t)((n >> 1) - 1) & 1u)) return false;
+          // (a segment takes as long as its item is: the limit holds for one in which nothing moves)
+          for (int seen = -1; n >= 2 && !wait_phase<500>(bar(kSegEmpty + (n & 1)), (uint32_t)((n >> 1) - 1) & 1u, a.max_polls);) {
+            if (*progress == seen) {
+              atomicOr(lv.status, (uint32_t)MIXKVQ_DEV_COPY_TIMEOUT);
+              return false;
+            }
+            seen = *progress;
+          }
           if (n >= 2 && poison[n & 1].any != 0) {          // (all of the segment before in this place is over, its output too)
 #pragma unroll 1
             for (int i = 0; i < 3 * kD; ++i) poison[n & 1].first[0][i] = kNever;
