@@ -169,6 +169,67 @@ def test_decode_step_behind_a_chunk(binding):
         assert torch.equal(a, b)
 
 
+def test_scratch_and_padding_of_any_content(binding):
+    """What lies in the scratch, in the rows behind the counts and in the output before the call has no effect, and those rows stay."""
+    cache, _, gen = plain_cache(binding, 3, 8, 2, 1700, 6, extra=200)
+    new = [t.cuda() for t in chunk(gen, 3, 8, 2, 200)]
+    counts = [200, 7, 0]
+    want = cache.chunk_attention(0, *new, SCALE, counts=counts, dtype=torch.bfloat16)
+    for t in new:
+        for b, c in enumerate(counts):
+            t[b, :, c:] = float("nan")
+    scratch = torch.full((cache.chunk_scratch_bytes(200),), 255, dtype=torch.uint8, device="cuda")
+    out = torch.full_like(new[2], float("inf"))
+    cache.chunk_attention(0, *new, SCALE, counts=counts, out=out, scratch=scratch)
+    assert cache.status() == 0
+    for b, c in enumerate(counts):
+        assert torch.equal(out[b, :, :c], want[b, :, :c]) and torch.isposinf(out[b, :, c:]).all()
+
+
+@pytest.mark.parametrize("magnitude", [1e-3, 30.0])
+def test_large_and_small_values(binding, magnitude):
+    """The output follows the values' size; what the chunk adds to the tolerance is relative to it (fp16 keeps 2^-12 of 2^-14 and more: 1e-3 N(0, 1) values,
+    and their scales of a third of a group's range, lose at most half of 2^-24 each, 3e-8 of values whose tolerance is above 1e-6)."""
+    w = W.small(W.CONFIGS["llama8b"], n_layers=1, batch=1, n_kv_heads=1, n_q_heads=4, tokens=600, **W.P24)
+    k, v, q = W.tokens(w, 0, 0, 600)
+    v = (v.float() * magnitude).to(torch.bfloat16)
+    cache = U.make_cache(binding, w)
+    cache.quantize_append(0, *(t[:, :, :560].contiguous().cuda() for t in (k, v, q)))
+    new = [t[:, :, 560:].contiguous() for t in (k, v, q)]
+    out = cache.chunk_attention(0, *(t.cuda() for t in new), SCALE)
+    assert cache.status() == 0
+    CU.check(w, out, CU.streams(w, [560], k, v, q), *new, [40])
+
+
+def test_one_token_is_a_decode_step(binding):
+    """A single new token's chunk and the decode step see the same keys; both stay within the decode's tolerance."""
+    w = W.small(W.CONFIGS["qwen7b"], n_layers=1, batch=2, tokens=601, **W.P27)
+    k, v, q = W.tokens(w, 0, 0, 601)
+    a = U.make_cache(binding, w)
+    a.quantize_append(0, *(t[:, :, :600].contiguous().cuda() for t in (k, v, q)))
+    new = [t[:, :, 600:].contiguous().cuda() for t in (k, v, q)]
+    out = a.chunk_attention(0, *new, SCALE)
+    step = a.decode_step(0, *new, SCALE)
+    assert a.status() == 0
+    assert float((out[:, :, 0] - step).abs().max()) <= 2e-3 + 2e-3        # (each within 2e-3 of the definition)
+
+
+def test_streams_beyond_four_gigabytes(binding):
+    """A cache whose last streams start beyond 2^32 bytes gives what a small one gives."""
+    gen = torch.Generator().manual_seed(3)
+    k, v, q = chunk(gen, 2, 16, 8, 700)
+    outs = []
+    for max_tokens in (800, 4_000_000):
+        cache = binding.Cache(binding.make_config(1, 2, 16, 8, max_tokens, **W.P27))
+        cache.quantize_append(0, *(t[:, :, :600].contiguous().cuda() for t in (k, v, q)))
+        outs.append(cache.chunk_attention(0, *(t[:, :, 600:].contiguous().cuda() for t in (k, v, q)), SCALE))
+        assert cache.status() == 0
+        big = cache.describe(0)
+        last = big.base_off + 15 * big.base_stride
+        del cache
+    assert last > 1 << 32 and torch.equal(*outs)
+
+
 def test_another_stream_and_two_scratches(binding):
     cache, _, gen = plain_cache(binding, 2, 8, 2, 900, 3, extra=64)
     new = [[t.cuda() for t in chunk(gen, 2, 8, 2, n)] for n in (3, 64)]
