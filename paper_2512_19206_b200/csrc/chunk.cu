@@ -278,10 +278,11 @@ __device__ __forceinline__ void make_keys(const PackedKeys& p, uint32_t tile, ui
     sts32(at + 320, bf16x2_to_f16x2(__byte_perm(p.meta.z, p.meta.w, 0x7632)));
   }
   __syncwarp();
-  // (a rolled loop: every role's straight-line code together runs out of the instruction cache.  Four pieces a store: against a store of 4 bytes per piece
+  // (a rolled loop: every role's straight-line code together runs out of the instruction cache.  Without UINT4 channels two rounds of it are shorter, 8 x 32768
+  // tokens of the 7b shape with drafts 104.7 us and 106.0; with them longer, 124.7 and 119.7 over ragged lengths.  Four pieces a store: against a store of 4 bytes per piece
   // and lane, draft-sized chunk over 8 sequences of the 7b shape 108 us and 111; the values' warps, which have fewer registers, gained nothing by it.)
   const uint32_t out = tile + 4 * w * 2048 + 256 * (lane >> 3) + 16 * (lane & 7), in = scratch + 32 * (lane & 3);
-#pragma unroll 1
+#pragma unroll (kU4 == 0 ? 2 : 1)
   for (int i = 0; i < 4; ++i) {          // of every 16 channels the upper or lower 8 (ch), channels 64 kh ..
     const int ch = i >> 1, kh = i & 1;
     const uint32_t at = in + 144 * ch + 16 * kh, to = out + 128 * ch + 1024 * kh;
