@@ -18,9 +18,9 @@
 // The running maximum is raised (and O rescaled, in tensor memory) only when a row's logits exceed it by more than 2^10: P stays below 1024, far
 // inside fp16, and the rescaling is rare.  P is fp16 (11 significant bits); sums, maxima, O are fp32.
 //
-// What bounds it (B200).  Few rows, long caches: the making of the tiles.  A key tile of 128 x 128 takes about 7000 warp instructions, half of them logic and
-// fp16 operations on codes, and 58 % of the issue slots are taken; a tile every 2900 cycles.  Eight sequences of 32768 tokens, 7b shape, 5 new tokens each:
-// 104 us (the first version, one warp for every task's waits and loads in the loops, 225), 1.05 TB/s of the packed bytes.  Many rows: a slot's chain of
+// What bounds it (B200).  Few rows, long caches: the making of the tiles.  A key tile of 128 x 128 takes about 7000 warp instructions, three fifths of them logic,
+// fp16 operations and stores of codes; 58 % of the issue slots are taken, a tile every 2900 cycles.  Eight sequences of 32768 tokens, 7b shape, 5 new tokens each:
+// 104 us (the first version 225), 1.05 TB/s of the packed bytes.  Many rows: a slot's chain of
 // product, softmax (3400 cycles of 128 logits a thread beside the tiles' making) and product: 2048 tokens behind 32768, 7b shape, 1158 us = 0.86 PFLOP/s
 // (2328 at first), the tensor pipe a third to a half of the time.
 #include <algorithm>
