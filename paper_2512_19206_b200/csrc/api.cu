@@ -99,6 +99,9 @@ uint64_t plan(const mixkvq_config* c, mixkvq_cache* h) {
   return kHeaderBytes + h->layer_stride * (uint64_t)c->n_layers;
 }
 
+// of the cache's memory, those that hold something
+uint64_t memory_bytes(const mixkvq_cache* h) { return kHeaderBytes + h->layer_stride * (uint64_t)h->cfg.n_layers; }
+
 size_t workspace_bytes(int S) { return (size_t)(kMaxCtas + 2 * S) * kPartialFloats * sizeof(float); }
 
 inline int fi(const mixkvq_cache* h, int layer, int b) { return layer * h->cfg.batch + b; }
@@ -383,10 +386,11 @@ int check_chunk(const mixkvq_cache* cache, int layer, const void* k_dev, const v
   return MIXKVQ_OK;
 }
 
-// Rotation with several axes: fills in the launch's arguments, or says what is wrong with the call's.  in_place: the outputs are the inputs.
+// Rotation with several axes: fills in the launch's arguments, or says what is wrong with the call's.  v_kept: head-major values that the rotation
+// leaves alone and the call reads behind it (null: none).
 int plan_rope_axes(const mixkvq_cache* cache, const void* q_dev, const void* k_dev, const void* v_dev, const int64_t* strides_host, int n_tokens,
                    const float* cos_dev, const float* sin_dev, int n_positions, const int32_t* positions_dev, int n_axes,
-                   const uint8_t* axis_of_pair_host, void* q_out, void* k_out, void* v_out, RopeAxes* a) {
+                   const uint8_t* axis_of_pair_host, void* q_out, void* k_out, void* v_out, const void* v_kept, RopeAxes* a) {
   if (!cache || !q_dev || !k_dev || !q_out || !k_out || (v_dev == nullptr) != (v_out == nullptr) || !cos_dev || !sin_dev || !positions_dev ||
       !axis_of_pair_host || n_tokens < 1 || n_positions < 1 || n_axes < 1 || n_axes > MIXKVQ_ROPE_MAX_AXES)
     return MIXKVQ_E_INVALID_ARG;
@@ -401,7 +405,8 @@ int plan_rope_axes(const mixkvq_cache* cache, const void* q_dev, const void* k_d
   const void* in[3] = {q_dev, k_dev, v_dev};
   void* out[3] = {q_out, k_out, v_out};
   RopeTensor* t[3] = {&a->tq, &a->tk, &a->tv};
-  uintptr_t lo[6], hi[6];                                  // bytes that the inputs and the outputs lie in
+  constexpr int kRanges = 11;
+  uintptr_t lo[kRanges], hi[kRanges];                      // bytes that the inputs, the outputs and all else that the call reads or writes lie in
   for (int i = 0; i < 3; ++i) {
     const int H = i == 0 ? Hq : Hkv;
     const RopeTensor whole{(long long)H * n_tokens * kD, (long long)n_tokens * kD, kD};
@@ -417,9 +422,17 @@ int plan_rope_axes(const mixkvq_cache* cache, const void* q_dev, const void* k_d
     lo[3 + i] = reinterpret_cast<uintptr_t>(out[i]);
     hi[3 + i] = lo[3 + i] + 2 * (uintptr_t)(B * whole.batch);
   }
+  // (thread blocks gather angles and coordinates while others store rows)
+  const struct { const void* p; uintptr_t bytes; } others[kRanges - 6] = {
+      {cos_dev, (uintptr_t)n_positions * 256}, {sin_dev, (uintptr_t)n_positions * 256}, {positions_dev, (uintptr_t)n_axes * B * n_tokens * 4},
+      {v_kept, (uintptr_t)B * Hkv * n_tokens * kD * 2}, {cache->mem, memory_bytes(cache)}};
+  for (int i = 6; i < kRanges; ++i) {
+    lo[i] = reinterpret_cast<uintptr_t>(others[i - 6].p);
+    hi[i] = others[i - 6].p == nullptr ? 0 : lo[i] + others[i - 6].bytes;
+  }
   // An output may be its own input where that is head-major already; nothing else may overlap an output.
   for (int o = 3; o < 6; ++o)
-    for (int i = 0; i < 6; ++i) {
+    for (int i = 0; i < kRanges; ++i) {
       if (i == o || lo[o] >= hi[i] || lo[i] >= hi[o]) continue;
       const RopeTensor& x = *t[o - 3];
       const int H = o == 3 ? Hq : Hkv;
@@ -766,7 +779,7 @@ int mixkvq_rope_axes(mixkvq_cache* cache, const void* q_dev, const void* k_dev, 
                      const uint8_t* axis_of_pair_host, void* q_out_dev, void* k_out_dev, void* v_out_dev, void* stream) {
   RopeAxes a;
   const int rc = plan_rope_axes(cache, q_dev, k_dev, v_dev, strides_host, n_tokens, cos_dev, sin_dev, n_positions, positions_dev, n_axes,
-                                axis_of_pair_host, q_out_dev, k_out_dev, v_out_dev, &a);
+                                axis_of_pair_host, q_out_dev, k_out_dev, v_out_dev, nullptr, &a);
   return rc != MIXKVQ_OK ? rc : run_rope_axes(cache, a, static_cast<cudaStream_t>(stream));
 }
 
@@ -774,7 +787,7 @@ int mixkvq_rope_axes_append(mixkvq_cache* cache, int layer, void* k_dev, const v
                             int n_positions, const int32_t* positions_dev, int n_axes, const uint8_t* axis_of_pair_host, int n_tokens, void* stream) {
   RopeAxes a;
   int rc = plan_rope_axes(cache, q_dev, k_dev, nullptr, nullptr, n_tokens, cos_dev, sin_dev, n_positions, positions_dev, n_axes, axis_of_pair_host, q_dev,
-                          k_dev, nullptr, &a);
+                          k_dev, nullptr, v_dev, &a);
   if (rc != MIXKVQ_OK) return rc;
   if (!v_dev || layer < 0 || layer >= cache->cfg.n_layers) return MIXKVQ_E_INVALID_ARG;
   if (!aligned16(v_dev)) return MIXKVQ_E_ALIGNMENT;
@@ -788,7 +801,7 @@ int mixkvq_rope_axes_decode_step(mixkvq_cache* cache, int layer, void* k_dev, co
                                  float softmax_scale, void* workspace_dev, size_t workspace_bytes_given, void* stream) {
   RopeAxes a;
   int rc = plan_rope_axes(cache, q_dev, k_dev, nullptr, nullptr, 1, cos_dev, sin_dev, n_positions, positions_dev, n_axes, axis_of_pair_host, q_dev, k_dev,
-                          nullptr, &a);
+                          nullptr, v_dev, &a);
   if (rc != MIXKVQ_OK) return rc;
   if (!v_dev || !out_dev || !workspace_dev || layer < 0 || layer >= cache->cfg.n_layers) return MIXKVQ_E_INVALID_ARG;
   if (!aligned16(v_dev) || !aligned16(out_dev) || !aligned16(workspace_dev)) return MIXKVQ_E_ALIGNMENT;

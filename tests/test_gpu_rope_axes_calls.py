@@ -1,0 +1,96 @@
+"""GPU tests of the calls that rotate with several axes and then append or decode: what they refuse, and that a refused call has changed nothing."""
+import numpy as np
+import pytest
+import torch
+
+import gpu_util as U
+from paper_2512_19206_b200 import workloads as W
+
+pytestmark = pytest.mark.gpu
+SCALE = W.softmax_scale()
+
+
+@pytest.fixture(scope="module")
+def binding():
+    assert torch.cuda.is_available(), "GPU tests need a CUDA device"
+    from paper_2512_19206_b200 import build
+    build.build()
+    from paper_2512_19206_b200 import binding as b
+    b.lib()
+    return b
+
+
+def tables(n_pos):
+    ang = np.arange(n_pos, dtype=np.float64)[:, None] * 1e6 ** (-np.arange(64, dtype=np.float64) / 64)[None]
+    return [torch.from_numpy(f(ang).astype(np.float32)).cuda() for f in (np.cos, np.sin)]
+
+
+def refused(binding, code, call, *args, **kw):
+    with pytest.raises(binding.MixKVQError) as e:
+        call(*args, **kw)
+    assert e.value.code == code
+
+
+def bf16_at(memory, byte, shape):
+    """A bf16 tensor over the memory of another one, from a byte offset on."""
+    n = 2 * int(np.prod(shape))
+    flat = memory.view(torch.uint8).view(-1)
+    assert 0 <= byte <= flat.numel() - n
+    return flat[byte:byte + n].view(torch.bfloat16).view(shape)
+
+
+@pytest.mark.parametrize("which,end", [(w, e) for w in ("cos", "sin", "positions") for e in ("first", "last", "all")] + [("cache", "last"), ("cache", "all")])
+def test_outputs_over_what_the_rotation_reads(binding, which, end):
+    """An output over a part of the tables, the positions or the cache's memory is refused (thread blocks read angles while others store rows); directly
+    behind them it is not."""
+    B, Hq, Hkv, n = 2, 4, 2, 32
+    axes = binding.axis_sections((32, 32))
+    cache = binding.Cache(binding.make_config(1, B, Hq, Hkv, 64))
+    size = 2 * B * Hq * n * 128                                   # bytes of q: 65536
+    before = cache.launch_count()
+    q, k, v = (torch.randn((B, h, n, 128), device="cuda").bfloat16() for h in (Hq, Hkv, Hkv))
+    room = torch.zeros(4 * size, dtype=torch.uint8, device="cuda")
+    cos, sin = tables(256)                                        # 65536 bytes each
+    pos = torch.zeros((2, B, n), dtype=torch.int32, device="cuda")  # 512 bytes
+    target = {"cos": cos, "sin": sin, "positions": pos, "cache": None}[which]
+    if which == "cache":
+        memory, stop = cache.mem, cache.mem.numel()
+        at = {"last": stop - size, "all": 256}[end]
+    else:
+        start, stop = size, size + target.numel() * 4
+        held = room[start:stop].view(target.dtype).view(target.shape)
+        held.copy_(target)
+        cos, sin, pos = (held if t is target else t for t in (cos, sin, pos))
+        memory, at = room, {"first": start + 16 - size, "last": stop - 16, "all": start}[end]
+    k2, v2 = torch.empty_like(k), torch.empty_like(v)
+    over = bf16_at(memory, at, q.shape)
+    refused(binding, -1, cache.rope_axes, q, k, v, cos, sin, pos, axes, out=(over, k2, v2))
+    refused(binding, -1, cache.rope_axes, over, k, v, cos, sin, pos, axes, out=(over, k2, v2))        # in place too
+    assert cache.launch_count() == before
+    if which != "cache":
+        beside = bf16_at(room, {"first": start - size, "last": stop, "all": stop}[end], q.shape)
+        cache.rope_axes(q, k, v, cos, sin, pos, axes, out=(beside, k2, v2))
+        assert torch.equal(beside, q) and cache.status() == 0     # (position 0)
+
+
+@pytest.mark.parametrize("of", ["k", "q"])
+def test_values_over_what_is_rotated(binding, of):
+    """Values inside the keys or queries that are rotated in place are refused, by the append and by the decode step."""
+    B, Hq, Hkv = 2, 4, 2
+    axes = binding.axis_sections((32, 32))
+    cache = binding.Cache(binding.make_config(1, B, Hq, Hkv, 64))
+    cos, sin = tables(16)
+    before = cache.launch_count()
+    for n in (5, 1):
+        pos = torch.ones((2, B, n), dtype=torch.int32, device="cuda")
+        kq = [torch.randn((B, h, n, 128), device="cuda").bfloat16() for h in (Hkv, Hq)]
+        was = [t.clone() for t in kq]
+        k, q = kq
+        v = k if of == "k" else bf16_at(q, 2 * B * Hkv * n * 128, k.shape)
+        if n > 1:
+            refused(binding, -1, cache.rope_axes_append, 0, k, v, q, cos, sin, pos, axes)
+        else:
+            refused(binding, -1, cache.rope_axes_decode_step, 0, k, v, q, cos, sin, pos, axes, SCALE)
+        torch.cuda.synchronize()
+        assert torch.equal(k, was[0]) and torch.equal(q, was[1])
+    assert cache.launch_count() == before and cache.sequence_fill(0, 0) == (0, 0, 0)
