@@ -291,8 +291,8 @@ int mixkvq_rope_decode_step(mixkvq_cache* cache, int layer, void* k_dev, const v
  *   multiples of 8); NULL: head-major.  An output may be its own input where that is head-major; no output may overlap anything else,
  *   the tables, the positions and the cache's memory included (MIXKVQ_E_INVALID_ARG).
  * mixkvq_rope_axes_append and mixkvq_rope_axes_decode_step rotate k_dev and q_dev in place and then do what mixkvq_quantize_append and
- * mixkvq_decode_step do (one more launch than mixkvq_rope_decode_step); v_dev overlaps neither (MIXKVQ_E_INVALID_ARG); on MIXKVQ_E_CAPACITY
- * nothing was rotated. */
+ * mixkvq_decode_step do (one more launch than mixkvq_rope_decode_step); v_dev overlaps neither (MIXKVQ_E_INVALID_ARG); on MIXKVQ_E_CAPACITY and
+ * MIXKVQ_E_UNSUPPORTED nothing was rotated or appended. */
 #define MIXKVQ_ROPE_MAX_AXES 4
 int mixkvq_rope_axes(mixkvq_cache* cache, const void* q_dev, const void* k_dev, const void* v_dev, const int64_t* strides_host, int n_tokens,
                      const float* cos_dev, const float* sin_dev, int n_positions, const int32_t* positions_dev, int n_axes,

@@ -196,6 +196,11 @@ int zero_all_layers(mixkvq_cache* h, cudaStream_t st) {
   return MIXKVQ_OK;
 }
 
+// Whether the layer's sequences differ in a way that decode attention does not take.  (A decode step changes nothing about it: all sequences take a token.)
+bool unsupported_ragged(const mixkvq_cache* h, int layer) {
+  return (h->tile || h->attn_kind == 1 || h->cfg.batch > kMaxRaggedBatch) && !uniform(h, layer);
+}
+
 // Ragged batch: writes the fills of the layer's sequences to its table in device memory (as kernel arguments: ordered
 // in the stream, no copy) and points the view at it.
 int upload_seq_table(mixkvq_cache* h, int layer, cudaStream_t st, LayerView* lv) {
@@ -463,6 +468,7 @@ int run_rope_axes(mixkvq_cache* cache, const RopeAxes& a, cudaStream_t st) {
 int run_decode_step(mixkvq_cache* cache, int layer, const void* k_dev, const void* v_dev, const void* q_dev, float* out_dev, float softmax_scale,
                     void* workspace_dev, cudaStream_t st, const float* rope_cos = nullptr, const float* rope_sin = nullptr) {
   const int B = cache->cfg.batch;
+  if (unsupported_ragged(cache, layer)) return MIXKVQ_E_UNSUPPORTED;      // before anything is rotated or appended
   bool sink_room = false;
   for (int b = 0; b < B; ++b) sink_room = sink_room || cache->n_sink[fi(cache, layer, b)] < cache->cfg.sink_len;
   const bool apart = cache->attn_kind != 0 || sink_room;
@@ -807,6 +813,7 @@ int mixkvq_rope_axes_decode_step(mixkvq_cache* cache, int layer, void* k_dev, co
   if (!aligned16(v_dev) || !aligned16(out_dev) || !aligned16(workspace_dev)) return MIXKVQ_E_ALIGNMENT;
   if (workspace_bytes_given < workspace_bytes(cache->S)) return MIXKVQ_E_BUFFER_TOO_SMALL;
   if (max_tokens_held(cache, layer) + 1 > cache->cfg.max_tokens) return MIXKVQ_E_CAPACITY;
+  if (unsupported_ragged(cache, layer)) return MIXKVQ_E_UNSUPPORTED;
   rc = run_rope_axes(cache, a, static_cast<cudaStream_t>(stream));
   return rc != MIXKVQ_OK ? rc
                          : run_decode_step(cache, layer, k_dev, v_dev, q_dev, out_dev, softmax_scale, workspace_dev, static_cast<cudaStream_t>(stream));

@@ -94,3 +94,34 @@ def test_values_over_what_is_rotated(binding, of):
         torch.cuda.synchronize()
         assert torch.equal(k, was[0]) and torch.equal(q, was[1])
     assert cache.launch_count() == before and cache.sequence_fill(0, 0) == (0, 0, 0)
+
+
+@pytest.mark.parametrize("why", ["batch", "tile", "kernel", "kernel and sink"])
+@pytest.mark.parametrize("call", ["axes", "rope", "plain"])
+def test_a_step_that_is_not_supported_changes_nothing(binding, why, call):
+    """A diverged batch that decode attention does not take: the step's tensors and the cache are as they were, so that a retry on another path rotates
+    and appends once."""
+    B, Hq, Hkv = 130 if why == "batch" else 3, 4, 2
+    more = {"tile": dict(block_layout=1), "kernel and sink": dict(sink_len=32)}.get(why, {})
+    cache = binding.Cache(binding.make_config(1, B, Hq, Hkv, 300, **more))
+    new = lambda n: [torch.randn((B, h, n, 128), device="cuda").bfloat16() for h in (Hkv, Hkv, Hq)]        # noqa: E731
+    counts = [20] * B
+    counts[1] = 7
+    cache.quantize_append_ragged(0, *new(20), counts)
+    if why.startswith("kernel"):
+        cache.set_attention_kernel(1)
+    cos, sin = tables(16)
+    pos = torch.ones((2, B, 1), dtype=torch.int32, device="cuda")
+    kvq = new(1)
+    was, memory = [t.clone() for t in kvq], cache.mem.clone()
+    fill = [cache.sequence_fill(0, b) for b in range(B)]
+    before = cache.launch_count()
+    if call == "axes":
+        refused(binding, -2, cache.rope_axes_decode_step, 0, *kvq, cos, sin, pos, binding.axis_sections((32, 32)), SCALE)
+    elif call == "rope":
+        refused(binding, -2, cache.rope_decode_step, 0, *kvq, cos, sin, 1, SCALE)
+    else:
+        refused(binding, -2, cache.decode_step, 0, *kvq, SCALE)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(kvq, was)) and torch.equal(cache.mem, memory)
+    assert [cache.sequence_fill(0, b) for b in range(B)] == fill and cache.launch_count() == before
