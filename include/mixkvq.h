@@ -292,7 +292,8 @@ int mixkvq_rope_decode_step(mixkvq_cache* cache, int layer, void* k_dev, const v
  *   the tables, the positions and the cache's memory included (MIXKVQ_E_INVALID_ARG).
  * mixkvq_rope_axes_append and mixkvq_rope_axes_decode_step rotate k_dev and q_dev in place and then do what mixkvq_quantize_append and
  * mixkvq_decode_step do (one more launch than mixkvq_rope_decode_step); v_dev overlaps neither (MIXKVQ_E_INVALID_ARG); on MIXKVQ_E_CAPACITY and
- * MIXKVQ_E_UNSUPPORTED nothing was rotated or appended. */
+ * MIXKVQ_E_UNSUPPORTED nothing was rotated or appended.  They append every row of the call, those that the rotation leaves alone (a negative
+ * coordinate, one beyond the tables) as they came: a ragged batch takes mixkvq_rope_axes, then mixkvq_quantize_append_ragged with its counts. */
 #define MIXKVQ_ROPE_MAX_AXES 4
 int mixkvq_rope_axes(mixkvq_cache* cache, const void* q_dev, const void* k_dev, const void* v_dev, const int64_t* strides_host, int n_tokens,
                      const float* cos_dev, const float* sin_dev, int n_positions, const int32_t* positions_dev, int n_axes,

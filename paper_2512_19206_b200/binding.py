@@ -421,7 +421,8 @@ class Cache:
                 raise ValueError(f"{name}: {what} must be a contiguous bfloat16 {list(shape)} tensor on {dev}")
 
     def rope_axes_append(self, layer, k, v, q, cos, sin, positions, axes):
-        """rope_axes on k and q in place (all head-major), then quantize_append."""
+        """rope_axes on k and q in place (all head-major), then quantize_append of every row, those without a token too (ragged batches: rope_axes, then
+        quantize_append_ragged)."""
         n = k.shape[2] if k.dim() == 4 else 0
         self._head_major("rope_axes_append", n, k=k, v=v, q=q)
         angles = self._angles("rope_axes_append", cos, sin, positions, axes, n)

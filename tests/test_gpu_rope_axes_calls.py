@@ -125,3 +125,63 @@ def test_a_step_that_is_not_supported_changes_nothing(binding, why, call):
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(kvq, was)) and torch.equal(cache.mem, memory)
     assert [cache.sequence_fill(0, b) for b in range(B)] == fill and cache.launch_count() == before
+
+
+def test_rows_without_a_coordinate_are_appended_as_they_are(binding):
+    """The append and the step store every row of the call, those that the rotation leaves alone (no token, beyond the tables) unrotated."""
+    B, Hq, Hkv, n = 2, 4, 2, 9
+    axes = binding.axis_sections((32, 32))
+    cos, sin = tables(16)
+    k, v, q = (torch.randn((B, h, n, 128), device="cuda").bfloat16() for h in (Hkv, Hkv, Hq))
+    pos = torch.randint(1, 16, (2, B, n), device="cuda", dtype=torch.int32)
+    pos[1, 1, 5:], pos[0, 0, 3] = -1, 16
+    a, b = (binding.Cache(binding.make_config(1, B, Hq, Hkv, 64)) for _ in range(2))
+    for c in (a, b):
+        c.mem.zero_()
+        c.reset()
+    was_k, was_q = k.clone(), q.clone()
+    qr, kr = q.clone(), k.clone()
+    b.rope_axes(q, k, None, cos, sin, pos, axes, out=(qr, kr, None))
+    b.quantize_append(0, kr, v, qr)
+    a.rope_axes_append(0, k, v, q, cos, sin, pos, axes)
+    assert a.status() == b.status() == binding.DEV_BAD_POSITION
+    assert torch.equal(a.mem, b.mem) and a.sequence_fill(0, 1) == (0, 9, 0)
+    for t, was in ((k, was_k), (q, was_q)):
+        assert torch.equal(t[1, :, 5:], was[1, :, 5:]) and torch.equal(t[0, :, 3], was[0, :, 3])
+        assert not torch.equal(t[0, :, 4], was[0, :, 4])
+    step = [torch.randn((B, h, 1, 128), device="cuda").bfloat16() for h in (Hkv, Hkv, Hq)]
+    none = torch.full((2, B, 1), -1, device="cuda", dtype=torch.int32)
+    oa = a.rope_axes_decode_step(0, *[t.clone() for t in step], cos, sin, none, axes, SCALE)
+    assert torch.equal(oa, b.decode_step(0, *step, SCALE)) and torch.equal(a.mem, b.mem)
+
+
+@pytest.mark.parametrize("sections,interleaved", [((16, 24, 24), False), ((24, 20, 20), True), ((8, 24, 16, 16), True)])
+@pytest.mark.parametrize("kind,sink", [(0, 0), (0, 32), (1, 0)])
+def test_several_axes_into_the_cache(binding, sections, interleaved, kind, sink):
+    """A prompt and the steps behind it, every sequence at positions of its own: the append and the step leave the cache, the rotated rows and the outputs
+    that rope_axes, then quantize_append or decode_step leave."""
+    B, Hq, Hkv, n = 2, 14, 2, 205
+    axes, n_axes = binding.axis_sections(sections, interleaved), len(sections)
+    cos, sin = tables(500)
+    gen = torch.Generator().manual_seed(n_axes)
+    new = lambda m: [torch.randn((B, h, m, 128), generator=gen).bfloat16().cuda() for h in (Hkv, Hkv, Hq)]        # noqa: E731
+    where = lambda m: torch.randint(0, 500, (n_axes, B, m), generator=gen, dtype=torch.int32).cuda()              # noqa: E731
+    a, b = (binding.Cache(binding.make_config(1, B, Hq, Hkv, 256, residual_len=64, sink_len=sink, **W.P27)) for _ in range(2))
+    for c in (a, b):
+        c.mem.zero_()
+        c.reset()
+        c.set_attention_kernel(kind)
+    k, v, q = new(n)
+    pos = where(n)
+    qr, kr, _ = b.rope_axes(q, k, None, cos, sin, pos, axes, out=(torch.empty_like(q), torch.empty_like(k), None))
+    b.quantize_append(0, kr, v, qr)
+    a.rope_axes_append(0, k, v, q, cos, sin, pos, axes)
+    assert torch.equal(k, kr) and torch.equal(q, qr)
+    for _ in range(40):                                   # (over the end of a window)
+        k, v, q = new(1)
+        pos = where(1)
+        qr, kr, _ = b.rope_axes(q, k, None, cos, sin, pos, axes, out=(torch.empty_like(q), torch.empty_like(k), None))
+        ob = b.decode_step(0, kr, v, qr, SCALE)
+        oa = a.rope_axes_decode_step(0, k, v, q, cos, sin, pos, axes, SCALE)
+        assert torch.equal(oa, ob) and torch.equal(k, kr) and torch.equal(q, qr)
+    assert a.status() == b.status() == 0 and torch.equal(a.mem, b.mem)
