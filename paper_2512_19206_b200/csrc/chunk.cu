@@ -111,6 +111,17 @@ __device__ __forceinline__ uint32_t hmul2_u(uint32_t a, uint32_t b) {
   asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
   return d;
 }
+__device__ __forceinline__ uint32_t hsub2_u(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+// 1 where a half of a is above that of b, else 0
+__device__ __forceinline__ uint32_t above2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("set.gt.f16x2.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
 constexpr uint32_t kQuarter2 = 0x34003400u;               // the fp16 pair (0.25, 0.25)
 
 // c s + z of field f (2 bits at bit 2 f of each half word), one rounding.  The number with the field's bits in its mantissa is 1024 + c (f even) or
@@ -321,8 +332,11 @@ __device__ __forceinline__ void put_promoted(Promoted& p, uint32_t tile, uint32_
     if (((2 * i + 2) & 31) == 0 && 2 * i + 2 + lane < p.n16) mine = offset(reinterpret_cast<const uint8_t*>(p.ex)[2 * i + 2 + lane]);
   }
   if (kU4 == 1 && p.n4 > 0) {
-    // UINT4 channels: (c_lo + 4 c_hi) s + z is what the base store left, plus 4 c_hi s.  (A second rounding to fp16.  With the low codes read again, to round
-    // once, every four channels cost a round trip to the L2 cache: 7b shape, three tiers, draft-sized chunk of eight sequences, 158 / 137 us.)
+    // UINT4 channels: (c_lo + 4 c_hi) s + z, one rounding.  The low code is found again from what the base store left, c_lo s + z rounded: less z it lies
+    // nearest to its own multiple of s (where s is below the rounding, that of another multiple may be as near: the value is then off by at most
+    // three halves of a step instead of a half).  Both channels of a pair in fp16 pairs: 121 us for a draft-sized chunk of eight sequences, 7b shape, three
+    // tiers; one after the other in fp32 138; with the high code's 4 c_hi s added to the rounded c_lo s + z, a second rounding, 127.  (The low codes
+    // read again cost a round trip to the L2 cache every four channels.)
     const int pairs = (p.n4 + 1) >> 1, bit = high_bit(lane);
     const uint32_t* high = high_plane(p, lane);
 #pragma unroll 1
@@ -337,15 +351,22 @@ __device__ __forceinline__ void put_promoted(Promoted& p, uint32_t tile, uint32_
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const uint32_t two = i0 + k < pairs ? __shfl_sync(0xffffffffu, p.pair4, (i0 + k) & 31) : 0xFFFFu;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const uint32_t d = e ? two >> 8 : two & 0xFFu;
-          if (d < kD) {                  // (the whole warp's decision; odd 16-channel pieces have a quarter of the scale in store)
-            const uint32_t s = lds16(scratch + 4 * (36 * ((d >> 3) & 1) + 8 * ((d & 7) >> 1) + (d >> 4)) + 2 * (d & 1)), at = row + offset(d);
-            const float old = __half2float(__ushort_as_half((unsigned short)lds16(at))), scale = __half2float(__ushort_as_half((unsigned short)s));
-            const float c = (float)((hw[k] >> (bit + 16 * e)) & 3u) * (d & 16 ? 16.f : 4.f);
-            sts16(at, (uint32_t)__half_as_ushort(__float2half_rn(fmaf(c, scale, old))));
-          }
+        const uint32_t d0 = two & 0xFFu, d1 = two >> 8;
+        if (d0 < kD) {                   // (the whole warp's decision, and whether the pair has a second channel)
+          const uint32_t e1 = d1 < kD ? d1 : d0, at0 = row + offset(d0), at1 = row + offset(e1);
+          auto meta = [&](uint32_t d) { return scratch + 4 * (36 * ((d >> 3) & 1) + 8 * ((d & 7) >> 1) + (d >> 4)) + 2 * (d & 1); };
+          auto both = [](uint32_t a0, uint32_t a1) { return __byte_perm(lds16(a0), lds16(a1), 0x5410); };
+          const uint32_t m0 = meta(d0), m1 = meta(e1);
+          // (odd 16-channel pieces have a quarter of the scale in store)
+          const uint32_t s = hmul2_u(both(m0, m1), (d0 & 16 ? 0x4400u : 0x3C00u) | (e1 & 16 ? 0x44000000u : 0x3C000000u)), z = both(m0 + 288, m1 + 288);
+          const uint32_t low = hsub2_u(both(at0, at1), z), twice = hadd2_u(low, low);
+          uint32_t c = hadd2_u(((hw[k] >> bit << 2) & 0x000C000Cu) | 0x64006400u, 0xE400E400u);      // 4 c_hi
+          c = hadd2_u(c, above2(twice, s));
+          c = hadd2_u(c, above2(twice, hmul2_u(s, 0x42004200u)));            // 3 s
+          c = hadd2_u(c, above2(twice, hmul2_u(s, 0x45004500u)));            // 5 s
+          const uint32_t y = hfma2_u(c, s, z);
+          sts16(at0, y & 0xFFFFu);
+          if (d1 < kD) sts16(at1, y >> 16);
         }
       }
     }

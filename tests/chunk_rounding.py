@@ -6,6 +6,9 @@ bits.  What is left between this and the kernel is small enough that one key too
 import numpy as np
 import torch
 
+import chunk_util as CU
+from paper_2512_19206_b200 import workloads as W
+
 HALF_STEP = 2.0 ** -11            # of fp16
 TILE = 128
 
@@ -94,3 +97,21 @@ def simulated(K, V, q, scale, sees, lag=10.0, shift=5.0):
                 o += (p.astype(np.float16).astype(np.float64) @ V[t:t + TILE].numpy()).astype(np.float32)
             out[h, r] = torch.from_numpy(o / l).double()
     return out
+
+
+
+def offset_keys(n4, tokens=330, n=6, R=64):
+    """A stream whose keys' groups lie 3 to 18 scales below zero, n4 channels of it UINT4: there c_lo s + z has more bits than fp16 holds, while the
+    element itself has not.  Returns (stream, new keys, values [n, 128], queries [2, n, 128] on the UINT4 channels)."""
+    w = W.small(W.CONFIGS["tiny"], n_layers=1, n_q_heads=2, tokens=tokens, residual_len=R)
+    gen = torch.Generator().manual_seed(n4)
+    k = (-3 - 15 * torch.rand((1, 1, tokens, 128), generator=gen)).to(torch.bfloat16)
+    v = torch.randn((1, 1, tokens, 128), generator=gen).to(torch.bfloat16)
+    q = torch.randn((1, 2, tokens, 128), generator=gen)
+    q[..., torch.randperm(128, generator=gen)[:n4]] *= 8          # the same channels in every window
+    q = q.to(torch.bfloat16)
+    st = CU.streams(w, [tokens], k, v, q, budget_u4=n4)[(0, 0)]
+    st.source = (w, k, v, q)
+    qn = (2 * torch.randn((2, n, 128), generator=gen) * torch.from_numpy(st.blocks[0].tiers == 1)).to(torch.bfloat16)
+    kn, vn = k[0, 0, :n].clone(), v[0, 0, :n].clone()
+    return st, kn, vn, qn

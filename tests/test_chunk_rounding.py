@@ -96,3 +96,24 @@ def test_wrong_codes_are_refused(preset):
     values = V.clone()
     values[40, 32:64] = V[41, 32:64]
     assert CR.worst(CR.attend(K, values, q, SCALE, sees)[1], ref, tol) > 1.0
+
+
+@pytest.mark.parametrize("n4", [64, 37])
+def test_keys_rounded_twice_are_refused(n4):
+    """(c_lo s + z) rounded, then 4 c_hi s added and rounded again."""
+    st, kn, vn, qn = CR.offset_keys(n4)
+    K, V, q = CR.operands(st, kn, vn, qn)
+    held, n = K.shape[0] - kn.shape[0], kn.shape[0]
+    sees = CR.visible(held, n)
+    p, ref, s = CR.attend(K, V, q, SCALE, sees)
+    tol = CR.allowed(p, s, K, V, q, SCALE)
+    assert CR.worst(CR.simulated(K, V, q, SCALE, sees), ref, tol) <= 1.0
+    twice, t = K.clone(), 0
+    for b in st.blocks:
+        scale, zero = (torch.from_numpy(x.astype("float64")).repeat_interleave(st.G, 0) for x in (b.ks, b.kz))
+        codes = torch.from_numpy(b.kcodes.reshape(st.R, 128).astype("float64"))
+        once = CR.fp16((codes % 4 * scale + zero).numpy())
+        again = CR.fp16((once + torch.floor(codes / 4) * 4 * scale).numpy())
+        twice[t:t + st.R] = torch.where(torch.from_numpy(b.tiers == 1), again, twice[t:t + st.R])
+        t += st.R
+    assert CR.worst(CR.attend(twice, V, q, SCALE, sees)[1], ref, tol) > 1.5

@@ -90,3 +90,14 @@ def test_fixed_budgets(binding, n16, n4, n):
     sts = both(binding, w, [330], [n], budget_bf16=n16, budget_u4=n4)
     tiers = next(iter(sts.values())).blocks[0].tiers
     assert ((tiers == 2).sum(), (tiers == 1).sum()) == (n16, n4)
+
+
+@pytest.mark.parametrize("n4", [64, 37])
+def test_four_bit_keys_are_rounded_once(binding, n4):
+    st, kn, vn, qn = CR.offset_keys(n4)
+    w, k, v, q = st.source
+    cache = U.make_cache(binding, w, extras_budget_bytes=8 * 320 * w.residual_len, budget_u4=n4)
+    cache.quantize_append(0, k.cuda(), v.cuda(), q.cuda())
+    out = cache.chunk_attention(0, kn[None, None].cuda(), vn[None, None].cuda(), qn[None].cuda(), SCALE)
+    assert cache.status() == 0
+    CR.check(w, out, {(0, 0): st}, kn[None, None], vn[None, None], qn[None], [len(kn)], SCALE)
