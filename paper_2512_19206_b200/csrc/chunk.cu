@@ -660,6 +660,24 @@ __device__ __forceinline__ bool elect_one() {
   return e != 0;
 }
 
+// Weight of a partial result (maximum m, denominator l) in a sum that refers to `top`.  A NaN among the logits makes l NaN, whatever m is, and the row too,
+// even where its weight would round to zero.
+__device__ __forceinline__ float weight_of(float m, float l, float top) { return l != l ? l : m == -INFINITY ? 0.f : ex2(m - top); }
+// sum + w y of a partial result with denominator l; infinity where y is one (a weight that has rounded to zero is positive all the same).  A result
+// without a key (l = 0) is zeros.
+__device__ __forceinline__ void add_part(float w, float l, float4 y, float4& sum) {
+  if (w != 0.f) {
+    sum.x = fmaf(w, y.x, sum.x); sum.y = fmaf(w, y.y, sum.y); sum.z = fmaf(w, y.z, sum.z); sum.w = fmaf(w, y.w, sum.w);
+  } else if (l != 0.f) {
+    sum.x += isfinite(y.x) ? 0.f : y.x; sum.y += isfinite(y.y) ? 0.f : y.y; sum.z += isfinite(y.z) ? 0.f : y.z; sum.w += isfinite(y.w) ? 0.f : y.w;
+  }
+}
+__device__ __forceinline__ void scale_part(float w, float l, float4& sum) {
+  const float4 y = sum;
+  sum = make_float4(0.f, 0.f, 0.f, 0.f);
+  add_part(w, l, y, sum);
+}
+
 __device__ __forceinline__ void softmax_sync() { asm volatile("barrier.cta.sync 1, 256;" ::: "memory"); }
 
 // 4 channels of an output row
@@ -1151,7 +1169,6 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       ended[1] += both;
       float* part = a.parts + ((size_t)blockIdx.x * 2 + sg.part) * a.rows_cap * (kD + 2);
       const float l_run = mine ? state.sum() : 0.f, m_run = mine ? state.m : -INFINITY;
-      auto weight = [](float m, float l, float top) { return m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : ex2(m - top); };   // (a row of NaNs counts)
       if (dual) {
         if (!idle) {
           const bool exists = row < rows_all;
@@ -1198,7 +1215,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
         softmax_sync();
         if (slot == 0 && !idle) {
           const float2 other = ml[row_in];
-          const float top = fmaxf(m_run, other.x), f0 = l_run == 0.f ? 0.f : weight(m_run, l_run, top), f1 = weight(other.x, other.y, top);
+          const float top = fmaxf(m_run, other.x), f0 = l_run == 0.f ? 0.f : weight_of(m_run, l_run, top), f1 = weight_of(other.x, other.y, top);
           ml[row_in] = make_float2(top, l_run * f0 + other.y * f1);
 #pragma unroll 1
           for (int d = 0; d < kD; d += 32) {
@@ -1233,7 +1250,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
             f[i] = 0.f;
             if (i < 1 << lg_copies) {
               const float2 x = ml[r + i * per];
-              f[i] = weight(x.x, x.y, top);
+              f[i] = weight_of(x.x, x.y, top);
               l += x.y * f[i];
             }
           }
@@ -1339,17 +1356,14 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant_
       float top = M;
 #pragma unroll
       for (int k = 0; k < kFlight; ++k) top = fmaxf(top, ml[k].x);
-      const float f = M == -INFINITY ? (l == 0.f ? 0.f : 1.f) : exp2f(M - top);
+      const float f = weight_of(M, l, top);
+      scale_part(f, l, o);
       l *= f;
-      o.x *= f; o.y *= f; o.z *= f; o.w *= f;
 #pragma unroll
       for (int k = 0; k < kFlight; ++k) {
-        // (NaN sums of a row whose logits hold a NaN: their maximum may be -inf, and they count all the same)
-        const float w = ml[k].x == -INFINITY ? (ml[k].y == 0.f ? 0.f : 1.f) : exp2f(ml[k].x - top);
-        if (w != 0.f) {
-          l = fmaf(w, ml[k].y, l);
-          o.x = fmaf(w, y[k].x, o.x); o.y = fmaf(w, y[k].y, o.y); o.z = fmaf(w, y[k].z, o.z); o.w = fmaf(w, y[k].w, o.w);
-        }
+        const float w = weight_of(ml[k].x, ml[k].y, top);
+        l = fmaf(w, ml[k].y, l);
+        add_part(w, ml[k].y, y[k], o);
       }
       M = top;
     }
@@ -1360,17 +1374,15 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant_
       if (sub == 0) {
         float top = M;
         for (int w = 1; w < kWarps; ++w) top = fmaxf(top, mlS[warp + w].x);
-        const float f = M == -INFINITY ? (l == 0.f ? 0.f : 1.f) : exp2f(M - top);
+        const float f = weight_of(M, l, top);
+        scale_part(f, l, o);
         l *= f;
-        o.x *= f; o.y *= f; o.z *= f; o.w *= f;
         for (int w = 1; w < kWarps; ++w) {
           const float2 ml = mlS[warp + w];
-          const float fw = ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : 1.f) : exp2f(ml.x - top);
-          if (fw != 0.f) {
-            const float4 y = reinterpret_cast<const float4*>(oS[warp + w])[lane];
-            l = fmaf(fw, ml.y, l);
-            o.x = fmaf(fw, y.x, o.x); o.y = fmaf(fw, y.y, o.y); o.z = fmaf(fw, y.z, o.z); o.w = fmaf(fw, y.w, o.w);
-          }
+          const float fw = weight_of(ml.x, ml.y, top);
+          const float4 y = reinterpret_cast<const float4*>(oS[warp + w])[lane];
+          l = fmaf(fw, ml.y, l);
+          add_part(fw, ml.y, y, o);
         }
       }
     }
