@@ -15,8 +15,10 @@
 // Codes lie in the cache as mma.sync A fragments: the lane with row r and pair t of an 8 x 8 piece holds its two neighbouring channels (keys) or
 // tokens (values).  With keys and values both stored K-major in shared memory that pair is 4 bytes at 16 r + 4 t = 4 lane of a core matrix, so a
 // warp's store is 128 contiguous bytes (the keys': four of them).
-// The running maximum is raised (and O rescaled, in tensor memory) only when a row's logits exceed it by more than 2^10: P stays below 1024, far
-// inside fp16, and the rescaling is rare.  P is fp16 (11 significant bits); sums, maxima, O are fp32.
+// The running maximum is raised (and O rescaled, in tensor memory) only when a row's logits exceed it by more than 2^10, so that the rescaling is rare.  P is
+// fp16 (11 significant bits), 2^5 times the probability relative to that maximum: below 2^15, inside fp16, and numbers down to 2^-19 of the maximum are rounded
+// by 2^-11 of themselves, smaller ones by 2^-30 of the maximum.  The denominator sums what P was before the rounding.  Sums, maxima, O are fp32.
+// (Without the factor weights below 2^-25 were zero in P and counted in the denominator: 16384 keys 17.4 nats below one with values of zero gave nothing.)
 //
 // What bounds it (B200).  Few rows, long caches: the making of the tiles.  A key tile of 128 x 128 takes about 7000 warp instructions, three fifths of them logic,
 // fp16 operations and stores of codes; 58 % of the issue slots are taken, a tile every 2900 cycles.  Eight sequences of 32768 tokens, 7b shape, 5 new tokens each:
@@ -48,6 +50,7 @@ constexpr int kSmem = kPoisonOff + 2 * (4 + 3 * kD * 4);
 enum Bar { kQFull = 0, kKFull = 1, kVFull = 3, kKEmpty = 5, kVEmpty = 7, kSFull = 9, kPReady = 11, kODone = 13, kDone = 15, kSegFull = 17, kSegEmpty = 19 };
 constexpr uint32_t kPolls = 1u << 19;                    // a poll that finds nothing returns after about 4 us: two seconds
 constexpr float kRaise = 10.f;
+constexpr float kShift = 5.f;
 constexpr int kAhead = 8;
 constexpr int kProducerNap = 40;
 
@@ -554,7 +557,7 @@ __device__ __forceinline__ void raise(uint32_t s_addr, uint32_t o_addr, int writ
 
 // One tile of one slot's softmax, in one pass: the thread's row of S (128 fp32 at s_addr) becomes P (fp16 pairs over the first 64 of those columns), 32
 // columns at a time.  Piece h of P lies inside the columns of S's pieces <= h.  The reference is raised only when a piece's largest logit exceeds it by
-// more than 2^kRaise: P stays below 2^10, far inside fp16, and that is rare behind the first tile.  The row's own pieces are h0 .. h1 - 1 (another lane has
+// more than 2^kRaise: P stays below 2^(kRaise + kShift), inside fp16, and that is rare behind the first tile.  The row's own pieces are h0 .. h1 - 1 (another lane has
 // the same row's others); P is zero in the others.  kMask: the row sees the columns <= last only.
 template <bool kMask>
 __device__ __forceinline__ void softmax_tile(uint32_t s_addr, uint32_t o_addr, int h0, int h1, int last, bool first, float scale_log2e, RowState& row) {
@@ -581,7 +584,7 @@ __device__ __forceinline__ void softmax_tile(uint32_t s_addr, uint32_t o_addr, i
       }
       const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * scale_log2e;
       if (__any_sync(0xffffffffu, mx > row.m + kRaise)) raise(s_addr, o_addr, h, first, mx, row);
-      const float ref = row.m == -INFINITY ? 0.f : row.m;      // a row that has seen no key yet: all its logits are -inf, its P is 0
+      const float ref = row.m == -INFINITY ? 0.f : row.m - kShift;      // a row that has seen no key yet: all its logits are -inf, its P is 0
       const uint64_t ref2 = pack2(-ref, -ref);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
