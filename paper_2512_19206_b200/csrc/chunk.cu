@@ -48,11 +48,10 @@ constexpr int kSegOff = kBarOff + 8 * kBars + 16;         // (the tensor-memory 
 constexpr int kPoisonOff = kSegOff + 2 * 64;            // two segments' Poison
 constexpr int kSmem = kPoisonOff + 2 * (4 + 3 * kD * 4);
 enum Bar { kQFull = 0, kKFull = 1, kVFull = 3, kKEmpty = 5, kVEmpty = 7, kSFull = 9, kPReady = 11, kODone = 13, kDone = 15, kSegFull = 17, kSegEmpty = 19 };
-constexpr uint32_t kPolls = 1u << 19;                    // a poll that finds nothing returns after about 4 us: two seconds
+constexpr uint32_t kPolls = 1u << 19;                    // of 4 us each: two seconds
 constexpr float kRaise = 10.f;
 constexpr float kShift = 5.f;
 constexpr int kAhead = 8;
-constexpr int kProducerNap = 40;
 
 __device__ __forceinline__ void sts32(uint32_t a, uint32_t x) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(a), "r"(x) : "memory"); }
 __device__ __forceinline__ void sts16(uint32_t a, uint32_t x) { asm volatile("st.shared.u16 [%0], %1;" ::"r"(a), "h"((uint16_t)x) : "memory"); }
@@ -86,17 +85,14 @@ __device__ __forceinline__ bool phase_over(uint32_t bar, uint32_t parity) {
                : "memory");
   return ok != 0;
 }
-// Polls a phase of a barrier up to max_polls times; false if it never completed.  (Without a time hint: with one the instruction becomes a loop of
-// sleeps and polls.)  Who has time sleeps `ns` nanoseconds after a poll: a poll returns after a few dozen cycles, and those of the warps that wait for most
-// of the time took a third of the SM's issue slots.
-template <int ns>
+// Polls a phase of a barrier up to max_polls times; false if it never completed.  A poll that finds nothing suspends the warp and returns after 7840 cycles (4.0
+// us at 1.96 GHz), the same with other warps arriving on this barrier or completing phases of others beside it; a phase that completes ends it at once.
+// Sleeping between polls gained nothing (20 to 500 ns: within 0.6 % in all of eight cases, either way).
 __device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, uint32_t max_polls) {
 #pragma unroll 1
-  for (uint32_t n = 0;; ++n) {
-    if (phase_over(bar, parity)) return true;
+  for (uint32_t n = 0; !phase_over(bar, parity); ++n)
     if (n >= max_polls) return false;
-    if (ns > 0) __nanosleep(ns);
-  }
+  return true;
 }
 __device__ __forceinline__ uint4 rows_to_half(uint4 x) {
   return make_uint4(bf16x2_to_f16x2(x.x), bf16x2_to_f16x2(x.y), bf16x2_to_f16x2(x.z), bf16x2_to_f16x2(x.w));
@@ -650,7 +646,6 @@ struct Segment {
 
 template <int n>
 struct Literal {
-  static constexpr int value = n;
   __host__ __device__ constexpr operator int() const { return n; }
 };
 
@@ -743,19 +738,23 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
   dependency_wait();
   // tensor-memory columns: S / P of slot 0 at 0, of slot 1 at 128, O of slot 0 at 256, of slot 1 at 384
   bool dead = false;
-  auto wait_ns = [&](auto ns, int i, uint32_t parity) {
-    if (!dead && !wait_phase<decltype(ns)::value>(bar(i), parity, a.max_polls)) {
+  auto wait = [&](int i, uint32_t parity) {
+    if (!dead && !wait_phase(bar(i), parity, a.max_polls)) {
       dead = true;
       atomicOr(lv.status, (uint32_t)MIXKVQ_DEV_COPY_TIMEOUT);
     }
     return !dead;
   };
-  auto wait = [&](int i, uint32_t parity) { return wait_ns(Literal<0>{}, i, parity); };
-  // The same for a group of `threads` threads: one warp polls, the others wait for it in the named barrier `id`, which costs no issue slots (two dozen
-  // polling warps took a third of them).  The polling warp comes to the barrier in any case, and all learn what it saw.
+  // The same for a whole warp.  (The first poll apart from the loop of `wait`: 2048 new tokens behind 32768, 7b shape, 1163 us and 1265.)
+  auto there = [&](int i, uint32_t parity) {
+    if (__all_sync(0xffffffffu, phase_over(bar(i), parity))) return true;
+    return __all_sync(0xffffffffu, wait(i, parity)) != 0;
+  };
+  // The same for a group of `threads` threads: one warp polls, the others wait for it in the named barrier `id`.  The polling warp comes to the barrier in any
+  // case, and all learn what it saw.
   auto group_wait = [&](int id, int threads, bool polls, int i, uint32_t parity) {
     uint32_t ok = 1;
-    if (polls && i >= 0) ok = wait_ns(Literal<kProducerNap>{}, i, parity);
+    if (polls && i >= 0) ok = wait(i, parity);
     asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %0, 0;\n\tbarrier.cta.red.and.pred q, %1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
                  : "+r"(ok)
                  : "r"(id), "r"(threads)
@@ -763,7 +762,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
     return ok != 0;
   };
   // the n-th segment is there; (a reader's warp has taken what it needs)
-  auto segment_there = [&](int n) { return wait_ns(Literal<200>{}, kSegFull + (n & 1), (uint32_t)(n >> 1) & 1u); };
+  auto segment_there = [&](int n) { return wait(kSegFull + (n & 1), (uint32_t)(n >> 1) & 1u); };
   auto segment_taken = [&](int n) {
     __syncwarp();
     if (lane == 0) mbar_arrive(bar(kSegEmpty + (n & 1)));
@@ -779,10 +778,6 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       constexpr uint32_t kStep = kTileBytes >> 4;        // a tile further, in a descriptor
       const uint32_t qd = desc_lo(qs), kd = desc_lo(ks), vd = desc_lo(vs);
       const bool leader = elect_one();
-      auto there = [&](int i, uint32_t parity) {
-        if (__all_sync(0xffffffffu, phase_over(bar(i), parity))) return true;
-        return __all_sync(0xffffffffu, wait(i, parity)) != 0;
-      };
       uint32_t used = 0, cnt = 0;                        // bit st: parity of the tiles that stage st has had; bit slot: parity of the slot's steps
       // S of `slot` from Q tile `qt` and key stage st; kLast: the stage's last use
       auto issue_s = [&](auto slot_, auto st_, auto qt_, auto last_) {
@@ -883,7 +878,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
         int n = 0;
         auto publish = [&](const Segment& sg) {
           // (a segment takes as long as its item is: the limit holds for one in which nothing moves)
-          for (int seen = -1; n >= 2 && !wait_phase<500>(bar(kSegEmpty + (n & 1)), (uint32_t)((n >> 1) - 1) & 1u, a.max_polls);) {
+          for (int seen = -1; n >= 2 && !wait_phase(bar(kSegEmpty + (n & 1)), (uint32_t)((n >> 1) - 1) & 1u, a.max_polls);) {
             if (*progress == seen) {
               atomicOr(lv.status, (uint32_t)MIXKVQ_DEV_COPY_TIMEOUT);
               return false;
@@ -1142,8 +1137,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
         const int h0 = (row_in >> (7 - lg_copies)) << (2 - lg_copies), h1 = h0 + (4 >> lg_copies);
         bool first = true;
         for (int j = sg.j0 + (dual ? 0 : slot); j < j1; j += step, ++cnt) {
-          ok = __all_sync(0xffffffffu, phase_over(bar(kSFull + slot), (uint32_t)cnt & 1u)) ||
-               __all_sync(0xffffffffu, wait_ns(Literal<20>{}, kSFull + slot, (uint32_t)cnt & 1u));
+          ok = there(kSFull + slot, (uint32_t)cnt & 1u);
           if (!ok) break;
           tc_fence_after();
           if (!idle) {
