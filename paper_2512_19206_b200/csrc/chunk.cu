@@ -97,8 +97,6 @@ __device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, uint32
 __device__ __forceinline__ uint4 rows_to_half(uint4 x) {
   return make_uint4(bf16x2_to_f16x2(x.x), bf16x2_to_f16x2(x.y), bf16x2_to_f16x2(x.z), bf16x2_to_f16x2(x.w));
 }
-__device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
 __device__ __forceinline__ uint32_t hadd2_u(uint32_t a, uint32_t b) {
   uint32_t d;
@@ -650,7 +648,6 @@ struct Literal {
 };
 
 // the first lane's value, the whole warp's
-__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
 __device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 __device__ __forceinline__ bool elect_one() {
   uint32_t e;
@@ -1094,12 +1091,9 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       const volatile Segment& sg = segments[n & 1];
       if (sg.stream < 0) break;
       // Rows of a tile: with more than 128 rows slot 0 has the first 128 of them and slot 1 the others.  Otherwise both have the same ones, and with at most
-      // 64 (32) every row 2 (4) times over, 64 (32) lanes apart, each copy for a half (a quarter) of the tile's keys: a warp's softmax is that much
-      // shorter, and the copies' results meet at the end like the slots'.
-      auto copies_of = [&]() {
-        const int rows = sg.rows_all - sg.row0;
-        return rows > 64 ? 0 : 1;
-      };
+      // 64 every row twice, 64 lanes apart, each copy for half of the tile's keys: a warp's softmax is that much shorter, and the copies' results
+      // meet at the end like the slots'.  (The logarithm of the copies.)
+      auto copies_of = [&]() { return sg.rows_all - sg.row0 > 64 ? 0 : 1; };
       {
         const int row0 = sg.row0, rows_all = sg.rows_all, dual = sg.dual, per = kTile >> copies_of();
         // 16-byte piece p of the image: lane 8 (p / 128) + p % 8, channels 8 (p / 8 % 16) ..  A thread's pieces are 16 lanes apart; eight of them are
@@ -1238,35 +1232,24 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
         softmax_sync();
         const int lg_threads = 1 + lg_copies, r = tid >> lg_threads;             // row r of the item, pieces of 4 channels from c on
         if (r < rows) {
-          float top = -INFINITY, l = 0.f, f[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (i < 1 << lg_copies) top = fmaxf(top, ml[r + i * per].x);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            f[i] = 0.f;
-            if (i < 1 << lg_copies) {
-              const float2 x = ml[r + i * per];
-              f[i] = weight_of(x.x, x.y, top);
-              l += x.y * f[i];
-            }
-          }
+          const float2 x0 = ml[r], x1 = lg_copies ? ml[r + per] : make_float2(-INFINITY, 0.f);
+          const float top = fmaxf(x0.x, x1.x), f0 = weight_of(x0.x, x0.y, top), f1 = weight_of(x1.x, x1.y, top), l = x0.y * f0 + x1.y * f1;
           const float inv = whole ? 1.f / l : 1.f;
           const int t = (row0 + r) / g;
           const size_t orow = ((size_t)stream * g + (row0 + r - t * g)) * a.stride + t;
 #pragma unroll 1
           for (int c = tid & ((1 << lg_threads) - 1); c < 32; c += 1 << lg_threads) {
             float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (f[i] != 0.f) {
-                const int v = r + i * per;
-                const uint4 o = lds128(qs + v * 512 + ((c ^ (v & 31)) << 4));
-                y.x = fmaf(__uint_as_float(o.x), f[i], y.x);
-                y.y = fmaf(__uint_as_float(o.y), f[i], y.y);
-                y.z = fmaf(__uint_as_float(o.z), f[i], y.z);
-                y.w = fmaf(__uint_as_float(o.w), f[i], y.w);
-              }
+            auto add = [&](int v, float f) {             // lane v's sums
+              if (f == 0.f) return;
+              const uint4 o = lds128(qs + v * 512 + ((c ^ (v & 31)) << 4));
+              y.x = fmaf(__uint_as_float(o.x), f, y.x);
+              y.y = fmaf(__uint_as_float(o.y), f, y.y);
+              y.z = fmaf(__uint_as_float(o.z), f, y.z);
+              y.w = fmaf(__uint_as_float(o.w), f, y.w);
+            };
+            add(r, f0);
+            if (lg_copies) add(r + per, f1);
             y.x *= inv; y.y *= inv; y.z *= inv; y.w *= inv;
             if (whole)
               store4(a, orow * kD + 4 * c, y);
