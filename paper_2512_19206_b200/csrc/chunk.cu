@@ -52,6 +52,10 @@ constexpr uint32_t kPolls = 1u << 19;                    // of 4 us each: two se
 constexpr float kRaise = 10.f;
 constexpr float kShift = 5.f;
 constexpr int kAhead = 8;
+// Tiles whose values the tensor core sums.  It truncates: 3.5e-7 of the sum per tile, all in one direction, and addends below 2^-24 of it vanish.  Behind 512
+// tiles (1.8e-4) a sum is set aside and joined with the next one in fp32.  524288 keys of equal weight: 1.4e-3 below the mean in one sum.  (A joint costs
+// about 15 us of a segment's 1.4 ms; that there can be one, 1165 -> 1185 us for 2048 new tokens behind 32768, under 1 % elsewhere.)
+constexpr int kMaxTiles = 512;
 
 __device__ __forceinline__ void sts32(uint32_t a, uint32_t x) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(a), "r"(x) : "memory"); }
 __device__ __forceinline__ void sts16(uint32_t a, uint32_t x) { asm volatile("st.shared.u16 [%0], %1;" ::"r"(a), "h"((uint16_t)x) : "memory"); }
@@ -634,12 +638,12 @@ __device__ constexpr int arrivals(int i) {
   return i == kSegEmpty || i == kSegEmpty + 1 ? kReaders : 1;
 }
 
-// What the roles need to know of a segment (a thread block's key tiles of one item); stream < 0: there is none left.
+// What the roles need to know of a segment (a thread block's key tiles of one item, or up to kMaxTiles of them); stream < 0: there is none left.
 struct Segment {
   int stream, j0, j1, packed_tiles;
   int units, r, c0, total;               // packed units; residual rows; residual and sink rows; unquantized rows that the item's rows may see
-  int row0, rows_all, dual, whole;       // first row; rows of the stream; more than 128 rows; all of the item's key tiles
-  int part, pad[3];                      // which of the thread block's two results
+  int row0, rows_all, dual, whole;       // first row; rows of the stream; more than 128 rows; all of the item's key tiles end here: the result is its output
+  int part, behind, pad[2];              // which of the thread block's two results; it holds that of the item's tiles before these
 };
 
 template <int n>
@@ -873,51 +877,63 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       if (lane == 0) {
         a.at[blockIdx.x] = it;
         int n = 0;
-        auto publish = [&](const Segment& sg) {
-          // (a segment takes as long as its item is: the limit holds for one in which nothing moves)
-          for (int seen = -1; n >= 2 && !wait_phase(bar(kSegEmpty + (n & 1)), (uint32_t)((n >> 1) - 1) & 1u, a.max_polls);) {
-            if (*progress == seen) {
-              atomicOr(lv.status, (uint32_t)MIXKVQ_DEV_COPY_TIMEOUT);
-              return false;
-            }
-            seen = *progress;
+        // the place of the n-th segment, once the one before in it is over
+        auto place = [&]() -> Segment* {
+          if (n >= 2 && !wait_phase(bar(kSegEmpty + (n & 1)), (uint32_t)((n >> 1) - 1) & 1u, a.max_polls)) {
+            atomicOr(lv.status, (uint32_t)MIXKVQ_DEV_COPY_TIMEOUT);
+            return nullptr;
           }
-          if (n >= 2 && poison[n & 1].any != 0) {          // (all of the segment before in this place is over, its output too)
+          if (n >= 2 && poison[n & 1].any != 0) {
 #pragma unroll 1
             for (int i = 0; i < 3 * kD; ++i) poison[n & 1].first[0][i] = kNever;
             poison[n & 1].any = 0;
           }
-          segments[n & 1] = sg;
+          return &segments[n & 1];
+        };
+        auto announce = [&]() {
           mbar_arrive(bar(kSegFull + (n & 1)));
           n += 1;
-          return true;
         };
-        bool ok = true;
+        Segment* sg = nullptr;
         for (;;) {
-          Segment sg;
-          chunk_tiles(it, begin, end, sg.j0, sg.j1);
-          if (sg.j0 < sg.j1) {
+          int j, j1;
+          chunk_tiles(it, begin, end, j, j1);
+          const bool whole = j == 0 && j1 == it.kt;
+          int behind = 0;
+#pragma unroll 1
+          while (j < j1) {
+            sg = place();
+            if (sg == nullptr) break;
             const ChunkSeq sq = a.seq[it.b];
-            sg.stream = it.b * lv.Hkv + it.hk;
-            sg.packed_tiles = it.packed_tiles;
-            sg.units = sq.units;
-            sg.r = sq.tail & 0xFFFF;
-            sg.c0 = chunk_tail_rows(sq);
-            sg.total = sg.c0 + sq.n;
-            sg.row0 = kChunkRows * it.rt;
-            sg.rows_all = sq.n * g;
-            sg.dual = it.weight - 1;
-            sg.whole = sg.j0 == 0 && sg.j1 == it.kt;
-            sg.part = it.x0 <= begin ? 0 : 1;
-            ok = publish(sg);
+            const int left = j1 - j, next = left <= kMaxTiles ? j1 : j + (left >= 2 * kMaxTiles ? kMaxTiles : left / 2);
+            sg->stream = it.b * lv.Hkv + it.hk;
+            sg->j0 = j;
+            sg->j1 = next;
+            sg->packed_tiles = it.packed_tiles;
+            sg->units = sq.units;
+            sg->r = sq.tail & 0xFFFF;
+            sg->c0 = chunk_tail_rows(sq);
+            sg->total = sg->c0 + sq.n;
+            sg->row0 = kChunkRows * it.rt;
+            sg->rows_all = sq.n * g;
+            sg->dual = it.weight - 1;
+            sg->whole = whole && next == j1;
+            // (a whole item's pieces meet in the second result, which only the block's last item leaves to the merge)
+            sg->part = it.x0 <= begin && !whole ? 0 : 1;
+            sg->behind = behind;
+            announce();
+            behind = 1;
+            j = next;
           }
-          if (!ok || it.x0 + (long long)it.weight * it.kt >= end) break;
+          if (j < j1 || it.x0 + (long long)it.weight * it.kt >= end) break;
           chunk_next(a, lv.Hkv, g, it);
         }
-        if (ok) {
-          Segment none{};
-          none.stream = -1;
-          publish(none);
+        if (sg != nullptr || n == 0) {
+          sg = place();
+          if (sg != nullptr) {
+            sg->stream = -1;
+            announce();
+          }
         }
       }
     } else if (warp == kIssueWarp + 2) {
@@ -1148,7 +1164,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
         }
       }
       // ---- the segment's result
-      const int stream = sg.stream, dual = sg.dual, row0 = sg.row0, rows_all = sg.rows_all, whole = sg.whole;
+      const int stream = sg.stream, dual = sg.dual, row0 = sg.row0, rows_all = sg.rows_all, behind = sg.behind, whole = sg.whole && !behind;
       const int rows = min(rows_all - row0, kChunkRows), lg_copies = copies_of(), per = kTile >> lg_copies;
       const int row = row0 + (dual ? slot * kTile + row_in : row_in & (per - 1));
       const bool idle = (row & ~31) >= rows_all;
@@ -1158,7 +1174,8 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       tc_fence_after();
       ended[0] += 1;
       ended[1] += both;
-      float* part = a.parts + ((size_t)blockIdx.x * 2 + sg.part) * a.rows_cap * (kD + 2);
+      const size_t part_floats = (size_t)a.rows_cap * (kD + 2);
+      float* part = a.parts + ((size_t)blockIdx.x * kChunkParts + (behind ? kChunkParts - 1 : sg.part)) * part_floats;
       const float l_run = mine ? state.sum() : 0.f, m_run = mine ? state.m : -INFINITY;
       if (dual) {
         if (!idle) {
@@ -1259,6 +1276,34 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
           if (!whole && (tid & ((1 << lg_threads) - 1)) == 0) reinterpret_cast<float2*>(part + (size_t)a.rows_cap * kD)[r] = make_float2(top, l);
         }
       }
+      if (behind) {
+        // a later piece of the block's part of the item: its result joins that of the pieces before it (the same threads left both)
+        const int lg_threads = dual ? 0 : 1 + lg_copies, r = tid >> lg_threads, t = (row0 + r) / g;
+        const size_t orow = ((size_t)stream * g + (row0 + r - t * g)) * a.stride + t;
+        float* before = a.parts + ((size_t)blockIdx.x * kChunkParts + sg.part) * part_floats;
+        float2* before_ml = reinterpret_cast<float2*>(before + (size_t)a.rows_cap * kD) + r;
+        softmax_sync();
+        float2 x = make_float2(-INFINITY, 0.f), y = x;
+        if (r < rows) {
+          x = *before_ml;
+          y = reinterpret_cast<const float2*>(part + (size_t)a.rows_cap * kD)[r];
+        }
+        const float top = fmaxf(x.x, y.x), fx = weight_of(x.x, x.y, top), fy = weight_of(y.x, y.y, top), l = x.y * fx + y.y * fy, inv = sg.whole ? 1.f / l : 1.f;
+        softmax_sync();
+#pragma unroll 1
+        for (int c = tid & ((1 << lg_threads) - 1); c < 32 && r < rows; c += 1 << lg_threads) {
+          float4* dst = reinterpret_cast<float4*>(before + (size_t)r * kD) + c;
+          float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+          add_part(fx, x.y, *dst, sum);
+          add_part(fy, y.y, reinterpret_cast<const float4*>(part + (size_t)r * kD)[c], sum);
+          if (sg.whole)
+            store4(a, orow * kD + 4 * c, make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
+          else
+            *dst = sum;
+        }
+        if (!sg.whole && r < rows && (tid & ((1 << lg_threads) - 1)) == 0) *before_ml = make_float2(top, l);
+        part = before;
+      }
       if (*reinterpret_cast<volatile int*>(&poison[n & 1].any) != 0) {     // (the segment's products are over, and the thread's own outputs stored)
         const int lg_threads = dual ? 0 : 1 + lg_copies, r = tid >> lg_threads, t = (row0 + r) / g;
         const size_t orow = ((size_t)stream * g + (row0 + r - t * g)) * a.stride + t;
@@ -1266,7 +1311,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
         for (int d = 0; d < kD && r < rows; ++d) {
           const float x = poison_of(poison[n & 1], d, t);
           if (x == 0.f || (((d >> 2) ^ tid) & ((1 << lg_threads) - 1)) != 0) continue;
-          if (!whole)
+          if (!sg.whole)
             part[(size_t)r * kD + d] += x;
           else if (a.out_bf16)
             static_cast<__nv_bfloat16*>(a.out)[orow * kD + d] += __float2bfloat16_rn(x);
@@ -1328,7 +1373,7 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant_
         ml[k] = make_float2(-INFINITY, 0.f);
         y[k] = make_float4(0.f, 0.f, 0.f, 0.f);
         if (which >= 0) {
-          const float* part = a.parts + ((size_t)(c0 + i) * 2 + which) * part_floats;
+          const float* part = a.parts + ((size_t)(c0 + i) * kChunkParts + which) * part_floats;
           ml[k] = reinterpret_cast<const float2*>(part + (size_t)a.rows_cap * kD)[prow];
           y[k] = reinterpret_cast<const float4*>(part + (size_t)prow * kD)[lane];
         }
@@ -1395,7 +1440,7 @@ cudaError_t chunk_attention_setup() {
 // Rows that a thread block's result can have: an item's, and an even number, so that every result starts on 16 bytes.
 static int rows_cap(int g, int n_tokens) { return (int)std::min<long long>(kChunkRows, ((long long)n_tokens * g + 1) & ~1ll); }
 
-static size_t parts_bytes(int g, int n_tokens) { return (size_t)kChunkMaxCtas * 2 * rows_cap(g, n_tokens) * (kD + 2) * sizeof(float); }
+static size_t parts_bytes(int g, int n_tokens) { return (size_t)kChunkMaxCtas * kChunkParts * rows_cap(g, n_tokens) * (kD + 2) * sizeof(float); }
 
 size_t chunk_scratch_bytes(int g, int n_tokens) { return parts_bytes(g, n_tokens) + kChunkMaxCtas * sizeof(ChunkItem); }
 

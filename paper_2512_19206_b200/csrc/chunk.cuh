@@ -9,6 +9,7 @@ constexpr int kChunkMaxSeqs = 128;     // sequences of one launch (a larger batc
 constexpr int kChunkMaxCtas = 148;     // thread blocks of one launch: one per SM (sizes the scratch memory)
 constexpr int kChunkRows = 256;        // query rows of an item
 constexpr int kChunkTile = 128;        // keys of a tile
+constexpr int kChunkParts = 3;         // results of a thread block: of its first item, of its last one, of a later piece of an item
 
 struct ChunkItem;
 struct ChunkSeq {
@@ -25,7 +26,7 @@ struct ChunkArgs {
   struct ChunkItem* at;                // per thread block: the item that its first position lies in (behind parts; the merge reads it)
   const uint16_t *k, *v, *q;           // [B, Hkv, stride, 128], [B, Hq, stride, 128] bf16
   void* out;                           // [B, Hq, stride, 128]
-  float* parts;                        // two results of rows_cap rows per thread block: [rows_cap][128] sums, [rows_cap] (maximum, denominator)
+  float* parts;                        // kChunkParts results of rows_cap rows per thread block: [rows_cap][128] sums, [rows_cap] (maximum, denominator)
   int out_bf16, stride, ctas, rows_cap;
   float scale_log2e;
   uint32_t max_polls, test_silent;     // test_silent: the first key tile is never announced (test hook)

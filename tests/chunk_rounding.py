@@ -35,12 +35,13 @@ def attend(K, V, q, scale, sees):
     return p, p @ V, s
 
 
-def allowed(p, s, K, V, q, scale):
+def allowed(p, s, K, V, q, scale, deepest=516):
     """What the kernel's roundings may add, per output element.
 
     Probabilities are fp16, each rounded by at most HALF_STEP of itself, independently: six standard deviations of HALF_STEP / sqrt(3) of the root of
     sum (p v)^2; below 2^-19 of the row's reference by 2^-30 of the reference instead, which is no more than the row's denominator: 2^-30 sum |v|.
-    Sums in the tensor core lose at most a unit of 2^-23 for each of a tile's eight steps and one more for its products.  A logit is such a sum (one tile
+    Sums in the tensor core lose at most a unit of 2^-23 for each of a tile's eight steps and one more for its products, over 512 tiles at most (then they
+    are set aside).  A logit is such a sum (one tile
     deep), scaled and subtracted in fp32, and its exponential is good to 2^-21; a relative error d of the probabilities moves the output by at most
     d sum p |v - o|, here d sum p |v| twice.  Merging and dividing: 2^-20.  Equal logits give equal powers of two, which fp16 holds."""
     V1, flat = V.abs(), (q == 0).all(-1, keepdim=True)
@@ -48,7 +49,7 @@ def allowed(p, s, K, V, q, scale):
     rounding = 6 / 3 ** 0.5 * HALF_STEP * ((p * p) @ (V * V)).sqrt() + 2.0 ** -30 * V1.sum(0)
     depth = ((q.abs() @ K.abs().T).amax(-1, keepdim=True)) * scale
     logit = 9 * 2.0 ** -23 * depth + 4 * 2.0 ** -23 * s.abs().amax(-1, keepdim=True) + 2.0 ** -21
-    tiles = K.shape[0] / TILE + 4
+    tiles = min(K.shape[0] / TILE + 4, deepest)
     return torch.where(flat, torch.zeros_like(pv), rounding + 2 * logit * pv) + (9 * tiles * 2.0 ** -23 + 2.0 ** -20) * pv
 
 

@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+import chunk_rounding as CR
 from paper_2512_19206_b200 import workloads as W
 
 pytestmark = pytest.mark.gpu
@@ -38,3 +39,74 @@ def test_a_flat_tail_below_one_key(binding):
     # eight steps and one for its products; a logit of 21 in fp32 and its exponential 2^-18.
     tol = (T + n) * 2.0 ** -30 + tail * (2.0 ** -11 + 2.0 ** -18 + 9 * 2.0 ** -23 * ((T + n) / 128 + 4))
     assert bool(((out - ref).abs() <= tol).all()), float(((out - ref).abs() / tol).max())
+
+
+def test_a_long_flat_sum(binding):
+    """524288 keys of equal weight, values with a mean: what the tensor core's truncated sums lose does not grow with the context.  148 items of all keys."""
+    T, n, g = 524288, 4736, 8
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    cache = binding.Cache(binding.make_config(1, 1, g, 1, T))
+    total, part = torch.zeros(128, dtype=torch.float64, device="cuda"), 65536
+    for _ in range(T // part):
+        v = (1 + torch.rand((1, 1, part, 4, 1), generator=gen, device="cuda")).bfloat16().expand(1, 1, part, 4, 32).reshape(1, 1, part, 128)    # exact when packed
+        cache.quantize_append(0, torch.zeros_like(v), v, torch.zeros((1, g, part, 128), device="cuda", dtype=torch.bfloat16))
+        total += v.double().sum((0, 1, 2))
+    vn = (1 + torch.rand((1, 1, n, 128), generator=gen, device="cuda")).bfloat16()
+    out = cache.chunk_attention(0, torch.zeros_like(vn), vn, torch.zeros((1, g, n, 128), device="cuda", dtype=torch.bfloat16), SCALE).double()
+    assert cache.status() == 0
+    ref = (total + vn.double().cumsum(2)) / (T + 1 + torch.arange(n, device="cuda").double()[:, None])
+    # equal weights are powers of two; 9 * 2^-23 for each of at most 512 tiles and the few that join them
+    tol = (9 * 516 * 2.0 ** -23 + 2.0 ** -20) * ref
+    assert bool(((out - ref).abs() <= tol).all()), float(((out - ref).abs() / tol).max())
+
+
+@pytest.mark.parametrize("trend", [0.0, 1.0, -1.0])
+@pytest.mark.parametrize("g,n", [(1, 1), (1, 100), (2, 130)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_segments_in_pieces(binding, trend, g, n, dtype):
+    """An item of more than 512 key tiles is summed in pieces, whichever of them has the larger logits; 148 items, so that each is one thread block's.
+    Keys are the same over 32 tokens and values over 32 channels: packed, they are exact."""
+    B, Hkv, T = 37, 4, 70000
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    cache = binding.Cache(binding.make_config(1, B, Hkv * g, Hkv, T))
+    rand = lambda *shape: torch.randn(shape, generator=gen, device="cuda")            # noqa: E731
+    keep, held = [(0, 0), (20, 1), (36, 3)], {}
+    for t in range(0, T, 3500):
+        k = (rand(B, Hkv, 111, 1, 128) * (0.3 + trend * (t / T - 0.5) * 0.5)).bfloat16().expand(-1, -1, -1, 32, -1).reshape(B, Hkv, 3552, 128)[:, :, t % 32:][:, :, :3500]
+        v = (rand(B, Hkv, 3500, 4, 1) + 0.5).bfloat16().expand(-1, -1, -1, -1, 32).reshape(B, Hkv, 3500, 128)
+        cache.quantize_append(0, k.contiguous(), v.contiguous(), torch.zeros((B, Hkv * g, 3500, 128), device="cuda", dtype=torch.bfloat16))
+        for b, h in keep:
+            held.setdefault((b, h), []).append((k[b, h].clone(), v[b, h].clone()))
+    kn, vn, q = rand(B, Hkv, n, 128).bfloat16(), rand(B, Hkv, n, 128).bfloat16(), (1.5 * rand(B, Hkv * g, n, 128)).bfloat16()
+    out = cache.chunk_attention(0, kn, vn, q, SCALE, dtype=dtype)
+    assert cache.status() == 0
+    sees = CR.visible(T, n).cuda()
+    for b, h in keep:
+        K, V = (torch.cat([*(x[i] for x in held[(b, h)]), new[b, h]]).half().double() for i, new in ((0, kn), (1, vn)))
+        hs = slice(h * g, h * g + g)
+        qq = q[b, hs].half().double()
+        p, ref, s = CR.attend(K, V, qq, SCALE, sees)
+        step = 0.0 if dtype == torch.float32 else torch.finfo(dtype).eps / 2
+        share = CR.worst(out[b, hs].double(), ref, CR.allowed(p, s, K, V, qq, SCALE), step)
+        assert share <= 1.0, (b, h, share)
+
+
+def test_no_number_in_an_earlier_piece(binding):
+    """An infinity and a NaN among 70000 new tokens reach the rows behind them through the later pieces of their segments."""
+    n = 70000
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    k, v, q = (torch.randn((1, 1, n, 128), generator=gen, device="cuda").bfloat16() for _ in range(3))
+    cache = binding.Cache(binding.make_config(1, 1, 1, 1, 128))
+    want = cache.chunk_attention(0, k, v, q, SCALE)
+    v2 = v.clone()
+    v2[0, 0, 10, 3], v2[0, 0, 300, 4], v2[0, 0, 69000, 5] = float("nan"), float("inf"), float("-inf")
+    out = cache.chunk_attention(0, k, v2, q, SCALE)
+    assert cache.status() == 0
+    rows = torch.arange(n, device="cuda")
+    assert torch.equal(torch.isnan(out[0, 0, :, 3]), rows >= 10)
+    assert torch.equal(torch.isposinf(out[0, 0, :, 4]), rows >= 300) and torch.equal(torch.isneginf(out[0, 0, :, 5]), rows >= 69000)
+    fine = torch.isfinite(out)
+    assert int((~fine).sum()) == (n - 10) + (n - 300) + (n - 69000)
+    same = fine.clone()
+    same[..., 3:6] = False
+    assert torch.equal(out[same], want[same])
