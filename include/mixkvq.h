@@ -247,7 +247,7 @@ int mixkvq_prefill(mixkvq_cache* cache, int layer, const void* k_dev, const void
  * 2^-14 round to fp16 subnormals.  A key's weight is rounded by up to 2^-11 of itself or 2^-30 of the row's largest one.  A NaN or an infinity among the new tokens reaches the rows that attend to it and no others.
  * The tensor core's sums are truncated, not rounded: about 3.5e-7 of the output per 128 tokens held, in one direction, up to 1.8e-4; what a key adds
  * below 2^-24 of the sum is lost.  65536 tokens are summed so at most; the sums of more are joined in fp32.
- * softmax_scale > 0; out_dev and scratch_dev overlap no other argument (MIXKVQ_E_INVALID_ARG); fragment layout, n_tokens_max <=
+ * softmax_scale > 0; out_dev and scratch_dev overlap no other argument nor the cache's memory (MIXKVQ_E_INVALID_ARG); fragment layout, n_tokens_max <=
  * MIXKVQ_CHUNK_MAX_TOKENS (MIXKVQ_E_UNSUPPORTED otherwise); scratch too small: MIXKVQ_E_BUFFER_TOO_SMALL.  A wait that runs out sets
  * MIXKVQ_DEV_COPY_TIMEOUT; the rows concerned are then wrong.  Nothing is allocated and nothing synchronises with the host. */
 enum { MIXKVQ_OUT_FLOAT = 0, MIXKVQ_OUT_BF16 = 1 };

@@ -380,11 +380,12 @@ int check_chunk(const mixkvq_cache* cache, int layer, const void* k_dev, const v
   if (cache->tile || n_tokens_max > MIXKVQ_CHUNK_MAX_TOKENS) return MIXKVQ_E_UNSUPPORTED;
   const size_t need = chunk_scratch_bytes(cache->g, n_tokens_max);
   if (scratch_bytes < need) return MIXKVQ_E_BUFFER_TOO_SMALL;
-  // The output and the scratch overlap nothing: thread blocks read queries and keys after others have written rows.
+  // The output and the scratch overlap nothing, the cache's memory included: thread blocks read queries and keys after others have written rows.
   const size_t row = (size_t)cache->cfg.batch * n_tokens_max * kD, kv = 2 * row * cache->cfg.n_kv_heads, qo = row * cache->cfg.n_q_heads;
-  const struct { const void* p; size_t bytes; } mem[5] = {{out_dev, qo * (out_type == MIXKVQ_OUT_BF16 ? 2 : 4)}, {scratch_dev, need}, {k_dev, kv}, {v_dev, kv}, {q_dev, 2 * qo}};
+  const struct { const void* p; size_t bytes; } mem[6] = {{out_dev, qo * (out_type == MIXKVQ_OUT_BF16 ? 2 : 4)}, {scratch_dev, need}, {k_dev, kv}, {v_dev, kv},
+                                                          {q_dev, 2 * qo}, {cache->mem, memory_bytes(cache)}};
   for (int o = 0; o < 2; ++o)
-    for (int i = o + 1; i < 5; ++i) {
+    for (int i = o + 1; i < 6; ++i) {
       const uintptr_t a = reinterpret_cast<uintptr_t>(mem[o].p), b = reinterpret_cast<uintptr_t>(mem[i].p);
       if (a < b + mem[i].bytes && b < a + mem[o].bytes) return MIXKVQ_E_INVALID_ARG;
     }
