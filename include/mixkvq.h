@@ -237,14 +237,18 @@ int mixkvq_prefill(mixkvq_cache* cache, int layer, const void* k_dev, const void
  *   k_dev, v_dev [B, Hkv, n_tokens_max, 128], q_dev [B, Hq, n_tokens_max, 128] bf16 (post-RoPE)  ->  out_dev [B, Hq, n_tokens_max, 128]
  * New token j attends to everything the sequence holds (sink, packed blocks dequantized by Eq. 3, residual window) and to the new tokens
  * 0 .. j in full precision.  out_type: MIXKVQ_OUT_FLOAT or MIXKVQ_OUT_BF16 (rounded once, to nearest).  Rows behind a sequence's count are neither
- * read nor written.  The sequences may hold different numbers of tokens.  An empty layer gives the causal attention of mixkvq_prefill.
+ * read nor written.  The sequences may hold different numbers of tokens.  An empty layer gives the causal attention of mixkvq_prefill (that
+ * multiplies queries and keys in bf16 and so takes any magnitude; here they are fp16, see below).
  * mixkvq_chunk_attention appends nothing: accepted tokens go in with mixkvq_quantize_append_ragged, which takes the same tensors.
  * mixkvq_chunk_step is mixkvq_chunk_attention, then the chunk is appended as mixkvq_quantize_append_ragged does it; on
  * MIXKVQ_E_CAPACITY nothing was enqueued.
  *   scratch_dev: at least mixkvq_chunk_scratch_bytes(cfg, n_tokens_max) bytes, contents are scratch, free for reuse once the call's work has
  *   run (two calls that may overlap on the GPU need one each, two captured graphs too unless they never run at the same time).
- * Numeric range: products are fp16 with fp32 accumulation, so |q|, |k|, |v| and dequantized elements must stay below 65504; elements below
- * 2^-14 round to fp16 subnormals.  A key's weight is rounded by up to 2^-11 of itself or 2^-30 of the row's largest one.  A NaN or an infinity among the new tokens reaches the rows that attend to it and no others.
+ * The fills and the counts are parameters of the launches: a captured call is replayed with those of its capture.
+ * Numeric range: products are fp16 with fp32 accumulation, so |q|, |k|, |v| and dequantized elements must stay below 65504.  A dequantized element is
+ * rounded once, by 2^-11 of itself; below 2^-14 elements round to fp16 subnormals (2^-25), and those of a group whose scale is below 2^-15 by up to 2^-20
+ * (2-bit codes) or 2^-18 (4-bit).  A key's weight is rounded by up to 2^-11 of itself or 2^-30 of the row's largest one.  A NaN or an infinity
+ * among the new tokens reaches the rows that attend to it and no others.
  * The tensor core's sums are truncated, not rounded: about 3.5e-7 of the output per 128 tokens held, in one direction, up to 1.8e-4; what a key adds
  * below 2^-24 of the sum is lost.  65536 tokens are summed so at most; the sums of more are joined in fp32.
  * softmax_scale > 0; out_dev and scratch_dev overlap no other argument nor the cache's memory (MIXKVQ_E_INVALID_ARG); fragment layout, n_tokens_max <=

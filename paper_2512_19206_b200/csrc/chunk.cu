@@ -126,8 +126,9 @@ __device__ __forceinline__ uint32_t above2(uint32_t a, uint32_t b) {
 constexpr uint32_t kQuarter2 = 0x34003400u;               // the fp16 pair (0.25, 0.25)
 
 // c s + z of field f (2 bits at bit 2 f of each half word), one rounding.  The number with the field's bits in its mantissa is 1024 + c (f even) or
-// 1024 + 4 c (f odd), less 1024 it is exact, and for odd fields `s` is a quarter of the scale (exact as well: the scale has 8 significant bits; fewer than
-// two shifts and one constant per pair of fields, where a scale factor per field would cost a register or a move each).
+// 1024 + 4 c (f odd), less 1024 it is exact, and for odd fields `s` is a quarter of the scale (it has 8 significant bits: exact too from 2^-15 on, below that
+// off by up to 2^-25, 4 c times which goes into the value; fewer than two shifts and one constant per pair of fields, where a scale factor per field would cost a
+// register or a move each).
 __device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t b, uint32_t c) {
   uint32_t d;
   asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(a), "r"(b), "r"(c));

@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+import gpu_util as U
 from paper_2512_19206_b200 import workloads as W
 
 pytestmark = pytest.mark.gpu
@@ -40,3 +41,27 @@ def test_output_and_scratch_over_the_cache(binding):
         assert e.value.code == -1
     torch.cuda.synchronize()
     assert cache.launch_count() == before and torch.equal(cache.mem, was) and cache.sequence_fill(0, 0) == (0, n, 0)
+
+
+@pytest.mark.parametrize("preset", ["P24", "P27", "P4BASE"])
+@pytest.mark.parametrize("n", [1, 30])
+def test_behind_a_full_arena(binding, preset, n):
+    """Blocks that found no room for their promoted channels: the status says so, and the chunk reads them as the decode kernels do (the plain one, in 32
+    bits).  A token that all rows see decides nothing here: the last of the chunk's rows is the decode step's."""
+    w = W.small(W.CONFIGS["qwen7b"], n_layers=1, batch=2, tokens=700, **getattr(W, preset))
+    cache = U.make_cache(binding, w, extras_budget_bytes=2048 if preset == "P24" else 8192)
+    full = U.make_cache(binding, w, extras_budget_bytes=10 * 320 * 128)
+    part = [t.cuda() for t in W.tokens(w, 0, 0, 600)]
+    new = [t[:, :, :n].contiguous() for t in (x.cuda() for x in W.tokens(w, 0, 600, n))]
+    for c in (cache, full):
+        c.quantize_append(0, *part)
+    assert cache.status() == binding.DEV_EXTRAS_FULL and full.status() == 0
+    out = cache.chunk_attention(0, *new, SCALE)
+    assert not torch.equal(out, full.chunk_attention(0, *new, SCALE))
+    cache.quantize_append(0, *new)
+    cache.set_attention_kernel(1)
+    ref = cache.decode_attention(0, new[2][:, :, -1].contiguous(), SCALE)
+    assert cache.status() == binding.DEV_EXTRAS_FULL
+    # keys, values and probabilities in fp16: each moves the output by 2^-11 / sqrt(3) of its own root mean square, the keys' through logits of about 2
+    d = (out[:, :, -1] - ref).double()
+    assert float(d.norm() / ref.double().norm()) <= 8e-4

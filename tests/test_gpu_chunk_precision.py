@@ -3,6 +3,8 @@ import pytest
 import torch
 
 import chunk_rounding as CR
+import chunk_util as CU
+import gpu_util as U
 from paper_2512_19206_b200 import workloads as W
 
 pytestmark = pytest.mark.gpu
@@ -110,3 +112,49 @@ def test_no_number_in_an_earlier_piece(binding):
     same = fine.clone()
     same[..., 3:6] = False
     assert torch.equal(out[same], want[same])
+
+
+@pytest.mark.parametrize("name,batch,tokens,preset,v_bits", [("qwen7b", 4, 8000, "P24", 2), ("qwen7b", 4, 8000, "P27", 2), ("llama8b", 2, 8000, "P4BASE", 4),
+                                                              ("qwen7b", 1, 32700, "P24", 2), ("llama8b", 1, 32700, "P27", 2), ("llama8b", 1, 65400, "P24", 4)])
+def test_relative_error_of_long_caches(binding, name, batch, tokens, preset, v_bits):
+    """One new token's chunk against the plain decode kernel, 32 bits throughout, on the same cache with the token appended."""
+    w = W.small(W.CONFIGS[name], n_layers=1, batch=batch, tokens=tokens + 1, **getattr(W, preset))
+    cache = U.make_cache(binding, w, v_bits=v_bits, extras_budget_bytes=(tokens // 128 + 3) * 64 * 128)
+    for t in range(0, tokens, 4096):
+        cache.quantize_append(0, *W.tokens(w, 0, t, min(4096, tokens - t), device="cuda"))
+    new = W.tokens(w, 0, tokens, 1, device="cuda")
+    out = cache.chunk_attention(0, *new, SCALE)[:, :, 0].double()
+    fill = cache.sequence_fill(0, 0)
+    cache.quantize_append(0, *new)
+    assert cache.sequence_fill(0, 0) == (fill[0], fill[1] + 1, 0)                     # (no window was packed in between)
+    cache.set_attention_kernel(1)
+    ref = cache.decode_attention(0, new[2][:, :, 0].contiguous(), SCALE).double()
+    assert cache.status() == 0
+    # Elements of keys and values and probabilities are rounded to fp16, by at most 2^-11 / sqrt(3) = 2.8e-4 in the root mean square.  A logit is a sum
+    # of 128 products of keys of about 1 and queries of about 1.9, scaled by 128^-1/2: 5.4e-4.  Together 6.7e-4 of an output that is itself such a sum.
+    # The tensor core's truncation, 3.5e-7 per tile, adds 1.8e-4 at most.
+    assert float((out - ref).norm() / ref.norm()) <= 8e-4
+
+
+@pytest.mark.parametrize("v_bits,preset", [(2, "P24"), (4, "P4BASE")])
+@pytest.mark.parametrize("size", [2.0 ** -14, 2.0 ** -17, 2.0 ** -20])
+def test_tiny_values(binding, v_bits, preset, size):
+    """Values whose groups' scales are below what a quarter of them needs in fp16."""
+    w = W.small(W.CONFIGS["llama8b"], n_layers=1, batch=1, n_kv_heads=2, n_q_heads=8, tokens=800, **getattr(W, preset))
+    k, v, q = W.tokens(w, 0, 0, 806)
+    v = (v.float() * size).bfloat16()
+    held, new = [t[:, :, :800].contiguous() for t in (k, v, q)], [t[:, :, 800:].contiguous() for t in (k, v, q)]
+    cache = U.make_cache(binding, w, v_bits=v_bits, extras_budget_bytes=10 * 320 * 128)
+    cache.quantize_append(0, *(t.cuda() for t in held))
+    out = cache.chunk_attention(0, *(t.cuda() for t in new), SCALE).double().cpu()
+    assert cache.status() == 0
+    for (b, hk), st in CU.streams(w, [800], *held, v_bits=v_bits).items():
+        K = torch.cat([CR.fp16(st.keys()), new[0][b, hk].double()])
+        V = torch.cat([torch.from_numpy(st.values()), new[1][b, hk].double()])
+        qq = new[2][b, hk * 4:hk * 4 + 4].double()
+        p, ref, s = CR.attend(K, V, qq, SCALE, CR.visible(800, 6))
+        # scale and a quarter of it, zero-point and element each rounded by half a step of fp16 (2^-25 among the subnormals): 5 c + 2 of them for a
+        # code c, and the new tokens' one
+        tiny = (5 * (2 ** v_bits - 1) + 2) * 2.0 ** -25
+        tol = CR.allowed(p, s, K, V, qq, SCALE) + tiny + CR.HALF_STEP * (p @ V.abs())
+        assert CR.worst(out[b, hk * 4:hk * 4 + 4], ref, tol) <= 1.0
