@@ -158,3 +158,28 @@ def test_tiny_values(binding, v_bits, preset, size):
         tiny = (5 * (2 ** v_bits - 1) + 2) * 2.0 ** -25
         tol = CR.allowed(p, s, K, V, qq, SCALE) + tiny + CR.HALF_STEP * (p @ V.abs())
         assert CR.worst(out[b, hk * 4:hk * 4 + 4], ref, tol) <= 1.0
+
+
+def test_rows_beside_one_whose_maximum_rises(binding):
+    """A weight is rounded once where another row of the same 32 needs its sums rescaled: by 2^-11 of itself, not by that of three roundings.  The first
+    quarter of a tile's keys has values of one, the rest of zero; half a tile later every 32nd row's maximum rises by e^22, the others' by e^0.3 to e^2."""
+    Hkv, n = 8, 70
+    cache = binding.Cache(binding.make_config(1, 1, Hkv, Hkv, 256))
+    k, v = (torch.zeros((1, Hkv, 129, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    k[:, :, :32, 1], k[:, :, 64:128, 1], k[:, :, 64:128, 0], v[:, :, :32] = -1.0, 1.0, 16.0, 1.0            # (groups without a range: exact)
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    q = torch.zeros((1, Hkv, n, 128), dtype=torch.bfloat16, device="cuda")
+    q[..., 1] = (0.3 + 1.7 * torch.rand((1, Hkv, n), generator=gen, device="cuda")) / SCALE
+    q[:, :, ::32, 1], q[:, :, ::32, 0] = 0.0, 16.0
+    cache.quantize_append(0, k, v, torch.ones_like(k))
+    assert cache.sequence_fill(0, 0) == (1, 1, 0)
+    zero = torch.zeros((1, Hkv, n, 128), dtype=torch.bfloat16, device="cuda")
+    out = cache.chunk_attention(0, zero, zero, q, SCALE).double()
+    assert cache.status() == 0
+    x = q.double() @ k.double().transpose(-1, -2) * SCALE                            # the new tokens' logits are 0, as the 129th's
+    w = x.exp()
+    ref = (w[..., :32].sum(-1) / (w.sum(-1) + 1 + torch.arange(n, device="cuda")))[..., None].expand_as(out)
+    # one rounding of equal weights, and fp32: logits of up to 2 and their exponentials 2^-20, two tiles' sums 2^-18
+    share = ((out - ref).abs() / (ref * (2.0 ** -11 + 2.0 ** -17) + 2.0 ** -40))
+    share[:, :, ::32] = 0                                                            # (there the weights are e^-22 of the others)
+    assert float(share.max()) <= 1.0, float(share.max())
