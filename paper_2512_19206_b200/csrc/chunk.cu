@@ -665,19 +665,13 @@ __device__ __forceinline__ bool elect_one() {
 // Weight of a partial result (maximum m, denominator l) in a sum that refers to `top`.  A NaN among the logits makes l NaN, whatever m is, and the row too,
 // even where its weight would round to zero.
 __device__ __forceinline__ float weight_of(float m, float l, float top) { return l != l ? l : m == -INFINITY ? 0.f : ex2(m - top); }
-// sum + w y of a partial result with denominator l; infinity where y is one (a weight that has rounded to zero is positive all the same).  A result
-// without a key (l = 0) is zeros.
-__device__ __forceinline__ void add_part(float w, float l, float4 y, float4& sum) {
-  if (w != 0.f) {
-    sum.x = fmaf(w, y.x, sum.x); sum.y = fmaf(w, y.y, sum.y); sum.z = fmaf(w, y.z, sum.z); sum.w = fmaf(w, y.w, sum.w);
-  } else if (l != 0.f) {
-    sum.x += isfinite(y.x) ? 0.f : y.x; sum.y += isfinite(y.y) ? 0.f : y.y; sum.z += isfinite(y.z) ? 0.f : y.z; sum.w += isfinite(y.w) ? 0.f : y.w;
-  }
+// sum + w y
+__device__ __forceinline__ void add_scaled(float w, float4 y, float4& sum) {
+  sum.x = fmaf(w, y.x, sum.x); sum.y = fmaf(w, y.y, sum.y); sum.z = fmaf(w, y.z, sum.z); sum.w = fmaf(w, y.w, sum.w);
 }
-__device__ __forceinline__ void scale_part(float w, float l, float4& sum) {
-  const float4 y = sum;
-  sum = make_float4(0.f, 0.f, 0.f, 0.f);
-  add_part(w, l, y, sum);
+// Infinities and NaNs of y.  A weight that has rounded to zero is positive all the same: they stay what they are.
+__device__ __forceinline__ void add_not_finite(float4 y, float4& sum) {
+  sum.x += isfinite(y.x) ? 0.f : y.x; sum.y += isfinite(y.y) ? 0.f : y.y; sum.z += isfinite(y.z) ? 0.f : y.z; sum.w += isfinite(y.w) ? 0.f : y.w;
 }
 
 __device__ __forceinline__ void softmax_sync() { asm volatile("barrier.cta.sync 1, 256;" ::: "memory"); }
@@ -1111,7 +1105,8 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       if (sg.stream < 0) break;
       // Rows of a tile: with more than 128 rows slot 0 has the first 128 of them and slot 1 the others.  Otherwise both have the same ones, and with at most
       // 64 every row twice, 64 lanes apart, each copy for half of the tile's keys: a warp's softmax is that much shorter, and the copies' results
-      // meet at the end like the slots'.  (The logarithm of the copies.)
+      // meet at the end like the slots'.  (The logarithm of the copies.  One copy / two, us: 120000 tokens, 8b shape, 4, 32 and 64 rows 99.8 / 93.9, 118.7 /
+      // 107.2, 135.5 / 125.1; 8 x 32768, 7b shape, 7, 35 and 63 rows 106.2 / 102.6, 114.3 / 105.4, 116.5 / 107.0; 1024 tokens, 4 rows 18.1 / 18.5.)
       auto copies_of = [&]() { return sg.rows_all - sg.row0 > 64 ? 0 : 1; };
       {
         const int row0 = sg.row0, rows_all = sg.rows_all, dual = sg.dual, per = kTile >> copies_of();
@@ -1297,8 +1292,11 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
         for (int c = tid & ((1 << lg_threads) - 1); c < 32 && r < rows; c += 1 << lg_threads) {
           float4* dst = reinterpret_cast<float4*>(before + (size_t)r * kD) + c;
           float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-          add_part(fx, x.y, *dst, sum);
-          add_part(fy, y.y, reinterpret_cast<const float4*>(part + (size_t)r * kD)[c], sum);
+          const float4 fresh = reinterpret_cast<const float4*>(part + (size_t)r * kD)[c];
+          if (fx != 0.f) add_scaled(fx, *dst, sum);
+          else add_not_finite(*dst, sum);
+          if (fy != 0.f) add_scaled(fy, fresh, sum);
+          else add_not_finite(fresh, sum);
           if (sg.whole)
             store4(a, orow * kD + 4 * c, make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
           else
@@ -1334,7 +1332,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
 // The items that several thread blocks share: block x has the one around the boundary x + 1, if no earlier boundary lies inside it.  kRows rows at a time of
 // 8 / kRows warps each; a warp takes every (8 / kRows)-th result of its row, kFlight of them in flight.
 template <int kRows>
-__global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant__ LayerView lv, const __grid_constant__ ChunkArgs a, int rows_per_block) {
+__global__ void __launch_bounds__(256, 3) chunk_merge_kernel(const __grid_constant__ LayerView lv, const __grid_constant__ ChunkArgs a, int rows_per_block) {
   constexpr int kWarps = 8 / kRows, kFlight = 8;
   __shared__ float2 mlS[8];
   __shared__ __align__(16) float oS[8][kD];
@@ -1367,16 +1365,18 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant_
     const bool exists = prow < row_end;
     float M = -INFINITY, l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    bool lost = false;                                     // a result's weight has rounded to zero
+    auto part_of = [&](int i) { return a.parts + ((size_t)(c0 + i) * kChunkParts + partS[i]) * part_floats; };
     for (int i0 = sub; exists && i0 < count; i0 += kWarps * kFlight) {
       float2 ml[kFlight];
       float4 y[kFlight];
 #pragma unroll
       for (int k = 0; k < kFlight; ++k) {
-        const int i = i0 + k * kWarps, which = i < count ? partS[i] : -1;
+        const int i = i0 + k * kWarps;
         ml[k] = make_float2(-INFINITY, 0.f);
         y[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (which >= 0) {
-          const float* part = a.parts + ((size_t)(c0 + i) * kChunkParts + which) * part_floats;
+        if (i < count && partS[i] >= 0) {
+          const float* part = part_of(i);
           ml[k] = reinterpret_cast<const float2*>(part + (size_t)a.rows_cap * kD)[prow];
           y[k] = reinterpret_cast<const float4*>(part + (size_t)prow * kD)[lane];
         }
@@ -1385,32 +1385,50 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant_
 #pragma unroll
       for (int k = 0; k < kFlight; ++k) top = fmaxf(top, ml[k].x);
       const float f = weight_of(M, l, top);
-      scale_part(f, l, o);
+      lost = lost || (f == 0.f && l != 0.f);
       l *= f;
+      o = f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
 #pragma unroll
       for (int k = 0; k < kFlight; ++k) {
         const float w = weight_of(ml[k].x, ml[k].y, top);
-        l = fmaf(w, ml[k].y, l);
-        add_part(w, ml[k].y, y[k], o);
+        if (w != 0.f) {
+          l = fmaf(w, ml[k].y, l);
+          add_scaled(w, y[k], o);
+        }
+        lost = lost || (w == 0.f && ml[k].y != 0.f);
       }
       M = top;
     }
+    if (lost)
+#pragma unroll 1
+      for (int i = sub; i < count; i += kWarps)
+        if (partS[i] >= 0) add_not_finite(reinterpret_cast<const float4*>(part_of(i) + (size_t)prow * kD)[lane], o);
     if constexpr (kWarps > 1) {
       if (lane == 0) mlS[warp] = make_float2(M, l);
       reinterpret_cast<float4*>(oS[warp])[lane] = o;
       __syncthreads();
       if (sub == 0) {
+        const float4 first = o;
         float top = M;
         for (int w = 1; w < kWarps; ++w) top = fmaxf(top, mlS[warp + w].x);
         const float f = weight_of(M, l, top);
-        scale_part(f, l, o);
+        lost = f == 0.f && l != 0.f;
         l *= f;
+        o = f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+#pragma unroll 1
         for (int w = 1; w < kWarps; ++w) {
           const float2 ml = mlS[warp + w];
           const float fw = weight_of(ml.x, ml.y, top);
-          const float4 y = reinterpret_cast<const float4*>(oS[warp + w])[lane];
-          l = fmaf(fw, ml.y, l);
-          add_part(fw, ml.y, y, o);
+          if (fw != 0.f) {
+            l = fmaf(fw, ml.y, l);
+            add_scaled(fw, reinterpret_cast<const float4*>(oS[warp + w])[lane], o);
+          }
+          lost = lost || (fw == 0.f && ml.y != 0.f);
+        }
+        if (lost) {
+          add_not_finite(first, o);
+#pragma unroll 1
+          for (int w = 1; w < kWarps; ++w) add_not_finite(reinterpret_cast<const float4*>(oS[warp + w])[lane], o);
         }
       }
     }
