@@ -1494,9 +1494,10 @@ cudaError_t launch_chunk_attention(const LayerView& lv, ChunkArgs& a, int n_sms,
   if (e != cudaSuccess) return e;
   *launches = 1;
   if (a.ctas == 1) return cudaSuccess;
-  // Few results per item: a warp per row, 16 rows per block.  Many (one or two long sequences): the eight warps of a block share a row's results, one row after
-  // another; then there are few rows, one per block.
-  if (a.ctas > 8 * items)
+  // An item with fewer results than rows: a warp per row, 16 rows per block.  Otherwise (one or two long sequences, few new tokens) the eight warps of a block share
+  // a row's results, a row per block.  The whole call, us, a warp / a block per row, results an item x rows: 148 x 1 46.7 / 27.5, 74 x 5 35.8 / 27.1,
+  // 37 x 7 55.2 / 51.9, 18 x 4 95.2 / 92.0, 6 x 4 94.0 / 94.0, 37 x 35 64.4 / 61.0; 18 x 35 62.5 / 65.5, 9 x 35 62.5 / 70.2, 18 x 256 95 / 145.
+  if (a.ctas >= a.rows_cap * items)
     e = launch_dependent(chunk_merge_kernel<1>, dim3((unsigned)(a.ctas - 1), (unsigned)a.rows_cap), 256, 0, stream, lv, a, 1);
   else
     e = launch_dependent(chunk_merge_kernel<8>, dim3((unsigned)(a.ctas - 1), (unsigned)((a.rows_cap + 15) / 16)), 256, 0, stream, lv, a, 16);
