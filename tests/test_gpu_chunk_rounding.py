@@ -49,6 +49,14 @@ def test_presets_and_block_sizes(binding, preset, R, G):
     both(binding, w, [700], [9])
 
 
+@pytest.mark.parametrize("preset,v_bits", [("P24", 4), ("P27", 2), ("P4BASE", 2)])
+@pytest.mark.parametrize("R,G", [(160, 32), (192, 64), (224, 32)])
+def test_blocks_whose_units_divide_no_tile(binding, preset, v_bits, R, G):
+    """Five, six and seven units a block: tiles begin anywhere in a block, and a thread block's share anywhere in the sequence."""
+    w = W.small(W.CONFIGS["qwen7b"], n_layers=1, batch=1, n_kv_heads=2, n_q_heads=6, tokens=2900, residual_len=R, group_size=G, **getattr(W, preset))
+    both(binding, w, [2900], [7], v_bits=v_bits)
+
+
 @pytest.mark.parametrize("v_bits,sink,preset", [(4, 0, "P24"), (4, 32, "P4BASE"), (2, 64, "P27")])
 @pytest.mark.parametrize("tokens", [1, 31, 200, 901])
 def test_values_and_sinks(binding, v_bits, sink, preset, tokens):
