@@ -17,8 +17,8 @@
 // warp's store is 128 contiguous bytes (the keys': four of them).
 // The running maximum is raised (and O rescaled, in tensor memory) only when a row's logits exceed it by more than 2^10, so that the rescaling is rare.  P is
 // fp16 (11 significant bits), 2^5 times the probability relative to that maximum: below 2^15, inside fp16, and numbers down to 2^-19 of the maximum are rounded
-// by 2^-11 of themselves, smaller ones by 2^-30 of the maximum.  The denominator sums what P was before the rounding.  Sums, maxima, O are fp32.
-// (Without the factor weights below 2^-25 were zero in P and counted in the denominator: 16384 keys 17.4 nats below one with values of zero gave nothing.)
+// by 2^-11 of themselves, smaller ones by 2^-30 of the maximum.  The denominator sums P as it was rounded.  Sums, maxima, O are fp32.
+// (Without the factor weights below 2^-25 were zero in P: 16384 keys 17.4 nats below one with values of zero gave nothing.)
 //
 // What bounds it (B200).  Few rows, long caches: the making of the tiles.  A key tile of 128 x 128 takes about 6700 warp instructions, three fifths of them logic,
 // fp16 operations and stores of codes; 56 % of the issue slots are taken, a tile every 2500 cycles (2900 with start and end).  Eight sequences of 32768 tokens,
@@ -523,12 +523,16 @@ struct RowState {
   }
 };
 
-// Raises the reference towards mx by a whole number, so that it is less than one below: what lies in tensor memory on the old one is rescaled, the sums at
-// o_addr (unless they are the first tile's, which are not there yet) and the pieces of P before `written` at s_addr.  A power of two rounds nothing (with
-// the factor to mx itself the rows that another row's rise takes along had their P rounded twice more, up to 2.6 times 2^-11; rising alone they
-// took 3 % longer).  The products before this tile are complete: S is behind them in the tensor core's order.
-__device__ __forceinline__ void raise(uint32_t s_addr, uint32_t o_addr, int written, bool first, float mx, RowState& row) {
-  const float by = fmaxf(floorf(mx - row.m), 0.f), m_new = row.m == -INFINITY ? mx : row.m + by, alpha = row.m == -INFINITY ? 1.f : ex2(-by);
+// Raises the reference to mx if that is above it: what lies in tensor memory on the old one is rescaled, the sums at o_addr (unless they are the first tile's,
+// which are not there yet) and the pieces of P before `written` at s_addr.  At mx itself the largest probability is a power of two, which fp16 holds: the
+// error of a decode-sized call over 8000 tokens is 2.7e-5 of the output's norm (6.4e-5 with references a whole number higher).  Only where the row has
+// pieces of P already (`keep`) and rises because another row of the warp does, by 2^kRaise at most, it rises by a whole number: another factor would
+// round those pieces twice more, up to 2.6 times 2^-11 in all.  (Such rows not raised: 1201 us and 1211 for 2048 new tokens behind 32768.)  The
+// products before this tile are complete: S is behind them in the tensor core's order.
+__device__ __forceinline__ void raise(uint32_t s_addr, uint32_t o_addr, int written, bool keep, bool first, float mx, RowState& row) {
+  float by = fmaxf(mx - row.m, 0.f);
+  if (keep && by <= kRaise) by = floorf(by);
+  const float m_new = row.m == -INFINITY ? mx : row.m + by, alpha = row.m == -INFINITY ? 1.f : ex2(-by);
   row.l = mul2(row.l, pack2(alpha, alpha));
   row.m = m_new;
   if (!first) {
@@ -554,6 +558,13 @@ __device__ __forceinline__ void raise(uint32_t s_addr, uint32_t o_addr, int writ
     }
     tmem_st8(s_addr + 8 * h, u);
   }
+}
+
+// l0 and l1 plus the halves of an fp16 pair.  (The denominator sums the probabilities as the product takes them: what rounding does to a dominating one is
+// then in both.  With the ones before the rounding the error of the outputs was up to twice as large; 1185 us and 1201 for 2048 new tokens behind 32768,
+// under 2 % elsewhere.  Converted first and added in pairs: 1271.)
+__device__ __forceinline__ void add_half2(float& l0, float& l1, uint32_t pair) {
+  asm("{\n\t.reg .f16 a, b;\n\tmov.b32 {a, b}, %2;\n\tadd.rn.f32.f16 %0, a, %0;\n\tadd.rn.f32.f16 %1, b, %1;\n\t}" : "+f"(l0), "+f"(l1) : "r"(pair));
 }
 
 // One tile of one slot's softmax, in one pass: the thread's row of S (128 fp32 at s_addr) becomes P (fp16 pairs over the first 64 of those columns), 32
@@ -584,24 +595,24 @@ __device__ __forceinline__ void softmax_tile(uint32_t s_addr, uint32_t o_addr, i
         mx4[(i >> 1) & 3] = fmaxf(fmaxf(mx4[(i >> 1) & 3], __uint_as_float(u[i])), __uint_as_float(u[i + 1]));
       }
       const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * scale_log2e;
-      if (__any_sync(0xffffffffu, mx > row.m + kRaise)) raise(s_addr, o_addr, h, first, mx, row);
+      if (__any_sync(0xffffffffu, mx > row.m + kRaise)) raise(s_addr, o_addr, h, 2 * h > h0, first, mx, row);
       const float ref = row.m == -INFINITY ? 0.f : row.m - kShift;      // a row that has seen no key yet: all its logits are -inf, its P is 0
       const uint64_t ref2 = pack2(-ref, -ref);
+      float l0 = 0.f, l1 = 0.f;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         uint32_t wd[8];
-        uint64_t l2 = 0ull;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           float x0, x1;
           unpack2(fma2(pack2u(u[16 * k + 2 * i], u[16 * k + 2 * i + 1]), scale2, ref2), x0, x1);
           const float p0 = ex2(x0), p1 = ex2(x1);
-          l2 = add2(l2, pack2(p0, p1));
           wd[i] = pack_half2(p0, p1);
+          add_half2(l0, l1, wd[i]);
         }
-        row.l = add2(row.l, l2);
         tmem_st8(s_addr + 32 * h + 8 * k, wd);
       }
+      row.l = add2(row.l, pack2(l0, l1));
     } else {
       const uint32_t zero[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
       tmem_st8(s_addr + 32 * h, zero);

@@ -38,15 +38,17 @@ def attend(K, V, q, scale, sees):
 def allowed(p, s, K, V, q, scale, deepest=516):
     """What the kernel's roundings may add, per output element.
 
-    Probabilities are fp16, each rounded by at most HALF_STEP of itself, independently: six standard deviations of HALF_STEP / sqrt(3) of the root of
-    sum (p v)^2; below 2^-19 of the row's reference by 2^-30 of the reference instead, which is no more than the row's denominator: 2^-30 sum |v|.
+    Probabilities are fp16, each rounded by at most HALF_STEP of itself, independently, in the product and in the denominator alike: six standard
+    deviations of HALF_STEP / sqrt(3) of the root of sum (p (v - o))^2; below 2^-19 of the row's reference by 2^-30 of the reference instead, which is no
+    more than the row's denominator: 2^-30 sum |v - o|.
     Sums in the tensor core lose at most a unit of 2^-23 for each of a tile's eight steps and one more for its products, over 512 tiles at most (then they
     are set aside).  A logit is such a sum (one tile
     deep), scaled and subtracted in fp32, and its exponential is good to 2^-21; a relative error d of the probabilities moves the output by at most
     d sum p |v - o|, here d sum p |v| twice.  Merging and dividing: 2^-20.  Equal logits give equal powers of two, which fp16 holds."""
     V1, flat = V.abs(), (q == 0).all(-1, keepdim=True)
-    pv = p @ V1
-    rounding = 6 / 3 ** 0.5 * HALF_STEP * ((p * p) @ (V * V)).sqrt() + 2.0 ** -30 * V1.sum(0)
+    pv, o, p2 = p @ V1, p @ V, p * p
+    apart = (p2 @ (V * V) - 2 * o * (p2 @ V) + o * o * p2.sum(-1, keepdim=True)).clamp_min(0)
+    rounding = 6 / 3 ** 0.5 * HALF_STEP * apart.sqrt() + 2.0 ** -30 * (V1.sum(0) + V.shape[0] * o.abs())
     depth = ((q.abs() @ K.abs().T).amax(-1, keepdim=True)) * scale
     logit = 9 * 2.0 ** -23 * depth + 4 * 2.0 ** -23 * s.abs().amax(-1, keepdim=True) + 2.0 ** -21
     tiles = min(K.shape[0] / TILE + 4, deepest)
@@ -94,8 +96,9 @@ def simulated(K, V, q, scale, sees, lag=10.0, shift=5.0):
                     a = np.float32(np.exp2(m - mx))
                     m, l, o = mx, l * a, o * a
                 p = np.exp2(x[t:t + TILE] - (m if np.isfinite(m) else 0) + np.float32(shift)).astype(np.float32)
-                l += p.sum(dtype=np.float32)
-                o += (p.astype(np.float16).astype(np.float64) @ V[t:t + TILE].numpy()).astype(np.float32)
+                p = p.astype(np.float16)
+                l += p.astype(np.float32).sum(dtype=np.float32)
+                o += (p.astype(np.float64) @ V[t:t + TILE].numpy()).astype(np.float32)
             out[h, r] = torch.from_numpy(o / l).double()
     return out
 

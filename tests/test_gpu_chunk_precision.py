@@ -130,10 +130,11 @@ def test_relative_error_of_long_caches(binding, name, batch, tokens, preset, v_b
     cache.set_attention_kernel(1)
     ref = cache.decode_attention(0, new[2][:, :, 0].contiguous(), SCALE).double()
     assert cache.status() == 0
-    # Elements of keys and values and probabilities are rounded to fp16, by at most 2^-11 / sqrt(3) = 2.8e-4 in the root mean square.  A logit is a sum
-    # of 128 products of keys of about 1 and queries of about 1.9, scaled by 128^-1/2: 5.4e-4.  Together 6.7e-4 of an output that is itself such a sum.
-    # The tensor core's truncation, 3.5e-7 per tile, adds 1.8e-4 at most.
-    assert float((out - ref).norm() / ref.norm()) <= 8e-4
+    # Elements of keys and values and probabilities are rounded to fp16, by at most 2^-11 / sqrt(3) = 2.8e-4 in the root mean square, which would be 6.7e-4 of
+    # an output that is a sum of many.  Here one key dominates most rows: what its probability's rounding does is in the denominator too, and its
+    # value is a bf16 one or of few bits.  Half way between what that gives, 2.4e-5 to 5.6e-5, and what a denominator of unrounded probabilities
+    # gives with a reference that does not make the largest one a power of two, 17.6e-5 to 23.4e-5.
+    assert float((out - ref).norm() / ref.norm()) <= 12e-5
 
 
 @pytest.mark.parametrize("v_bits,preset", [(2, "P24"), (4, "P4BASE")])
@@ -179,7 +180,8 @@ def test_rows_beside_one_whose_maximum_rises(binding):
     x = q.double() @ k.double().transpose(-1, -2) * SCALE                            # the new tokens' logits are 0, as the 129th's
     w = x.exp()
     ref = (w[..., :32].sum(-1) / (w.sum(-1) + 1 + torch.arange(n, device="cuda")))[..., None].expand_as(out)
-    # one rounding of equal weights, and fp32: logits of up to 2 and their exponentials 2^-20, two tiles' sums 2^-18
-    share = ((out - ref).abs() / (ref * (2.0 ** -11 + 2.0 ** -17) + 2.0 ** -40))
+    # One rounding of equal weights: 2^-11 of the first quarter's in the product, 2^-11 of all in the denominator.  In fp32 logits of up to 2 and their
+    # exponentials 2^-20, two tiles' sums 2^-18.
+    share = ((out - ref).abs() / (ref * (2.0 ** -10 + 2.0 ** -17) + 2.0 ** -40))
     share[:, :, ::32] = 0                                                            # (there the weights are e^-22 of the others)
     assert float(share.max()) <= 1.0, float(share.max())
