@@ -514,13 +514,8 @@ __device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&u)[8]) {
 }
 // The state of a row's softmax: its reference (in the log2 domain) and the sum of its probabilities, two halves.
 struct RowState {
-  float m;
-  uint64_t l;
-  __device__ __forceinline__ float sum() const {
-    float a, b;
-    unpack2(l, a, b);
-    return a + b;
-  }
+  float m, l0, l1;
+  __device__ __forceinline__ float sum() const { return l0 + l1; }
 };
 
 // Raises the reference to mx if that is above it: what lies in tensor memory on the old one is rescaled, the sums at o_addr (unless they are the first tile's,
@@ -533,7 +528,8 @@ __device__ __forceinline__ void raise(uint32_t s_addr, uint32_t o_addr, int writ
   float by = fmaxf(mx - row.m, 0.f);
   if (keep && by <= kRaise) by = floorf(by);
   const float m_new = row.m == -INFINITY ? mx : row.m + by, alpha = row.m == -INFINITY ? 1.f : ex2(-by);
-  row.l = mul2(row.l, pack2(alpha, alpha));
+  row.l0 *= alpha;
+  row.l1 *= alpha;
   row.m = m_new;
   if (!first) {
 #pragma unroll 1
@@ -598,7 +594,6 @@ __device__ __forceinline__ void softmax_tile(uint32_t s_addr, uint32_t o_addr, i
       if (__any_sync(0xffffffffu, mx > row.m + kRaise)) raise(s_addr, o_addr, h, 2 * h > h0, first, mx, row);
       const float ref = row.m == -INFINITY ? 0.f : row.m - kShift;      // a row that has seen no key yet: all its logits are -inf, its P is 0
       const uint64_t ref2 = pack2(-ref, -ref);
-      float l0 = 0.f, l1 = 0.f;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         uint32_t wd[8];
@@ -608,11 +603,10 @@ __device__ __forceinline__ void softmax_tile(uint32_t s_addr, uint32_t o_addr, i
           unpack2(fma2(pack2u(u[16 * k + 2 * i], u[16 * k + 2 * i + 1]), scale2, ref2), x0, x1);
           const float p0 = ex2(x0), p1 = ex2(x1);
           wd[i] = pack_half2(p0, p1);
-          add_half2(l0, l1, wd[i]);
+          add_half2(row.l0, row.l1, wd[i]);
         }
         tmem_st8(s_addr + 32 * h + 8 * k, wd);
       }
-      row.l = add2(row.l, pack2(l0, l1));
     } else {
       const uint32_t zero[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
       tmem_st8(s_addr + 32 * h, zero);
@@ -1146,7 +1140,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attention_kernel(const __gr
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(kQFull));
-      RowState state{-INFINITY, 0ull};
+      RowState state{-INFINITY, 0.f, 0.f};
       bool ok = true;
       {
         const int dual = sg.dual, lg_copies = copies_of(), step = 2 - dual, j1 = sg.j1, packed_tiles = sg.packed_tiles, units = sg.units;
@@ -1419,28 +1413,25 @@ __global__ void __launch_bounds__(256, 3) chunk_merge_kernel(const __grid_consta
       reinterpret_cast<float4*>(oS[warp])[lane] = o;
       __syncthreads();
       if (sub == 0) {
-        const float4 first = o;
-        float top = M;
-        for (int w = 1; w < kWarps; ++w) top = fmaxf(top, mlS[warp + w].x);
-        const float f = weight_of(M, l, top);
-        lost = f == 0.f && l != 0.f;
-        l *= f;
-        o = f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
-#pragma unroll 1
-        for (int w = 1; w < kWarps; ++w) {
-          const float2 ml = mlS[warp + w];
-          const float fw = weight_of(ml.x, ml.y, top);
-          if (fw != 0.f) {
-            l = fmaf(fw, ml.y, l);
-            add_scaled(fw, reinterpret_cast<const float4*>(oS[warp + w])[lane], o);
-          }
-          lost = lost || (fw == 0.f && ml.y != 0.f);
+        // lane w: the weight of warp w's result
+        const float2 ml = lane < kWarps ? mlS[warp + lane] : make_float2(-INFINITY, 0.f);
+        float top = ml.x;
+#pragma unroll
+        for (int d = 1; d < kWarps; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        const float w = weight_of(ml.x, ml.y, top);
+        float sum = w * ml.y;
+#pragma unroll
+        for (int d = 1; d < kWarps; d *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        l = __shfl_sync(0xffffffffu, sum, 0);
+        o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) {
+          const float wi = __shfl_sync(0xffffffffu, w, i);
+          if (wi != 0.f) add_scaled(wi, reinterpret_cast<const float4*>(oS[warp + i])[lane], o);
         }
-        if (lost) {
-          add_not_finite(first, o);
+        if (__any_sync(0xffffffffu, w == 0.f && ml.y != 0.f))
 #pragma unroll 1
-          for (int w = 1; w < kWarps; ++w) add_not_finite(reinterpret_cast<const float4*>(oS[warp + w])[lane], o);
-        }
+          for (int i = 0; i < kWarps; ++i) add_not_finite(reinterpret_cast<const float4*>(oS[warp + i])[lane], o);
       }
     }
     if (exists && sub == 0) {
@@ -1505,10 +1496,12 @@ cudaError_t launch_chunk_attention(const LayerView& lv, ChunkArgs& a, int n_sms,
   if (e != cudaSuccess) return e;
   *launches = 1;
   if (a.ctas == 1) return cudaSuccess;
-  // An item with fewer results than rows: a warp per row, 16 rows per block.  Otherwise (one or two long sequences, few new tokens) the eight warps of a block share
-  // a row's results, a row per block.  The whole call, us, a warp / a block per row, results an item x rows: 148 x 1 46.7 / 27.5, 74 x 5 35.8 / 27.1,
-  // 37 x 7 55.2 / 51.9, 18 x 4 95.2 / 92.0, 6 x 4 94.0 / 94.0, 37 x 35 64.4 / 61.0; 18 x 35 62.5 / 65.5, 9 x 35 62.5 / 70.2, 18 x 256 95 / 145.
-  if (a.ctas >= a.rows_cap * items)
+  // A warp per row, 16 rows per block; or, for items of more results than a warp has in flight, the eight warps of a block share a row's results, a row per
+  // block: where the rows are no more than the results, or the blocks no more than run at a time.  The whole call, us, a warp / a block per row, results an
+  // item x rows: 148 x 1 46.4 / 27.3, 74 x 5 36.0 / 26.9, 37 x 7 55.5 / 51.7, 18 x 4 95.7 / 92.6, 37 x 35 64.8 / 60.7, 12 x 16 (one item) 19.1 / 15.6;
+  // 12 x 7 (eight items) 17.6 / 18.0, 18 x 35 63.2 / 65.4, 9 x 35 63.1 / 69.7, 18 x 256 95.7 / 143.6.
+  const bool few_rows = a.rows_cap * items <= a.ctas || (a.ctas - 1) * a.rows_cap <= 3 * n_sms;
+  if (a.ctas > 8 * items && few_rows)
     e = launch_dependent(chunk_merge_kernel<1>, dim3((unsigned)(a.ctas - 1), (unsigned)a.rows_cap), 256, 0, stream, lv, a, 1);
   else
     e = launch_dependent(chunk_merge_kernel<8>, dim3((unsigned)(a.ctas - 1), (unsigned)((a.rows_cap + 15) / 16)), 256, 0, stream, lv, a, 16);
