@@ -20,11 +20,11 @@
 // by 2^-11 of themselves, smaller ones by 2^-30 of the maximum.  The denominator sums P as it was rounded.  Sums, maxima, O are fp32.
 // (Without the factor weights below 2^-25 were zero in P: 16384 keys 17.4 nats below one with values of zero gave nothing.)
 //
-// What bounds it (B200).  Few rows, long caches: the making of the tiles.  A key tile of 128 x 128 takes about 6700 warp instructions, three fifths of them logic,
+// What bounds it (B200).  Few rows, long caches: the making of the tiles.  A key tile of 128 x 128 takes about 6900 warp instructions, three fifths of them logic,
 // fp16 operations and stores of codes; 56 % of the issue slots are taken, a tile every 2500 cycles (2900 with start and end).  Eight sequences of 32768 tokens,
-// 7b shape, 5 new tokens each: 104 us (the first version 225), 1.05 TB/s of the packed bytes.  Many rows: a slot's chain of
-// product, softmax (3400 cycles of 128 logits a thread beside the tiles' making) and product, 5000 cycles per tile of 256 rows: 2048 tokens behind 32768, 7b
-// shape, 1183 us = 0.84 PFLOP/s (2328 at first), the tensor pipe a third of the time.
+// 7b shape, 5 new tokens each: 105 us (the first version 225), 1.05 TB/s of the packed bytes.  Many rows: a slot's chain of
+// product, softmax (3400 cycles of 128 logits a thread beside the tiles' making) and product, 5100 cycles per tile of 256 rows: 2048 tokens behind 32768, 7b
+// shape, 1190 us = 0.83 PFLOP/s (2328 at first), the tensor pipe a third of the time.
 #include <algorithm>
 
 #include "chunk.cuh"
@@ -522,7 +522,7 @@ struct RowState {
 // which are not there yet) and the pieces of P before `written` at s_addr.  At mx itself the largest probability is a power of two, which fp16 holds: the
 // error of a decode-sized call over 8000 tokens is 2.7e-5 of the output's norm (6.4e-5 with references a whole number higher).  Only where the row has
 // pieces of P already (`keep`) and rises because another row of the warp does, by 2^kRaise at most, it rises by a whole number: another factor would
-// round those pieces twice more, up to 2.6 times 2^-11 in all.  (Such rows not raised: 1201 us and 1211 for 2048 new tokens behind 32768.)  The
+// round those pieces twice more, up to 2.6 times 2^-11 in all.  (Such rows not raised: 0.9 % longer for 2048 new tokens behind 32768.)  The
 // products before this tile are complete: S is behind them in the tensor core's order.
 __device__ __forceinline__ void raise(uint32_t s_addr, uint32_t o_addr, int written, bool keep, bool first, float mx, RowState& row) {
   float by = fmaxf(mx - row.m, 0.f);
@@ -557,7 +557,7 @@ __device__ __forceinline__ void raise(uint32_t s_addr, uint32_t o_addr, int writ
 }
 
 // l0 and l1 plus the halves of an fp16 pair.  (The denominator sums the probabilities as the product takes them: what rounding does to a dominating one is
-// then in both.  With the ones before the rounding the error of the outputs was up to twice as large; 1185 us and 1201 for 2048 new tokens behind 32768,
+// then in both.  With the ones before the rounding the error of the outputs was up to twice as large; 1185 us and 1193 for 2048 new tokens behind 32768,
 // under 2 % elsewhere.  Converted first and added in pairs: 1271.)
 __device__ __forceinline__ void add_half2(float& l0, float& l1, uint32_t pair) {
   asm("{\n\t.reg .f16 a, b;\n\tmov.b32 {a, b}, %2;\n\tadd.rn.f32.f16 %0, a, %0;\n\tadd.rn.f32.f16 %1, b, %1;\n\t}" : "+f"(l0), "+f"(l1) : "r"(pair));
