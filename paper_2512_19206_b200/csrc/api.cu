@@ -334,6 +334,31 @@ int append_run(mixkvq_cache* cache, int layer, int b0, int nb, const void* k_dev
   return rc;
 }
 
+// Appends n_tokens_host[b] tokens to sequence b (null: n_tokens_max to each).
+int append_tokens(mixkvq_cache* cache, int layer, const void* k_dev, const void* v_dev, const void* q_dev, int n_tokens_max, const int32_t* n_tokens_host,
+                  cudaStream_t st) {
+  if (!cache || !k_dev || !v_dev || !q_dev || layer < 0 || layer >= cache->cfg.n_layers || n_tokens_max < 1) return MIXKVQ_E_INVALID_ARG;
+  if (!aligned16(k_dev) || !aligned16(v_dev) || !aligned16(q_dev)) return MIXKVQ_E_ALIGNMENT;
+  const int B = cache->cfg.batch;
+  auto count = [&](int b) { return n_tokens_host ? n_tokens_host[b] : n_tokens_max; };
+  for (int b = 0; b < B; ++b) {
+    if (count(b) < 0 || count(b) > n_tokens_max) return MIXKVQ_E_INVALID_ARG;
+    if (tokens_held(cache, layer, b) + count(b) > cache->cfg.max_tokens) return MIXKVQ_E_CAPACITY;
+  }
+  // runs of neighbouring sequences with the same fill and the same number of new tokens go through the kernels together
+  // (a batch of equal lengths is one run)
+  for (int b0 = 0; b0 < B;) {
+    int b1 = b0 + 1;
+    while (b1 < B && count(b1) == count(b0) && same_fill(cache, layer, b0, b1)) ++b1;
+    if (count(b0) > 0) {
+      const int rc = append_run(cache, layer, b0, b1 - b0, k_dev, v_dev, q_dev, n_tokens_max, count(b0), false, st);
+      if (rc != MIXKVQ_OK) return rc;
+    }
+    b0 = b1;
+  }
+  return MIXKVQ_OK;
+}
+
 // Chunk attention whose arguments have been checked: up to kChunkMaxSeqs sequences per launch.
 int run_chunk(mixkvq_cache* cache, int layer, const void* k_dev, const void* v_dev, const void* q_dev, int n_tokens_max, const int32_t* n_tokens_host,
               void* out_dev, int out_type, float softmax_scale, void* scratch_dev, cudaStream_t st) {
@@ -616,34 +641,13 @@ int mixkvq_select_channels_raw(const void* q_dev, const void* k_dev, int batch, 
 
 int mixkvq_quantize_append(mixkvq_cache* cache, int layer, const void* k_dev, const void* v_dev, const void* q_dev,
                            int n_tokens, void* stream) {
-  if (!cache || n_tokens < 1) return MIXKVQ_E_INVALID_ARG;
-  std::vector<int32_t> counts((size_t)cache->cfg.batch, n_tokens);
-  return mixkvq_quantize_append_ragged(cache, layer, k_dev, v_dev, q_dev, n_tokens, counts.data(), stream);
+  return append_tokens(cache, layer, k_dev, v_dev, q_dev, n_tokens, nullptr, static_cast<cudaStream_t>(stream));
 }
 
 int mixkvq_quantize_append_ragged(mixkvq_cache* cache, int layer, const void* k_dev, const void* v_dev, const void* q_dev,
                                   int n_tokens_max, const int32_t* n_tokens_host, void* stream) {
-  if (!cache || !k_dev || !v_dev || !q_dev || !n_tokens_host || layer < 0 || layer >= cache->cfg.n_layers || n_tokens_max < 1)
-    return MIXKVQ_E_INVALID_ARG;
-  if (!aligned16(k_dev) || !aligned16(v_dev) || !aligned16(q_dev)) return MIXKVQ_E_ALIGNMENT;
-  const int B = cache->cfg.batch;
-  for (int b = 0; b < B; ++b) {
-    if (n_tokens_host[b] < 0 || n_tokens_host[b] > n_tokens_max) return MIXKVQ_E_INVALID_ARG;
-    if (tokens_held(cache, layer, b) + n_tokens_host[b] > cache->cfg.max_tokens) return MIXKVQ_E_CAPACITY;
-  }
-  // runs of neighbouring sequences with the same fill and the same number of new tokens go through the kernels together
-  // (a batch of equal lengths is one run)
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
-  for (int b0 = 0; b0 < B;) {
-    int b1 = b0 + 1;
-    while (b1 < B && n_tokens_host[b1] == n_tokens_host[b0] && same_fill(cache, layer, b0, b1)) ++b1;
-    if (n_tokens_host[b0] > 0) {
-      const int rc = append_run(cache, layer, b0, b1 - b0, k_dev, v_dev, q_dev, n_tokens_max, n_tokens_host[b0], false, st);
-      if (rc != MIXKVQ_OK) return rc;
-    }
-    b0 = b1;
-  }
-  return MIXKVQ_OK;
+  if (!n_tokens_host) return MIXKVQ_E_INVALID_ARG;
+  return append_tokens(cache, layer, k_dev, v_dev, q_dev, n_tokens_max, n_tokens_host, static_cast<cudaStream_t>(stream));
 }
 
 int mixkvq_decode_attention(mixkvq_cache* cache, int layer, const void* q_dev, float* out_dev, float softmax_scale,
@@ -746,8 +750,7 @@ int mixkvq_chunk_step(mixkvq_cache* cache, int layer, const void* k_dev, const v
   rc = run_chunk(cache, layer, k_dev, v_dev, q_dev, n_tokens_max, n_tokens_host, out_dev, out_type, softmax_scale, scratch_dev,
                  static_cast<cudaStream_t>(stream));
   if (rc != MIXKVQ_OK) return rc;
-  return n_tokens_host ? mixkvq_quantize_append_ragged(cache, layer, k_dev, v_dev, q_dev, n_tokens_max, n_tokens_host, stream)
-                       : mixkvq_quantize_append(cache, layer, k_dev, v_dev, q_dev, n_tokens_max, stream);
+  return append_tokens(cache, layer, k_dev, v_dev, q_dev, n_tokens_max, n_tokens_host, static_cast<cudaStream_t>(stream));
 }
 
 int mixkvq_rope_append(mixkvq_cache* cache, int layer, void* k_dev, const void* v_dev, void* q_dev, const float* cos_dev,
