@@ -24,7 +24,7 @@
 // fp16 operations and stores of codes; 56 % of the issue slots are taken, a tile every 2500 cycles (2900 with start and end).  Eight sequences of 32768 tokens,
 // 7b shape, 5 new tokens each: 105 us (the first version 225), 1.05 TB/s of the packed bytes.  Many rows: a slot's chain of
 // product, softmax (3400 cycles of 128 logits a thread beside the tiles' making) and product, 5100 cycles per tile of 256 rows: 2048 tokens behind 32768, 7b
-// shape, 1190 us = 0.83 PFLOP/s (2328 at first), the tensor pipe a third of the time.
+// shape, 1204 us = 0.82 PFLOP/s (2328 at first), the tensor pipe a third of the time.
 #include <algorithm>
 
 #include "chunk.cuh"
@@ -557,8 +557,9 @@ __device__ __forceinline__ void raise(uint32_t s_addr, uint32_t o_addr, int writ
 }
 
 // l0 and l1 plus the halves of an fp16 pair.  (The denominator sums the probabilities as the product takes them: what rounding does to a dominating one is
-// then in both.  With the ones before the rounding the error of the outputs was up to twice as large; 1185 us and 1193 for 2048 new tokens behind 32768,
-// under 2 % elsewhere.  Converted first and added in pairs: 1271.)
+// then in both.  With the ones before the rounding the error of the outputs was up to twice as large; 1185 us and 1204 for 2048 new tokens behind 32768,
+// under 2 % elsewhere.  Converted first and added in pairs: 1271.  A piece is summed by itself: the same 65000 probabilities one after the other made the
+// denominator wrong by up to 4.9e-4, and 32 of them are exact.)
 __device__ __forceinline__ void add_half2(float& l0, float& l1, uint32_t pair) {
   asm("{\n\t.reg .f16 a, b;\n\tmov.b32 {a, b}, %2;\n\tadd.rn.f32.f16 %0, a, %0;\n\tadd.rn.f32.f16 %1, b, %1;\n\t}" : "+f"(l0), "+f"(l1) : "r"(pair));
 }
@@ -594,6 +595,7 @@ __device__ __forceinline__ void softmax_tile(uint32_t s_addr, uint32_t o_addr, i
       if (__any_sync(0xffffffffu, mx > row.m + kRaise)) raise(s_addr, o_addr, h, 2 * h > h0, first, mx, row);
       const float ref = row.m == -INFINITY ? 0.f : row.m - kShift;      // a row that has seen no key yet: all its logits are -inf, its P is 0
       const uint64_t ref2 = pack2(-ref, -ref);
+      float l0 = 0.f, l1 = 0.f;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         uint32_t wd[8];
@@ -603,10 +605,12 @@ __device__ __forceinline__ void softmax_tile(uint32_t s_addr, uint32_t o_addr, i
           unpack2(fma2(pack2u(u[16 * k + 2 * i], u[16 * k + 2 * i + 1]), scale2, ref2), x0, x1);
           const float p0 = ex2(x0), p1 = ex2(x1);
           wd[i] = pack_half2(p0, p1);
-          add_half2(row.l0, row.l1, wd[i]);
+          add_half2(l0, l1, wd[i]);
         }
         tmem_st8(s_addr + 32 * h + 8 * k, wd);
       }
+      row.l0 += l0;
+      row.l1 += l1;
     } else {
       const uint32_t zero[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
       tmem_st8(s_addr + 32 * h, zero);

@@ -185,3 +185,27 @@ def test_rows_beside_one_whose_maximum_rises(binding):
     share = ((out - ref).abs() / (ref * (2.0 ** -10 + 2.0 ** -17) + 2.0 ** -40))
     share[:, :, ::32] = 0                                                            # (there the weights are e^-22 of the others)
     assert float(share.max()) <= 1.0, float(share.max())
+
+
+def test_denominator_of_many_equal_weights(binding):
+    """65000 keys of one weight that is no power of two, beside 32 of twice that: every fourth key's value is one, so that the tensor core's sums stay within 24
+    bits and only the denominator can be off.  148 items of all keys and 256 rows."""
+    B, Hkv, T, n, part = 37, 4, 65000, 256, 3250
+    cache = binding.Cache(binding.make_config(1, B, Hkv, Hkv, T))
+    v = torch.zeros((B, Hkv, T, 128), device="cuda", dtype=torch.bfloat16)
+    v[:, :, ::4] = 1.0
+    for t in range(0, T, part):
+        k = torch.zeros((B, Hkv, part, 128), device="cuda", dtype=torch.bfloat16)
+        if t == 0:
+            k[:, :, :32, 0] = 1.0                            # (a group without a range: exact)
+        cache.quantize_append(0, k, v[:, :, t:t + part].contiguous(), torch.ones_like(k))
+    q, new = (torch.zeros((B, Hkv, n, 128), device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    q[..., 0] = 7.8125                                       # e^-0.6905 of the largest: 16.042 in units of its 32nd part, 16.047 in fp16
+    out = cache.chunk_attention(0, new, new, q, SCALE).double()
+    assert cache.status() == 0
+    w = torch.full((T,), 1.0, dtype=torch.float64, device="cuda")
+    w[:32] = torch.tensor(7.8125 * SCALE, dtype=torch.float64).exp()
+    ref = (w[::4].sum() / (w.sum() + 1 + torch.arange(n, device="cuda")))[:, None].expand_as(out)
+    # the rounding of the weights, 3e-4, is in the sum and in the denominator; 64 of 65000 weights are not the others'.  fp32: 2^-18
+    share = ((out - ref).abs() / (ref * (2.0 ** -11 * 64 / 16000 + 2.0 ** -18))).max()
+    assert float(share) <= 1.0, float(share)
