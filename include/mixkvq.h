@@ -247,7 +247,7 @@ int mixkvq_prefill(mixkvq_cache* cache, int layer, const void* k_dev, const void
  * The fills and the counts are parameters of the launches: a captured call is replayed with those of its capture.
  * Numeric range: products are fp16 with fp32 accumulation, so |q|, |k|, |v| and dequantized elements must stay below 65504.  A dequantized element is
  * rounded once, by 2^-11 of itself; below 2^-14 elements round to fp16 subnormals (2^-25), and those of a group whose scale is below 2^-15 by up to 2^-20
- * (2-bit codes) or 2^-18 (4-bit).  A key's weight is rounded by up to 2^-11 of itself (below 2^-10 of the row's largest one up to three times
+ * (2-bit codes) or 2^-18 (4-bit).  A key's weight is rounded by up to 2^-11 of itself (below 2^-10 of the row's largest one up to twice
  * that) or 2^-30 of the largest, in the sum and in its denominator alike.  A NaN or an infinity among the new tokens reaches the rows that attend to
  * it and no others.
  * The tensor core's sums are truncated, not rounded: about 3.5e-7 of the output per 128 tokens held, in one direction, up to 1.8e-4; what a key adds

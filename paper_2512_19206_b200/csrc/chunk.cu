@@ -22,9 +22,9 @@
 //
 // What bounds it (B200).  Few rows, long caches: the making of the tiles.  A key tile of 128 x 128 takes about 6900 warp instructions, three fifths of them logic,
 // fp16 operations and stores of codes; 56 % of the issue slots are taken, a tile every 2500 cycles (2900 with start and end).  Eight sequences of 32768 tokens,
-// 7b shape, 5 new tokens each: 105 us (the first version 225), 1.05 TB/s of the packed bytes.  Many rows: a slot's chain of
+// 7b shape, 5 new tokens each: 104 us (the first version 225), 1.05 TB/s of the packed bytes.  Many rows: a slot's chain of
 // product, softmax (3400 cycles of 128 logits a thread beside the tiles' making) and product, 5100 cycles per tile of 256 rows: 2048 tokens behind 32768, 7b
-// shape, 1204 us = 0.82 PFLOP/s (2328 at first), the tensor pipe a third of the time.
+// shape, 1211 us = 0.82 PFLOP/s (2328 at first), the tensor pipe a third of the time.
 #include <algorithm>
 
 #include "chunk.cuh"
@@ -519,14 +519,14 @@ struct RowState {
 };
 
 // Raises the reference to mx if that is above it: what lies in tensor memory on the old one is rescaled, the sums at o_addr (unless they are the first tile's,
-// which are not there yet) and the pieces of P before `written` at s_addr.  At mx itself the largest probability is a power of two, which fp16 holds: the
+// which are not there yet) and the row's `written` pieces of P at s_addr.  At mx itself the largest probability is a power of two, which fp16 holds: the
 // error of a decode-sized call over 8000 tokens is 2.7e-5 of the output's norm (6.4e-5 with references a whole number higher).  Only where the row has
-// pieces of P already (`keep`) and rises because another row of the warp does, by 2^kRaise at most, it rises by a whole number: another factor would
-// round those pieces twice more, up to 2.6 times 2^-11 in all.  (Such rows not raised: 0.9 % longer for 2048 new tokens behind 32768.)  The
+// pieces of P already and rises because another row of the warp does, by 2^kRaise at most, it rises by a whole number: another factor would
+// round those pieces again, and weights of more than 2^-10.  (Such rows not raised: 0.9 % longer for 2048 new tokens behind 32768.)  The
 // products before this tile are complete: S is behind them in the tensor core's order.
-__device__ __forceinline__ void raise(uint32_t s_addr, uint32_t o_addr, int written, bool keep, bool first, float mx, RowState& row) {
+__device__ __forceinline__ void raise(uint32_t s_addr, uint32_t o_addr, int written, bool first, float mx, RowState& row) {
   float by = fmaxf(mx - row.m, 0.f);
-  if (keep && by <= kRaise) by = floorf(by);
+  if (written > 0 && by <= kRaise) by = floorf(by);
   const float m_new = row.m == -INFINITY ? mx : row.m + by, alpha = row.m == -INFINITY ? 1.f : ex2(-by);
   row.l0 *= alpha;
   row.l1 *= alpha;
@@ -541,7 +541,7 @@ __device__ __forceinline__ void raise(uint32_t s_addr, uint32_t o_addr, int writ
       tmem_st8(o_addr + d, u);
     }
   }
-  const __half2 a2 = __float2half2_rn(alpha);
+  // (in fp32: a factor of 2^-20 has four bits in fp16.  2048 new tokens behind 32768 1204 us with that, 1211.)
 #pragma unroll 1
   for (int h = 0; h < 4 * written; ++h) {
     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
@@ -549,8 +549,8 @@ __device__ __forceinline__ void raise(uint32_t s_addr, uint32_t o_addr, int writ
     tmem_ld8(s_addr + 8 * h, u);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const __half2 p = __hmul2(*reinterpret_cast<const __half2*>(&u[i]), a2);
-      u[i] = *reinterpret_cast<const uint32_t*>(&p);
+      const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&u[i]));
+      u[i] = pack_half2(p.x * alpha, p.y * alpha);
     }
     tmem_st8(s_addr + 8 * h, u);
   }
@@ -592,7 +592,7 @@ __device__ __forceinline__ void softmax_tile(uint32_t s_addr, uint32_t o_addr, i
         mx4[(i >> 1) & 3] = fmaxf(fmaxf(mx4[(i >> 1) & 3], __uint_as_float(u[i])), __uint_as_float(u[i + 1]));
       }
       const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * scale_log2e;
-      if (__any_sync(0xffffffffu, mx > row.m + kRaise)) raise(s_addr, o_addr, h, 2 * h > h0, first, mx, row);
+      if (__any_sync(0xffffffffu, mx > row.m + kRaise)) raise(s_addr, o_addr, 2 * h > h0 ? h : 0, first, mx, row);
       const float ref = row.m == -INFINITY ? 0.f : row.m - kShift;      // a row that has seen no key yet: all its logits are -inf, its P is 0
       const uint64_t ref2 = pack2(-ref, -ref);
       float l0 = 0.f, l1 = 0.f;

@@ -1,4 +1,6 @@
 """GPU tests of the chunk attention's precision over long segments: weights far below a row's largest one, sums over many tiles."""
+import math
+
 import pytest
 import torch
 
@@ -208,4 +210,29 @@ def test_denominator_of_many_equal_weights(binding):
     ref = (w[::4].sum() / (w.sum() + 1 + torch.arange(n, device="cuda")))[:, None].expand_as(out)
     # the rounding of the weights, 3e-4, is in the sum and in the denominator; 64 of 65000 weights are not the others'.  fp32: 2^-18
     share = ((out - ref).abs() / (ref * (2.0 ** -11 * 64 / 16000 + 2.0 ** -18))).max()
+    assert float(share) <= 1.0, float(share)
+
+
+@pytest.mark.parametrize("g,n", [(1, 140), (1, 70), (3, 90)])
+def test_weights_of_a_tile_whose_second_half_is_far_above(binding, g, n):
+    """A first half whose logits are 9 to 10 (in powers of two) above the ones before, which raises nothing, and a second half 11 to 12 above that: the first half's
+    probabilities are scaled by 2^-20 to 2^-22.  Only its keys have values.  148 items and more, so that a thread block has all their tiles."""
+    B, Hkv, T = 37, 4, 513
+    cache = binding.Cache(binding.make_config(1, B, Hkv * g, Hkv, T))
+    k, v = (torch.zeros((B, Hkv, T, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    for tile in (1, 2):                                       # (slots of few rows take turns at the tiles)
+        k[:, :, 128 * tile:128 * tile + 32, 1], k[:, :, 128 * tile + 64:128 * tile + 96, 1], v[:, :, 128 * tile:128 * tile + 32] = 0.90625, 2.0, 1.0
+    cache.quantize_append(0, k, v, torch.ones((B, Hkv * g, T, 128), dtype=torch.bfloat16, device="cuda"))
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    q = torch.zeros((B, Hkv * g, n, 128), dtype=torch.bfloat16, device="cuda")
+    q[..., 1] = (10 + torch.rand((B, Hkv * g, n), generator=gen, device="cuda")) / (SCALE * math.log2(math.e))
+    zero = torch.zeros((B, Hkv, n, 128), dtype=torch.bfloat16, device="cuda")
+    out = cache.chunk_attention(0, zero, zero, q, SCALE).double()
+    assert cache.status() == 0
+    x = q.double() @ k.double().repeat_interleave(g, 1).transpose(-1, -2) * SCALE
+    w = (x - x.amax(-1, keepdim=True)).exp()
+    new = (1 + torch.arange(n, device="cuda")) * (-x.amax(-1)).exp()
+    ref = ((w * v.double()[:, :, :, 0].repeat_interleave(g, 1)[:, :, None]).sum(-1) / (w.sum(-1) + new))[..., None].expand_as(out)
+    # two roundings of the weight, one more of all in the denominator; logits of 15 in fp32 2^-19, sums 2^-18
+    share = ((out - ref).abs() / (ref * (3 * 2.0 ** -11 + 2.0 ** -17))).max()
     assert float(share) <= 1.0, float(share)
