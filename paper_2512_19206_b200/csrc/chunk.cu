@@ -20,8 +20,8 @@
 // by 2^-11 of themselves, smaller ones by 2^-30 of the maximum.  The denominator sums P as it was rounded.  Sums, maxima, O are fp32.
 // (Without the factor weights below 2^-25 were zero in P: 16384 keys 17.4 nats below one with values of zero gave nothing.)
 //
-// What bounds it (B200).  Few rows, long caches: the making of the tiles.  A key tile of 128 x 128 takes about 6900 warp instructions, three fifths of them logic,
-// fp16 operations and stores of codes; 56 % of the issue slots are taken, a tile every 2500 cycles (2900 with start and end).  Eight sequences of 32768 tokens,
+// What bounds it (B200).  Few rows, long caches: the making of the tiles.  A key tile of 128 x 128 takes about 6850 warp instructions, three fifths of them logic,
+// fp16 operations and stores of codes; 57 % of the issue slots are taken, a tile every 2500 cycles (2900 with start and end).  Eight sequences of 32768 tokens,
 // 7b shape, 5 new tokens each: 104 us (the first version 225), 1.05 TB/s of the packed bytes.  Many rows: a slot's chain of
 // product, softmax (3400 cycles of 128 logits a thread beside the tiles' making) and product, 5100 cycles per tile of 256 rows: 2048 tokens behind 32768, 7b
 // shape, 1211 us = 0.82 PFLOP/s (2328 at first), the tensor pipe a third of the time.
