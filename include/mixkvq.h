@@ -57,7 +57,11 @@ enum {
                                          channels then read as 0 and its UINT4 channels lose their high plane, so the
                                          layer's attention is wrong from that block on, until the cache is reset
                                          (with a larger extras_budget_bytes).  Earlier blocks are unaffected            */
-  MIXKVQ_DEV_BAD_POSITION = 4,        /* a rotation with several axes met a coordinate beyond the tables: that token's rows were left alone */
+  MIXKVQ_DEV_BAD_POSITION = 4,        /* a rotation with several axes, of part of the head or of a paged append met a position beyond the tables: that
+                                         token's rows were left alone (and it was not appended) */
+  MIXKVQ_DEV_BAD_LENGTH = 8,          /* paged cache: a length or a count of a call was negative or beyond the page table or the call's tokens: it
+                                         was taken as the nearest that is possible, and a token that has no place was left out */
+  MIXKVQ_DEV_BAD_PAGE = 16,           /* paged cache: a page that a call needed is none of the pool's: its tokens were left out */
   MIXKVQ_DEV_COPY_TIMEOUT = 2         /* a bounded wait (for a staged bulk copy, or for the partner warp of a pair) ran out:
                                          the warps concerned contributed nothing to that call's output, which is
                                          therefore wrong (0 where no warp contributed); later calls are unaffected    */
@@ -309,6 +313,105 @@ int mixkvq_rope_axes_append(mixkvq_cache* cache, int layer, void* k_dev, const v
 int mixkvq_rope_axes_decode_step(mixkvq_cache* cache, int layer, void* k_dev, const void* v_dev, void* q_dev, const float* cos_dev, const float* sin_dev,
                                  int n_positions, const int32_t* positions_dev, int n_axes, const uint8_t* axis_of_pair_host, float* out_dev,
                                  float softmax_scale, void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* Rotary positions of part of the head.  Channels 0 .. rotary_dim - 1 of a row turn, the others stay: pairs (i, i + rotary_dim / 2), or (2 i, 2 i + 1) where
+ * `interleaved` is 1.  Tables as mixkvq_rope_tables makes them: float [n_positions, rotary_dim / 2], 16-byte aligned.  Arithmetic as for mixkvq_rope_append:
+ * y0 = x0 c - x1 s, y1 = x1 c + x0 s, every product and the sum one fp32 operation rounded to nearest, the result rounded to bf16. */
+typedef struct mixkvq_rotation {
+  const float *cos_dev, *sin_dev;
+  const int32_t* positions_dev;       /* [B, n] int32, DEVICE: the table row of every token */
+  int32_t n_positions;                /* rows of the tables */
+  int32_t rotary_dim;                 /* a multiple of 16 up to 128 */
+  int32_t interleaved;
+  int32_t reserved;
+} mixkvq_rotation;
+/* Rotates q_dev, k_dev (and copies v_dev; NULL with v_out_dev NULL: left out) from any layout whose last dimension is contiguous into the head-major
+ * q_out_dev [B, Hq, n, 128], k_out_dev, v_out_dev [B, Hkv, n, 128] that the append, prefill and chunk calls take.  Strides, overlaps, tokens with a negative
+ * position (none: their rows of the outputs are left alone) and with one beyond the tables (MIXKVQ_DEV_BAD_POSITION) as for mixkvq_rope_axes. */
+int mixkvq_rope_partial(mixkvq_cache* cache, const void* q_dev, const void* k_dev, const void* v_dev, const int64_t* strides_host, int n_tokens,
+                        const mixkvq_rotation* rotation, void* q_out_dev, void* k_out_dev, void* v_out_dev, void* stream);
+
+/* The tables of a rotation: entry [p - start][i] is m cos(p f_i) and m sin(p f_i) for p = start .. start + n_positions - 1, f_i the frequency of channel pair i,
+ * d = rotary_dim, computed in 64 bits and rounded to float once.  Frequencies base^(-2 i / d), and for contexts beyond the one trained on:
+ *   PLAIN   as they are
+ *   LINEAR  divided by factor
+ *   NTK     base * factor^(d / (d - 2)) for base: the lowest is divided by factor, the highest stays
+ *   BANDS   those with at least `high` turns in `original` positions stay, those with at most `low` are divided by factor, between them a linear mix
+ *   YARN    the same with the mix linear in i, between the pairs (rounded outwards) that turn `high` and `low` times in `original` positions; m = 0.1 ln factor + 1
+ * attention_factor: m; 0: the kind's own (1 but for YARN with a factor above 1).  Stateless, enqueued on the current device. */
+enum { MIXKVQ_ROPE_PLAIN = 0, MIXKVQ_ROPE_LINEAR = 1, MIXKVQ_ROPE_NTK = 2, MIXKVQ_ROPE_BANDS = 3, MIXKVQ_ROPE_YARN = 4 };
+typedef struct mixkvq_rope_scaling {
+  int32_t kind, rotary_dim;           /* rotary_dim: a multiple of 16 up to 128 */
+  double base, factor, original, low, high, attention_factor;
+  int32_t reserved;                   /* must be 0 */
+} mixkvq_rope_scaling;
+int mixkvq_rope_tables(const mixkvq_rope_scaling* scaling, int64_t start, int n_positions, float* cos_dev, float* sin_dev, void* stream);
+
+/* ---- A cache held in 4 bits, in pages (no counterpart in the paper but its uniform 4-bit baseline): for servers that give sequences memory page by page, share
+ * pages between them and capture their steps into graphs.  Keys and values are both quantized token by token when they come (Eq. 2 with 16 levels,
+ * groups of G channels of one token, scale and zero-point bf16 as everywhere: reading of the stored scale included), so there is no window, no flush and no
+ * state but the pages.  Which pages belong to a sequence and how many tokens it has is the caller's, in DEVICE memory: nothing about a call but its shape is
+ * known to the host.
+ *
+ * Pool: `n_layers` times `n_pages` pages of page_tokens tokens of all KV heads, behind a header of 256 bytes with the status word; page p of a layer is one contiguous piece
+ * of Hkv * page_tokens * (128 + 1024 / G) bytes.  A page has the same number in all layers. */
+typedef struct mixkvq_paged_config {
+  int32_t n_layers, n_q_heads, n_kv_heads;   /* Hq a multiple of Hkv, Hq / Hkv <= 8 */
+  int32_t head_dim;                   /* must be 128 */
+  int32_t n_pages;                    /* per layer */
+  int32_t page_tokens;                /* 16, 32, 64, 128 or 256 */
+  int32_t group_size;                 /* G: 32, 64 or 128 */
+  int32_t reserved;                   /* must be 0 */
+} mixkvq_paged_config;
+typedef struct mixkvq_paged mixkvq_paged;
+
+/* The sequences of a call.  Token t of sequence b lies on page pages_dev[b * pages_stride + t / page_tokens], slot t % page_tokens.  Pages beyond those that a call's tokens need
+ * are not looked at.  Lengths and counts that are impossible set MIXKVQ_DEV_BAD_LENGTH, pages that are none MIXKVQ_DEV_BAD_PAGE (see there). */
+typedef struct mixkvq_paged_sequences {
+  int32_t batch;                      /* B */
+  int32_t n_tokens;                   /* n: tokens of the call per sequence, at most */
+  const int32_t* pages_dev;           /* [B, max_pages] int32, rows pages_stride apart */
+  int32_t max_pages, pages_stride;    /* max_pages * page_tokens <= MIXKVQ_PAGED_MAX_TOKENS */
+  const int32_t* lens_dev;            /* [B] int32: tokens of each sequence (what each call says) */
+  const int32_t* counts_dev;          /* [B] int32 or NULL (n each): tokens of the call in each sequence, its first rows of the tensors */
+} mixkvq_paged_sequences;
+#define MIXKVQ_PAGED_MAX_TOKENS (1 << 28)
+#define MIXKVQ_PAGED_MAX_BATCH 4096
+
+int mixkvq_paged_bytes(const mixkvq_paged_config* cfg, size_t* pool_bytes);
+/* Workspace of an attention call of this batch and number of tokens.  Contents are scratch and need not be anything; two calls that may overlap on the GPU
+ * need one each, two captured graphs too unless they never run at the same time. */
+size_t mixkvq_paged_workspace_bytes(const mixkvq_paged_config* cfg, int batch, int n_tokens);
+/* The handle over caller-owned memory (256-byte aligned); the pages are left as they are, the status word is cleared on `stream`. */
+int mixkvq_paged_init(const mixkvq_paged_config* cfg, void* pool_dev, size_t bytes, void* stream, mixkvq_paged** out);
+int mixkvq_paged_destroy(mixkvq_paged* cache);
+
+/* Stores tokens: token i < counts[b] of sequence b becomes token lens[b] + i of the sequence (lens: tokens before the call).
+ *   k_dev, v_dev [B, Hkv, n, 128], q_dev [B, Hq, n, 128] bf16 with strides_host [9] (q, k, v: batch, head, token; NULL: head-major) as for mixkvq_rope_axes.
+ *   rotation: NULL (keys are stored as they are), or keys and queries turn on the way; its positions_dev may be NULL: a token turns by its place in
+ *   its sequence.  A token with a negative position is none.
+ *   q_dev, q_out_dev: both NULL, or the queries and where they go, rotated, head-major; q_out_dev may be q_dev itself where that is head-major.
+ * Rows of q_out_dev behind a sequence's count are left as they are.  Two tokens of a call in the same slot (a page used twice) leave either. */
+int mixkvq_paged_append(mixkvq_paged* cache, int layer, const mixkvq_paged_sequences* seqs, const void* k_dev, const void* v_dev, const void* q_dev,
+                        const int64_t* strides_host, const mixkvq_rotation* rotation, void* q_out_dev, void* stream);
+/* The values that tokens lens[b] .. lens[b] + counts[b] - 1 of every sequence are held as (Eq. 3, rounded to bf16): k_out_dev, v_out_dev [B, Hkv, n, 128] bf16.  Other rows
+ * are left as they are. */
+int mixkvq_paged_read(mixkvq_paged* cache, int layer, const mixkvq_paged_sequences* seqs, void* k_out_dev, void* v_out_dev, void* stream);
+/* Eq. 1 over the pages: the newest counts[b] tokens of sequence b, which has lens[b] tokens, these included; query row i sees tokens 0 .. lens[b] - counts[b] + i.
+ *   q_dev [B, Hq, n, 128] bf16 (rotated), out_dev [B, Hq, n, 128] of out_type (MIXKVQ_OUT_*), rounded once.
+ * A row that sees no token is zeros; rows behind a sequence's count are left as they are.  Nothing is read of tokens that no row sees: freed pages and the rest of a last
+ * page may hold anything.  softmax_scale > 0 and finite. */
+int mixkvq_paged_attention(mixkvq_paged* cache, int layer, const mixkvq_paged_sequences* seqs, const void* q_dev, void* out_dev, int out_type, float softmax_scale,
+                           void* workspace_dev, size_t workspace_bytes, void* stream);
+/* mixkvq_paged_append, then mixkvq_paged_attention of the tokens appended: a decode step, or a chunk of a prompt.  lens: tokens before the call. */
+int mixkvq_paged_step(mixkvq_paged* cache, int layer, const mixkvq_paged_sequences* seqs, const void* k_dev, const void* v_dev, const void* q_dev,
+                      const int64_t* strides_host, const mixkvq_rotation* rotation, void* q_out_dev, void* out_dev, int out_type, float softmax_scale,
+                      void* workspace_dev, size_t workspace_bytes, void* stream);
+/* As their counterparts of mixkvq_cache; the status word stays until it is cleared. */
+int mixkvq_paged_test_arm_copy_timeout(mixkvq_paged* cache, uint32_t extra_bytes, uint32_t max_polls);
+int mixkvq_paged_query_status(mixkvq_paged* cache, int* device_status, void* stream);
+int mixkvq_paged_clear_status(mixkvq_paged* cache, void* stream);
+uint64_t mixkvq_paged_launch_count(const mixkvq_paged* cache);
 
 /* (The paper has no counterpart of this entry point; it exists for integration reasons only.)
  * Same computation and same results as mixkvq_decode_attention, for callers that have no way to hand

@@ -22,9 +22,12 @@ EXPORTS = [
     "mixkvq_decode_attention", "mixkvq_decode_attention_noalloc", "mixkvq_decode_step", "mixkvq_set_attention_kernel", "mixkvq_query_status",
     "mixkvq_cache_describe", "mixkvq_last_attention", "mixkvq_last_attention_ctas", "mixkvq_launch_count", "mixkvq_status_string",
     "mixkvq_cache_written_externally", "mixkvq_test_arm_copy_timeout", "mixkvq_test_arm_value_copy_timeout", "mixkvq_rope_append", "mixkvq_rope_decode_step", "mixkvq_prefill", "mixkvq_prefill_scratch_bytes", "mixkvq_chunk_attention", "mixkvq_chunk_step", "mixkvq_chunk_scratch_bytes", "mixkvq_rope_axes", "mixkvq_rope_axes_append", "mixkvq_rope_axes_decode_step", "mixkvq_quantize_append_ragged", "mixkvq_sequence_fill", "mixkvq_decode_attention_partial", "mixkvq_merge_partials",
+    "mixkvq_rope_partial", "mixkvq_rope_tables", "mixkvq_paged_bytes", "mixkvq_paged_workspace_bytes", "mixkvq_paged_init", "mixkvq_paged_destroy",
+    "mixkvq_paged_append", "mixkvq_paged_read", "mixkvq_paged_attention", "mixkvq_paged_step", "mixkvq_paged_test_arm_copy_timeout",
+    "mixkvq_paged_query_status", "mixkvq_paged_clear_status", "mixkvq_paged_launch_count",
 ]
 
-DEV_EXTRAS_FULL, DEV_COPY_TIMEOUT, DEV_BAD_POSITION = 1, 2, 4
+DEV_EXTRAS_FULL, DEV_COPY_TIMEOUT, DEV_BAD_POSITION, DEV_BAD_LENGTH, DEV_BAD_PAGE = 1, 2, 4, 8, 16
 _OUT_TYPES = {torch.float32: 0, torch.bfloat16: 1}
 ATTN_ONE_UNIT, ATTN_TWO_UNITS, ATTN_DIRECT, ATTN_EARLY, ATTN_OTHER, ATTN_EIGHT_PAIRS = 1, 2, 4, 8, 16, 32
 
@@ -45,6 +48,28 @@ class LayoutDesc(C.Structure):
         "resv_off", "resv_stride", "base_off", "base_stride", "extras_off", "extras_stride", "base_bytes")] + [
         (n, C.c_uint32) for n in ("max_blocks", "n_streams", "n_blocks", "residual_tokens")] + [
         ("sink_off", C.c_uint64), ("sink_stride", C.c_uint64), ("sink_tokens", C.c_uint32), ("sink_len", C.c_uint32)]
+
+
+class PagedConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_layers", "n_q_heads", "n_kv_heads", "head_dim", "n_pages", "page_tokens", "group_size", "reserved")]
+
+
+class Sequences(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("n_tokens", C.c_int32), ("pages_dev", C.c_void_p), ("max_pages", C.c_int32), ("pages_stride", C.c_int32),
+                ("lens_dev", C.c_void_p), ("counts_dev", C.c_void_p)]
+
+
+class Rotation(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("cos_dev", "sin_dev", "positions_dev")] + [
+        (n, C.c_int32) for n in ("n_positions", "rotary_dim", "interleaved", "reserved")]
+
+
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "bands": 3, "yarn": 4}
+
+
+class RopeScaling(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("rotary_dim", C.c_int32)] + [
+        (n, C.c_double) for n in ("base", "factor", "original", "low", "high", "attention_factor")] + [("reserved", C.c_int32)]
 
 
 class MixKVQError(RuntimeError):
@@ -98,10 +123,27 @@ def lib():
         L.mixkvq_cache_describe.argtypes = [vp, i32, C.POINTER(LayoutDesc)]
         L.mixkvq_launch_count.argtypes = L.mixkvq_last_attention.argtypes = L.mixkvq_last_attention_ctas.argtypes = [vp]
         L.mixkvq_launch_count.restype = u64
+        rot, seqs = C.POINTER(Rotation), C.POINTER(Sequences)
+        L.mixkvq_rope_partial.argtypes = [vp, vp, vp, vp, i64s, i32, rot, vp, vp, vp, vp]
+        L.mixkvq_rope_tables.argtypes = [C.POINTER(RopeScaling), C.c_int64, i32, vp, vp, vp]
+        L.mixkvq_paged_bytes.argtypes = [C.POINTER(PagedConfig), C.POINTER(C.c_size_t)]
+        L.mixkvq_paged_workspace_bytes.argtypes = [C.POINTER(PagedConfig), i32, i32]
+        L.mixkvq_paged_init.argtypes = [C.POINTER(PagedConfig), vp, C.c_size_t, vp, C.POINTER(vp)]
+        L.mixkvq_paged_destroy.argtypes = L.mixkvq_paged_launch_count.argtypes = [vp]
+        L.mixkvq_paged_append.argtypes = [vp, i32, seqs, vp, vp, vp, i64s, rot, vp, vp]
+        L.mixkvq_paged_read.argtypes = [vp, i32, seqs, vp, vp, vp]
+        L.mixkvq_paged_attention.argtypes = [vp, i32, seqs, vp, vp, i32, f32, vp, C.c_size_t, vp]
+        L.mixkvq_paged_step.argtypes = [vp, i32, seqs, vp, vp, vp, i64s, rot, vp, vp, i32, f32, vp, C.c_size_t, vp]
+        L.mixkvq_paged_test_arm_copy_timeout.argtypes = [vp, C.c_uint32, C.c_uint32]
+        L.mixkvq_paged_query_status.argtypes = [vp, C.POINTER(i32), vp]
+        L.mixkvq_paged_clear_status.argtypes = [vp, vp]
+        L.mixkvq_paged_workspace_bytes.restype = C.c_size_t
+        L.mixkvq_paged_launch_count.restype = u64
         L.mixkvq_status_string.argtypes = [i32]
         L.mixkvq_status_string.restype = C.c_char_p
         for name in EXPORTS:
-            if name not in ("mixkvq_launch_count", "mixkvq_status_string", "mixkvq_prefill_scratch_bytes", "mixkvq_chunk_scratch_bytes"):
+            if name not in ("mixkvq_launch_count", "mixkvq_status_string", "mixkvq_prefill_scratch_bytes", "mixkvq_chunk_scratch_bytes",
+                            "mixkvq_paged_workspace_bytes", "mixkvq_paged_launch_count"):
                 getattr(L, name).restype = i32
         _lib = L
     return _lib
@@ -208,6 +250,45 @@ def axis_sections(sections, interleaved=False):
                 pairs.append(a)
                 left[a] -= 1
     return pairs
+
+
+def rope_tables(n_positions, rotary_dim=128, base=10000.0, scaling="none", factor=1.0, original=0, low=1.0, high=4.0, fast=32.0, slow=1.0,
+                attention_factor=None, start=0, device="cuda", out=None):
+    """cos and sin of positions start .. start + n_positions - 1, float32 [n_positions, rotary_dim / 2] each (`out`: two such tensors to write), as the
+    rotations take them.  `scaling` of the frequencies base ** (-2 i / rotary_dim): "none"; "linear" (divided by `factor`); "ntk" (the base grows, so that the lowest is);
+    "bands" (those with at most `low` turns in `original` positions are, those with at least `high` stay, a mix between); "yarn" (a mix along the pairs, from the
+    one with `fast` turns to the one with `slow`, and the entries times `attention_factor`, 0.1 ln(factor) + 1 when absent)."""
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"rope_tables: the scaling is one of {', '.join(ROPE_SCALINGS)}, not {scaling!r}")
+    if attention_factor is not None and not attention_factor > 0:
+        raise ValueError("rope_tables: the attention factor is positive")
+    n_positions, rotary_dim, start = int(n_positions), int(rotary_dim), int(start)
+    shape = (n_positions, rotary_dim // 2)
+    if out is None:
+        if n_positions < 1 or rotary_dim < 2:
+            raise ValueError("rope_tables: at least one position and two channels are needed")
+        out = tuple(torch.empty(shape, dtype=torch.float32, device=device) for _ in range(2))
+    cos, sin = out
+    for t in out:
+        if t.dtype != torch.float32 or t.shape != shape or not t.is_contiguous() or not t.is_cuda or t.device != cos.device:
+            raise ValueError(f"rope_tables: the outputs must be contiguous float32 {list(shape)} CUDA tensors on one device")
+    lo, hi = (slow, fast) if scaling == "yarn" else (low, high)
+    how = RopeScaling(ROPE_SCALINGS[scaling], rotary_dim, base, factor, original, lo, hi, attention_factor or 0.0, 0)
+    with _device_of(cos.device):
+        _check(lib().mixkvq_rope_tables(C.byref(how), start, n_positions, _ptr(cos), _ptr(sin), _stream()), "mixkvq_rope_tables")
+    return out
+
+
+def _rotation(name, cos, sin, positions, interleaved, shape, dev):
+    """The arguments that say what a rotation of part of the head turns by."""
+    if cos.dtype != torch.float32 or sin.dtype != torch.float32 or cos.dim() != 2 or cos.shape != sin.shape:
+        raise ValueError(f"{name}: cos and sin must be float32 tables [n_positions, rotary_dim / 2]")
+    if positions is not None and (positions.dtype != torch.int32 or positions.shape != shape):
+        raise ValueError(f"{name}: positions must be int32 {list(shape)}")
+    for t in (cos, sin) if positions is None else (cos, sin, positions):
+        if not t.is_contiguous() or t.device != dev:
+            raise ValueError(f"{name}: cos, sin and positions must be contiguous tensors on {dev}")
+    return (cos.data_ptr(), sin.data_ptr(), cos.shape[0], None if positions is None else positions.data_ptr(), 2 * cos.shape[1], int(bool(interleaved)))
 
 
 class Cache:
@@ -413,6 +494,39 @@ class Cache:
             raise MixKVQError(code, "mixkvq_rope_axes")
         return out
 
+    def rope_partial(self, q, k, v, cos, sin, positions, interleaved=False, out=None):
+        """Rotates the first channels of q [B,Hq,n,128] and k [B,Hkv,n,128] (twice as many as cos, sin float32 [n_positions, pairs] have columns) by positions int32
+        [B,n] (negative: no token, its rows are left alone): pairs (i, i + half), or neighbours where `interleaved`.  Layouts, v and `out` as in rope_axes."""
+        cfg, dev, n = self.cfg, self.mem.device, q.shape[2] if q.dim() == 4 else 0
+        turn = _rotation("rope_partial", cos, sin, positions, interleaved, (cfg.batch, n), dev)
+        ins = (q, k, v)
+        if out is None:
+            out = tuple(None if t is None else torch.zeros(t.shape, dtype=torch.bfloat16, device=dev) for t in ins)
+        strides, ptrs, outs = [], [], []
+        for i, (t, o, heads) in enumerate(zip(ins, out, (cfg.n_q_heads, cfg.n_kv_heads, cfg.n_kv_heads))):
+            if i == 2 and t is None and o is None:
+                strides += (0, 0, 0)
+                ptrs.append(None)
+                outs.append(None)
+                continue
+            if t is None or o is None:
+                raise ValueError("rope_partial: an input and its output come together")
+            shape = (cfg.batch, heads, n, 128)
+            if t.shape != shape or o.shape != shape or t.dtype != torch.bfloat16 or o.dtype != torch.bfloat16 or t.device != dev or o.device != dev:
+                raise ValueError(f"rope_partial: {'qkv'[i]} and its output must be bfloat16 {list(shape)} tensors on {dev}")
+            s = t.stride()
+            if s[3] != 1 or not o.is_contiguous():
+                raise ValueError("rope_partial: the inputs' last dimension and the outputs must be contiguous")
+            strides += s[:3]
+            ptrs.append(t.data_ptr())
+            outs.append(o.data_ptr())
+        call = (_native or _calls()).rope_partial
+        with _device_of(dev):
+            code = call(self.handle.value, *ptrs, strides, n, *turn, *outs, _stream())
+        if code:
+            raise MixKVQError(code, "mixkvq_rope_partial")
+        return out
+
     def _head_major(self, name, n, **tensors):
         cfg, dev = self.cfg, self.mem.device
         for what, t in tensors.items():
@@ -519,3 +633,172 @@ class Cache:
             "sinkK": cut(d.sink_off, d.sink_stride, n_sink * 256),
             "sinkV": cut(d.sink_off + d.sink_len * 256, d.sink_stride, n_sink * 256),
         }
+
+
+def make_paged_config(n_layers, n_q_heads, n_kv_heads, n_pages, page_tokens=64, group_size=32) -> PagedConfig:
+    return PagedConfig(n_layers, n_q_heads, n_kv_heads, 128, n_pages, page_tokens, group_size, 0)
+
+
+class PagedCache:
+    """A cache held in 4 bits, in pages: owns the pool (a torch uint8 tensor) and the library's host handle.
+
+    Which pages a sequence has and how many tokens are the caller's tensors on the device: `pages` int32 [B, most pages of a sequence], `lens` int32 [B], and where the
+    sequences of a call take part with unequal numbers of tokens `counts` int32 [B].  Nothing of a call but its shapes comes from the host, so that a
+    captured call is replayed with what these tensors hold then."""
+
+    def __init__(self, cfg: PagedConfig, device="cuda"):
+        self.cfg = cfg
+        n = C.c_size_t()
+        _check(lib().mixkvq_paged_bytes(C.byref(cfg), C.byref(n)), "mixkvq_paged_bytes")
+        self.mem = torch.empty(n.value, dtype=torch.uint8, device=device)
+        self.handle = C.c_void_p()
+        with torch.cuda.device(self.mem.device):
+            _check(lib().mixkvq_paged_init(C.byref(cfg), _ptr(self.mem), n.value, _stream(), C.byref(self.handle)), "mixkvq_paged_init")
+
+    def close(self):
+        if self.handle:
+            lib().mixkvq_paged_destroy(self.handle)
+            self.handle = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _sequences(self, name, n, pages, lens, counts):
+        dev = self.mem.device
+        if pages.dtype != torch.int32 or pages.dim() != 2 or pages.stride(1) != 1 or pages.device != dev or pages.shape[1] < 1:
+            raise ValueError(f"{name}: pages must be an int32 [B, pages] tensor on {dev} whose rows are contiguous")
+        B = pages.shape[0]
+        for t, what in ((lens, "lens"), (counts, "counts")):
+            if t is None and what == "counts":
+                continue
+            if t.dtype != torch.int32 or t.shape != (B,) or not t.is_contiguous() or t.device != dev:
+                raise ValueError(f"{name}: {what} must be a contiguous int32 [{B}] tensor on {dev}")
+        stride = pages.stride(0) if B > 1 else pages.shape[1]
+        return (B, n, pages.data_ptr(), pages.shape[1], stride, lens.data_ptr(), None if counts is None else counts.data_ptr())
+
+    def _rows(self, name, B, n, **tensors):
+        """Checks rows [B, heads, n, 128] in bf16 of any layout with a contiguous last dimension; the strides and addresses of q, k and v."""
+        cfg, dev, strides = self.cfg, self.mem.device, []
+        for what, t in tensors.items():
+            if t is None:
+                strides += (0, 0, 0)
+                continue
+            shape = (B, cfg.n_q_heads if what == "q" else cfg.n_kv_heads, n, 128)
+            if t.shape != shape or t.dtype != torch.bfloat16 or t.device != dev or t.stride(3) != 1:
+                raise ValueError(f"{name}: {what} must be a bfloat16 {list(shape)} tensor on {dev} with a contiguous last dimension")
+            strides += t.stride()[:3]
+        return strides
+
+    def _append_args(self, name, layer, k, v, q, pages, lens, counts, cos, sin, positions, interleaved, q_out):
+        n, dev = k.shape[2] if k.dim() == 4 else 0, self.mem.device
+        seqs = self._sequences(name, n, pages, lens, counts)
+        B = seqs[0]
+        strides = self._rows(name, B, n, q=q, k=k, v=v)
+        if (cos is None) != (sin is None) or (positions is not None and cos is None):
+            raise ValueError(f"{name}: cos and sin come together, positions with them")
+        turn = (None,) * 6 if cos is None else _rotation(name, cos, sin, positions, interleaved, (B, n), dev)
+        if q is not None:
+            if q_out is None:
+                q_out = (torch.empty if counts is None and positions is None else torch.zeros)(q.shape, dtype=torch.bfloat16, device=dev)
+            elif q_out.shape != q.shape or q_out.dtype != torch.bfloat16 or not q_out.is_contiguous() or q_out.device != dev:
+                raise ValueError(f"{name}: q_out must be a contiguous bfloat16 {list(q.shape)} tensor on {dev}")
+        elif q_out is not None:
+            raise ValueError(f"{name}: q and q_out come together")
+        ptr = lambda t: None if t is None else t.data_ptr()                                        # noqa: E731
+        return (self.handle.value, layer, *seqs, k.data_ptr(), v.data_ptr(), ptr(q), strides, *turn, ptr(q_out)), q_out
+
+    def _out(self, name, q, counts, out, workspace, dtype):
+        dev, shape = self.mem.device, q.shape
+        if out is None:
+            if dtype not in _OUT_TYPES:
+                raise ValueError(f"{name}: the output is float32 or bfloat16")
+            out = (torch.empty if counts is None else torch.zeros)(shape, dtype=dtype, device=dev)
+        elif out.shape != shape or out.dtype not in _OUT_TYPES or not out.is_contiguous() or out.device != dev:
+            raise ValueError(f"{name}: out must be a contiguous float32 or bfloat16 {list(shape)} tensor on {dev}")
+        if workspace is None:
+            workspace = torch.empty(self.workspace_bytes(shape[0], shape[2]), dtype=torch.uint8, device=dev)
+        elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != dev:
+            raise ValueError(f"{name}: the workspace must be a contiguous uint8 tensor on {dev}")
+        return out, workspace
+
+    def append(self, layer, k, v, pages, lens, counts=None, q=None, cos=None, sin=None, positions=None, interleaved=False, q_out=None):
+        """Stores k, v [B,Hkv,n,128] (bf16, any strides with a contiguous last dimension: views of a fused projection's output too) behind the lens[b] tokens
+        that each sequence has; `lens` is not changed.  With cos, sin (tables of rope_tables) keys and q [B,Hq,n,128] turn on the way, by `positions` int32 [B,n] or
+        by their places in their sequences.  Returns q rotated and head-major (`q_out`, which may be q itself where it is head-major; None without q)."""
+        args, q_out = self._append_args("append", layer, k, v, q, pages, lens, counts, cos, sin, positions, interleaved, q_out)
+        call = (_native or _calls()).paged_append
+        with _device_of(self.mem.device):
+            code = call(*args, _stream())
+        if code:
+            raise MixKVQError(code, "mixkvq_paged_append")
+        return q_out
+
+    def read(self, layer, pages, lens, n_tokens, counts=None, out=None):
+        """The values that tokens lens[b] .. lens[b] + n_tokens - 1 (counts[b]) of every sequence are held as: (k, v) bf16 [B,Hkv,n_tokens,128]."""
+        seqs = self._sequences("read", int(n_tokens), pages, lens, counts)
+        dev, shape = self.mem.device, (seqs[0], self.cfg.n_kv_heads, int(n_tokens), 128)
+        if out is None:
+            out = tuple((torch.empty if counts is None else torch.zeros)(shape, dtype=torch.bfloat16, device=dev) for _ in range(2))
+        for t in out:
+            if t.shape != shape or t.dtype != torch.bfloat16 or not t.is_contiguous() or t.device != dev:
+                raise ValueError(f"read: the outputs must be contiguous bfloat16 {list(shape)} tensors on {dev}")
+        k, v = out
+        call = (_native or _calls()).paged_read
+        with _device_of(dev):
+            code = call(self.handle.value, layer, *seqs, k.data_ptr(), v.data_ptr(), _stream())
+        if code:
+            raise MixKVQError(code, "mixkvq_paged_read")
+        return out
+
+    def attention(self, layer, q, pages, lens, scale, counts=None, out=None, dtype=torch.float32, workspace=None):
+        """The newest n (counts[b]) tokens of every sequence, which has lens[b] tokens with them, attend to its pages, causally among themselves: q [B,Hq,n,128]
+        bf16 (rotated, as append returns it) -> [B,Hq,n,128].  `out`: float32 or bfloat16 (allocated as `dtype` when absent, zeros behind the counts).
+        `workspace`: a uint8 tensor of at least workspace_bytes(B, n) bytes (allocated here when absent)."""
+        n, dev = q.shape[2] if q.dim() == 4 else 0, self.mem.device
+        seqs = self._sequences("attention", n, pages, lens, counts)
+        self._rows("attention", seqs[0], n, q=q)
+        if not q.is_contiguous():
+            raise ValueError("attention: q must be contiguous")
+        out, workspace = self._out("attention", q, counts, out, workspace, dtype)
+        call = (_native or _calls()).paged_attention
+        with _device_of(dev):
+            code = call(self.handle.value, layer, *seqs, q.data_ptr(), out.data_ptr(), _OUT_TYPES[out.dtype], scale, workspace.data_ptr(), workspace.numel(), _stream())
+        if code:
+            raise MixKVQError(code, "mixkvq_paged_attention")
+        return out
+
+    def step(self, layer, k, v, q, pages, lens, scale, counts=None, cos=None, sin=None, positions=None, interleaved=False, q_out=None, out=None,
+             dtype=torch.float32, workspace=None):
+        """append, then attention of the tokens appended (lens: tokens before the call; it is not changed): a decode step, or a chunk of a prompt."""
+        if q is None:
+            raise ValueError("step: queries are needed")
+        args, q_out = self._append_args("step", layer, k, v, q, pages, lens, counts, cos, sin, positions, interleaved, q_out)
+        out, workspace = self._out("step", q_out, counts, out, workspace, dtype)
+        call = (_native or _calls()).paged_step
+        with _device_of(self.mem.device):
+            code = call(*args, out.data_ptr(), _OUT_TYPES[out.dtype], scale, workspace.data_ptr(), workspace.numel(), _stream())
+        if code:
+            raise MixKVQError(code, "mixkvq_paged_step")
+        return out
+
+    def workspace_bytes(self, batch, n_tokens):
+        return int(lib().mixkvq_paged_workspace_bytes(C.byref(self.cfg), int(batch), int(n_tokens)))
+
+    def status(self) -> int:
+        s = C.c_int()
+        with _device_of(self.mem.device):
+            _check(lib().mixkvq_paged_query_status(self.handle, C.byref(s), _stream()), "mixkvq_paged_query_status")
+        return s.value
+
+    def clear_status(self):
+        with _device_of(self.mem.device):
+            _check(lib().mixkvq_paged_clear_status(self.handle, _stream()), "mixkvq_paged_clear_status")
+
+    def test_arm_copy_timeout(self, extra_bytes: int, max_polls: int):
+        _check(lib().mixkvq_paged_test_arm_copy_timeout(self.handle, extra_bytes, max_polls), "mixkvq_paged_test_arm_copy_timeout")
+
+    def launch_count(self) -> int:
+        return int(lib().mixkvq_paged_launch_count(self.handle))

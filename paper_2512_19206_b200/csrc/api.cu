@@ -5,6 +5,7 @@
 #include <vector>
 
 #include "chunk.cuh"
+#include "host_checks.h"
 
 using namespace mixkvq;
 
@@ -163,8 +164,6 @@ LayerView view(const mixkvq_cache* h, int layer, int b0 = 0, int nb = -1) {
   v.wait_polls = h->test_wait_polls;
   return v;
 }
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // every call that enqueues work on the handle notes it
 void note_enqueued(mixkvq_cache* h, cudaStream_t st, int packed_writer) {
@@ -821,6 +820,38 @@ int mixkvq_rope_axes_decode_step(mixkvq_cache* cache, int layer, void* k_dev, co
   rc = run_rope_axes(cache, a, static_cast<cudaStream_t>(stream));
   return rc != MIXKVQ_OK ? rc
                          : run_decode_step(cache, layer, k_dev, v_dev, q_dev, out_dev, softmax_scale, workspace_dev, static_cast<cudaStream_t>(stream));
+}
+
+int mixkvq_rope_partial(mixkvq_cache* cache, const void* q_dev, const void* k_dev, const void* v_dev, const int64_t* strides_host, int n_tokens,
+                        const mixkvq_rotation* rotation, void* q_out_dev, void* k_out_dev, void* v_out_dev, void* stream) {
+  if (!cache || !q_dev || !k_dev || !q_out_dev || !k_out_dev || (v_dev == nullptr) != (v_out_dev == nullptr) || n_tokens < 1) return MIXKVQ_E_INVALID_ARG;
+  const int B = cache->cfg.batch;
+  if ((long long)B * n_tokens > 0x7FFFFFFFll) return MIXKVQ_E_UNSUPPORTED;               // (thread blocks of a grid)
+  RopePartial a{};
+  Ranges r;
+  const void* in[3] = {q_dev, k_dev, v_dev};
+  void* out[3] = {q_out_dev, k_out_dev, v_out_dev};
+  RopeTensor* t[3] = {&a.tq, &a.tk, &a.tv};
+  for (int i = 0; i < 3; ++i) {
+    const int H = i == 0 ? cache->cfg.n_q_heads : cache->cfg.n_kv_heads;
+    *t[i] = strides_host ? RopeTensor{strides_host[3 * i], strides_host[3 * i + 1], strides_host[3 * i + 2]} : head_major(H, n_tokens);
+    const int bad = check_strided(in[i], *t[i], B, H, n_tokens, &r, same_rows(in[i], *t[i], out[i], B, H, n_tokens));
+    if (bad != MIXKVQ_OK) return bad;
+    if (!aligned16(out[i])) return MIXKVQ_E_ALIGNMENT;
+    r.write(out[i], (size_t)B * H * n_tokens * kD * 2);
+  }
+  const int bad = check_rotation(rotation, B, n_tokens, false, &a.turn, &r);
+  if (bad != MIXKVQ_OK) return bad;
+  r.read(cache->mem, memory_bytes(cache));
+  if (r.clash()) return MIXKVQ_E_INVALID_ARG;
+  a.q = q_dev; a.k = k_dev; a.v = v_dev;
+  a.q_out = q_out_dev; a.k_out = k_out_dev; a.v_out = v_out_dev;
+  a.status = reinterpret_cast<uint32_t*>(cache->mem);
+  a.B = B; a.Hq = cache->cfg.n_q_heads; a.Hkv = cache->cfg.n_kv_heads; a.n = n_tokens;
+  if (launch_rope_partial(a, cache->n_sms, static_cast<cudaStream_t>(stream)) != cudaSuccess) return MIXKVQ_E_CUDA;
+  cache->launches += 1;
+  note_enqueued(cache, static_cast<cudaStream_t>(stream), kNoPackedWrite);
+  return MIXKVQ_OK;
 }
 
 // ---- decode attention with the split partials in storage compiled into the library (no allocation)

@@ -212,6 +212,120 @@ PyObject* rope_axes(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return PyLong_FromLong(rc);
 }
 
+mixkvq_paged* paged_of(void* p) { return static_cast<mixkvq_paged*>(p); }
+
+// (batch, tokens, address of the page table, its columns, its stride, address of the lengths, of the counts)
+bool sequences(PyObject* const* a, mixkvq_paged_sequences* s) {
+  void *pages, *lens, *counts;
+  if (!integer(a[0], &s->batch) || !integer(a[1], &s->n_tokens) || !raw(a[2], &pages) || !integer(a[3], &s->max_pages) || !integer(a[4], &s->pages_stride) ||
+      !raw(a[5], &lens) || !raw(a[6], &counts))
+    return false;
+  s->pages_dev = static_cast<const int32_t*>(pages);
+  s->lens_dev = static_cast<const int32_t*>(lens);
+  s->counts_dev = static_cast<const int32_t*>(counts);
+  return true;
+}
+
+// (addresses of cos and sin, their rows, address of the positions, rotated channels, whether pairs are neighbours), the first None: no rotation
+bool rotation(PyObject* const* a, mixkvq_rotation* r, mixkvq_rotation** given) {
+  void *cos, *sin, *positions;
+  *given = nullptr;
+  if (a[0] == Py_None) return true;
+  if (!raw(a[0], &cos) || !raw(a[1], &sin) || !integer(a[2], &r->n_positions) || !raw(a[3], &positions) || !integer(a[4], &r->rotary_dim) || !integer(a[5], &r->interleaved))
+    return false;
+  r->cos_dev = static_cast<const float*>(cos);
+  r->sin_dev = static_cast<const float*>(sin);
+  r->positions_dev = static_cast<const int32_t*>(positions);
+  r->reserved = 0;
+  *given = r;
+  return true;
+}
+
+// Nine strides.
+bool nine(PyObject* o, std::vector<int64_t>* v) {
+  if (!whole_numbers(o, v)) return false;
+  if (v->size() != 9) PyErr_SetString(PyExc_ValueError, "nine strides are needed");
+  return v->size() == 9;
+}
+
+// (handle, addresses of q, k, v, their nine strides, tokens, the rotation (6), addresses of the outputs, stream)
+PyObject* rope_partial(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  void *p[7], *st;
+  int tokens, rc;
+  std::vector<int64_t> strides;
+  mixkvq_rotation r, *turn;
+  if (!count_is(n, 16) || !raw(a[0], &p[0]) || !raw(a[1], &p[1]) || !raw(a[2], &p[2]) || !raw(a[3], &p[3]) || !nine(a[4], &strides) || !integer(a[5], &tokens) ||
+      !rotation(a + 6, &r, &turn) || !raw(a[12], &p[4]) || !raw(a[13], &p[5]) || !raw(a[14], &p[6]) || !raw(a[15], &st))
+    return nullptr;
+  Py_BEGIN_ALLOW_THREADS
+  rc = mixkvq_rope_partial(cache_of(p[0]), p[1], p[2], p[3], strides.data(), tokens, turn, p[4], p[5], p[6], st);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+// (handle, layer, the sequences (7), addresses of k, v, q, their nine strides (q, k, v), the rotation (6), address of the rotated queries, stream)
+PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  void *h, *k, *v, *q, *q_out, *st;
+  int layer, rc;
+  std::vector<int64_t> strides;
+  mixkvq_paged_sequences s;
+  mixkvq_rotation r, *turn;
+  if (!count_is(n, 21) || !raw(a[0], &h) || !integer(a[1], &layer) || !sequences(a + 2, &s) || !raw(a[9], &k) || !raw(a[10], &v) || !raw(a[11], &q) ||
+      !nine(a[12], &strides) || !rotation(a + 13, &r, &turn) || !raw(a[19], &q_out) || !raw(a[20], &st))
+    return nullptr;
+  Py_BEGIN_ALLOW_THREADS
+  rc = mixkvq_paged_append(paged_of(h), layer, &s, k, v, q, strides.data(), turn, q_out, st);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+// (handle, layer, the sequences (7), addresses of the keys' and the values' rows, stream)
+PyObject* paged_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  void *h, *k, *v, *st;
+  int layer, rc;
+  mixkvq_paged_sequences s;
+  if (!count_is(n, 12) || !raw(a[0], &h) || !integer(a[1], &layer) || !sequences(a + 2, &s) || !raw(a[9], &k) || !raw(a[10], &v) || !raw(a[11], &st)) return nullptr;
+  Py_BEGIN_ALLOW_THREADS
+  rc = mixkvq_paged_read(paged_of(h), layer, &s, k, v, st);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+// (handle, layer, the sequences (7), addresses of q and of the output, its type, scale, address of the workspace, its bytes, stream)
+PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  void *h, *q, *out, *ws, *st;
+  int layer, type, rc;
+  float scale;
+  size_t bytes;
+  mixkvq_paged_sequences s;
+  if (!count_is(n, 16) || !raw(a[0], &h) || !integer(a[1], &layer) || !sequences(a + 2, &s) || !raw(a[9], &q) || !raw(a[10], &out) || !integer(a[11], &type) ||
+      !real(a[12], &scale) || !raw(a[13], &ws) || !size(a[14], &bytes) || !raw(a[15], &st))
+    return nullptr;
+  Py_BEGIN_ALLOW_THREADS
+  rc = mixkvq_paged_attention(paged_of(h), layer, &s, q, out, type, scale, ws, bytes, st);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+// (as paged_append up to the rotated queries, then address of the output, its type, scale, address of the workspace, its bytes, stream)
+PyObject* paged_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  void *h, *k, *v, *q, *q_out, *out, *ws, *st;
+  int layer, type, rc;
+  float scale;
+  size_t bytes;
+  std::vector<int64_t> strides;
+  mixkvq_paged_sequences s;
+  mixkvq_rotation r, *turn;
+  if (!count_is(n, 26) || !raw(a[0], &h) || !integer(a[1], &layer) || !sequences(a + 2, &s) || !raw(a[9], &k) || !raw(a[10], &v) || !raw(a[11], &q) ||
+      !nine(a[12], &strides) || !rotation(a + 13, &r, &turn) || !raw(a[19], &q_out) || !raw(a[20], &out) || !integer(a[21], &type) || !real(a[22], &scale) ||
+      !raw(a[23], &ws) || !size(a[24], &bytes) || !raw(a[25], &st))
+    return nullptr;
+  Py_BEGIN_ALLOW_THREADS
+  rc = mixkvq_paged_step(paged_of(h), layer, &s, k, v, q, strides.data(), turn, q_out, out, type, scale, ws, bytes, st);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
 template <typename F>
 PyCFunction fast(F f) {
   return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f));
@@ -223,6 +337,11 @@ PyMethodDef methods[] = {{"decode_attention", fast(decode_attention), METH_FASTC
                          {"quantize_append", fast(quantize_append), METH_FASTCALL, nullptr},
                          {"chunk", fast(chunk), METH_FASTCALL, nullptr},
                          {"rope_axes", fast(rope_axes), METH_FASTCALL, nullptr},
+                         {"rope_partial", fast(rope_partial), METH_FASTCALL, nullptr},
+                         {"paged_append", fast(paged_append), METH_FASTCALL, nullptr},
+                         {"paged_read", fast(paged_read), METH_FASTCALL, nullptr},
+                         {"paged_attention", fast(paged_attention), METH_FASTCALL, nullptr},
+                         {"paged_step", fast(paged_step), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
