@@ -1,81 +1,687 @@
 // Attention of the newest tokens of every sequence over the pages of the 4-bit cache.
 //
-// The plain form: a thread block per query row, a warp goes through every fourth token, a lane has four channels.
+// Mathematics.  A key is k_c = s_g c_c + z_g in group g of G channels, so a logit is sum_g s_g (sum_{c in g} q_c c_c) + z_g (sum_{c in g} q_c): the codes enter the
+// tensor core as they are (a nibble masked out of a word is an fp16 subnormal, 2^-24 or 2^-20 times the code; the factor 16 is taken out of the query), the sums of a group
+// are scaled behind it in fp32.  A value is s_g c + z_g with a scale per token, so the weight p s_g of (token, group) is the other operand of the second product, in fp16,
+// and sum p z_g is added up in fp32.  One pass over the tokens with a running reference of the logits.
+//
+// Operands stay inside fp16's range whatever the inputs' magnitudes: a query row is scaled by a power of two (exactly) to a largest entry of 2^14 to 2^15, and p s_g by a power of
+// two per group, lowered as larger scales come.  References are raised, and sums rescaled, only when a logit is 4 (in powers of two) above its row's.
+//
+// Split: work is units of 32 tokens of one (sequence, KV head, block of query rows), all of them in one line, cut evenly over the thread blocks on the device (the
+// lengths are known there alone).  A thread block goes through the pieces of streams in its range, its warps through the units of a piece, each with a ring of
+// bulk copies of its own, so that no warp waits for another before the end of a piece.  A piece that is no whole stream leaves sums, which merge_kernel joins.
 #include <algorithm>
 
 #include "paged.cuh"
+#include "warp_ops.cuh"
 
 namespace mixkvq {
 
 namespace {
 
-__global__ void __launch_bounds__(128)
-row_kernel(const __grid_constant__ PagedAttention a) {
+constexpr int kWarps = 4;
+constexpr int kUnit = 32;                        // tokens
+constexpr int kStages = 2;                       // units in a warp's ring, per tile of 8 query rows
+constexpr int kPartFloats = kD + 2;              // of a row's sums: o[128], reference, denominator
+constexpr uint32_t kPolls = 1u << 21;
+constexpr float kRise = 4.f;                     // a logit this much above the reference raises it
+constexpr float kMostScale = 2048.f;             // of a value scale times its group's factor
+
+struct Plan {
+  int rows;                                      // of a block of query rows
+  int direct;                                    // a thread block per stream, nothing to merge
+  float* parts;                                  // [2 * thread blocks][rows][kPartFloats]
+  long long* prefix;                             // [B + 1] units before each sequence, behind the parts; then the number of parts
+};
+
+__device__ __forceinline__ int row_blocks(int count, int g, int rows) { return (count * g + rows - 1) / rows; }
+
+__device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
+
+// A stream: a block of query rows of a KV head of a sequence.
+struct Stream {
+  int b, h, row0;                                // first row of the block: token * g + head
+  int len, count, units;
+};
+
+// The state of one warp over its units of a piece.
+template <int kNG, int kNT>
+struct WarpState {
+  float acc[8][4 * kNT];                         // tile 2 j + e: channels 32 j + 4 r + e (and + 2), per row tile; times 2^-24 (e = 0), 2^-20 (e = 1) and the group's factor
+  float zsum[kNG][2 * kNT];                      // sum p z of the lane's tokens
+  float ref[2 * kNT], l[2 * kNT];
+  float factor[kNG];
+};
+
+// 16 bytes of metas of a token: the words {s, z} of its groups.
+template <int kNG>
+__device__ __forceinline__ void load_meta(uint32_t a, uint32_t (&w)[kNG]) {
+  if constexpr (kNG == 4) {
+    const uint4 x = lds128(a);
+    w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+  } else if constexpr (kNG == 2) {
+    const uint2 x = lds64(a);
+    w[0] = x.x; w[1] = x.y;
+  } else {
+    w[0] = lds32(a);
+  }
+}
+
+template <int kG, int kNT>
+__global__ void __launch_bounds__(kWarps * 32, kNT == 1 ? 4 : 2)
+pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ Plan plan) {
+  constexpr int kNG = kD / kG, kMeta = 512 / kG, kTileBytes = 2048 + 32 * kMeta, kRows = 8 * kNT, kUnitBytes = 2 * kTileBytes, stages = kStages * kNT;
+  extern __shared__ __align__(128) unsigned char smem[];
+  const PagedView& v = a.view;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, t = lane & 3;
+  const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * stages * kUnitBytes);
+  unsigned char* behind = smem + kWarps * stages * kUnitBytes;
+  const uint32_t bars = smem_u32(behind) + 8u * (uint32_t)(warp * stages);
+  long long* prefix = reinterpret_cast<long long*>(behind + 8 * kWarps * stages);
+  if (lane == 0) {
+    for (int i = 0; i < stages; ++i) mbar_init(bars + 8u * i, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncwarp();
+  dependency_wait();
+  auto units_of = [&](int len) { return max(1, (len + kUnit - 1) / kUnit); };
+  long long pos, end, total = 0;
+  int parts = gridDim.x;
+  if (plan.direct) {
+    pos = 0;
+    end = 1;
+  } else {
+    for (int b = tid; b < v.B; b += kWarps * 32) {
+      const int count = v.count(b), len = v.length(b, v.add_counts ? count : 0);
+      prefix[b + 1] = (long long)row_blocks(count, v.g, kRows) * v.Hkv * units_of(len);
+    }
+    if (tid == 0) prefix[0] = 0;
+    __syncthreads();
+    if (warp == 0) {
+      long long sum = 0;
+      for (int b0 = 0; b0 < v.B; b0 += 32) {
+        long long x = b0 + lane < v.B ? prefix[b0 + lane + 1] : 0;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const long long y = __shfl_up_sync(0xffffffffu, x, d);
+          if (lane >= d) x += y;
+        }
+        if (b0 + lane < v.B) prefix[b0 + lane + 1] = sum + x;
+        sum += __shfl_sync(0xffffffffu, x, 31);
+      }
+    }
+    __syncthreads();
+    total = prefix[v.B];
+    // at least a unit for every warp of a thread block
+    parts = (int)min((long long)gridDim.x, max(1ll, (total + kWarps - 1) / kWarps));
+    if (blockIdx.x == 0) {
+      for (int b = tid; b <= v.B; b += kWarps * 32) plan.prefix[b] = prefix[b];
+      if (tid == 0) plan.prefix[v.B + 1] = parts;
+    }
+    if ((int)blockIdx.x >= parts) return;
+    pos = split_begin(total, parts, blockIdx.x);
+    end = split_begin(total, parts, blockIdx.x + 1);
+  }
+  const int pi = r ^ (r >> 1 & 1);               // token of a tile that the lane's rows of its products are (and 8 more)
+  uint32_t phase = 0;                            // of the warp's barriers, a bit each
+  bool dead = false;
+  auto wait = [&](uint32_t bar, uint32_t parity) {
+    if (!__all_sync(0xffffffffu, mbar_wait_polls(bar, parity, a.max_polls ? a.max_polls : kPolls))) {
+      dead = true;
+      if (lane == 0) atomicOr(v.status, (uint32_t)MIXKVQ_DEV_COPY_TIMEOUT);
+    }
+  };
+
+  int b_at = 0;
+  while (pos < end) {
+    // ---- the piece: units u0 .. u1 - 1 of a stream
+    Stream st;
+    int u0, u1, stream;
+    if (plan.direct) {
+      const int blocks = row_blocks(v.n, v.g, kRows);
+      stream = blockIdx.x;
+      st.b = stream / (blocks * v.Hkv);
+      st.count = v.count(st.b);
+      st.len = v.length(st.b, v.add_counts ? st.count : 0);
+      const int s = stream - st.b * blocks * v.Hkv;
+      st.h = s / blocks;
+      st.row0 = (s - st.h * blocks) * kRows;
+      st.units = units_of(st.len);
+      u0 = 0;
+      u1 = st.units;
+      pos = 1;
+      if (st.row0 >= st.count * v.g) return;
+    } else {
+      if (b_at == 0) {
+        int lo = 0, hi = v.B;                    // the last b with prefix[b] <= pos that has units
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (prefix[mid] <= pos) lo = mid; else hi = mid;
+        }
+        b_at = lo;
+      }
+      while (prefix[b_at + 1] <= pos) ++b_at;
+      st.b = b_at;
+      st.count = v.count(st.b);
+      st.len = v.length(st.b, v.add_counts ? st.count : 0);
+      st.units = units_of(st.len);
+      const long long off = pos - prefix[b_at];
+      const int s = (int)(off / st.units), blocks = row_blocks(st.count, v.g, kRows);
+      st.h = s / blocks;
+      st.row0 = (s - st.h * blocks) * kRows;
+      u0 = (int)(off - (long long)s * st.units);
+      u1 = (int)min((long long)st.units, u0 + (end - pos));
+      pos += u1 - u0;
+    }
+    const bool begins = u0 == 0, whole = begins && u1 == st.units;
+    // tokens that the last row of the block sees: units behind them are left out
+    const int last_row = min(st.row0 + kRows, st.count * v.g) - 1;
+    const int most = min(st.len, max(0, st.len - st.count + last_row / v.g + 1));
+    const int u_last = min(u1, (most + kUnit - 1) / kUnit);
+    const int mine = !dead && u_last > u0 + warp ? (u_last - u0 - warp + kWarps - 1) / kWarps : 0;      // units of the warp: u0 + warp + kWarps i
+
+    // ---- copies: the page numbers of 32 of the warp's units at a time, a lane each (two where a page is half a unit)
+    int id0 = -1, id1 = -1;
+    uint32_t halves = 0;                         // per stage two bits: which half of the unit is there
+    auto issue = [&](int i) {
+      const int stage = i % stages;
+      if ((i & 31) == 0) {
+        const int tok = (u0 + warp + kWarps * (i + lane)) * kUnit;
+        const int32_t* row = v.pages + (size_t)st.b * v.pages_stride;
+        id0 = i + lane < mine && tok < most ? row[tok >> v.lg_page] : 0;
+        id1 = v.lg_page == 4 ? (i + lane < mine && tok + 16 < most ? row[(tok + 16) >> 4] : 0) : id0;
+        if (id0 < 0 || id0 >= v.n_pages || id1 < 0 || id1 >= v.n_pages) atomicOr(v.status, (uint32_t)MIXKVQ_DEV_BAD_PAGE);
+      }
+      const int tok = (u0 + warp + kWarps * i) * kUnit;
+      const int p0 = __shfl_sync(0xffffffffu, id0, i & 31), p1 = __shfl_sync(0xffffffffu, id1, i & 31);
+      const bool ok0 = p0 >= 0 && p0 < v.n_pages, ok1 = p1 >= 0 && p1 < v.n_pages && tok + 16 < most;
+      halves = (halves & ~(3u << (2 * stage))) | ((ok0 ? 1u : 0u) | (ok1 ? 2u : 0u)) << (2 * stage);
+      if (lane == 0) {
+        const uint32_t bar = bars + 8u * stage, dst = ring + (uint32_t)(stage * kUnitBytes);
+        const uint32_t bytes = ((ok0 ? 1u : 0u) + (ok1 ? 1u : 0u)) * kTileBytes;
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes + (i == 0 ? a.test_extra : 0u)) : "memory");
+        const char* src0 = v.pool + (uint64_t)(uint32_t)p0 * v.page_bytes + (uint64_t)st.h * v.piece_bytes + v.tile_of(tok);
+        const char* src1 = v.pool + (uint64_t)(uint32_t)p1 * v.page_bytes + (uint64_t)st.h * v.piece_bytes + v.tile_of(tok + 16);
+        if (ok0 && ok1 && v.lg_page > 4) {
+          asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src0), "r"(bytes), "r"(bar) : "memory");
+        } else {
+          if (ok0)
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src0), "r"(kTileBytes), "r"(bar)
+                         : "memory");
+          if (ok1)
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst + kTileBytes), "l"(src1), "r"(kTileBytes),
+                         "r"(bar)
+                         : "memory");
+        }
+      }
+    };
+    for (int i = 0; i < min(stages, mine); ++i) issue(i);
+
+    // ---- queries: lane (r, t) has channels 32 j + 8 t .. + 7 of row r of every row tile as operands
+    uint32_t qb[kNT][4][4];                      // word j: {0,4} {2,6} {1,5}/16 {3,7}/16
+    float qsum[kNT][kNG][2], qscale[kNT][2];
+    int sees[kNT][2];
+#pragma unroll
+    for (int nt = 0; nt < kNT; ++nt) {
+      const int row = st.row0 + 8 * nt + r;
+      const bool there = row < st.count * v.g;
+      const int i = row / v.g, head = row - i * v.g;
+      const uint16_t* src = static_cast<const uint16_t*>(a.q) + (((size_t)st.b * v.Hq + st.h * v.g + head) * v.n + i) * kD + 8 * t;
+      uint4 w[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = there ? *reinterpret_cast<const uint4*>(src + 32 * j) : make_uint4(0u, 0u, 0u, 0u);
+      uint32_t top = 0;                          // the largest magnitude's bits (finite or not)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t x[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) top = max(top, max(x[k] & 0x7FFFu, x[k] >> 16 & 0x7FFFu));
+      }
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      // 2^e: the largest entry to 2^14 .. 2^15 (or as near as a factor of 2^126 brings it)
+      const int e = min(max(14 + 127 - (int)(top >> 7), -114), 126);
+      const float up = pow2i(e);
+      float part[kNG];
+#pragma unroll
+      for (int k = 0; k < kNG; ++k) part[k] = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t x[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+        float f[8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          f[2 * k] = bf_lo(x[k]);
+          f[2 * k + 1] = bf_hi(x[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) part[j * kNG / 4] += f[k];
+        qb[nt][j][0] = pack_half2(f[0] * up, f[4] * up);
+        qb[nt][j][1] = pack_half2(f[2] * up, f[6] * up);
+        qb[nt][j][2] = pack_half2(f[1] * (up * 0.0625f), f[5] * (up * 0.0625f));
+        qb[nt][j][3] = pack_half2(f[3] * (up * 0.0625f), f[7] * (up * 0.0625f));
+      }
+#pragma unroll
+      for (int k = 0; k < kNG; ++k) {
+        part[k] += __shfl_xor_sync(0xffffffffu, part[k], 1);
+        part[k] += __shfl_xor_sync(0xffffffffu, part[k], 2);
+      }
+      // the columns of the lane's products: rows 2 t and 2 t + 1
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const int from = 4 * (2 * t + c);
+#pragma unroll
+        for (int k = 0; k < kNG; ++k) qsum[nt][k][c] = __shfl_sync(0xffffffffu, part[k], from) * a.scale_log2e;
+        qscale[nt][c] = a.scale_log2e * (pow2i(-__shfl_sync(0xffffffffu, e, from)) * 16777216.f);
+        const int x = st.row0 + 8 * nt + 2 * t + c;
+        // (rows that are none are computed like the others and written nowhere)
+        sees[nt][c] = x < st.count * v.g ? max(0, st.len - st.count + x / v.g + 1) : st.len;
+      }
+    }
+    int fewest = st.len;
+#pragma unroll
+    for (int nt = 0; nt < kNT; ++nt) fewest = min(fewest, min(sees[nt][0], sees[nt][1]));
+    fewest = __reduce_min_sync(0xffffffffu, fewest);
+
+    WarpState<kNG, kNT> w;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int k = 0; k < 4 * kNT; ++k) w.acc[i][k] = 0.f;
+#pragma unroll
+    for (int i = 0; i < kNG; ++i) {
+      w.factor[i] = pow2i(120);
+#pragma unroll
+      for (int k = 0; k < 2 * kNT; ++k) w.zsum[i][k] = 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < 2 * kNT; ++k) {
+      w.ref[k] = -1e30f;
+      w.l[k] = 0.f;
+    }
+
+    // ---- one unit: tokens tok .. tok + 31
+    auto unit = [&](uint32_t base, int tok, uint32_t there, auto masked) {
+      constexpr bool kMask = decltype(masked)::value;
+      float x[kNT][2][4];                        // [tile of 16 tokens][row r: columns 2 t, 2 t + 1; row r + 8]
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        const uint32_t tile = base + m * kTileBytes;
+        const uint4 k0 = lds128(tile + pi * 64 + t * 16), k1 = lds128(tile + (pi + 8) * 64 + t * 16);
+        uint32_t m0[kNG], m1[kNG];
+        load_meta<kNG>(tile + 2048 + pi * kMeta, m0);
+        load_meta<kNG>(tile + 2048 + (pi + 8) * kMeta, m1);
+        const uint32_t w0[4] = {k0.x, k0.y, k0.z, k0.w}, w1[4] = {k1.x, k1.y, k1.z, k1.w};
+        float sum[kNT][4], zs[kNT][4];
+#pragma unroll
+        for (int g = 0; g < kNG; ++g) {
+          float c[kNT][4];
+#pragma unroll
+          for (int nt = 0; nt < kNT; ++nt) c[nt][0] = c[nt][1] = c[nt][2] = c[nt][3] = 0.f;
+#pragma unroll
+          for (int j = g * 4 / kNG; j < (g + 1) * 4 / kNG; ++j) {
+            const uint32_t u0w = w0[j], u1w = w1[j], h0 = u0w >> 8, h1 = u1w >> 8;
+            const uint32_t e0 = u0w & 0x000F000Fu, e1 = u1w & 0x000F000Fu, e2 = h0 & 0x000F000Fu, e3 = h1 & 0x000F000Fu;
+            const uint32_t o0 = u0w & 0x00F000F0u, o1 = u1w & 0x00F000F0u, o2 = h0 & 0x00F000F0u, o3 = h1 & 0x00F000F0u;
+#pragma unroll
+            for (int nt = 0; nt < kNT; ++nt) {
+              mma_f16(c[nt], e0, e1, e2, e3, qb[nt][j][0], qb[nt][j][1]);
+              mma_f16(c[nt], o0, o1, o2, o3, qb[nt][j][2], qb[nt][j][3]);
+            }
+          }
+          const float s0 = bf_lo(m0[g]), z0 = bf_hi(m0[g]), s1 = bf_lo(m1[g]), z1 = bf_hi(m1[g]);
+#pragma unroll
+          for (int nt = 0; nt < kNT; ++nt) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float s = k < 2 ? s0 : s1, z = k < 2 ? z0 : z1, qs = qsum[nt][g][k & 1];
+              sum[nt][k] = g == 0 ? s * c[nt][k] : fmaf(s, c[nt][k], sum[nt][k]);
+              zs[nt][k] = g == 0 ? z * qs : fmaf(z, qs, zs[nt][k]);
+            }
+          }
+        }
+#pragma unroll
+        for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            x[nt][m][k] = fmaf(sum[nt][k], qscale[nt][k & 1], zs[nt][k]);
+            if constexpr (kMask) {
+              const int at = tok + 16 * m + pi + (k < 2 ? 0 : 8);
+              if (at >= sees[nt][k & 1] || !(there >> m & 1)) x[nt][m][k] = -INFINITY;
+            }
+          }
+      }
+      // ---- value scales times their groups' factors, and whether a reference or a factor has to move
+      float sk[2][2][kNG];
+      uint32_t vm[2][2][kNG];
+      float top_s = 0.f;
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        const uint32_t meta = base + m * kTileBytes + 2048 + 16 * kMeta + pi * kMeta;
+        load_meta<kNG>(meta, vm[m][0]);
+        load_meta<kNG>(meta + 8 * kMeta, vm[m][1]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int g = 0; g < kNG; ++g) {
+            if constexpr (kMask) {               // what lies behind the last token may be anything
+              const int at = tok + 16 * m + pi + 8 * h;
+              if (at >= most || !(there >> m & 1)) vm[m][h][g] = 0u;
+            }
+            sk[m][h][g] = bf_lo(vm[m][h][g]) * w.factor[g];
+            top_s = fmaxf(top_s, sk[m][h][g]);
+          }
+      }
+      bool move = top_s > kMostScale;
+      float top[2 * kNT];
+#pragma unroll
+      for (int c = 0; c < 2 * kNT; ++c) {
+        const int nt = c >> 1, k = c & 1;
+        top[c] = fmaxf(fmaxf(x[nt][0][k], x[nt][0][k + 2]), fmaxf(x[nt][1][k], x[nt][1][k + 2]));
+        move = move || top[c] > w.ref[c] + kRise;
+      }
+      if (__any_sync(0xffffffffu, move)) {
+#pragma unroll
+        for (int c = 0; c < 2 * kNT; ++c) {
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], d));
+          const float up = fmaxf(w.ref[c], top[c]), f = ex2_approx(w.ref[c] - up);
+          w.ref[c] = up;
+          w.l[c] *= f;
+#pragma unroll
+          for (int g = 0; g < kNG; ++g) w.zsum[g][c] *= f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            w.acc[i][4 * (c >> 1) + (c & 1)] *= f;
+            w.acc[i][4 * (c >> 1) + (c & 1) + 2] *= f;
+          }
+        }
+#pragma unroll
+        for (int g = 0; g < kNG; ++g) {
+          uint32_t s = 0;                        // the largest finite scale of the group, as bits (scales are not negative)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t y = vm[i >> 1][i & 1][g] << 16 & 0x7FFFFFFFu;
+            s = y < 0x7F800000u ? max(s, y) : s;
+          }
+          s = __reduce_max_sync(0xffffffffu, s);
+          if (__uint_as_float(s) * w.factor[g] > kMostScale) {
+            const float down = pow2i(min(max(9 + 127 - (int)(s >> 23), -118), 120)), f = down / w.factor[g];
+            w.factor[g] = down;
+#pragma unroll
+            for (int i = g * 8 / kNG; i < (g + 1) * 8 / kNG; ++i)
+#pragma unroll
+              for (int k = 0; k < 4 * kNT; ++k) w.acc[i][k] *= f;
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sk[i >> 1][i & 1][g] = bf_lo(vm[i >> 1][i & 1][g]) * w.factor[g];
+        }
+      }
+      // ---- weights and the second product
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        const uint32_t tile = base + m * kTileBytes + 1024;
+        uint2 vw[4];                             // tokens of the operand's columns 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int row = 2 * t + (i & 1), token = (row ^ (row >> 1 & 1)) + 8 * (i >> 1);
+          vw[i] = lds64(tile + token * 64 + ((8 * r) ^ ((token & 4) << 3)));
+        }
+        float p[kNT][4];
+#pragma unroll
+        for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            p[nt][k] = ex2_approx(x[nt][m][k] - w.ref[2 * nt + (k & 1)]);
+            w.l[2 * nt + (k & 1)] += p[nt][k];
+          }
+#pragma unroll
+        for (int g = 0; g < kNG; ++g) {
+          uint32_t ub[kNT][2];
+#pragma unroll
+          for (int nt = 0; nt < kNT; ++nt) {
+            float u[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float z = bf_hi(vm[m][k >> 1][g]);
+              float pz = p[nt][k] * z;
+              u[k] = p[nt][k] * sk[m][k >> 1][g];
+              if constexpr (kMask) {             // a row that does not see a token takes nothing of it, an infinity neither
+                if (x[nt][m][k] == -INFINITY) u[k] = pz = 0.f;
+              }
+              w.zsum[g][2 * nt + (k & 1)] += pz;
+            }
+            ub[nt][0] = movmatrix_trans(pack_half2(u[0], u[1]));
+            ub[nt][1] = movmatrix_trans(pack_half2(u[2], u[3]));
+          }
+#pragma unroll
+          for (int j = g * 4 / kNG; j < (g + 1) * 4 / kNG; ++j) {
+            const uint32_t sel = j & 1 ? 0x7632u : 0x5410u;
+            const uint32_t ab = __byte_perm(j < 2 ? vw[0].x : vw[0].y, j < 2 ? vw[1].x : vw[1].y, sel);
+            const uint32_t cd = __byte_perm(j < 2 ? vw[2].x : vw[2].y, j < 2 ? vw[3].x : vw[3].y, sel);
+            const uint32_t ab8 = ab >> 8, cd8 = cd >> 8;
+#pragma unroll
+            for (int nt = 0; nt < kNT; ++nt) {
+              mma_f16(reinterpret_cast<float(&)[4]>(w.acc[2 * j][4 * nt]), ab & 0x000F000Fu, ab8 & 0x000F000Fu, cd & 0x000F000Fu, cd8 & 0x000F000Fu, ub[nt][0], ub[nt][1]);
+              mma_f16(reinterpret_cast<float(&)[4]>(w.acc[2 * j + 1][4 * nt]), ab & 0x00F000F0u, ab8 & 0x00F000F0u, cd & 0x00F000F0u, cd8 & 0x00F000F0u, ub[nt][0],
+                      ub[nt][1]);
+            }
+          }
+        }
+      }
+    };
+    int done = 0;                                // units waited for
+    for (; done < mine; ++done) {
+      const int stage = done % stages, tok = (u0 + warp + kWarps * done) * kUnit;
+      const uint32_t there = halves >> (2 * stage) & 3u;
+      wait(bars + 8u * stage, phase >> stage & 1u);
+      if (dead) break;
+      phase ^= 1u << stage;
+      const uint32_t base = ring + (uint32_t)(stage * kUnitBytes);
+      if (tok + kUnit > fewest || there != 3u)
+        unit(base, tok, there, std::true_type{});
+      else
+        unit(base, tok, there, std::false_type{});
+      __syncwarp();
+      if (done + stages < mine) issue(done + stages);
+    }
+    if (dead) {
+      // what is under way is waited for, and the piece is left without this warp's part
+      for (int i = done; i < min(mine, done + stages); ++i) {
+        const int stage = i % stages;
+        wait(bars + 8u * stage, phase >> stage & 1u);
+      }
+#pragma unroll
+      for (int k = 0; k < 2 * kNT; ++k) {
+        w.ref[k] = -1e30f;
+        w.l[k] = 0.f;
+#pragma unroll
+        for (int g = 0; g < kNG; ++g) w.zsum[g][k] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w.acc[i][4 * (k >> 1) + (k & 1)] = w.acc[i][4 * (k >> 1) + (k & 1) + 2] = 0.f;
+      }
+    }
+
+    // ---- the warp's sums into its ring: [rows][132] floats: o[128], reference, denominator
+#pragma unroll
+    for (int k = 0; k < 2 * kNT; ++k) {
+#pragma unroll
+      for (int d = 4; d < 32; d <<= 1) {
+        w.l[k] += __shfl_xor_sync(0xffffffffu, w.l[k], d);
+#pragma unroll
+        for (int g = 0; g < kNG; ++g) w.zsum[g][k] += __shfl_xor_sync(0xffffffffu, w.zsum[g][k], d);
+      }
+    }
+    constexpr int kStride = kD + 4;
+    __syncwarp();
+#pragma unroll
+    for (int c = 0; c < 2 * kNT; ++c) {
+      const int nt = c >> 1, k = c & 1, row = 8 * nt + 2 * t + k;
+      const uint32_t at = ring + (uint32_t)row * (kStride * 4);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int g = j * kNG / 4;
+        const float back = pow2i(127 - (int)(__float_as_uint(w.factor[g]) >> 23)), z = w.zsum[g][c];
+        const float y0 = fmaf(w.acc[2 * j][4 * nt + k] * 16777216.f, back, z), y2 = fmaf(w.acc[2 * j][4 * nt + k + 2] * 16777216.f, back, z);
+        const float y1 = fmaf(w.acc[2 * j + 1][4 * nt + k] * 1048576.f, back, z), y3 = fmaf(w.acc[2 * j + 1][4 * nt + k + 2] * 1048576.f, back, z);
+        sts128(at + (32 * j + 4 * r) * 4, __float_as_uint(y0), __float_as_uint(y1), __float_as_uint(y2), __float_as_uint(y3));
+      }
+      if (r == 0) sts64(at + kD * 4, __float_as_uint(w.ref[c]), __float_as_uint(w.l[c]));
+    }
+    __syncthreads();
+    // ---- the warps' sums together: a warp has every fourth row, a lane four channels
+    const uint32_t first = smem_u32(smem);
+    for (int row = warp; row < kRows; row += kWarps) {
+      const int x = st.row0 + row;
+      if (x >= st.count * v.g) break;
+      float m[kWarps], l[kWarps], top = -1e30f;
+#pragma unroll
+      for (int i = 0; i < kWarps; ++i) {
+        const uint2 ml = lds64(first + (uint32_t)(i * stages * kUnitBytes + (row * kStride + kD) * 4));
+        m[i] = __uint_as_float(ml.x);
+        l[i] = __uint_as_float(ml.y);
+        top = fmaxf(top, m[i]);
+      }
+      float y[4] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < kWarps; ++i) {
+        const float f = ex2_approx(m[i] - top);
+        const uint4 o = lds128(first + (uint32_t)(i * stages * kUnitBytes + (row * kStride + 4 * lane) * 4));
+        sum = fmaf(l[i], f, sum);
+        y[0] = fmaf(__uint_as_float(o.x), f, y[0]);
+        y[1] = fmaf(__uint_as_float(o.y), f, y[1]);
+        y[2] = fmaf(__uint_as_float(o.z), f, y[2]);
+        y[3] = fmaf(__uint_as_float(o.w), f, y[3]);
+      }
+      if (whole) {
+        const int i = x / v.g, head = x - i * v.g;
+        const size_t at = (((size_t)st.b * v.Hq + st.h * v.g + head) * v.n + i) * kD + 4 * lane;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        if (a.out_bf16)
+          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + at) = make_uint2(pack_bf162(y[0] * inv, y[1] * inv), pack_bf162(y[2] * inv, y[3] * inv));
+        else
+          *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at) = make_float4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
+      } else {
+        float* to = plan.parts + ((size_t)(2 * blockIdx.x + (begins ? 1 : 0)) * kRows + row) * kPartFloats;
+        *reinterpret_cast<float2*>(to + 4 * lane) = make_float2(y[0], y[1]);
+        *reinterpret_cast<float2*>(to + 4 * lane + 2) = make_float2(y[2], y[3]);
+        if (lane == 0) *reinterpret_cast<float2*>(to + kD) = make_float2(top, sum);
+      }
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // the rings take copies again
+    __syncthreads();
+  }
+}
+
+// Joins the pieces of a stream: a thread block per (stream, row), a warp has every eighth piece, a lane four channels.
+__global__ void __launch_bounds__(256)
+merge_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ Plan plan) {
   dependency_wait();
   const PagedView& v = a.view;
-  const int i = blockIdx.x % v.n, hq = blockIdx.x / v.n % v.Hq, b = blockIdx.x / v.n / v.Hq;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = hq / v.g, G = v.G;
-  const int count = v.count(b), len = v.length(b, v.add_counts ? count : 0);
-  if (i >= count) return;
-  const int sees = min(len, len - count + i + 1);
-  const size_t at = (((size_t)b * v.Hq + hq) * v.n + i) * kD + 4 * lane;
-  const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(a.q) + at);
-  const float q[4] = {bf16_half(w.x, 0), bf16_half(w.x, 1), bf16_half(w.y, 0), bf16_half(w.y, 1)};
-  float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  const int c = 4 * lane;                                   // the lane's channels
-  for (int t = warp; t < sees; t += 4) {
-    const char* tile = v.piece(b, h, t);
-    if (tile == nullptr) continue;
-    tile += v.tile_of(t);
-    const int row = t & 15;
-    const uint32_t kc = *reinterpret_cast<const uint16_t*>(tile + row * 64 + 16 * ((c >> 3) & 3) + 4 * (c >> 5) + ((c & 7) >> 1));
-    const uint32_t vc = *reinterpret_cast<const uint16_t*>(tile + 1024 + row * 64 + ((8 * ((c & 31) >> 2) + 2 * (c >> 5)) ^ ((row & 4) << 3)));
-    const uint32_t km = *reinterpret_cast<const uint32_t*>(tile + paged_k_meta(row, G) + 4 * (c / G)), vm = *reinterpret_cast<const uint32_t*>(tile + paged_v_meta(row, G) + 4 * (c / G));
-    float x = 0.f;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) x = fmaf(q[k], fmaf((float)(kc >> (4 * k) & 15u), bf16_half(km, 0), bf16_half(km, 1)), x);
-#pragma unroll
-    for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-    x *= a.scale_log2e;
-    const float top = fmaxf(m, x), f = m == -INFINITY ? 0.f : exp2f(m - top), p = exp2f(x - top);
-    l = l * f + p;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) o[k] = o[k] * f + p * fmaf((float)(vc >> (4 * k) & 15u), bf16_half(vm, 0), bf16_half(vm, 1));
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // blockIdx.x: row of all rows of a KV head's queries, then KV head, then sequence
+  const int most_rows = v.n * v.g, x = blockIdx.x % most_rows, h = blockIdx.x / most_rows % v.Hkv, b = blockIdx.x / most_rows / v.Hkv;
+  const int count = v.count(b);
+  if (x >= count * v.g) return;
+  const int len = v.length(b, v.add_counts ? count : 0), units = max(1, (len + kUnit - 1) / kUnit);
+  const long long total = plan.prefix[v.B];
+  const int parts = (int)plan.prefix[v.B + 1], block = x / plan.rows, row = x - block * plan.rows;
+  const long long lo = plan.prefix[b] + ((long long)h * row_blocks(count, v.g, plan.rows) + block) * units, hi = lo + units;
+  // the thread block whose range has a unit: the last one that begins at or before it
+  auto owner = [&](long long u) {
+    int c = (int)min((long long)parts - 1, u * parts / total);
+    while (c > 0 && split_begin(total, parts, c) > u) --c;
+    while (c + 1 < parts && split_begin(total, parts, c + 1) <= u) ++c;
+    return c;
+  };
+  const int c0 = owner(lo), c1 = owner(hi - 1);
+  if (c0 == c1) return;                          // one thread block had it all
+  __shared__ float join[8][kD + 4];
+  float m = -1e30f, l = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int c = c0 + warp; c <= c1; c += 8) {
+    const float* from = plan.parts + ((size_t)(2 * c + (c == c0 ? 1 : 0)) * plan.rows + row) * kPartFloats;
+    const float2 o01 = *reinterpret_cast<const float2*>(from + 4 * lane), o23 = *reinterpret_cast<const float2*>(from + 4 * lane + 2);
+    const float2 ml = *reinterpret_cast<const float2*>(from + kD);
+    const float top = fmaxf(m, ml.x), f = ex2_approx(m - top), g = ex2_approx(ml.x - top);
     m = top;
+    l = l * f + ml.y * g;
+    y[0] = y[0] * f + o01.x * g;
+    y[1] = y[1] * f + o01.y * g;
+    y[2] = y[2] * f + o23.x * g;
+    y[3] = y[3] * f + o23.y * g;
   }
-  __shared__ float part[4][kD + 2];
+  *reinterpret_cast<float4*>(&join[warp][4 * lane]) = make_float4(y[0], y[1], y[2], y[3]);
   if (lane == 0) {
-    part[warp][kD] = m;
-    part[warp][kD + 1] = l;
+    join[warp][kD] = m;
+    join[warp][kD + 1] = l;
   }
-#pragma unroll
-  for (int k = 0; k < 4; ++k) part[warp][c + k] = o[k];
   __syncthreads();
-  if (warp == 0) {
-    float top = -INFINITY, sum = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < 4; ++k) top = fmaxf(top, part[k][kD]);
-    for (int k = 0; k < 4; ++k) {
-      const float f = part[k][kD + 1] == 0.f ? 0.f : exp2f(part[k][kD] - top);
-      sum += f * part[k][kD + 1];
+  if (warp != 0) return;
+  const int n = min(8, c1 - c0 + 1);
+  float top = -1e30f, sum = 0.f;
+  for (int i = 0; i < n; ++i) top = fmaxf(top, join[i][kD]);
+  y[0] = y[1] = y[2] = y[3] = 0.f;
+  for (int i = 0; i < n; ++i) {
+    const float f = ex2_approx(join[i][kD] - top);
+    sum = fmaf(join[i][kD + 1], f, sum);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] += f * part[k][c + e];
-    }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    if (a.out_bf16)
-      *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + at) = make_uint2(bf16_pair(y[0] * inv, y[1] * inv), bf16_pair(y[2] * inv, y[3] * inv));
-    else
-      *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at) = make_float4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
+    for (int k = 0; k < 4; ++k) y[k] = fmaf(join[i][4 * lane + k], f, y[k]);
   }
+  const int i = x / v.g, head = x - i * v.g;
+  const size_t at = (((size_t)b * v.Hq + h * v.g + head) * v.n + i) * kD + 4 * lane;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  if (a.out_bf16)
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + at) = make_uint2(pack_bf162(y[0] * inv, y[1] * inv), pack_bf162(y[2] * inv, y[3] * inv));
+  else
+    *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at) = make_float4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
+}
+
+constexpr int kMostBlocks = 148 * 4;             // thread blocks of the split kernel: sizes the workspace
+
+using Kernel = void (*)(PagedAttention, Plan);
+Kernel kernel_of(int G, int tiles) {
+  if (tiles == 1) return G == 32 ? pages_kernel<32, 1> : G == 64 ? pages_kernel<64, 1> : pages_kernel<128, 1>;
+  return G == 32 ? pages_kernel<32, 2> : G == 64 ? pages_kernel<64, 2> : pages_kernel<128, 2>;
+}
+int tiles_of(int g, int n) { return g * n <= 8 ? 1 : 2; }
+size_t smem_bytes(int G, int tiles, int B, bool direct) {
+  return (size_t)kWarps * kStages * tiles * 2 * paged_tile_bytes(G) + 8 * kWarps * kStages * tiles + (direct ? 0 : 8 * (size_t)(B + 1));
 }
 
 }  // namespace
 
-size_t paged_workspace_bytes(int, int, int, int) { return 256; }
-cudaError_t paged_attention_setup() { return cudaSuccess; }
+size_t paged_workspace_bytes(int, int g, int batch, int n) {
+  return ((size_t)2 * kMostBlocks * 8 * tiles_of(g, n) * kPartFloats * 4 + 8 * (size_t)(batch + 2) + 15) / 16 * 16;
+}
 
-cudaError_t launch_paged_attention(const PagedAttention& a, int, cudaStream_t stream, int* launches) {
+cudaError_t paged_attention_setup() {
+  for (int G = 32; G <= 128; G *= 2)
+    for (int tiles = 1; tiles <= 2; ++tiles) {
+      const cudaError_t e = cudaFuncSetAttribute(kernel_of(G, tiles), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                 (int)smem_bytes(G, tiles, MIXKVQ_PAGED_MAX_BATCH, false));
+      if (e != cudaSuccess) return e;
+    }
+  return cudaSuccess;
+}
+
+cudaError_t launch_paged_attention(const PagedAttention& a, int n_sms, cudaStream_t stream, int* launches) {
+  const PagedView& v = a.view;
+  const int tiles = tiles_of(v.g, v.n);
+  Plan plan{};
+  plan.rows = 8 * tiles;
+  plan.parts = a.parts;
+  const int most = std::min(kMostBlocks, n_sms * (tiles == 1 ? 4 : 2));
+  plan.prefix = reinterpret_cast<long long*>(a.parts + (size_t)2 * kMostBlocks * plan.rows * kPartFloats);
+  // Sequences whose pages hold few tokens at most: a thread block each, no merge.
+  const long long streams = (long long)v.B * v.Hkv * ((v.n * (long long)v.g + plan.rows - 1) / plan.rows);
+  plan.direct = ((long long)v.max_pages << v.lg_page) <= 4 * kWarps * kUnit;
+  cudaError_t e = launch_dependent(kernel_of(v.G, tiles), dim3((unsigned)(plan.direct ? streams : most)), kWarps * 32, smem_bytes(v.G, tiles, v.B, plan.direct), stream, a,
+                                   plan);
   *launches = 1;
-  return launch_dependent(row_kernel, dim3((unsigned)((long long)a.view.B * a.view.Hq * a.view.n)), 128, 0, stream, a);
+  if (e != cudaSuccess || plan.direct) return e;
+  *launches = 2;
+  return launch_dependent(merge_kernel, dim3((unsigned)((long long)v.B * v.Hkv * v.n * v.g)), 256, 0, stream, a, plan);
 }
 
 }  // namespace mixkvq
