@@ -17,7 +17,7 @@ constexpr int kBatch = 4;
 // Scale, zero-point and codes of a row's groups.  Every lane of the warp calls this; group_lanes = G / 8 neighbouring lanes share a group.
 struct Quantized {
   uint32_t codes;                          // channel i at bits 4 i
-  uint32_t meta;                           // s | z << 16, bf16 bits
+  uint32_t meta;                           // z | s << 16, bf16 bits
 };
 __device__ __forceinline__ Quantized quantize_chunk(uint4 w, int group_lanes) {
   const uint32_t a[4] = {w.x, w.y, w.z, w.w};
@@ -39,7 +39,7 @@ __device__ __forceinline__ Quantized quantize_chunk(uint4 w, int group_lanes) {
   y.codes = 0u;
 #pragma unroll
   for (int i = 0; i < 8; ++i) y.codes |= (uint32_t)quant_code(x[i], lo, s, 15) << (4 * i);
-  y.meta = float_to_bf16_bits_exact(s) | (__float_as_uint(lo) & 0xFFFF0000u);
+  y.meta = (__float_as_uint(lo) >> 16) | (__float_as_uint(s) & 0xFFFF0000u);
   return y;
 }
 
@@ -140,7 +140,7 @@ read_kernel(const __grid_constant__ PagedRead a, int heads_per_block) {
       codes = *reinterpret_cast<const uint16_t*>(tile + 1024 + row * 64 + at) | (uint32_t)*reinterpret_cast<const uint16_t*>(tile + 1024 + row * 64 + at + 8) << 16;
       meta = *reinterpret_cast<const uint32_t*>(tile + paged_v_meta(row, G) + 4 * grp);
     }
-    const float s = bf16_half(meta, 0), z = bf16_half(meta, 1);
+    const float s = bf16_half(meta, 1), z = bf16_half(meta, 0);
     uint32_t y[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j)             // (code times scale is exact: 4 bits by 8)

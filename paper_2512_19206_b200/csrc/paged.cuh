@@ -3,7 +3,7 @@
 //
 // Pool: [layer][page][KV head] pieces of page_tokens tokens, a piece is page_tokens / 16 tiles of 16 tokens:
 //   [K codes 1024 B][V codes 1024 B][K scales 16 x 512/G B][V scales 16 x 512/G B]
-// A token has 64 bytes of codes in each of the two (Eq. 2 with 16 levels per group of G channels) and 128 / G words {s bf16, z bf16}.  Keys: channel
+// A token has 64 bytes of codes in each of the two (Eq. 2 with 16 levels per group of G channels) and 128 / G words {z bf16, s bf16}: the scale above, so that words compare like scales.  Keys: channel
 // c = 32 j + 8 t + i at byte 16 t + 4 j + i / 2, nibble i % 2, so that lane t of a quad finds eight channels of every group of 32 in one 16-byte load, in
 // the order of a matrix operand.  Values: channel c = 32 j + 4 r + x at byte 8 r + 2 j + x / 2, nibble x % 2, the two halves of the 64 bytes swapped in
 // tokens with bit 2 set: the eight bytes that lane group r takes of four tokens lie on different banks.

@@ -6,7 +6,7 @@
 // and sum p z_g is added up in fp32.  One pass over the tokens with a running reference of the logits.
 //
 // Operands stay inside fp16's range whatever the inputs' magnitudes: a query row is scaled by a power of two (exactly) to a largest entry of 2^14 to 2^15, and p s_g by a power of
-// two per group, lowered as larger scales come.  References are raised, and sums rescaled, only when a logit is 4 (in powers of two) above its row's.
+// two per group, lowered as larger scales come.  References are raised, and sums rescaled, only when a logit comes 8 (in powers of two) above the largest so far.
 //
 // Split: work is units of 32 tokens of one (sequence, KV head, block of query rows), all of them in one line, cut evenly over the thread blocks on the device (the
 // lengths are known there alone).  A thread block goes through the pieces of streams in its range, its warps through the units of a piece, each with a ring of
@@ -25,8 +25,10 @@ constexpr int kUnit = 32;                        // tokens
 constexpr int kStages = 2;                       // units in a warp's ring, per tile of 8 query rows
 constexpr int kPartFloats = kD + 2;              // of a row's sums: o[128], reference, denominator
 constexpr uint32_t kPolls = 1u << 21;
-constexpr float kRise = 4.f;                     // a logit this much above the reference raises it
-constexpr float kMostScale = 2048.f;             // of a value scale times its group's factor
+constexpr int kBelow = 16;                       // a reference is brought this much (in powers of two) above its row's largest logit: sums of large values keep off fp32's end
+constexpr int kRise = 8;                         // and raised when a logit comes this much nearer
+constexpr int kScaleTo = 5 + kBelow;             // the largest value scale of a group times its factor is brought to 2^21 .. 2^22, and lowered when it comes to 2^23
+constexpr int kAhead = 8;                        // units that the beginning of a piece counts as
 
 struct Plan {
   int rows;                                      // of a block of query rows
@@ -52,9 +54,12 @@ struct WarpState {
   float zsum[kNG][2 * kNT];                      // sum p z of the lane's tokens
   float ref[2 * kNT], l[2 * kNT];
   float factor[kNG];
+  uint32_t limit[kNG];                           // a word of a larger scale than this lowers the factor
 };
+// the largest word of a scale whose product with 2^e stays below 2^23
+__device__ __forceinline__ uint32_t limit_of(int e) { return ((uint32_t)min(127 + kScaleTo + 2 - e, 254) << 23) - 1u; }
 
-// 16 bytes of metas of a token: the words {s, z} of its groups.
+// The words {z, s} of a token's groups.
 template <int kNG>
 __device__ __forceinline__ void load_meta(uint32_t a, uint32_t (&w)[kNG]) {
   if constexpr (kNG == 4) {
@@ -69,7 +74,7 @@ __device__ __forceinline__ void load_meta(uint32_t a, uint32_t (&w)[kNG]) {
 }
 
 template <int kG, int kNT>
-__global__ void __launch_bounds__(kWarps * 32, kNT == 1 ? 4 : 2)
+__global__ void __launch_bounds__(kWarps * 32, kNT == 1 ? 3 : 2)
 pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ Plan plan) {
   constexpr int kNG = kD / kG, kMeta = 512 / kG, kTileBytes = 2048 + 32 * kMeta, kRows = 8 * kNT, kUnitBytes = 2 * kTileBytes, stages = kStages * kNT;
   extern __shared__ __align__(128) unsigned char smem[];
@@ -94,7 +99,7 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
   } else {
     for (int b = tid; b < v.B; b += kWarps * 32) {
       const int count = v.count(b), len = v.length(b, v.add_counts ? count : 0);
-      prefix[b + 1] = (long long)row_blocks(count, v.g, kRows) * v.Hkv * units_of(len);
+      prefix[b + 1] = (long long)row_blocks(count, v.g, kRows) * v.Hkv * (kAhead + units_of(len));
     }
     if (tid == 0) prefix[0] = 0;
     __syncthreads();
@@ -113,8 +118,8 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
     }
     __syncthreads();
     total = prefix[v.B];
-    // at least a unit for every warp of a thread block
-    parts = (int)min((long long)gridDim.x, max(1ll, (total + kWarps - 1) / kWarps));
+    // at least the beginning of a piece and a unit for every warp
+    parts = (int)min((long long)gridDim.x, max(1ll, (total + kAhead + kWarps - 1) / (kAhead + kWarps)));
     if (blockIdx.x == 0) {
       for (int b = tid; b <= v.B; b += kWarps * 32) plan.prefix[b] = prefix[b];
       if (tid == 0) plan.prefix[v.B + 1] = parts;
@@ -167,12 +172,14 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
       st.len = v.length(st.b, v.add_counts ? st.count : 0);
       st.units = units_of(st.len);
       const long long off = pos - prefix[b_at];
-      const int s = (int)(off / st.units), blocks = row_blocks(st.count, v.g, kRows);
+      const int s = (int)(off / (kAhead + st.units)), blocks = row_blocks(st.count, v.g, kRows);
       st.h = s / blocks;
       st.row0 = (s - st.h * blocks) * kRows;
-      u0 = (int)(off - (long long)s * st.units);
-      u1 = (int)min((long long)st.units, u0 + (end - pos));
-      pos += u1 - u0;
+      const long long first = pos - (off - (long long)s * (kAhead + st.units)) + kAhead;     // where the stream's first unit is in the line
+      u0 = (int)max(0ll, pos - first);
+      u1 = (int)min((long long)st.units, end - first);
+      pos = min(end, first + st.units);
+      if (u1 <= u0) continue;                    // nothing but the beginning
     }
     const bool begins = u0 == 0, whole = begins && u1 == st.units;
     // tokens that the last row of the block sees: units behind them are left out
@@ -181,46 +188,47 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
     const int u_last = min(u1, (most + kUnit - 1) / kUnit);
     const int mine = !dead && u_last > u0 + warp ? (u_last - u0 - warp + kWarps - 1) / kWarps : 0;      // units of the warp: u0 + warp + kWarps i
 
-    // ---- copies: the page numbers of 32 of the warp's units at a time, a lane each (two where a page is half a unit)
-    int id0 = -1, id1 = -1;
-    uint32_t halves = 0;                         // per stage two bits: which half of the unit is there
+    // ---- copies: a lane has one of 32 of the warp's units: where it lies (and the page of its second half where a page is half a unit)
+    const char* src0 = nullptr;
+    int p1 = 0;
+    bool gaps = false;                           // some page so far was none
+    const int32_t* page_row = v.pages + (size_t)st.b * v.pages_stride;
     auto issue = [&](int i) {
-      const int stage = i % stages;
       if ((i & 31) == 0) {
         const int tok = (u0 + warp + kWarps * (i + lane)) * kUnit;
-        const int32_t* row = v.pages + (size_t)st.b * v.pages_stride;
-        id0 = i + lane < mine && tok < most ? row[tok >> v.lg_page] : 0;
-        id1 = v.lg_page == 4 ? (i + lane < mine && tok + 16 < most ? row[(tok + 16) >> 4] : 0) : id0;
-        if (id0 < 0 || id0 >= v.n_pages || id1 < 0 || id1 >= v.n_pages) atomicOr(v.status, (uint32_t)MIXKVQ_DEV_BAD_PAGE);
+        const bool need0 = i + lane < mine, need1 = need0 && tok + 16 < most;
+        const int p0 = need0 && tok < most ? page_row[tok >> v.lg_page] : 0;
+        p1 = v.lg_page == 4 ? (need1 ? page_row[(tok + 16) >> 4] : 0) : p0;
+        const bool bad = p0 < 0 || p0 >= v.n_pages || p1 < 0 || p1 >= v.n_pages;
+        if (bad) atomicOr(v.status, (uint32_t)MIXKVQ_DEV_BAD_PAGE);
+        gaps = gaps || __any_sync(0xffffffffu, bad);
+        src0 = p0 < 0 || p0 >= v.n_pages || tok >= most ? nullptr : v.pool + (uint64_t)(uint32_t)p0 * v.page_bytes + (uint64_t)st.h * v.piece_bytes + v.tile_of(tok);
+        if (p1 >= v.n_pages || !need1) p1 = -1;
       }
-      const int tok = (u0 + warp + kWarps * i) * kUnit;
-      const int p0 = __shfl_sync(0xffffffffu, id0, i & 31), p1 = __shfl_sync(0xffffffffu, id1, i & 31);
-      const bool ok0 = p0 >= 0 && p0 < v.n_pages, ok1 = p1 >= 0 && p1 < v.n_pages && tok + 16 < most;
-      halves = (halves & ~(3u << (2 * stage))) | ((ok0 ? 1u : 0u) | (ok1 ? 2u : 0u)) << (2 * stage);
-      if (lane == 0) {
-        const uint32_t bar = bars + 8u * stage, dst = ring + (uint32_t)(stage * kUnitBytes);
-        const uint32_t bytes = ((ok0 ? 1u : 0u) + (ok1 ? 1u : 0u)) * kTileBytes;
-        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes + (i == 0 ? a.test_extra : 0u)) : "memory");
-        const char* src0 = v.pool + (uint64_t)(uint32_t)p0 * v.page_bytes + (uint64_t)st.h * v.piece_bytes + v.tile_of(tok);
-        const char* src1 = v.pool + (uint64_t)(uint32_t)p1 * v.page_bytes + (uint64_t)st.h * v.piece_bytes + v.tile_of(tok + 16);
-        if (ok0 && ok1 && v.lg_page > 4) {
+      if (lane == (i & 31)) {
+        const uint32_t at = (uint32_t)(i % stages), bar = bars + 8u * at, dst = ring + at * kUnitBytes;
+        const bool ok0 = src0 != nullptr, ok1 = p1 >= 0, one = ok0 && ok1 && v.lg_page > 4;
+        const uint32_t bytes = one ? 2 * kTileBytes : kTileBytes;
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar),
+                     "r"(((ok0 ? 1u : 0u) + (ok1 ? 1u : 0u)) * kTileBytes + (i == 0 ? a.test_extra : 0u))
+                     : "memory");
+        if (ok0)
           asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src0), "r"(bytes), "r"(bar) : "memory");
-        } else {
-          if (ok0)
-            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src0), "r"(kTileBytes), "r"(bar)
-                         : "memory");
-          if (ok1)
-            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst + kTileBytes), "l"(src1), "r"(kTileBytes),
-                         "r"(bar)
-                         : "memory");
+        if (ok1 && !one) {
+          const char* src1 = v.pool + (uint64_t)(uint32_t)p1 * v.page_bytes + (uint64_t)st.h * v.piece_bytes;
+          asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst + kTileBytes), "l"(src1), "r"(kTileBytes),
+                       "r"(bar)
+                       : "memory");
         }
       }
     };
-    for (int i = 0; i < min(stages, mine); ++i) issue(i);
+    int asked = min(stages, mine);               // units asked for
+    for (int i = 0; i < asked; ++i) issue(i);
 
     // ---- queries: lane (r, t) has channels 32 j + 8 t .. + 7 of row r of every row tile as operands
     uint32_t qb[kNT][4][4];                      // word j: {0,4} {2,6} {1,5}/16 {3,7}/16
-    float qsum[kNT][kNG][2], qscale[kNT][2];
+    uint32_t qz[kNT][3];                         // sums of the row's groups as three bf16 terms each: {sum of group t, 0}
+    float qscale[kNT][2];
     int sees[kNT][2];
 #pragma unroll
     for (int nt = 0; nt < kNT; ++nt) {
@@ -267,12 +275,18 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
         part[k] += __shfl_xor_sync(0xffffffffu, part[k], 1);
         part[k] += __shfl_xor_sync(0xffffffffu, part[k], 2);
       }
+      float rest = 0.f;
+#pragma unroll
+      for (int k = 0; k < kNG; ++k) rest = t == k ? part[k] * a.scale_log2e : rest;
+#pragma unroll
+      for (int k = 0; k < 3; ++k) {
+        qz[nt][k] = pack_bf162(rest, 0.f);
+        rest -= bf_lo(qz[nt][k]);
+      }
       // the columns of the lane's products: rows 2 t and 2 t + 1
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const int from = 4 * (2 * t + c);
-#pragma unroll
-        for (int k = 0; k < kNG; ++k) qsum[nt][k][c] = __shfl_sync(0xffffffffu, part[k], from) * a.scale_log2e;
         qscale[nt][c] = a.scale_log2e * (pow2i(-__shfl_sync(0xffffffffu, e, from)) * 16777216.f);
         const int x = st.row0 + 8 * nt + 2 * t + c;
         // (rows that are none are computed like the others and written nowhere)
@@ -291,20 +305,23 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
       for (int k = 0; k < 4 * kNT; ++k) w.acc[i][k] = 0.f;
 #pragma unroll
     for (int i = 0; i < kNG; ++i) {
-      w.factor[i] = pow2i(120);
+      w.factor[i] = pow2i(126);
+      w.limit[i] = limit_of(126);
 #pragma unroll
       for (int k = 0; k < 2 * kNT; ++k) w.zsum[i][k] = 0.f;
     }
 #pragma unroll
     for (int k = 0; k < 2 * kNT; ++k) {
-      w.ref[k] = -1e30f;
+      w.ref[k] = 0.f;
       w.l[k] = 0.f;
     }
+    bool fresh = true;                           // no reference yet: the first tile's largest logits, whatever they are
 
-    // ---- one unit: tokens tok .. tok + 31
-    auto unit = [&](uint32_t base, int tok, uint32_t there, auto masked) {
+    // ---- one unit: tokens tok .. tok + 31.  there: which of its tiles of 16 tokens are
+    auto unit_step = [&](uint32_t base, int tok, uint32_t there, auto masked) {
       constexpr bool kMask = decltype(masked)::value;
-      float x[kNT][2][4];                        // [tile of 16 tokens][row r: columns 2 t, 2 t + 1; row r + 8]
+      // logits above the references; row r: columns 2 t, 2 t + 1, then row r + 8
+      float x[2][kNT][4];
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
         const uint32_t tile = base + m * kTileBytes;
@@ -312,143 +329,155 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
         uint32_t m0[kNG], m1[kNG];
         load_meta<kNG>(tile + 2048 + pi * kMeta, m0);
         load_meta<kNG>(tile + 2048 + (pi + 8) * kMeta, m1);
+        // {z, s} of the lane's group as an operand: the scales meet zeros
+        const uint32_t zt = tile + 2048 + pi * kMeta + 4 * (t % kNG), z0 = lds32(zt), z1 = lds32(zt + 8 * kMeta);
         const uint32_t w0[4] = {k0.x, k0.y, k0.z, k0.w}, w1[4] = {k1.x, k1.y, k1.z, k1.w};
         float sum[kNT][4], zs[kNT][4];
+#pragma unroll
+        for (int nt = 0; nt < kNT; ++nt) {
+          mma_bf16_k8_to(zs[nt], z0, z1, qz[nt][0], -w.ref[2 * nt], -w.ref[2 * nt + 1], -w.ref[2 * nt], -w.ref[2 * nt + 1]);
+          mma_bf16_k8(zs[nt], z0, z1, qz[nt][1]);
+          mma_bf16_k8(zs[nt], z0, z1, qz[nt][2]);
+        }
 #pragma unroll
         for (int g = 0; g < kNG; ++g) {
           float c[kNT][4];
 #pragma unroll
-          for (int nt = 0; nt < kNT; ++nt) c[nt][0] = c[nt][1] = c[nt][2] = c[nt][3] = 0.f;
-#pragma unroll
           for (int j = g * 4 / kNG; j < (g + 1) * 4 / kNG; ++j) {
-            const uint32_t u0w = w0[j], u1w = w1[j], h0 = u0w >> 8, h1 = u1w >> 8;
-            const uint32_t e0 = u0w & 0x000F000Fu, e1 = u1w & 0x000F000Fu, e2 = h0 & 0x000F000Fu, e3 = h1 & 0x000F000Fu;
-            const uint32_t o0 = u0w & 0x00F000F0u, o1 = u1w & 0x00F000F0u, o2 = h0 & 0x00F000F0u, o3 = h1 & 0x00F000F0u;
+            const uint32_t h0 = w0[j] >> 8, h1 = w1[j] >> 8;
+            const uint32_t e0 = w0[j] & 0x000F000Fu, e1 = w1[j] & 0x000F000Fu, e2 = h0 & 0x000F000Fu, e3 = h1 & 0x000F000Fu;
+            const uint32_t o0 = w0[j] & 0x00F000F0u, o1 = w1[j] & 0x00F000F0u, o2 = h0 & 0x00F000F0u, o3 = h1 & 0x00F000F0u;
 #pragma unroll
             for (int nt = 0; nt < kNT; ++nt) {
-              mma_f16(c[nt], e0, e1, e2, e3, qb[nt][j][0], qb[nt][j][1]);
+              if (j == g * 4 / kNG)
+                mma_f16_to(c[nt], e0, e1, e2, e3, qb[nt][j][0], qb[nt][j][1], 0.f, 0.f, 0.f, 0.f);
+              else
+                mma_f16(c[nt], e0, e1, e2, e3, qb[nt][j][0], qb[nt][j][1]);
               mma_f16(c[nt], o0, o1, o2, o3, qb[nt][j][2], qb[nt][j][3]);
             }
           }
-          const float s0 = bf_lo(m0[g]), z0 = bf_hi(m0[g]), s1 = bf_lo(m1[g]), z1 = bf_hi(m1[g]);
+          const float s0 = bf_hi(m0[g]), s1 = bf_hi(m1[g]);
 #pragma unroll
-          for (int nt = 0; nt < kNT; ++nt) {
+          for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const float s = k < 2 ? s0 : s1, z = k < 2 ? z0 : z1, qs = qsum[nt][g][k & 1];
-              sum[nt][k] = g == 0 ? s * c[nt][k] : fmaf(s, c[nt][k], sum[nt][k]);
-              zs[nt][k] = g == 0 ? z * qs : fmaf(z, qs, zs[nt][k]);
-            }
-          }
+            for (int k = 0; k < 4; ++k) sum[nt][k] = g == 0 ? (k < 2 ? s0 : s1) * c[nt][k] : fmaf(k < 2 ? s0 : s1, c[nt][k], sum[nt][k]);
         }
 #pragma unroll
         for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            x[nt][m][k] = fmaf(sum[nt][k], qscale[nt][k & 1], zs[nt][k]);
+            x[m][nt][k] = fmaf(sum[nt][k], qscale[nt][k & 1], zs[nt][k]);
             if constexpr (kMask) {
-              const int at = tok + 16 * m + pi + (k < 2 ? 0 : 8);
-              if (at >= sees[nt][k & 1] || !(there >> m & 1)) x[nt][m][k] = -INFINITY;
+              if (tok + 16 * m + pi + (k < 2 ? 0 : 8) >= sees[nt][k & 1] || !(there >> m & 1)) x[m][nt][k] = -INFINITY;
             }
           }
       }
-      // ---- value scales times their groups' factors, and whether a reference or a factor has to move
-      float sk[2][2][kNG];
-      uint32_t vm[2][2][kNG];
-      float top_s = 0.f;
-#pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        const uint32_t meta = base + m * kTileBytes + 2048 + 16 * kMeta + pi * kMeta;
-        load_meta<kNG>(meta, vm[m][0]);
-        load_meta<kNG>(meta + 8 * kMeta, vm[m][1]);
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
+      // ---- whether a reference or a factor has to move (scales are not negative: words compare like them)
+      auto value_meta = [&](int m, uint32_t (&vm)[2][kNG]) {
+        const uint32_t at = base + m * kTileBytes + 2048 + 16 * kMeta + pi * kMeta;
+        load_meta<kNG>(at, vm[0]);
+        load_meta<kNG>(at + 8 * kMeta, vm[1]);
+        if constexpr (kMask) {                   // what lies behind the last token may be anything
 #pragma unroll
           for (int g = 0; g < kNG; ++g) {
-            if constexpr (kMask) {               // what lies behind the last token may be anything
-              const int at = tok + 16 * m + pi + 8 * h;
-              if (at >= most || !(there >> m & 1)) vm[m][h][g] = 0u;
-            }
-            sk[m][h][g] = bf_lo(vm[m][h][g]) * w.factor[g];
-            top_s = fmaxf(top_s, sk[m][h][g]);
+            if (tok + 16 * m + pi >= most || !(there >> m & 1)) vm[0][g] = 0u;
+            if (tok + 16 * m + pi + 8 >= most || !(there >> m & 1)) vm[1][g] = 0u;
           }
-      }
-      bool move = top_s > kMostScale;
-      float top[2 * kNT];
+        }
+      };
+      uint32_t largest[kNG];
 #pragma unroll
-      for (int c = 0; c < 2 * kNT; ++c) {
-        const int nt = c >> 1, k = c & 1;
-        top[c] = fmaxf(fmaxf(x[nt][0][k], x[nt][0][k + 2]), fmaxf(x[nt][1][k], x[nt][1][k + 2]));
-        move = move || top[c] > w.ref[c] + kRise;
+      for (int m = 0; m < 2; ++m) {
+        uint32_t vm[2][kNG];
+        value_meta(m, vm);
+#pragma unroll
+        for (int g = 0; g < kNG; ++g) largest[g] = m == 0 ? max(vm[0][g], vm[1][g]) : max(largest[g], max(vm[0][g], vm[1][g]));
       }
-      if (__any_sync(0xffffffffu, move)) {
+      bool move = false;
+#pragma unroll
+      for (int g = 0; g < kNG; ++g) move = move || largest[g] > w.limit[g];
+      float above = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 2 * kNT; ++i) {
+        const float* y = x[i & 1][i >> 1];
+        above = fmaxf(fmaxf(above, fmaxf(y[0], y[1])), fmaxf(y[2], y[3]));
+      }
+      if (__any_sync(0xffffffffu, move || fresh || above > kRise - kBelow)) {
 #pragma unroll
         for (int c = 0; c < 2 * kNT; ++c) {
+          const int nt = c >> 1, k = c & 1;
+          float up = fmaxf(fmaxf(x[0][nt][k], x[0][nt][k + 2]), fmaxf(x[1][nt][k], x[1][nt][k + 2]));
 #pragma unroll
-          for (int d = 4; d < 32; d <<= 1) top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], d));
-          const float up = fmaxf(w.ref[c], top[c]), f = ex2_approx(w.ref[c] - up);
-          w.ref[c] = up;
+          for (int d = 4; d < 32; d <<= 1) up = fmaxf(up, __shfl_xor_sync(0xffffffffu, up, d));
+          // (a row moves by its own logits alone: its result does not depend on the rows beside it)
+          up = up > kRise - kBelow || (fresh && up > -INFINITY) ? up + kBelow : 0.f;
+          const float f = ex2_approx(-up);
+          w.ref[c] += up;
+#pragma unroll
+          for (int m = 0; m < 2; ++m) {
+            x[m][nt][k] -= up;
+            x[m][nt][k + 2] -= up;
+          }
           w.l[c] *= f;
 #pragma unroll
           for (int g = 0; g < kNG; ++g) w.zsum[g][c] *= f;
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            w.acc[i][4 * (c >> 1) + (c & 1)] *= f;
-            w.acc[i][4 * (c >> 1) + (c & 1) + 2] *= f;
+            w.acc[i][4 * nt + k] *= f;
+            w.acc[i][4 * nt + k + 2] *= f;
           }
         }
 #pragma unroll
         for (int g = 0; g < kNG; ++g) {
-          uint32_t s = 0;                        // the largest finite scale of the group, as bits (scales are not negative)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t y = vm[i >> 1][i & 1][g] << 16 & 0x7FFFFFFFu;
-            s = y < 0x7F800000u ? max(s, y) : s;
-          }
-          s = __reduce_max_sync(0xffffffffu, s);
-          if (__uint_as_float(s) * w.factor[g] > kMostScale) {
-            const float down = pow2i(min(max(9 + 127 - (int)(s >> 23), -118), 120)), f = down / w.factor[g];
+          // the largest scale of the group; one that is not finite moves nothing (its products are not finite whatever the factor)
+          uint32_t s = largest[g] & 0xFFFF0000u;
+          s = __reduce_max_sync(0xffffffffu, s < 0x7F800000u ? s : 0u);
+          if (s > w.limit[g]) {
+            const int e = min(max(kScaleTo + 127 - (int)(s >> 23), -122), 126);
+            const float down = pow2i(e), f = down / w.factor[g];
             w.factor[g] = down;
+            w.limit[g] = limit_of(e);
 #pragma unroll
             for (int i = g * 8 / kNG; i < (g + 1) * 8 / kNG; ++i)
 #pragma unroll
               for (int k = 0; k < 4 * kNT; ++k) w.acc[i][k] *= f;
           }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) sk[i >> 1][i & 1][g] = bf_lo(vm[i >> 1][i & 1][g]) * w.factor[g];
         }
+        fresh = fresh && there == 0;
       }
       // ---- weights and the second product
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
-        const uint32_t tile = base + m * kTileBytes + 1024;
-        uint2 vw[4];                             // tokens of the operand's columns 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+        const uint32_t tile = base + m * kTileBytes;
+        uint32_t vm[2][kNG];
+        value_meta(m, vm);
+        uint2 vw[4];                               // tokens of the operand's columns 2 t, 2 t + 1, 2 t + 8, 2 t + 9
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int row = 2 * t + (i & 1), token = (row ^ (row >> 1 & 1)) + 8 * (i >> 1);
-          vw[i] = lds64(tile + token * 64 + ((8 * r) ^ ((token & 4) << 3)));
+          vw[i] = lds64(tile + 1024 + token * 64 + ((8 * r) ^ ((token & 4) << 3)));
         }
         float p[kNT][4];
 #pragma unroll
         for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            p[nt][k] = ex2_approx(x[nt][m][k] - w.ref[2 * nt + (k & 1)]);
+            p[nt][k] = ex2_approx(x[m][nt][k]);
             w.l[2 * nt + (k & 1)] += p[nt][k];
           }
 #pragma unroll
         for (int g = 0; g < kNG; ++g) {
           uint32_t ub[kNT][2];
+          const float sk[2] = {bf_hi(vm[0][g]) * w.factor[g], bf_hi(vm[1][g]) * w.factor[g]}, zv[2] = {bf_lo(vm[0][g]), bf_lo(vm[1][g])};
 #pragma unroll
           for (int nt = 0; nt < kNT; ++nt) {
             float u[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              const float z = bf_hi(vm[m][k >> 1][g]);
-              float pz = p[nt][k] * z;
-              u[k] = p[nt][k] * sk[m][k >> 1][g];
-              if constexpr (kMask) {             // a row that does not see a token takes nothing of it, an infinity neither
-                if (x[nt][m][k] == -INFINITY) u[k] = pz = 0.f;
+              float pz = p[nt][k] * zv[k >> 1];
+              u[k] = p[nt][k] * sk[k >> 1];
+              if constexpr (kMask) {               // a row that does not see a token takes nothing of it, an infinity neither
+                if (x[m][nt][k] == -INFINITY) u[k] = pz = 0.f;
               }
               w.zsum[g][2 * nt + (k & 1)] += pz;
             }
@@ -464,8 +493,7 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
 #pragma unroll
             for (int nt = 0; nt < kNT; ++nt) {
               mma_f16(reinterpret_cast<float(&)[4]>(w.acc[2 * j][4 * nt]), ab & 0x000F000Fu, ab8 & 0x000F000Fu, cd & 0x000F000Fu, cd8 & 0x000F000Fu, ub[nt][0], ub[nt][1]);
-              mma_f16(reinterpret_cast<float(&)[4]>(w.acc[2 * j + 1][4 * nt]), ab & 0x00F000F0u, ab8 & 0x00F000F0u, cd & 0x00F000F0u, cd8 & 0x00F000F0u, ub[nt][0],
-                      ub[nt][1]);
+              mma_f16(reinterpret_cast<float(&)[4]>(w.acc[2 * j + 1][4 * nt]), ab & 0x00F000F0u, ab8 & 0x00F000F0u, cd & 0x00F000F0u, cd8 & 0x00F000F0u, ub[nt][0], ub[nt][1]);
             }
           }
         }
@@ -474,27 +502,31 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
     int done = 0;                                // units waited for
     for (; done < mine; ++done) {
       const int stage = done % stages, tok = (u0 + warp + kWarps * done) * kUnit;
-      const uint32_t there = halves >> (2 * stage) & 3u;
+      uint32_t there = tok + 16 < most ? 3u : 1u;
+      if (gaps) {
+        const int q0 = page_row[tok >> v.lg_page], q1 = there == 3u ? page_row[(tok + 16) >> v.lg_page] : -1;
+        there = (q0 >= 0 && q0 < v.n_pages ? 1u : 0u) | (q1 >= 0 && q1 < v.n_pages ? 2u : 0u);
+      }
       wait(bars + 8u * stage, phase >> stage & 1u);
       if (dead) break;
       phase ^= 1u << stage;
       const uint32_t base = ring + (uint32_t)(stage * kUnitBytes);
-      if (tok + kUnit > fewest || there != 3u)
-        unit(base, tok, there, std::true_type{});
-      else
-        unit(base, tok, there, std::false_type{});
+      if (tok + kUnit > fewest || there != 3u) {
+        unit_step(base, tok, there, std::true_type{});
+      } else {
+        unit_step(base, tok, 3u, std::false_type{});
+      }
       __syncwarp();
-      if (done + stages < mine) issue(done + stages);
+      if (asked < mine) issue(asked++);
     }
     if (dead) {
       // what is under way is waited for, and the piece is left without this warp's part
-      for (int i = done; i < min(mine, done + stages); ++i) {
+      for (int i = done; i < asked; ++i) {
         const int stage = i % stages;
         wait(bars + 8u * stage, phase >> stage & 1u);
       }
 #pragma unroll
       for (int k = 0; k < 2 * kNT; ++k) {
-        w.ref[k] = -1e30f;
         w.l[k] = 0.f;
 #pragma unroll
         for (int g = 0; g < kNG; ++g) w.zsum[g][k] = 0.f;
@@ -512,6 +544,7 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
 #pragma unroll
         for (int g = 0; g < kNG; ++g) w.zsum[g][k] += __shfl_xor_sync(0xffffffffu, w.zsum[g][k], d);
       }
+      if (w.l[k] == 0.f) w.ref[k] = -1e30f;      // nothing seen
     }
     constexpr int kStride = kD + 4;
     __syncwarp();
@@ -580,17 +613,16 @@ merge_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
   dependency_wait();
   const PagedView& v = a.view;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  // blockIdx.x: row of all rows of a KV head's queries, then KV head, then sequence
-  const int most_rows = v.n * v.g, x = blockIdx.x % most_rows, h = blockIdx.x / most_rows % v.Hkv, b = blockIdx.x / most_rows / v.Hkv;
+  const int x = blockIdx.x, h = blockIdx.y, b = blockIdx.z;      // row of a KV head's queries, KV head, sequence
   const int count = v.count(b);
   if (x >= count * v.g) return;
   const int len = v.length(b, v.add_counts ? count : 0), units = max(1, (len + kUnit - 1) / kUnit);
   const long long total = plan.prefix[v.B];
   const int parts = (int)plan.prefix[v.B + 1], block = x / plan.rows, row = x - block * plan.rows;
-  const long long lo = plan.prefix[b] + ((long long)h * row_blocks(count, v.g, plan.rows) + block) * units, hi = lo + units;
-  // the thread block whose range has a unit: the last one that begins at or before it
+  const long long lo = plan.prefix[b] + ((long long)h * row_blocks(count, v.g, plan.rows) + block) * (kAhead + units) + kAhead, hi = lo + units;
+  // the thread block whose range has a unit: the last one that begins at or before it (the quotient is off by one at most, in either direction)
   auto owner = [&](long long u) {
-    int c = (int)min((long long)parts - 1, u * parts / total);
+    int c = (int)min((long long)parts - 1, (long long)((double)u * parts / (double)total));
     while (c > 0 && split_begin(total, parts, c) > u) --c;
     while (c + 1 < parts && split_begin(total, parts, c + 1) <= u) ++c;
     return c;
@@ -671,7 +703,7 @@ cudaError_t launch_paged_attention(const PagedAttention& a, int n_sms, cudaStrea
   Plan plan{};
   plan.rows = 8 * tiles;
   plan.parts = a.parts;
-  const int most = std::min(kMostBlocks, n_sms * (tiles == 1 ? 4 : 2));
+  const int most = std::min(kMostBlocks, n_sms * (tiles == 1 ? 3 : 2));
   plan.prefix = reinterpret_cast<long long*>(a.parts + (size_t)2 * kMostBlocks * plan.rows * kPartFloats);
   // Sequences whose pages hold few tokens at most: a thread block each, no merge.
   const long long streams = (long long)v.B * v.Hkv * ((v.n * (long long)v.g + plan.rows - 1) / plan.rows);
@@ -681,7 +713,7 @@ cudaError_t launch_paged_attention(const PagedAttention& a, int n_sms, cudaStrea
   *launches = 1;
   if (e != cudaSuccess || plan.direct) return e;
   *launches = 2;
-  return launch_dependent(merge_kernel, dim3((unsigned)((long long)v.B * v.Hkv * v.n * v.g)), 256, 0, stream, a, plan);
+  return launch_dependent(merge_kernel, dim3((unsigned)(v.n * v.g), (unsigned)v.Hkv, (unsigned)v.B), 256, 0, stream, a, plan);
 }
 
 }  // namespace mixkvq

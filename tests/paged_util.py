@@ -45,7 +45,7 @@ def token_bytes(x, G, values_of, row):
         else:
             at = 16 * (ch // 8 % 4) + 4 * j + ch % 8 // 2
         out[at] |= c[ch] << (4 * (ch % 2))
-    meta = np.stack([O.bf16_to_u16(s), O.bf16_to_u16(z)], -1).astype("<u2").tobytes()
+    meta = np.stack([O.bf16_to_u16(z), O.bf16_to_u16(s)], -1).astype("<u2").tobytes()
     return out.tobytes(), meta
 
 
@@ -89,8 +89,9 @@ def reference(q, k, v, G, scale, sees):
 
     Logits: keys' codes and queries enter exactly; sums of 128 products in fp32 and of the groups' parts lose at most 2^-19 of the sum of the magnitudes |q| (15 s + |z|)
     (fewer than 16 roundings or truncations of 2^-23 each); a deviation d of all logits moves the output by at most 2 d max |v - o|.
-    Weights: p s is rounded to fp16 once per token and group: by 2^-11 of itself, so the output by 2^-11 sum p 15 s; below 2^-14 of its range (that is, of 2^-23 of the
-    largest s) by 2^-34 of the largest s, which p >= 2^-4 of the row's largest turns into 2^-30 per token seen.  Sums in fp32: 2^-18 of sum p (15 s + |z|)."""
+    Weights: p s is rounded to fp16 once per token and group, times a power of two that brings the group's largest s to 2^5 at least: by 2^-11 of itself, so the output
+    by 2^-11 sum p 15 s; where that is below 2^-14 by 2^-25, 2^-30 of the largest s, so by 2^-26 of it per token and code (the reference is never above a row's largest
+    logit, its denominator at least 1).  Sums in fp32: 2^-18 of sum p (15 s + |z|)."""
     kc, ks, kz = quantized(k, G)
     vc, vs, vz = quantized(v, G)
     K, V = torch.from_numpy(values(kc, ks, kz)), torch.from_numpy(values(vc, vs, vz))
@@ -110,7 +111,7 @@ def reference(q, k, v, G, scale, sees):
     s15 = torch.from_numpy(np.repeat(15.0 * vs.astype(np.float64), G, -1))
     s15 = torch.where(torch.isfinite(s15), s15, 0.0)
     biggest = float(s15.max()) if T else 0.0
-    tol = 2 * d * (V.abs().max() if T else 0.0) + HALF_STEP * (p @ s15) + 2.0 ** -30 * biggest * T + 2.0 ** -18 * (p @ torch.nan_to_num(reach(vs, vz), 0.0, 0.0, 0.0))
+    tol = 2 * d * (V.abs().max() if T else 0.0) + HALF_STEP * (p @ s15) + 2.0 ** -26 * biggest * T + 2.0 ** -18 * (p @ torch.nan_to_num(reach(vs, vz), 0.0, 0.0, 0.0))
     return out, tol
 
 
