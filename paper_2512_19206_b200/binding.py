@@ -127,7 +127,7 @@ def lib():
         L.mixkvq_rope_partial.argtypes = [vp, vp, vp, vp, i64s, i32, rot, vp, vp, vp, vp]
         L.mixkvq_rope_tables.argtypes = [C.POINTER(RopeScaling), C.c_int64, i32, vp, vp, vp]
         L.mixkvq_paged_bytes.argtypes = [C.POINTER(PagedConfig), C.POINTER(C.c_size_t)]
-        L.mixkvq_paged_workspace_bytes.argtypes = [C.POINTER(PagedConfig), i32, i32]
+        L.mixkvq_paged_workspace_bytes.argtypes = [C.POINTER(PagedConfig), i32, i32, i32]
         L.mixkvq_paged_init.argtypes = [C.POINTER(PagedConfig), vp, C.c_size_t, vp, C.POINTER(vp)]
         L.mixkvq_paged_destroy.argtypes = L.mixkvq_paged_launch_count.argtypes = [vp]
         L.mixkvq_paged_append.argtypes = [vp, i32, seqs, vp, vp, vp, i64s, rot, vp, vp]
@@ -710,7 +710,7 @@ class PagedCache:
         ptr = lambda t: None if t is None else t.data_ptr()                                        # noqa: E731
         return (self.handle.value, layer, *seqs, k.data_ptr(), v.data_ptr(), ptr(q), strides, *turn, ptr(q_out)), q_out
 
-    def _out(self, name, q, counts, out, workspace, dtype):
+    def _out(self, name, q, max_pages, counts, out, workspace, dtype):
         dev, shape = self.mem.device, q.shape
         if out is None:
             if dtype not in _OUT_TYPES:
@@ -719,7 +719,7 @@ class PagedCache:
         elif out.shape != shape or out.dtype not in _OUT_TYPES or not out.is_contiguous() or out.device != dev:
             raise ValueError(f"{name}: out must be a contiguous float32 or bfloat16 {list(shape)} tensor on {dev}")
         if workspace is None:
-            workspace = torch.empty(self.workspace_bytes(shape[0], shape[2]), dtype=torch.uint8, device=dev)
+            workspace = torch.empty(self.workspace_bytes(shape[0], shape[2], max_pages), dtype=torch.uint8, device=dev)
         elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != dev:
             raise ValueError(f"{name}: the workspace must be a contiguous uint8 tensor on {dev}")
         return out, workspace
@@ -756,13 +756,13 @@ class PagedCache:
     def attention(self, layer, q, pages, lens, scale, counts=None, out=None, dtype=torch.float32, workspace=None):
         """The newest n (counts[b]) tokens of every sequence, which has lens[b] tokens with them, attend to its pages, causally among themselves: q [B,Hq,n,128]
         bf16 (rotated, as append returns it) -> [B,Hq,n,128].  `out`: float32 or bfloat16 (allocated as `dtype` when absent, zeros behind the counts).
-        `workspace`: a uint8 tensor of at least workspace_bytes(B, n) bytes (allocated here when absent)."""
+        `workspace`: a uint8 tensor of at least workspace_bytes(B, n, pages.shape[1]) bytes (allocated here when absent)."""
         n, dev = q.shape[2] if q.dim() == 4 else 0, self.mem.device
         seqs = self._sequences("attention", n, pages, lens, counts)
         self._rows("attention", seqs[0], n, q=q)
         if not q.is_contiguous():
             raise ValueError("attention: q must be contiguous")
-        out, workspace = self._out("attention", q, counts, out, workspace, dtype)
+        out, workspace = self._out("attention", q, pages.shape[1], counts, out, workspace, dtype)
         call = (_native or _calls()).paged_attention
         with _device_of(dev):
             code = call(self.handle.value, layer, *seqs, q.data_ptr(), out.data_ptr(), _OUT_TYPES[out.dtype], scale, workspace.data_ptr(), workspace.numel(), _stream())
@@ -776,7 +776,7 @@ class PagedCache:
         if q is None:
             raise ValueError("step: queries are needed")
         args, q_out = self._append_args("step", layer, k, v, q, pages, lens, counts, cos, sin, positions, interleaved, q_out)
-        out, workspace = self._out("step", q_out, counts, out, workspace, dtype)
+        out, workspace = self._out("step", q_out, pages.shape[1], counts, out, workspace, dtype)
         call = (_native or _calls()).paged_step
         with _device_of(self.mem.device):
             code = call(*args, out.data_ptr(), _OUT_TYPES[out.dtype], scale, workspace.data_ptr(), workspace.numel(), _stream())
@@ -784,8 +784,9 @@ class PagedCache:
             raise MixKVQError(code, "mixkvq_paged_step")
         return out
 
-    def workspace_bytes(self, batch, n_tokens):
-        return int(lib().mixkvq_paged_workspace_bytes(C.byref(self.cfg), int(batch), int(n_tokens)))
+    def workspace_bytes(self, batch, n_tokens, max_pages):
+        """Bytes of the workspace of an attention or step of `batch` sequences, n_tokens each at most, with a page table of max_pages columns."""
+        return int(lib().mixkvq_paged_workspace_bytes(C.byref(self.cfg), int(batch), int(n_tokens), int(max_pages)))
 
     def status(self) -> int:
         s = C.c_int()

@@ -19,7 +19,7 @@ LIB = os.path.join(HERE, "libmixkvq.so")
 # the interpreter's own suffix: another Python version finds no module of its own here and builds one
 CALLS = os.path.join(HERE, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["api.cu", "append.cu", "rope.cu", "prefill.cu", "chunk.cu", "select.cu", "flush.cu", "combine.cu", "attention_simt.cu", "attention_ws.cu", "attention_single.cu",
-           "attention_tc.cu", "rope_partial.cu", "paged.cu", "paged_attention.cu", "paged_api.cu"]
+           "attention_tc.cu", "rope_partial.cu", "paged.cu", "paged_attention.cu", "paged_chunk.cu", "paged_api.cu"]
 FLAGS = ["-Xcompiler", "-fPIC", "-O3", "-std=c++17", "-lineinfo", "-gencode", "arch=compute_100a,code=sm_100a",
          "--fmad=true"]
 

@@ -111,7 +111,12 @@ struct RopeTables {
 cudaError_t launch_paged_append(const PagedAppend& a, int n_sms, cudaStream_t stream);
 cudaError_t launch_paged_read(const PagedRead& a, int n_sms, cudaStream_t stream);
 cudaError_t launch_paged_attention(const PagedAttention& a, int n_sms, cudaStream_t stream, int* launches);
-size_t paged_workspace_bytes(int Hkv, int g, int batch, int n);
+size_t paged_workspace_bytes(int Hkv, int g, int batch, int n, long long capacity);
+// many query rows (tcgen05); capacity: tokens that the pages of a sequence hold at most
+bool paged_chunk_fits(long long capacity);
+size_t paged_chunk_workspace_bytes(int Hkv, int batch, long long capacity);
+cudaError_t paged_chunk_setup();
+cudaError_t launch_paged_chunk(const PagedAttention& a, int n_sms, cudaStream_t stream, int* launches);
 cudaError_t paged_attention_setup();
 cudaError_t launch_rope_partial(const RopePartial& a, int n_sms, cudaStream_t stream);
 cudaError_t launch_rope_tables(const RopeTables& a, int n_sms, cudaStream_t stream);

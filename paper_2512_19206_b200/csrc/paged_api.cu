@@ -112,7 +112,7 @@ int plan_attention(const mixkvq_paged* h, int layer, const mixkvq_paged_sequence
     return MIXKVQ_E_INVALID_ARG;
   if (!aligned16(q_dev) || !aligned16(out_dev) || !aligned16(workspace_dev)) return MIXKVQ_E_ALIGNMENT;
   if ((long long)s->batch * s->n_tokens * h->cfg.n_q_heads > 0x7FFFFFFFll) return MIXKVQ_E_UNSUPPORTED;      // (thread blocks of a grid)
-  const size_t need = paged_workspace_bytes(h->cfg.n_kv_heads, h->g, s->batch, s->n_tokens);
+  const size_t need = paged_workspace_bytes(h->cfg.n_kv_heads, h->g, s->batch, s->n_tokens, (long long)s->max_pages * h->cfg.page_tokens);
   if (workspace_bytes < need) return MIXKVQ_E_BUFFER_TOO_SMALL;
   const size_t rows = (size_t)s->batch * h->cfg.n_q_heads * s->n_tokens * kD;
   Ranges r;
@@ -202,9 +202,9 @@ int mixkvq_paged_bytes(const mixkvq_paged_config* cfg, size_t* pool_bytes) {
   return MIXKVQ_OK;
 }
 
-size_t mixkvq_paged_workspace_bytes(const mixkvq_paged_config* cfg, int batch, int n_tokens) {
-  if (check_config(cfg) != MIXKVQ_OK || batch < 1 || n_tokens < 1) return 0;
-  return paged_workspace_bytes(cfg->n_kv_heads, cfg->n_q_heads / cfg->n_kv_heads, batch, n_tokens);
+size_t mixkvq_paged_workspace_bytes(const mixkvq_paged_config* cfg, int batch, int n_tokens, int max_pages) {
+  if (check_config(cfg) != MIXKVQ_OK || batch < 1 || n_tokens < 1 || max_pages < 1 || (long long)max_pages * cfg->page_tokens > MIXKVQ_PAGED_MAX_TOKENS) return 0;
+  return paged_workspace_bytes(cfg->n_kv_heads, cfg->n_q_heads / cfg->n_kv_heads, batch, n_tokens, (long long)max_pages * cfg->page_tokens);
 }
 
 int mixkvq_paged_init(const mixkvq_paged_config* cfg, void* pool_dev, size_t bytes, void* stream, mixkvq_paged** out) {

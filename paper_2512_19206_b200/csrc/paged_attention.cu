@@ -669,6 +669,7 @@ merge_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
     *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at) = make_float4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
 }
 
+constexpr int kUnpackRows = 128;                 // query rows of a KV head above which unpacking pays
 constexpr int kMostBlocks = 148 * 4;             // thread blocks of the split kernel: sizes the workspace
 
 using Kernel = void (*)(PagedAttention, Plan);
@@ -683,7 +684,11 @@ size_t smem_bytes(int G, int tiles, int B, bool direct) {
 
 }  // namespace
 
-size_t paged_workspace_bytes(int, int g, int batch, int n) {
+// Whether a call goes to the kernel that unpacks the pages once for all query rows.
+static bool unpacks(int g, int n, long long capacity) { return (long long)g * n > kUnpackRows && paged_chunk_fits(capacity); }
+
+size_t paged_workspace_bytes(int Hkv, int g, int batch, int n, long long capacity) {
+  if (unpacks(g, n, capacity)) return paged_chunk_workspace_bytes(Hkv, batch, capacity);
   return ((size_t)2 * kMostBlocks * 8 * tiles_of(g, n) * kPartFloats * 4 + 8 * (size_t)(batch + 2) + 15) / 16 * 16;
 }
 
@@ -694,11 +699,13 @@ cudaError_t paged_attention_setup() {
                                                  (int)smem_bytes(G, tiles, MIXKVQ_PAGED_MAX_BATCH, false));
       if (e != cudaSuccess) return e;
     }
-  return cudaSuccess;
+  return paged_chunk_setup();
 }
 
 cudaError_t launch_paged_attention(const PagedAttention& a, int n_sms, cudaStream_t stream, int* launches) {
   const PagedView& v = a.view;
+  *launches = 0;
+  if (unpacks(v.g, v.n, (long long)v.max_pages << v.lg_page)) return launch_paged_chunk(a, n_sms, stream, launches);
   const int tiles = tiles_of(v.g, v.n);
   Plan plan{};
   plan.rows = 8 * tiles;

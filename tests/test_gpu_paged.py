@@ -117,7 +117,8 @@ CASES = [
     (1, 1, [1], [1], 16, 32), (1, 1, [31], [1], 16, 128), (7, 1, [33, 1, 16], [1, 1, 1], 16, 64), (28, 4, [300, 17, 512], [1, 1, 1], 64, 32),
     (32, 8, [1000], [1], 128, 64), (8, 8, [65, 64, 63], [1, 1, 1], 32, 128), (40, 8, [257, 700], [1, 0], 256, 128), (8, 1, [5000], [1], 64, 32),
     (28, 4, [40, 3, 700], [5, 3, 2], 64, 32), (5, 1, [200, 9], [8, 9], 16, 64), (32, 8, [333], [33], 128, 128), (16, 2, [130, 500], [130, 77], 32, 32),
-    (6, 2, [600, 129], [300, 129], 64, 64),
+    (6, 2, [600, 129], [300, 129], 64, 64), (28, 4, [1000, 40, 0, 257], [200, 40, 0, 256], 128, 32), (1, 1, [700], [129], 16, 128), (8, 1, [2100, 5], [700, 1], 256, 64),
+    (7, 7, [300, 1500], [150, 300], 32, 32),
 ]
 
 
@@ -136,18 +137,19 @@ def test_attention(binding, Hq, Hkv, lens, counts, page, G, dtype):
         assert torch.equal(cache.attention(1, q.cuda(), table.cuda(), ints(lens), SCALE, dtype=dtype), out)
 
 
-def test_rows_that_see_nothing(binding):
+@pytest.mark.parametrize("n", [5, 70])
+def test_rows_that_see_nothing(binding, n):
     """A sequence without tokens, and query rows in front of a sequence's first token, are zeros."""
     cache, table, k, v = filled(binding, 4, 2, [0, 3, 70], 16, 32, 2)
-    q, _, _ = P.draw(3, 4, 2, 5, 8)
+    q, _, _ = P.draw(3, 4, 2, n, 8)
     out = cache.attention(0, q.cuda(), table.cuda(), ints([0, 3, 70]), SCALE)
     assert cache.status() == 0
-    assert (out[0] == 0).all() and (out[1, :, :2] == 0).all()
-    P.check(out, q, k, v, 32, SCALE, [0, 3, 70], [0, 5, 5])
+    assert (out[0] == 0).all() and (out[1, :, :n - 3] == 0).all()
+    P.check(out, q, k, v, 32, SCALE, [0, 3, 70], [0, n, n])
 
 
 @pytest.mark.parametrize("size", [1e-30, 1e-6, 1e3, 1e20, 1e36])
-@pytest.mark.parametrize("n", [1, 4])
+@pytest.mark.parametrize("n", [1, 4, 40])
 def test_magnitudes(binding, size, n):
     """Values and keys of any magnitude: the softmax's input stays ordinary (queries shrink as keys grow), the output grows with the values."""
     lens = [90, 400]
@@ -161,7 +163,7 @@ def test_magnitudes(binding, size, n):
     P.check(out, q, k, v, 32, SCALE, lens, [n, n])
 
 
-@pytest.mark.parametrize("n", [1, 3])
+@pytest.mark.parametrize("n", [1, 3, 90])
 def test_peaked_and_flat_softmax(binding, n):
     """One key that takes all, logits that rise along the sequence, and equal logits."""
     lens = [500, 500, 500]
@@ -176,10 +178,11 @@ def test_peaked_and_flat_softmax(binding, n):
     P.check(cache.attention(0, q.cuda(), table.cuda(), ints(lens), SCALE), q, k, v, 32, SCALE, lens, [n] * 3)
 
 
-def test_nan_and_infinity_stay_where_they_are(binding):
+@pytest.mark.parametrize("n", [2, 50])
+def test_nan_and_infinity_stay_where_they_are(binding, n):
     """A NaN among the queries reaches its own row, an infinite value its group's channels of the rows that see it."""
     cache, table, k, v = filled(binding, 8, 2, [200, 60], 32, 32, 21)
-    q, _, _ = P.draw(2, 8, 2, 2, 22)
+    q, _, _ = P.draw(2, 8, 2, n, 22)
     ref = cache.attention(0, q.cuda(), table.cuda(), ints([200, 60]), SCALE)
     bad = q.clone()
     bad[0, 3, 0, 5] = float("nan")
@@ -191,10 +194,41 @@ def test_nan_and_infinity_stay_where_they_are(binding):
     vi[1, 1, 59, 40] = float("inf")                                        # the newest token of sequence 1: its second row sees it
     cache.append(0, k.cuda(), vi.cuda(), table.cuda(), ints([0, 0]), counts=ints([200, 60]))
     out = cache.attention(0, q.cuda(), table.cuda(), ints([200, 60]), SCALE)
-    assert not torch.isfinite(out[1, 4:, 1, 32:64]).any()
-    out[1, 4:, 1, 32:64] = ref[1, 4:, 1, 32:64]
+    assert not torch.isfinite(out[1, 4:, n - 1, 32:64]).any()
+    out[1, 4:, n - 1, 32:64] = ref[1, 4:, n - 1, 32:64]
     assert torch.isfinite(out).all()
-    P.check(out, q, k, v, 32, SCALE, [200, 60], [2, 2])
+    P.check(out, q, k, v, 32, SCALE, [200, 60], [n, n])
+    ki = k.clone()
+    ki[1, 0, 58, 7] = float("inf")                                         # a key: the last two rows of its heads
+    cache.append(0, ki.cuda(), v.cuda(), table.cuda(), ints([0, 0]), counts=ints([200, 60]))
+    out = cache.attention(0, q.cuda(), table.cuda(), ints([200, 60]), SCALE)
+    assert not torch.isfinite(out[1, :4, n - 2:]).any()
+    out[1, :4, n - 2:] = ref[1, :4, n - 2:]
+    assert torch.isfinite(out).all()
+    P.check(out, q, k, v, 32, SCALE, [200, 60], [n, n])
+
+
+def test_bad_pages_of_many_rows(binding):
+    """The kernel for many query rows leaves out the tokens of pages that are none, too."""
+    cache, table, k, v = filled(binding, 8, 1, [400, 300], 16, 32, 33)
+    q, _, _ = P.draw(2, 8, 1, 30, 34)
+    wrong = table.clone()
+    wrong[0, 3], wrong[0, 9], wrong[1, 18] = -1, cache.cfg.n_pages, -7
+    out = cache.attention(0, q.cuda(), wrong.cuda(), ints([400, 300]), SCALE)
+    assert cache.status() == binding.DEV_BAD_PAGE
+    for b, gone in ((0, (3, 9)), (1, (18,))):
+        keep = [t for t in range([400, 300][b]) if t // 16 not in gone]
+        late = 30 if b == 0 else 17                                        # rows that see more or fewer of the page left out are compared up to there
+        at = 0 if b == 0 else 17
+        if b == 0:
+            P.check(out[:1], q[:1], k[:1, :, keep], v[:1, :, keep], 32, SCALE, [len(keep)], [late])
+        else:
+            x = q[1:, :, :at].contiguous()
+            # the first rows of sequence 1 (tokens 270 .. 286) do not reach page 18 (tokens 288 ..)
+            for i in range(at):
+                ref, tol = P.reference(x[0, :, i:i + 1], k[1, 0, :271 + i], v[1, 0, :271 + i], 32, SCALE, [271 + i], 240)
+                assert ((out[1, :, i:i + 1].double().cpu() - ref).abs() <= tol + 2.0 ** -24 * ref.abs()).all()
+    assert torch.isfinite(out).all()
 
 
 def test_bad_pages_and_lengths(binding):
@@ -260,7 +294,7 @@ def test_steps_are_append_then_attention(binding):
         c.append(0, k.cuda(), v.cuda(), pages, ints([0, 0]), counts=ints(start), cos=cd, sin=sd)
     lens, xq, xk, xv = ints(start), *(torch.empty((2, h, 1, 128), dtype=torch.bfloat16, device="cuda") for h in (Hq, Hkv, Hkv))
     q_out, out = torch.empty_like(xq), torch.empty(xq.shape, device="cuda")
-    ws = torch.empty(caches[0].workspace_bytes(2, 1), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(caches[0].workspace_bytes(2, 1, pages.shape[1]), dtype=torch.uint8, device="cuda")
 
     def one():
         caches[0].step(0, xk, xv, xq, pages, lens, SCALE, cos=cd, sin=sd, q_out=q_out, out=out, workspace=ws)
@@ -296,7 +330,7 @@ def test_streams_and_two_calls_at_once(binding):
     torch.cuda.synchronize()
     streams = [torch.cuda.Stream() for _ in qs]
     outs = [torch.empty_like(w) for w in want]
-    spaces = [torch.empty(cache.workspace_bytes(2, 1), dtype=torch.uint8, device="cuda") for _ in qs]
+    spaces = [torch.empty(cache.workspace_bytes(2, 1, pages.shape[1]), dtype=torch.uint8, device="cuda") for _ in qs]
     for _ in range(10):
         for s, x, o, w in zip(streams, qs, outs, spaces):
             with torch.cuda.stream(s):
@@ -336,7 +370,7 @@ def test_refusals(binding):
     before = cache.launch_count()
     wide = torch.zeros((2, Hkv, n, 132), dtype=torch.bfloat16, device="cuda")
     pool = cache.mem[256:256 + q.numel() * 2].view(torch.bfloat16).view(q.shape)
-    ws = torch.empty(cache.workspace_bytes(2, n), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(cache.workspace_bytes(2, n, 2), dtype=torch.uint8, device="cuda")
     for call, code in ((lambda: cache.append(1, k, v, pages, lens), -1), (lambda: cache.append(0, wide[..., :128], v, pages, lens), -3),
                        (lambda: cache.append(0, k, v, pages, lens, q=q, q_out=pool), -1),
                        (lambda: cache.append(0, pool[:, :2], v, pages, lens), -1),

@@ -67,7 +67,7 @@ def test_arguments_are_passed_on(cache):
     assert (n0, n1, n2, n3, n4) == ("paged_append", "paged_append", "paged_attention", "paged_step", "paged_read")
     assert a0[2:4] == (B, N) and a0[5:7] == (3, 3) and a0[8] is None and a0[11] is None and a0[13:19] == (None,) * 6
     assert a1[5:7] == (4, 9) and a1[8] == w["lens"].data_ptr() and a1[15] == 7 and a1[16] is None and a1[17:19] == (64, 1)
-    assert a2[11] == 1 and a2[14] == cache.workspace_bytes(B, N) and len(a3) == 26 and len(a1) == 21 and a4[3] == 3
+    assert a2[11] == 1 and a2[14] == cache.workspace_bytes(B, N, 3) and len(a3) == 26 and len(a1) == 21 and a4[3] == 3
 
 
 @pytest.mark.parametrize("bad", ["dtype", "batch", "heads", "tokens", "last dimension", "flat", "pages type", "pages rows", "pages strided", "lens", "lens type", "counts",
@@ -142,14 +142,15 @@ def test_null_handles_sizes_and_configurations():
     assert lib.mixkvq_rope_tables(None, 0, 1, None, None, None) == -1
     assert lib.mixkvq_paged_query_status(None, None, None) == -1 and lib.mixkvq_paged_clear_status(None, None) == -1
     assert lib.mixkvq_paged_launch_count(None) == 0 and lib.mixkvq_paged_init(None, None, 0, None, None) == -1
-    assert lib.mixkvq_paged_workspace_bytes(None, 1, 1) == 0
+    assert lib.mixkvq_paged_workspace_bytes(None, 1, 1, 1) == 0
     n = C.c_size_t()
     for G, tile in ((32, 2560), (64, 2304), (128, 2176)):
         cfg = binding.make_paged_config(3, 8, 2, 10, page_tokens=64, group_size=G)
         assert lib.mixkvq_paged_bytes(C.byref(cfg), C.byref(n)) == 0 and n.value == 256 + 3 * 10 * 2 * 4 * tile
-        assert lib.mixkvq_paged_workspace_bytes(C.byref(cfg), 0, 1) == lib.mixkvq_paged_workspace_bytes(C.byref(cfg), 1, -1) == 0
-        sizes = [lib.mixkvq_paged_workspace_bytes(C.byref(cfg), b, t) for b, t in ((1, 1), (8, 1), (8, 8), (64, 100), (4096, 2))]
-        assert all(0 < s < 1 << 30 and s % 16 == 0 for s in sizes)
+        assert lib.mixkvq_paged_workspace_bytes(C.byref(cfg), 0, 1, 1) == lib.mixkvq_paged_workspace_bytes(C.byref(cfg), 1, -1, 1) == 0
+        assert lib.mixkvq_paged_workspace_bytes(C.byref(cfg), 1, 1, 0) == lib.mixkvq_paged_workspace_bytes(C.byref(cfg), 1, 1, 1 << 30) == 0
+        sizes = [lib.mixkvq_paged_workspace_bytes(C.byref(cfg), b, t, p) for b, t, p in ((1, 1, 1), (8, 1, 600), (8, 8, 1), (64, 100, 500), (4096, 2, 9), (1, 5000, 16384), (1, 5000, 1 << 20))]
+        assert all(0 < s < 6 << 27 and s % 16 == 0 for s in sizes)
     for field, bad, code in (("n_layers", 0, -1), ("n_q_heads", 7, -1), ("n_q_heads", 32, -2), ("n_kv_heads", 0, -1), ("head_dim", 64, -2), ("n_pages", 0, -1), ("page_tokens", 8, -2),
                              ("page_tokens", 48, -2), ("page_tokens", 512, -2), ("group_size", 16, -2), ("reserved", 1, -1)):
         cfg = binding.make_paged_config(1, 8, 2, 4)
