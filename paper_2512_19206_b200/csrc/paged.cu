@@ -1,8 +1,10 @@
 // Tokens into the pages of the 4-bit cache, and the values that they hold back out of them.
 //
 // append_kernel: new tokens' keys and queries turn by their positions (rotary positions of part of the head, either pairing), keys and values are quantized
-// (Eq. 2 with 16 levels, a group of G channels of one token) and go to the page and slot of the token.  Memory-bound; a thread has 8 channels of one token and goes
-// through a range of heads, sixteen lanes have a row: the extrema of a group are two to four exchanges between them, a lane's eight codes are one word.
+// (Eq. 2 with 16 levels, a group of G channels of one token) and go to the page and slot of the token.  Memory-bound by its bytes, by instruction issue in its first form (306
+// instructions per two rows of 16384 prompt tokens, 176 us for 324 MB).  Thread blocks for keys and values: sixteen lanes have a row, a lane 8 channels, so that a lane's eight
+// codes are one word and the extrema of a group two to four exchanges; thread blocks for queries: eight lanes have a row (turn_pair).  A thread has one token and goes
+// through a range of heads.
 #include <algorithm>
 
 #include "paged.cuh"
@@ -11,10 +13,64 @@ namespace mixkvq {
 
 namespace {
 
-constexpr int kTokens = 16;
-constexpr int kBatch = 4;
+constexpr int kTokens = 16;                // of a thread block for keys and values, twice as many of one for queries
+constexpr int kBatch = 4;                  // rows in flight per thread
+
+// What a lane of sixteen turns its 8 channels by.
+struct ChunkLane {
+  Angles x;                                // sines negative where the channels are the first of their pairs
+  int other;                               // the lane of the row with the other channels
+  int mode;                                // 0: left as they are, 1: halves, 2: neighbours
+};
+__device__ __forceinline__ ChunkLane chunk_lane(const RopeTurn& t, int pos, int c, bool turns) {
+  ChunkLane l;
+  const int half = t.rotary >> 4;
+  l.mode = !turns || c >= 2 * half ? 0 : t.interleaved ? 2 : 1;
+  l.other = l.mode != 1 ? c : c < half ? c + half : c - half;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) l.x.c[i] = l.x.s[i] = f2(0.f, 0.f);
+  if (l.mode == 0) return l;
+  const size_t row = (size_t)pos * (t.rotary >> 1);
+  if (l.mode == 2) {
+    load_angles(t.cos_t, t.sin_t, row + 4 * c, 4, l.x);
+  } else {
+    load_angles(t.cos_t, t.sin_t, row + 8 * (c < half ? c : c - half), 8, l.x);
+    if (c < half) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float lo, hi;
+        f2_get(l.x.s[i], lo, hi);
+        l.x.s[i] = f2(-lo, -hi);           // x c - y s is x c + y (-s), the product rounds alike
+      }
+    }
+  }
+  return l;
+}
+// Every lane of the warp calls this.
+__device__ __forceinline__ uint4 turn_chunk(uint4 own, const ChunkLane& l, F2 mz) {
+  const uint32_t a[4] = {own.x, own.y, own.z, own.w};
+  uint32_t y[4] = {own.x, own.y, own.z, own.w}, b[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) b[j] = __shfl_sync(0xffffffffu, a[j], l.other, 16);
+  if (l.mode == 1) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float lo, hi;
+      f2_get(f2_add(f2_mul(f2(bf16_half(a[j], 0), bf16_half(a[j], 1)), l.x.c[j], mz), f2_mul(f2(bf16_half(b[j], 0), bf16_half(b[j], 1)), l.x.s[j], mz)), lo, hi);
+      y[j] = bf16_pair(lo, hi);
+    }
+  } else if (l.mode == 2) {
+    turn_neighbours(y[0], y[1], l.x.c[0], l.x.s[0], mz);
+    turn_neighbours(y[2], y[3], l.x.c[1], l.x.s[1], mz);
+  }
+  return make_uint4(y[0], y[1], y[2], y[3]);
+}
 
 // Scale, zero-point and codes of a row's groups.  Every lane of the warp calls this; group_lanes = G / 8 neighbouring lanes share a group.
+//
+// The code of an element is the rounded single-precision quotient (x - z) / s.  With r = 1 / s rounded, (x - z) r is off that quotient's exact value by 2^-23 of itself at
+// most and the quotient by 2^-24: 2.7e-6 together, as no quotient is above 15.  So unless the product lies within 4e-6 of a half-integer both round to the same whole number;
+// the few that do (exact ties of bf16 numbers among them) are divided, and so is what has no product: NaN, infinities, groups without a scale.
 struct Quantized {
   uint32_t codes;                          // channel i at bits 4 i
   uint32_t meta;                           // z | s << 16, bf16 bits
@@ -24,87 +80,122 @@ __device__ __forceinline__ Quantized quantize_chunk(uint4 w, int group_lanes) {
   float x[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] = bf16_half(a[i >> 1], i & 1);
-  float lo = x[0], hi = x[0];
-#pragma unroll
-  for (int i = 1; i < 8; ++i) {
-    lo = fminf(lo, x[i]);
-    hi = fmaxf(hi, x[i]);
-  }
+  float lo = fminf(fminf(fminf(x[0], x[1]), fminf(x[2], x[3])), fminf(fminf(x[4], x[5]), fminf(x[6], x[7])));
+  float hi = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
   for (int d = 1; d < group_lanes; d <<= 1) {
     lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
     hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, d));
   }
-  const float s = stored_scale(hi, lo, 15.f);
-  Quantized y;
-  y.codes = 0u;
+  const float s = stored_scale(hi, lo, 15.f), inv = __frcp_rn(s);
+  constexpr float kMagic = 12582912.f;     // 1.5 2^23: adding it rounds to a whole number, the low bits of the sum
+  uint32_t codes = 0;
+  bool near = false;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) y.codes |= (uint32_t)quant_code(x[i], lo, s, 15) << (4 * i);
+  for (int i = 7; i >= 0; --i) {
+    const float y = __fmul_rn(__fsub_rn(x[i], lo), inv), f = __fadd_rn(y, kMagic), d = __fsub_rn(y, __fsub_rn(f, kMagic));
+    near = near || !(fabsf(d) <= 0.5f - 4e-6f);
+    codes = codes * 16u + (__float_as_uint(f) - 0x4B400000u);
+  }
+  if (near) {
+    codes = 0;
+#pragma unroll 1
+    for (int i = 7; i >= 0; --i) codes = codes * 16u + (uint32_t)quant_code(__uint_as_float(i & 1 ? a[i >> 1] & 0xFFFF0000u : a[i >> 1] << 16), lo, s, 15);
+  }
+  Quantized y;
+  y.codes = codes;
   y.meta = (__float_as_uint(lo) >> 16) | (__float_as_uint(s) & 0xFFFF0000u);
   return y;
 }
 
-__global__ void __launch_bounds__(256)
-append_kernel(const __grid_constant__ PagedAppend a, int heads_per_block) {
-  dependency_wait();
+// Token i of sequence b of an append: where it goes and what it turns by; false: nowhere.
+__device__ __forceinline__ bool token_place(const PagedAppend& a, long long tok, int& b, int& i, int& place, int& pos) {
   const PagedView& v = a.view;
-  const int c = threadIdx.x & 15;
-  const long long tok = (long long)blockIdx.x * kTokens + (threadIdx.x >> 4);
-  const bool there = tok < (long long)v.B * v.n;
-  const int b = there ? (int)(tok / v.n) : 0, i = there ? (int)(tok - (long long)b * v.n) : 0;
-  bool live = there && i < v.count(b);
-  int place = 0, pos = 0;
-  if (live) {
-    place = v.place(b, i);
-    live = place >= 0;
-  }
-  if (live && a.turn.cos_t != nullptr) {
+  b = i = place = pos = 0;
+  if (tok >= (long long)v.B * v.n) return false;
+  b = (int)(tok / v.n);
+  i = (int)(tok - (long long)b * v.n);
+  if (i >= v.count(b)) return false;
+  place = v.place(b, i);
+  if (place < 0) return false;
+  if (a.turn.cos_t != nullptr) {
     pos = a.turn.positions != nullptr ? a.turn.positions[tok] : place;
     if (pos >= a.turn.n_positions) atomicOr(v.status, (uint32_t)MIXKVQ_DEV_BAD_POSITION);
-    live = pos >= 0 && pos < a.turn.n_positions;
+    if (pos < 0 || pos >= a.turn.n_positions) return false;
   }
-  char* piece = live ? v.piece(b, 0, place) : nullptr;
-  live = piece != nullptr;
+  return true;
+}
+
+__global__ void __launch_bounds__(256)
+append_kernel(const __grid_constant__ PagedAppend a, int kv_blocks, int kv_each, int kv_splits, int q_each, int q_splits) {
+  dependency_wait();
+  const PagedView& v = a.view;
+  int b, i, place, pos;
+  if ((int)blockIdx.x >= kv_blocks) {
+    // ---- queries
+    const int block = blockIdx.x - kv_blocks, tokens = block / q_splits, split = block - tokens * q_splits;
+    const long long tok = (long long)tokens * (2 * kTokens) + (threadIdx.x >> 3);
+    // (a token on a page that is none is not stored, and its queries are left alone like its keys)
+    if (!token_place(a, tok, b, i, place, pos) || v.piece(b, 0, place) == nullptr) return;
+    const PairLane p = pair_lane(a.turn, pos, threadIdx.x & 7, a.turn.cos_t != nullptr);
+    const int h0 = split * q_each, h1 = min(h0 + q_each, v.Hq);
+    for (int h = h0; h < h1; h += kBatch) {
+      uint4 w[kBatch][2];
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + b * a.tq.batch + min(h + k, h1 - 1) * a.tq.head + i * a.tq.token);
+        w[k][0] = src[p.first];
+        w[k][1] = src[p.second];
+      }
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        if (h + k >= h1) break;
+        turn_pair(w[k][0], w[k][1], p, F2{a.turn.minus_zero});
+        uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.q_out) + (((size_t)b * v.Hq + h + k) * v.n + i) * kD);
+        dst[p.first] = w[k][0];
+        dst[p.second] = w[k][1];
+      }
+    }
+    return;
+  }
+  // ---- keys, then values
+  const int tokens = blockIdx.x / kv_splits, split = blockIdx.x - tokens * kv_splits, c = threadIdx.x & 15;
+  const bool found = token_place(a, (long long)tokens * kTokens + (threadIdx.x >> 4), b, i, place, pos);
+  char* piece = found ? v.piece(b, 0, place) : nullptr;
+  const bool live = piece != nullptr;
   if (live) piece += v.tile_of(place);
-  RopeTurn turn = a.turn;
-  if (!live) turn.cos_t = nullptr;
-  const TurnChunk x = turn_chunk_load(turn, pos, c);
-  const int row = place & 15, G = v.G;
-  // heads: keys, values, queries
-  const int heads = 2 * v.Hkv + (a.q != nullptr ? v.Hq : 0);
-  const int h0 = blockIdx.y * heads_per_block, h1 = min(h0 + heads_per_block, heads);
+  const ChunkLane lane = chunk_lane(a.turn, pos, c, live && a.turn.cos_t != nullptr);
+  const int row = place & 15, G = v.G, group_lanes = G / 8;
+  const int v_at = (16 * (c & 3) + 2 * (c >> 2)) ^ ((row & 4) << 3);
+  char* k_to = piece + row * 64 + 16 * (c & 3) + 4 * (c >> 2);
+  char* v_to = piece + 1024 + row * 64 + v_at;
+  char* m_to = piece + paged_k_meta(row, G) + 4 * (c / group_lanes);
+  const bool first = c % group_lanes == 0;
+  const int h0 = split * kv_each, h1 = min(h0 + kv_each, 2 * v.Hkv);
   for (int h = h0; h < h1; h += kBatch) {
     uint4 w[kBatch];
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
       w[k] = make_uint4(0u, 0u, 0u, 0u);
-      const int hh = h + k;
-      if (hh >= h1 || !live) continue;
-      const int which = hh < v.Hkv ? 1 : hh < 2 * v.Hkv ? 2 : 0, head = which == 1 ? hh : which == 2 ? hh - v.Hkv : hh - 2 * v.Hkv;
-      const RopeTensor& s = which == 0 ? a.tq : which == 1 ? a.tk : a.tv;
-      w[k] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(which == 0 ? a.q : which == 1 ? a.k : a.v) + b * s.batch + head * s.head + i * s.token +
-                                             8 * c);
+      const int hh = min(h + k, h1 - 1);
+      const RopeTensor& s = hh < v.Hkv ? a.tk : a.tv;
+      if (live)
+        w[k] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(hh < v.Hkv ? a.k : a.v) + b * s.batch + (hh < v.Hkv ? hh : hh - v.Hkv) * s.head + i * s.token + 8 * c);
     }
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
       const int hh = h + k;
       if (hh >= h1) break;
-      const int which = hh < v.Hkv ? 1 : hh < 2 * v.Hkv ? 2 : 0, head = which == 1 ? hh : which == 2 ? hh - v.Hkv : hh - 2 * v.Hkv;
-      const uint4 y = which == 2 ? w[k] : turn_chunk(w[k], x);
-      Quantized z{0u, 0u};
-      if (which != 0) z = quantize_chunk(y, G / 8);
-      if (live && which == 0) {
-        *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.q_out) + (((size_t)b * v.Hq + head) * v.n + i) * kD + 8 * c) = y;
-      } else if (live) {
-        char* tile = piece + (uint64_t)head * v.piece_bytes;
-        if (which == 1) {
-          *reinterpret_cast<uint32_t*>(tile + row * 64 + 16 * (c & 3) + 4 * (c >> 2)) = z.codes;
+      const bool keys = hh < v.Hkv;
+      const Quantized z = quantize_chunk(keys ? turn_chunk(w[k], lane, F2{a.turn.minus_zero}) : w[k], group_lanes);
+      const uint64_t at = (uint64_t)(keys ? hh : hh - v.Hkv) * v.piece_bytes;
+      if (live) {
+        if (keys) {
+          *reinterpret_cast<uint32_t*>(k_to + at) = z.codes;
         } else {
-          const int at = (16 * (c & 3) + 2 * (c >> 2)) ^ ((row & 4) << 3);
-          *reinterpret_cast<uint16_t*>(tile + 1024 + row * 64 + at) = (uint16_t)z.codes;
-          *reinterpret_cast<uint16_t*>(tile + 1024 + row * 64 + at + 8) = (uint16_t)(z.codes >> 16);
+          *reinterpret_cast<uint16_t*>(v_to + at) = (uint16_t)z.codes;
+          *reinterpret_cast<uint16_t*>(v_to + at + 8) = (uint16_t)(z.codes >> 16);
         }
-        if (c % (G / 8) == 0)
-          *reinterpret_cast<uint32_t*>(tile + (which == 1 ? paged_k_meta(row, G) : paged_v_meta(row, G)) + 4 * (c / (G / 8))) = z.meta;
+        if (first) *reinterpret_cast<uint32_t*>(m_to + at + (keys ? 0u : 16u * paged_meta_bytes(G))) = z.meta;
       }
     }
   }
@@ -159,9 +250,10 @@ int split_heads(long long blocks, int heads, int n_sms) {
 }  // namespace
 
 cudaError_t launch_paged_append(const PagedAppend& a, int n_sms, cudaStream_t stream) {
-  const long long blocks = ((long long)a.view.B * a.view.n + kTokens - 1) / kTokens;
-  const int heads = 2 * a.view.Hkv + (a.q != nullptr ? a.view.Hq : 0), each = split_heads(blocks, heads, n_sms);
-  return launch_dependent(append_kernel, dim3((unsigned)blocks, (unsigned)((heads + each - 1) / each)), 256, 0, stream, a, each);
+  const long long tokens = (long long)a.view.B * a.view.n, kv = (tokens + kTokens - 1) / kTokens, q = a.q != nullptr ? (tokens + 2 * kTokens - 1) / (2 * kTokens) : 0;
+  const int kv_each = split_heads(kv, 2 * a.view.Hkv, n_sms), q_each = split_heads(std::max(q, 1ll), a.view.Hq, n_sms);
+  const int kv_splits = (2 * a.view.Hkv + kv_each - 1) / kv_each, q_splits = (a.view.Hq + q_each - 1) / q_each;
+  return launch_dependent(append_kernel, dim3((unsigned)(kv * kv_splits + q * q_splits)), 256, 0, stream, a, (int)(kv * kv_splits), kv_each, kv_splits, q_each, q_splits);
 }
 
 cudaError_t launch_paged_read(const PagedRead& a, int n_sms, cudaStream_t stream) {

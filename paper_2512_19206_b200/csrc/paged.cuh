@@ -70,6 +70,7 @@ struct RopeTurn {
   const float *cos_t, *sin_t;              // [n_positions][rotary / 2]; null: no rotation
   const int32_t* positions;                // [B][n]; null: the token's place in its sequence
   int n_positions, rotary, interleaved;
+  uint64_t minus_zero = 0x8000000080000000ull;      // two of them (see f2_mul)
 };
 
 struct PagedAppend {
@@ -123,57 +124,111 @@ cudaError_t launch_rope_tables(const RopeTables& a, int n_sms, cudaStream_t stre
 
 namespace {
 
-// What a thread turns its 8 channels (chunk c of a row of 16) by.  Sixteen neighbouring lanes have a row.
-struct TurnChunk {
-  float c[8], s[8];
-  int other;                               // pairs in halves: the lane of the row that has the other channel of every pair
-  int mode;                                // 0: left as they are, 1: first halves, 2: second halves, 3: pairs of neighbours
-};
-__device__ __forceinline__ TurnChunk turn_chunk_load(const RopeTurn& t, int pos, int c) {
-  TurnChunk x;
-  const int half = t.rotary >> 4;          // chunks of half a rotated part
-  x.other = c;
-  x.mode = t.cos_t == nullptr || c >= 2 * half ? 0 : t.interleaved ? 3 : c < half ? 1 : 2;
-  if (x.mode == 1) x.other = c + half;
-  if (x.mode == 2) x.other = c - half;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x.c[i] = 1.f, x.s[i] = 0.f;
-  if (x.mode == 0) return x;
-  const size_t at = (size_t)pos * (t.rotary >> 1) + (x.mode == 3 ? 4 * c : 8 * (x.mode == 1 ? c : c - half));
-  const float4 c0 = *reinterpret_cast<const float4*>(t.cos_t + at), s0 = *reinterpret_cast<const float4*>(t.sin_t + at);
-  x.c[0] = c0.x; x.c[1] = c0.y; x.c[2] = c0.z; x.c[3] = c0.w;
-  x.s[0] = s0.x; x.s[1] = s0.y; x.s[2] = s0.z; x.s[3] = s0.w;
-  if (x.mode != 3) {
-    const float4 c1 = *reinterpret_cast<const float4*>(t.cos_t + at + 4), s1 = *reinterpret_cast<const float4*>(t.sin_t + at + 4);
-    x.c[4] = c1.x; x.c[5] = c1.y; x.c[6] = c1.z; x.c[7] = c1.w;
-    x.s[4] = s1.x; x.s[5] = s1.y; x.s[6] = s1.z; x.s[7] = s1.w;
-  }
-  return x;
-}
 __device__ __forceinline__ float bf16_half(uint32_t w, int e) { return e ? __uint_as_float(w & 0xFFFF0000u) : __uint_as_float(w << 16); }
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-// The thread's 8 channels turned (every lane of the warp calls this): the arithmetic of rotate_one, that is single fp32 operations without contraction and
-// one rounding to bf16.
-__device__ __forceinline__ uint4 turn_chunk(uint4 own, const TurnChunk& t) {
-  const uint32_t a[4] = {own.x, own.y, own.z, own.w};
-  uint32_t b[4], y[4];
+
+// ---- Rotation, two channels per instruction of the FMA pipe.  The arithmetic is that of rotate_one: every product and every sum a single fp32 operation rounded to
+// nearest (no contraction: the products and sums below are instructions of their own), the result rounded to bf16.
+struct F2 {
+  uint64_t v;
+};
+__device__ __forceinline__ F2 f2(float a, float b) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+  return r;
+}
+// (As a multiply-add of -0, which is the product with its sign: a product instruction of this form is contracted with the sum behind it, its .rn notwithstanding, and 1 bf16 result
+// in 60000 differed.  The -0 is a parameter of the launch: one that the assembler sees leads to the same.)
+__device__ __forceinline__ F2 f2_mul(F2 a, F2 b, F2 minus_zero) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(minus_zero.v));
+  return r;
+}
+__device__ __forceinline__ F2 f2_add(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 f2_sub(F2 a, F2 b) {
+  F2 r;
+  asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ void f2_get(F2 x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.v)); }
+
+// 8 cosines and sines of a token: pairs at .. at + 7 of the table row, two per register pair.
+struct Angles {
+  F2 c[4], s[4];
+};
+__device__ __forceinline__ void load_angles(const float* cos_t, const float* sin_t, size_t at, int n, Angles& x) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) b[j] = __shfl_sync(0xffffffffu, a[j], t.other, 16);
-  if (t.mode == 0) return own;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    if (t.mode == 3) {
-      const float x0 = bf16_half(a[j], 0), x1 = bf16_half(a[j], 1);
-      y[j] = bf16_pair(rotate_one(x0, x1, t.c[j], t.s[j], true), rotate_one(x1, x0, t.c[j], t.s[j], false));
-    } else {
-      y[j] = bf16_pair(rotate_one(bf16_half(a[j], 0), bf16_half(b[j], 0), t.c[2 * j], t.s[2 * j], t.mode == 1),
-                       rotate_one(bf16_half(a[j], 1), bf16_half(b[j], 1), t.c[2 * j + 1], t.s[2 * j + 1], t.mode == 1));
-    }
+  for (int k = 0; k < 2; ++k) {
+    if (4 * k >= n) break;
+    const float4 c = *reinterpret_cast<const float4*>(cos_t + at + 4 * k), s = *reinterpret_cast<const float4*>(sin_t + at + 4 * k);
+    x.c[2 * k] = f2(c.x, c.y);
+    x.c[2 * k + 1] = f2(c.z, c.w);
+    x.s[2 * k] = f2(s.x, s.y);
+    x.s[2 * k + 1] = f2(s.z, s.w);
   }
-  return make_uint4(y[0], y[1], y[2], y[3]);
+}
+// Two pairs whose first channels are a and whose second channels are b.
+__device__ __forceinline__ void turn2(F2& a, F2& b, F2 c, F2 s, F2 mz) {
+  const F2 y = f2_sub(f2_mul(a, c, mz), f2_mul(b, s, mz));
+  b = f2_add(f2_mul(b, c, mz), f2_mul(a, s, mz));
+  a = y;
+}
+// Pairs of neighbours in two words.
+__device__ __forceinline__ void turn_neighbours(uint32_t& w0, uint32_t& w1, F2 c, F2 s, F2 mz) {
+  F2 a = f2(bf16_half(w0, 0), bf16_half(w1, 0)), b = f2(bf16_half(w0, 1), bf16_half(w1, 1));
+  turn2(a, b, c, s, mz);
+  float a0, a1, b0, b1;
+  f2_get(a, a0, a1);
+  f2_get(b, b0, b1);
+  w0 = bf16_pair(a0, b0);
+  w1 = bf16_pair(a1, b1);
+}
+
+// Rows that are turned and nothing else: eight lanes have a row, a lane two chunks of 8 channels: in halves the two chunks of 8 pairs, otherwise neighbours; lanes behind the
+// rotated part have two neighbouring chunks.
+struct PairLane {
+  int first, second;                       // chunks
+  int mode;                                // 0: left as they are, 1: halves, 2: neighbours
+  Angles x;
+};
+__device__ __forceinline__ PairLane pair_lane(const RopeTurn& t, int pos, int l, bool turns) {
+  PairLane p;
+  const int half = t.rotary >> 4;          // lanes with rotated channels
+  p.mode = !turns || l >= half ? 0 : t.interleaved ? 2 : 1;
+  p.first = turns && !t.interleaved ? (l < half ? l : 2 * l) : 2 * l;       // (l >= half: 2 half + 2 (l - half))
+  p.second = p.mode == 1 ? l + half : p.first + 1;
+  if (p.mode != 0) load_angles(t.cos_t, t.sin_t, (size_t)pos * (t.rotary >> 1) + 8 * l, 8, p.x);
+  return p;
+}
+__device__ __forceinline__ void turn_pair(uint4& wa, uint4& wb, const PairLane& p, F2 mz) {
+  if (p.mode == 0) return;
+  uint32_t a[4] = {wa.x, wa.y, wa.z, wa.w}, b[4] = {wb.x, wb.y, wb.z, wb.w};
+  if (p.mode == 1) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      F2 u = f2(bf16_half(a[j], 0), bf16_half(a[j], 1)), w = f2(bf16_half(b[j], 0), bf16_half(b[j], 1));
+      turn2(u, w, p.x.c[j], p.x.s[j], mz);
+      float lo, hi;
+      f2_get(u, lo, hi);
+      a[j] = bf16_pair(lo, hi);
+      f2_get(w, lo, hi);
+      b[j] = bf16_pair(lo, hi);
+    }
+  } else {
+    turn_neighbours(a[0], a[1], p.x.c[0], p.x.s[0], mz);
+    turn_neighbours(a[2], a[3], p.x.c[1], p.x.s[1], mz);
+    turn_neighbours(b[0], b[1], p.x.c[2], p.x.s[2], mz);
+    turn_neighbours(b[2], b[3], p.x.c[3], p.x.s[3], mz);
+  }
+  wa = make_uint4(a[0], a[1], a[2], a[3]);
+  wb = make_uint4(b[0], b[1], b[2], b[3]);
 }
 
 }  // namespace

@@ -1,8 +1,8 @@
 // Rotary positions of a part of the head in either pairing, and the tables of scaled frequencies that they turn by.
 //
 // rope_partial_kernel: channels 0 .. d-1 of a row turn by the row of the token's position, the others are copied; pairs (i, i + d/2) or (2 i, 2 i + 1).
-// Memory-bound: every row is read and written once.  A thread has 8 channels of one token and keeps their cosines and sines in registers while it goes
-// through a range of heads, so that the tables are read once per token and range instead of once per row.
+// Memory-bound: every row is read and written once.  Eight lanes have a token's rows, a lane 8 pairs; it keeps their cosines and sines in registers while it goes through a
+// range of heads, so that the tables are read once per token and range instead of once per row, and no lane needs another's channels.
 //
 // rope_tables_kernel: cos and sin of p f_i.  Angles of far positions need more than 32 bits (p f of 10^5 rad leaves 2^-7 of a turn in fp32), so they are 64-bit, in
 // half turns, which are reduced exactly.  A 64-bit sine and cosine per entry would cost more than writing them; a thread has one pair and some neighbouring
@@ -15,51 +15,42 @@ namespace mixkvq {
 
 namespace {
 
-constexpr int kTokens = 16;                                // of a thread block
+constexpr int kTokens = 32;                                // of a thread block
 constexpr int kBatch = 4;                                  // rows in flight per thread
 
 __global__ void __launch_bounds__(256)
 rope_partial_kernel(const __grid_constant__ RopePartial a, int heads_per_block) {
   dependency_wait();
-  const int c = threadIdx.x & 15;
-  const long long tok = (long long)blockIdx.x * kTokens + (threadIdx.x >> 4);
-  const bool there = tok < (long long)a.B * a.n;
-  const int b = there ? (int)(tok / a.n) : 0, t = there ? (int)(tok - (long long)b * a.n) : 0;
-  int pos = -1;
-  if (there) {
-    pos = a.turn.positions[tok];
-    if (pos >= a.turn.n_positions) {
-      atomicOr(a.status, (uint32_t)MIXKVQ_DEV_BAD_POSITION);
-      pos = -1;
-    }
-  }
-  const bool live = pos >= 0;
-  RopeTurn turn = a.turn;
-  if (!live) turn.cos_t = nullptr;
-  const TurnChunk x = turn_chunk_load(turn, pos, c);
+  const long long tok = (long long)blockIdx.x * kTokens + (threadIdx.x >> 3);
+  if (tok >= (long long)a.B * a.n) return;
+  const int pos = a.turn.positions[tok];
+  if (pos >= a.turn.n_positions) atomicOr(a.status, (uint32_t)MIXKVQ_DEV_BAD_POSITION);
+  if (pos < 0 || pos >= a.turn.n_positions) return;
+  const int b = (int)(tok / a.n), t = (int)(tok - (long long)b * a.n);
+  const PairLane p = pair_lane(a.turn, pos, threadIdx.x & 7, true);
   const int heads = a.Hq + a.Hkv + (a.v != nullptr ? a.Hkv : 0);
   const int h0 = blockIdx.y * heads_per_block, h1 = min(h0 + heads_per_block, heads);
   for (int h = h0; h < h1; h += kBatch) {
-    uint4 w[kBatch];
+    uint4 w[kBatch][2];
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
-      w[i] = make_uint4(0u, 0u, 0u, 0u);
-      const int hh = h + i;
-      if (hh >= h1 || !live) continue;
+      const int hh = min(h + i, h1 - 1);
       const int which = hh < a.Hq ? 0 : hh < a.Hq + a.Hkv ? 1 : 2, head = which == 0 ? hh : which == 1 ? hh - a.Hq : hh - a.Hq - a.Hkv;
       const RopeTensor& s = which == 0 ? a.tq : which == 1 ? a.tk : a.tv;
-      w[i] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(which == 0 ? a.q : which == 1 ? a.k : a.v) + b * s.batch + head * s.head + t * s.token +
-                                             8 * c);
+      const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(which == 0 ? a.q : which == 1 ? a.k : a.v) + b * s.batch + head * s.head + t * s.token);
+      w[i][0] = src[p.first];
+      w[i][1] = src[p.second];
     }
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
       const int hh = h + i;
       if (hh >= h1) break;
       const int which = hh < a.Hq ? 0 : hh < a.Hq + a.Hkv ? 1 : 2, head = which == 0 ? hh : which == 1 ? hh - a.Hq : hh - a.Hq - a.Hkv;
-      const uint4 y = which == 2 ? w[i] : turn_chunk(w[i], x);
-      if (live)
-        *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(which == 0 ? a.q_out : which == 1 ? a.k_out : a.v_out) +
-                                  (((size_t)b * (which == 0 ? a.Hq : a.Hkv) + head) * a.n + t) * kD + 8 * c) = y;
+      if (which != 2) turn_pair(w[i][0], w[i][1], p, F2{a.turn.minus_zero});
+      uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(which == 0 ? a.q_out : which == 1 ? a.k_out : a.v_out) +
+                                            (((size_t)b * (which == 0 ? a.Hq : a.Hkv) + head) * a.n + t) * kD);
+      dst[p.first] = w[i][0];
+      dst[p.second] = w[i][1];
     }
   }
 }
