@@ -94,12 +94,15 @@ __device__ __forceinline__ Quantized quantize_chunk(uint4 w, int group_lanes) {
   for (int i = 7; i >= 0; --i) {
     const float y = __fmul_rn(__fsub_rn(x[i], lo), inv), f = __fadd_rn(y, kMagic), d = __fsub_rn(y, __fsub_rn(f, kMagic));
     near = near || !(fabsf(d) <= 0.5f - 4e-6f);
-    codes = codes * 16u + (__float_as_uint(f) - 0x4B400000u);
+    codes = codes * 16u + (__float_as_uint(f) & 15u);
   }
-  if (near) {
-    codes = 0;
+  if (near) {                              // (one element as a rule)
 #pragma unroll 1
-    for (int i = 7; i >= 0; --i) codes = codes * 16u + (uint32_t)quant_code(__uint_as_float(i & 1 ? a[i >> 1] & 0xFFFF0000u : a[i >> 1] << 16), lo, s, 15);
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t w2 = i < 4 ? (i < 2 ? w.x : w.y) : (i < 6 ? w.z : w.w);
+      const float e = __uint_as_float(i & 1 ? w2 & 0xFFFF0000u : w2 << 16), y = __fmul_rn(__fsub_rn(e, lo), inv), d = __fsub_rn(y, __fsub_rn(__fadd_rn(y, kMagic), kMagic));
+      if (!(fabsf(d) <= 0.5f - 4e-6f)) codes = (codes & ~(15u << (4 * i))) | (uint32_t)quant_code(e, lo, s, 15) << (4 * i);
+    }
   }
   Quantized y;
   y.codes = codes;
@@ -108,12 +111,12 @@ __device__ __forceinline__ Quantized quantize_chunk(uint4 w, int group_lanes) {
 }
 
 // Token i of sequence b of an append: where it goes and what it turns by; false: nowhere.
-__device__ __forceinline__ bool token_place(const PagedAppend& a, long long tok, int& b, int& i, int& place, int& pos) {
+__device__ __forceinline__ bool token_place(const PagedAppend& a, int tok, int& b, int& i, int& place, int& pos) {
   const PagedView& v = a.view;
   b = i = place = pos = 0;
-  if (tok >= (long long)v.B * v.n) return false;
-  b = (int)(tok / v.n);
-  i = (int)(tok - (long long)b * v.n);
+  if (tok >= v.B * v.n) return false;      // (the host takes no call of 2^27 tokens or more)
+  b = tok / v.n;
+  i = tok - b * v.n;
   if (i >= v.count(b)) return false;
   place = v.place(b, i);
   if (place < 0) return false;
@@ -125,7 +128,7 @@ __device__ __forceinline__ bool token_place(const PagedAppend& a, long long tok,
   return true;
 }
 
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 3)
 append_kernel(const __grid_constant__ PagedAppend a, int kv_blocks, int kv_each, int kv_splits, int q_each, int q_splits) {
   dependency_wait();
   const PagedView& v = a.view;
@@ -133,7 +136,7 @@ append_kernel(const __grid_constant__ PagedAppend a, int kv_blocks, int kv_each,
   if ((int)blockIdx.x >= kv_blocks) {
     // ---- queries
     const int block = blockIdx.x - kv_blocks, tokens = block / q_splits, split = block - tokens * q_splits;
-    const long long tok = (long long)tokens * (2 * kTokens) + (threadIdx.x >> 3);
+    const int tok = tokens * (2 * kTokens) + (threadIdx.x >> 3);
     // (a token on a page that is none is not stored, and its queries are left alone like its keys)
     if (!token_place(a, tok, b, i, place, pos) || v.piece(b, 0, place) == nullptr) return;
     const PairLane p = pair_lane(a.turn, pos, threadIdx.x & 7, a.turn.cos_t != nullptr);
@@ -159,7 +162,7 @@ append_kernel(const __grid_constant__ PagedAppend a, int kv_blocks, int kv_each,
   }
   // ---- keys, then values
   const int tokens = blockIdx.x / kv_splits, split = blockIdx.x - tokens * kv_splits, c = threadIdx.x & 15;
-  const bool found = token_place(a, (long long)tokens * kTokens + (threadIdx.x >> 4), b, i, place, pos);
+  const bool found = token_place(a, tokens * kTokens + (threadIdx.x >> 4), b, i, place, pos);
   char* piece = found ? v.piece(b, 0, place) : nullptr;
   const bool live = piece != nullptr;
   if (live) piece += v.tile_of(place);
@@ -201,15 +204,14 @@ append_kernel(const __grid_constant__ PagedAppend a, int kv_blocks, int kv_each,
   }
 }
 
-// A thread has 8 channels of one token and goes through the heads.
+// A thread has 8 channels of one token and goes through the heads, some rows' loads under way together.
 __global__ void __launch_bounds__(256)
 read_kernel(const __grid_constant__ PagedRead a, int heads_per_block) {
   dependency_wait();
   const PagedView& v = a.view;
-  const int c = threadIdx.x & 15;
-  const long long tok = (long long)blockIdx.x * kTokens + (threadIdx.x >> 4);
-  if (tok >= (long long)v.B * v.n) return;
-  const int b = (int)(tok / v.n), i = (int)(tok - (long long)b * v.n);
+  const int c = threadIdx.x & 15, tok = blockIdx.x * kTokens + (threadIdx.x >> 4);
+  if (tok >= v.B * v.n) return;
+  const int b = tok / v.n, i = tok - b * v.n;
   if (i >= v.count(b)) return;
   const int place = v.place(b, i);
   if (place < 0) return;
@@ -217,33 +219,43 @@ read_kernel(const __grid_constant__ PagedRead a, int heads_per_block) {
   if (piece == nullptr) return;
   piece += v.tile_of(place);
   const int row = place & 15, G = v.G, grp = c / (G / 8);
+  const char* k_from = piece + row * 64 + 16 * (c & 3) + 4 * (c >> 2);
+  const char* v_from = piece + 1024 + row * 64 + ((16 * (c & 3) + 2 * (c >> 2)) ^ ((row & 4) << 3));
+  const char* m_from = piece + paged_k_meta(row, G) + 4 * grp;
   const int h0 = blockIdx.y * heads_per_block, h1 = min(h0 + heads_per_block, 2 * v.Hkv);
-  for (int h = h0; h < h1; ++h) {
-    const bool keys = h < v.Hkv;
-    const int head = keys ? h : h - v.Hkv;
-    const char* tile = piece + (uint64_t)head * v.piece_bytes;
-    uint32_t codes, meta;
-    if (keys) {
-      codes = *reinterpret_cast<const uint32_t*>(tile + row * 64 + 16 * (c & 3) + 4 * (c >> 2));
-      meta = *reinterpret_cast<const uint32_t*>(tile + paged_k_meta(row, G) + 4 * grp);
-    } else {
-      const int at = (16 * (c & 3) + 2 * (c >> 2)) ^ ((row & 4) << 3);
-      codes = *reinterpret_cast<const uint16_t*>(tile + 1024 + row * 64 + at) | (uint32_t)*reinterpret_cast<const uint16_t*>(tile + 1024 + row * 64 + at + 8) << 16;
-      meta = *reinterpret_cast<const uint32_t*>(tile + paged_v_meta(row, G) + 4 * grp);
-    }
-    const float s = bf16_half(meta, 1), z = bf16_half(meta, 0);
-    uint32_t y[4];
+  for (int h = h0; h < h1; h += kBatch) {
+    uint32_t codes[kBatch], meta[kBatch];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)             // (code times scale is exact: 4 bits by 8)
-      y[j] = bf16_pair(fmaf((float)(codes >> (8 * j) & 15u), s, z), fmaf((float)(codes >> (8 * j + 4) & 15u), s, z));
-    *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(keys ? a.k : a.v) + (((size_t)b * v.Hkv + head) * v.n + i) * kD + 8 * c) = make_uint4(y[0], y[1], y[2], y[3]);
+    for (int k = 0; k < kBatch; ++k) {
+      const int hh = min(h + k, h1 - 1);
+      const bool keys = hh < v.Hkv;
+      const uint64_t at = (uint64_t)(keys ? hh : hh - v.Hkv) * v.piece_bytes;
+      if (keys)
+        codes[k] = *reinterpret_cast<const uint32_t*>(k_from + at);
+      else
+        codes[k] = *reinterpret_cast<const uint16_t*>(v_from + at) | (uint32_t)*reinterpret_cast<const uint16_t*>(v_from + at + 8) << 16;
+      meta[k] = *reinterpret_cast<const uint32_t*>(m_from + at + (keys ? 0u : 16u * paged_meta_bytes(G)));
+    }
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const int hh = h + k;
+      if (hh >= h1) break;
+      const bool keys = hh < v.Hkv;
+      const float s = bf16_half(meta[k], 1), z = bf16_half(meta[k], 0);
+      uint32_t y[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)           // (code times scale is exact: 4 bits by 8)
+        y[j] = bf16_pair(fmaf((float)(codes[k] >> (8 * j) & 15u), s, z), fmaf((float)(codes[k] >> (8 * j + 4) & 15u), s, z));
+      *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(keys ? a.k : a.v) + (((size_t)b * v.Hkv + (keys ? hh : hh - v.Hkv)) * v.n + i) * kD + 8 * c) =
+          make_uint4(y[0], y[1], y[2], y[3]);
+    }
   }
 }
 
-// Heads per thread block: all of a token's, fewer as long as the SMs have room.
+// Heads per thread block: all of a token's, fewer as long as the SMs have room (but what a thread has in flight).
 int split_heads(long long blocks, int heads, int n_sms) {
   int each = heads;
-  while (each > 1 && blocks * ((heads + each - 1) / each) < 4 * n_sms) each = (each + 1) / 2;
+  while (each > kBatch && blocks * ((heads + each - 1) / each) < 4 * n_sms) each = (each + 1) / 2;
   return each;
 }
 
