@@ -64,6 +64,7 @@ class Rotation(C.Structure):
         (n, C.c_int32) for n in ("n_positions", "rotary_dim", "interleaved", "reserved")]
 
 
+_DL_CPU, _DL_CUDA = 1, 2                                     # device types of the DLPack interface
 ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "bands": 3, "yarn": 4}
 
 
@@ -262,33 +263,27 @@ def rope_tables(n_positions, rotary_dim=128, base=10000.0, scaling="none", facto
         raise ValueError(f"rope_tables: the scaling is one of {', '.join(ROPE_SCALINGS)}, not {scaling!r}")
     if attention_factor is not None and not attention_factor > 0:
         raise ValueError("rope_tables: the attention factor is positive")
-    n_positions, rotary_dim, start = int(n_positions), int(rotary_dim), int(start)
-    shape = (n_positions, rotary_dim // 2)
     if out is None:
         if n_positions < 1 or rotary_dim < 2:
             raise ValueError("rope_tables: at least one position and two channels are needed")
-        out = tuple(torch.empty(shape, dtype=torch.float32, device=device) for _ in range(2))
+        out = tuple(torch.empty((n_positions, rotary_dim // 2), dtype=torch.float32, device=device) for _ in range(2))
     cos, sin = out
-    for t in out:
-        if t.dtype != torch.float32 or t.shape != shape or not t.is_contiguous() or not t.is_cuda or t.device != cos.device:
-            raise ValueError(f"rope_tables: the outputs must be contiguous float32 {list(shape)} CUDA tensors on one device")
+    dev = cos.device
+    if dev.type != "cuda":
+        raise ValueError("rope_tables: the outputs must be CUDA tensors")
     lo, hi = (slow, fast) if scaling == "yarn" else (low, high)
-    how = RopeScaling(ROPE_SCALINGS[scaling], rotary_dim, base, factor, original, lo, hi, attention_factor or 0.0, 0)
-    with _device_of(cos.device):
-        _check(lib().mixkvq_rope_tables(C.byref(how), start, n_positions, _ptr(cos), _ptr(sin), _stream()), "mixkvq_rope_tables")
+    with _device_of(dev):
+        code = (_native or _calls()).rope_tables(n_positions, rotary_dim, ROPE_SCALINGS[scaling], base, factor, original, lo, hi, attention_factor or 0.0, start, cos, sin,
+                                                 _DL_CUDA, dev.index)
+    if code:
+        raise MixKVQError(code, "mixkvq_rope_tables")
     return out
 
 
-def _rotation(name, cos, sin, positions, interleaved, shape, dev):
-    """The arguments that say what a rotation of part of the head turns by."""
-    if cos.dtype != torch.float32 or sin.dtype != torch.float32 or cos.dim() != 2 or cos.shape != sin.shape:
-        raise ValueError(f"{name}: cos and sin must be float32 tables [n_positions, rotary_dim / 2]")
-    if positions is not None and (positions.dtype != torch.int32 or positions.shape != shape):
-        raise ValueError(f"{name}: positions must be int32 {list(shape)}")
-    for t in (cos, sin) if positions is None else (cos, sin, positions):
-        if not t.is_contiguous() or t.device != dev:
-            raise ValueError(f"{name}: cos, sin and positions must be contiguous tensors on {dev}")
-    return (cos.data_ptr(), sin.data_ptr(), cos.shape[0], None if positions is None else positions.data_ptr(), 2 * cos.shape[1], int(bool(interleaved)))
+def _owner(handle, mem, cfg):
+    """What a call is made on, for the native calls that check their tensors themselves."""
+    dev = mem.device
+    return (handle.value, _DL_CUDA if dev.type == "cuda" else _DL_CPU, dev.index or 0, cfg.n_q_heads, cfg.n_kv_heads)
 
 
 class Cache:
@@ -497,32 +492,11 @@ class Cache:
     def rope_partial(self, q, k, v, cos, sin, positions, interleaved=False, out=None):
         """Rotates the first channels of q [B,Hq,n,128] and k [B,Hkv,n,128] (twice as many as cos, sin float32 [n_positions, pairs] have columns) by positions int32
         [B,n] (negative: no token, its rows are left alone): pairs (i, i + half), or neighbours where `interleaved`.  Layouts, v and `out` as in rope_axes."""
-        cfg, dev, n = self.cfg, self.mem.device, q.shape[2] if q.dim() == 4 else 0
-        turn = _rotation("rope_partial", cos, sin, positions, interleaved, (cfg.batch, n), dev)
-        ins = (q, k, v)
+        dev = self.mem.device
         if out is None:
-            out = tuple(None if t is None else torch.zeros(t.shape, dtype=torch.bfloat16, device=dev) for t in ins)
-        strides, ptrs, outs = [], [], []
-        for i, (t, o, heads) in enumerate(zip(ins, out, (cfg.n_q_heads, cfg.n_kv_heads, cfg.n_kv_heads))):
-            if i == 2 and t is None and o is None:
-                strides += (0, 0, 0)
-                ptrs.append(None)
-                outs.append(None)
-                continue
-            if t is None or o is None:
-                raise ValueError("rope_partial: an input and its output come together")
-            shape = (cfg.batch, heads, n, 128)
-            if t.shape != shape or o.shape != shape or t.dtype != torch.bfloat16 or o.dtype != torch.bfloat16 or t.device != dev or o.device != dev:
-                raise ValueError(f"rope_partial: {'qkv'[i]} and its output must be bfloat16 {list(shape)} tensors on {dev}")
-            s = t.stride()
-            if s[3] != 1 or not o.is_contiguous():
-                raise ValueError("rope_partial: the inputs' last dimension and the outputs must be contiguous")
-            strides += s[:3]
-            ptrs.append(t.data_ptr())
-            outs.append(o.data_ptr())
-        call = (_native or _calls()).rope_partial
+            out = tuple(None if t is None else torch.zeros(t.shape, dtype=torch.bfloat16, device=dev) for t in (q, k, v))
         with _device_of(dev):
-            code = call(self.handle.value, *ptrs, strides, n, *turn, *outs, _stream())
+            code = (_native or _calls()).rope_partial(_owner(self.handle, self.mem, self.cfg), self.cfg.batch, q, k, v, cos, sin, positions, interleaved, *out)
         if code:
             raise MixKVQError(code, "mixkvq_rope_partial")
         return out
@@ -652,6 +626,7 @@ class PagedCache:
         _check(lib().mixkvq_paged_bytes(C.byref(cfg), C.byref(n)), "mixkvq_paged_bytes")
         self.mem = torch.empty(n.value, dtype=torch.uint8, device=device)
         self.handle = C.c_void_p()
+        self._sizes = {}
         with torch.cuda.device(self.mem.device):
             _check(lib().mixkvq_paged_init(C.byref(cfg), _ptr(self.mem), n.value, _stream(), C.byref(self.handle)), "mixkvq_paged_init")
 
@@ -659,6 +634,7 @@ class PagedCache:
         if self.handle:
             lib().mixkvq_paged_destroy(self.handle)
             self.handle = C.c_void_p()
+            self.__dict__.pop("_who", None)
 
     def __del__(self):
         try:
@@ -666,89 +642,54 @@ class PagedCache:
         except Exception:
             pass
 
-    def _sequences(self, name, n, pages, lens, counts):
-        dev = self.mem.device
-        if pages.dtype != torch.int32 or pages.dim() != 2 or pages.stride(1) != 1 or pages.device != dev or pages.shape[1] < 1:
-            raise ValueError(f"{name}: pages must be an int32 [B, pages] tensor on {dev} whose rows are contiguous")
-        B = pages.shape[0]
-        for t, what in ((lens, "lens"), (counts, "counts")):
-            if t is None and what == "counts":
-                continue
-            if t.dtype != torch.int32 or t.shape != (B,) or not t.is_contiguous() or t.device != dev:
-                raise ValueError(f"{name}: {what} must be a contiguous int32 [{B}] tensor on {dev}")
-        stride = pages.stride(0) if B > 1 else pages.shape[1]
-        return (B, n, pages.data_ptr(), pages.shape[1], stride, lens.data_ptr(), None if counts is None else counts.data_ptr())
+    def _on(self):
+        """What the calls are made on (kept: it never changes)."""
+        who = self.__dict__.get("_who")
+        if who is None:
+            who = self._who = _owner(self.handle, self.mem, self.cfg)
+        return who
 
-    def _rows(self, name, B, n, **tensors):
-        """Checks rows [B, heads, n, 128] in bf16 of any layout with a contiguous last dimension; the strides and addresses of q, k and v."""
-        cfg, dev, strides = self.cfg, self.mem.device, []
-        for what, t in tensors.items():
-            if t is None:
-                strides += (0, 0, 0)
-                continue
-            shape = (B, cfg.n_q_heads if what == "q" else cfg.n_kv_heads, n, 128)
-            if t.shape != shape or t.dtype != torch.bfloat16 or t.device != dev or t.stride(3) != 1:
-                raise ValueError(f"{name}: {what} must be a bfloat16 {list(shape)} tensor on {dev} with a contiguous last dimension")
-            strides += t.stride()[:3]
-        return strides
+    def _rotated(self, q, counts, positions):
+        """Room for rotated queries; zeros where rows may be left alone."""
+        return (torch.empty if counts is None and positions is None else torch.zeros)(q.shape, dtype=torch.bfloat16, device=self.mem.device)
 
-    def _append_args(self, name, layer, k, v, q, pages, lens, counts, cos, sin, positions, interleaved, q_out):
-        n, dev = k.shape[2] if k.dim() == 4 else 0, self.mem.device
-        seqs = self._sequences(name, n, pages, lens, counts)
-        B = seqs[0]
-        strides = self._rows(name, B, n, q=q, k=k, v=v)
-        if (cos is None) != (sin is None) or (positions is not None and cos is None):
-            raise ValueError(f"{name}: cos and sin come together, positions with them")
-        turn = (None,) * 6 if cos is None else _rotation(name, cos, sin, positions, interleaved, (B, n), dev)
-        if q is not None:
-            if q_out is None:
-                q_out = (torch.empty if counts is None and positions is None else torch.zeros)(q.shape, dtype=torch.bfloat16, device=dev)
-            elif q_out.shape != q.shape or q_out.dtype != torch.bfloat16 or not q_out.is_contiguous() or q_out.device != dev:
-                raise ValueError(f"{name}: q_out must be a contiguous bfloat16 {list(q.shape)} tensor on {dev}")
-        elif q_out is not None:
-            raise ValueError(f"{name}: q and q_out come together")
-        ptr = lambda t: None if t is None else t.data_ptr()                                        # noqa: E731
-        return (self.handle.value, layer, *seqs, k.data_ptr(), v.data_ptr(), ptr(q), strides, *turn, ptr(q_out)), q_out
+    def _output(self, name, q, counts, dtype):
+        if dtype not in _OUT_TYPES:
+            raise ValueError(f"{name}: the output is float32 or bfloat16")
+        return (torch.empty if counts is None else torch.zeros)(q.shape, dtype=dtype, device=self.mem.device)
 
-    def _out(self, name, q, max_pages, counts, out, workspace, dtype):
-        dev, shape = self.mem.device, q.shape
-        if out is None:
-            if dtype not in _OUT_TYPES:
-                raise ValueError(f"{name}: the output is float32 or bfloat16")
-            out = (torch.empty if counts is None else torch.zeros)(shape, dtype=dtype, device=dev)
-        elif out.shape != shape or out.dtype not in _OUT_TYPES or not out.is_contiguous() or out.device != dev:
-            raise ValueError(f"{name}: out must be a contiguous float32 or bfloat16 {list(shape)} tensor on {dev}")
-        if workspace is None:
-            workspace = torch.empty(self.workspace_bytes(shape[0], shape[2], max_pages), dtype=torch.uint8, device=dev)
-        elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != dev:
-            raise ValueError(f"{name}: the workspace must be a contiguous uint8 tensor on {dev}")
-        return out, workspace
+    def _workspace(self, q, pages):
+        """Scratch of a call that brings none: from torch's allocator, so that it belongs to the current stream, or to the graph that is being captured."""
+        if q.dim() != 4 or pages.dim() != 2:
+            raise ValueError("the queries must be [B, heads, n, 128], the pages [B, pages]")
+        key = (q.shape[0], q.shape[2], pages.shape[1])
+        n = self._sizes.get(key)
+        if n is None:
+            if len(self._sizes) > 4096:
+                self._sizes.clear()
+            n = self._sizes[key] = max(16, self.workspace_bytes(*key))
+        return torch.empty(n, dtype=torch.uint8, device=self.mem.device)
 
     def append(self, layer, k, v, pages, lens, counts=None, q=None, cos=None, sin=None, positions=None, interleaved=False, q_out=None):
         """Stores k, v [B,Hkv,n,128] (bf16, any strides with a contiguous last dimension: views of a fused projection's output too) behind the lens[b] tokens
         that each sequence has; `lens` is not changed.  With cos, sin (tables of rope_tables) keys and q [B,Hq,n,128] turn on the way, by `positions` int32 [B,n] or
         by their places in their sequences.  Returns q rotated and head-major (`q_out`, which may be q itself where it is head-major; None without q)."""
-        args, q_out = self._append_args("append", layer, k, v, q, pages, lens, counts, cos, sin, positions, interleaved, q_out)
-        call = (_native or _calls()).paged_append
+        if q_out is None and q is not None:
+            q_out = self._rotated(q, counts, positions)
         with _device_of(self.mem.device):
-            code = call(*args, _stream())
+            code = (_native or _calls()).paged_append(self._on(), layer, k, v, q, pages, lens, counts, cos, sin, positions, interleaved, q_out)
         if code:
             raise MixKVQError(code, "mixkvq_paged_append")
         return q_out
 
     def read(self, layer, pages, lens, n_tokens, counts=None, out=None):
         """The values that tokens lens[b] .. lens[b] + n_tokens - 1 (counts[b]) of every sequence are held as: (k, v) bf16 [B,Hkv,n_tokens,128]."""
-        seqs = self._sequences("read", int(n_tokens), pages, lens, counts)
-        dev, shape = self.mem.device, (seqs[0], self.cfg.n_kv_heads, int(n_tokens), 128)
         if out is None:
-            out = tuple((torch.empty if counts is None else torch.zeros)(shape, dtype=torch.bfloat16, device=dev) for _ in range(2))
-        for t in out:
-            if t.shape != shape or t.dtype != torch.bfloat16 or not t.is_contiguous() or t.device != dev:
-                raise ValueError(f"read: the outputs must be contiguous bfloat16 {list(shape)} tensors on {dev}")
+            shape = (pages.shape[0], self.cfg.n_kv_heads, max(n_tokens, 0), 128)
+            out = tuple((torch.empty if counts is None else torch.zeros)(shape, dtype=torch.bfloat16, device=self.mem.device) for _ in range(2))
         k, v = out
-        call = (_native or _calls()).paged_read
-        with _device_of(dev):
-            code = call(self.handle.value, layer, *seqs, k.data_ptr(), v.data_ptr(), _stream())
+        with _device_of(self.mem.device):
+            code = (_native or _calls()).paged_read(self._on(), layer, pages, lens, n_tokens, counts, k, v)
         if code:
             raise MixKVQError(code, "mixkvq_paged_read")
         return out
@@ -757,15 +698,12 @@ class PagedCache:
         """The newest n (counts[b]) tokens of every sequence, which has lens[b] tokens with them, attend to its pages, causally among themselves: q [B,Hq,n,128]
         bf16 (rotated, as append returns it) -> [B,Hq,n,128].  `out`: float32 or bfloat16 (allocated as `dtype` when absent, zeros behind the counts).
         `workspace`: a uint8 tensor of at least workspace_bytes(B, n, pages.shape[1]) bytes (allocated here when absent)."""
-        n, dev = q.shape[2] if q.dim() == 4 else 0, self.mem.device
-        seqs = self._sequences("attention", n, pages, lens, counts)
-        self._rows("attention", seqs[0], n, q=q)
-        if not q.is_contiguous():
-            raise ValueError("attention: q must be contiguous")
-        out, workspace = self._out("attention", q, pages.shape[1], counts, out, workspace, dtype)
-        call = (_native or _calls()).paged_attention
-        with _device_of(dev):
-            code = call(self.handle.value, layer, *seqs, q.data_ptr(), out.data_ptr(), _OUT_TYPES[out.dtype], scale, workspace.data_ptr(), workspace.numel(), _stream())
+        if out is None:
+            out = self._output("attention", q, counts, dtype)
+        if workspace is None:
+            workspace = self._workspace(q, pages)
+        with _device_of(self.mem.device):
+            code = (_native or _calls()).paged_attention(self._on(), layer, q, pages, lens, scale, counts, out, workspace)
         if code:
             raise MixKVQError(code, "mixkvq_paged_attention")
         return out
@@ -775,11 +713,14 @@ class PagedCache:
         """append, then attention of the tokens appended (lens: tokens before the call; it is not changed): a decode step, or a chunk of a prompt."""
         if q is None:
             raise ValueError("step: queries are needed")
-        args, q_out = self._append_args("step", layer, k, v, q, pages, lens, counts, cos, sin, positions, interleaved, q_out)
-        out, workspace = self._out("step", q_out, pages.shape[1], counts, out, workspace, dtype)
-        call = (_native or _calls()).paged_step
+        if q_out is None:
+            q_out = self._rotated(q, counts, positions)
+        if out is None:
+            out = self._output("step", q, counts, dtype)
+        if workspace is None:
+            workspace = self._workspace(q, pages)
         with _device_of(self.mem.device):
-            code = call(*args, out.data_ptr(), _OUT_TYPES[out.dtype], scale, workspace.data_ptr(), workspace.numel(), _stream())
+            code = (_native or _calls()).paged_step(self._on(), layer, k, v, q, pages, lens, counts, cos, sin, positions, interleaved, q_out, scale, out, workspace)
         if code:
             raise MixKVQError(code, "mixkvq_paged_step")
         return out

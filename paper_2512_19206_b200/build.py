@@ -6,6 +6,7 @@ the headers of the interpreter that builds).
 """
 from __future__ import annotations
 
+import importlib.util
 import os
 import subprocess
 import sys
@@ -27,6 +28,11 @@ FLAGS = ["-Xcompiler", "-fPIC", "-O3", "-std=c++17", "-lineinfo", "-gencode", "a
 def _headers() -> list[str]:
     return [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cuh", ".h"))] + [
         os.path.join(HERE, "..", "include", "mixkvq.h")]
+
+
+def _torch_headers() -> str:
+    """Where torch keeps its headers (of which _calls needs the C declarations of the DLPack interface); torch itself is not imported."""
+    return os.path.join(importlib.util.find_spec("torch").submodule_search_locations[0], "include")
 
 
 def _newer(path: str, than: float) -> bool:
@@ -64,7 +70,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     src = os.path.join(CSRC, "calls.cpp")
     if force or not os.path.exists(CALLS) or max(os.path.getmtime(src), hdr_time) > os.path.getmtime(CALLS):
         res = subprocess.run(["g++", "-O2", "-std=c++17", "-Wall", "-Wno-cast-function-type", "-fPIC", "-shared",
-                              "-I" + sysconfig.get_paths()["include"], src, "-o", CALLS, "-L" + HERE, "-l:libmixkvq.so",
+                              "-I" + sysconfig.get_paths()["include"], "-isystem", _torch_headers(), src, "-o", CALLS, "-L" + HERE, "-l:libmixkvq.so",
                               "-Wl,-rpath,$ORIGIN"], capture_output=True, text=True)
         if res.returncode != 0:
             raise RuntimeError("g++ failed on " + src + ":\n" + res.stdout + res.stderr)

@@ -5,9 +5,16 @@
 // are a few attribute lookups in C (0.15 us on the null handle).  decode_attention on one sequence of 1024 tokens, calls
 // one after the other: 6.30 -> 5.26 us; calls whose GPU work is longer than the host's are unchanged.  Only the calls that a generation loop makes per layer and token (or draft) are here; the
 // others move enough data for ctypes not to matter.
+//
+// The calls of the paged cache and of the partial rotation take up to thirteen tensors each, whose shapes, types and devices cost 0.5 us apiece in Python: append 10.8 us
+// of the host, attention 10.3, before any launch.  They read them through the tensor type's DLPack exchange table (a published C interface: one call fills in address, shape,
+// strides, type and device) and check everything here.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <ATen/dlpack.h>      // (the interface's declarations alone, plain C)
+
+#include <string>
 #include <vector>
 
 #include "../../include/mixkvq.h"
@@ -212,116 +219,344 @@ PyObject* rope_axes(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return PyLong_FromLong(rc);
 }
 
-mixkvq_paged* paged_of(void* p) { return static_cast<mixkvq_paged*>(p); }
+// ---- Tensors by the exchange table of their type.
+const DLPackExchangeAPI* g_exchange;
+PyTypeObject* g_tensor_type;
 
-// (batch, tokens, address of the page table, its columns, its stride, address of the lengths, of the counts)
-bool sequences(PyObject* const* a, mixkvq_paged_sequences* s) {
-  void *pages, *lens, *counts;
-  if (!integer(a[0], &s->batch) || !integer(a[1], &s->n_tokens) || !raw(a[2], &pages) || !integer(a[3], &s->max_pages) || !integer(a[4], &s->pages_stride) ||
-      !raw(a[5], &lens) || !raw(a[6], &counts))
+bool exchange() {
+  if (g_exchange) return true;
+  PyObject* torch = PyImport_ImportModule("torch");
+  if (!torch) return false;
+  PyObject* type = PyObject_GetAttrString(torch, "Tensor");
+  Py_DECREF(torch);
+  if (!type) return false;
+  PyObject* capsule = PyObject_GetAttrString(type, "__dlpack_c_exchange_api__");
+  const DLPackExchangeAPI* api = capsule ? static_cast<const DLPackExchangeAPI*>(PyCapsule_GetPointer(capsule, "dlpack_exchange_api")) : nullptr;
+  Py_XDECREF(capsule);
+  if (!api || api->header.version.major != DLPACK_MAJOR_VERSION || !api->dltensor_from_py_object_no_sync || !api->current_work_stream) {
+    Py_DECREF(type);
+    if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, "torch's DLPack exchange table is of another version than this module was built for");
     return false;
-  s->pages_dev = static_cast<const int32_t*>(pages);
-  s->lens_dev = static_cast<const int32_t*>(lens);
-  s->counts_dev = static_cast<const int32_t*>(counts);
+  }
+  g_tensor_type = reinterpret_cast<PyTypeObject*>(type);      // (kept)
+  g_exchange = api;
   return true;
 }
 
-// (addresses of cos and sin, their rows, address of the positions, rotated channels, whether pairs are neighbours), the first None: no rotation
-bool rotation(PyObject* const* a, mixkvq_rotation* r, mixkvq_rotation** given) {
-  void *cos, *sin, *positions;
+enum Kind { kBf16, kFloat, kInt32, kUint8, kBf16OrFloat };
+
+struct View {
+  DLTensor t{};
+  bool given = false;
+  void* p() const { return given ? static_cast<char*>(t.data) + t.byte_offset : nullptr; }
+  int64_t stride(int i) const { return t.strides[i]; }
+  bool is_float() const { return t.dtype.code == kDLFloat; }
+  bool of(Kind k) const {
+    const DLDataType& d = t.dtype;
+    if (d.lanes != 1) return false;
+    const bool bf16 = d.code == kDLBfloat && d.bits == 16, f32 = d.code == kDLFloat && d.bits == 32;
+    switch (k) {
+      case kBf16: return bf16;
+      case kFloat: return f32;
+      case kInt32: return d.code == kDLInt && d.bits == 32;
+      case kUint8: return d.code == kDLUInt && d.bits == 8;
+      default: return bf16 || f32;
+    }
+  }
+  bool contiguous() const {
+    for (int i = 0; i < t.ndim; ++i)
+      if (t.shape[i] == 0) return true;
+    int64_t n = 1;
+    for (int i = t.ndim - 1; i >= 0; --i) {
+      if (t.shape[i] != 1 && t.strides[i] != n) return false;
+      n *= t.shape[i];
+    }
+    return true;
+  }
+};
+
+// What a call is made on: the handle, the device of its memory and the heads.
+struct Owner {
+  const char* call;
+  void* handle;
+  DLDevice device;
+  int64_t hq, hkv;
+};
+
+bool refuse(const Owner& o, const char* what, const char* must, const std::vector<int64_t>& shape = {}) {
+  std::string text = std::string(o.call) + ": " + what + " must be " + must;
+  if (!shape.empty()) {
+    text += " [";
+    for (size_t i = 0; i < shape.size(); ++i) text += (i ? ", " : "") + (shape[i] < 0 ? std::string("any") : std::to_string(shape[i]));
+    text += "]";
+  }
+  text += o.device.device_type == kDLCUDA ? " on cuda:" + std::to_string(o.device.device_id) : std::string(" on the CPU");
+  PyErr_SetString(PyExc_ValueError, text.c_str());
+  return false;
+}
+
+// A tensor (None only where `optional`) of this type on the owner's device; its own type and shape errors name `must`.
+bool tensor(const Owner& o, PyObject* x, View* v, Kind kind, int ndim, const char* what, const char* must, bool optional = false) {
+  v->given = false;
+  if (x == Py_None && optional) return true;
+  if (!exchange()) return false;
+  if (!PyObject_TypeCheck(x, g_tensor_type)) return refuse(o, what, must);
+  if (g_exchange->dltensor_from_py_object_no_sync(x, &v->t)) return false;
+  v->given = true;
+  if (v->t.ndim != ndim || !v->of(kind) || v->t.device.device_type != o.device.device_type || v->t.device.device_id != o.device.device_id || (ndim && !v->t.strides))
+    return refuse(o, what, must);
+  return true;
+}
+bool shaped(const Owner& o, const View& v, const char* what, const char* must, const std::vector<int64_t>& shape) {
+  for (int i = 0; i < v.t.ndim; ++i)
+    if (shape[(size_t)i] >= 0 && v.t.shape[i] != shape[(size_t)i]) return refuse(o, what, must, shape);
+  return true;
+}
+
+// Rows [B, heads, n, 128] of bf16 numbers, any strides with a contiguous last dimension, or contiguous ones.
+bool rows(const Owner& o, PyObject* x, View* v, int64_t B, int64_t heads, int64_t n, bool packed, const char* what, bool optional = false, Kind kind = kBf16) {
+  const char* must = kind == kBf16OrFloat ? "a contiguous float32 or bfloat16 tensor" : packed ? "a contiguous bfloat16 tensor" : "a bfloat16 tensor with a contiguous last dimension";
+  if (!tensor(o, x, v, kind, 4, what, must, optional)) return false;
+  if (!v->given) return true;
+  if (!shaped(o, *v, what, must, {B, heads, n, 128})) return false;
+  if (packed ? !v->contiguous() : v->stride(3) != 1) return refuse(o, what, must, {B, heads, n, 128});
+  return true;
+}
+void strides_of(const View& v, int64_t* s) {
+  for (int i = 0; i < 3; ++i) s[i] = v.given ? v.stride(i) : 0;
+}
+
+bool vector_of(const Owner& o, PyObject* x, View* v, int64_t B, const char* what, bool optional) {
+  const char* must = "a contiguous int32 tensor";
+  if (!tensor(o, x, v, kInt32, 1, what, must, optional)) return false;
+  return !v->given || (shaped(o, *v, what, must, {B}) && (v->contiguous() || refuse(o, what, must, {B})));
+}
+
+// The sequences of a call: pages (whose rows say how many sequences), lens, counts.
+bool sequences(const Owner& o, PyObject* pages, PyObject* lens, PyObject* counts, int64_t n, mixkvq_paged_sequences* s) {
+  View p, l, c;
+  const char* must = "an int32 [sequences, pages] tensor with contiguous rows";
+  if (!tensor(o, pages, &p, kInt32, 2, "pages", must)) return false;
+  const int64_t B = p.t.shape[0], P = p.t.shape[1], stride = B > 1 ? p.stride(0) : P;
+  if (P < 1 || (P > 1 && p.stride(1) != 1)) return refuse(o, "pages", must);
+  if (B > INT32_MAX || P > INT32_MAX || stride > INT32_MAX || stride < P || n > INT32_MAX) return refuse(o, "pages", "smaller, and its rows apart");
+  if (!vector_of(o, lens, &l, B, "lens", false) || !vector_of(o, counts, &c, B, "counts", true)) return false;
+  *s = mixkvq_paged_sequences{(int32_t)B, (int32_t)n, static_cast<const int32_t*>(p.p()), (int32_t)P, (int32_t)stride, static_cast<const int32_t*>(l.p()),
+                              static_cast<const int32_t*>(c.p())};
+  return true;
+}
+
+// cos, sin (both None: no rotation, *given null), positions (None: not given)
+bool rotation(const Owner& o, PyObject* cos, PyObject* sin, PyObject* positions, PyObject* interleaved, int64_t B, int64_t n, mixkvq_rotation* r, mixkvq_rotation** given) {
   *given = nullptr;
-  if (a[0] == Py_None) return true;
-  if (!raw(a[0], &cos) || !raw(a[1], &sin) || !integer(a[2], &r->n_positions) || !raw(a[3], &positions) || !integer(a[4], &r->rotary_dim) || !integer(a[5], &r->interleaved))
+  if ((cos == Py_None) != (sin == Py_None) || (cos == Py_None && positions != Py_None)) {
+    PyErr_Format(PyExc_ValueError, "%s: cos and sin come together, positions with them", o.call);
     return false;
-  r->cos_dev = static_cast<const float*>(cos);
-  r->sin_dev = static_cast<const float*>(sin);
-  r->positions_dev = static_cast<const int32_t*>(positions);
-  r->reserved = 0;
+  }
+  if (cos == Py_None) return true;
+  View c, s, p;
+  const char *must = "a contiguous float32 table, cos and sin alike,", *ints = "a contiguous int32 tensor";
+  if (!tensor(o, cos, &c, kFloat, 2, "cos", must) || !tensor(o, sin, &s, kFloat, 2, "sin", must)) return false;
+  if (!c.contiguous() || !s.contiguous() || c.t.shape[0] != s.t.shape[0] || c.t.shape[1] != s.t.shape[1] || c.t.shape[0] > INT32_MAX || c.t.shape[1] > 64)
+    return refuse(o, "cos and sin", must);
+  if (!tensor(o, positions, &p, kInt32, 2, "positions", ints, true)) return false;
+  if (p.given && !(shaped(o, p, "positions", ints, {B, n}) && (p.contiguous() || refuse(o, "positions", ints, {B, n})))) return false;
+  const int side = PyObject_IsTrue(interleaved);
+  if (side < 0) return false;
+  *r = mixkvq_rotation{static_cast<const float*>(c.p()), static_cast<const float*>(s.p()), static_cast<const int32_t*>(p.p()), (int32_t)c.t.shape[0], (int32_t)(2 * c.t.shape[1]), side, 0};
   *given = r;
   return true;
 }
 
-// Nine strides.
-bool nine(PyObject* o, std::vector<int64_t>* v) {
-  if (!whole_numbers(o, v)) return false;
-  if (v->size() != 9) PyErr_SetString(PyExc_ValueError, "nine strides are needed");
-  return v->size() == 9;
+// The owner as the binding describes it: (handle or None, device type, device index, query heads, KV heads)
+bool owner(PyObject* x, const char* call, Owner* o) {
+  o->call = call;
+  int type, index, hq, hkv;
+  if (!PyTuple_Check(x) || PyTuple_GET_SIZE(x) != 5) {
+    PyErr_SetString(PyExc_TypeError, "a tuple of five says what the call is made on");
+    return false;
+  }
+  if (!raw(PyTuple_GET_ITEM(x, 0), &o->handle) || !integer(PyTuple_GET_ITEM(x, 1), &type) || !integer(PyTuple_GET_ITEM(x, 2), &index) || !integer(PyTuple_GET_ITEM(x, 3), &hq) ||
+      !integer(PyTuple_GET_ITEM(x, 4), &hkv))
+    return false;
+  o->device = DLDevice{static_cast<DLDeviceType>(type), index};
+  o->hq = hq;
+  o->hkv = hkv;
+  return true;
+}
+// The device's current stream.
+bool stream_of(const Owner& o, void** st) {
+  *st = nullptr;
+  return o.device.device_type != kDLCUDA || (exchange() && g_exchange->current_work_stream(kDLCUDA, o.device.device_id, st) == 0);
 }
 
-// (handle, addresses of q, k, v, their nine strides, tokens, the rotation (6), addresses of the outputs, stream)
+mixkvq_paged* paged_of(void* p) { return static_cast<mixkvq_paged*>(p); }
+int64_t tokens_of(PyObject* x) {                 // of a [B, heads, n, 128] tensor; what is none is refused later
+  if (!exchange() || !PyObject_TypeCheck(x, g_tensor_type)) {
+    PyErr_Clear();
+    return 0;
+  }
+  DLTensor t{};
+  if (g_exchange->dltensor_from_py_object_no_sync(x, &t)) {
+    PyErr_Clear();
+    return 0;
+  }
+  return t.ndim == 4 ? t.shape[2] : 0;
+}
+
+// (positions, rotated channels, kind, base, factor, original, low, high, attention factor, start, cos, sin, device type, device index)
+PyObject* rope_tables(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!count_is(n, 14)) return nullptr;
+  int count, type, index, rc;
+  mixkvq_rope_scaling sc{};
+  Owner o{"rope_tables", nullptr, {}, 0, 0};
+  if (!integer(a[0], &count) || !integer(a[1], &sc.rotary_dim) || !integer(a[2], &sc.kind) || !integer(a[12], &type) || !integer(a[13], &index)) return nullptr;
+  double* real[6] = {&sc.base, &sc.factor, &sc.original, &sc.low, &sc.high, &sc.attention_factor};
+  for (int i = 0; i < 6; ++i) {
+    *real[i] = PyFloat_AsDouble(a[3 + i]);
+    if (PyErr_Occurred()) return nullptr;
+  }
+  const long long start = PyLong_AsLongLong(a[9]);
+  if (PyErr_Occurred()) return nullptr;
+  o.device = DLDevice{static_cast<DLDeviceType>(type), index};
+  View t[2];
+  void* st;
+  for (int i = 0; i < 2; ++i) {
+    const char* must = "a contiguous float32 tensor";
+    if (!tensor(o, a[10 + i], &t[i], kFloat, 2, "an output", must) || !shaped(o, t[i], "an output", must, {count, sc.rotary_dim / 2})) return nullptr;
+    if (!t[i].contiguous()) {
+      refuse(o, "an output", must);
+      return nullptr;
+    }
+  }
+  if (!stream_of(o, &st)) return nullptr;
+  Py_BEGIN_ALLOW_THREADS
+  rc = mixkvq_rope_tables(&sc, start, count, static_cast<float*>(t[0].p()), static_cast<float*>(t[1].p()), st);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+// (owner, batch, q, k, v or None, cos, sin, positions, interleaved, outputs of q, k, v)
 PyObject* rope_partial(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  void *p[7], *st;
-  int tokens, rc;
-  std::vector<int64_t> strides;
-  mixkvq_rotation r, *turn;
-  if (!count_is(n, 16) || !raw(a[0], &p[0]) || !raw(a[1], &p[1]) || !raw(a[2], &p[2]) || !raw(a[3], &p[3]) || !nine(a[4], &strides) || !integer(a[5], &tokens) ||
-      !rotation(a + 6, &r, &turn) || !raw(a[12], &p[4]) || !raw(a[13], &p[5]) || !raw(a[14], &p[6]) || !raw(a[15], &st))
+  Owner o;
+  int batch, rc;
+  if (!count_is(n, 12) || !owner(a[0], "rope_partial", &o) || !integer(a[1], &batch)) return nullptr;
+  const int64_t tokens = tokens_of(a[2]);
+  if ((a[4] == Py_None) != (a[11] == Py_None)) {
+    PyErr_SetString(PyExc_ValueError, "rope_partial: an input and its output come together");
     return nullptr;
+  }
+  View in[3], out[3];
+  const char *names[3] = {"q", "k", "v"}, *outs[3] = {"the output of q", "the output of k", "the output of v"};
+  int64_t strides[9];
+  for (int i = 0; i < 3; ++i) {
+    const int64_t heads = i == 0 ? o.hq : o.hkv;
+    if (!rows(o, a[2 + i], &in[i], batch, heads, tokens, false, names[i], i == 2) || !rows(o, a[9 + i], &out[i], batch, heads, tokens, true, outs[i], i == 2)) return nullptr;
+    strides_of(in[i], strides + 3 * i);
+  }
+  mixkvq_rotation r, *turn;
+  void* st;
+  if (a[7] == Py_None) {
+    PyErr_SetString(PyExc_ValueError, "rope_partial: positions are needed");
+    return nullptr;
+  }
+  if (!rotation(o, a[5], a[6], a[7], a[8], batch, tokens, &r, &turn) || !stream_of(o, &st)) return nullptr;
   Py_BEGIN_ALLOW_THREADS
-  rc = mixkvq_rope_partial(cache_of(p[0]), p[1], p[2], p[3], strides.data(), tokens, turn, p[4], p[5], p[6], st);
+  rc = mixkvq_rope_partial(cache_of(o.handle), in[0].p(), in[1].p(), in[2].p(), strides, (int)tokens, turn, out[0].p(), out[1].p(), out[2].p(), st);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(rc);
 }
 
-// (handle, layer, the sequences (7), addresses of k, v, q, their nine strides (q, k, v), the rotation (6), address of the rotated queries, stream)
+// What append and step share: k, v, q or None, pages, lens, counts, cos, sin, positions, interleaved, the rotated queries or None
+struct Append {
+  View k, v, q, q_out;
+  int64_t strides[9];
+  mixkvq_paged_sequences s;
+  mixkvq_rotation r, *turn;
+  void* st;
+};
+bool append_arguments(const Owner& o, PyObject* const* a, Append* x) {
+  const int64_t n = tokens_of(a[0]);
+  if (!sequences(o, a[3], a[4], a[5], n, &x->s)) return false;
+  if ((a[2] == Py_None) != (a[10] == Py_None)) {
+    PyErr_Format(PyExc_ValueError, "%s: q and q_out come together", o.call);
+    return false;
+  }
+  if (!rows(o, a[0], &x->k, x->s.batch, o.hkv, n, false, "k") || !rows(o, a[1], &x->v, x->s.batch, o.hkv, n, false, "v") ||
+      !rows(o, a[2], &x->q, x->s.batch, o.hq, n, false, "q", true) || !rows(o, a[10], &x->q_out, x->s.batch, o.hq, n, true, "q_out", true) ||
+      !rotation(o, a[6], a[7], a[8], a[9], x->s.batch, n, &x->r, &x->turn) || !stream_of(o, &x->st))
+    return false;
+  strides_of(x->q, x->strides);
+  strides_of(x->k, x->strides + 3);
+  strides_of(x->v, x->strides + 6);
+  return true;
+}
+// Output and workspace of an attention.
+bool results(const Owner& o, PyObject* out, PyObject* ws, int64_t B, int64_t n, View* y, View* w) {
+  if (!rows(o, out, y, B, o.hq, n, true, "out", false, kBf16OrFloat) || !tensor(o, ws, w, kUint8, 1, "the workspace", "a contiguous uint8 tensor")) return false;
+  return w->contiguous() || refuse(o, "the workspace", "a contiguous uint8 tensor");
+}
+
+// (owner, layer, k, v, q, pages, lens, counts, cos, sin, positions, interleaved, q_out)
 PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  void *h, *k, *v, *q, *q_out, *st;
+  Owner o;
+  Append x;
   int layer, rc;
-  std::vector<int64_t> strides;
-  mixkvq_paged_sequences s;
-  mixkvq_rotation r, *turn;
-  if (!count_is(n, 21) || !raw(a[0], &h) || !integer(a[1], &layer) || !sequences(a + 2, &s) || !raw(a[9], &k) || !raw(a[10], &v) || !raw(a[11], &q) ||
-      !nine(a[12], &strides) || !rotation(a + 13, &r, &turn) || !raw(a[19], &q_out) || !raw(a[20], &st))
-    return nullptr;
+  if (!count_is(n, 13) || !owner(a[0], "append", &o) || !integer(a[1], &layer) || !append_arguments(o, a + 2, &x)) return nullptr;
   Py_BEGIN_ALLOW_THREADS
-  rc = mixkvq_paged_append(paged_of(h), layer, &s, k, v, q, strides.data(), turn, q_out, st);
+  rc = mixkvq_paged_append(paged_of(o.handle), layer, &x.s, x.k.p(), x.v.p(), x.q.p(), x.strides, x.turn, x.q_out.p(), x.st);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(rc);
 }
 
-// (handle, layer, the sequences (7), addresses of the keys' and the values' rows, stream)
+// (owner, layer, pages, lens, tokens, counts, keys, values)
 PyObject* paged_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  void *h, *k, *v, *st;
-  int layer, rc;
+  Owner o;
   mixkvq_paged_sequences s;
-  if (!count_is(n, 12) || !raw(a[0], &h) || !integer(a[1], &layer) || !sequences(a + 2, &s) || !raw(a[9], &k) || !raw(a[10], &v) || !raw(a[11], &st)) return nullptr;
+  View k, v;
+  void* st;
+  int layer, tokens, rc;
+  if (!count_is(n, 8) || !owner(a[0], "read", &o) || !integer(a[1], &layer) || !integer(a[4], &tokens) || !sequences(o, a[2], a[3], a[5], tokens, &s) ||
+      !rows(o, a[6], &k, s.batch, o.hkv, tokens, true, "the keys' output") || !rows(o, a[7], &v, s.batch, o.hkv, tokens, true, "the values' output") || !stream_of(o, &st))
+    return nullptr;
   Py_BEGIN_ALLOW_THREADS
-  rc = mixkvq_paged_read(paged_of(h), layer, &s, k, v, st);
+  rc = mixkvq_paged_read(paged_of(o.handle), layer, &s, k.p(), v.p(), st);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(rc);
 }
 
-// (handle, layer, the sequences (7), addresses of q and of the output, its type, scale, address of the workspace, its bytes, stream)
+// (owner, layer, q, pages, lens, scale, counts, out, workspace)
 PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  void *h, *q, *out, *ws, *st;
-  int layer, type, rc;
-  float scale;
-  size_t bytes;
+  Owner o;
   mixkvq_paged_sequences s;
-  if (!count_is(n, 16) || !raw(a[0], &h) || !integer(a[1], &layer) || !sequences(a + 2, &s) || !raw(a[9], &q) || !raw(a[10], &out) || !integer(a[11], &type) ||
-      !real(a[12], &scale) || !raw(a[13], &ws) || !size(a[14], &bytes) || !raw(a[15], &st))
+  View q, y, w;
+  void* st;
+  int layer, rc;
+  float scale;
+  if (!count_is(n, 9) || !owner(a[0], "attention", &o) || !integer(a[1], &layer)) return nullptr;
+  const int64_t tokens = tokens_of(a[2]);
+  if (!sequences(o, a[3], a[4], a[6], tokens, &s) || !rows(o, a[2], &q, s.batch, o.hq, tokens, true, "q") || !real(a[5], &scale) ||
+      !results(o, a[7], a[8], s.batch, tokens, &y, &w) || !stream_of(o, &st))
     return nullptr;
   Py_BEGIN_ALLOW_THREADS
-  rc = mixkvq_paged_attention(paged_of(h), layer, &s, q, out, type, scale, ws, bytes, st);
+  rc = mixkvq_paged_attention(paged_of(o.handle), layer, &s, q.p(), y.p(), y.is_float() ? MIXKVQ_OUT_FLOAT : MIXKVQ_OUT_BF16, scale, w.p(), (size_t)w.t.shape[0], st);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(rc);
 }
 
-// (as paged_append up to the rotated queries, then address of the output, its type, scale, address of the workspace, its bytes, stream)
+// (owner, layer, k, v, q, pages, lens, counts, cos, sin, positions, interleaved, q_out, scale, out, workspace)
 PyObject* paged_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  void *h, *k, *v, *q, *q_out, *out, *ws, *st;
-  int layer, type, rc;
+  Owner o;
+  Append x;
+  View y, w;
+  int layer, rc;
   float scale;
-  size_t bytes;
-  std::vector<int64_t> strides;
-  mixkvq_paged_sequences s;
-  mixkvq_rotation r, *turn;
-  if (!count_is(n, 26) || !raw(a[0], &h) || !integer(a[1], &layer) || !sequences(a + 2, &s) || !raw(a[9], &k) || !raw(a[10], &v) || !raw(a[11], &q) ||
-      !nine(a[12], &strides) || !rotation(a + 13, &r, &turn) || !raw(a[19], &q_out) || !raw(a[20], &out) || !integer(a[21], &type) || !real(a[22], &scale) ||
-      !raw(a[23], &ws) || !size(a[24], &bytes) || !raw(a[25], &st))
+  if (!count_is(n, 16) || !owner(a[0], "step", &o) || !integer(a[1], &layer) || !append_arguments(o, a + 2, &x) || !real(a[13], &scale) ||
+      !results(o, a[14], a[15], x.s.batch, x.s.n_tokens, &y, &w))
     return nullptr;
   Py_BEGIN_ALLOW_THREADS
-  rc = mixkvq_paged_step(paged_of(h), layer, &s, k, v, q, strides.data(), turn, q_out, out, type, scale, ws, bytes, st);
+  rc = mixkvq_paged_step(paged_of(o.handle), layer, &x.s, x.k.p(), x.v.p(), x.q.p(), x.strides, x.turn, x.q_out.p(), y.p(),
+                         y.is_float() ? MIXKVQ_OUT_FLOAT : MIXKVQ_OUT_BF16, scale, w.p(), (size_t)w.t.shape[0], x.st);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(rc);
 }
@@ -337,6 +572,7 @@ PyMethodDef methods[] = {{"decode_attention", fast(decode_attention), METH_FASTC
                          {"quantize_append", fast(quantize_append), METH_FASTCALL, nullptr},
                          {"chunk", fast(chunk), METH_FASTCALL, nullptr},
                          {"rope_axes", fast(rope_axes), METH_FASTCALL, nullptr},
+                         {"rope_tables", fast(rope_tables), METH_FASTCALL, nullptr},
                          {"rope_partial", fast(rope_partial), METH_FASTCALL, nullptr},
                          {"paged_append", fast(paged_append), METH_FASTCALL, nullptr},
                          {"paged_read", fast(paged_read), METH_FASTCALL, nullptr},

@@ -12,11 +12,6 @@ from paper_2512_19206_b200 import binding
 B, HQ, HKV, N = 2, 8, 2, 5
 
 
-class Recorder:
-    def __getattr__(self, name):
-        return lambda *args: self.calls.append((name, args)) or 0
-
-
 @pytest.fixture(scope="module", autouse=True)
 def built():
     from paper_2512_19206_b200 import build
@@ -24,23 +19,21 @@ def built():
 
 
 @pytest.fixture
-def native(monkeypatch):
-    n = Recorder()
-    n.calls = []
-    monkeypatch.setattr(binding, "_native", n)
-    monkeypatch.setattr(binding, "_stream", lambda: 0)
+def cache(monkeypatch):
+    """A cache without a handle, its memory on the CPU: the calls check their arguments and the library refuses the handle (-1)."""
     monkeypatch.setattr(binding, "_device_of", lambda dev: contextlib.nullcontext())
-    return n
-
-
-@pytest.fixture
-def cache(native):
     c = object.__new__(binding.PagedCache)
     c.handle = C.c_void_p(None)
     c.cfg = binding.make_paged_config(1, HQ, HKV, 4, page_tokens=16)
     c.mem = torch.empty(1, dtype=torch.uint8)
-    c.native = native
+    c._sizes = {}
     return c
+
+
+def passes(call):
+    with pytest.raises(binding.MixKVQError) as e:
+        call()
+    assert e.value.code == -1
 
 
 def tensors(n=N):
@@ -51,23 +44,20 @@ def where():
     return dict(pages=torch.zeros((B, 3), dtype=torch.int32), lens=torch.zeros(B, dtype=torch.int32))
 
 
-def test_arguments_are_passed_on(cache):
+def test_arguments_that_are_in_order(cache):
     t, w = tensors(), where()
     cos = torch.zeros((7, 32))
     wide = torch.zeros((B, 9), dtype=torch.int32)
-    assert cache.append(0, t["k"], t["v"], **w) is None
-    q = cache.append(0, **t, pages=wide[:, 2:6], lens=w["lens"], counts=w["lens"], cos=cos, sin=cos, interleaved=True)
-    assert q.shape == t["q"].shape and not q.any()
-    out = cache.attention(0, t["q"], **w, scale=0.1, dtype=torch.bfloat16)
-    assert out.dtype == torch.bfloat16
-    cache.step(0, **t, **w, scale=0.1)
-    k, v = cache.read(0, **w, n_tokens=3)
-    assert k.shape == v.shape == (B, HKV, 3, 128)
-    (n0, a0), (n1, a1), (n2, a2), (n3, a3), (n4, a4) = cache.native.calls
-    assert (n0, n1, n2, n3, n4) == ("paged_append", "paged_append", "paged_attention", "paged_step", "paged_read")
-    assert a0[2:4] == (B, N) and a0[5:7] == (3, 3) and a0[8] is None and a0[11] is None and a0[13:19] == (None,) * 6
-    assert a1[5:7] == (4, 9) and a1[8] == w["lens"].data_ptr() and a1[15] == 7 and a1[16] is None and a1[17:19] == (64, 1)
-    assert a2[11] == 1 and a2[14] == cache.workspace_bytes(B, N, 3) and len(a3) == 26 and len(a1) == 21 and a4[3] == 3
+    x = torch.zeros((B, N, HQ + 2 * HKV, 128), dtype=torch.bfloat16)
+    views = dict(zip("qkv", (y.transpose(1, 2) for y in x.split((HQ, HKV, HKV), 2))))
+    passes(lambda: cache.append(0, t["k"], t["v"], **w))
+    passes(lambda: cache.append(0, **views, pages=wide[:, 2:6], lens=w["lens"], counts=w["lens"], cos=cos, sin=cos, interleaved=True))
+    passes(lambda: cache.append(0, **t, **w, cos=cos, sin=cos, positions=torch.zeros((B, N), dtype=torch.int32), q_out=t["q"]))
+    passes(lambda: cache.attention(0, t["q"], **w, scale=0.1, dtype=torch.bfloat16))
+    passes(lambda: cache.step(0, **views, **w, scale=1))
+    passes(lambda: cache.read(0, **w, n_tokens=3))
+    one = torch.zeros((1, 1), dtype=torch.int32)
+    passes(lambda: cache.read(0, one.expand(1, 1), torch.zeros(1, dtype=torch.int32), 1))
 
 
 @pytest.mark.parametrize("bad", ["dtype", "batch", "heads", "tokens", "last dimension", "flat", "pages type", "pages rows", "pages strided", "lens", "lens type", "counts",
@@ -87,7 +77,6 @@ def test_append_refusals(cache, bad):
         cache.append(**args)
     with pytest.raises(ValueError):
         cache.step(**args, scale=1.0)
-    assert not cache.native.calls
 
 
 def test_append_and_step_without_queries(cache):
@@ -96,7 +85,6 @@ def test_append_and_step_without_queries(cache):
         cache.append(0, t["k"], t["v"], **where(), q_out=t["q"])
     with pytest.raises(ValueError):
         cache.step(0, t["k"], t["v"], None, **where(), scale=1.0)
-    assert not cache.native.calls
 
 
 @pytest.mark.parametrize("bad", ["dtype", "heads", "strided", "out shape", "out dtype", "out type", "workspace", "pages", "counts"])
@@ -110,26 +98,54 @@ def test_attention_refusals(cache, bad):
         cache.attention(**args)
     with pytest.raises(ValueError):
         cache.read(0, **where(), n_tokens=2, out=(q, q))
-    assert not cache.native.calls
+
+
+@pytest.mark.parametrize("bad", ["dtype", "heads", "tokens", "tables", "no tables", "positions", "no positions", "out", "out alone", "last dimension"])
+def test_rotation_refusals(monkeypatch, bad):
+    monkeypatch.setattr(binding, "_device_of", lambda dev: contextlib.nullcontext())
+    c = object.__new__(binding.Cache)
+    c.handle, c.cfg, c.mem = C.c_void_p(None), binding.make_config(1, B, HQ, HKV, 16), torch.empty(1, dtype=torch.uint8)
+    t, cos, pos = tensors(), torch.zeros((7, 32)), torch.zeros((B, N), dtype=torch.int32)
+    args = dict(**t, cos=cos, sin=cos, positions=pos)
+    passes(lambda: c.rope_partial(**args))
+    passes(lambda: c.rope_partial(**{**args, "v": None}, out=(t["q"], t["k"], None)))
+    args.update({"dtype": dict(q=t["q"].float()), "heads": dict(k=t["q"]), "tokens": dict(v=t["v"][:, :, :4]), "tables": dict(sin=cos[:3]), "no tables": dict(cos=None, sin=None),
+                 "positions": dict(positions=pos.long()), "no positions": dict(positions=None), "out": dict(out=(t["q"].transpose(1, 2), t["k"], t["v"])),
+                 "out alone": dict(out=(t["q"], t["k"], None)), "last dimension": dict(k=t["k"].transpose(2, 3).contiguous().transpose(2, 3))}[bad])
+    with pytest.raises(ValueError if bad != "no tables" else (ValueError, binding.MixKVQError)):
+        c.rope_partial(**args)
 
 
 def test_native_calls_check_their_arguments():
     n = binding._calls()
-    seqs = [1, 1, None, 1, 1, None, None]
-    rest = {"rope_partial": [None, None, None, None, [0] * 9, 1, None, None, 0, None, 0, 0, None, None, None, 0],
-            "paged_append": [None, 0, *seqs, None, None, None, [0] * 9, None, None, 0, None, 0, 0, None, 0], "paged_read": [None, 0, *seqs, None, None, 0],
-            "paged_attention": [None, 0, *seqs, None, None, 0, 1.0, None, 0, 0],
-            "paged_step": [None, 0, *seqs, None, None, None, [0] * 9, None, None, 0, None, 0, 0, None, None, 0, 1.0, None, 0, 0]}
-    for name, args in rest.items():
+    who = (None, 1, 0, HQ, HKV)
+    t, w = tensors(), where()
+    seqs, turn, ws = (w["pages"], w["lens"], None), (None, None, None, False), torch.zeros(16, dtype=torch.uint8)
+    calls = {"rope_partial": [who, B, t["q"], t["k"], None, torch.zeros((7, 32)), torch.zeros((7, 32)), torch.zeros((B, N), dtype=torch.int32), 0, t["q"], t["k"], None],
+             "paged_append": [who, 0, t["k"], t["v"], None, *seqs, *turn, None], "paged_read": [who, 0, w["pages"], w["lens"], N, None, t["k"], t["v"]],
+             "paged_attention": [who, 0, t["q"], w["pages"], w["lens"], 1.0, None, t["q"], ws],
+             "paged_step": [who, 0, t["k"], t["v"], t["q"], *seqs, *turn, t["q"].clone(), 1.0, t["q"].clone(), ws]}
+    for name, args in calls.items():
         call = getattr(n, name)
         assert call(*args) == -1
         with pytest.raises(TypeError):
             call(*args[:-1])
+        with pytest.raises(TypeError):
+            call(who[:4], *args[1:])
         for i, a in enumerate(args):
-            if isinstance(a, list):
-                for bad in ([0] * 8, None, [1 << 80] * 9):
-                    with pytest.raises((ValueError, TypeError, OverflowError)):
+            if isinstance(a, torch.Tensor):
+                for bad in (3, "x", a.double(), a[None]):
+                    with pytest.raises(ValueError):
                         call(*args[:i], bad, *args[i + 1:])
+        with pytest.raises(ValueError):                       # another device than the tensors'
+            call((None, 2, 0, HQ, HKV), *args[1:])
+    x = torch.zeros((9, 64))
+    assert n.rope_tables(9, 128, 0, 1e4, 1.0, 0.0, 1.0, 4.0, 0.0, 0, x, x.clone(), 1, 0) in (0, -1, -6)
+    for i, bad, error in ((10, x[:3], ValueError), (3, "a", TypeError), (9, 1 << 80, OverflowError), (10, 5, ValueError)):
+        args = [9, 128, 0, 1e4, 1.0, 0.0, 1.0, 4.0, 0.0, 0, x, x.clone(), 1, 0]
+        args[i] = bad
+        with pytest.raises(error):
+            n.rope_tables(*args)
 
 
 def test_null_handles_sizes_and_configurations():
