@@ -47,6 +47,15 @@ struct PagedView {
     if (ok != l) atomicOr(status, (uint32_t)MIXKVQ_DEV_BAD_LENGTH);
     return ok;
   }
+  // both, their loads under way together
+  __device__ void sequence(int b, int& c, int& l) const {
+    const int given = counts == nullptr ? n : counts[b];
+    const long long held = lens[b], most = (long long)max_pages << lg_page;
+    c = min(max(given, 0), n);
+    const long long all = held + (add_counts ? c : 0);
+    l = (int)(all < 0 ? 0 : all > most ? most : all);
+    if (c != given || l != all) atomicOr(status, (uint32_t)MIXKVQ_DEV_BAD_LENGTH);
+  }
   // where token i behind the lens[b] of sequence b goes, -1: nowhere
   __device__ int place(int b, int i) const {
     const long long t = (long long)lens[b] + i;

@@ -20,26 +20,36 @@ namespace mixkvq {
 
 namespace {
 
-constexpr int kWarps = 4;
+constexpr int kWarps = 4;                        // of a thread block with pieces of streams, 16 of one with a whole short stream
 constexpr int kUnit = 32;                        // tokens
 constexpr int kStages = 2;                       // units in a warp's ring, per tile of 8 query rows
-constexpr int kPartFloats = kD + 2;              // of a row's sums: o[128], reference, denominator
+constexpr int kPartFloats = kD + 4;              // of a row's sums: o[128], reference, denominator, (pad)
 constexpr uint32_t kPolls = 1u << 21;
 constexpr int kBelow = 16;                       // a reference is brought this much (in powers of two) above its row's largest logit: sums of large values keep off fp32's end
 constexpr int kRise = 8;                         // and raised when a logit comes this much nearer
 constexpr int kScaleTo = 5 + kBelow;             // the largest value scale of a group times its factor is brought to 2^21 .. 2^22, and lowered when it comes to 2^23
-constexpr int kAhead = 8;                        // units that the beginning of a piece counts as
+constexpr int kAhead = 12;                       // units that the beginning of a piece counts as
 
+struct __align__(16) Broken {                    // a stream that begins in a thread block's range and ends in another's
+  int b, h, row0, last;                          // last: the thread block that has its end, -1: none
+};
 struct Plan {
   int rows;                                      // of a block of query rows
   int direct;                                    // a thread block per stream, nothing to merge
+  uint32_t g_inv;                                // x / g is the upper half of x * g_inv (x below 2^28; 0: g is 1)
   float* parts;                                  // [2 * thread blocks][rows][kPartFloats]
-  long long* prefix;                             // [B + 1] units before each sequence, behind the parts; then the number of parts
+  Broken* broken;                                // [thread blocks]
 };
 
-__device__ __forceinline__ int row_blocks(int count, int g, int rows) { return (count * g + rows - 1) / rows; }
-
 __device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
+
+__device__ __forceinline__ int row_blocks(int count, int g, int rows) { return (count * g + rows - 1) / rows; }
+__device__ __forceinline__ int over_heads(const Plan& plan, int x) { return plan.g_inv == 0u ? x : (int)__umulhi((uint32_t)x, plan.g_inv); }
+// total * i / parts, in 32 bits where that is enough
+__device__ __forceinline__ long long cut(long long total, int parts, int i) {
+  const unsigned long long x = (unsigned long long)total * (unsigned)i;
+  return x >> 32 ? (long long)(x / (unsigned)parts) : (long long)((unsigned)x / (unsigned)parts);
+}
 
 // A stream: a block of query rows of a KV head of a sequence.
 struct Stream {
@@ -73,17 +83,17 @@ __device__ __forceinline__ void load_meta(uint32_t a, uint32_t (&w)[kNG]) {
   }
 }
 
-template <int kG, int kNT>
-__global__ void __launch_bounds__(kWarps * 32, kNT == 1 ? 3 : 2)
+template <int kG, int kNT, int kW>
+__global__ void __launch_bounds__(kW * 32, kW > kWarps ? 1 : kNT == 1 ? 3 : 2)
 pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ Plan plan) {
   constexpr int kNG = kD / kG, kMeta = 512 / kG, kTileBytes = 2048 + 32 * kMeta, kRows = 8 * kNT, kUnitBytes = 2 * kTileBytes, stages = kStages * kNT;
   extern __shared__ __align__(128) unsigned char smem[];
   const PagedView& v = a.view;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, t = lane & 3;
   const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * stages * kUnitBytes);
-  unsigned char* behind = smem + kWarps * stages * kUnitBytes;
+  unsigned char* behind = smem + kW * stages * kUnitBytes;
   const uint32_t bars = smem_u32(behind) + 8u * (uint32_t)(warp * stages);
-  long long* prefix = reinterpret_cast<long long*>(behind + 8 * kWarps * stages);
+  long long* prefix = reinterpret_cast<long long*>(behind + 8 * kW * stages);
   if (lane == 0) {
     for (int i = 0; i < stages; ++i) mbar_init(bars + 8u * i, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -91,42 +101,58 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
   __syncwarp();
   dependency_wait();
   auto units_of = [&](int len) { return max(1, (len + kUnit - 1) / kUnit); };
-  long long pos, end, total = 0;
+  auto over_g = [&](int x) { return over_heads(plan, x); };
+  auto positions = [&](int count, int len) { return (long long)row_blocks(count, v.g, kRows) * v.Hkv * (kAhead + units_of(len)); };
+  // ---- the line: the positions of all sequences, in a lane each where there are 32 at most (no shared memory, no barrier), and the thread block's range of them
+  const bool few = v.B <= 32;
+  int seq_count = 0, seq_len = 0;
+  long long pos, end, total = 0, upto = 0;       // upto: positions of the sequences up to the lane's
   int parts = gridDim.x;
   if (plan.direct) {
     pos = 0;
     end = 1;
   } else {
-    for (int b = tid; b < v.B; b += kWarps * 32) {
-      const int count = v.count(b), len = v.length(b, v.add_counts ? count : 0);
-      prefix[b + 1] = (long long)row_blocks(count, v.g, kRows) * v.Hkv * (kAhead + units_of(len));
-    }
-    if (tid == 0) prefix[0] = 0;
-    __syncthreads();
-    if (warp == 0) {
-      long long sum = 0;
-      for (int b0 = 0; b0 < v.B; b0 += 32) {
-        long long x = b0 + lane < v.B ? prefix[b0 + lane + 1] : 0;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-          const long long y = __shfl_up_sync(0xffffffffu, x, d);
-          if (lane >= d) x += y;
-        }
-        if (b0 + lane < v.B) prefix[b0 + lane + 1] = sum + x;
-        sum += __shfl_sync(0xffffffffu, x, 31);
+    if (few) {
+      if (lane < v.B) {
+        v.sequence(lane, seq_count, seq_len);
+        upto = positions(seq_count, seq_len);
       }
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const long long y = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += y;
+      }
+      total = __shfl_sync(0xffffffffu, upto, 31);
+    } else {
+      for (int b = tid; b < v.B; b += kW * 32) {
+        int count, len;
+        v.sequence(b, count, len);
+        prefix[b + 1] = positions(count, len);
+      }
+      if (tid == 0) prefix[0] = 0;
+      __syncthreads();
+      if (warp == 0) {
+        long long sum = 0;
+        for (int b0 = 0; b0 < v.B; b0 += 32) {
+          long long x = b0 + lane < v.B ? prefix[b0 + lane + 1] : 0;
+#pragma unroll
+          for (int d = 1; d < 32; d <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, x, d);
+            if (lane >= d) x += y;
+          }
+          if (b0 + lane < v.B) prefix[b0 + lane + 1] = sum + x;
+          sum += __shfl_sync(0xffffffffu, x, 31);
+        }
+      }
+      __syncthreads();
+      total = prefix[v.B];
     }
-    __syncthreads();
-    total = prefix[v.B];
     // at least the beginning of a piece and a unit for every warp
-    parts = (int)min((long long)gridDim.x, max(1ll, (total + kAhead + kWarps - 1) / (kAhead + kWarps)));
-    if (blockIdx.x == 0) {
-      for (int b = tid; b <= v.B; b += kWarps * 32) plan.prefix[b] = prefix[b];
-      if (tid == 0) plan.prefix[v.B + 1] = parts;
-    }
+    parts = (int)min((long long)gridDim.x, max(1ll, (total + kAhead + kW - 1) / (kAhead + kW)));
+    if (tid == 0) plan.broken[blockIdx.x] = Broken{0, 0, 0, -1};
     if ((int)blockIdx.x >= parts) return;
-    pos = split_begin(total, parts, blockIdx.x);
-    end = split_begin(total, parts, blockIdx.x + 1);
+    pos = cut(total, parts, blockIdx.x);
+    end = cut(total, parts, blockIdx.x + 1);
   }
   const int pi = r ^ (r >> 1 & 1);               // token of a tile that the lane's rows of its products are (and 8 more)
   uint32_t phase = 0;                            // of the warp's barriers, a bit each
@@ -138,17 +164,15 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
     }
   };
 
-  int b_at = 0;
   while (pos < end) {
     // ---- the piece: units u0 .. u1 - 1 of a stream
     Stream st;
-    int u0, u1, stream;
+    int u0, u1;
+    long long first;
     if (plan.direct) {
-      const int blocks = row_blocks(v.n, v.g, kRows);
-      stream = blockIdx.x;
+      const int blocks = row_blocks(v.n, v.g, kRows), stream = blockIdx.x;
       st.b = stream / (blocks * v.Hkv);
-      st.count = v.count(st.b);
-      st.len = v.length(st.b, v.add_counts ? st.count : 0);
+      v.sequence(st.b, st.count, st.len);
       const int s = stream - st.b * blocks * v.Hkv;
       st.h = s / blocks;
       st.row0 = (s - st.h * blocks) * kRows;
@@ -156,26 +180,33 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
       u0 = 0;
       u1 = st.units;
       pos = 1;
+      first = 0;
       if (st.row0 >= st.count * v.g) return;
     } else {
-      if (b_at == 0) {
-        int lo = 0, hi = v.B;                    // the last b with prefix[b] <= pos that has units
+      long long off;
+      if (few) {
+        st.b = __ffs(__ballot_sync(0xffffffffu, upto > pos)) - 1;
+        st.count = __shfl_sync(0xffffffffu, seq_count, st.b);
+        st.len = __shfl_sync(0xffffffffu, seq_len, st.b);
+        const long long before = __shfl_sync(0xffffffffu, upto, max(st.b - 1, 0));
+        off = pos - (st.b > 0 ? before : 0);
+      } else {
+        int lo = 0, hi = v.B;                    // the last sequence that begins at or before the position, and has any
         while (hi - lo > 1) {
           const int mid = (lo + hi) >> 1;
           if (prefix[mid] <= pos) lo = mid; else hi = mid;
         }
-        b_at = lo;
+        while (prefix[lo + 1] <= pos) ++lo;
+        st.b = lo;
+        v.sequence(st.b, st.count, st.len);
+        off = pos - prefix[st.b];
       }
-      while (prefix[b_at + 1] <= pos) ++b_at;
-      st.b = b_at;
-      st.count = v.count(st.b);
-      st.len = v.length(st.b, v.add_counts ? st.count : 0);
       st.units = units_of(st.len);
-      const long long off = pos - prefix[b_at];
-      const int s = (int)(off / (kAhead + st.units)), blocks = row_blocks(st.count, v.g, kRows);
+      const int blocks = row_blocks(st.count, v.g, kRows), each = kAhead + st.units;
+      const int s = off >> 32 ? (int)(off / each) : (int)((uint32_t)off / (uint32_t)each);
       st.h = s / blocks;
       st.row0 = (s - st.h * blocks) * kRows;
-      const long long first = pos - (off - (long long)s * (kAhead + st.units)) + kAhead;     // where the stream's first unit is in the line
+      first = pos - (off - (long long)s * each) + kAhead;     // where the stream's first unit is in the line
       u0 = (int)max(0ll, pos - first);
       u1 = (int)min((long long)st.units, end - first);
       pos = min(end, first + st.units);
@@ -184,9 +215,21 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
     const bool begins = u0 == 0, whole = begins && u1 == st.units;
     // tokens that the last row of the block sees: units behind them are left out
     const int last_row = min(st.row0 + kRows, st.count * v.g) - 1;
-    const int most = min(st.len, max(0, st.len - st.count + last_row / v.g + 1));
+    const int most = min(st.len, max(0, st.len - st.count + over_g(last_row) + 1));
     const int u_last = min(u1, (most + kUnit - 1) / kUnit);
-    const int mine = !dead && u_last > u0 + warp ? (u_last - u0 - warp + kWarps - 1) / kWarps : 0;      // units of the warp: u0 + warp + kWarps i
+    const int mine = !dead && u_last > u0 + warp ? (u_last - u0 - warp + kW - 1) / kW : 0;      // units of the warp: u0 + warp + kW i
+
+    // ---- the queries' loads, under way before the page numbers are waited for
+    uint4 qw[kNT][4];
+#pragma unroll
+    for (int nt = 0; nt < kNT; ++nt) {
+      const int row = st.row0 + 8 * nt + r;
+      const bool there = row < st.count * v.g;
+      const int i = over_g(row), head = row - i * v.g;
+      const uint16_t* src = static_cast<const uint16_t*>(a.q) + (((size_t)st.b * v.Hq + st.h * v.g + head) * v.n + i) * kD + 8 * t;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) qw[nt][j] = there ? *reinterpret_cast<const uint4*>(src + 32 * j) : make_uint4(0u, 0u, 0u, 0u);
+    }
 
     // ---- copies: a lane has one of 32 of the warp's units: where it lies (and the page of its second half where a page is half a unit)
     const char* src0 = nullptr;
@@ -195,7 +238,7 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
     const int32_t* page_row = v.pages + (size_t)st.b * v.pages_stride;
     auto issue = [&](int i) {
       if ((i & 31) == 0) {
-        const int tok = (u0 + warp + kWarps * (i + lane)) * kUnit;
+        const int tok = (u0 + warp + kW * (i + lane)) * kUnit;
         const bool need0 = i + lane < mine, need1 = need0 && tok + 16 < most;
         const int p0 = need0 && tok < most ? page_row[tok >> v.lg_page] : 0;
         p1 = v.lg_page == 4 ? (need1 ? page_row[(tok + 16) >> 4] : 0) : p0;
@@ -232,13 +275,7 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
     int sees[kNT][2];
 #pragma unroll
     for (int nt = 0; nt < kNT; ++nt) {
-      const int row = st.row0 + 8 * nt + r;
-      const bool there = row < st.count * v.g;
-      const int i = row / v.g, head = row - i * v.g;
-      const uint16_t* src = static_cast<const uint16_t*>(a.q) + (((size_t)st.b * v.Hq + st.h * v.g + head) * v.n + i) * kD + 8 * t;
-      uint4 w[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) w[j] = there ? *reinterpret_cast<const uint4*>(src + 32 * j) : make_uint4(0u, 0u, 0u, 0u);
+      const uint4(&w)[4] = qw[nt];
       uint32_t top = 0;                          // the largest magnitude's bits (finite or not)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -290,7 +327,7 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
         qscale[nt][c] = a.scale_log2e * (pow2i(-__shfl_sync(0xffffffffu, e, from)) * 16777216.f);
         const int x = st.row0 + 8 * nt + 2 * t + c;
         // (rows that are none are computed like the others and written nowhere)
-        sees[nt][c] = x < st.count * v.g ? max(0, st.len - st.count + x / v.g + 1) : st.len;
+        sees[nt][c] = x < st.count * v.g ? max(0, st.len - st.count + over_g(x) + 1) : st.len;
       }
     }
     int fewest = st.len;
@@ -501,7 +538,7 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
     };
     int done = 0;                                // units waited for
     for (; done < mine; ++done) {
-      const int stage = done % stages, tok = (u0 + warp + kWarps * done) * kUnit;
+      const int stage = done % stages, tok = (u0 + warp + kW * done) * kUnit;
       uint32_t there = tok + 16 < most ? 3u : 1u;
       if (gaps) {
         const int q0 = page_row[tok >> v.lg_page], q1 = there == 3u ? page_row[(tok + 16) >> v.lg_page] : -1;
@@ -563,24 +600,24 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
       if (r == 0) sts64(at + kD * 4, __float_as_uint(w.ref[c]), __float_as_uint(w.l[c]));
     }
     __syncthreads();
-    // ---- the warps' sums together: a warp has every fourth row, a lane four channels
-    const uint32_t first = smem_u32(smem);
-    for (int row = warp; row < kRows; row += kWarps) {
+    // ---- the warps' sums together: a warp per row, a lane four channels
+    const uint32_t base0 = smem_u32(smem);
+    for (int row = warp; row < kRows; row += kW) {
       const int x = st.row0 + row;
       if (x >= st.count * v.g) break;
-      float m[kWarps], l[kWarps], top = -1e30f;
+      float m[kW], l[kW], top = -1e30f;
 #pragma unroll
-      for (int i = 0; i < kWarps; ++i) {
-        const uint2 ml = lds64(first + (uint32_t)(i * stages * kUnitBytes + (row * kStride + kD) * 4));
+      for (int i = 0; i < kW; ++i) {
+        const uint2 ml = lds64(base0 + (uint32_t)(i * stages * kUnitBytes + (row * kStride + kD) * 4));
         m[i] = __uint_as_float(ml.x);
         l[i] = __uint_as_float(ml.y);
         top = fmaxf(top, m[i]);
       }
       float y[4] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < kWarps; ++i) {
+      for (int i = 0; i < kW; ++i) {
         const float f = ex2_approx(m[i] - top);
-        const uint4 o = lds128(first + (uint32_t)(i * stages * kUnitBytes + (row * kStride + 4 * lane) * 4));
+        const uint4 o = lds128(base0 + (uint32_t)(i * stages * kUnitBytes + (row * kStride + 4 * lane) * 4));
         sum = fmaf(l[i], f, sum);
         y[0] = fmaf(__uint_as_float(o.x), f, y[0]);
         y[1] = fmaf(__uint_as_float(o.y), f, y[1]);
@@ -588,7 +625,7 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
         y[3] = fmaf(__uint_as_float(o.w), f, y[3]);
       }
       if (whole) {
-        const int i = x / v.g, head = x - i * v.g;
+        const int i = over_g(x), head = x - i * v.g;
         const size_t at = (((size_t)st.b * v.Hq + st.h * v.g + head) * v.n + i) * kD + 4 * lane;
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         if (a.out_bf16)
@@ -597,89 +634,105 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
           *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at) = make_float4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
       } else {
         float* to = plan.parts + ((size_t)(2 * blockIdx.x + (begins ? 1 : 0)) * kRows + row) * kPartFloats;
-        *reinterpret_cast<float2*>(to + 4 * lane) = make_float2(y[0], y[1]);
-        *reinterpret_cast<float2*>(to + 4 * lane + 2) = make_float2(y[2], y[3]);
+        *reinterpret_cast<float4*>(to + 4 * lane) = make_float4(y[0], y[1], y[2], y[3]);
         if (lane == 0) *reinterpret_cast<float2*>(to + kD) = make_float2(top, sum);
       }
+    }
+    if (begins && !whole && tid == 0) {
+      // the thread block whose range has the stream's last unit: the last one that begins at or before it
+      const long long u = first + st.units - 1;
+      int c = min(parts - 1, (int)((double)u * parts / (double)total));
+      while (c > 0 && cut(total, parts, c) > u) --c;
+      while (c + 1 < parts && cut(total, parts, c + 1) <= u) ++c;
+      plan.broken[blockIdx.x] = Broken{st.b, st.h, st.row0, c};
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // the rings take copies again
     __syncthreads();
   }
 }
 
-// Joins the pieces of a stream: a thread block per (stream, row), a warp has every eighth piece, a lane four channels.
+// Joins the pieces of the stream that begins in thread block blockIdx.x of pages_kernel and ends in another: a warp has a row, a lane four channels, the pieces' weights a lane
+// each, 32 pieces at a time.
 __global__ void __launch_bounds__(256)
 merge_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ Plan plan) {
   dependency_wait();
+  const Broken it = plan.broken[blockIdx.x];
+  const int c0 = blockIdx.x, c1 = it.last;
+  if (c1 <= c0) return;
   const PagedView& v = a.view;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int x = blockIdx.x, h = blockIdx.y, b = blockIdx.z;      // row of a KV head's queries, KV head, sequence
-  const int count = v.count(b);
-  if (x >= count * v.g) return;
-  const int len = v.length(b, v.add_counts ? count : 0), units = max(1, (len + kUnit - 1) / kUnit);
-  const long long total = plan.prefix[v.B];
-  const int parts = (int)plan.prefix[v.B + 1], block = x / plan.rows, row = x - block * plan.rows;
-  const long long lo = plan.prefix[b] + ((long long)h * row_blocks(count, v.g, plan.rows) + block) * (kAhead + units) + kAhead, hi = lo + units;
-  // the thread block whose range has a unit: the last one that begins at or before it (the quotient is off by one at most, in either direction)
-  auto owner = [&](long long u) {
-    int c = (int)min((long long)parts - 1, (long long)((double)u * parts / (double)total));
-    while (c > 0 && split_begin(total, parts, c) > u) --c;
-    while (c + 1 < parts && split_begin(total, parts, c + 1) <= u) ++c;
-    return c;
-  };
-  const int c0 = owner(lo), c1 = owner(hi - 1);
-  if (c0 == c1) return;                          // one thread block had it all
-  __shared__ float join[8][kD + 4];
-  float m = -1e30f, l = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int c = c0 + warp; c <= c1; c += 8) {
-    const float* from = plan.parts + ((size_t)(2 * c + (c == c0 ? 1 : 0)) * plan.rows + row) * kPartFloats;
-    const float2 o01 = *reinterpret_cast<const float2*>(from + 4 * lane), o23 = *reinterpret_cast<const float2*>(from + 4 * lane + 2);
-    const float2 ml = *reinterpret_cast<const float2*>(from + kD);
-    const float top = fmaxf(m, ml.x), f = ex2_approx(m - top), g = ex2_approx(ml.x - top);
-    m = top;
-    l = l * f + ml.y * g;
-    y[0] = y[0] * f + o01.x * g;
-    y[1] = y[1] * f + o01.y * g;
-    y[2] = y[2] * f + o23.x * g;
-    y[3] = y[3] * f + o23.y * g;
-  }
-  *reinterpret_cast<float4*>(&join[warp][4 * lane]) = make_float4(y[0], y[1], y[2], y[3]);
-  if (lane == 0) {
-    join[warp][kD] = m;
-    join[warp][kD + 1] = l;
-  }
-  __syncthreads();
-  if (warp != 0) return;
-  const int n = min(8, c1 - c0 + 1);
-  float top = -1e30f, sum = 0.f;
-  for (int i = 0; i < n; ++i) top = fmaxf(top, join[i][kD]);
-  y[0] = y[1] = y[2] = y[3] = 0.f;
-  for (int i = 0; i < n; ++i) {
-    const float f = ex2_approx(join[i][kD] - top);
-    sum = fmaf(join[i][kD + 1], f, sum);
+  int count, len;
+  v.sequence(it.b, count, len);
+  for (int row = warp; row < plan.rows; row += 8) {
+    const int x = it.row0 + row;
+    if (x >= count * v.g) return;
+    const size_t stride = (size_t)2 * plan.rows * kPartFloats;                 // from a thread block's first piece to the next one's
+    const float* from = plan.parts + (size_t)row * kPartFloats;
+    float m = -1e30f, l = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int c = c0; c <= c1; c += 32) {
+      const int n = min(32, c1 - c + 1);
+      // a thread block's second piece is the one that begins its stream
+      const float* mine = from + (c + min(lane, n - 1)) * stride + (c + min(lane, n - 1) == c0 ? stride / 2 : 0);
+      float2 ml = *reinterpret_cast<const float2*>(mine + kD);
+      if (lane >= n) ml = make_float2(-1e30f, 0.f);
+      float top = ml.x;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) y[k] = fmaf(join[i][4 * lane + k], f, y[k]);
+      for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+      top = fmaxf(top, m);
+      const float old = ex2_approx(m - top), w = ex2_approx(ml.x - top);
+      float sum = ml.y * w;
+#pragma unroll
+      for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+      m = top;
+      l = fmaf(l, old, sum);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) y[k] *= old;
+      for (int i0 = 0; i0 < n; i0 += 8) {
+        float4 o[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int k = c + min(i0 + i, n - 1);
+          o[i] = *reinterpret_cast<const float4*>(from + k * stride + (k == c0 ? stride / 2 : 0) + 4 * lane);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float f = __shfl_sync(0xffffffffu, w, i0 + i);
+          if (i0 + i < n) {
+            y[0] = fmaf(o[i].x, f, y[0]);
+            y[1] = fmaf(o[i].y, f, y[1]);
+            y[2] = fmaf(o[i].z, f, y[2]);
+            y[3] = fmaf(o[i].w, f, y[3]);
+          }
+        }
+      }
+    }
+    const int i = over_heads(plan, x), head = x - i * v.g;
+    const size_t at = (((size_t)it.b * v.Hq + it.h * v.g + head) * v.n + i) * kD + 4 * lane;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if (a.out_bf16)
+      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + at) = make_uint2(pack_bf162(y[0] * inv, y[1] * inv), pack_bf162(y[2] * inv, y[3] * inv));
+    else
+      *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at) = make_float4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
   }
-  const int i = x / v.g, head = x - i * v.g;
-  const size_t at = (((size_t)b * v.Hq + h * v.g + head) * v.n + i) * kD + 4 * lane;
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  if (a.out_bf16)
-    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + at) = make_uint2(pack_bf162(y[0] * inv, y[1] * inv), pack_bf162(y[2] * inv, y[3] * inv));
-  else
-    *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at) = make_float4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
 }
 
+constexpr int kDirectTokens = 512;               // capacity up to which a thread block has a stream to itself
 constexpr int kUnpackRows = 128;                 // query rows of a KV head above which unpacking pays
 constexpr int kMostBlocks = 148 * 4;             // thread blocks of the split kernel: sizes the workspace
 
 using Kernel = void (*)(PagedAttention, Plan);
-Kernel kernel_of(int G, int tiles) {
-  if (tiles == 1) return G == 32 ? pages_kernel<32, 1> : G == 64 ? pages_kernel<64, 1> : pages_kernel<128, 1>;
-  return G == 32 ? pages_kernel<32, 2> : G == 64 ? pages_kernel<64, 2> : pages_kernel<128, 2>;
+template <int kNT, int kW>
+Kernel kernel_for(int G) {
+  return G == 32 ? pages_kernel<32, kNT, kW> : G == 64 ? pages_kernel<64, kNT, kW> : pages_kernel<128, kNT, kW>;
 }
+// Short streams of 8 query rows: sixteen warps, a unit or two each.  (16 rows need the registers of four warps.)
+constexpr int kDirectWarps = 16;
+Kernel kernel_of(int G, int tiles, bool direct) { return tiles == 1 ? (direct ? kernel_for<1, kDirectWarps>(G) : kernel_for<1, kWarps>(G)) : kernel_for<2, kWarps>(G); }
+int warps_of(int tiles, bool direct) { return tiles == 1 && direct ? kDirectWarps : kWarps; }
 int tiles_of(int g, int n) { return g * n <= 8 ? 1 : 2; }
 size_t smem_bytes(int G, int tiles, int B, bool direct) {
-  return (size_t)kWarps * kStages * tiles * 2 * paged_tile_bytes(G) + 8 * kWarps * kStages * tiles + (direct ? 0 : 8 * (size_t)(B + 1));
+  const int warps = warps_of(tiles, direct);
+  return (size_t)warps * kStages * tiles * 2 * paged_tile_bytes(G) + 8 * warps * kStages * tiles + (direct || B <= 32 ? 0 : 8 * (size_t)(B + 1));
 }
 
 }  // namespace
@@ -689,14 +742,16 @@ static bool unpacks(int g, int n, long long capacity) { return (long long)g * n 
 
 size_t paged_workspace_bytes(int Hkv, int g, int batch, int n, long long capacity) {
   if (unpacks(g, n, capacity)) return paged_chunk_workspace_bytes(Hkv, batch, capacity);
-  return ((size_t)2 * kMostBlocks * 8 * tiles_of(g, n) * kPartFloats * 4 + 8 * (size_t)(batch + 2) + 15) / 16 * 16;
+  return (size_t)2 * kMostBlocks * 8 * tiles_of(g, n) * kPartFloats * 4 + kMostBlocks * sizeof(Broken);
 }
 
 cudaError_t paged_attention_setup() {
   for (int G = 32; G <= 128; G *= 2)
-    for (int tiles = 1; tiles <= 2; ++tiles) {
-      const cudaError_t e = cudaFuncSetAttribute(kernel_of(G, tiles), cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                 (int)smem_bytes(G, tiles, MIXKVQ_PAGED_MAX_BATCH, false));
+    for (int k = 0; k < 3; ++k) {
+      const int tiles = k == 2 ? 2 : 1;
+      const bool direct = k == 1;
+      const cudaError_t e = cudaFuncSetAttribute(kernel_of(G, tiles, direct), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                 (int)smem_bytes(G, tiles, MIXKVQ_PAGED_MAX_BATCH, direct));
       if (e != cudaSuccess) return e;
     }
   return paged_chunk_setup();
@@ -711,16 +766,18 @@ cudaError_t launch_paged_attention(const PagedAttention& a, int n_sms, cudaStrea
   plan.rows = 8 * tiles;
   plan.parts = a.parts;
   const int most = std::min(kMostBlocks, n_sms * (tiles == 1 ? 3 : 2));
-  plan.prefix = reinterpret_cast<long long*>(a.parts + (size_t)2 * kMostBlocks * plan.rows * kPartFloats);
+  plan.broken = reinterpret_cast<Broken*>(a.parts + (size_t)2 * kMostBlocks * plan.rows * kPartFloats);
+  plan.g_inv = v.g == 1 ? 0u : (uint32_t)(((1ull << 32) + v.g - 1) / v.g);
   // Sequences whose pages hold few tokens at most: a thread block each, no merge.
   const long long streams = (long long)v.B * v.Hkv * ((v.n * (long long)v.g + plan.rows - 1) / plan.rows);
-  plan.direct = ((long long)v.max_pages << v.lg_page) <= 4 * kWarps * kUnit;
-  cudaError_t e = launch_dependent(kernel_of(v.G, tiles), dim3((unsigned)(plan.direct ? streams : most)), kWarps * 32, smem_bytes(v.G, tiles, v.B, plan.direct), stream, a,
-                                   plan);
+  plan.direct = ((long long)v.max_pages << v.lg_page) <= kDirectTokens;
+  const int warps = warps_of(tiles, plan.direct);
+  cudaError_t e = launch_dependent(kernel_of(v.G, tiles, plan.direct), dim3((unsigned)(plan.direct ? streams : most)), warps * 32, smem_bytes(v.G, tiles, v.B, plan.direct), stream,
+                                   a, plan);
   *launches = 1;
   if (e != cudaSuccess || plan.direct) return e;
   *launches = 2;
-  return launch_dependent(merge_kernel, dim3((unsigned)(v.n * v.g), (unsigned)v.Hkv, (unsigned)v.B), 256, 0, stream, a, plan);
+  return launch_dependent(merge_kernel, dim3((unsigned)most), 256, 0, stream, a, plan);
 }
 
 }  // namespace mixkvq
