@@ -31,7 +31,9 @@ constexpr int kScaleTo = 5 + kBelow;             // the largest value scale of a
 constexpr int kAhead = 12;                       // units that the beginning of a piece counts as
 
 struct __align__(16) Broken {                    // a stream that begins in a thread block's range and ends in another's
-  int b, h, row0, last;                          // last: the thread block that has its end, -1: none
+  int last, row0, rows, pad;                     // last: the thread block that has its end, -1: none; its query rows
+  long long out;                                 // where its KV head's first query row is in the output: (sequence * query heads + head) * n
+  long long pad2;
 };
 struct Plan {
   int rows;                                      // of a block of query rows
@@ -147,9 +149,9 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
       __syncthreads();
       total = prefix[v.B];
     }
-    // at least the beginning of a piece and a unit for every warp
-    parts = (int)min((long long)gridDim.x, max(1ll, (total + kAhead + kW - 1) / (kAhead + kW)));
-    if (tid == 0) plan.broken[blockIdx.x] = Broken{0, 0, 0, -1};
+    // at least a unit for every warp
+    parts = (int)min((long long)gridDim.x, (total + kW - 1) / kW);
+    if (tid == 0) plan.broken[blockIdx.x].last = -1;
     if ((int)blockIdx.x >= parts) return;
     pos = cut(total, parts, blockIdx.x);
     end = cut(total, parts, blockIdx.x + 1);
@@ -644,15 +646,15 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
       int c = min(parts - 1, (int)((double)u * parts / (double)total));
       while (c > 0 && cut(total, parts, c) > u) --c;
       while (c + 1 < parts && cut(total, parts, c + 1) <= u) ++c;
-      plan.broken[blockIdx.x] = Broken{st.b, st.h, st.row0, c};
+      plan.broken[blockIdx.x] = Broken{c, st.row0, min(kRows, st.count * v.g - st.row0), 0, ((long long)st.b * v.Hq + st.h * v.g) * v.n, 0};
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // the rings take copies again
     __syncthreads();
   }
 }
 
-// Joins the pieces of the stream that begins in thread block blockIdx.x of pages_kernel and ends in another: a warp has a row, a lane four channels, the pieces' weights a lane
-// each, 32 pieces at a time.
+// Joins the pieces of the stream that begins in thread block blockIdx.x of pages_kernel and ends in another.  Eight warps share the rows, or where there are few the rows and
+// their pieces; a lane has four channels, and the weight of one of 32 pieces at a time.
 __global__ void __launch_bounds__(256)
 merge_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ Plan plan) {
   dependency_wait();
@@ -661,19 +663,21 @@ merge_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
   if (c1 <= c0) return;
   const PagedView& v = a.view;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  int count, len;
-  v.sequence(it.b, count, len);
-  for (int row = warp; row < plan.rows; row += 8) {
-    const int x = it.row0 + row;
-    if (x >= count * v.g) return;
-    const size_t stride = (size_t)2 * plan.rows * kPartFloats;                 // from a thread block's first piece to the next one's
+  const int share = it.rows <= 1 ? 8 : it.rows <= 2 ? 4 : it.rows <= 4 ? 2 : 1;          // warps of a row
+  const int mine = warp % share;
+  const size_t stride = (size_t)2 * plan.rows * kPartFloats;                 // from a thread block's first piece to the next one's
+  __shared__ float join[8][kD + 4];
+  for (int row = warp / share; row < it.rows; row += 8 / share) {            // (one round where a row has several warps)
     const float* from = plan.parts + (size_t)row * kPartFloats;
     float m = -1e30f, l = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int c = c0; c <= c1; c += 32) {
+    for (int c = c0 + 32 * mine; c <= c1; c += 32 * share) {
       const int n = min(32, c1 - c + 1);
       // a thread block's second piece is the one that begins its stream
-      const float* mine = from + (c + min(lane, n - 1)) * stride + (c + min(lane, n - 1) == c0 ? stride / 2 : 0);
-      float2 ml = *reinterpret_cast<const float2*>(mine + kD);
+      auto piece = [&](int k) { return from + (c + k) * stride + (c + k == c0 ? stride / 2 : 0); };
+      float4 o[12];
+#pragma unroll
+      for (int i = 0; i < 12; ++i) o[i] = *reinterpret_cast<const float4*>(piece(min(i, n - 1)) + 4 * lane);
+      float2 ml = *reinterpret_cast<const float2*>(piece(min(lane, n - 1)) + kD);
       if (lane >= n) ml = make_float2(-1e30f, 0.f);
       float top = ml.x;
 #pragma unroll
@@ -687,15 +691,9 @@ merge_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
       l = fmaf(l, old, sum);
 #pragma unroll
       for (int k = 0; k < 4; ++k) y[k] *= old;
-      for (int i0 = 0; i0 < n; i0 += 8) {
-        float4 o[8];
+      for (int i0 = 0; i0 < n; i0 += 12) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int k = c + min(i0 + i, n - 1);
-          o[i] = *reinterpret_cast<const float4*>(from + k * stride + (k == c0 ? stride / 2 : 0) + 4 * lane);
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 12; ++i) {
           const float f = __shfl_sync(0xffffffffu, w, i0 + i);
           if (i0 + i < n) {
             y[0] = fmaf(o[i].x, f, y[0]);
@@ -704,10 +702,27 @@ merge_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
             y[3] = fmaf(o[i].w, f, y[3]);
           }
         }
+        if (i0 + 12 < n) {
+#pragma unroll
+          for (int i = 0; i < 12; ++i) o[i] = *reinterpret_cast<const float4*>(piece(min(i0 + 12 + i, n - 1)) + 4 * lane);
+        }
       }
     }
-    const int i = over_heads(plan, x), head = x - i * v.g;
-    const size_t at = (((size_t)it.b * v.Hq + it.h * v.g + head) * v.n + i) * kD + 4 * lane;
+    if (share > 1) {
+      *reinterpret_cast<float4*>(&join[warp][4 * lane]) = make_float4(y[0], y[1], y[2], y[3]);
+      if (lane == 0) *reinterpret_cast<float2*>(&join[warp][kD]) = make_float2(m, l);
+      asm volatile("bar.sync %0, %1;" ::"r"(1 + warp / share), "r"(32 * share) : "memory");      // the row's warps
+      if (mine != 0) return;
+      for (int i = 1; i < share; ++i) {
+        const float m1 = join[warp + i][kD], l1 = join[warp + i][kD + 1], top = fmaxf(m, m1), f0 = ex2_approx(m - top), f1 = ex2_approx(m1 - top);
+        m = top;
+        l = l * f0 + l1 * f1;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) y[k] = y[k] * f0 + join[warp + i][4 * lane + k] * f1;
+      }
+    }
+    const int x = it.row0 + row, i = over_heads(plan, x), head = x - i * v.g;
+    const size_t at = ((size_t)it.out + (size_t)head * v.n + i) * kD + 4 * lane;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     if (a.out_bf16)
       *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + at) = make_uint2(pack_bf162(y[0] * inv, y[1] * inv), pack_bf162(y[2] * inv, y[3] * inv));
