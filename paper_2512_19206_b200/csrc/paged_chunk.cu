@@ -9,9 +9,11 @@
 //   warps 0-3, 4-7   two softmax groups of 128 query rows (thread = row = lane of tensor memory); a row is head x % g of token x / g;
 //   warp 8           one thread issues every tcgen05.mma;
 //   warp 9           one thread issues the bulk copies of the key and value tiles into two-stage rings.
-// Per key tile and group: S = Q K^T, the thread reads its row of S, writes its row of P = 2^(S - max + 14) as fp16 over S (2^14 at most, so that weights down to 2^-28 of the
-// largest keep 11 bits), O = P V, which the thread adds to an fp32 sum in registers at the start of the next tile.  While one group is in its softmax the
-// tensor core has the other one's products.
+// Per key tile and group: S = Q K^T; the thread takes its row of S into registers, writes its row of P = 2^(S - reference + 4) as fp16 over S; O += P V in tensor memory.
+// A reference is raised, and the row of O rescaled, only when a logit comes 2^8 above it, so that almost no tile touches O outside the tensor core.  The scale of a value tile goes into
+// the exponents of P as its ratio to the scale that O has.  (In the first form every tile's product was added to a sum in registers, which left none for the row of S: it was read twice,
+// and a softmax took 717 instructions a tile instead of the present ones: 2048 tokens over 32768, 7b shape, 1031 us.)  The tensor core truncates its sums, about 3.5e-7 of O per tile
+// in one direction: after 512 tiles O is added to a sum in memory and begins again.
 //
 // Split: a row tile of 256 rows of a KV head is an item with as many positions as its last row sees key tiles; all items' positions in one line are cut evenly over the
 // thread blocks, on the device.  A thread block that has a part of an item leaves sums, which join_kernel puts together.
@@ -32,7 +34,10 @@ constexpr int kPartFloats = kD + 4;              // sums of a row: o[128], refer
 constexpr int kAhead = 2;                        // positions that the beginning of an item counts as
 constexpr uint32_t kPolls = 1u << 21;
 constexpr size_t kImageBytes = (size_t)512 << 20;      // of images at a time: sequences (or heads) beyond are a pass of their own
-constexpr int kShift = 14;                       // weights are 2^kShift at most
+constexpr int kShift = 4;                        // the weight of a logit equal to the reference is 2^kShift
+constexpr float kRise = 8.f;                     // a logit this much above the reference raises it: weights are 2^12 at most
+constexpr int kSlack = 3;                        // powers of two that a value tile's scale may be above that of O: 2^15 at most
+constexpr int kFlush = 512;                      // tiles summed up in tensor memory
 constexpr int kDown = 30;                        // and sums of values 2^-kDown as large: they keep off fp32's end
 
 struct __align__(16) TileHead {
@@ -217,69 +222,144 @@ __device__ __forceinline__ int owner_of(long long u, long long total, int parts)
   return c;
 }
 
-// Adds the row's product in tensor memory, times the value tile's scale, to the sum kept in registers.
-__device__ __forceinline__ void add_output(uint32_t o_addr, float scale, float (&sum_o)[128]) {
-  const uint64_t s2 = pack2(scale, scale);
-  for_pieces<true>(o_addr, 8, [&](int h, const uint32_t (&x)[16]) {
+// 32 columns of the thread's tensor-memory row; valid after the wait, which names them.
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* u) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]),
+        "=r"(u[13]), "=r"(u[14]), "=r"(u[15]), "=r"(u[16]), "=r"(u[17]), "=r"(u[18]), "=r"(u[19]), "=r"(u[20]), "=r"(u[21]), "=r"(u[22]), "=r"(u[23]), "=r"(u[24]), "=r"(u[25]),
+        "=r"(u[26]), "=r"(u[27]), "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait32(uint32_t* u) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(u[0]), "+r"(u[1]), "+r"(u[2]), "+r"(u[3]), "+r"(u[4]), "+r"(u[5]), "+r"(u[6]), "+r"(u[7]), "+r"(u[8]), "+r"(u[9]), "+r"(u[10]), "+r"(u[11]), "+r"(u[12]),
+                 "+r"(u[13]), "+r"(u[14]), "+r"(u[15]), "+r"(u[16]), "+r"(u[17]), "+r"(u[18]), "+r"(u[19]), "+r"(u[20]), "+r"(u[21]), "+r"(u[22]), "+r"(u[23]), "+r"(u[24]), "+r"(u[25]),
+                 "+r"(u[26]), "+r"(u[27]), "+r"(u[28]), "+r"(u[29]), "+r"(u[30]), "+r"(u[31])
+               :
+               : "memory");
+}
+__device__ __forceinline__ float fmax_of(const uint32_t* u, float m) {      // of 32 values and m, four chains
+  float a[4] = {m, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-    for (int k = 0; k < 16; k += 2)
-      unpack2(fma2(pack2u(x[k], x[k + 1]), s2, pack2(sum_o[16 * h + k], sum_o[16 * h + k + 1])), sum_o[16 * h + k], sum_o[16 * h + k + 1]);
-  });
+  for (int i = 0; i < 32; i += 2) a[i >> 1 & 3] = fmaxf(fmaxf(a[i >> 1 & 3], __uint_as_float(u[i])), __uint_as_float(u[i + 1]));
+  return fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3]));
 }
 
-// One key tile of a row's softmax; the row of S is at s_addr, the product of the tile before at o_addr.  kMask: the row sees the columns <= last of those 16
-// that `there` has; what it does not see gets the weight 0.
-template <bool kMask>
-__device__ __forceinline__ void softmax_tile(uint32_t s_addr, uint32_t o_addr, int last, uint32_t there, bool first, float factor, float v_scale, float& ref, float& denom,
-                                             uint32_t half_bar, float (&sum_o)[128]) {
-  if (!first) add_output(o_addr, v_scale, sum_o);
-  float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-  for_pieces<true>(s_addr, 8, [&](int h, const uint32_t (&u)[16]) {
-    const int lim = kMask ? (there >> h & 1u ? last - 16 * h : -1) : 0;
+// What a thread keeps of its row over the tiles of a segment.
+struct Row {
+  float ref, denom;                        // in powers of two; sum of the weights
+  float v_scale;                           // what O is to be multiplied with
+  bool flushed;                            // the row of `parts` has the sums of earlier tiles, at the reference that it says
+};
+
+// Adds the row of O to its sums in memory (kPartFloats floats at `to`), relative to the present reference, which is left there.
+__device__ __forceinline__ void flush_row(uint32_t o_addr, float* to, Row& row) {
+  const float old = row.flushed ? ex2(to[kD] - row.ref) : 0.f;
+#pragma unroll 1
+  for (int h = 0; h < 8; ++h) {
+    uint32_t x[16];
+    tmem_ld16_issue(o_addr + 16 * h, x);
+    tmem_wait_ld16(x);
 #pragma unroll
-    for (int i = 0; i < 16; i += 2) {
-      const float x0 = kMask && i > lim ? -INFINITY : __uint_as_float(u[i]), x1 = kMask && i + 1 > lim ? -INFINITY : __uint_as_float(u[i + 1]);
-      mx4[(i >> 1) & 3] = fmaxf(fmaxf(mx4[(i >> 1) & 3], x0), x1);
+    for (int k = 0; k < 16; k += 4) {
+      float4 y = row.flushed ? *reinterpret_cast<const float4*>(to + 16 * h + k) : make_float4(0.f, 0.f, 0.f, 0.f);
+      y.x = fmaf(__uint_as_float(x[k]), row.v_scale, row.flushed ? y.x * old : 0.f);
+      y.y = fmaf(__uint_as_float(x[k + 1]), row.v_scale, row.flushed ? y.y * old : 0.f);
+      y.z = fmaf(__uint_as_float(x[k + 2]), row.v_scale, row.flushed ? y.z * old : 0.f);
+      y.w = fmaf(__uint_as_float(x[k + 3]), row.v_scale, row.flushed ? y.w * old : 0.f);
+      *reinterpret_cast<float4*>(to + 16 * h + k) = y;
     }
-  });
-  const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * factor;
-  if (__any_sync(0xffffffffu, mx > ref)) {
-    const float up = fmaxf(ref, mx), alpha = ex2(ref - up);
-    const uint64_t alpha2 = pack2(alpha, alpha);
-#pragma unroll
-    for (int d = 0; d < 128; d += 2) unpack2(mul2(pack2(sum_o[d], sum_o[d + 1]), alpha2), sum_o[d], sum_o[d + 1]);
-    denom *= alpha;
-    ref = up;
   }
-  auto half_ready = [&]() {
-    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-    tc_fence_before();
-    mbar_arrive(half_bar);
-  };
-  const uint64_t factor2 = pack2(factor, factor), ref2 = pack2(kShift - ref, kShift - ref);
+  to[kD] = row.ref;
+  row.flushed = true;
+}
+
+// One key tile of a row's softmax; S is at s_addr, O at o_addr.  masked: the row sees the columns <= last of those 16 that `there` has.  fresh: O has nothing yet.
+__device__ __forceinline__ void softmax_tile(uint32_t s_addr, uint32_t o_addr, bool masked, int last, uint32_t there, bool fresh, float factor, float v_scale, Row& row,
+                                             uint32_t half_bar) {
+  uint32_t u[128];
+  float mx = -INFINITY;
+  tmem_ld32(s_addr, u);
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    tmem_wait32(u + 32 * q);
+    if (q < 3) tmem_ld32(s_addr + 32 * (q + 1), u + 32 * (q + 1));
+    if (masked) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int lim = there >> (2 * q + h) & 1u ? last - 32 * q - 16 * h : -1;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (i > lim) u[32 * q + 16 * h + i] = 0xFF800000u;      // weight 0
+      }
+    }
+    mx = fmax_of(u + 32 * q, mx);
+  }
+  mx *= factor;
+  // ---- the reference of the row and the scale of O
+  if (fresh) {
+    if (mx > row.ref + kRise || row.ref == -1e30f) {               // (what memory has of the row is brought to the new reference when it is added to)
+      const float up = mx > -INFINITY ? mx : row.ref;
+      row.denom *= ex2(row.ref - up);
+      row.ref = up;
+    }
+    row.v_scale = v_scale;
+  }
+  const bool rises = !fresh && mx > row.ref + kRise;
+  int v_shift = (int)(__float_as_uint(v_scale) >> 23) - (int)(__float_as_uint(row.v_scale) >> 23);      // (powers of two)
+  const bool outgrown = v_shift > kSlack;
+  if (__any_sync(0xffffffffu, rises || outgrown)) {
+    float f = 1.f;
+    if (rises) {
+      f = ex2(row.ref - mx);
+      row.denom *= f;
+      row.ref = mx;
+    }
+    if (outgrown) {
+      f *= pow2i(max(-v_shift, -126));
+      row.v_scale = v_scale;
+      v_shift = 0;
+    }
+#pragma unroll 1
+    for (int h = 0; h < 8; ++h) {
+      uint32_t x[16];
+      tmem_ld16_issue(o_addr + 16 * h, x);
+      tmem_wait_ld16(x);
+#pragma unroll
+      for (int k = 0; k < 16; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * f);
+      tmem_st8(o_addr + 16 * h, reinterpret_cast<uint32_t(&)[8]>(x[0]));
+      tmem_st8(o_addr + 16 * h + 8, reinterpret_cast<uint32_t(&)[8]>(x[8]));
+    }
+  }
+  // ---- weights
+  v_shift = max(v_shift, -100);
+  const float offset = (float)(kShift + v_shift) - row.ref;
+  const uint64_t factor2 = pack2(factor, factor), offset2 = pack2(offset, offset);
   uint64_t sum[2] = {0ull, 0ull};
-  for_pieces<true>(s_addr, 8, [&](int h, const uint32_t (&u)[16]) {
+#pragma unroll
+  for (int h = 0; h < 8; ++h) {
     uint32_t wd[8];
-    const int lim = kMask ? (there >> h & 1u ? last - 16 * h : -1) : 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       float x0, x1;
-      unpack2(fma2(pack2u(u[2 * i], u[2 * i + 1]), factor2, ref2), x0, x1);
-      float p0 = ex2(x0), p1 = ex2(x1);
-      if constexpr (kMask) {
-        p0 = 2 * i <= lim ? p0 : 0.f;
-        p1 = 2 * i + 1 <= lim ? p1 : 0.f;
-      }
+      unpack2(fma2(pack2u(u[16 * h + 2 * i], u[16 * h + 2 * i + 1]), factor2, offset2), x0, x1);
+      const float p0 = ex2(x0), p1 = ex2(x1);
       sum[i & 1] = add2(sum[i & 1], pack2(p0, p1));
       wd[i] = pack_half2(p0, p1);
     }
     tmem_st8(s_addr + 8 * h, wd);
-    if (h == 3) half_ready();
-  });
+    if (h == 3) {
+      asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+      tc_fence_before();
+      mbar_arrive(half_bar);
+    }
+  }
   asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
   float s0, s1;
   unpack2(add2(sum[0], sum[1]), s0, s1);
-  denom += s0 + s1;
+  row.denom = fmaf(s0 + s1, pow2i(-v_shift), row.denom);
 }
 
 // A row of results; lost: quarters (bits 0 .. 3) that are not finite, bit 4: all of them.
@@ -422,13 +502,13 @@ attend_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ 
         for (int ks = 0; ks < 8; ++ks) tc_mma_ss(tbase + 128 * g, qd + (uint64_t)(ks * 16), kd + (uint64_t)(ks * 16), idesc_qk, ks > 0);
         tc_commit(bar(kSFull + g));
       };
-      auto issue_o = [&](int g, uint32_t tile, uint32_t parity) {
+      auto issue_o = [&](int g, uint32_t tile, uint32_t parity, bool more) {
         const uint64_t vd = make_desc(smem_u32(Vs + (tile & 1) * kTileBytes), 128, 2048);
         const uint32_t o = tbase + 256 + 128 * g, p = tbase + 128 * g;
         if (!wait(kPHalf + g, parity)) return false;
         tc_fence_after();
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) tc_mma_ts(o, p + 8 * ks, vd + (uint64_t)(ks * 16), idesc_pv, ks > 0);
+        for (int ks = 0; ks < 4; ++ks) tc_mma_ts(o, p + 8 * ks, vd + (uint64_t)(ks * 16), idesc_pv, ks > 0 || more);
         if (!wait(kPReady + g, parity)) return false;
         tc_fence_after();
 #pragma unroll
@@ -452,7 +532,7 @@ attend_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ 
             const bool more = j + 1 < s.j1;
             if (!(ok = wait(kVFull + (t & 1), t >> 1 & 1))) break;
             tc_fence_after();
-            if (!(ok = issue_o(0, t, t & 1))) break;
+            if (!(ok = issue_o(0, t, t & 1, (j - s.j0) % kFlush != 0))) break;
             if (!both) tc_commit(bar(kVEmpty + (t & 1)));
             if (!more) tc_commit(bar(kDone));
             if (more) {
@@ -462,7 +542,7 @@ attend_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ 
               if (!both) tc_commit(bar(kKEmpty + ((t + 1) & 1)));
             }
             if (both) {
-              if (!(ok = issue_o(1, t, tiles_b & 1))) break;
+              if (!(ok = issue_o(1, t, tiles_b & 1, (j - s.j0) % kFlush != 0))) break;
               ++tiles_b;
               tc_commit(bar(kVEmpty + (t & 1)));
               if (!more) tc_commit(bar(kDone + 1));
@@ -555,65 +635,68 @@ attend_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ 
         }
         const int warp_sees = __reduce_min_sync(0xffffffffu, sees);
         const TileHead* heads = plan.heads + (size_t)(walk.i * plan.nh + walk.h) * plan.max_tiles;
-        float ref = -1e30f, denom = 0.f, v_scale = 0.f;
+        Row sums{-1e30f, 0.f, 0.f, false};
         uint32_t lost = 0;
-        float sum_o[128];
-#pragma unroll
-        for (int d = 0; d < 128; ++d) sum_o[d] = 0.f;
+        const bool whole = s.j0 == 0 && s.j1 == s.tiles;
+        // the thread block's first part of an item and its last have a place each; a whole item's sums in between take the second one
+        float* to = plan.parts + ((size_t)(2 * blockIdx.x + (s.j0 == 0 ? 1 : 0)) * kRows + g * kTile + (tid & 127)) * kPartFloats;
 #pragma unroll 1
         for (int j = s.j0; j < s.j1; ++j) {
           const float4 head_of = *reinterpret_cast<const float4*>(heads + j);       // (under way while the thread waits)
           const uint32_t flags = __float_as_uint(head_of.z);
+          const bool masked = (j + 1) * kTile > warp_sees || flags != 0xFFu, fresh = (j - s.j0) % kFlush == 0;
           if (!wait(kSFull + g, t & 1)) break;
           tc_fence_after();
-          if ((j + 1) * kTile <= warp_sees && flags == 0xFFu) {
-            softmax_tile<false>(s_addr, o_addr, 0, 0u, j == s.j0, factor * head_of.x, v_scale, ref, denom, bar(kPHalf + g), sum_o);
-          } else {
-            softmax_tile<true>(s_addr, o_addr, sees - 1 - j * kTile, flags, j == s.j0, factor * head_of.x, v_scale, ref, denom, bar(kPHalf + g), sum_o);
-            if (flags >> 8 & 1u)
-              for (int k = 0; k < kTile && j * kTile + k < sees; ++k) lost |= heads[j].lost[k];
-          }
-          v_scale = head_of.y;
+          if (fresh && j > s.j0) flush_row(o_addr, to, sums);
+          softmax_tile(s_addr, o_addr, masked, sees - 1 - j * kTile, flags, fresh, factor * head_of.x, head_of.y, sums, bar(kPHalf + g));
+          if (flags >> 8 & 1u)
+            for (int k = 0; k < kTile && j * kTile + k < sees; ++k) lost |= heads[j].lost[k];
           tc_fence_before();
           mbar_arrive(bar(kPReady + g));
           ++t;
         }
         if (!dead && wait(kDone + g, segs & 1)) {
           tc_fence_after();
-          add_output(o_addr, v_scale, sum_o);
-          const bool whole = s.j0 == 0 && s.j1 == s.tiles;
-          if (whole) {
-            const float inv = denom == 0.f ? 0.f : pow2i(kDown) / denom;
-            if (mine) {
+          if (sums.flushed) flush_row(o_addr, to, sums);
+          const float inv = whole ? (sums.denom == 0.f ? 0.f : pow2i(kDown) / sums.denom) : 1.f;
+#pragma unroll 1
+          for (int q = 0; q < 4; ++q) {                  // 32 channels
+            float y[32];
+            {
+              uint32_t x[32];
+              tmem_ld32(o_addr + 32 * q, x);
+              tmem_wait32(x);
+              const float f = lost >> q & 1u || lost & 16u ? NAN : inv;
 #pragma unroll
-              for (int q = 0; q < 4; ++q) {
-                const float f = lost >> q & 1u || lost & 16u ? NAN : inv;
-                if (a.out_bf16) {
-                  char* to = static_cast<char*>(a.out) + row * (2 * kD) + 64 * q;
+              for (int d = 0; d < 32; ++d) y[d] = (sums.flushed ? to[32 * q + d] : __uint_as_float(x[d]) * sums.v_scale) * (whole ? f : 1.f);
+            }
+            if (!whole) {
+              if (!sums.flushed) {
 #pragma unroll
-                  for (int k = 0; k < 2; ++k) {
-                    uint32_t y[8];
+                for (int d = 0; d < 32; d += 4) *reinterpret_cast<float4*>(to + 32 * q + d) = make_float4(y[d], y[d + 1], y[d + 2], y[d + 3]);
+              }
+            } else if (mine && a.out_bf16) {
+              char* out = static_cast<char*>(a.out) + row * (2 * kD) + 64 * q;
 #pragma unroll
-                    for (int d = 0; d < 8; ++d) y[d] = bf16_pair(sum_o[32 * q + 16 * k + 2 * d] * f, sum_o[32 * q + 16 * k + 2 * d + 1] * f);
-                    store32(to + 32 * k, y, wide);
-                  }
-                } else {
-                  char* to = static_cast<char*>(a.out) + row * (4 * kD) + 128 * q;
+              for (int k = 0; k < 2; ++k) {
+                uint32_t z[8];
 #pragma unroll
-                  for (int k = 0; k < 4; ++k) {
-                    uint32_t y[8];
+                for (int d = 0; d < 8; ++d) z[d] = bf16_pair(y[16 * k + 2 * d], y[16 * k + 2 * d + 1]);
+                store32(out + 32 * k, z, wide);
+              }
+            } else if (mine) {
+              char* out = static_cast<char*>(a.out) + row * (4 * kD) + 128 * q;
 #pragma unroll
-                    for (int d = 0; d < 8; ++d) y[d] = __float_as_uint(sum_o[32 * q + 8 * k + d] * f);
-                    store32(to + 32 * k, y, wide);
-                  }
-                }
+              for (int k = 0; k < 4; ++k) {
+                uint32_t z[8];
+#pragma unroll
+                for (int d = 0; d < 8; ++d) z[d] = __float_as_uint(y[8 * k + d]);
+                store32(out + 32 * k, z, wide);
               }
             }
-          } else {
-            float* to = plan.parts + ((size_t)(2 * blockIdx.x + (s.j0 == 0 ? 1 : 0)) * kRows + g * kTile + (tid & 127)) * kPartFloats;
-#pragma unroll
-            for (int d = 0; d < kD; d += 4) *reinterpret_cast<float4*>(to + d) = make_float4(sum_o[d], sum_o[d + 1], sum_o[d + 2], sum_o[d + 3]);
-            *reinterpret_cast<float4*>(to + kD) = make_float4(ref, denom, __uint_as_float(lost), 0.f);
+          }
+          if (!whole) {
+            *reinterpret_cast<float4*>(to + kD) = make_float4(sums.ref, sums.denom, __uint_as_float(lost), 0.f);
             if (tid == 0 && s.j0 == 0)
               plan.broken[blockIdx.x] = Broken{walk.i, walk.h, walk.r, owner_of(split_begin(total, parts, blockIdx.x + 1) + (s.tiles - s.j1) - 1, total, parts)};
           }
