@@ -66,47 +66,68 @@ __device__ __forceinline__ uint4 turn_chunk(uint4 own, const ChunkLane& l, F2 mz
   return make_uint4(y[0], y[1], y[2], y[3]);
 }
 
-// Scale, zero-point and codes of a row's groups.  Every lane of the warp calls this; group_lanes = G / 8 neighbouring lanes share a group.
+// Scale, zero-point and codes of a row's groups.  Every lane of the warp calls this; kLanes = G / 8 neighbouring lanes share a group.
 //
-// The code of an element is the rounded single-precision quotient (x - z) / s.  With r = 1 / s rounded, (x - z) r is off that quotient's exact value by 2^-23 of itself at
-// most and the quotient by 2^-24: 2.7e-6 together, as no quotient is above 15.  So unless the product lies within 4e-6 of a half-integer both round to the same whole number;
-// the few that do (exact ties of bf16 numbers among them) are divided, and so is what has no product: NaN, infinities, groups without a scale.
+// The code of an element is the rounded single-precision quotient (x - z) / s.  With r = 1 / s within 2^-23 of itself (the approximation's bound), (x - z) r is off that
+// quotient's exact value by 2^-23 + 2^-24 of itself at most and the quotient by 2^-24: 3.6e-6 together, as no quotient is above 15.  So unless the product lies within 5e-6 of a
+// half-integer both round to the same whole number; the few that do (exact ties of bf16 numbers among them) are divided, and so is what has no product: NaN, infinities,
+// groups without a scale.  The product and its rounding may be contracted: that moves the result by less than the rest of the margin.
+// The scale likewise: range times 1 / 15 is within two units of the last place of the quotient, whose low 16 bits are then rounded up; where they are that near to nothing the
+// range is divided.
 struct Quantized {
   uint32_t codes;                          // channel i at bits 4 i
   uint32_t meta;                           // z | s << 16, bf16 bits
 };
-__device__ __forceinline__ Quantized quantize_chunk(uint4 w, int group_lanes) {
-  const uint32_t a[4] = {w.x, w.y, w.z, w.w};
-  float x[8];
+__device__ __forceinline__ uint32_t bf16_min2(uint32_t a, uint32_t b) {      // (passes over NaNs)
+  uint32_t y;
+  asm("min.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(a), "r"(b));
+  return y;
+}
+__device__ __forceinline__ float scale_of(float hi, float lo) {
+  const float range = __fsub_rn(hi, lo), near = __fmul_rn(range, 0.06666667f);
+  const uint32_t u = __float_as_uint(near);
+  // (u + 2) mod 2^16 below 5: the quotient may be a bf16 number, or the product on the other side of one; tiny and infinite ranges have no such product
+  if (((u + 2u) & 0xFFFFu) < 5u || !(near > 1e-37f && near < 3e38f)) return stored_scale(hi, lo, 15.f);
+  return __uint_as_float((u + 0x10000u) & 0xFFFF0000u);
+}
+template <int kLanes>
+__device__ __forceinline__ Quantized quantize_chunk(uint4 w) {
+  // the least of the values and of their negatives, two at a time
+  uint32_t lo2 = bf16_min2(bf16_min2(w.x, w.y), bf16_min2(w.z, w.w));
+  uint32_t hi2 = bf16_min2(bf16_min2(w.x ^ 0x80008000u, w.y ^ 0x80008000u), bf16_min2(w.z ^ 0x80008000u, w.w ^ 0x80008000u));
+  uint32_t both = bf16_min2(__byte_perm(lo2, hi2, 0x5410), __byte_perm(lo2, hi2, 0x7632));      // least value | least negative << 16
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = bf16_half(a[i >> 1], i & 1);
-  float lo = fminf(fminf(fminf(x[0], x[1]), fminf(x[2], x[3])), fminf(fminf(x[4], x[5]), fminf(x[6], x[7])));
-  float hi = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-  for (int d = 1; d < group_lanes; d <<= 1) {
-    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
-    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, d));
-  }
-  const float s = stored_scale(hi, lo, 15.f), inv = __frcp_rn(s);
-  constexpr float kMagic = 12582912.f;     // 1.5 2^23: adding it rounds to a whole number, the low bits of the sum
+  for (int d = 1; d < kLanes; d <<= 1) both = bf16_min2(both, __shfl_xor_sync(0xffffffffu, both, d));
+  const float lo = bf16_half(both, 0), s = scale_of(-bf16_half(both, 1), lo);
+  float inv;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+  constexpr float kMagic = 12582912.f, kMargin = 0.5f - 5e-6f;      // 1.5 2^23: adding it rounds to a whole number, the low bits of the sum
+  const F2 lo_2 = f2(lo, lo), inv_2 = f2(inv, inv), magic_2 = f2(kMagic, kMagic), zero_2 = f2(0.f, 0.f);
+  const uint32_t a[4] = {w.x, w.y, w.z, w.w};
   uint32_t codes = 0;
   bool near = false;
 #pragma unroll
-  for (int i = 7; i >= 0; --i) {
-    const float y = __fmul_rn(__fsub_rn(x[i], lo), inv), f = __fadd_rn(y, kMagic), d = __fsub_rn(y, __fsub_rn(f, kMagic));
-    near = near || !(fabsf(d) <= 0.5f - 4e-6f);
-    codes = codes * 16u + (__float_as_uint(f) & 15u);
+  for (int i = 3; i >= 0; --i) {
+    const F2 y = f2_mul(f2_sub(f2(bf16_half(a[i], 0), bf16_half(a[i], 1)), lo_2), inv_2, zero_2), f = f2_add(y, magic_2), d = f2_sub(y, f2_sub(f, magic_2));
+    float f0, f1, d0, d1;
+    f2_get(f, f0, f1);
+    f2_get(d, d0, d1);
+    near = near || !(fabsf(d0) <= kMargin) || !(fabsf(d1) <= kMargin);
+    codes = codes * 256u + (__float_as_uint(f1) * 16u + __float_as_uint(f0));      // (what is above the codes is taken off at the end)
   }
+  codes -= (uint32_t)(0x4B400000ull * 0x11111111ull);
   if (near) {                              // (one element as a rule)
+    codes = 0;
 #pragma unroll 1
     for (int i = 0; i < 8; ++i) {
       const uint32_t w2 = i < 4 ? (i < 2 ? w.x : w.y) : (i < 6 ? w.z : w.w);
-      const float e = __uint_as_float(i & 1 ? w2 & 0xFFFF0000u : w2 << 16), y = __fmul_rn(__fsub_rn(e, lo), inv), d = __fsub_rn(y, __fsub_rn(__fadd_rn(y, kMagic), kMagic));
-      if (!(fabsf(d) <= 0.5f - 4e-6f)) codes = (codes & ~(15u << (4 * i))) | (uint32_t)quant_code(e, lo, s, 15) << (4 * i);
+      const float e = __uint_as_float(i & 1 ? w2 & 0xFFFF0000u : w2 << 16), y = __fmul_rn(__fsub_rn(e, lo), inv), f = __fadd_rn(y, kMagic), d = __fsub_rn(y, __fsub_rn(f, kMagic));
+      codes |= (uint32_t)(fabsf(d) <= kMargin ? __float_as_int(f) & 15 : quant_code(e, lo, s, 15)) << (4 * i);
     }
   }
   Quantized y;
   y.codes = codes;
-  y.meta = (__float_as_uint(lo) >> 16) | (__float_as_uint(s) & 0xFFFF0000u);
+  y.meta = (both & 0xFFFFu) | (__float_as_uint(s) & 0xFFFF0000u);
   return y;
 }
 
@@ -128,6 +149,7 @@ __device__ __forceinline__ bool token_place(const PagedAppend& a, int tok, int& 
   return true;
 }
 
+template <int kLanes>
 __global__ void __launch_bounds__(256, 3)
 append_kernel(const __grid_constant__ PagedAppend a, int kv_blocks, int kv_each, int kv_splits, int q_each, int q_splits) {
   dependency_wait();
@@ -167,12 +189,13 @@ append_kernel(const __grid_constant__ PagedAppend a, int kv_blocks, int kv_each,
   const bool live = piece != nullptr;
   if (live) piece += v.tile_of(place);
   const ChunkLane lane = chunk_lane(a.turn, pos, c, live && a.turn.cos_t != nullptr);
-  const int row = place & 15, G = v.G, group_lanes = G / 8;
+  constexpr int G = 8 * kLanes;
+  const int row = place & 15;
   const int v_at = (16 * (c & 3) + 2 * (c >> 2)) ^ ((row & 4) << 3);
   char* k_to = piece + row * 64 + 16 * (c & 3) + 4 * (c >> 2);
   char* v_to = piece + 1024 + row * 64 + v_at;
-  char* m_to = piece + paged_k_meta(row, G) + 4 * (c / group_lanes);
-  const bool first = c % group_lanes == 0;
+  char* m_to = piece + paged_k_meta(row, G) + 4 * (c / kLanes);
+  const bool first = c % kLanes == 0;
   const int h0 = split * kv_each, h1 = min(h0 + kv_each, 2 * v.Hkv);
   for (int h = h0; h < h1; h += kBatch) {
     uint4 w[kBatch];
@@ -189,7 +212,7 @@ append_kernel(const __grid_constant__ PagedAppend a, int kv_blocks, int kv_each,
       const int hh = h + k;
       if (hh >= h1) break;
       const bool keys = hh < v.Hkv;
-      const Quantized z = quantize_chunk(keys ? turn_chunk(w[k], lane, F2{a.turn.minus_zero}) : w[k], group_lanes);
+      const Quantized z = quantize_chunk<kLanes>(keys ? turn_chunk(w[k], lane, F2{a.turn.minus_zero}) : w[k]);
       const uint64_t at = (uint64_t)(keys ? hh : hh - v.Hkv) * v.piece_bytes;
       if (live) {
         if (keys) {
@@ -265,7 +288,8 @@ cudaError_t launch_paged_append(const PagedAppend& a, int n_sms, cudaStream_t st
   const long long tokens = (long long)a.view.B * a.view.n, kv = (tokens + kTokens - 1) / kTokens, q = a.q != nullptr ? (tokens + 2 * kTokens - 1) / (2 * kTokens) : 0;
   const int kv_each = split_heads(kv, 2 * a.view.Hkv, n_sms), q_each = split_heads(std::max(q, 1ll), a.view.Hq, n_sms);
   const int kv_splits = (2 * a.view.Hkv + kv_each - 1) / kv_each, q_splits = (a.view.Hq + q_each - 1) / q_each;
-  return launch_dependent(append_kernel, dim3((unsigned)(kv * kv_splits + q * q_splits)), 256, 0, stream, a, (int)(kv * kv_splits), kv_each, kv_splits, q_each, q_splits);
+  const auto kernel = a.view.G == 32 ? append_kernel<4> : a.view.G == 64 ? append_kernel<8> : append_kernel<16>;
+  return launch_dependent(kernel, dim3((unsigned)(kv * kv_splits + q * q_splits)), 256, 0, stream, a, (int)(kv * kv_splits), kv_each, kv_splits, q_each, q_splits);
 }
 
 cudaError_t launch_paged_read(const PagedRead& a, int n_sms, cudaStream_t stream) {

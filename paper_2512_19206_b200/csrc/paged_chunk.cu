@@ -32,7 +32,7 @@ constexpr int kRows = 2 * kTile;                 // of an item
 constexpr int kThreads = 384;
 constexpr int kPartFloats = kD + 4;              // sums of a row: o[128], reference, denominator, lost channels, (pad)
 constexpr int kAhead = 2;                        // positions that the beginning of an item counts as
-constexpr uint32_t kPolls = 1u << 21;
+constexpr uint32_t kPolls = 1u << 19;            // (a poll that finds nothing returns after about 4 us)
 constexpr size_t kImageBytes = (size_t)512 << 20;      // of images at a time: sequences (or heads) beyond are a pass of their own
 constexpr int kShift = 4;                        // the weight of a logit equal to the reference is 2^kShift
 constexpr float kRise = 8.f;                     // a logit this much above the reference raises it: weights are 2^12 at most
@@ -167,6 +167,16 @@ unpack_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ 
 }
 
 // ---------------------------------------------------------------------------------------------------------------- attention
+// Polls a phase of a barrier up to max_polls times; false if it never completed.  Without a suspend hint: a phase that completes ends the poll at once.
+__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, uint32_t max_polls) {
+  uint32_t ok;
+#pragma unroll 1
+  for (uint32_t n = 0;; ++n) {
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    if (ok != 0) return true;
+    if (n >= max_polls) return false;
+  }
+}
 enum Bar { kKFull = 0, kVFull = 2, kKEmpty = 4, kVEmpty = 6, kSFull = 8, kPHalf = 10, kPReady = 12, kDone = 14, kQReady = 16, kAllDone = 18, kBars = 19 };
 constexpr int kBehind = 6 * kTileBytes;          // bytes of shared memory before the barriers
 constexpr int kSmem = kBehind + 256;             // and before the sequences' positions
@@ -482,7 +492,7 @@ attend_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ 
   const uint32_t max_polls = a.max_polls ? a.max_polls : kPolls;
   bool dead = false;
   auto wait = [&](int i, uint32_t parity) {
-    if (!dead && !mbar_wait_polls(bar(i), parity, max_polls)) {
+    if (!dead && !wait_phase(bar(i), parity, max_polls)) {
       dead = true;
       atomicOr(v.status, (uint32_t)MIXKVQ_DEV_COPY_TIMEOUT);
     }
@@ -491,7 +501,7 @@ attend_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ 
   auto two_groups = [&](const Walk& w) { return w.r * kRows + kTile < w.rows; };
 
   if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;" ::: "memory");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;" ::: "memory");
     if (warp == 8 && lane == 0) {
       // ---------------------------------------------------------------- tensor-core issue
       const uint32_t idesc_qk = make_idesc(128, 128, 0, 0), idesc_pv = make_idesc(128, 128, 0, 1);
@@ -590,7 +600,7 @@ attend_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ 
       }
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;" ::: "memory");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 200;" ::: "memory");
     // ------------------------------------------------------------------ softmax and output rows
     const int g = warp >> 2;
     const uint32_t lane_base = tbase + ((uint32_t)((warp & 3) * 32) << 16), s_addr = lane_base + 128 * g, o_addr = lane_base + 256 + 128 * g;
