@@ -6,6 +6,7 @@
 // codes are one word and the extrema of a group two to four exchanges; thread blocks for queries: eight lanes have a row (turn_pair).  A thread has one token and goes
 // through a range of heads.
 #include <algorithm>
+#include <type_traits>
 
 #include "paged.cuh"
 
@@ -116,13 +117,20 @@ __device__ __forceinline__ Quantized quantize_chunk(uint4 w) {
     codes = codes * 256u + (__float_as_uint(f1) * 16u + __float_as_uint(f0));      // (what is above the codes is taken off at the end)
   }
   codes -= (uint32_t)(0x4B400000ull * 0x11111111ull);
-  if (near) {                              // (one element as a rule)
+  if (near) {                              // some element (one as a rule) is divided
+    uint32_t which = 0;
     codes = 0;
-#pragma unroll 1
+#pragma unroll
     for (int i = 0; i < 8; ++i) {
+      const float y = __fmul_rn(__fsub_rn(bf16_half(a[i >> 1], i & 1), lo), inv), f = __fadd_rn(y, kMagic);
+      which |= fabsf(__fsub_rn(y, __fsub_rn(f, kMagic))) <= kMargin ? 0u : 1u << i;
+      codes |= (__float_as_uint(f) & 15u) << (4 * i);
+    }
+#pragma unroll 1
+    for (; which != 0; which &= which - 1) {
+      const int i = __ffs(which) - 1;
       const uint32_t w2 = i < 4 ? (i < 2 ? w.x : w.y) : (i < 6 ? w.z : w.w);
-      const float e = __uint_as_float(i & 1 ? w2 & 0xFFFF0000u : w2 << 16), y = __fmul_rn(__fsub_rn(e, lo), inv), f = __fadd_rn(y, kMagic), d = __fsub_rn(y, __fsub_rn(f, kMagic));
-      codes |= (uint32_t)(fabsf(d) <= kMargin ? __float_as_int(f) & 15 : quant_code(e, lo, s, 15)) << (4 * i);
+      codes = (codes & ~(15u << (4 * i))) | (uint32_t)quant_code(__uint_as_float(i & 1 ? w2 & 0xFFFF0000u : w2 << 16), lo, s, 15) << (4 * i);
     }
   }
   Quantized y;
@@ -163,21 +171,26 @@ append_kernel(const __grid_constant__ PagedAppend a, int kv_blocks, int kv_each,
     if (!token_place(a, tok, b, i, place, pos) || v.piece(b, 0, place) == nullptr) return;
     const PairLane p = pair_lane(a.turn, pos, threadIdx.x & 7, a.turn.cos_t != nullptr);
     const int h0 = split * q_each, h1 = min(h0 + q_each, v.Hq);
+    const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q) + b * a.tq.batch + h0 * a.tq.head + i * a.tq.token;
+    __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.q_out) + (((size_t)b * v.Hq + h0) * v.n + i) * kD;
+    const size_t out_head = (size_t)v.n * kD;
     for (int h = h0; h < h1; h += kBatch) {
       uint4 w[kBatch][2];
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) {
-        const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + b * a.tq.batch + min(h + k, h1 - 1) * a.tq.head + i * a.tq.token);
-        w[k][0] = src[p.first];
-        w[k][1] = src[p.second];
+        const uint4* from = reinterpret_cast<const uint4*>(src);
+        w[k][0] = from[p.first];
+        w[k][1] = from[p.second];
+        if (h + k + 1 < h1) src += a.tq.head;    // (the last row again beyond it)
       }
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) {
         if (h + k >= h1) break;
         turn_pair(w[k][0], w[k][1], p, F2{a.turn.minus_zero});
-        uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.q_out) + (((size_t)b * v.Hq + h + k) * v.n + i) * kD);
-        dst[p.first] = w[k][0];
-        dst[p.second] = w[k][1];
+        uint4* to = reinterpret_cast<uint4*>(dst);
+        to[p.first] = w[k][0];
+        to[p.second] = w[k][1];
+        dst += out_head;
       }
     }
     return;
@@ -192,39 +205,43 @@ append_kernel(const __grid_constant__ PagedAppend a, int kv_blocks, int kv_each,
   constexpr int G = 8 * kLanes;
   const int row = place & 15;
   const int v_at = (16 * (c & 3) + 2 * (c >> 2)) ^ ((row & 4) << 3);
-  char* k_to = piece + row * 64 + 16 * (c & 3) + 4 * (c >> 2);
-  char* v_to = piece + 1024 + row * 64 + v_at;
-  char* m_to = piece + paged_k_meta(row, G) + 4 * (c / kLanes);
   const bool first = c % kLanes == 0;
   const int h0 = split * kv_each, h1 = min(h0 + kv_each, 2 * v.Hkv);
-  for (int h = h0; h < h1; h += kBatch) {
-    uint4 w[kBatch];
+  // heads h0 .. h1 - 1 of keys, then values
+  auto rows = [&](auto keys_, const void* in, const RopeTensor& t, int from, int to) {
+    constexpr bool keys = decltype(keys_)::value;
+    const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(in) + b * t.batch + from * t.head + i * t.token + 8 * c;
+    char* at = piece + (uint64_t)from * v.piece_bytes;
+    char* codes_to = at + (keys ? row * 64 + 16 * (c & 3) + 4 * (c >> 2) : 1024 + row * 64 + v_at);
+    char* meta_to = at + (keys ? paged_k_meta(row, G) : paged_v_meta(row, G)) + 4 * (c / kLanes);
+    for (int h = from; h < to; h += kBatch) {
+      uint4 w[kBatch];
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-      w[k] = make_uint4(0u, 0u, 0u, 0u);
-      const int hh = min(h + k, h1 - 1);
-      const RopeTensor& s = hh < v.Hkv ? a.tk : a.tv;
-      if (live)
-        w[k] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(hh < v.Hkv ? a.k : a.v) + b * s.batch + (hh < v.Hkv ? hh : hh - v.Hkv) * s.head + i * s.token + 8 * c);
-    }
+      for (int k = 0; k < kBatch; ++k) {
+        w[k] = make_uint4(0u, 0u, 0u, 0u);
+        if (live) w[k] = *reinterpret_cast<const uint4*>(src);
+        if (h + k + 1 < to) src += t.head;       // (the last row again beyond it)
+      }
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-      const int hh = h + k;
-      if (hh >= h1) break;
-      const bool keys = hh < v.Hkv;
-      const Quantized z = quantize_chunk<kLanes>(keys ? turn_chunk(w[k], lane, F2{a.turn.minus_zero}) : w[k]);
-      const uint64_t at = (uint64_t)(keys ? hh : hh - v.Hkv) * v.piece_bytes;
-      if (live) {
-        if (keys) {
-          *reinterpret_cast<uint32_t*>(k_to + at) = z.codes;
-        } else {
-          *reinterpret_cast<uint16_t*>(v_to + at) = (uint16_t)z.codes;
-          *reinterpret_cast<uint16_t*>(v_to + at + 8) = (uint16_t)(z.codes >> 16);
+      for (int k = 0; k < kBatch; ++k) {
+        if (h + k >= to) break;
+        const Quantized z = quantize_chunk<kLanes>(keys ? turn_chunk(w[k], lane, F2{a.turn.minus_zero}) : w[k]);
+        if (live) {
+          if (keys) {
+            *reinterpret_cast<uint32_t*>(codes_to) = z.codes;
+          } else {
+            *reinterpret_cast<uint16_t*>(codes_to) = (uint16_t)z.codes;
+            *reinterpret_cast<uint16_t*>(codes_to + 8) = (uint16_t)(z.codes >> 16);
+          }
+          if (first) *reinterpret_cast<uint32_t*>(meta_to) = z.meta;
         }
-        if (first) *reinterpret_cast<uint32_t*>(m_to + at + (keys ? 0u : 16u * paged_meta_bytes(G))) = z.meta;
+        codes_to += v.piece_bytes;
+        meta_to += v.piece_bytes;
       }
     }
-  }
+  };
+  if (h0 < v.Hkv) rows(std::true_type{}, a.k, a.tk, h0, min(h1, v.Hkv));
+  if (h1 > v.Hkv) rows(std::false_type{}, a.v, a.tv, max(h0, v.Hkv) - v.Hkv, h1 - v.Hkv);
 }
 
 // A thread has 8 channels of one token and goes through the heads, some rows' loads under way together.
@@ -242,37 +259,45 @@ read_kernel(const __grid_constant__ PagedRead a, int heads_per_block) {
   if (piece == nullptr) return;
   piece += v.tile_of(place);
   const int row = place & 15, G = v.G, grp = c / (G / 8);
-  const char* k_from = piece + row * 64 + 16 * (c & 3) + 4 * (c >> 2);
-  const char* v_from = piece + 1024 + row * 64 + ((16 * (c & 3) + 2 * (c >> 2)) ^ ((row & 4) << 3));
-  const char* m_from = piece + paged_k_meta(row, G) + 4 * grp;
+  const int v_at = (16 * (c & 3) + 2 * (c >> 2)) ^ ((row & 4) << 3);
   const int h0 = blockIdx.y * heads_per_block, h1 = min(h0 + heads_per_block, 2 * v.Hkv);
-  for (int h = h0; h < h1; h += kBatch) {
-    uint32_t codes[kBatch], meta[kBatch];
+  // heads h0 .. h1 - 1 of keys, then values
+  auto rows = [&](auto keys_, void* out, int from, int to) {
+    constexpr bool keys = decltype(keys_)::value;
+    const char* at = piece + (uint64_t)from * v.piece_bytes;
+    const char* codes_at = at + (keys ? row * 64 + 16 * (c & 3) + 4 * (c >> 2) : 1024 + row * 64 + v_at);
+    const char* meta_at = at + (keys ? paged_k_meta(row, G) : paged_v_meta(row, G)) + 4 * grp;
+    __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(out) + (((size_t)b * v.Hkv + from) * v.n + i) * kD + 8 * c;
+    const size_t out_head = (size_t)v.n * kD;
+    for (int h = from; h < to; h += kBatch) {
+      uint32_t codes[kBatch], meta[kBatch];
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-      const int hh = min(h + k, h1 - 1);
-      const bool keys = hh < v.Hkv;
-      const uint64_t at = (uint64_t)(keys ? hh : hh - v.Hkv) * v.piece_bytes;
-      if (keys)
-        codes[k] = *reinterpret_cast<const uint32_t*>(k_from + at);
-      else
-        codes[k] = *reinterpret_cast<const uint16_t*>(v_from + at) | (uint32_t)*reinterpret_cast<const uint16_t*>(v_from + at + 8) << 16;
-      meta[k] = *reinterpret_cast<const uint32_t*>(m_from + at + (keys ? 0u : 16u * paged_meta_bytes(G)));
+      for (int k = 0; k < kBatch; ++k) {
+        if (keys)
+          codes[k] = *reinterpret_cast<const uint32_t*>(codes_at);
+        else
+          codes[k] = *reinterpret_cast<const uint16_t*>(codes_at) | (uint32_t)*reinterpret_cast<const uint16_t*>(codes_at + 8) << 16;
+        meta[k] = *reinterpret_cast<const uint32_t*>(meta_at);
+        if (h + k + 1 < to) {                    // (the last row again beyond it)
+          codes_at += v.piece_bytes;
+          meta_at += v.piece_bytes;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        if (h + k >= to) break;
+        const float s = bf16_half(meta[k], 1), z = bf16_half(meta[k], 0);
+        uint32_t y[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)         // (code times scale is exact: 4 bits by 8)
+          y[j] = bf16_pair(fmaf((float)(codes[k] >> (8 * j) & 15u), s, z), fmaf((float)(codes[k] >> (8 * j + 4) & 15u), s, z));
+        *reinterpret_cast<uint4*>(dst) = make_uint4(y[0], y[1], y[2], y[3]);
+        dst += out_head;
+      }
     }
-#pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-      const int hh = h + k;
-      if (hh >= h1) break;
-      const bool keys = hh < v.Hkv;
-      const float s = bf16_half(meta[k], 1), z = bf16_half(meta[k], 0);
-      uint32_t y[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j)           // (code times scale is exact: 4 bits by 8)
-        y[j] = bf16_pair(fmaf((float)(codes[k] >> (8 * j) & 15u), s, z), fmaf((float)(codes[k] >> (8 * j + 4) & 15u), s, z));
-      *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(keys ? a.k : a.v) + (((size_t)b * v.Hkv + (keys ? hh : hh - v.Hkv)) * v.n + i) * kD + 8 * c) =
-          make_uint4(y[0], y[1], y[2], y[3]);
-    }
-  }
+  };
+  if (h0 < v.Hkv) rows(std::true_type{}, a.k, h0, min(h1, v.Hkv));
+  if (h1 > v.Hkv) rows(std::false_type{}, a.v, max(h0, v.Hkv) - v.Hkv, h1 - v.Hkv);
 }
 
 // Heads per thread block: all of a token's, fewer as long as the SMs have room (but what a thread has in flight).
