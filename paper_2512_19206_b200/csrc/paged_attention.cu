@@ -23,6 +23,7 @@ namespace {
 constexpr int kWarps = 4;                        // of a thread block with pieces of streams, 16 of one with a whole short stream
 constexpr int kUnit = 32;                        // tokens
 constexpr int kStages = 2;                       // units in a warp's ring, per tile of 8 query rows
+constexpr int kQueryBytes = 2048;                // operands of 8 query rows
 constexpr int kPartFloats = kD + 4;              // of a row's sums: o[128], reference, denominator, (pad)
 constexpr uint32_t kPolls = 1u << 21;
 constexpr int kBelow = 16;                       // a reference is brought this much (in powers of two) above its row's largest logit: sums of large values keep off fp32's end
@@ -94,6 +95,10 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, t = lane & 3;
   const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * stages * kUnitBytes);
   unsigned char* behind = smem + kW * stages * kUnitBytes;
+  // The queries' operands: in registers for 16 rows; for 8 rows, where they would cost the SM four warps, in shared memory (a copy per warp: no barrier)
+  constexpr bool kQueriesInRegisters = kNT > 1;
+  const uint32_t q_at = smem_u32(behind) + (uint32_t)(warp * kQueryBytes) + 16u * (uint32_t)lane;
+  if constexpr (!kQueriesInRegisters) behind += kW * kQueryBytes;
   const uint32_t bars = smem_u32(behind) + 8u * (uint32_t)(warp * stages);
   long long* prefix = reinterpret_cast<long long*>(behind + 8 * kW * stages);
   if (lane == 0) {
@@ -271,7 +276,7 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
     for (int i = 0; i < asked; ++i) issue(i);
 
     // ---- queries: lane (r, t) has channels 32 j + 8 t .. + 7 of row r of every row tile as operands
-    uint32_t qb[kNT][4][4];                      // word j: {0,4} {2,6} {1,5}/16 {3,7}/16
+    uint32_t qb[kQueriesInRegisters ? kNT : 1][4][4];                      // word j: {0,4} {2,6} {1,5}/16 {3,7}/16
     uint32_t qz[kNT][3];                         // sums of the row's groups as three bf16 terms each: {sum of group t, 0}
     float qscale[kNT][2];
     int sees[kNT][2];
@@ -308,6 +313,7 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
         qb[nt][j][1] = pack_half2(f[2] * up, f[6] * up);
         qb[nt][j][2] = pack_half2(f[1] * (up * 0.0625f), f[5] * (up * 0.0625f));
         qb[nt][j][3] = pack_half2(f[3] * (up * 0.0625f), f[7] * (up * 0.0625f));
+        if constexpr (!kQueriesInRegisters) sts128(q_at + 512 * j, qb[nt][j][0], qb[nt][j][1], qb[nt][j][2], qb[nt][j][3]);      // (the lane's own words: no other reads them)
       }
 #pragma unroll
       for (int k = 0; k < kNG; ++k) {
@@ -388,11 +394,16 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
             const uint32_t o0 = w0[j] & 0x00F000F0u, o1 = w1[j] & 0x00F000F0u, o2 = h0 & 0x00F000F0u, o3 = h1 & 0x00F000F0u;
 #pragma unroll
             for (int nt = 0; nt < kNT; ++nt) {
-              if (j == g * 4 / kNG)
-                mma_f16_to(c[nt], e0, e1, e2, e3, qb[nt][j][0], qb[nt][j][1], 0.f, 0.f, 0.f, 0.f);
+              uint4 q;
+              if constexpr (kQueriesInRegisters)
+                q = make_uint4(qb[nt][j][0], qb[nt][j][1], qb[nt][j][2], qb[nt][j][3]);
               else
-                mma_f16(c[nt], e0, e1, e2, e3, qb[nt][j][0], qb[nt][j][1]);
-              mma_f16(c[nt], o0, o1, o2, o3, qb[nt][j][2], qb[nt][j][3]);
+                q = lds128(q_at + 512 * j);
+              if (j == g * 4 / kNG)
+                mma_f16_to(c[nt], e0, e1, e2, e3, q.x, q.y, 0.f, 0.f, 0.f, 0.f);
+              else
+                mma_f16(c[nt], e0, e1, e2, e3, q.x, q.y);
+              mma_f16(c[nt], o0, o1, o2, o3, q.z, q.w);
             }
           }
           const float s0 = bf_hi(m0[g]), s1 = bf_hi(m1[g]);
@@ -747,7 +758,7 @@ int warps_of(int tiles, bool direct) { return tiles == 1 && direct ? kDirectWarp
 int tiles_of(int g, int n) { return g * n <= 8 ? 1 : 2; }
 size_t smem_bytes(int G, int tiles, int B, bool direct) {
   const int warps = warps_of(tiles, direct);
-  return (size_t)warps * kStages * tiles * 2 * paged_tile_bytes(G) + 8 * warps * kStages * tiles + (direct || B <= 32 ? 0 : 8 * (size_t)(B + 1));
+  return (size_t)warps * (kStages * tiles * 2 * paged_tile_bytes(G) + (tiles == 1 ? kQueryBytes : 0)) + 8 * warps * kStages * tiles + (direct || B <= 32 ? 0 : 8 * (size_t)(B + 1));
 }
 
 }  // namespace
