@@ -412,6 +412,13 @@ int mixkvq_paged_test_arm_copy_timeout(mixkvq_paged* cache, uint32_t extra_bytes
 int mixkvq_paged_query_status(mixkvq_paged* cache, int* device_status, void* stream);
 int mixkvq_paged_clear_status(mixkvq_paged* cache, void* stream);
 uint64_t mixkvq_paged_launch_count(const mixkvq_paged* cache);
+/* Which kernel the last attention on this handle enqueued (diagnostic), 0 before the first. */
+enum {
+  MIXKVQ_PAGED_DIRECT = 1,            /* a thread block per KV head and block of query rows, which wrote the output */
+  MIXKVQ_PAGED_PIECES = 2,            /* pieces of streams, joined by a second kernel                */
+  MIXKVQ_PAGED_UNPACKED = 4           /* the pages unpacked once into fp16 tiles, tcgen05            */
+};
+int mixkvq_paged_last_attention(const mixkvq_paged* cache);
 
 /* (The paper has no counterpart of this entry point; it exists for integration reasons only.)
  * Same computation and same results as mixkvq_decode_attention, for callers that have no way to hand

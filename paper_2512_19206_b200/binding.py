@@ -24,11 +24,12 @@ EXPORTS = [
     "mixkvq_cache_written_externally", "mixkvq_test_arm_copy_timeout", "mixkvq_test_arm_value_copy_timeout", "mixkvq_rope_append", "mixkvq_rope_decode_step", "mixkvq_prefill", "mixkvq_prefill_scratch_bytes", "mixkvq_chunk_attention", "mixkvq_chunk_step", "mixkvq_chunk_scratch_bytes", "mixkvq_rope_axes", "mixkvq_rope_axes_append", "mixkvq_rope_axes_decode_step", "mixkvq_quantize_append_ragged", "mixkvq_sequence_fill", "mixkvq_decode_attention_partial", "mixkvq_merge_partials",
     "mixkvq_rope_partial", "mixkvq_rope_tables", "mixkvq_paged_bytes", "mixkvq_paged_workspace_bytes", "mixkvq_paged_init", "mixkvq_paged_destroy",
     "mixkvq_paged_append", "mixkvq_paged_read", "mixkvq_paged_attention", "mixkvq_paged_step", "mixkvq_paged_test_arm_copy_timeout",
-    "mixkvq_paged_query_status", "mixkvq_paged_clear_status", "mixkvq_paged_launch_count",
+    "mixkvq_paged_query_status", "mixkvq_paged_clear_status", "mixkvq_paged_launch_count", "mixkvq_paged_last_attention",
 ]
 
 DEV_EXTRAS_FULL, DEV_COPY_TIMEOUT, DEV_BAD_POSITION, DEV_BAD_LENGTH, DEV_BAD_PAGE = 1, 2, 4, 8, 16
 _OUT_TYPES = {torch.float32: 0, torch.bfloat16: 1}
+PAGED_DIRECT, PAGED_PIECES, PAGED_UNPACKED = 1, 2, 4
 ATTN_ONE_UNIT, ATTN_TWO_UNITS, ATTN_DIRECT, ATTN_EARLY, ATTN_OTHER, ATTN_EIGHT_PAIRS = 1, 2, 4, 8, 16, 32
 
 
@@ -130,7 +131,7 @@ def lib():
         L.mixkvq_paged_bytes.argtypes = [C.POINTER(PagedConfig), C.POINTER(C.c_size_t)]
         L.mixkvq_paged_workspace_bytes.argtypes = [C.POINTER(PagedConfig), i32, i32, i32]
         L.mixkvq_paged_init.argtypes = [C.POINTER(PagedConfig), vp, C.c_size_t, vp, C.POINTER(vp)]
-        L.mixkvq_paged_destroy.argtypes = L.mixkvq_paged_launch_count.argtypes = [vp]
+        L.mixkvq_paged_destroy.argtypes = L.mixkvq_paged_launch_count.argtypes = L.mixkvq_paged_last_attention.argtypes = [vp]
         L.mixkvq_paged_append.argtypes = [vp, i32, seqs, vp, vp, vp, i64s, rot, vp, vp]
         L.mixkvq_paged_read.argtypes = [vp, i32, seqs, vp, vp, vp]
         L.mixkvq_paged_attention.argtypes = [vp, i32, seqs, vp, vp, i32, f32, vp, C.c_size_t, vp]
@@ -744,3 +745,7 @@ class PagedCache:
 
     def launch_count(self) -> int:
         return int(lib().mixkvq_paged_launch_count(self.handle))
+
+    def last_attention(self) -> int:
+        """PAGED_*: which kernel the last attention on this cache took."""
+        return int(lib().mixkvq_paged_last_attention(self.handle))

@@ -120,7 +120,7 @@ struct RopeTables {
 
 cudaError_t launch_paged_append(const PagedAppend& a, int n_sms, cudaStream_t stream);
 cudaError_t launch_paged_read(const PagedRead& a, int n_sms, cudaStream_t stream);
-cudaError_t launch_paged_attention(const PagedAttention& a, int n_sms, cudaStream_t stream, int* launches);
+cudaError_t launch_paged_attention(const PagedAttention& a, int n_sms, cudaStream_t stream, int* launches, int* form);      // form: MIXKVQ_PAGED_*
 size_t paged_workspace_bytes(int Hkv, int g, int batch, int n, long long capacity);
 // many query rows (tcgen05); capacity: tokens that the pages of a sequence hold at most
 bool paged_chunk_fits(long long capacity);

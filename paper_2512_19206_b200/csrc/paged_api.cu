@@ -14,6 +14,7 @@ struct mixkvq_paged {
   uint32_t tile_bytes, piece_bytes;
   int g, lg_page, n_sms;
   uint64_t launches;
+  int last_form;                             // mixkvq_paged_last_attention
   uint32_t test_extra_tx, test_wait_polls;   // mixkvq_paged_test_arm_copy_timeout
 };
 
@@ -138,7 +139,7 @@ int run_append(mixkvq_paged* h, const PagedAppend& a, cudaStream_t st) {
 }
 int run_attention(mixkvq_paged* h, const PagedAttention& a, cudaStream_t st) {
   int launches = 0;
-  const cudaError_t e = launch_paged_attention(a, h->n_sms, st, &launches);
+  const cudaError_t e = launch_paged_attention(a, h->n_sms, st, &launches, &h->last_form);
   h->launches += launches;
   return e == cudaSuccess ? MIXKVQ_OK : MIXKVQ_E_CUDA;
 }
@@ -302,6 +303,8 @@ int mixkvq_paged_clear_status(mixkvq_paged* cache, void* stream) {
   if (!cache) return MIXKVQ_E_INVALID_ARG;
   return cudaMemsetAsync(cache->mem, 0, kHeaderBytes, static_cast<cudaStream_t>(stream)) == cudaSuccess ? MIXKVQ_OK : MIXKVQ_E_CUDA;
 }
+
+int mixkvq_paged_last_attention(const mixkvq_paged* cache) { return cache ? cache->last_form : 0; }
 
 uint64_t mixkvq_paged_launch_count(const mixkvq_paged* cache) { return cache ? cache->launches : 0; }
 

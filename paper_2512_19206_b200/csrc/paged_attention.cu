@@ -743,7 +743,11 @@ merge_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
 }
 
 constexpr int kDirectTokens = 512;               // capacity up to which a thread block has a stream to itself
-constexpr int kUnpackRows = 128;                 // query rows of a KV head above which unpacking pays
+// Query rows of a KV head above which unpacking the pages pays: kUnpackRows, and more where there is little to unpack (kUnpackWork / tokens of all KV heads), as its three
+// launches take longer than two.  By what the pages could hold, the lengths being unknown here.  7b shape, us with the pages as they are / unpacked: 8 x 32768 tokens 63 rows 214 / 248,
+// 98 rows 357 / 253; 8 x 8192 63 rows 69 / 85, 98 rows 108 / 89; 1 x 32768 98 rows 60 / 75, 252 rows 115 / 115; 1 x 1024 896 rows 34 / 39.
+constexpr int kUnpackRows = 72;
+constexpr double kUnpackWork = 5e6;
 constexpr int kMostBlocks = 148 * 4;             // thread blocks of the split kernel: sizes the workspace
 
 using Kernel = void (*)(PagedAttention, Plan);
@@ -764,10 +768,12 @@ size_t smem_bytes(int G, int tiles, int B, bool direct) {
 }  // namespace
 
 // Whether a call goes to the kernel that unpacks the pages once for all query rows.
-static bool unpacks(int g, int n, long long capacity) { return (long long)g * n > kUnpackRows && paged_chunk_fits(capacity); }
+static bool unpacks(int Hkv, int g, int batch, int n, long long capacity) {
+  return (double)g * n > kUnpackRows + kUnpackWork / ((double)batch * Hkv * capacity) && paged_chunk_fits(capacity);
+}
 
 size_t paged_workspace_bytes(int Hkv, int g, int batch, int n, long long capacity) {
-  if (unpacks(g, n, capacity)) return paged_chunk_workspace_bytes(Hkv, batch, capacity);
+  if (unpacks(Hkv, g, batch, n, capacity)) return paged_chunk_workspace_bytes(Hkv, batch, capacity);
   return (size_t)2 * kMostBlocks * 8 * tiles_of(g, n) * kPartFloats * 4 + kMostBlocks * sizeof(Broken);
 }
 
@@ -783,10 +789,13 @@ cudaError_t paged_attention_setup() {
   return paged_chunk_setup();
 }
 
-cudaError_t launch_paged_attention(const PagedAttention& a, int n_sms, cudaStream_t stream, int* launches) {
+cudaError_t launch_paged_attention(const PagedAttention& a, int n_sms, cudaStream_t stream, int* launches, int* form) {
   const PagedView& v = a.view;
   *launches = 0;
-  if (unpacks(v.g, v.n, (long long)v.max_pages << v.lg_page)) return launch_paged_chunk(a, n_sms, stream, launches);
+  if (unpacks(v.Hkv, v.g, v.B, v.n, (long long)v.max_pages << v.lg_page)) {
+    *form = MIXKVQ_PAGED_UNPACKED;
+    return launch_paged_chunk(a, n_sms, stream, launches);
+  }
   const int tiles = tiles_of(v.g, v.n);
   Plan plan{};
   plan.rows = 8 * tiles;
@@ -800,6 +809,7 @@ cudaError_t launch_paged_attention(const PagedAttention& a, int n_sms, cudaStrea
   const int warps = warps_of(tiles, plan.direct);
   cudaError_t e = launch_dependent(kernel_of(v.G, tiles, plan.direct), dim3((unsigned)(plan.direct ? streams : most)), warps * 32, smem_bytes(v.G, tiles, v.B, plan.direct), stream,
                                    a, plan);
+  *form = plan.direct ? MIXKVQ_PAGED_DIRECT : MIXKVQ_PAGED_PIECES;
   *launches = 1;
   if (e != cudaSuccess || plan.direct) return e;
   *launches = 2;

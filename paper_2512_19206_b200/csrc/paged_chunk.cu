@@ -721,30 +721,42 @@ attend_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ 
   if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tbase), "r"(512));
 }
 
-// Joins the parts of the item that begins in thread block blockIdx.x of attend_kernel and ends in another: a warp per row, a lane four channels.
+// Joins the parts of the item that begins in thread block blockIdx.x of attend_kernel and ends in another: a warp has a row, a lane four channels, eight parts' loads are
+// under way together.
+constexpr int kJoinBlocks = 16;                  // thread blocks of an item
 __global__ void __launch_bounds__(256)
 join_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ ChunkPlan plan) {
   dependency_wait();
   const PagedView& v = a.view;
   const Broken it = plan.broken[blockIdx.x];
   if (it.last <= (int)blockIdx.x) return;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rows = v.count(plan.b0 + it.b) * v.g;
-  for (int k = blockIdx.y * 8 + warp; k < kRows; k += 8 * gridDim.y) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rows = v.count(plan.b0 + it.b) * v.g, c0 = blockIdx.x;
+  for (int k = blockIdx.y * 8 + warp; k < kRows; k += 8 * kJoinBlocks) {
     const int x = it.r * kRows + k;
     if (x >= rows) return;
     float ref = -1e30f, denom = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
     uint32_t lost = 0;
-    for (int c = blockIdx.x; c <= it.last; ++c) {
-      const float* from = plan.parts + ((size_t)(2 * c + (c == (int)blockIdx.x ? 1 : 0)) * kRows + k) * kPartFloats;
-      const float4 o = *reinterpret_cast<const float4*>(from + 4 * lane), m = *reinterpret_cast<const float4*>(from + kD);
-      const float up = fmaxf(ref, m.x), f0 = ex2(ref - up), f1 = ex2(m.x - up);
-      ref = up;
-      denom = denom * f0 + m.y * f1;
-      lost |= __float_as_uint(m.z);
-      y[0] = y[0] * f0 + o.x * f1;
-      y[1] = y[1] * f0 + o.y * f1;
-      y[2] = y[2] * f0 + o.z * f1;
-      y[3] = y[3] * f0 + o.w * f1;
+    for (int c = c0; c <= it.last; c += 8) {
+      float4 o[8], m[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int part = min(c + i, it.last);
+        const float* from = plan.parts + ((size_t)(2 * part + (part == c0 ? 1 : 0)) * kRows + k) * kPartFloats;
+        o[i] = *reinterpret_cast<const float4*>(from + 4 * lane);
+        m[i] = *reinterpret_cast<const float4*>(from + kD);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (c + i > it.last) break;
+        const float up = fmaxf(ref, m[i].x), f0 = ex2(ref - up), f1 = ex2(m[i].x - up);
+        ref = up;
+        denom = denom * f0 + m[i].y * f1;
+        lost |= __float_as_uint(m[i].z);
+        y[0] = y[0] * f0 + o[i].x * f1;
+        y[1] = y[1] * f0 + o[i].y * f1;
+        y[2] = y[2] * f0 + o[i].z * f1;
+        y[3] = y[3] * f0 + o[i].w * f1;
+      }
     }
     float inv = denom == 0.f ? 0.f : pow2i(kDown) / denom;
     if (lost >> (lane >> 3) & 1u || lost & 16u) inv = NAN;
@@ -808,7 +820,7 @@ cudaError_t launch_paged_chunk(const PagedAttention& a, int n_sms, cudaStream_t 
       if (e != cudaSuccess) return e;
       e = launch_dependent(attend_kernel, dim3(blocks), kThreads, kSmem + 8 * (size_t)(plan.nb + 1), stream, a, plan);
       if (e != cudaSuccess) return e;
-      e = launch_dependent(join_kernel, dim3(blocks, 4), 256, 0, stream, a, plan);
+      e = launch_dependent(join_kernel, dim3(blocks, kJoinBlocks), 256, 0, stream, a, plan);
       if (e != cudaSuccess) return e;
       *launches += 3;
     }

@@ -60,7 +60,7 @@ def place(cfg, layer, page, head, slot):
 
 
 def pages_for(lens, page_tokens, seed, spare=3, extra=0):
-    """A page table int32 [B, P] (CPU) with the pages in any order, -1 behind a sequence's last, and the number of pages."""
+    """A page table int32 [B, P] (CPU) with the pages in any order, -1 behind a sequence's last (`extra` columns of that beyond the longest), and the number of pages."""
     each = [-(-t // page_tokens) for t in lens]
     n = sum(each) + spare
     order = torch.randperm(n, generator=torch.Generator().manual_seed(seed))
@@ -84,9 +84,6 @@ def draw(B, Hq, Hkv, n, seed, outliers=True):
 HALF_STEP = 2.0 ** -11        # of fp16: the weights of the values are rounded to it, once per token and group
 
 
-UNPACKED_ROWS = 128           # more query rows of a KV head than this go to the kernel that rounds keys and values to fp16
-
-
 def unpacked(p, qd, K, V, scale):
     """What rounding the elements of keys and values to fp16 once, independently, may add: a logit is a sum of 128 products, its deviation d at most HALF_STEP scale
     sqrt(sum (q k)^2) by size of a standard deviation; the output moves by sum_t p_t d_t (v_t - o), and by the roundings of p_t and v_t: at most 2 d + 2 HALF_STEP times |p|_2
@@ -96,7 +93,7 @@ def unpacked(p, qd, K, V, scale):
     return 8 * (2 * dev + 2 * HALF_STEP) * p.square().sum(-1, keepdim=True).sqrt() * big + 16 * (K.shape[0] / 128 + 4) * 2.0 ** -23 * big
 
 
-def reference(q, k, v, G, scale, sees, rows=1):
+def reference(q, k, v, G, scale, sees, rounded=False):
     """One KV head: q [g, m, 128], k, v [T, 128] (bf16 rows as appended), sees [m]: the tokens that each row sees -> (output [g, m, 128], allowed error) in 64 bits.
 
     Logits: keys' codes and queries enter exactly; sums of 128 products in fp32 and of the groups' parts lose at most 2^-19 of the sum of the magnitudes |q| (15 s + |z|)
@@ -124,24 +121,24 @@ def reference(q, k, v, G, scale, sees, rows=1):
     s15 = torch.where(torch.isfinite(s15), s15, 0.0)
     biggest = float(s15.max()) if T else 0.0
     tol = 2 * d * (V.abs().max() if T else 0.0) + HALF_STEP * (p @ s15) + 2.0 ** -26 * biggest * T + 2.0 ** -18 * (p @ torch.nan_to_num(reach(vs, vz), 0.0, 0.0, 0.0))
-    if rows > UNPACKED_ROWS:
+    if rounded:
         tol = tol + unpacked(p, qd, K, V, scale)
     return out, tol
 
 
-def check(out, q, k, v, G, scale, lens, counts, only=None):
-    """out [B,Hq,n,128] (any device) against rows q [B,Hq,n,128] over the first lens[b] tokens of k, v [B,Hkv,T,128] (CPU, as appended)."""
+def check(out, q, k, v, G, scale, lens, counts, rounded=False):
+    """out [B,Hq,n,128] (any device) against rows q [B,Hq,n,128] over the first lens[b] tokens of k, v [B,Hkv,T,128] (CPU, as appended).
+    rounded: by the kernel that unpacks keys and values to fp16 (PagedCache.last_attention)."""
     step = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}[out.dtype]
     out = out.double().cpu()
     g = q.shape[1] // k.shape[1]
-    rows = g * q.shape[2]                                  # of the call: it chooses the kernel
     for b, (t, m) in enumerate(zip(lens, counts)):
         for h in range(k.shape[1]):
-            if m == 0 or (only is not None and (b, h) not in only):
+            if m == 0:
                 continue
             hs = slice(h * g, h * g + g)
             sees = [max(0, t - m + i + 1) for i in range(m)]
-            ref, tol = reference(q[b, hs, :m], k[b, h, :t], v[b, h, :t], G, scale, sees, rows)
+            ref, tol = reference(q[b, hs, :m], k[b, h, :t], v[b, h, :t], G, scale, sees, rounded)
             got = out[b, hs, :m]
             fine = torch.isfinite(ref)
             assert torch.equal(torch.isfinite(got), fine), f"sequence {b}, head {h}: not finite"

@@ -29,6 +29,18 @@ def ints(x):
     return torch.tensor(x, dtype=torch.int32, device="cuda")
 
 
+def wide(table, page, room):
+    """The table with columns (none of them looked at) up to `room` tokens: what a call could have to read chooses its kernel."""
+    more = max(0, room // page - table.shape[1])
+    return torch.cat([table, torch.full((table.shape[0], more), -1, dtype=torch.int32)], 1) if more else table
+
+
+def attend(cache, q, table, lens, **kw):
+    """attention, and whether it went to the kernel that rounds keys and values."""
+    out = cache.attention(0, q.cuda(), table.cuda(), ints(lens), SCALE, **kw)
+    return out, cache.last_attention() == 4
+
+
 def filled(binding, Hq, Hkv, lens, page, G, seed, layers=1, layer=0, extra=0, poison=True):
     """A cache whose sequences hold lens[b] tokens of k, v (CPU), its page table and the rows.  poison: the rest of the pool holds NaNs and infinities."""
     T = max(max(lens), 1)
@@ -124,13 +136,20 @@ CASES = [
 
 @pytest.mark.parametrize("Hq,Hkv,lens,counts,page,G", CASES)
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-def test_attention(binding, Hq, Hkv, lens, counts, page, G, dtype):
+@pytest.mark.parametrize("room", [0, 1 << 16])
+def test_attention(binding, Hq, Hkv, lens, counts, page, G, dtype, room):
     cache, table, k, v = filled(binding, Hq, Hkv, lens, page, G, sum(lens), layers=2, layer=1)
+    table = wide(table, page, room)
     q, _, _ = P.draw(len(lens), Hq, Hkv, max(counts), 91)
     out = torch.full(q.shape, 7.0, dtype=dtype, device="cuda")
     cache.attention(1, q.cuda(), table.cuda(), ints(lens), SCALE, counts=ints(counts), out=out)
     assert cache.status() == 0
-    P.check(out, q, k, v, G, SCALE, lens, counts)
+    rows, form = Hq // Hkv * max(counts), cache.last_attention()
+    if rows <= 72:
+        assert form == (binding.PAGED_PIECES if table.shape[1] * page > 512 else binding.PAGED_DIRECT)
+    elif room and rows > 148:
+        assert form == binding.PAGED_UNPACKED
+    P.check(out, q, k, v, G, SCALE, lens, counts, form == binding.PAGED_UNPACKED)
     for b, m in enumerate(counts):
         assert (out[b, :, m:] == 7.0).all()
     if min(counts) == max(counts):
@@ -142,10 +161,11 @@ def test_rows_that_see_nothing(binding, n):
     """A sequence without tokens, and query rows in front of a sequence's first token, are zeros."""
     cache, table, k, v = filled(binding, 4, 2, [0, 3, 70], 16, 32, 2)
     q, _, _ = P.draw(3, 4, 2, n, 8)
-    out = cache.attention(0, q.cuda(), table.cuda(), ints([0, 3, 70]), SCALE)
-    assert cache.status() == 0
-    assert (out[0] == 0).all() and (out[1, :, :n - 3] == 0).all()
-    P.check(out, q, k, v, 32, SCALE, [0, 3, 70], [0, n, n])
+    for room in (0, 1 << 16):
+        out, rounded = attend(cache, q, wide(table, 16, room), [0, 3, 70])
+        assert cache.status() == 0 and rounded == (room > 0 and n == 70)
+        assert (out[0] == 0).all() and (out[1, :, :n - 3] == 0).all()
+        P.check(out, q, k, v, 32, SCALE, [0, 3, 70], [0, n, n], rounded)
 
 
 @pytest.mark.parametrize("size", [1e-30, 1e-6, 1e3, 1e20, 1e36])
@@ -159,8 +179,10 @@ def test_magnitudes(binding, size, n):
     v[1, :, 200:] = (v[1, :, 200:].float() * 64).to(torch.bfloat16)                  # values that grow on the way
     cache = binding.PagedCache(binding.make_paged_config(1, 7, 1, n_pages, page_tokens=32))
     cache.append(0, k.cuda(), v.cuda(), table.cuda(), ints([0, 0]), counts=ints(lens))
-    out = cache.attention(0, q.cuda(), table.cuda(), ints(lens), SCALE)
-    P.check(out, q, k, v, 32, SCALE, lens, [n, n])
+    for room in (0, 1 << 16):
+        out, rounded = attend(cache, q, wide(table, 32, room), lens)
+        assert rounded == (room > 0 and n == 40)
+        P.check(out, q, k, v, 32, SCALE, lens, [n, n], rounded)
 
 
 @pytest.mark.parametrize("n", [1, 3, 90])
@@ -175,60 +197,60 @@ def test_peaked_and_flat_softmax(binding, n):
     k[2] = k[2, :, :1]
     cache = binding.PagedCache(binding.make_paged_config(1, 4, 1, n_pages))
     cache.append(0, k.cuda(), v.cuda(), table.cuda(), ints([0] * 3), counts=ints(lens))
-    P.check(cache.attention(0, q.cuda(), table.cuda(), ints(lens), SCALE), q, k, v, 32, SCALE, lens, [n] * 3)
+    for room in (0, 1 << 16):
+        out, rounded = attend(cache, q, wide(table, 64, room), lens)
+        assert rounded == (room > 0 and n == 90)
+        P.check(out, q, k, v, 32, SCALE, lens, [n] * 3, rounded)
 
 
 @pytest.mark.parametrize("n", [2, 50])
-def test_nan_and_infinity_stay_where_they_are(binding, n):
-    """A NaN among the queries reaches its own row, an infinite value its group's channels of the rows that see it."""
-    cache, table, k, v = filled(binding, 8, 2, [200, 60], 32, 32, 21)
+@pytest.mark.parametrize("room", [0, 1 << 16])
+def test_nan_and_infinity_stay_where_they_are(binding, n, room):
+    """A NaN among the queries reaches its own row, an infinite value its group's channels of the rows that see it, an infinite key the rows that see it."""
+    lens = [200, 60]
+    cache, table, k, v = filled(binding, 8, 2, lens, 32, 32, 21)
+    where = wide(table, 32, room)
     q, _, _ = P.draw(2, 8, 2, n, 22)
-    ref = cache.attention(0, q.cuda(), table.cuda(), ints([200, 60]), SCALE)
+    ref, rounded = attend(cache, q, where, lens)
+    assert rounded == (room > 0 and n == 50)
     bad = q.clone()
     bad[0, 3, 0, 5] = float("nan")
-    out = cache.attention(0, bad.cuda(), table.cuda(), ints([200, 60]), SCALE)
+    out, _ = attend(cache, bad, where, lens)
     assert torch.isnan(out[0, 3, 0]).all()
     out[0, 3, 0] = ref[0, 3, 0]
     assert torch.equal(out, ref)
-    vi = v.clone()
-    vi[1, 1, 59, 40] = float("inf")                                        # the newest token of sequence 1: its second row sees it
-    cache.append(0, k.cuda(), vi.cuda(), table.cuda(), ints([0, 0]), counts=ints([200, 60]))
-    out = cache.attention(0, q.cuda(), table.cuda(), ints([200, 60]), SCALE)
+    vi, ki = v.clone(), k.clone()
+    vi[1, 1, 59, 40] = float("inf")                                        # the newest token of sequence 1: its last row sees it
+    cache.append(0, k.cuda(), vi.cuda(), table.cuda(), ints([0, 0]), counts=ints(lens))
+    out, _ = attend(cache, q, where, lens)
     assert not torch.isfinite(out[1, 4:, n - 1, 32:64]).any()
     out[1, 4:, n - 1, 32:64] = ref[1, 4:, n - 1, 32:64]
     assert torch.isfinite(out).all()
-    P.check(out, q, k, v, 32, SCALE, [200, 60], [n, n])
-    ki = k.clone()
+    P.check(out, q, k, v, 32, SCALE, lens, [n, n], rounded)
     ki[1, 0, 58, 7] = float("inf")                                         # a key: the last two rows of its heads
-    cache.append(0, ki.cuda(), v.cuda(), table.cuda(), ints([0, 0]), counts=ints([200, 60]))
-    out = cache.attention(0, q.cuda(), table.cuda(), ints([200, 60]), SCALE)
+    cache.append(0, ki.cuda(), v.cuda(), table.cuda(), ints([0, 0]), counts=ints(lens))
+    out, _ = attend(cache, q, where, lens)
     assert not torch.isfinite(out[1, :4, n - 2:]).any()
     out[1, :4, n - 2:] = ref[1, :4, n - 2:]
     assert torch.isfinite(out).all()
-    P.check(out, q, k, v, 32, SCALE, [200, 60], [n, n])
+    P.check(out, q, k, v, 32, SCALE, lens, [n, n], rounded)
 
 
-def test_bad_pages_of_many_rows(binding):
-    """The kernel for many query rows leaves out the tokens of pages that are none, too."""
+@pytest.mark.parametrize("room", [0, 1 << 16])
+def test_bad_pages_of_many_rows(binding, room):
+    """Tokens of pages that are none are left out, for many query rows too."""
     cache, table, k, v = filled(binding, 8, 1, [400, 300], 16, 32, 33)
     q, _, _ = P.draw(2, 8, 1, 30, 34)
-    wrong = table.clone()
-    wrong[0, 3], wrong[0, 9], wrong[1, 18] = -1, cache.cfg.n_pages, -7
-    out = cache.attention(0, q.cuda(), wrong.cuda(), ints([400, 300]), SCALE)
-    assert cache.status() == binding.DEV_BAD_PAGE
-    for b, gone in ((0, (3, 9)), (1, (18,))):
-        keep = [t for t in range([400, 300][b]) if t // 16 not in gone]
-        late = 30 if b == 0 else 17                                        # rows that see more or fewer of the page left out are compared up to there
-        at = 0 if b == 0 else 17
-        if b == 0:
-            P.check(out[:1], q[:1], k[:1, :, keep], v[:1, :, keep], 32, SCALE, [len(keep)], [late])
-        else:
-            x = q[1:, :, :at].contiguous()
-            # the first rows of sequence 1 (tokens 270 .. 286) do not reach page 18 (tokens 288 ..)
-            for i in range(at):
-                ref, tol = P.reference(x[0, :, i:i + 1], k[1, 0, :271 + i], v[1, 0, :271 + i], 32, SCALE, [271 + i], 240)
-                assert ((out[1, :, i:i + 1].double().cpu() - ref).abs() <= tol + 2.0 ** -24 * ref.abs()).all()
-    assert torch.isfinite(out).all()
+    table = wide(table, 16, room)
+    table[0, 3], table[0, 9], table[1, 18] = -1, cache.cfg.n_pages, -7
+    out, rounded = attend(cache, q, table, [400, 300])
+    assert rounded == (room > 0) and cache.status() == binding.DEV_BAD_PAGE and torch.isfinite(out).all()
+    keep = [t for t in range(400) if t // 16 not in (3, 9)]
+    P.check(out[:1], q[:1], k[:1, :, keep], v[:1, :, keep], 32, SCALE, [len(keep)], [30], rounded)
+    # sequence 1: page 18 is its last (tokens 288 .. 299); the 30 rows are tokens 270 .. 299
+    sees = [min(271 + i, 288) for i in range(30)]
+    ref, tol = P.reference(q[1], k[1, 0, :288], v[1, 0, :288], 32, SCALE, sees, rounded)
+    assert ((out[1].double().cpu() - ref).abs() <= tol + 2.0 ** -24 * ref.abs()).all()
 
 
 def test_bad_pages_and_lengths(binding):
@@ -339,7 +361,8 @@ def test_streams_and_two_calls_at_once(binding):
     assert all(torch.equal(a, b) for a, b in zip(outs, want))
 
 
-def test_prompt_in_chunks_then_steps(binding):
+@pytest.mark.parametrize("room", [0, 1 << 17])
+def test_prompt_in_chunks_then_steps(binding, room):
     """As a server runs it: tables, a prompt in two chunks from the projection's output, then decode steps, with a part of the head turned."""
     Hq, Hkv, B, T, n = 8, 2, 2, 130, 64
     q, k, v = P.draw(B, Hq, Hkv, T, 81)
@@ -348,7 +371,7 @@ def test_prompt_in_chunks_then_steps(binding):
     table, n_pages = P.pages_for([T, T], 32, 5)
     cache = binding.PagedCache(binding.make_paged_config(1, Hq, Hkv, n_pages, page_tokens=32, group_size=64))
     cache.mem[256:] = 0xFF
-    pages, lens = table.cuda(), ints([0, 0])
+    pages, lens = wide(table, 32, room).cuda(), ints([0, 0])
     qr, kr = (P.rotate(t, cos, sin, np.arange(T)[None].repeat(B, 0), True) for t in (q, k))
     at = 0
     while at < T:
@@ -358,7 +381,9 @@ def test_prompt_in_chunks_then_steps(binding):
         out = cache.step(0, xk, xv, xq, pages, lens, SCALE, cos=cd, sin=sd, interleaved=True, dtype=torch.bfloat16)
         lens.add_(m)
         at += m
-        P.check(out, qr[:, :, at - m:at].contiguous(), kr, v, 64, SCALE, [at, at], [m, m])
+        rounded = cache.last_attention() == binding.PAGED_UNPACKED
+        assert rounded == (room > 0 and m == n)
+        P.check(out, qr[:, :, at - m:at].contiguous(), kr, v, 64, SCALE, [at, at], [m, m], rounded)
     assert cache.status() == 0
 
 
