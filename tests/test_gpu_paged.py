@@ -342,6 +342,83 @@ def test_steps_are_append_then_attention(binding):
     assert lens.tolist() == [51, 32] and caches[0].status() == 0
 
 
+@pytest.mark.parametrize("counts_max,room", [(1, 1 << 10), (3, 1 << 10), (40, 1 << 15), (1, 0)])
+def test_many_sequences(binding, counts_max, room):
+    """More sequences than a warp has lanes, of very different length, some without tokens or queries."""
+    B, Hq, Hkv, page, G = 70, 8, 2, 16, 64
+    gen = torch.Generator().manual_seed(7)
+    lens = torch.randint(0, 130, (B,), generator=gen).tolist()
+    lens[3], lens[40], lens[69] = 400, 0, 390
+    counts = [min(t, c) for t, c in zip(lens, torch.randint(0, counts_max + 1, (B,), generator=gen).tolist())]
+    counts[3] = counts_max
+    cache, table, k, v = filled(binding, Hq, Hkv, lens, page, G, 71)
+    q, _, _ = P.draw(B, Hq, Hkv, counts_max, 72)
+    out, rounded = attend(cache, q, wide(table, page, room), lens, counts=ints(counts))
+    assert cache.status() == 0 and rounded == (counts_max == 40)
+    assert cache.last_attention() == (binding.PAGED_UNPACKED if rounded else binding.PAGED_PIECES if room else binding.PAGED_DIRECT)
+    P.check(out, q, k, v, G, SCALE, lens, counts, rounded)
+    for b, m in enumerate(counts):
+        assert (out[b, :, m:] == 0).all()
+
+
+def test_page_table_that_is_a_view_and_a_pool_beyond_four_gigabytes(binding):
+    """Pages at the end of a pool of 5 GB, in the second layer; the table's rows lie apart."""
+    Hq, Hkv, page, lens = 8, 8, 64, [150, 130]
+    n_pages = 31000
+    cache = binding.PagedCache(binding.make_paged_config(2, Hq, Hkv, n_pages, page_tokens=page))
+    assert cache.mem.numel() > 5e9
+    table = torch.tensor([[n_pages - 1, n_pages - 4, n_pages - 2], [n_pages - 3, n_pages - 7, n_pages - 5]], dtype=torch.int32)
+    room = torch.full((2, 40), -9, dtype=torch.int32, device="cuda")
+    pages = room[:, 5:8]
+    pages.copy_(table)
+    q, k, v = P.draw(2, Hq, Hkv, 150, 77)
+    cache.append(1, k.cuda(), v.cuda(), pages, ints([0, 0]), counts=ints(lens))
+    for n, columns in ((1, 3), (3, 20), (140, 3)):
+        x = q[:, :, :n].contiguous()
+        out = cache.attention(1, x.cuda(), room[:, 5:5 + columns], ints(lens), SCALE, counts=ints([n, min(n, 130)]))
+        P.check(out, x, k, v, 32, SCALE, lens, [n, min(n, 130)], cache.last_attention() == binding.PAGED_UNPACKED)
+    ko, vo = cache.read(1, pages, ints([149, 129]), 1)
+    for got, src in ((ko, k), (vo, v)):
+        for b, t in enumerate((149, 129)):
+            ref = torch.from_numpy(P.values(*P.quantized(src[b, :, t], 32)).astype(np.float32)).to(torch.bfloat16)
+            assert torch.equal(got[b, :, 0].cpu(), ref)
+    assert cache.status() == 0
+
+
+@pytest.mark.parametrize("n,room", [(1, 0), (1, 1 << 12), (3, 1 << 12), (60, 1 << 16)])
+def test_waits_that_run_out(binding, n, room):
+    """A staged copy that never completes: the call returns, the status says so, and the next call is as usual."""
+    lens = [700, 300] if room else [400, 300]
+    cache, table, k, v = filled(binding, 7, 1, lens, 64, 32, 81)
+    where = wide(table, 64, room)
+    q, _, _ = P.draw(2, 7, 1, n, 82)
+    want, _ = attend(cache, q, where, lens)
+    cache.test_arm_copy_timeout(16, 200)
+    attend(cache, q, where, lens)
+    assert cache.status() == binding.DEV_COPY_TIMEOUT
+    cache.test_arm_copy_timeout(0, 0)
+    cache.clear_status()
+    again, _ = attend(cache, q, where, lens)
+    assert torch.equal(again, want) and cache.status() == 0
+
+
+def test_long_segments_are_summed_in_parts(binding):
+    """More key tiles than are summed up in tensor memory at a time, in one thread block's range: one KV head, 600 tiles, many query rows."""
+    T, n = 76900, 256
+    table, n_pages = P.pages_for([T], 256, 5)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    k, v = (torch.empty((1, 1, T, 128), dtype=torch.bfloat16, device="cuda").normal_(generator=gen) for _ in range(2))
+    q = torch.empty((1, 8, 20000, 128), dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    cache = binding.PagedCache(binding.make_paged_config(1, 8, 1, n_pages, page_tokens=256))
+    cache.append(0, k, v, table.cuda(), ints([0]))
+    out = cache.attention(0, q, table.cuda(), ints([T]), SCALE)
+    assert cache.last_attention() == binding.PAGED_UNPACKED and cache.status() == 0
+    rows = [0, 1, 4097, 9999, 19998, 19999]
+    sees = [T - 20000 + i + 1 for i in rows]
+    ref, tol = P.reference(q[0][:, rows].cpu(), k[0, 0].cpu(), v[0, 0].cpu(), 32, SCALE, sees, True)
+    assert ((out[0][:, rows].double().cpu() - ref).abs() <= tol + 2.0 ** -24 * ref.abs()).all()
+
+
 def test_streams_and_two_calls_at_once(binding):
     """Calls on streams of their own with workspaces of their own do not disturb one another."""
     lens = [900, 1500]
