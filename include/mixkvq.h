@@ -389,9 +389,10 @@ int mixkvq_paged_destroy(mixkvq_paged* cache);
 /* Stores tokens: token i < counts[b] of sequence b becomes token lens[b] + i of the sequence (lens: tokens before the call).
  *   k_dev, v_dev [B, Hkv, n, 128], q_dev [B, Hq, n, 128] bf16 with strides_host [9] (q, k, v: batch, head, token; NULL: head-major) as for mixkvq_rope_axes.
  *   rotation: NULL (keys are stored as they are), or keys and queries turn on the way; its positions_dev may be NULL: a token turns by its place in
- *   its sequence.  A token with a negative position is none.
+ *   its sequence.  A token with a negative position is none: its slot stays as it was (and a step reckons with lens + counts all the same).
  *   q_dev, q_out_dev: both NULL, or the queries and where they go, rotated, head-major; q_out_dev may be q_dev itself where that is head-major.
- * Rows of q_out_dev behind a sequence's count are left as they are.  Two tokens of a call in the same slot (a page used twice) leave either. */
+ * Rows of q_out_dev behind a sequence's count are left as they are.  Two tokens of a call in the same slot (a page used twice) leave
+ * a mix of both. */
 int mixkvq_paged_append(mixkvq_paged* cache, int layer, const mixkvq_paged_sequences* seqs, const void* k_dev, const void* v_dev, const void* q_dev,
                         const int64_t* strides_host, const mixkvq_rotation* rotation, void* q_out_dev, void* stream);
 /* The values that tokens lens[b] .. lens[b] + counts[b] - 1 of every sequence are held as (Eq. 3, rounded to bf16): k_out_dev, v_out_dev [B, Hkv, n, 128] bf16.  Other rows
@@ -400,10 +401,13 @@ int mixkvq_paged_read(mixkvq_paged* cache, int layer, const mixkvq_paged_sequenc
 /* Eq. 1 over the pages: the newest counts[b] tokens of sequence b, which has lens[b] tokens, these included; query row i sees tokens 0 .. lens[b] - counts[b] + i.
  *   q_dev [B, Hq, n, 128] bf16 (rotated), out_dev [B, Hq, n, 128] of out_type (MIXKVQ_OUT_*), rounded once.
  * A row that sees no token is zeros; rows behind a sequence's count are left as they are.  Nothing is read of tokens that no row sees: freed pages and the rest of a last
- * page may hold anything.  softmax_scale > 0 and finite. */
+ * page may hold anything.  softmax_scale > 0 and finite.
+ * Logits and sums are fp32; weights are fp16 numbers (2^-11), and calls that unpack the pages (MIXKVQ_PAGED_UNPACKED) round keys and values to fp16 once more.  Inputs of any
+ * magnitude are scaled by powers of two on the way.  What is not finite in the pages or a query reaches the rows that see it only. */
 int mixkvq_paged_attention(mixkvq_paged* cache, int layer, const mixkvq_paged_sequences* seqs, const void* q_dev, void* out_dev, int out_type, float softmax_scale,
                            void* workspace_dev, size_t workspace_bytes, void* stream);
-/* mixkvq_paged_append, then mixkvq_paged_attention of the tokens appended: a decode step, or a chunk of a prompt.  lens: tokens before the call. */
+/* mixkvq_paged_append, then mixkvq_paged_attention of the tokens appended: a decode step, or a chunk of a prompt.  lens: tokens before the call.
+ * q_out_dev is written (as the append does) and may be q_dev; out_dev and the workspace lie over none of the inputs. */
 int mixkvq_paged_step(mixkvq_paged* cache, int layer, const mixkvq_paged_sequences* seqs, const void* k_dev, const void* v_dev, const void* q_dev,
                       const int64_t* strides_host, const mixkvq_rotation* rotation, void* q_out_dev, void* out_dev, int out_type, float softmax_scale,
                       void* workspace_dev, size_t workspace_bytes, void* stream);

@@ -20,9 +20,11 @@ struct Ranges {
   void read(const void* p, size_t bytes) { add(p, bytes, false); }
   void write(const void* p, size_t bytes) { add(p, bytes, true); }
   bool clash() const {
-    for (int i = 0; i < n; ++i)
+    for (int i = 0; i < n; ++i) {
+      if (!all[i].written) continue;
       for (int j = 0; j < n; ++j)
-        if (i != j && all[i].written && all[i].lo < all[j].hi && all[j].lo < all[i].hi) return true;
+        if (i != j && all[i].lo < all[j].hi && all[j].lo < all[i].hi) return true;
+    }
     return false;
   }
   // whether anything but the range itself lies over it

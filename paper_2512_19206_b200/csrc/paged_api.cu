@@ -28,6 +28,8 @@ int check_config(const mixkvq_paged_config* c) {
   if (c->head_dim != kD || c->n_q_heads / c->n_kv_heads > 8) return MIXKVQ_E_UNSUPPORTED;
   if (c->group_size != 32 && c->group_size != 64 && c->group_size != 128) return MIXKVQ_E_UNSUPPORTED;
   if (c->page_tokens < 16 || c->page_tokens > 256 || (c->page_tokens & (c->page_tokens - 1))) return MIXKVQ_E_UNSUPPORTED;
+  // (sizes fit 64 bits with room to spare)
+  if ((double)c->n_layers * c->n_pages * c->n_kv_heads * c->page_tokens / kPagedTile * paged_tile_bytes(c->group_size) > 0x1p60) return MIXKVQ_E_UNSUPPORTED;
   return MIXKVQ_OK;
 }
 
@@ -74,13 +76,13 @@ void add_sequences(const mixkvq_paged* h, const mixkvq_paged_sequences* s, Range
 }
 
 int plan_append(const mixkvq_paged* h, int layer, const mixkvq_paged_sequences* s, const void* k_dev, const void* v_dev, const void* q_dev, const int64_t* strides_host,
-                const mixkvq_rotation* rotation, void* q_out_dev, PagedAppend* a) {
+                const mixkvq_rotation* rotation, void* q_out_dev, PagedAppend* a, Ranges* ranges) {
   *a = PagedAppend{};
   const int rc = check_sequences(h, layer, s, &a->view);
   if (rc != MIXKVQ_OK) return rc;
   if (!k_dev || !v_dev || (q_dev == nullptr) != (q_out_dev == nullptr)) return MIXKVQ_E_INVALID_ARG;
   const int B = s->batch, n = s->n_tokens;
-  Ranges r;
+  Ranges& r = *ranges;
   const void* in[3] = {q_dev, k_dev, v_dev};
   RopeTensor* t[3] = {&a->tq, &a->tk, &a->tv};
   for (int i = 0; i < 3; ++i) {
@@ -104,8 +106,9 @@ int plan_append(const mixkvq_paged* h, int layer, const mixkvq_paged_sequences* 
   return MIXKVQ_OK;
 }
 
+// ranges: empty, or those of the append that the call begins with, which writes q_dev
 int plan_attention(const mixkvq_paged* h, int layer, const mixkvq_paged_sequences* s, const void* q_dev, const void* out_dev, int out_type, float softmax_scale,
-                   const void* workspace_dev, size_t workspace_bytes, bool q_written, PagedAttention* a) {
+                   const void* workspace_dev, size_t workspace_bytes, PagedAttention* a, Ranges* ranges) {
   *a = PagedAttention{};
   const int rc = check_sequences(h, layer, s, &a->view);
   if (rc != MIXKVQ_OK) return rc;
@@ -116,11 +119,14 @@ int plan_attention(const mixkvq_paged* h, int layer, const mixkvq_paged_sequence
   const size_t need = paged_workspace_bytes(h->cfg.n_kv_heads, h->g, s->batch, s->n_tokens, (long long)s->max_pages * h->cfg.page_tokens);
   if (workspace_bytes < need) return MIXKVQ_E_BUFFER_TOO_SMALL;
   const size_t rows = (size_t)s->batch * h->cfg.n_q_heads * s->n_tokens * kD;
-  Ranges r;
+  Ranges& r = *ranges;
+  const bool alone = r.n == 0;
   r.write(out_dev, rows * (out_type == MIXKVQ_OUT_BF16 ? 2 : 4));
   r.write(workspace_dev, need);
-  if (!q_written) r.read(q_dev, 2 * rows);
-  add_sequences(h, s, &r);
+  if (alone) {
+    r.read(q_dev, 2 * rows);
+    add_sequences(h, s, &r);
+  }
   if (r.clash()) return MIXKVQ_E_INVALID_ARG;
   a->q = q_dev;
   a->out = const_cast<void*>(out_dev);
@@ -238,7 +244,8 @@ int mixkvq_paged_destroy(mixkvq_paged* cache) {
 int mixkvq_paged_append(mixkvq_paged* cache, int layer, const mixkvq_paged_sequences* seqs, const void* k_dev, const void* v_dev, const void* q_dev,
                         const int64_t* strides_host, const mixkvq_rotation* rotation, void* q_out_dev, void* stream) {
   PagedAppend a;
-  const int rc = plan_append(cache, layer, seqs, k_dev, v_dev, q_dev, strides_host, rotation, q_out_dev, &a);
+  Ranges r;
+  const int rc = plan_append(cache, layer, seqs, k_dev, v_dev, q_dev, strides_host, rotation, q_out_dev, &a, &r);
   return rc != MIXKVQ_OK ? rc : run_append(cache, a, static_cast<cudaStream_t>(stream));
 }
 
@@ -264,7 +271,8 @@ int mixkvq_paged_read(mixkvq_paged* cache, int layer, const mixkvq_paged_sequenc
 int mixkvq_paged_attention(mixkvq_paged* cache, int layer, const mixkvq_paged_sequences* seqs, const void* q_dev, void* out_dev, int out_type, float softmax_scale,
                            void* workspace_dev, size_t workspace_bytes, void* stream) {
   PagedAttention a;
-  const int rc = plan_attention(cache, layer, seqs, q_dev, out_dev, out_type, softmax_scale, workspace_dev, workspace_bytes, false, &a);
+  Ranges r;
+  const int rc = plan_attention(cache, layer, seqs, q_dev, out_dev, out_type, softmax_scale, workspace_dev, workspace_bytes, &a, &r);
   return rc != MIXKVQ_OK ? rc : run_attention(cache, a, static_cast<cudaStream_t>(stream));
 }
 
@@ -274,9 +282,10 @@ int mixkvq_paged_step(mixkvq_paged* cache, int layer, const mixkvq_paged_sequenc
   PagedAppend a;
   PagedAttention b;
   if (!q_dev) return MIXKVQ_E_INVALID_ARG;
-  int rc = plan_append(cache, layer, seqs, k_dev, v_dev, q_dev, strides_host, rotation, q_out_dev, &a);
+  Ranges r;
+  int rc = plan_append(cache, layer, seqs, k_dev, v_dev, q_dev, strides_host, rotation, q_out_dev, &a, &r);
   if (rc != MIXKVQ_OK) return rc;
-  rc = plan_attention(cache, layer, seqs, q_out_dev, out_dev, out_type, softmax_scale, workspace_dev, workspace_bytes, false, &b);
+  rc = plan_attention(cache, layer, seqs, q_out_dev, out_dev, out_type, softmax_scale, workspace_dev, workspace_bytes, &b, &r);
   if (rc != MIXKVQ_OK) return rc;
   b.view.add_counts = 1;
   rc = run_append(cache, a, static_cast<cudaStream_t>(stream));

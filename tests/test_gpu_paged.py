@@ -484,3 +484,17 @@ def test_refusals(binding):
             call()
         assert e.value.code == code
     assert cache.launch_count() == before and cache.status() == 0
+
+
+def test_a_step_writes_over_none_of_its_inputs(binding):
+    Hq, Hkv, n = 4, 2, 3
+    cache = binding.PagedCache(binding.make_paged_config(1, Hq, Hkv, 4, page_tokens=16))
+    pages, lens = ints([[0, 1], [2, 3]]), ints([0, 0])
+    q, k, v, out = (torch.zeros((2, h, n, 128), dtype=torch.bfloat16, device="cuda") for h in (Hq, Hkv, Hkv, Hq))
+    cos = torch.ones((9, 64), device="cuda")
+    before = cache.launch_count()
+    for over in (dict(k=out[:, :Hkv]), dict(v=out[:, Hkv:]), dict(q=out, q_out=q), dict(q=out, q_out=out), dict(cos=out.view(-1).view(torch.float32)[:9 * 64].view(9, 64))):
+        with pytest.raises(binding.MixKVQError) as e:
+            cache.step(0, **{**dict(k=k, v=v, q=q, cos=cos, sin=cos), **over}, pages=pages, lens=lens, scale=1.0, out=out)
+        assert e.value.code == -1
+    assert cache.launch_count() == before and cache.status() == 0

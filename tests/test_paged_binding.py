@@ -188,3 +188,12 @@ def test_tables_refusals():
     for bad in (dict(scaling="other"), dict(n_positions=0), dict(attention_factor=0.0), dict(out=(torch.zeros((9, 64)), torch.zeros((9, 64))))):
         with pytest.raises(ValueError):
             binding.rope_tables(**{"n_positions": 9, "device": "cpu", **bad})
+
+
+def test_sizes_beyond_64_bits_are_refused():
+    most, n = (1 << 31) - 1, C.c_size_t()
+    for shape, code in (((most, 8, 8, 4), 0), ((most, 8, 8, most), -2), ((1, most, most, most), -2), ((1, 8, 8, most), 0)):
+        cfg = binding.make_paged_config(*shape)
+        assert binding.lib().mixkvq_paged_bytes(C.byref(cfg), C.byref(n)) == code
+        if code == 0:
+            assert n.value == 256 + shape[0] * shape[2] * shape[3] * (cfg.page_tokens // 16) * (2048 + 32 * 512 // cfg.group_size)
