@@ -498,3 +498,20 @@ def test_a_step_writes_over_none_of_its_inputs(binding):
             cache.step(0, **{**dict(k=k, v=v, q=q, cos=cos, sin=cos), **over}, pages=pages, lens=lens, scale=1.0, out=out)
         assert e.value.code == -1
     assert cache.launch_count() == before and cache.status() == 0
+
+
+@pytest.mark.parametrize("n,room", [(1, 1 << 10), (4, 1 << 10), (30, 1 << 12), (1, 0)])
+def test_as_many_sequences_as_there_may_be(binding, n, room):
+    """4096 sequences: every kernel's table of positions at its largest.  A sample of them against 64 bits."""
+    B, Hq, Hkv, page, G = 4096, 8, 1, 16, 128
+    lens = torch.randint(n, 60, (B,), generator=torch.Generator().manual_seed(8)).tolist()
+    lens[17], lens[B - 1] = 130, 120
+    cache, table, k, v = filled(binding, Hq, Hkv, lens, page, G, 81)
+    q, _, _ = P.draw(B, Hq, Hkv, n, 82)
+    table = wide(table, page, room)
+    out, rounded = attend(cache, q, table, lens)
+    assert cache.status() == 0 and rounded == (n == 30)
+    some = [0, 17, 31, 32, 2047, 4000, B - 1]
+    P.check(out[some], q[some], k[some], v[some], G, SCALE, [lens[b] for b in some], [n] * len(some), rounded)
+    with pytest.raises(binding.MixKVQError):
+        cache.attention(0, torch.cat([q, q[:1]]).cuda(), torch.cat([table, table[:1]]).cuda(), ints(lens + lens[:1]), SCALE)
