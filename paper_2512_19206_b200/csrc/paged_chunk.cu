@@ -502,6 +502,11 @@ attend_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ 
     }
     return !dead;
   };
+  // The same for a whole warp: all of its lanes go on or none, as the instructions on tensor memory and the votes behind a wait are the warp's.
+  auto wait_warp = [&](int i, uint32_t parity) {
+    dead = __all_sync(0xffffffffu, wait(i, parity)) == 0;
+    return !dead;
+  };
   auto two_groups = [&](const Walk& w) { return w.r * kRows + kTile < w.rows; };
 
   if (warp >= 8) {
@@ -659,7 +664,7 @@ attend_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ 
           const float4 head_of = *reinterpret_cast<const float4*>(heads + j);       // (under way while the thread waits)
           const uint32_t flags = __float_as_uint(head_of.z);
           const bool masked = (j + 1) * kTile > warp_sees || flags != 0xFFu, fresh = (j - s.j0) % kFlush == 0;
-          if (!wait(kSFull + g, t & 1)) break;
+          if (!wait_warp(kSFull + g, t & 1)) break;
           tc_fence_after();
           if (fresh && j > s.j0) flush_row(o_addr, to, sums);
           softmax_tile(s_addr, o_addr, masked, sees - 1 - j * kTile, flags, fresh, factor * head_of.x, head_of.y, sums, bar(kPHalf + g));
@@ -669,7 +674,7 @@ attend_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ 
           mbar_arrive(bar(kPReady + g));
           ++t;
         }
-        if (!dead && wait(kDone + g, segs & 1)) {
+        if (!dead && wait_warp(kDone + g, segs & 1)) {
           tc_fence_after();
           if (sums.flushed) flush_row(o_addr, to, sums);
           const float inv = whole ? (sums.denom == 0.f ? 0.f : pow2i(kDown) / sums.denom) : 1.f;

@@ -1,0 +1,56 @@
+"""GPU tests of the paged 4-bit cache at the edges of its inputs: zeros, magnitudes, infinities beside large values, NaNs that are appended, rows that a call leaves out."""
+import numpy as np
+import pytest
+import torch
+
+import paged_util as P
+
+pytestmark = pytest.mark.gpu
+SCALE = 128 ** -0.5
+UNPACKED = 4
+
+
+@pytest.fixture(scope="module")
+def binding():
+    assert torch.cuda.is_available(), "GPU tests need a CUDA device"
+    from paper_2512_19206_b200 import build
+    build.build()
+    from paper_2512_19206_b200 import binding as b
+    b.lib()
+    return b
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def wide(table, page, room):
+    more = max(0, room // page - table.shape[1])
+    return torch.cat([table, torch.full((table.shape[0], more), -1, dtype=torch.int32)], 1) if more else table
+
+
+def held(binding, Hq, Hkv, k, v, lens, page=32, G=32):
+    """A cache that holds lens[b] tokens of k, v (CPU), and its page table (CPU)."""
+    table, n_pages = P.pages_for(lens, page, 3)
+    cache = binding.PagedCache(binding.make_paged_config(1, Hq, Hkv, n_pages, page_tokens=page, group_size=G))
+    cache.mem[256:] = 0xFF
+    cache.append(0, k.cuda(), v.cuda(), table.cuda(), ints([0] * len(lens)), counts=ints(lens))
+    return cache, table
+
+
+@pytest.mark.parametrize("Hq,Hkv,n,lens,polls", [(7, 1, 60, [700, 300], 100), (28, 4, 300, [5000, 900, 301], 300), (8, 1, 1000, [40000], 1000)])
+def test_time_outs_of_many_rows(binding, Hq, Hkv, n, lens, polls):
+    """Copies that never arrive in every thread block of the kernel for many rows: the call ends, the status says so, and the next call is as usual."""
+    q, k, v = P.draw(len(lens), Hq, Hkv, max(lens), 83)
+    q = q[:, :, :n].contiguous().cuda()
+    cache, table = held(binding, Hq, Hkv, k, v, lens, page=64)
+    pages = wide(table, 64, 1 << 16).cuda()
+    want = cache.attention(0, q, pages, ints(lens), SCALE)
+    assert cache.last_attention() == UNPACKED
+    for _ in range(3):
+        cache.test_arm_copy_timeout(16, polls)
+        cache.attention(0, q, pages, ints(lens), SCALE)
+        assert cache.status() == binding.DEV_COPY_TIMEOUT
+        cache.test_arm_copy_timeout(0, 0)
+        cache.clear_status()
+        assert torch.equal(cache.attention(0, q, pages, ints(lens), SCALE), want) and cache.status() == 0
