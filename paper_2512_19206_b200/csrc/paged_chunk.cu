@@ -615,7 +615,7 @@ attend_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ 
     const uint32_t lane_base = tbase + ((uint32_t)((warp & 3) * 32) << 16), s_addr = lane_base + 128 * g, o_addr = lane_base + 256 + 128 * g;
     const bool wide = (reinterpret_cast<uintptr_t>(a.out) & 31u) == 0;
     uint32_t t = 0, segs = 0;                            // of this group
-    while (walk.pos < walk.end && !dead) {
+    while (walk.pos < walk.end) {                        // (a warp whose wait has run out has nothing to add, and says so in every place that is read later)
       const Segment s = take(v, walk);
       if (s.j1 > s.j0 && (g == 0 || two_groups(walk))) {
         const int x = walk.r * kRows + g * kTile + (tid & 127);
@@ -624,8 +624,8 @@ attend_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ 
         const int xi = min(x, walk.rows - 1) / v.g, head = x - xi * v.g;
         const int sees = min(walk.len, max(0, walk.len - walk.count + xi + 1));
         const size_t row = ((size_t)(plan.b0 + walk.i) * v.Hq + (size_t)(plan.h0 + walk.h) * v.g + (mine ? head : 0)) * v.n + xi;
-        float factor;
-        {
+        float factor = 0.f;
+        if (!dead) {
           uint4 w[16];
           const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + row * kD);
 #pragma unroll
@@ -660,7 +660,7 @@ attend_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ 
         // the thread block's first part of an item and its last have a place each; a whole item's sums in between take the second one
         float* to = plan.parts + ((size_t)(2 * blockIdx.x + (s.j0 == 0 ? 1 : 0)) * kRows + g * kTile + (tid & 127)) * kPartFloats;
 #pragma unroll 1
-        for (int j = s.j0; j < s.j1; ++j) {
+        for (int j = s.j0; j < s.j1 && !dead; ++j) {
           const float4 head_of = *reinterpret_cast<const float4*>(heads + j);       // (under way while the thread waits)
           const uint32_t flags = __float_as_uint(head_of.z);
           const bool masked = (j + 1) * kTile > warp_sees || flags != 0xFFu, fresh = (j - s.j0) % kFlush == 0;
@@ -674,51 +674,60 @@ attend_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ 
           mbar_arrive(bar(kPReady + g));
           ++t;
         }
-        if (!dead && wait_warp(kDone + g, segs & 1)) {
+        const bool done = !dead && wait_warp(kDone + g, segs & 1);
+        if (done) {
           tc_fence_after();
           if (sums.flushed) flush_row(o_addr, to, sums);
-          const float inv = whole ? (sums.denom == 0.f ? 0.f : pow2i(kDown) / sums.denom) : 1.f;
+        } else {
+          sums = Row{-1e30f, 0.f, 0.f, false};
+          lost = 0;
+        }
+        const float inv = whole ? (sums.denom == 0.f ? 0.f : pow2i(kDown) / sums.denom) : 1.f;
 #pragma unroll 1
-          for (int q = 0; q < 4; ++q) {                  // 32 channels
-            float y[32];
-            {
-              uint32_t x[32];
+        for (int q = 0; q < 4; ++q) {                  // 32 channels
+          float y[32];
+          {
+            uint32_t x[32];
+            if (done) {
               tmem_ld32(o_addr + 32 * q, x);
               tmem_wait32(x);
-              const float f = lost >> q & 1u || lost & 16u ? NAN : inv;
+            } else {
 #pragma unroll
-              for (int d = 0; d < 32; ++d) y[d] = (sums.flushed ? to[32 * q + d] : __uint_as_float(x[d]) * sums.v_scale) * (whole ? f : 1.f);
+              for (int d = 0; d < 32; ++d) x[d] = 0u;
             }
-            if (!whole) {
-              if (!sums.flushed) {
+            const float f = lost >> q & 1u || lost & 16u ? NAN : inv;
 #pragma unroll
-                for (int d = 0; d < 32; d += 4) *reinterpret_cast<float4*>(to + 32 * q + d) = make_float4(y[d], y[d + 1], y[d + 2], y[d + 3]);
-              }
-            } else if (mine && a.out_bf16) {
-              char* out = static_cast<char*>(a.out) + row * (2 * kD) + 64 * q;
-#pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                uint32_t z[8];
-#pragma unroll
-                for (int d = 0; d < 8; ++d) z[d] = bf16_pair(y[16 * k + 2 * d], y[16 * k + 2 * d + 1]);
-                store32(out + 32 * k, z, wide);
-              }
-            } else if (mine) {
-              char* out = static_cast<char*>(a.out) + row * (4 * kD) + 128 * q;
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                uint32_t z[8];
-#pragma unroll
-                for (int d = 0; d < 8; ++d) z[d] = __float_as_uint(y[8 * k + d]);
-                store32(out + 32 * k, z, wide);
-              }
-            }
+            for (int d = 0; d < 32; ++d) y[d] = (sums.flushed ? to[32 * q + d] : __uint_as_float(x[d]) * sums.v_scale) * (whole ? f : 1.f);
           }
           if (!whole) {
-            *reinterpret_cast<float4*>(to + kD) = make_float4(sums.ref, sums.denom, __uint_as_float(lost), 0.f);
-            if (tid == 0 && s.j0 == 0)
-              plan.broken[blockIdx.x] = Broken{walk.i, walk.h, walk.r, owner_of(split_begin(total, parts, blockIdx.x + 1) + (s.tiles - s.j1) - 1, total, parts)};
+            if (!sums.flushed) {
+#pragma unroll
+              for (int d = 0; d < 32; d += 4) *reinterpret_cast<float4*>(to + 32 * q + d) = make_float4(y[d], y[d + 1], y[d + 2], y[d + 3]);
+            }
+          } else if (mine && a.out_bf16) {
+            char* out = static_cast<char*>(a.out) + row * (2 * kD) + 64 * q;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              uint32_t z[8];
+#pragma unroll
+              for (int d = 0; d < 8; ++d) z[d] = bf16_pair(y[16 * k + 2 * d], y[16 * k + 2 * d + 1]);
+              store32(out + 32 * k, z, wide);
+            }
+          } else if (mine) {
+            char* out = static_cast<char*>(a.out) + row * (4 * kD) + 128 * q;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              uint32_t z[8];
+#pragma unroll
+              for (int d = 0; d < 8; ++d) z[d] = __float_as_uint(y[8 * k + d]);
+              store32(out + 32 * k, z, wide);
+            }
           }
+        }
+        if (!whole) {
+          *reinterpret_cast<float4*>(to + kD) = make_float4(sums.ref, sums.denom, __uint_as_float(lost), 0.f);
+          if (tid == 0 && s.j0 == 0)
+            plan.broken[blockIdx.x] = Broken{walk.i, walk.h, walk.r, owner_of(split_begin(total, parts, blockIdx.x + 1) + (s.tiles - s.j1) - 1, total, parts)};
         }
         ++segs;
       }

@@ -54,3 +54,23 @@ def test_time_outs_of_many_rows(binding, Hq, Hkv, n, lens, polls):
         cache.test_arm_copy_timeout(0, 0)
         cache.clear_status()
         assert torch.equal(cache.attention(0, q, pages, ints(lens), SCALE), want) and cache.status() == 0
+
+
+@pytest.mark.parametrize("n,lens,room,dtype", [(1, [400, 300], 0, torch.float32), (1, [700, 300], 1 << 12, torch.bfloat16), (3, [700, 300], 1 << 12, torch.float32),
+                                               (60, [700, 300], 1 << 16, torch.float32), (300, [5000, 900], 1 << 16, torch.bfloat16)])
+def test_calls_whose_copies_never_arrive_are_zeros(binding, n, lens, room, dtype):
+    """Where no warp contributed the output is 0: nothing of the workspace's former contents, nothing left unwritten."""
+    q, k, v = P.draw(2, 28, 4, max(lens), 85)
+    q = q[:, :, :n].contiguous().cuda()
+    cache, table = held(binding, 28, 4, k, v, lens, page=64)
+    pages = wide(table, 64, room).cuda()
+    space = torch.full((cache.workspace_bytes(2, n, pages.shape[1]),), 0xFF, dtype=torch.uint8, device="cuda")
+    out = torch.full(q.shape, 7.0, dtype=dtype, device="cuda")
+    cache.test_arm_copy_timeout(16, 200)
+    cache.attention(0, q, pages, ints(lens), SCALE, out=out, workspace=space)
+    assert cache.status() == binding.DEV_COPY_TIMEOUT and (cache.last_attention() == UNPACKED) == (n >= 60)
+    assert (out == 0).all()
+    cache.test_arm_copy_timeout(0, 0)
+    cache.clear_status()
+    cache.attention(0, q, pages, ints(lens), SCALE, out=out, workspace=space)
+    assert cache.status() == 0 and (out.flatten(0, 2).float().abs().amax(1) > 0).all()
