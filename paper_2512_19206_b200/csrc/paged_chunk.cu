@@ -42,6 +42,7 @@ constexpr int kShift = 4;                        // the weight of a logit equal 
 constexpr float kRise = 8.f;                     // a logit this much above the reference raises it: weights are 2^12 at most
 constexpr int kSlack = 3;                        // powers of two that a value tile's scale may be above that of O: 2^15 at most
 constexpr int kFlush = 512;                      // tiles summed up in tensor memory
+constexpr float kLeast = 0x1p-120f;              // the factor of the logits is no less: sums of products are below 2^38, so smaller ones give the same weights, and -infinity stays what it is
 constexpr int kDown = 30;                        // and sums of values 2^-kDown as large: they keep off fp32's end
 
 struct __align__(16) TileHead {
@@ -667,7 +668,7 @@ attend_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ 
           if (!wait_warp(kSFull + g, t & 1)) break;
           tc_fence_after();
           if (fresh && j > s.j0) flush_row(o_addr, to, sums);
-          softmax_tile(s_addr, o_addr, masked, sees - 1 - j * kTile, flags, fresh, factor * head_of.x, head_of.y, sums, bar(kPHalf + g));
+          softmax_tile(s_addr, o_addr, masked, sees - 1 - j * kTile, flags, fresh, fmaxf(factor * head_of.x, kLeast), head_of.y, sums, bar(kPHalf + g));
           if (flags >> 8 & 1u)
             for (int k = 0; k < kTile && j * kTile + k < sees; ++k) lost |= heads[j].lost[k];
           tc_fence_before();

@@ -38,6 +38,28 @@ def held(binding, Hq, Hkv, k, v, lens, page=32, G=32):
     return cache, table
 
 
+@pytest.mark.parametrize("n", [1, 5, 90])
+@pytest.mark.parametrize("room", [0, 1 << 16])
+@pytest.mark.parametrize("what", ["queries", "keys", "both", "queries, small keys", "keys, small queries", "one tile's keys"])
+def test_zeros(binding, n, room, what):
+    """Equal logits: the mean of the values seen, whatever factor of the logits a row and a tile of zeros come to."""
+    lens, counts = [300, 131], [n, n]
+    q, k, v = P.draw(2, 8, 2, 300, 17)
+    q = q[:, :, :n].contiguous()
+    if what in ("queries", "both", "queries, small keys"):
+        q.zero_()
+    if what in ("keys", "both", "keys, small queries"):
+        k.zero_()
+    if what == "one tile's keys":
+        k[:, :, 128:] = 0
+    if "small" in what:
+        q, k = ((x.float() * 2.0 ** -9).to(torch.bfloat16) for x in (q, k))
+    cache, table = held(binding, 8, 2, k, v, lens)
+    out = cache.attention(0, q.cuda(), wide(table, 32, room).cuda(), ints(lens), SCALE)
+    assert cache.status() == 0 and (cache.last_attention() == UNPACKED) == (room > 0 and n == 90)
+    P.check(out, q, k, v, 32, SCALE, lens, counts, cache.last_attention() == UNPACKED)
+
+
 @pytest.mark.parametrize("Hq,Hkv,n,lens,polls", [(7, 1, 60, [700, 300], 100), (28, 4, 300, [5000, 900, 301], 300), (8, 1, 1000, [40000], 1000)])
 def test_time_outs_of_many_rows(binding, Hq, Hkv, n, lens, polls):
     """Copies that never arrive in every thread block of the kernel for many rows: the call ends, the status says so, and the next call is as usual."""
