@@ -284,7 +284,7 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
     uint32_t qb[kQueriesInRegisters ? kNT : 1][4][4];                      // word j: {0,4} {2,6} {1,5}/16 {3,7}/16
     uint32_t qz[kNT][3];                         // sums of the row's groups as three bf16 terms each: {sum of group t, 0}
     float qscale[kNT][2];
-    int sees[kNT][2];
+    int sees[kNT][2], fewest = st.len;
 #pragma unroll
     for (int nt = 0; nt < kNT; ++nt) {
       const uint4(&w)[4] = qw[nt];
@@ -337,13 +337,17 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const int from = 4 * (2 * t + c);
-        qscale[nt][c] = a.scale_log2e * (pow2i(-__shfl_sync(0xffffffffu, e, from)) * 16777216.f);
+        // what a sum is multiplied with.  Where fp32 has no room for the 2^24 of the codes (queries from 2^117 on or so) it is left out and the sign says so: such sums
+        // are brought up first, in masked units, which all units of the piece then are.  (e is -114 for rows that are not finite; their results are not either.)
+        const int e_row = __shfl_sync(0xffffffffu, e, from);
+        const float back = a.scale_log2e * pow2i(-e_row);
+        qscale[nt][c] = back >= 0x1p103f && e_row > -114 ? -back : back * 16777216.f;
         const int x = st.row0 + 8 * nt + 2 * t + c;
         // (rows that are none are computed like the others and written nowhere)
         sees[nt][c] = x < st.count * v.g ? max(0, st.len - st.count + over_g(x) + 1) : st.len;
+        if (qscale[nt][c] < 0.f) fewest = 0;
       }
     }
-    int fewest = st.len;
 #pragma unroll
     for (int nt = 0; nt < kNT; ++nt) fewest = min(fewest, min(sees[nt][0], sees[nt][1]));
     fewest = __reduce_min_sync(0xffffffffu, fewest);
@@ -421,8 +425,11 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
         for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            x[m][nt][k] = fmaf(sum[nt][k], qscale[nt][k & 1], zs[nt][k]);
-            if constexpr (kMask) {
+            const float by = qscale[nt][k & 1];
+            if constexpr (!kMask) {
+              x[m][nt][k] = fmaf(sum[nt][k], by, zs[nt][k]);
+            } else {
+              x[m][nt][k] = fmaf(by < 0.f ? sum[nt][k] * 16777216.f : sum[nt][k], fabsf(by), zs[nt][k]);
               if (tok + 16 * m + pi + (k < 2 ? 0 : 8) >= sees[nt][k & 1] || !(there >> m & 1)) x[m][nt][k] = -INFINITY;
             }
           }

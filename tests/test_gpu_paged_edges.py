@@ -60,6 +60,24 @@ def test_zeros(binding, n, room, what):
     P.check(out, q, k, v, 32, SCALE, lens, counts, cache.last_attention() == UNPACKED)
 
 
+@pytest.mark.parametrize("size", [1e34, 1e35, 1e36])
+@pytest.mark.parametrize("n", [1, 4, 40])
+@pytest.mark.parametrize("which", ["all", "one"])
+def test_queries_near_the_end_of_the_range(binding, size, n, which):
+    """Queries as large as bf16 allows before a key: logits that are ordinary, as the keys are as small; or one such row beside ordinary ones."""
+    lens = [90, 400]
+    q, k, v = P.draw(2, 7, 1, max(lens), 6)
+    k = (k.float() / size).to(torch.bfloat16)
+    big = (q[:, :, :n].float() * size).to(torch.bfloat16)
+    q = big if which == "all" else torch.cat([q[:, :3, :n], big[:, 3:4], q[:, 4:, :n]], 1)
+    cache, table = held(binding, 7, 1, k, v, lens)
+    for room in (0, 1 << 16):
+        out = cache.attention(0, q.contiguous().cuda(), wide(table, 32, room).cuda(), ints(lens), SCALE)
+        rounded = cache.last_attention() == UNPACKED
+        assert rounded == (room > 0 and n == 40)
+        P.check(out, q, k, v, 32, SCALE, lens, [n, n], rounded)
+
+
 @pytest.mark.parametrize("Hq,Hkv,n,lens,polls", [(7, 1, 60, [700, 300], 100), (28, 4, 300, [5000, 900, 301], 300), (8, 1, 1000, [40000], 1000)])
 def test_time_outs_of_many_rows(binding, Hq, Hkv, n, lens, polls):
     """Copies that never arrive in every thread block of the kernel for many rows: the call ends, the status says so, and the next call is as usual."""
