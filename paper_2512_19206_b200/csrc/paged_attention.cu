@@ -491,9 +491,22 @@ pages_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
         }
 #pragma unroll
         for (int g = 0; g < kNG; ++g) {
-          // the largest scale of the group; one that is not finite moves nothing (its products are not finite whatever the factor)
+          // the largest scale of the group; one that is not finite moves nothing (its products are not finite whatever the factor), and hides none of the lane's others
           uint32_t s = largest[g] & 0xFFFF0000u;
-          s = __reduce_max_sync(0xffffffffu, s < 0x7F800000u ? s : 0u);
+          if (s >= 0x7F800000u) {
+            s = 0u;
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+              uint32_t vm[2][kNG];
+              value_meta(m, vm);
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                const uint32_t one = vm[i][g] & 0xFFFF0000u;
+                s = max(s, one < 0x7F800000u ? one : 0u);
+              }
+            }
+          }
+          s = __reduce_max_sync(0xffffffffu, s);
           if (s > w.limit[g]) {
             const int e = min(max(kScaleTo + 127 - (int)(s >> 23), -122), 126);
             const float down = pow2i(e), f = down / w.factor[g];

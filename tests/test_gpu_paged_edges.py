@@ -78,6 +78,34 @@ def test_queries_near_the_end_of_the_range(binding, size, n, which):
         P.check(out, q, k, v, 32, SCALE, lens, [n, n], rounded)
 
 
+@pytest.mark.parametrize("Hq", [2, 8])
+@pytest.mark.parametrize("room", [0, 1 << 10])
+@pytest.mark.parametrize("G", [32, 64, 128])
+@pytest.mark.parametrize("bad", ["inf", "-inf", "nan"])
+def test_an_infinity_beside_a_large_value(binding, Hq, room, G, bad):
+    """The newest value is not finite; the rows that do not see it keep their results, though the same lane of the kernel has a value far larger than the others'."""
+    lens, n = [9, 41], 2
+    q, k, v = P.draw(2, Hq, 1, 41, 23)
+    q = q[:, :, :n].contiguous()
+    group = slice(40 // G * G, 40 // G * G + G)
+    for b, t in enumerate(lens):
+        v[b, :, t - 9] = (v[b, :, t - 9].float() * 2.0 ** 14).to(torch.bfloat16)
+        v[b, :, t - 1, group if bad == "nan" else 40] = float(bad)
+    cache, table = held(binding, Hq, 1, k, v, lens, G=G)
+    out = cache.attention(0, q.cuda(), wide(table, 32, room).cuda(), ints(lens), SCALE).cpu()
+    assert cache.status() == 0 and torch.isfinite(out[:, :, 0]).all()
+    assert not torch.isfinite(out[:, :, 1, group]).any()
+    # (the reference's quantizer has no groups of NaNs: the newest value as zeros, compared in the other channels and rows)
+    clean = v.clone()
+    for b, t in enumerate(lens):
+        clean[b, :, t - 1, group] = 0.0
+    rest = [c for c in range(128) if not group.start <= c < group.stop]
+    for b, t in enumerate(lens):
+        ref, tol = P.reference(q[b], k[b, 0, :t], clean[b, 0, :t], G, SCALE, [t - 1, t])
+        err = (out[b].double() - ref).abs() / (tol + 2.0 ** -24 * ref.abs() + 1e-37)
+        assert err[:, 0].max() <= 1.0 and (not rest or err[:, 1, rest].max() <= 1.0)
+
+
 @pytest.mark.parametrize("Hq,Hkv,n,lens,polls", [(7, 1, 60, [700, 300], 100), (28, 4, 300, [5000, 900, 301], 300), (8, 1, 1000, [40000], 1000)])
 def test_time_outs_of_many_rows(binding, Hq, Hkv, n, lens, polls):
     """Copies that never arrive in every thread block of the kernel for many rows: the call ends, the status says so, and the next call is as usual."""
