@@ -650,9 +650,9 @@ class PagedCache:
             who = self._who = _owner(self.handle, self.mem, self.cfg)
         return who
 
-    def _rotated(self, q, counts, positions):
-        """Room for rotated queries; zeros where rows may be left alone."""
-        return (torch.empty if counts is None and positions is None else torch.zeros)(q.shape, dtype=torch.bfloat16, device=self.mem.device)
+    def _rotated(self, q):
+        """Room for rotated queries: zeros, as rows may be left alone (behind a count, beyond the tables, without a place)."""
+        return torch.zeros(q.shape, dtype=torch.bfloat16, device=self.mem.device)
 
     def _output(self, name, q, counts, dtype):
         if dtype not in _OUT_TYPES:
@@ -674,9 +674,10 @@ class PagedCache:
     def append(self, layer, k, v, pages, lens, counts=None, q=None, cos=None, sin=None, positions=None, interleaved=False, q_out=None):
         """Stores k, v [B,Hkv,n,128] (bf16, any strides with a contiguous last dimension: views of a fused projection's output too) behind the lens[b] tokens
         that each sequence has; `lens` is not changed.  With cos, sin (tables of rope_tables) keys and q [B,Hq,n,128] turn on the way, by `positions` int32 [B,n] or
-        by their places in their sequences.  Returns q rotated and head-major (`q_out`, which may be q itself where it is head-major; None without q)."""
+        by their places in their sequences.  Returns q rotated and head-major (`q_out`, which may be q itself where it is head-major; None without q), zeros in the rows
+        that are left alone when it is allocated here."""
         if q_out is None and q is not None:
-            q_out = self._rotated(q, counts, positions)
+            q_out = self._rotated(q)
         with _device_of(self.mem.device):
             code = (_native or _calls()).paged_append(self._on(), layer, k, v, q, pages, lens, counts, cos, sin, positions, interleaved, q_out)
         if code:
@@ -684,10 +685,11 @@ class PagedCache:
         return q_out
 
     def read(self, layer, pages, lens, n_tokens, counts=None, out=None):
-        """The values that tokens lens[b] .. lens[b] + n_tokens - 1 (counts[b]) of every sequence are held as: (k, v) bf16 [B,Hkv,n_tokens,128]."""
+        """The values that tokens lens[b] .. lens[b] + n_tokens - 1 (counts[b]) of every sequence are held as: (k, v) bf16 [B,Hkv,n_tokens,128]
+        (`out`: two such tensors; allocated when absent, zeros in the rows that are left alone)."""
         if out is None:
             shape = (pages.shape[0], self.cfg.n_kv_heads, max(n_tokens, 0), 128)
-            out = tuple((torch.empty if counts is None else torch.zeros)(shape, dtype=torch.bfloat16, device=self.mem.device) for _ in range(2))
+            out = tuple(torch.zeros(shape, dtype=torch.bfloat16, device=self.mem.device) for _ in range(2))
         k, v = out
         with _device_of(self.mem.device):
             code = (_native or _calls()).paged_read(self._on(), layer, pages, lens, n_tokens, counts, k, v)
@@ -715,7 +717,7 @@ class PagedCache:
         if q is None:
             raise ValueError("step: queries are needed")
         if q_out is None:
-            q_out = self._rotated(q, counts, positions)
+            q_out = self._rotated(q)
         if out is None:
             out = self._output("step", q, counts, dtype)
         if workspace is None:

@@ -106,6 +106,33 @@ def test_an_infinity_beside_a_large_value(binding, Hq, room, G, bad):
         assert err[:, 0].max() <= 1.0 and (not rest or err[:, 1, rest].max() <= 1.0)
 
 
+@pytest.mark.parametrize("why", ["tables", "page", "length"])
+def test_rows_that_are_left_out_are_zeros(binding, why):
+    """Outputs that a call allocates hold zeros where it writes nothing: tokens beyond the tables, on pages that are none, behind the page table."""
+    Hq, Hkv, n, page = 4, 2, 6, 16
+    q, k, v = (x.cuda() for x in P.draw(2, Hq, Hkv, n, 37))
+    table, n_pages = P.pages_for([32, 32], page, 2)
+    cache = binding.PagedCache(binding.make_paged_config(1, Hq, Hkv, n_pages, page_tokens=page))
+    cache.mem[256:] = 0
+    cos, sin = (x[:20 if why == "tables" else 40].contiguous() for x in binding.rope_tables(40))
+    pages, lens = table.cuda(), ints([12, 18 if why != "length" else 30])
+    if why == "page":
+        pages[1, 1] = -3
+    left = {"tables": [2, 3, 4, 5], "page": list(range(6)), "length": [2, 3, 4, 5]}[why]       # of sequence 1
+    stale = [torch.full((2, h, n, 128), float("nan"), dtype=torch.bfloat16, device="cuda") for h in (Hq, Hkv, Hkv)]
+    del stale                                                                    # what the next allocations of these sizes find
+    turned = cache.append(0, k, v, pages, lens, q=q, cos=cos, sin=sin)
+    assert (turned[1, :, left] == 0).all() and torch.isfinite(turned).all() and (turned[0] != 0).any()
+    stale = [torch.full((2, h, n, 128), float("nan"), dtype=torch.bfloat16, device="cuda") for h in (Hq, Hkv, Hkv)]
+    del stale
+    for out in cache.read(0, pages, lens, n):
+        assert (out[1, :, left] == 0).all() and torch.isfinite(out).all() and (out[0] != 0).any()
+    stale = [torch.full((2, h, n, 128), float("nan"), dtype=torch.bfloat16, device="cuda") for h in (Hq, Hkv, Hkv)]
+    del stale
+    assert torch.isfinite(cache.step(0, k, v, q, pages, lens, SCALE, cos=cos, sin=sin)).all()
+    assert cache.status() != 0
+
+
 @pytest.mark.parametrize("Hq,Hkv,n,lens,polls", [(7, 1, 60, [700, 300], 100), (28, 4, 300, [5000, 900, 301], 300), (8, 1, 1000, [40000], 1000)])
 def test_time_outs_of_many_rows(binding, Hq, Hkv, n, lens, polls):
     """Copies that never arrive in every thread block of the kernel for many rows: the call ends, the status says so, and the next call is as usual."""
