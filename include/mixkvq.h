@@ -379,7 +379,8 @@ typedef struct mixkvq_paged_sequences {
 #define MIXKVQ_PAGED_MAX_BATCH 4096
 
 int mixkvq_paged_bytes(const mixkvq_paged_config* cfg, size_t* pool_bytes);
-/* Workspace of an attention call of this batch, number of tokens and columns of the page table.  Contents are scratch and need not be anything; two calls that may overlap on the GPU
+/* Workspace of an attention call of this batch, number of tokens and columns of the page table, and of every call of a smaller batch, number and table: it never falls as they
+ * grow, so that one workspace serves all calls up to the largest.  Contents are scratch and need not be anything; two calls that may overlap on the GPU
  * need one each, two captured graphs too unless they never run at the same time. */
 size_t mixkvq_paged_workspace_bytes(const mixkvq_paged_config* cfg, int batch, int n_tokens, int max_pages);
 /* The handle over caller-owned memory (256-byte aligned); the pages are left as they are, the status word is cleared on `stream`. */

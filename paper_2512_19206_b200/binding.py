@@ -729,7 +729,8 @@ class PagedCache:
         return out
 
     def workspace_bytes(self, batch, n_tokens, max_pages):
-        """Bytes of the workspace of an attention or step of `batch` sequences, n_tokens each at most, with a page table of max_pages columns."""
+        """Bytes of the workspace of an attention or step of `batch` sequences, n_tokens each at most, with a page table of max_pages columns,
+        and of all smaller ones."""
         return int(lib().mixkvq_paged_workspace_bytes(C.byref(self.cfg), int(batch), int(n_tokens), int(max_pages)))
 
     def status(self) -> int:

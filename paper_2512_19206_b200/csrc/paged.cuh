@@ -121,9 +121,12 @@ struct RopeTables {
 cudaError_t launch_paged_append(const PagedAppend& a, int n_sms, cudaStream_t stream);
 cudaError_t launch_paged_read(const PagedRead& a, int n_sms, cudaStream_t stream);
 cudaError_t launch_paged_attention(const PagedAttention& a, int n_sms, cudaStream_t stream, int* launches, int* form);      // form: MIXKVQ_PAGED_*
+// capacity: tokens that the pages of a sequence hold at most.  _need: what a launch of these sizes uses; _bytes: that or more, never less for a larger batch, n or capacity
+size_t paged_workspace_need(int Hkv, int g, int batch, int n, long long capacity);
 size_t paged_workspace_bytes(int Hkv, int g, int batch, int n, long long capacity);
-// many query rows (tcgen05); capacity: tokens that the pages of a sequence hold at most
-bool paged_chunk_fits(long long capacity);
+// many query rows (tcgen05)
+long long paged_chunk_capacity();                // the largest that it takes
+size_t paged_chunk_workspace_need(int Hkv, int batch, long long capacity);
 size_t paged_chunk_workspace_bytes(int Hkv, int batch, long long capacity);
 cudaError_t paged_chunk_setup();
 cudaError_t launch_paged_chunk(const PagedAttention& a, int n_sms, cudaStream_t stream, int* launches);

@@ -116,7 +116,7 @@ int plan_attention(const mixkvq_paged* h, int layer, const mixkvq_paged_sequence
     return MIXKVQ_E_INVALID_ARG;
   if (!aligned16(q_dev) || !aligned16(out_dev) || !aligned16(workspace_dev)) return MIXKVQ_E_ALIGNMENT;
   if ((long long)s->batch * s->n_tokens * h->cfg.n_q_heads > 0x7FFFFFFFll || (long long)s->n_tokens * h->g >= 1 << 28) return MIXKVQ_E_UNSUPPORTED;      // (thread blocks of a grid)
-  const size_t need = paged_workspace_bytes(h->cfg.n_kv_heads, h->g, s->batch, s->n_tokens, (long long)s->max_pages * h->cfg.page_tokens);
+  const size_t need = paged_workspace_need(h->cfg.n_kv_heads, h->g, s->batch, s->n_tokens, (long long)s->max_pages * h->cfg.page_tokens);
   if (workspace_bytes < need) return MIXKVQ_E_BUFFER_TOO_SMALL;
   const size_t rows = (size_t)s->batch * h->cfg.n_q_heads * s->n_tokens * kD;
   Ranges& r = *ranges;

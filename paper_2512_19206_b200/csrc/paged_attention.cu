@@ -797,12 +797,17 @@ size_t smem_bytes(int G, int tiles, int B, bool direct) {
 
 // Whether a call goes to the kernel that unpacks the pages once for all query rows.
 static bool unpacks(int Hkv, int g, int batch, int n, long long capacity) {
-  return (double)g * n > kUnpackRows + kUnpackWork / ((double)batch * Hkv * capacity) && paged_chunk_fits(capacity);
+  return (double)g * n > kUnpackRows + kUnpackWork / ((double)batch * Hkv * capacity) && capacity <= paged_chunk_capacity();
 }
 
+static size_t pieces_bytes(int g, int n) { return (size_t)2 * kMostBlocks * 8 * tiles_of(g, n) * kPartFloats * 4 + kMostBlocks * sizeof(Broken); }
+size_t paged_workspace_need(int Hkv, int g, int batch, int n, long long capacity) {
+  return unpacks(Hkv, g, batch, n, capacity) ? paged_chunk_workspace_need(Hkv, batch, capacity) : pieces_bytes(g, n);
+}
+// (a capacity beyond what is unpacked counts as the largest that is: a narrower page table may need that)
 size_t paged_workspace_bytes(int Hkv, int g, int batch, int n, long long capacity) {
-  if (unpacks(Hkv, g, batch, n, capacity)) return paged_chunk_workspace_bytes(Hkv, batch, capacity);
-  return (size_t)2 * kMostBlocks * 8 * tiles_of(g, n) * kPartFloats * 4 + kMostBlocks * sizeof(Broken);
+  const long long most = std::min(capacity, paged_chunk_capacity());
+  return unpacks(Hkv, g, batch, n, most) ? std::max(paged_chunk_workspace_bytes(Hkv, batch, most), pieces_bytes(g, n)) : pieces_bytes(g, n);
 }
 
 cudaError_t paged_attention_setup() {

@@ -800,14 +800,21 @@ size_t rounded(size_t x) { return (x + 255) / 256 * 256; }
 
 }  // namespace
 
-bool paged_chunk_fits(long long capacity) { return (capacity + kTile - 1) / kTile * 2 * kTileBytes <= (long long)kImageBytes; }
+long long paged_chunk_capacity() { return (long long)(kImageBytes / (2 * (size_t)kTileBytes)) * kTile; }
 
-size_t paged_chunk_workspace_bytes(int Hkv, int batch, long long capacity) {
+static size_t bytes_of(size_t images) {
+  return images * 2 * kTileBytes + rounded(images * sizeof(TileHead)) + rounded((size_t)2 * kMostBlocks * kRows * kPartFloats * 4) + rounded(kMostBlocks * sizeof(Broken)) + 256;
+}
+size_t paged_chunk_workspace_need(int Hkv, int batch, long long capacity) {
   const long long tiles = (capacity + kTile - 1) / kTile;
   int nb, nh;
   pass_of(batch, Hkv, tiles, &nb, &nh);
-  const size_t images = (size_t)nb * nh * tiles;
-  return images * 2 * kTileBytes + rounded(images * sizeof(TileHead)) + rounded((size_t)2 * kMostBlocks * kRows * kPartFloats * 4) + rounded(kMostBlocks * sizeof(Broken)) + 256;
+  return bytes_of((size_t)nb * nh * tiles);
+}
+// No less than what any smaller batch or capacity needs: a pass holds whole streams, so that what it needs falls where one fewer fits.
+size_t paged_chunk_workspace_bytes(int Hkv, int batch, long long capacity) {
+  const long long tiles = (capacity + kTile - 1) / kTile;
+  return bytes_of((size_t)std::min((long long)batch * Hkv * tiles, (long long)(kImageBytes / (2 * (size_t)kTileBytes))));
 }
 
 cudaError_t paged_chunk_setup() { return cudaFuncSetAttribute(attend_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem + 8 * (MIXKVQ_PAGED_MAX_BATCH + 1)); }

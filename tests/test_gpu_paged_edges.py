@@ -169,3 +169,20 @@ def test_calls_whose_copies_never_arrive_are_zeros(binding, n, lens, room, dtype
     cache.clear_status()
     cache.attention(0, q, pages, ints(lens), SCALE, out=out, workspace=space)
     assert cache.status() == 0 and (out.flatten(0, 2).float().abs().amax(1) > 0).all()
+
+
+def test_one_workspace_for_all_smaller_calls(binding):
+    """A workspace of the widest table and the most tokens serves every narrower and shorter call, whatever pass such a call makes."""
+    Hq, Hkv, page, lens = 64, 8, 256, [400, 90]
+    q, k, v = P.draw(2, Hq, Hkv, 400, 87)
+    cache, table = held(binding, Hq, Hkv, k, v, lens, page=page)
+    widths = [2, 64, 511, 512, 513, 1025, 2048, 4097]
+    space = torch.empty(cache.workspace_bytes(2, 90, widths[-1]), dtype=torch.uint8, device="cuda")
+    for n in (1, 30, 90):
+        x = q[:, :, :n].contiguous().cuda()
+        for width in widths:
+            pages = wide(table, 1, width).cuda()
+            assert torch.equal(cache.attention(0, x, pages, ints(lens), SCALE, workspace=space), cache.attention(0, x, pages, ints(lens), SCALE))
+    assert cache.last_attention() != UNPACKED and cache.status() == 0        # (the widest table holds more than is unpacked)
+    cache.attention(0, x, wide(table, 1, 513).cuda(), ints(lens), SCALE, workspace=space)
+    assert cache.last_attention() == UNPACKED
