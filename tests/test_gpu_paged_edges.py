@@ -106,6 +106,35 @@ def test_an_infinity_beside_a_large_value(binding, Hq, room, G, bad):
         assert err[:, 0].max() <= 1.0 and (not rest or err[:, 1, rest].max() <= 1.0)
 
 
+def test_keys_alone_and_positions_of_their_own(binding):
+    """An append without queries stores what one with them does; a token with a negative position leaves its slot as it was."""
+    Hkv, n, page = 2, 8, 32
+    _, k, v = P.draw(2, 4, Hkv, n, 5)
+    ang = np.arange(50, dtype=np.float64)[:, None] * 1e4 ** (-np.arange(32, dtype=np.float64) / 32)[None]
+    cos, sin = np.cos(ang).astype(np.float32), np.sin(ang).astype(np.float32)
+    table, n_pages = P.pages_for([20, 20], page, 1)
+    cache = binding.PagedCache(binding.make_paged_config(1, 4, Hkv, n_pages, page_tokens=page))
+    cache.mem[256:] = 0x5A
+    pos = torch.randint(0, 50, (2, n), dtype=torch.int32, generator=torch.Generator().manual_seed(0))
+    pos[0, 3], pos[1, 5] = -1, 49
+    want = cache.mem.cpu().numpy().copy()
+    lens = [4, 9]
+    assert cache.append(0, k.cuda(), v.cuda(), table.cuda(), ints(lens), cos=torch.from_numpy(cos).cuda(), sin=torch.from_numpy(sin).cuda(), positions=pos.cuda()) is None
+    assert cache.status() == 0
+    kr = P.rotate(k, cos, sin, pos.clamp(min=0).numpy())
+    for b in range(2):
+        for i in range(n):
+            if pos[b, i] < 0:
+                continue
+            t = lens[b] + i
+            for h in range(Hkv):
+                kb, km = P.token_bytes(kr[b, h, i], 32, False, t % 16)
+                vb, vm = P.token_bytes(v[b, h, i], 32, True, t % 16)
+                for at, data in zip(P.place(cache.cfg, 0, int(table[b, t // page]), h, t % page), (kb, vb, km, vm)):
+                    want[at:at + len(data)] = np.frombuffer(data, np.uint8)
+    assert np.array_equal(cache.mem.cpu().numpy()[256:], want[256:])
+
+
 @pytest.mark.parametrize("why", ["tables", "page", "length"])
 def test_rows_that_are_left_out_are_zeros(binding, why):
     """Outputs that a call allocates hold zeros where it writes nothing: tokens beyond the tables, on pages that are none, behind the page table."""
