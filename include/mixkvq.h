@@ -392,6 +392,8 @@ int mixkvq_paged_destroy(mixkvq_paged* cache);
  *   rotation: NULL (keys are stored as they are), or keys and queries turn on the way; its positions_dev may be NULL: a token turns by its place in
  *   its sequence.  A token with a negative position is none: its slot stays as it was (and a step reckons with lens + counts all the same).
  *   q_dev, q_out_dev: both NULL, or the queries and where they go, rotated, head-major; q_out_dev may be q_dev itself where that is head-major.
+ * A NaN is held as the least value of its group, whose other channels are as they are without it (no quantizer of this library has a code for one); a group of nothing else
+ * reads back as NaN, and one with an infinity is finite in no channel.
  * Rows of q_out_dev behind a sequence's count are left as they are.  Two tokens of a call in the same slot (a page used twice) leave
  * a mix of both. */
 int mixkvq_paged_append(mixkvq_paged* cache, int layer, const mixkvq_paged_sequences* seqs, const void* k_dev, const void* v_dev, const void* q_dev,

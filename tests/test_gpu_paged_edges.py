@@ -106,6 +106,35 @@ def test_an_infinity_beside_a_large_value(binding, Hq, room, G, bad):
         assert err[:, 0].max() <= 1.0 and (not rest or err[:, 1, rest].max() <= 1.0)
 
 
+def test_nans_that_are_appended(binding):
+    """A NaN is held as the least value of its group, whose other channels are as without it; a group of NaNs alone is NaN, one with an infinity finite nowhere."""
+    G = 32
+    _, k, v = P.draw(1, 2, 2, 20, 29)
+    bad = {}
+    for name, x in (("k", k), ("v", v)):
+        y = x.clone()
+        y[0, 0, 3, 5] = y[0, 1, 19, 64] = y[0, 1, 19, 95] = float("nan")
+        y[0, 0, 7, 96:] = float("nan")
+        y[0, 1, 8, 33], y[0, 1, 9, 34] = float("inf"), float("-inf")
+        y[0, 0, 11, :32] = 2.5
+        y[0, 0, 11, 9] = float("nan")
+        bad[name] = y
+    cache, table = held(binding, 2, 2, bad["k"], bad["v"], [20])
+    got = cache.read(0, table.cuda(), ints([0]), 20)
+    assert cache.status() == 0
+    for y, out in zip(bad.values(), got):
+        rows = P.f32(y).reshape(1, 2, 20, 4, G)
+        least = np.nanmin(np.where(np.isnan(rows).all(-1, keepdims=True), 0.0, rows), -1, keepdims=True)
+        filled = torch.from_numpy(np.where(np.isnan(rows), least, rows).reshape(1, 2, 20, 128)).to(torch.bfloat16)
+        finite = torch.isfinite(filled).view(1, 2, 20, 4, G).all(-1, keepdim=True).expand(1, 2, 20, 4, G).reshape(1, 2, 20, 128).clone()
+        finite[0, 0, 7, 96:] = False
+        calm = torch.where(finite, filled, torch.zeros_like(filled))
+        ref = torch.from_numpy(P.values(*P.quantized(calm, G)).astype(np.float32)).to(torch.bfloat16)
+        out = out.cpu()
+        assert torch.equal(torch.isfinite(out), finite)
+        assert torch.equal(out[finite], ref[finite])
+
+
 def test_keys_alone_and_positions_of_their_own(binding):
     """An append without queries stores what one with them does; a token with a negative position leaves its slot as it was."""
     Hkv, n, page = 2, 8, 32
