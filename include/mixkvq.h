@@ -347,10 +347,11 @@ typedef struct mixkvq_rope_scaling {
 } mixkvq_rope_scaling;
 int mixkvq_rope_tables(const mixkvq_rope_scaling* scaling, int64_t start, int n_positions, float* cos_dev, float* sin_dev, void* stream);
 
-/* ---- A cache held in 4 bits, in pages (no counterpart in the paper but its uniform 4-bit baseline): for servers that give sequences memory page by page, share
+/* ---- A cache held in 4 bits, in pages (no counterpart in the paper): for servers that give sequences memory page by page, share
  * pages between them and capture their steps into graphs.  Keys and values are both quantized token by token when they come (Eq. 2 with 16 levels,
  * groups of G channels of one token, scale and zero-point bf16 as everywhere: reading of the stored scale included), so there is no window, no flush and no
- * state but the pages.  Which pages belong to a sequence and how many tokens it has is the caller's, in DEVICE memory: nothing about a call but its shape is
+ * state but the pages.  (The paper quantizes keys per channel, as do the methods it compares with: an outlier channel then costs the others nothing.  Here it widens the
+ * step of its group of G channels.)  Which pages belong to a sequence and how many tokens it has is the caller's, in DEVICE memory: nothing about a call but its shape is
  * known to the host.
  *
  * Pool: `n_layers` times `n_pages` pages of page_tokens tokens of all KV heads, behind a header of 256 bytes with the status word; page p of a layer is one contiguous piece
@@ -405,8 +406,10 @@ int mixkvq_paged_read(mixkvq_paged* cache, int layer, const mixkvq_paged_sequenc
  *   q_dev [B, Hq, n, 128] bf16 (rotated), out_dev [B, Hq, n, 128] of out_type (MIXKVQ_OUT_*), rounded once.
  * A row that sees no token is zeros; rows behind a sequence's count are left as they are.  Nothing is read of tokens that no row sees: freed pages and the rest of a last
  * page may hold anything.  softmax_scale > 0 and finite.
- * Logits and sums are fp32; weights are fp16 numbers (2^-11), and calls that unpack the pages (MIXKVQ_PAGED_UNPACKED) round keys and values to fp16 once more.  Inputs of any
- * magnitude are scaled by powers of two on the way.  What is not finite in the pages or a query reaches the rows that see it only. */
+ * Logits and sums are fp32; weights are fp16 numbers (2^-11), and calls that unpack the pages (MIXKVQ_PAGED_UNPACKED) round keys and values to fp16 once more.  Which calls do follows
+ * from batch, heads, n_tokens and max_pages, not from the lengths (mixkvq_paged_last_attention).  Queries, keys and values are scaled by powers of two on the way, so that those
+ * bits are kept at any magnitude, within two limits: what a token adds is held no finer than 2^-28 of the row's largest weight times the largest value of the sequence and KV head,
+ * and values below 2^-110 lose bits.  What is not finite in the pages or a query reaches the rows that see it only. */
 int mixkvq_paged_attention(mixkvq_paged* cache, int layer, const mixkvq_paged_sequences* seqs, const void* q_dev, void* out_dev, int out_type, float softmax_scale,
                            void* workspace_dev, size_t workspace_bytes, void* stream);
 /* mixkvq_paged_append, then mixkvq_paged_attention of the tokens appended: a decode step, or a chunk of a prompt.  lens: tokens before the call.

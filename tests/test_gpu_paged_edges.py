@@ -244,3 +244,26 @@ def test_one_workspace_for_all_smaller_calls(binding):
     assert cache.last_attention() != UNPACKED and cache.status() == 0        # (the widest table holds more than is unpacked)
     cache.attention(0, x, wide(table, 1, 513).cuda(), ints(lens), SCALE, workspace=space)
     assert cache.last_attention() == UNPACKED
+
+
+@pytest.mark.parametrize("n", [1, 4, 40])
+@pytest.mark.parametrize("room", [0, 1 << 16])
+@pytest.mark.parametrize("power", [8, 12])
+def test_large_values_of_no_weight(binding, n, room, power):
+    """The first tokens' values are 2^power times the others' and have next to no weight.  What a token adds is held to 2^-28 of the largest weight times the largest value
+    at worst, which for T tokens is T 2^-28 max |v| of the output, beside what the roundings of the others allow."""
+    T, heavy = 300, 128
+    q, k, v = P.draw(1, 7, 1, T, 91)
+    q = q[:, :, :n].contiguous()
+    q[..., 0], k[..., 0] = 8.0, 0.0
+    k[:, :, :heavy, 0] = -100.0                                       # logits 70 below the others'
+    v[:, :, :heavy] = (v[:, :, :heavy].float() * 2.0 ** power).to(torch.bfloat16)
+    cache, table = held(binding, 7, 1, k, v, [T])
+    out = cache.attention(0, q.cuda(), wide(table, 32, room).cuda(), ints([T]), SCALE)
+    rounded = cache.last_attention() == UNPACKED
+    assert cache.status() == 0 and rounded == (room > 0 and n == 40)
+    ref, _ = P.reference(q[0], k[0, 0], v[0, 0], 32, SCALE, [T - n + i + 1 for i in range(n)], rounded)
+    _, tol = P.reference(q[0], k[0, 0, heavy:], v[0, 0, heavy:], 32, SCALE, [T - heavy - n + i + 1 for i in range(n)], rounded)
+    most = float(v.double().abs().max())
+    assert ((out[0].double().cpu() - ref).abs() <= tol + T * 2.0 ** -28 * most + 2.0 ** -24 * ref.abs()).all()
+    assert (out[0].abs().amax(-1) > 0.01).all()
