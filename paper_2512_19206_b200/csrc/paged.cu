@@ -2,7 +2,7 @@
 //
 // append_kernel: new tokens' keys and queries turn by their positions (rotary positions of part of the head, either pairing), keys and values are quantized
 // (Eq. 2 with 16 levels, a group of G channels of one token) and go to the page and slot of the token.  Memory-bound by its bytes, by instruction issue in its first form
-// (16384 prompt tokens of 8 KV heads and 32 query heads, 356 MB: 176 us; now 74, 0.74 of the rate of a copy, with half of the issue slots taken).  Thread blocks for keys and values: sixteen lanes have a row, a lane 8 channels, so that a lane's eight
+// (16384 prompt tokens of 8 KV heads and 32 query heads, 356 MB: 176 us; now 74, 0.74 of the rate of a copy: half of the issue slots and half of the DRAM throughput, as the warps wait for their rows first).  Thread blocks for keys and values: sixteen lanes have a row, a lane 8 channels, so that a lane's eight
 // codes are one word and the extrema of a group two to four exchanges; thread blocks for queries: eight lanes have a row (turn_pair).  A thread has one token and goes
 // through a range of heads.
 #include <algorithm>

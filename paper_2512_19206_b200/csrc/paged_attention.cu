@@ -5,15 +5,15 @@
 // are scaled behind it in fp32.  A value is s_g c + z_g with a scale per token, so the weight p s_g of (token, group) is the other operand of the second product, in fp16,
 // and sum p z_g is added up in fp32.  One pass over the tokens with a running reference of the logits.
 //
-// Operands stay inside fp16's range whatever the inputs' magnitudes: a query row is scaled by a power of two (exactly) to a largest entry of 2^14 to 2^15, and p s_g by a power of
+// Operands stay inside fp16's range whatever the inputs' magnitudes (a value far smaller than the largest of its group so far keeps fewer bits): a query row is scaled by a power of two (exactly) to a largest entry of 2^14 to 2^15, and p s_g by a power of
 // two per group, lowered as larger scales come.  References are raised, and sums rescaled, only when a logit comes 8 (in powers of two) above the largest so far.
 //
 // Split: work is units of 32 tokens of one (sequence, KV head, block of query rows), all of them in one line, cut evenly over the thread blocks on the device (the
 // lengths are known there alone).  A thread block goes through the pieces of streams in its range, its warps through the units of a piece, each with a ring of
 // bulk copies of its own, so that no warp waits for another before the end of a piece.  A piece that is no whole stream leaves sums, which merge_kernel joins.
 //
-// What bounds it: instruction issue and its latencies, not the bytes.  7b shape, 8 x 32768 tokens, one new each (168 MB, G = 32): 46 us, 0.56 of the rate of a copy; 358 warp
-// instructions per 16 tokens, 54 % of the issue slots with three warps per scheduler; about 10 us are the beginning (lengths, page, first copies, one behind the other) and the end with the
+// What bounds it: each warp's chain of instructions with three warps per scheduler to cover it, not the bytes.  7b shape, 8 x 32768 tokens, one new each (168 MB, G = 32): 46 us, 0.56 of
+// the rate of a copy; 360 warp instructions per 16 tokens, 54 % of the issue slots; thread blocks that share an SM end unevenly (27 to 35 us); about 10 us are the beginning (lengths, page, first copies, one behind the other) and the end with the
 // merge.  Measured against it: four warps per scheduler (128 registers) 48.8 us; 16 query rows' operands in shared memory (drafts) 58.4 against 58.1.
 // Rows in blocks of 16 cost 1.44 times blocks of 8, so that 9 to 72 rows are taken in several passes over the pages, which the L2 cache holds.
 #include <algorithm>
@@ -771,7 +771,8 @@ merge_kernel(const __grid_constant__ PagedAttention a, const __grid_constant__ P
 // 1 x 1000 10.1 / 8.6, 64 x 1000 20.0 / 23.2 (and the longest sequence decides).
 constexpr int kDirectTokens = 512;
 // Query rows of a KV head above which unpacking the pages pays: kUnpackRows, and more where there is little to unpack (kUnpackWork / tokens of all KV heads), as its three
-// launches take longer than two.  By what the pages could hold, the lengths being unknown here.  7b shape, us with the pages as they are / unpacked: 8 x 32768 tokens 63 rows 214 / 248,
+// launches take longer than two.  By what the pages could hold, the lengths being unknown here (and by the largest count): measured with page tables as wide as the sequences are long,
+// so under a much wider one short sequences are unpacked from fewer rows on than pays.  7b shape, us with the pages as they are / unpacked: 8 x 32768 tokens 63 rows 214 / 248,
 // 98 rows 355 / 250; 8 x 8192 63 rows 69 / 84, 98 rows 107 / 85; 1 x 32768 98 rows 59 / 61, 126 rows 65 / 61; 1 x 8192 189 rows 35 / 45, 448 rows 62 / 49; 8 x 1024 63 rows 25 / 29,
 // 252 rows 58 / 42; 1 x 1024 448 rows 23 / 34, 896 rows 34 / 36.
 constexpr int kUnpackRows = 72;

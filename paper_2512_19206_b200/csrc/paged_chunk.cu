@@ -2,8 +2,8 @@
 //
 // The codes of a token are used by thousands of query rows, so they are unpacked once: unpack_kernel writes tiles of 128 tokens of a KV head as fp16 images in the tensor
 // core's shared-memory layout, so that a tile arrives as one 32 KB bulk copy.  c s + z is rounded to fp16 once (2^-11 of itself); every tile is scaled by a power of two of
-// its own to a largest element of 2^14 to 2^15, and every query row likewise, so that operands of any magnitude stay inside fp16's range.  The scales of a key tile and a query
-// row go into the factor of the logits, that of a value tile into the sum of the products.
+// its own to a largest element of 2^14 to 2^15, and every query row likewise, so that operands of any magnitude stay inside fp16's range (a value tile's power is 2^96 at most: values
+// below 2^-110 lose bits).  The scales of a key tile and a query row go into the factor of the logits, that of a value tile into the sum of the products.
 //
 // attend_kernel: one thread block per SM of 384 threads:
 //   warps 0-3, 4-7   two softmax groups of 128 query rows (thread = row = lane of tensor memory); a row is head x % g of token x / g;
@@ -18,7 +18,7 @@
 // thread blocks, on the device.  A thread block that has a part of an item leaves sums, which join_kernel puts together.
 //
 // What bounds it: a group's chain of product, softmax, product and the hand-overs between them, about 4000 cycles for a key tile of both groups whose products take 2048 of the tensor core.
-// 2048 tokens over 32768 more, 7b shape (9.9e11 operations): 1040 us, 954 TFLOP/s, with the images and the join; tensor pipe 47 %, exponentials 47 % of their unit, 1000 W when calls
+// 2048 tokens over 32768 more, 7b shape (9.9e11 operations): 1055 us, 940 TFLOP/s, with the images and the join; tensor pipe 46 %, exponentials 46 % of their unit, 1000 W when calls
 // follow each other.  The exponentials are not it: with half of them left out the kernel takes as long.  Measured against it: sums of every tile added up in registers, which left
 // none for the row of S (read twice), 1078; weights from the reference before the tile 1242; steps of 64 keys with two S under way 1267.
 #include <algorithm>
